@@ -399,6 +399,132 @@ int soma_debug_body_probe(uint64_t seed, uint64_t step, int expert, int pert, so
                           int probe_kind, int64_t p0, int64_t count, int8_t* z_out,
                           void* stream);
 
+/* ---- First-order training ----------------------------------------------
+ * The operators of a training step by gradients, which the paper runs next to
+ * the zero-order one (the BPTT controls, the decoder-path rule of the seed
+ * run, and an optimizer over real gradients).  The conventions at the top of
+ * this file hold, except that tensors of these entry points need only the
+ * alignment of their element type: each kernel takes its wide loads where
+ * the addresses and strides allow them, and gives the same results where
+ * they do not. */
+typedef enum soma_dtype {
+  SOMA_FP32 = 0,
+  SOMA_BF16 = 1,
+  SOMA_FP16 = 2
+} soma_dtype;
+
+/* AdamW (Loshchilov & Hutter, ICLR'19) over many tensors at once.
+ * For every element with gradient g = grad_scale[0] * grad:
+ *   m' = beta1 m + (1 - beta1) g;   v' = beta2 v + (1 - beta2) g^2
+ *   p' = p (1 - lr * weight_decay)
+ *        - lr / (1 - beta1^t) * m' / (sqrt(v') / sqrt(1 - beta2^t) + eps)
+ * in fp32.  With a master, p is the fp32
+ * master, which is updated, and the parameter is its rounded copy.
+ *
+ * state_bits = 32: m and v are fp32 [count].
+ * state_bits = 8: m and the root r = sqrt(v) are e4m3 bytes [count] with one
+ *   fp32 scale per 256 elements, [ceil(count / 256)]: the value is
+ *   byte * scale and scale = (largest magnitude of the 256) / 448.  A value
+ *   is rounded up or down at random, with the odds of its two neighbours'
+ *   distances: without that an average that moves by less than half a step
+ *   per update would never move.  Element j of the group of eight q of
+ *   tensor k takes 16 bits, half j % 2 of word j / 2, of the Philox4x32-10
+ *   block with key (seed halves) and counter (q, k, t, 0x80000002): a
+ *   domain disjoint from the probes' and the initialisation's.  A root above
+ *   zero is never rounded to zero.
+ * An element whose new moments would not be finite keeps its parameter and
+ * moments (up to their rounding to 8 bits), and SOMA_ERR_NONFINITE is
+ * recorded; a grad_scale that is not finite skips the whole step the same
+ * way. */
+typedef struct soma_adamw_tensor {
+  void* param;         /* [count] of param_dtype, updated */
+  const void* grad;    /* [count] of grad_dtype */
+  void* m;             /* first moment, updated */
+  void* v;             /* second moment (32 bits) or its root (8 bits), updated */
+  float* m_scale;      /* 8 bits only, else NULL */
+  float* v_scale;      /* 8 bits only, else NULL */
+  float* master;       /* fp32 [count], updated, or NULL (fp32 param: NULL) */
+  int64_t count;       /* elements, 0 .. 2^40 */
+  double weight_decay; /* lambda >= 0, decoupled */
+} soma_adamw_tensor;
+
+typedef struct soma_adamw_config {
+  double lr;    /* finite */
+  double beta1; /* in [0, 1) */
+  double beta2; /* in [0, 1) */
+  double eps;   /* > 0, finite, and not 0 in fp32 */
+  uint64_t seed; /* of the random rounding (8 bits) */
+  int32_t t;     /* 1-based update count */
+  int32_t param_dtype, grad_dtype; /* soma_dtype, the same for all tensors */
+  int32_t state_bits;              /* 32 or 8 */
+} soma_adamw_config;
+
+/* tensors: HOST array [n_tensors], read before the call returns; grad_scale:
+ * device fp32 [1], or NULL for 1.  Tensors must not overlap.  No workspace.
+ * One launch per 360 non-empty tensors. */
+int soma_adamw_step(const soma_adamw_tensor* tensors, int n_tensors, soma_adamw_config cfg,
+                    const float* grad_scale, void* stream);
+
+/* Gated linear recurrence: the cell of the LSTM expert with gates that depend
+ * on the input alone (W_hh dropped), so that the state is linear in its past
+ * and the time axis can be split (the ifo-pooling of quasi-recurrent networks,
+ * Bradbury et al., ICLR'17, with the LSTM's output).  For sequence b, step t
+ * and channel d, from the pre-activations a of the gates in the order
+ * i, f, g, o:
+ *   i, f, o = sigmoid(a_i, a_f, a_o);  g = tanh(a_g)
+ *   c_t = f c_{t-1} + i g;  h_t = o tanh(c_t)
+ * States are fp32; gates, h and their gradients are of one soma_dtype.
+ *
+ * Sequence b ends after lengths[b] steps (clamped to 0 .. steps): later steps
+ * are not read, leave the state as it is and have h = 0 and gradient 0.  A
+ * step with resets[b][t] != 0 starts a document: it takes c_{t-1} = 0.
+ * Any size may be 0.  A state that is not finite is passed on as it is. */
+typedef struct soma_scan_dims {
+  int64_t batch; /* 0 .. 2^31 - 1 */
+  int64_t steps; /* 0 .. 2^31 - 1 */
+  int64_t dim;   /* 0 .. 2^24 */
+} soma_scan_dims;
+
+/* Elements between neighbouring sequences, steps and (gate tensors) gates;
+ * channels are adjacent.  Negative strides are invalid. */
+typedef struct soma_scan_strides {
+  int64_t b, t, g;
+} soma_scan_strides;
+
+/* Floats of the checkpoints that soma_scan_forward leaves for
+ * soma_scan_backward (states at regular steps); -1 if the sizes are invalid. */
+int64_t soma_scan_checkpoint_count(soma_scan_dims d);
+
+/*   gates        [batch][steps][4][dim] by gate_strides
+ *   c0           fp32 [batch][dim] or NULL for 0
+ *   lengths      int32 [batch] or NULL;  resets: uint8 [batch][steps] or NULL
+ *   h            [batch][steps][dim] by h_strides (g unused)
+ *   c_last       fp32 [batch][dim], the state after the last step, or NULL;
+ *                may be c0
+ *   checkpoints  fp32 [soma_scan_checkpoint_count()], or NULL when no
+ *                backward call follows */
+int soma_scan_forward(const void* gates, soma_scan_strides gate_strides, int dtype,
+                      soma_scan_dims d, const float* c0, const int32_t* lengths,
+                      const uint8_t* resets, void* h, soma_scan_strides h_strides,
+                      float* c_last, float* checkpoints, void* stream);
+
+/* The gradients, from dh and dc_last (fp32, the gradient of c_last; NULL: 0):
+ *   dc_t = dh_t o (1 - tanh(c_t)^2) + f_{t+1} dc_{t+1}
+ *   d a_i = dc g i (1 - i);  d a_f = dc c_{t-1} f (1 - f);
+ *   d a_g = dc i (1 - g^2);  d a_o = dh tanh(c) o (1 - o)
+ *   dgates  as gates, by dgate_strides;  dc0: fp32 [batch][dim] or NULL
+ * gates, lengths, resets: as in the forward call that wrote checkpoints. */
+int soma_scan_backward(const void* gates, soma_scan_strides gate_strides, int dtype,
+                       soma_scan_dims d, const float* checkpoints, const int32_t* lengths,
+                       const uint8_t* resets, const void* dh, soma_scan_strides dh_strides,
+                       const float* dc_last, void* dgates, soma_scan_strides dgate_strides,
+                       float* dc0, void* stream);
+
+/* One token of each of `batch` running sequences: gates [batch][4][dim] and
+ * h [batch][dim] by their strides (t unused); c [batch][dim] is updated. */
+int soma_scan_step(const void* gates, soma_scan_strides gate_strides, int dtype, int64_t batch,
+                   int64_t dim, float* c, void* h, soma_scan_strides h_strides, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -54,6 +54,28 @@ class soma_estimate_options(ctypes.Structure):
                 ("summed_loss", ctypes.c_int32)]
 
 
+class soma_adamw_tensor(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("param", "grad", "m", "v", "m_scale", "v_scale",
+                                               "master")] + \
+               [("count", ctypes.c_int64), ("weight_decay", ctypes.c_double)]
+
+
+class soma_adamw_config(ctypes.Structure):
+    _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double),
+                ("eps", ctypes.c_double), ("seed", ctypes.c_uint64), ("t", ctypes.c_int32),
+                ("param_dtype", ctypes.c_int32), ("grad_dtype", ctypes.c_int32),
+                ("state_bits", ctypes.c_int32)]
+
+
+class soma_scan_dims(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int64) for n in ("batch", "steps", "dim")]
+
+
+class soma_scan_strides(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int64) for n in ("b", "t", "g")]
+
+
+DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 PROBE_KINDS = {"dense": 0, "sparse": 1}
 MAX_ACCUM = 64
 
@@ -145,6 +167,14 @@ def _open(path: str):
                                                ctypes.POINTER(ctypes.c_uint64), i32, vp,
                                                soma_adam_config, vp])
         _sig(L, "soma_debug_body_probe", i32, [u64, u64, i32, i32, bd, i32, i64, i64, vp, vp])
+        _sig(L, "soma_adamw_step", i32, [ctypes.POINTER(soma_adamw_tensor), i32,
+                                         soma_adamw_config, vp, vp])
+        sd, ss = soma_scan_dims, soma_scan_strides
+        _sig(L, "soma_scan_checkpoint_count", i64, [sd])
+        _sig(L, "soma_scan_forward", i32, [vp, ss, i32, sd, vp, vp, vp, vp, ss, vp, vp, vp])
+        _sig(L, "soma_scan_backward", i32, [vp, ss, i32, sd, vp, vp, vp, vp, ss, vp, vp, ss, vp,
+                                            vp])
+        _sig(L, "soma_scan_step", i32, [vp, ss, i32, i64, i64, vp, vp, ss, vp])
         _sig(L, "soma_checked_build", i32, [])
         _sig(L, "soma_debug_check_line", i32, [vp])
         _sig(L, "soma_debug_check_fail", i32, [vp])
@@ -560,3 +590,166 @@ class SomaBodies:
         body_adam_update(self.params, self.m, self.v, self.d, self.D, kind, seed, steps, coef, lr,
                          beta1, beta2, delta, weight_decay, t, stream)
         return losses, coef
+
+
+# ---------------------------------------------------------------------------
+# First-order training: the gated linear recurrence, AdamW.
+# ---------------------------------------------------------------------------
+
+def _rows(t: torch.Tensor, name: str, shape, dtype) -> tuple:
+    """(pointer, strides) of a gate or output tensor: any strides but the
+    last dimension's, which must be adjacent."""
+    if not t.is_cuda or t.dtype != dtype or tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name}: expected a CUDA {dtype} tensor of shape {tuple(shape)}, got "
+                         f"{t.dtype} {tuple(t.shape)} on {t.device}")
+    if t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError(f"{name}: the last dimension must be contiguous")
+    return ctypes.c_void_p(t.data_ptr()), t.stride()
+
+
+def _opt(t, dtype, name, numel):
+    return _dev(t, dtype, name, numel) if t is not None else None
+
+
+def _gate_dtype(gates: torch.Tensor) -> int:
+    if gates.dtype not in DTYPES:
+        raise ValueError(f"gates: unsupported dtype {gates.dtype}")
+    return DTYPES[gates.dtype]
+
+
+def scan_alloc_checkpoints(batch: int, steps: int, dim: int, device="cuda") -> torch.Tensor:
+    n = int(lib().soma_scan_checkpoint_count(soma_scan_dims(batch, steps, dim)))
+    if n < 0:
+        raise ValueError("invalid sizes for the checkpoints")
+    return torch.empty(n, dtype=torch.float32, device=device)
+
+
+def scan_forward(gates: torch.Tensor, h: torch.Tensor, c_last: torch.Tensor | None = None,
+                 c0: torch.Tensor | None = None, lengths: torch.Tensor | None = None,
+                 resets: torch.Tensor | None = None, checkpoints: torch.Tensor | None = None,
+                 stream=None):
+    """The gated linear recurrence over gates [B, T, 4, D] (pre-activations in
+    the order i, f, g, o) into h [B, T, D]; c0 and c_last fp32 [B, D], lengths
+    int32 [B], resets uint8 [B, T], checkpoints of scan_alloc_checkpoints for
+    a scan_backward call."""
+    B, T, _, D = gates.shape
+    dt, d = _gate_dtype(gates), soma_scan_dims(B, T, D)
+    gp, gs = _rows(gates, "gates", (B, T, 4, D), gates.dtype)
+    hp, hs = _rows(h, "h", (B, T, D), gates.dtype)
+    f32 = torch.float32
+    _check(lib().soma_scan_forward(
+        gp, soma_scan_strides(*gs[:3]), dt, d, _opt(c0, f32, "c0", B * D),
+        _opt(lengths, torch.int32, "lengths", B), _opt(resets, torch.uint8, "resets", B * T), hp,
+        soma_scan_strides(hs[0], hs[1], 0), _opt(c_last, f32, "c_last", B * D),
+        _opt(checkpoints, f32, "checkpoints", None if checkpoints is None else
+             lib().soma_scan_checkpoint_count(d)), _stream(stream)), "soma_scan_forward")
+
+
+def scan_backward(gates: torch.Tensor, checkpoints: torch.Tensor, dh: torch.Tensor,
+                  dgates: torch.Tensor, dc0: torch.Tensor | None = None,
+                  dc_last: torch.Tensor | None = None, lengths: torch.Tensor | None = None,
+                  resets: torch.Tensor | None = None, stream=None):
+    """Gradients of scan_forward: dgates [B, T, 4, D] and dc0 [B, D] from dh
+    [B, T, D] and dc_last [B, D], with that call's checkpoints."""
+    B, T, _, D = gates.shape
+    dt, d = _gate_dtype(gates), soma_scan_dims(B, T, D)
+    gp, gs = _rows(gates, "gates", (B, T, 4, D), gates.dtype)
+    hp, hs = _rows(dh, "dh", (B, T, D), gates.dtype)
+    dp, ds = _rows(dgates, "dgates", (B, T, 4, D), gates.dtype)
+    f32 = torch.float32
+    _check(lib().soma_scan_backward(
+        gp, soma_scan_strides(*gs[:3]), dt, d,
+        _dev(checkpoints, f32, "checkpoints", lib().soma_scan_checkpoint_count(d)),
+        _opt(lengths, torch.int32, "lengths", B), _opt(resets, torch.uint8, "resets", B * T), hp,
+        soma_scan_strides(hs[0], hs[1], 0), _opt(dc_last, f32, "dc_last", B * D), dp,
+        soma_scan_strides(*ds[:3]), _opt(dc0, f32, "dc0", B * D), _stream(stream)),
+        "soma_scan_backward")
+
+
+def scan_step(gates: torch.Tensor, c: torch.Tensor, h: torch.Tensor, stream=None):
+    """One token: gates [B, 4, D], state c [B, D] fp32 (updated), h [B, D]."""
+    B, _, D = gates.shape
+    dt = _gate_dtype(gates)
+    gp, gs = _rows(gates, "gates", (B, 4, D), gates.dtype)
+    hp, hs = _rows(h, "h", (B, D), gates.dtype)
+    _check(lib().soma_scan_step(gp, soma_scan_strides(gs[0], 0, gs[1]), dt, B, D,
+                                _dev(c, torch.float32, "c", B * D), hp,
+                                soma_scan_strides(hs[0], 0, 0), _stream(stream)),
+           "soma_scan_step")
+
+
+class AdamW:
+    """AdamW over a list of tensors, one library call per step.
+
+    params: contiguous CUDA tensors of one dtype (fp32, bf16 or fp16).
+    exp_avg, exp_avg_sq: their moments.  fp32 tensors, or float8_e4m3fn ones
+    with the fp32 scales m_scales, v_scales (one per 256 elements); in 8 bits
+    exp_avg_sq holds the root of the second moment.  masters: fp32 copies of
+    16-bit params, or None.  weight_decay: one value, or one per tensor.
+    ``AdamW.zero_state(params, bits)`` makes the moments.  The object keeps
+    the tensors and their table; gradients are passed to every step."""
+
+    def __init__(self, params, exp_avg, exp_avg_sq, m_scales=None, v_scales=None, masters=None,
+                 weight_decay=0.0):
+        n = len(params)
+        for name, ts in (("exp_avg", exp_avg), ("exp_avg_sq", exp_avg_sq), ("m_scales", m_scales),
+                         ("v_scales", v_scales), ("masters", masters)):
+            if ts is not None and len(ts) != n:
+                raise ValueError(f"{name}: expected {n} tensors, got {len(ts)}")
+        self.param_dtype = params[0].dtype if n else torch.float32
+        if self.param_dtype not in DTYPES:
+            raise ValueError(f"params: unsupported dtype {self.param_dtype}")
+        self.bits = 32 if m_scales is None else 8
+        if (m_scales is None) != (v_scales is None):
+            raise ValueError("m_scales and v_scales go together")
+        state = torch.float32 if self.bits == 32 else torch.float8_e4m3fn
+        decay = [float(weight_decay)] * n if not hasattr(weight_decay, "__len__") else weight_decay
+        if len(decay) != n:
+            raise ValueError(f"weight_decay: expected {n} values, got {len(decay)}")
+        self.tensors = (list(params), list(exp_avg), list(exp_avg_sq), m_scales, v_scales, masters)
+        self._table = (soma_adamw_tensor * max(n, 1))()
+        for k, p in enumerate(params):
+            row, size, blocks = self._table[k], p.numel(), -(-p.numel() // 256)
+            row.param = _dev(p, self.param_dtype, f"params[{k}]").value
+            row.m = _dev(exp_avg[k], state, f"exp_avg[{k}]", size).value
+            row.v = _dev(exp_avg_sq[k], state, f"exp_avg_sq[{k}]", size).value
+            if self.bits == 8:
+                row.m_scale = _dev(m_scales[k], torch.float32, f"m_scales[{k}]", blocks).value
+                row.v_scale = _dev(v_scales[k], torch.float32, f"v_scales[{k}]", blocks).value
+            if masters is not None:
+                row.master = _dev(masters[k], torch.float32, f"masters[{k}]", size).value
+            row.count, row.weight_decay = size, float(decay[k])
+
+    @staticmethod
+    def zero_state(params, bits: int = 32) -> dict:
+        """Zero moments as keyword arguments of the constructor."""
+        if bits == 32:
+            return {k: [torch.zeros_like(p, dtype=torch.float32) for p in params]
+                    for k in ("exp_avg", "exp_avg_sq")}
+        state = {k: [torch.zeros(p.shape, dtype=torch.uint8, device=p.device)
+                     .view(torch.float8_e4m3fn) for p in params]
+                 for k in ("exp_avg", "exp_avg_sq")}
+        return {**state, **{k: [torch.zeros(-(-p.numel() // 256), device=p.device)
+                                for p in params] for k in ("m_scales", "v_scales")}}
+
+    def step(self, grads, t: int, lr: float, beta1: float = 0.9, beta2: float = 0.999,
+             eps: float = 1e-8, seed: int = 0, grad_scale: torch.Tensor | None = None,
+             stream=None):
+        """Update t (1-based) from grads (one per tensor, one dtype);
+        grad_scale: a device fp32 scalar the gradients are multiplied by."""
+        params = self.tensors[0]
+        if len(grads) != len(params):
+            raise ValueError(f"grads: expected {len(params)} tensors, got {len(grads)}")
+        dtype = grads[0].dtype if grads else torch.float32
+        if dtype not in DTYPES:
+            raise ValueError(f"grads: unsupported dtype {dtype}")
+        for k, (g, p, row) in enumerate(zip(grads, params, self._table)):
+            row.grad = _dev(g, dtype, f"grads[{k}]", row.count).value
+            if p.data_ptr() != (row.param or 0):
+                raise ValueError(f"params[{k}] was given other memory since the table was made")
+        cfg = soma_adamw_config(lr, beta1, beta2, eps, seed & (2 ** 64 - 1), t,
+                                DTYPES[self.param_dtype], DTYPES[dtype], self.bits)
+        _check(lib().soma_adamw_step(
+            self._table, len(params), cfg,
+            _dev(grad_scale, torch.float32, "grad_scale", 1) if grad_scale is not None else None,
+            _stream(stream)), "soma_adamw_step")

@@ -1,0 +1,331 @@
+// adamw.cu -- AdamW over many tensors in one launch, moments in 32 bits or in
+// 8 (soma_adamw_step in include/soma_api.h has the formulas).
+//
+// Work is cut into chunks of kChunk elements of one tensor; a persistent grid
+// takes them in turn and finds a chunk's tensor by bisection over the first
+// chunks, a table in the kernel's parameters.  A thread owns eight consecutive
+// elements, so every stream is read and written in 8- to 32-byte pieces, and
+// a warp owns 256: exactly one block of the 8-bit state, whose new scale is
+// the warp's maximum.
+#include <cmath>
+#include <cuda_fp8.h>
+
+#define SOMA_CHECK_FILE 8
+#include "checked.cuh"
+#include "numeric.cuh"
+#include "soma_api.h"
+#include "soma_launch.h"
+
+namespace soma {
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kGroup = 8;                          // elements of one thread
+constexpr int kBlock8 = 256;                       // elements that share a scale
+constexpr int kChunk = kThreads * kGroup;          // elements of one CTA's turn
+constexpr int kMaxTensors = 360;                   // table rows of one launch
+static_assert(kBlock8 == 32 * kGroup, "a warp owns one block of the 8-bit state");
+
+constexpr float kE4M3Max = 448.f;      // largest e4m3 value
+constexpr float kE4M3Normal = 0x1p-6f; // smallest normal one; the step below it is 2^-9
+constexpr float kE4M3Least = 0x1p-9f;  // smallest above zero
+
+struct Row {
+  void* p;
+  const void* g;
+  void* m;
+  void* v;
+  float* ms;
+  float* vs;
+  float* master;
+  int64_t n;
+  float decay;    // lr * weight_decay
+  int32_t index;  // of the tensor in the caller's list
+  int64_t first;  // its first chunk
+  int64_t vec;    // every address allows 8-element accesses
+};
+
+struct Table {
+  int32_t rows;
+  int64_t chunks;
+  Row row[kMaxTensors];
+};
+static_assert(sizeof(Table) + 256 <= 32764, "kernel parameter space");
+
+struct Args {
+  float b1, c1, b2, c2;  // beta and 1 - beta
+  float lr, s2, eps;     // lr / (1 - beta1^t), 1 / sqrt(1 - beta2^t)
+  uint32_t k0, k1, t;    // Philox key, update
+};
+
+// One value's e4m3 neighbour, up or down at random.  y = |x| / scale lies in
+// [0, 448]; adding 16 random bits right below the last kept mantissa bit and
+// cutting the rest off rounds up with the odds of the cut-off part.  Below
+// the smallest normal value the grid has the step 2^-9, which is the step of
+// [2^-6, 2^-5): the value is moved there and back.
+__device__ __forceinline__ float round_e4m3(float y, uint32_t bits16) {
+  const float low = y < kE4M3Normal ? kE4M3Normal : 0.f;
+  const uint32_t u = (__float_as_uint(__fadd_rn(y, low)) + (bits16 << 4)) & 0xFFF00000u;
+  return __fsub_rn(__uint_as_float(u), low);
+}
+
+// Rounds the warp's 256 values x and returns this lane's eight bytes; the
+// scale goes to *scale.  `floor`: what is above zero stays above zero.
+__device__ __forceinline__ uint2 pack_block(const float (&x)[8], const uint4& rnd, bool floor,
+                                            float* scale) {
+  float top = 0.f;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) top = fmaxf(top, fabsf(x[j]));
+#pragma unroll
+  for (int s = 16; s; s >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, s));
+  // below 2^-100 the reciprocal could overflow: such a block is zero
+  const bool some = top > 0x1p-100f;
+  const float inv = some ? __fdiv_rn(kE4M3Max, top) : 0.f;
+  if ((threadIdx.x & 31) == 0) *scale = some ? __fdiv_rn(top, kE4M3Max) : 0.f;
+  float z[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const uint32_t w = word_of(rnd, j >> 1);
+    const float y = fminf(__fmul_rn(fabsf(x[j]), inv), kE4M3Max);
+    float r = round_e4m3(y, (j & 1) ? w >> 16 : w & 0xFFFFu);
+    if (floor && y > 0.f) r = fmaxf(r, kE4M3Least);
+    z[j] = x[j] < 0.f ? -r : r;
+  }
+  // z is on the e4m3 grid: the conversion is exact
+  uint32_t h[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    h[j] = __nv_cvt_float2_to_fp8x2(make_float2(z[2 * j], z[2 * j + 1]), __NV_SATFINITE, __NV_E4M3);
+  return make_uint2(h[0] | (h[1] << 16), h[2] | (h[3] << 16));
+}
+
+__device__ __forceinline__ void unpack8(const uint2& b, float scale, float (&x)[8]) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const uint32_t w = (j < 2 ? b.x : b.y) >> (16 * (j & 1));
+    const __half2 h = __half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w & 0xFFFFu), __NV_E4M3));
+    const float2 f = __half22float2(h);
+    x[2 * j] = __fmul_rn(f.x, scale);
+    x[2 * j + 1] = __fmul_rn(f.y, scale);
+  }
+}
+
+template <typename T>
+__device__ __forceinline__ void load_n(const T* p, bool vec, int n, float (&x)[8]) {
+  if (vec && n == kGroup) {
+    load8(p, x);
+  } else {
+#pragma unroll
+    for (int j = 0; j < kGroup; ++j) x[j] = j < n ? to_f32(p[j]) : 0.f;
+  }
+}
+
+template <typename T>
+__device__ __forceinline__ void store_n(T* p, bool vec, int n, const float (&x)[8]) {
+  if (vec && n == kGroup) {
+    store8(p, x);
+  } else {
+#pragma unroll
+    for (int j = 0; j < kGroup; ++j)
+      if (j < n) p[j] = from_f32<T>(x[j]);
+  }
+}
+
+__device__ __forceinline__ uint2 load_bytes(const uint8_t* p, bool vec, int n) {
+  if (vec && n == kGroup) return *reinterpret_cast<const uint2*>(p);
+  uint32_t w[2] = {0u, 0u};
+#pragma unroll
+  for (int j = 0; j < kGroup; ++j)
+    if (j < n) w[j >> 2] |= (uint32_t)p[j] << (8 * (j & 3));
+  return make_uint2(w[0], w[1]);
+}
+
+__device__ __forceinline__ void store_bytes(uint8_t* p, bool vec, int n, const uint2& b) {
+  if (vec && n == kGroup) {
+    *reinterpret_cast<uint2*>(p) = b;
+  } else {
+#pragma unroll
+    for (int j = 0; j < kGroup; ++j)
+      if (j < n) p[j] = (uint8_t)((j < 4 ? b.x : b.y) >> (8 * (j & 3)));
+  }
+}
+
+template <typename P, typename G, bool MASTER, bool EIGHT>
+__global__ void __launch_bounds__(kThreads)
+adamw_kernel(const __grid_constant__ Table tab, Args a, const float* __restrict__ grad_scale,
+             int* status) {
+  const float gs = grad_scale ? *grad_scale : 1.f;
+  if (!isfinite(gs)) {
+    if (blockIdx.x == 0 && threadIdx.x == 0) atomicCAS(status, 0, SOMA_ERR_NONFINITE);
+    return;
+  }
+  bool bad = false;
+  for (int64_t chunk = blockIdx.x; chunk < tab.chunks; chunk += gridDim.x) {
+    int lo = 0, hi = tab.rows - 1;  // the last row whose first chunk is <= chunk
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (tab.row[mid].first <= chunk) lo = mid; else hi = mid - 1;
+    }
+    const Row& t = tab.row[lo];
+    const int64_t base = (chunk - t.first) * kChunk;
+    const int64_t i = base + (int64_t)threadIdx.x * kGroup;
+    if (i - (threadIdx.x & 31) * kGroup >= t.n) continue;  // the whole warp is past the end
+    const int n = i >= t.n ? 0 : (int)(t.n - i < kGroup ? t.n - i : kGroup);
+    const bool vec = t.vec != 0;
+
+    float g[8], w[8], m[8], v[8], r[8];
+    load_n(static_cast<const G*>(t.g) + i, vec, n, g);
+    if (MASTER) load_n(t.master + i, vec, n, w);
+    else load_n(static_cast<const P*>(t.p) + i, vec, n, w);
+    if (EIGHT) {
+      unpack8(load_bytes(static_cast<const uint8_t*>(t.m) + i, vec, n), t.ms[i / kBlock8], m);
+      unpack8(load_bytes(static_cast<const uint8_t*>(t.v) + i, vec, n), t.vs[i / kBlock8], r);
+    } else {
+      load_n(static_cast<const float*>(t.m) + i, vec, n, m);
+      load_n(static_cast<const float*>(t.v) + i, vec, n, v);
+    }
+#pragma unroll
+    for (int j = 0; j < kGroup; ++j) {
+      if (EIGHT) v[j] = __fmul_rn(r[j], r[j]);
+      const float x = __fmul_rn(g[j], gs);
+      const float m1 = __fadd_rn(__fmul_rn(m[j], a.b1), __fmul_rn(x, a.c1));
+      const float v1 = __fadd_rn(__fmul_rn(v[j], a.b2), __fmul_rn(__fmul_rn(x, x), a.c2));
+      const float r1 = __fsqrt_rn(v1);
+      const float step = __fdiv_rn(m1, __fadd_rn(__fmul_rn(r1, a.s2), a.eps));
+      if (isfinite(m1) && isfinite(v1)) {
+        // w - decay w in one rounding: 1 - decay would be rounded before the product
+        w[j] = __fmaf_rn(-step, a.lr, __fmaf_rn(-w[j], t.decay, w[j]));
+        m[j] = m1;
+        v[j] = v1;
+        r[j] = r1;
+      } else {
+        bad = true;
+      }
+    }
+    if (MASTER) store_n(t.master + i, vec, n, w);
+    store_n(static_cast<P*>(t.p) + i, vec, n, w);
+    if (EIGHT) {
+      const uint64_t q = (uint64_t)i / kGroup;
+      const uint4 rnd = philox4x32_10(
+          make_uint4((uint32_t)q, (uint32_t)t.index, a.t, 0x80000002u), a.k0, a.k1);
+      const uint2 bm = pack_block(m, rnd, false, t.ms + i / kBlock8);
+      const uint2 bv = pack_block(r, rnd, true, t.vs + i / kBlock8);
+      store_bytes(static_cast<uint8_t*>(t.m) + i, vec, n, bm);
+      store_bytes(static_cast<uint8_t*>(t.v) + i, vec, n, bv);
+    } else {
+      store_n(static_cast<float*>(t.m) + i, vec, n, m);
+      store_n(static_cast<float*>(t.v) + i, vec, n, v);
+    }
+  }
+  if (bad) atomicCAS(status, 0, SOMA_ERR_NONFINITE);
+}
+
+using Kernel = void (*)(const Table, Args, const float*, int*);
+
+template <typename P, typename G>
+Kernel pick(bool master, bool eight) {
+  if (master) return eight ? adamw_kernel<P, G, true, true> : adamw_kernel<P, G, true, false>;
+  return eight ? adamw_kernel<P, G, false, true> : adamw_kernel<P, G, false, false>;
+}
+
+template <typename P>
+Kernel pick(int grad, bool master, bool eight) {
+  if (grad == SOMA_FP32) return pick<P, float>(master, eight);
+  if (grad == SOMA_BF16) return pick<P, __nv_bfloat16>(master, eight);
+  return pick<P, __half>(master, eight);
+}
+
+Kernel pick(int param, int grad, bool master, bool eight) {
+  if (param == SOMA_FP32) return pick<float>(grad, false, eight);
+  if (param == SOMA_BF16) return pick<__nv_bfloat16>(grad, master, eight);
+  return pick<__half>(grad, master, eight);
+}
+
+int width(int dtype) { return dtype == SOMA_FP32 ? 4 : 2; }
+
+bool aligned(const void* p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
+
+}  // namespace
+
+}  // namespace soma
+
+using namespace soma;
+
+extern "C" int soma_adamw_step(const soma_adamw_tensor* tensors, int n_tensors,
+                               soma_adamw_config cfg, const float* grad_scale, void* stream) {
+  const auto dtype_ok = [](int d) { return d == SOMA_FP32 || d == SOMA_BF16 || d == SOMA_FP16; };
+  if (n_tensors < 0 || (n_tensors > 0 && !tensors) || !dtype_ok(cfg.param_dtype) ||
+      !dtype_ok(cfg.grad_dtype) || (cfg.state_bits != 8 && cfg.state_bits != 32) || cfg.t < 1 ||
+      !std::isfinite(cfg.lr) || !(cfg.beta1 >= 0 && cfg.beta1 < 1) ||
+      !(cfg.beta2 >= 0 && cfg.beta2 < 1) || !((float)cfg.eps > 0.f) ||
+      !std::isfinite((float)cfg.eps) || !aligned(grad_scale, 4))
+    return SOMA_ERR_INVALID_ARG;
+  const bool eight = cfg.state_bits == 8;
+  const int pw = width(cfg.param_dtype), gw = width(cfg.grad_dtype), sw = eight ? 1 : 4;
+  bool master = false, plain = false;
+  for (int k = 0; k < n_tensors; ++k) {
+    const soma_adamw_tensor& t = tensors[k];
+    if (t.count < 0 || t.count > ((int64_t)1 << 40) || !(t.weight_decay >= 0) ||
+        !std::isfinite(t.weight_decay))
+      return SOMA_ERR_INVALID_ARG;
+    if (t.count == 0) continue;
+    if (!t.param || !t.grad || !t.m || !t.v || !aligned(t.param, pw) || !aligned(t.grad, gw) ||
+        !aligned(t.m, sw) || !aligned(t.v, sw) || !aligned(t.master, 4) ||
+        !aligned(t.m_scale, 4) || !aligned(t.v_scale, 4) ||
+        (eight ? !t.m_scale || !t.v_scale : t.m_scale || t.v_scale) ||
+        (t.master && cfg.param_dtype == SOMA_FP32))
+      return SOMA_ERR_INVALID_ARG;
+    (t.master ? master : plain) = true;
+  }
+  if (master && plain) return SOMA_ERR_INVALID_ARG;  // masters for all tensors or for none
+  int* status = status_ptr();
+  if (!status) return SOMA_ERR_CUDA;
+
+  Args a;
+  a.b1 = (float)cfg.beta1;
+  a.c1 = (float)(1.0 - cfg.beta1);
+  a.b2 = (float)cfg.beta2;
+  a.c2 = (float)(1.0 - cfg.beta2);
+  a.lr = (float)(cfg.lr / (1.0 - std::pow(cfg.beta1, (double)cfg.t)));
+  a.s2 = (float)(1.0 / std::sqrt(1.0 - std::pow(cfg.beta2, (double)cfg.t)));
+  a.eps = (float)cfg.eps;
+  a.k0 = (uint32_t)cfg.seed;
+  a.k1 = (uint32_t)(cfg.seed >> 32);
+  a.t = (uint32_t)cfg.t;
+  const Kernel kernel = pick(cfg.param_dtype, cfg.grad_dtype, master, eight);
+
+  Table tab;
+  int k = 0;
+  while (k < n_tensors) {
+    tab.rows = 0;
+    tab.chunks = 0;
+    for (; k < n_tensors && tab.rows < kMaxTensors; ++k) {
+      const soma_adamw_tensor& t = tensors[k];
+      if (t.count == 0) continue;
+      Row& r = tab.row[tab.rows++];
+      r.p = t.param;
+      r.g = t.grad;
+      r.m = t.m;
+      r.v = t.v;
+      r.ms = t.m_scale;
+      r.vs = t.v_scale;
+      r.master = t.master;
+      r.n = t.count;
+      r.decay = (float)(cfg.lr * t.weight_decay);
+      r.index = k;
+      r.first = tab.chunks;
+      r.vec = aligned(t.param, 16) && aligned(t.grad, 16) && aligned(t.m, eight ? 8 : 16) &&
+              aligned(t.v, eight ? 8 : 16) && aligned(t.master, 16);
+      tab.chunks += (t.count + kChunk - 1) / kChunk;
+    }
+    if (!tab.rows) break;
+    const int64_t resident = 152 * 4;
+    const unsigned grid = (unsigned)(tab.chunks < resident ? tab.chunks : resident);
+    trace_begin(SOMA_TRACE_UPDATE, (cudaStream_t)stream);
+    kernel<<<grid, kThreads, 0, (cudaStream_t)stream>>>(tab, a, grad_scale, status);
+    trace_end(SOMA_TRACE_UPDATE, (cudaStream_t)stream);
+    if (cudaGetLastError() != cudaSuccess) return SOMA_ERR_CUDA;
+  }
+  return SOMA_OK;
+}

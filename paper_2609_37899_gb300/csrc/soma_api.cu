@@ -21,13 +21,10 @@ using namespace soma;
 // soma_get_status and soma_debug_check_line read and clear it.
 __device__ int g_soma_status[2] = {0, 0};
 
-namespace {
-
 constexpr int kMaxDevices = 64;
-constexpr int kMaxPert = 12 * 1024;  // coefficients of one expert staged in shared memory
-int* g_status_ptr[kMaxDevices] = {nullptr};
+static int* g_status_ptr[kMaxDevices] = {nullptr};
 
-int* status_ptr() {
+int* soma::status_ptr() {
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return nullptr;
   if (!g_status_ptr[dev]) {
@@ -37,6 +34,10 @@ int* status_ptr() {
   }
   return g_status_ptr[dev];
 }
+
+namespace {
+
+constexpr int kMaxPert = 12 * 1024;  // coefficients of one expert staged in shared memory
 
 bool dims_ok(const soma_dims& d) {
   return d.vocab == kVocab && d.embed >= 1 && d.embed <= 1024 && d.hidden >= 1 &&

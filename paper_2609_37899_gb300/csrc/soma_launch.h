@@ -11,6 +11,10 @@
 
 namespace soma {
 
+// The current device's status word (soma_get_status) and, after it, the
+// position word of the checked build; nullptr if it cannot be found.
+int* status_ptr();
+
 // Tracing hooks: bracket one kernel launch of class `kind` (SOMA_TRACE_*).
 void trace_begin(int kind, cudaStream_t stream);
 void trace_end(int kind, cudaStream_t stream);
