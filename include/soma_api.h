@@ -525,6 +525,54 @@ int soma_scan_backward(const void* gates, soma_scan_strides gate_strides, int dt
 int soma_scan_step(const void* gates, soma_scan_strides gate_strides, int dtype, int64_t batch,
                    int64_t dim, float* c, void* h, soma_scan_strides h_strides, void* stream);
 
+/* Linear cross entropy: an output head and its softmax cross entropy over a
+ * vocabulary of any size, in pieces, so that the logits of all rows are never
+ * in memory.  For row n with state h_n, target y_n and head emb [vocab][dim]:
+ *   l_nv = <h_n, emb_v>;  lse_n = log sum_v exp l_nv;  loss_n = lse_n - l_{n,y_n}
+ * and with the gradient dloss_n of loss_n, G_nv = dloss_n (exp(l_nv - lse_n) -
+ * [v = y_n]):
+ *   dh_n = sum_v G_nv emb_v;   demb_v = sum_n G_nv h_n
+ * (demb with dloss = 1/(BT) is the decoder-path rule of the paper's seed run,
+ * Eq. delta).  h, emb and their gradients are of one 16-bit soma_dtype;
+ * products accumulate in fp32, losses are fp32.  G is rounded to the 16-bit
+ * type before it meets emb and h (fp16: scaled by a power of two so that the
+ * largest |dloss| lies in [2^13, 2^14)).
+ *
+ * A row whose target is ignore_index has loss 0, lse 0 and no gradient; its h
+ * is never used, whatever it holds.  A row with a target outside 0 .. vocab - 1
+ * or a loss that is not finite gets loss NaN, and SOMA_ERR_NONFINITE is
+ * recorded; in the backward call a row with such a target or an lse that is
+ * not finite has no gradient.
+ *
+ * Rows are h_stride (emb_stride) elements apart, h and emb 16-byte aligned.
+ * Strides that are no multiple of 8 are allowed and cost a copy.  rows
+ * may be 0; vocab and dim are at least 1. */
+typedef struct soma_linear_ce_dims {
+  int64_t rows;  /* 0 .. 2^30 */
+  int64_t vocab; /* 1 .. 2^30 */
+  int64_t dim;   /* 1 .. 65536 */
+  int64_t h_stride, emb_stride; /* >= dim */
+  int32_t dtype; /* SOMA_BF16 or SOMA_FP16 */
+} soma_linear_ce_dims;
+
+/* Bytes of workspace of the forward (backward = 0) or the backward call (1);
+ * 0 if the sizes are invalid.  One workspace of the larger size serves both. */
+size_t soma_linear_ce_workspace_bytes(soma_linear_ce_dims d, int backward);
+
+/* targets int64 [rows]; loss, lse fp32 [rows]. */
+int soma_linear_ce_forward(const void* h, const void* emb, soma_linear_ce_dims d,
+                           const int64_t* targets, int64_t ignore_index, float* loss, float* lse,
+                           void* workspace, size_t workspace_bytes, void* stream);
+
+/* lse: of the forward call on the same h, emb and targets; dloss fp32 [rows];
+ * dh [rows][dim] by dh_stride, demb [vocab][dim] by demb_stride, both written
+ * in full. */
+int soma_linear_ce_backward(const void* h, const void* emb, soma_linear_ce_dims d,
+                            const int64_t* targets, int64_t ignore_index, const float* lse,
+                            const float* dloss, void* dh, int64_t dh_stride, void* demb,
+                            int64_t demb_stride, void* workspace, size_t workspace_bytes,
+                            void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -75,6 +75,11 @@ class soma_scan_strides(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int64) for n in ("b", "t", "g")]
 
 
+class soma_linear_ce_dims(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int64) for n in ("rows", "vocab", "dim", "h_stride",
+                                              "emb_stride")] + [("dtype", ctypes.c_int32)]
+
+
 DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 PROBE_KINDS = {"dense": 0, "sparse": 1}
 MAX_ACCUM = 64
@@ -175,6 +180,11 @@ def _open(path: str):
         _sig(L, "soma_scan_backward", i32, [vp, ss, i32, sd, vp, vp, vp, vp, ss, vp, vp, ss, vp,
                                             vp])
         _sig(L, "soma_scan_step", i32, [vp, ss, i32, i64, i64, vp, vp, ss, vp])
+        cd = soma_linear_ce_dims
+        _sig(L, "soma_linear_ce_workspace_bytes", sz, [cd, i32])
+        _sig(L, "soma_linear_ce_forward", i32, [vp, vp, cd, vp, i64, vp, vp, vp, sz, vp])
+        _sig(L, "soma_linear_ce_backward", i32, [vp, vp, cd, vp, i64, vp, vp, vp, i64, vp, i64,
+                                                 vp, sz, vp])
         _sig(L, "soma_checked_build", i32, [])
         _sig(L, "soma_debug_check_line", i32, [vp])
         _sig(L, "soma_debug_check_fail", i32, [vp])
@@ -593,7 +603,8 @@ class SomaBodies:
 
 
 # ---------------------------------------------------------------------------
-# First-order training: the gated linear recurrence, AdamW.
+# First-order training: the gated linear recurrence, linear cross entropy,
+# AdamW.
 # ---------------------------------------------------------------------------
 
 def _rows(t: torch.Tensor, name: str, shape, dtype) -> tuple:
@@ -676,6 +687,66 @@ def scan_step(gates: torch.Tensor, c: torch.Tensor, h: torch.Tensor, stream=None
                                 _dev(c, torch.float32, "c", B * D), hp,
                                 soma_scan_strides(hs[0], 0, 0), _stream(stream)),
            "soma_scan_step")
+
+
+def _row_stride(t: torch.Tensor) -> int:
+    """Elements between rows; what the stride of fewer than two rows says does not matter."""
+    return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], 1)
+
+
+def _ce_dims(h: torch.Tensor, emb: torch.Tensor) -> soma_linear_ce_dims:
+    return soma_linear_ce_dims(h.shape[0], emb.shape[0], h.shape[1], _row_stride(h),
+                               _row_stride(emb), DTYPES.get(h.dtype, -1))
+
+
+def linear_ce_workspace_bytes(rows: int, vocab: int, dim: int, dtype: torch.dtype,
+                              backward: bool = True, h_stride: int | None = None,
+                              emb_stride: int | None = None) -> int:
+    """Bytes that linear_ce_forward needs, and linear_ce_backward with `backward`."""
+    d = soma_linear_ce_dims(rows, vocab, dim, h_stride or dim, emb_stride or dim,
+                            DTYPES.get(dtype, -1))
+    return max(int(lib().soma_linear_ce_workspace_bytes(d, k)) for k in range(1 + bool(backward)))
+
+
+def linear_ce_alloc_workspace(rows, vocab, dim, dtype, backward=True, h_stride=None,
+                              emb_stride=None, device="cuda") -> torch.Tensor:
+    n = linear_ce_workspace_bytes(rows, vocab, dim, dtype, backward, h_stride, emb_stride)
+    if n == 0:
+        raise ValueError("invalid sizes or dtype for the workspace")
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def linear_ce_forward(h: torch.Tensor, emb: torch.Tensor, targets: torch.Tensor,
+                      loss: torch.Tensor, lse: torch.Tensor, workspace: torch.Tensor,
+                      ignore_index: int = -100, stream=None):
+    """Cross entropy of the head emb [V, d] on states h [N, d] (bf16 or fp16)
+    for targets [N] int64: loss and lse [N] fp32, per row."""
+    N = h.shape[0]
+    hp, _ = _rows(h, "h", (N, emb.shape[1]), emb.dtype)
+    ep, _ = _rows(emb, "emb", emb.shape, h.dtype)
+    _check(lib().soma_linear_ce_forward(
+        hp, ep, _ce_dims(h, emb), _dev(targets, torch.int64, "targets", N), ignore_index,
+        _dev(loss, torch.float32, "loss", N), _dev(lse, torch.float32, "lse", N),
+        _dev(workspace, torch.uint8, "workspace"), workspace.numel(), _stream(stream)),
+        "soma_linear_ce_forward")
+
+
+def linear_ce_backward(h: torch.Tensor, emb: torch.Tensor, targets: torch.Tensor,
+                       lse: torch.Tensor, dloss: torch.Tensor, dh: torch.Tensor,
+                       demb: torch.Tensor, workspace: torch.Tensor, ignore_index: int = -100,
+                       stream=None):
+    """Gradients of linear_ce_forward: dh [N, d] and demb [V, d] from its lse
+    and the gradient dloss [N] fp32 of its losses."""
+    N = h.shape[0]
+    hp, _ = _rows(h, "h", (N, emb.shape[1]), emb.dtype)
+    ep, _ = _rows(emb, "emb", emb.shape, h.dtype)
+    dhp, _ = _rows(dh, "dh", h.shape, h.dtype)
+    dep, _ = _rows(demb, "demb", emb.shape, h.dtype)
+    _check(lib().soma_linear_ce_backward(
+        hp, ep, _ce_dims(h, emb), _dev(targets, torch.int64, "targets", N), ignore_index,
+        _dev(lse, torch.float32, "lse", N), _dev(dloss, torch.float32, "dloss", N), dhp,
+        _row_stride(dh), dep, _row_stride(demb), _dev(workspace, torch.uint8, "workspace"),
+        workspace.numel(), _stream(stream)), "soma_linear_ce_backward")
 
 
 class AdamW:

@@ -73,3 +73,39 @@ def test_scan_refusals(soma):
     # nothing to do is fine without pointers
     assert L.soma_scan_forward(None, s, 0, dims(0, 3, 8), None, None, None, None, s, None, None,
                                None) == 0
+
+
+def test_linear_ce_refusals(soma):
+    L, D = soma.lib(), soma.soma_linear_ce_dims
+    ok, odd = D(20, 30, 16, 16, 16, 1), ctypes.c_void_p(0x10008)
+    big = 1 << 40
+    fw, bw = L.soma_linear_ce_workspace_bytes(ok, 0), L.soma_linear_ce_workspace_bytes(ok, 1)
+    assert fw > 0 and bw > 0
+    for bad in (D(-1, 30, 16, 16, 16, 1), D(20, 0, 16, 16, 16, 1), D(20, 30, 0, 16, 16, 1),
+                D(20, 30, 16, 15, 16, 1), D(20, 30, 16, 16, 15, 1), D(20, 30, 16, 16, 16, 0),
+                D(20, 30, 16, 16, 16, 3), D((1 << 30) + 1, 30, 16, 16, 16, 1),
+                D(20, (1 << 30) + 1, 16, 16, 16, 1), D(20, 30, 65537, 65537, 65537, 1)):
+        assert L.soma_linear_ce_workspace_bytes(bad, 0) == 0
+        assert L.soma_linear_ce_workspace_bytes(bad, 1) == 0
+        assert L.soma_linear_ce_forward(FAKE, FAKE, bad, FAKE, -1, FAKE, FAKE, FAKE, big, None) == 2
+        assert L.soma_linear_ce_backward(FAKE, FAKE, bad, FAKE, -1, FAKE, FAKE, FAKE, 16, FAKE, 16,
+                                         FAKE, big, None) == 2
+    for k in range(5):  # h, emb, targets, loss, lse missing
+        p = [None if j == k else FAKE for j in range(5)]
+        assert L.soma_linear_ce_forward(p[0], p[1], ok, p[2], -1, p[3], p[4], FAKE, big, None) == 1
+    assert L.soma_linear_ce_forward(odd, FAKE, ok, FAKE, -1, FAKE, FAKE, FAKE, big, None) == 1
+    assert L.soma_linear_ce_forward(FAKE, odd, ok, FAKE, -1, FAKE, FAKE, FAKE, big, None) == 1
+    assert L.soma_linear_ce_forward(FAKE, FAKE, ok, FAKE, -1, FAKE, FAKE, None, big, None) == 3
+    assert L.soma_linear_ce_forward(FAKE, FAKE, ok, FAKE, -1, FAKE, FAKE, FAKE, fw - 1, None) == 3
+    assert L.soma_linear_ce_forward(None, FAKE, D(0, 30, 16, 16, 16, 1), None, -1, None, None, None,
+                                    0, None) == 0
+    for k in range(7):  # h, emb, targets, lse, dloss, dh, demb missing
+        p = [None if j == k else FAKE for j in range(7)]
+        assert L.soma_linear_ce_backward(p[0], p[1], ok, p[2], -1, p[3], p[4], p[5], 16, p[6], 16,
+                                         FAKE, big, None) == 1
+    assert L.soma_linear_ce_backward(FAKE, FAKE, ok, FAKE, -1, FAKE, FAKE, FAKE, 15, FAKE, 16, FAKE,
+                                     big, None) == 1
+    assert L.soma_linear_ce_backward(FAKE, FAKE, ok, FAKE, -1, FAKE, FAKE, FAKE, 16, FAKE, 15, FAKE,
+                                     big, None) == 1
+    assert L.soma_linear_ce_backward(FAKE, FAKE, ok, FAKE, -1, FAKE, FAKE, FAKE, 16, FAKE, 16, FAKE,
+                                     bw - 1, None) == 3
