@@ -1,0 +1,92 @@
+// tc_tiles.cuh -- what the 16-bit matrix products of the first-order operators
+// need beyond tc_primitives.cuh: tensor maps and tiled bulk copies, and the
+// descriptors of 128-byte-swizzled operand tiles, K-major and MN-major.
+//
+// A stage of an operand is made of boxes of 64 columns (128 bytes) by some
+// rows of the matrix in memory, each row 128 bytes further, the 16-byte pieces
+// of a row permuted by the row's index modulo 8 (the 128-byte swizzle).
+//  - K-major (the columns are the product's depth): one box of 128 or 256
+//    rows; eight rows lie 1024 bytes apart from the next eight.
+//  - MN-major (the columns are the operand's rows): one box of 64 rows per 64
+//    columns; the depth runs over the box's rows.
+#pragma once
+
+#include <cstdint>
+#include <cuda.h>
+#include <cuda_runtime.h>
+
+#include "tc_primitives.cuh"
+
+namespace soma {
+namespace tc {
+
+constexpr int kBoxCols = 64;                // 16-bit elements of one swizzled row
+constexpr int kDepth = 64;                  // depth of one stage
+constexpr uint32_t kBoxBytes = 64 * 128;    // an MN-major box
+
+// 2-D tiled copy of one box at (x, y) = (column, row).
+__device__ __forceinline__ void tile_g2s(void* smem_dst, const CUtensorMap* map, int x, int y,
+                                         uint64_t* bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
+      " [%0], [%1, {%2, %3}], [%4];" ::"r"(smem_u32(smem_dst)),
+      "l"(map), "r"(x), "r"(y), "r"(smem_u32(bar))
+      : "memory");
+}
+
+__device__ __forceinline__ void prefetch_map(const CUtensorMap* map) {
+  asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
+}
+
+// High word of a swizzled operand descriptor: 1024 bytes between groups of
+// eight rows, descriptor version 1, 128-byte swizzle.
+constexpr uint32_t kDescHi = (1024u >> 4) | (1u << 14) | (2u << 29);
+
+// Low word: start address, and between 64-column blocks of an MN-major
+// operand the size of a box (K-major operands have a single block: unused).
+__device__ __forceinline__ uint32_t desc_lo(uint32_t saddr, bool mn_major) {
+  return ((saddr & 0x3FFFFu) >> 4) | ((mn_major ? kBoxBytes >> 4 : 1u) << 16);
+}
+
+// What 16 steps of depth add to the low word: 32 bytes of a row, or 16 rows.
+__host__ __device__ constexpr uint32_t desc_step(bool mn_major) {
+  return mn_major ? (16u * 128u) >> 4 : 32u >> 4;
+}
+
+// Instruction descriptor of kind::f16 with fp32 accumulation.
+__host__ __device__ constexpr uint32_t idesc_16(int M, int N, bool bf16, bool a_mn, bool b_mn) {
+  return (1u << 4) | ((bf16 ? 1u : 0u) << 7) | ((bf16 ? 1u : 0u) << 10) |
+         ((a_mn ? 1u : 0u) << 15) | ((b_mn ? 1u : 0u) << 16) | ((uint32_t)(N >> 3) << 17) |
+         ((uint32_t)(M >> 4) << 24);
+}
+
+// 32 consecutive fp32 columns of this thread's TMEM lane; valid after
+// tmem_wait_ld().
+__device__ __forceinline__ void tmem_ld32_nowait(uint32_t taddr, float (&v)[32]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,"
+      "%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+      : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]),
+        "=f"(v[7]), "=f"(v[8]), "=f"(v[9]), "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]),
+        "=f"(v[14]), "=f"(v[15]), "=f"(v[16]), "=f"(v[17]), "=f"(v[18]), "=f"(v[19]),
+        "=f"(v[20]), "=f"(v[21]), "=f"(v[22]), "=f"(v[23]), "=f"(v[24]), "=f"(v[25]),
+        "=f"(v[26]), "=f"(v[27]), "=f"(v[28]), "=f"(v[29]), "=f"(v[30]), "=f"(v[31])
+      : "r"(taddr));
+}
+
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+}  // namespace tc
+
+// Tensor map of a row-major 16-bit matrix [rows][cols], `stride` elements
+// between rows, read in boxes of 64 columns by box_rows rows.  The address
+// must be 16-byte aligned and the stride a multiple of 8.  What lies outside
+// the matrix reads as zero.
+bool make_tile_map(CUtensorMap* map, const void* base, bool bf16, int64_t rows, int64_t cols,
+                   int64_t stride, int box_rows);
+
+}  // namespace soma
