@@ -1,15 +1,18 @@
 // linear_ce.cu -- linear cross entropy and its gradients in pieces of the
 // vocabulary (soma_linear_ce_* in include/soma_api.h have the formulas).
 //
-// Every product is a tcgen05 one of 128 x 256 tiles: a persistent kernel whose
-// CTAs copy operand tiles with TMA into a ring of shared-memory stages,
-// multiply them into one of two accumulators in tensor memory, and read the
-// other one back in the epilogue.  What differs is the epilogue:
+// Every product is a tcgen05 one of 256 x 256 tiles: a persistent kernel of
+// CTA pairs that copy operand tiles with TMA into a ring of shared-memory
+// stages, multiply them into one of two accumulators in tensor memory, and
+// read the other one back in the epilogue.  What differs is the epilogue:
 //   stats  h emb^T        per row the running maximum and sum of the exponentials
 //                         over a range of the vocabulary, and the target's logit
 //   grad   h emb^T        G of one piece of the vocabulary, in 16 bits
-//   dh     G emb          added to fp32 sums over the pieces
 //   demb   G^T h          the piece's rows of demb
+//   dh     G emb          the rows of dh, where one piece holds the vocabulary
+//   demb_sums, dh_sums    fp32 sums over pieces, or over parts of the depth where
+//                         there are too few tiles to occupy the GPU otherwise;
+//                         sums_kernel rounds them
 #include <cmath>
 
 #define SOMA_CHECK_FILE 10
@@ -21,7 +24,7 @@
 
 namespace soma {
 
-bool make_tile_map(CUtensorMap* map, const void* base, bool bf16, int64_t rows, int64_t cols,
+bool make_tile_map(CUtensorMap* map, const void* base, int dtype, int64_t rows, int64_t cols,
                    int64_t stride, int box_rows) {
   using Encode = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*,
                               const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
@@ -38,115 +41,139 @@ bool make_tile_map(CUtensorMap* map, const void* base, bool bf16, int64_t rows, 
   }();
   if (!encode) return false;
   const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
-  const cuuint64_t strides[1] = {(cuuint64_t)stride * 2};
-  const cuuint32_t box[2] = {(cuuint32_t)tc::kBoxCols, (cuuint32_t)box_rows};
+  const int width = dtype == SOMA_FP32 ? 4 : 2;
+  const cuuint64_t strides[1] = {(cuuint64_t)stride * width};
+  const cuuint32_t box[2] = {128u / width, (cuuint32_t)box_rows};
   const cuuint32_t step[2] = {1, 1};
-  return encode(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2,
-                const_cast<void*>(base), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+  const CUtensorMapDataType type = dtype == SOMA_FP32   ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
+                                   : dtype == SOMA_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16
+                                                        : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+  return encode(map, type, 2, const_cast<void*>(base), dims, strides, box, step,
+                CU_TENSOR_MAP_INTERLEAVE_NONE,
                 CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                 CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 namespace {
 
-constexpr int kSms = 152;
-constexpr int kM = 128, kN = 256;             // one accumulator tile
-constexpr int kStages = 4;
-constexpr uint32_t kABytes = kM * 128, kBBytes = kN * 128;
-constexpr uint32_t kStageBytes = kABytes + kBBytes;
+constexpr int kPairs = 76;                    // CTA pairs that are resident: 152 SMs
+constexpr int kTile = 256;                    // rows and columns of a pair's tile
+constexpr int kHalf = 128;                    // rows of A, and of B, that one CTA stages
+constexpr int kStages = 6;
+constexpr uint32_t kOperandBytes = kHalf * 128;
+constexpr uint32_t kStageBytes = 2 * kOperandBytes;
 constexpr int kEpilogueWarps = 8;
+constexpr uint32_t kOutBytes = 32 * 128;      // a warp's output box: 32 rows of 128 bytes
 constexpr int kThreads = 128 + 32 * kEpilogueWarps;
-constexpr size_t kSmem = kStages * kStageBytes + 1024;  // and what aligns the stages
-constexpr size_t kPieceBytes = (size_t)256 << 20;       // of G of one piece
+constexpr size_t kSmem =                      // and what aligns the stages
+    kStages * kStageBytes + kEpilogueWarps * kOutBytes + 1024;
+constexpr size_t kPieceBytes = (size_t)256 << 20;  // of G of one piece, at most
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kLn2 = 0.6931471805599453f;
+constexpr double kLn2 = 0.69314718055994530942;
 
-enum Kind { kStats, kGrad, kDh, kDemb };
-__host__ __device__ constexpr bool a_mn(int kind) { return kind == kDemb; }
-__host__ __device__ constexpr bool b_mn(int kind) { return kind == kDh || kind == kDemb; }
+enum Kind { kStats, kGrad, kDemb, kDh, kDembSums, kDhSums };
+__host__ __device__ constexpr bool a_mn(int kind) { return kind == kDemb || kind == kDembSums; }
+__host__ __device__ constexpr bool b_mn(int kind) { return kind >= kDemb; }
+__host__ __device__ constexpr bool sums(int kind) { return kind >= kDembSums; }
 
-// What a row of the backward call takes part with; y = -1: no part.
-struct RowInfo {
-  float lse2, g;  // lse in powers of two, the scaled gradient of the loss
-  int64_t y;
+// What a row of the backward call takes part with; y = -1: no part.  The
+// entry of G at the target is by far the row's largest, and its rounding to 16
+// bits would be most of dh's error: what the rounding took off is kept, and dh
+// gets it back times the target's row of emb.
+struct __align__(16) RowInfo {
+  float lse2;  // lse in powers of two
+  float g;     // gradient of the loss
+  float rest;  // of the (scaled) entry of G at the target; written by grad
+  int32_t y;
 };
 
 // One launch.  Stats: unit (m, split) covers the n tiles of the split.  Grad
-// and demb: a unit is one tile.  Dh: the depth of all tiles laid end to end is
-// cut into equal shares, one per CTA; a tile that several CTAs share is summed
-// in as many slots.
+// and demb: a unit is one tile.  Sums: `columns` pairs form a group that works
+// on the same rows and depth, one n tile each (then n + columns, ...); the
+// depth of all m tiles laid end to end is cut into equal shares, one per
+// group, and a tile that several groups share is summed in as many slots.
 struct Work {
-  int32_t m_tiles, n_tiles, k_stages, splits;
-  int32_t ctas;
+  int32_t m_tiles, n_tiles, k_stages;
+  int32_t splits;             // stats
+  int32_t pairs;              // of the grid
+  int32_t columns, groups;    // sums
   int64_t M, N;               // rows and columns that exist
-  int32_t x_a, y_a, x_b, y_b; // first column or row of the operands' depth-free axis (pieces)
+  int32_t y_b;                // first row of B (the piece's place in emb)
   // stats
   const int64_t* targets;
   float2* partial;            // [2 splits][M]: maximum (powers of two), sum
   float* own;                 // [M] logit of the target
-  // grad
-  const RowInfo* info;
-  void* out;                  // G, or demb
-  int64_t out_stride;
+  // grad, dh
+  RowInfo* info;
+  const void* emb;            // dh: 16-byte aligned rows of emb
+  int64_t emb_stride;
   int64_t v0;                 // first vocabulary entry of the piece
-  int32_t vec;                // rows of out allow 16-byte stores
-  // dh
-  float* acc;                 // [slots][M][N4]
-  int64_t acc_stride, slot_stride;
-  int32_t add;                // add to acc instead of writing it
   const float* top;           // largest |dloss|
+  // demb, dh: where its rows are not 16-byte aligned, or null
+  void* out;
+  int64_t out_stride;
+  // sums
+  int32_t slot_rows;          // rows of one slot
+  int32_t add;                // add to the sums instead of writing them
 };
 
-__device__ __forceinline__ int64_t share_start(int64_t c, int64_t total, int64_t ctas) {
-  return c * total / ctas;
+// The first depth stage of share g, and the share that holds stage x.
+__host__ __device__ __forceinline__ int64_t share_start(int64_t g, int64_t total, int64_t groups) {
+  return g * total / groups;
 }
-// The CTA whose share holds depth stage x.
-__host__ __device__ __forceinline__ int64_t share_owner(int64_t x, int64_t total, int64_t ctas) {
-  return ((x + 1) * ctas - 1) / total;
+__host__ __device__ __forceinline__ int64_t share_owner(int64_t x, int64_t total, int64_t groups) {
+  return ((x + 1) * groups - 1) / total;
 }
 
-// A stretch of one CTA's work: stages [k0, k1) of tile (m, n).
+// A stretch of one pair's work: stages [k0, k1) of tile (m, n).
 struct Span {
   int32_t m, n, k0, k1;
+  int32_t part;     // stats: the split; sums: the slot
+  bool first, last; // stats: whether the span begins / ends its unit
 };
 
-// The spans of CTA `cta` in order.
+// The spans of one pair in order; every warp role walks them by itself.
 template <int KIND>
 struct Walk {
   const Work& w;
   int64_t at, end;
   int32_t n, n_end;
 
-  __device__ Walk(const Work& work, int cta) : w(work) {
-    if (KIND == kDh) {
-      const int64_t total = (int64_t)w.m_tiles * w.n_tiles * w.k_stages;
-      at = share_start(cta, total, w.ctas);
-      end = share_start(cta + 1, total, w.ctas);
+  __device__ Walk(const Work& work, int pair) : w(work), n_end(0) {
+    if (sums(KIND)) {
+      const int64_t total = (int64_t)w.m_tiles * w.k_stages;
+      const int g = pair / w.columns;
+      at = share_start(g, total, w.groups);
+      end = share_start(g + 1, total, w.groups);
+      n = pair % w.columns;
     } else {
-      at = cta;
+      at = pair;
       end = (int64_t)w.m_tiles * (KIND == kStats ? w.splits : w.n_tiles);
+      n = 0;
     }
-    n = n_end = 0;
   }
-  // first / last: whether the span begins / ends a unit (stats)
-  __device__ bool next(Span& s, bool& first, bool& last) {
-    if (KIND == kDh) {
-      if (at >= end) return false;
-      const int64_t tile = at / w.k_stages;
-      s.n = (int32_t)(tile % w.n_tiles);
-      s.m = (int32_t)(tile / w.n_tiles);
-      s.k0 = (int32_t)(at - tile * w.k_stages);
-      const int64_t left = end - at;
-      s.k1 = left < w.k_stages - s.k0 ? (int32_t)(s.k0 + left) : w.k_stages;
-      at += s.k1 - s.k0;
-      first = last = true;
-      return true;
-    }
+  __device__ bool next(Span& s, int pair) {
     s.k0 = 0;
     s.k1 = w.k_stages;
-    if (KIND == kStats) {
-      first = n == n_end;
-      if (first) {
+    s.part = 0;
+    if (sums(KIND)) {
+      const int64_t total = (int64_t)w.m_tiles * w.k_stages;
+      const int64_t g = pair / w.columns;
+      if (at >= end) {  // the next n tile of this pair, from the share's start
+        n += w.columns;
+        at = share_start(g, total, w.groups);
+      }
+      if (n >= w.n_tiles || at >= end) return false;
+      s.m = (int32_t)(at / w.k_stages);
+      s.n = n;
+      const int64_t begin = (int64_t)s.m * w.k_stages;
+      s.k0 = (int32_t)(at - begin);
+      if (end - at < w.k_stages - s.k0) s.k1 = (int32_t)(s.k0 + (end - at));
+      s.part = (int32_t)(g - share_owner(begin, total, w.groups));
+      at += s.k1 - s.k0;
+    } else if (KIND == kStats) {
+      s.first = n == n_end;
+      if (s.first) {
         if (at >= end) return false;
         const int64_t split = at / w.m_tiles;
         n = (int32_t)(split * w.n_tiles / w.splits);
@@ -154,23 +181,22 @@ struct Walk {
       }
       s.m = (int32_t)(at % w.m_tiles);
       s.n = n++;
-      last = n == n_end;
-      if (last) at += w.ctas;
-      return true;
+      s.part = (int32_t)(at / w.m_tiles);
+      s.last = n == n_end;
+      if (s.last) at += w.pairs;
+    } else {
+      if (at >= end) return false;
+      if (KIND == kGrad) {  // pairs that run together share rows of emb
+        s.m = (int32_t)(at % w.m_tiles);
+        s.n = (int32_t)(at / w.m_tiles);
+      } else {              // ... the part of G
+        s.n = (int32_t)(at % w.n_tiles);
+        s.m = (int32_t)(at / w.n_tiles);
+      }
+      at += w.pairs;
     }
-    if (at >= end) return false;
-    if (KIND == kGrad) {  // CTAs that run together share columns of emb
-      s.m = (int32_t)(at % w.m_tiles);
-      s.n = (int32_t)(at / w.m_tiles);
-    } else {              // ... columns of G
-      s.n = (int32_t)(at % w.n_tiles);
-      s.m = (int32_t)(at / w.n_tiles);
-    }
-    at += w.ctas;
-    first = last = true;
     return true;
   }
-  __device__ int64_t unit_split() const { return (at - w.ctas) / w.m_tiles; }  // after `last`
 };
 
 // The power of two that the 16-bit G is scaled by.
@@ -200,25 +226,47 @@ __device__ __forceinline__ bool wait_or_abort(uint64_t* bar, uint32_t parity, Sh
   return false;
 }
 
+// Eight elements from column j of a row of `dim`; zeros past its end.
 template <typename T>
-__device__ __forceinline__ void store16(T* p, const float (&x)[32], int from) {
-  float a[8];
+__device__ __forceinline__ uint4 row_piece(const T* row, int64_t j, int64_t dim, bool vec) {
+  if (vec && j + 8 <= dim) return *reinterpret_cast<const uint4*>(row + j);
+  union {
+    T t[8];
+    uint4 u;
+  } v;
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) a[j] = x[from + 8 * h + j];
-    store8(p + 8 * h, a);
-  }
+  for (int k = 0; k < 8; ++k) v.t[k] = j + k < dim ? row[j + k] : from_f32<T>(0.f);
+  return v.u;
+}
+
+// One 128-byte row of a warp's output box: 16-byte piece j of row r lies at
+// piece j ^ (r % 8), as the tiled store expects it.
+__device__ __forceinline__ uint4* box_piece(uint8_t* box, int row, int j) {
+  return reinterpret_cast<uint4*>(box + row * 128 + ((j ^ (row & 7)) << 4));
+}
+
+template <typename T>
+__device__ __forceinline__ uint32_t pack2(float a, float b) {
+  union {
+    T t[2];
+    uint32_t u;
+  } w;
+  w.t[0] = from_f32<T>(a);
+  w.t[1] = from_f32<T>(b);
+  return w.u;
 }
 
 template <int KIND, typename T>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
-               const __grid_constant__ Work w, int* status) {
+               const __grid_constant__ CUtensorMap map_out, const __grid_constant__ Work w,
+               int* status) {
   extern __shared__ uint8_t raw[];
   __shared__ Shared sh;
   uint8_t* stages = raw + (1024 - (tc::smem_u32(raw) & 1023)) % 1024;
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  const int pair = blockIdx.x / 2;
+  const uint32_t rank = tc::pair_rank();
 
   if (warp == 0 && lane == 0) {
     for (int i = 0; i < kStages; ++i) {
@@ -227,30 +275,33 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     }
     for (int i = 0; i < 2; ++i) {
       tc::mbar_init(&sh.acc_full[i], 1);
-      tc::mbar_init(&sh.acc_empty[i], kEpilogueWarps);
+      tc::mbar_init(&sh.acc_empty[i], 2 * kEpilogueWarps);
     }
     tc::mbar_init(&sh.done, 1);
     tc::mbar_fence_init();
     sh.abort = 0;
     tc::prefetch_map(&map_a);
     tc::prefetch_map(&map_b);
+    if (KIND != kStats) tc::prefetch_map(&map_out);
   }
-  if (warp == 2) tc::tmem_alloc(&sh.tmem, 512);
+  if (warp == 2) tc::tmem_alloc_pair(&sh.tmem, 512);
   tc::tc_fence_before();
   __syncthreads();
+  tc::cluster_sync();
   tc::tc_fence_after();
   const uint32_t tmem = sh.tmem;
 
-  Walk<KIND> walk(w, blockIdx.x);
+  Walk<KIND> walk(w, pair);
   Span s;
-  bool first, last;
 
   if (warp == 0) {
-    // loader
+    // loader: this CTA's halves of A and B; both CTAs' bytes count on the even
+    // CTA's barrier
     if (lane == 0) {
       uint32_t it = 0;
       bool ok = true;
-      while (ok && walk.next(s, first, last)) {
+      while (ok && walk.next(s, pair)) {
+        const int m0 = s.m * kTile + (int)rank * kHalf, n0 = s.n * kTile + (int)rank * kHalf;
         for (int k = s.k0; k < s.k1; ++k, ++it) {
           const uint32_t slot = it % kStages, round = it / kStages;
           if (!wait_or_abort(&sh.empty[slot], (round & 1) ^ 1, &sh, status)) {
@@ -258,41 +309,41 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             break;
           }
           uint8_t* a = stages + slot * kStageBytes;
-          uint8_t* b = a + kABytes;
-          uint64_t* bar = &sh.full[slot];
-          tc::mbar_arrive_expect_tx(bar, kStageBytes);
+          uint8_t* b = a + kOperandBytes;
+          if (rank == 0) tc::mbar_arrive_expect_tx(&sh.full[slot], 2 * kStageBytes);
+          const uint32_t bar = tc::leader_addr(&sh.full[slot]);
+          const int kx = k * tc::kDepth;
           if (a_mn(KIND)) {
-            for (int j = 0; j < kM / 64; ++j)
-              tc::tile_g2s(a + j * tc::kBoxBytes, &map_a, w.x_a + s.m * kM + j * 64,
-                           w.y_a + k * tc::kDepth, bar);
+            for (int j = 0; j < kHalf / 64; ++j)
+              tc::tile_g2s_pair(a + j * tc::kBoxBytes, &map_a, m0 + j * 64, kx, bar);
           } else {
-            tc::tile_g2s(a, &map_a, w.x_a + k * tc::kDepth, w.y_a + s.m * kM, bar);
+            tc::tile_g2s_pair(a, &map_a, kx, m0, bar);
           }
           if (b_mn(KIND)) {
-            for (int j = 0; j < kN / 64; ++j)
-              tc::tile_g2s(b + j * tc::kBoxBytes, &map_b, w.x_b + s.n * kN + j * 64,
-                           w.y_b + k * tc::kDepth, bar);
+            for (int j = 0; j < kHalf / 64; ++j)
+              tc::tile_g2s_pair(b + j * tc::kBoxBytes, &map_b, n0 + j * 64, w.y_b + kx, bar);
           } else {
-            tc::tile_g2s(b, &map_b, w.x_b + k * tc::kDepth, w.y_b + s.n * kN, bar);
+            tc::tile_g2s_pair(b, &map_b, kx, w.y_b + n0, bar);
           }
         }
       }
-      // an aborting CTA leaves only after its copies have landed
-      if (!ok)
+      // an aborting CTA leaves only after its copies have landed (the even
+      // CTA's barriers count both CTAs' copies)
+      if (!ok && rank == 0)
         for (uint32_t j = it > kStages ? it - kStages : 0; j < it; ++j)
           tc::mbar_wait(&sh.full[j % kStages], (j / kStages) & 1);
     }
-  } else if (warp == 1) {
-    // MMA issuer: the whole warp waits, one elected thread issues
-    constexpr uint32_t idesc = tc::idesc_16(kM, kN, sizeof(T) == 2 && !std::is_same<T, __half>::value,
-                                            a_mn(KIND), b_mn(KIND));
+  } else if (warp == 1 && rank == 0) {
+    // MMA issuer of the pair: the whole warp waits, one elected thread issues
+    constexpr uint32_t idesc =
+        tc::idesc_16(kTile, kTile, !std::is_same<T, __half>::value, a_mn(KIND), b_mn(KIND));
     uint32_t it = 0, n_acc = 0;
     bool ok = true;
-    while (ok && walk.next(s, first, last)) {
+    while (ok && walk.next(s, pair)) {
       const uint32_t buf = n_acc & 1;
       if (!wait_or_abort(&sh.acc_empty[buf], ((n_acc >> 1) & 1) ^ 1, &sh, status)) break;
       tc::tc_fence_after();
-      const uint32_t d = tmem + buf * kN;
+      const uint32_t d = tmem + buf * kTile;
       for (int k = s.k0; k < s.k1; ++k, ++it) {
         const uint32_t slot = it % kStages;
         if (!wait_or_abort(&sh.full[slot], (it / kStages) & 1, &sh, status)) {
@@ -302,60 +353,63 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         tc::tc_fence_after();
         const uint32_t a = tc::smem_u32(stages + slot * kStageBytes);
         const uint32_t a_lo = tc::desc_lo(a, a_mn(KIND));
-        const uint32_t b_lo = tc::desc_lo(a + kABytes, b_mn(KIND));
+        const uint32_t b_lo = tc::desc_lo(a + kOperandBytes, b_mn(KIND));
         if (tc::elect_one()) {
 #pragma unroll
           for (int j = 0; j < tc::kDepth / 16; ++j)
-            tc::mma_f16_ss_lohi(d, a_lo + j * tc::desc_step(a_mn(KIND)), tc::kDescHi,
+            tc::mma_f16_ss_pair(d, a_lo + j * tc::desc_step(a_mn(KIND)),
                                 b_lo + j * tc::desc_step(b_mn(KIND)), tc::kDescHi, idesc,
                                 k > s.k0 || j > 0);
-          tc::mma_commit(&sh.empty[slot]);
+          tc::mma_commit_pair(&sh.empty[slot]);
         }
         __syncwarp();
       }
-      if (ok && tc::elect_one()) tc::mma_commit(&sh.acc_full[buf]);
+      if (ok && tc::elect_one()) tc::mma_commit_pair(&sh.acc_full[buf]);
       __syncwarp();
       ++n_acc;
     }
-    if (tc::elect_one()) tc::mma_commit(&sh.done);
+    if (tc::elect_one()) tc::mma_commit_pair(&sh.done);
     __syncwarp();
     if (!tc::mbar_wait(&sh.done, 0)) atomicCAS(status, 0, SOMA_ERR_TIMEOUT);
   } else if (warp >= 4) {
     // epilogue: warp w reads lane quarter w % 4 (a warp can read no other) and
     // columns half (w - 4) / 4; a thread has one row
     const int quarter = warp % 4, half = (warp - 4) / 4;
-    const int row = quarter * 32 + lane;
+    const int m_in = (int)rank * kHalf + quarter * 32;  // the warp's first row in the tile
+    uint8_t* box = stages + kStages * kStageBytes + (warp - 4) * kOutBytes;
+    const uint32_t empty_bar[2] = {tc::leader_addr(&sh.acc_empty[0]),
+                                   tc::leader_addr(&sh.acc_empty[1])};
     uint32_t n_acc = 0;
     float top = -INFINITY, sum = 0.f;  // stats
     int64_t y = -1;
-    RowInfo info = {0.f, 0.f, -1};
+    RowInfo info = {0.f, 0.f, 0.f, -1};
     float scale = 1.f;
     if (KIND == kGrad) scale = g_scale<T>(*w.top);
-    if (KIND == kDemb) scale = 1.f / g_scale<T>(*w.top);
-    while (walk.next(s, first, last)) {
-      const int64_t m = (int64_t)s.m * kM + row;
+    if (KIND == kDemb || KIND == kDh) scale = 1.f / g_scale<T>(*w.top);
+    while (walk.next(s, pair)) {
+      const int64_t m0 = (int64_t)s.m * kTile + m_in, m = m0 + lane;
       const bool live = m < w.M;
-      if (KIND == kStats && first) {
+      if (KIND == kStats && s.first) {
         top = -INFINITY;
         sum = 0.f;
         y = live ? w.targets[m] : -1;
       }
-      if (KIND == kGrad) {
-        info = {0.f, 0.f, -1};
+      if (KIND == kGrad || KIND == kDh) {
+        info = {0.f, 0.f, 0.f, -1};
         if (live) info = w.info[m];
       }
       const uint32_t buf = n_acc & 1;
       // a tile's whole depth may lie before this: allow it more time
       if (!wait_or_abort(&sh.acc_full[buf], (n_acc >> 1) & 1, &sh, status, 1u << 27)) break;
       tc::tc_fence_after();
-      const uint32_t src = tmem + buf * kN + half * (kN / 2) + ((uint32_t)(quarter * 32) << 16);
-      const int64_t n0 = (int64_t)s.n * kN + half * (kN / 2);
-      for (int c = 0; c < kN / 2; c += 32) {
+      const uint32_t src = tmem + buf * kTile + half * kHalf + ((uint32_t)(quarter * 32) << 16);
+      const int64_t n0 = (int64_t)s.n * kTile + half * kHalf;
+      for (int c = 0; c < kHalf; c += 32) {
+        const int64_t n = n0 + c;
+        if (n >= w.N || m0 >= w.M) break;  // nothing there (the whole warp)
         float x[32];
         tc::tmem_ld32_nowait(src + c, x);
         tc::tmem_wait_ld();
-        const int64_t n = n0 + c;
-        if (n >= w.N) continue;  // columns that do not exist (the whole warp)
         if (KIND == kStats) {
           const int64_t hit = y - n;
           if (hit >= 0 && hit < 32) {
@@ -379,69 +433,107 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
           for (int j = 0; j < 32; ++j) t += tc::ex2(fmaf(x[j], kLog2e, -ref));
           sum = fmaf(sum, tc::ex2(top - ref), t);
           top = now;
-        } else if (KIND == kGrad) {
-          const int64_t hit = info.y - w.v0 - n;
-          const float g = info.y >= 0 ? scale * info.g : 0.f;
+          continue;
+        }
+        // the last box has been read before this one is written
+        const bool new_box = sums(KIND) || c % 64 == 0;
+        if (new_box) {
+          if (lane == 0) tc::bulk_wait_read();
+          __syncwarp();
+        }
+        if (KIND == kGrad) {
+          if (info.y >= 0) {
+            const int64_t hit = info.y - w.v0 - n;
+            const float g = scale * info.g;
 #pragma unroll
-          for (int j = 0; j < 32; ++j) {
-            const float p = tc::ex2(fmaf(x[j], kLog2e, -info.lse2));
-            x[j] = info.y >= 0 && n + j < w.N ? g * (p - (j == hit ? 1.f : 0.f)) : 0.f;
+            for (int j = 0; j < 32; ++j)
+              x[j] = g * (tc::ex2(fmaf(x[j], kLog2e, -info.lse2)) - (j == hit ? 1.f : 0.f));
+            if (hit >= 0 && hit < 32) {
+              float v = 0.f;
+#pragma unroll
+              for (int j = 0; j < 32; ++j) v = j == hit ? x[j] : v;
+              w.info[m].rest = v - to_f32(from_f32<T>(v));
+            }
+          } else {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) x[j] = 0.f;
           }
-          if (live) {
-            T* p = static_cast<T*>(w.out) + m * w.out_stride + n;
-            store16(p, x, 0);
-            store16(p + 16, x, 16);
-          }
-        } else if (KIND == kDemb) {
-          if (live) {
-            T* p = static_cast<T*>(w.out) + m * w.out_stride + n;
+        }
+        if (KIND == kDemb) {
 #pragma unroll
-            for (int j = 0; j < 32; ++j) x[j] *= scale;
-            if (w.vec && n + 32 <= w.N) {
-              store16(p, x, 0);
-              store16(p + 16, x, 16);
-            } else {
+          for (int j = 0; j < 32; ++j) x[j] *= scale;
+        }
+        if (KIND == kDh) {
+          const T* e = static_cast<const T*>(w.emb) + (info.y < 0 ? 0 : info.y) * w.emb_stride;
 #pragma unroll
-              for (int j = 0; j < 32; ++j)
-                if (n + j < w.N) p[j] = from_f32<T>(x[j]);
+          for (int j = 0; j < 4; ++j) {
+            union {
+              uint4 u;
+              T t[8];
+            } v;
+            v.u = make_uint4(0u, 0u, 0u, 0u);
+            if (info.y >= 0) v.u = row_piece(e, n + 8 * j, w.N, true);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+              float& o = x[8 * j + k];
+              o = info.y >= 0 ? scale * fmaf(info.rest, to_f32(v.t[k]), o) : 0.f;
             }
           }
-        } else {
-          const int64_t tile = (int64_t)s.m * w.n_tiles + s.n;
-          const int64_t slot =
-              blockIdx.x - share_owner(tile * w.k_stages,
-                                       (int64_t)w.m_tiles * w.n_tiles * w.k_stages, w.ctas);
-          if (live) {
-            float4* p = reinterpret_cast<float4*>(w.acc + slot * w.slot_stride +
-                                                  m * w.acc_stride + n);
+        }
+        if (sums(KIND)) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
-              if (n + 4 * j < w.acc_stride) {
-                float4 v = make_float4(x[4 * j], x[4 * j + 1], x[4 * j + 2], x[4 * j + 3]);
-                if (w.add) {
-                  const float4 o = p[j];
-                  v = make_float4(v.x + o.x, v.y + o.y, v.z + o.z, v.w + o.w);
-                }
-                p[j] = v;
-              }
-          }
+          for (int j = 0; j < 8; ++j)
+            *box_piece(box, lane, j) =
+                make_uint4(__float_as_uint(x[4 * j]), __float_as_uint(x[4 * j + 1]),
+                           __float_as_uint(x[4 * j + 2]), __float_as_uint(x[4 * j + 3]));
+        } else {
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            *box_piece(box, lane, (c % 64) / 8 + j) =
+                make_uint4(pack2<T>(x[8 * j], x[8 * j + 1]), pack2<T>(x[8 * j + 2], x[8 * j + 3]),
+                           pack2<T>(x[8 * j + 4], x[8 * j + 5]),
+                           pack2<T>(x[8 * j + 6], x[8 * j + 7]));
+        }
+        if (!sums(KIND) && c % 64 == 0 && n + 32 < w.N) continue;  // half a box so far
+        const int bx = (int)(sums(KIND) ? n : n - c % 64);
+        if (!sums(KIND) && w.out) {
+          __syncwarp();
+          for (int r = 0; r < 32 && m0 + r < w.M; ++r)
+            for (int j = lane; j < 64 && bx + j < w.N; j += 32)
+              static_cast<T*>(w.out)[(m0 + r) * w.out_stride + bx + j] =
+                  reinterpret_cast<const T*>(box_piece(box, r, j / 8))[j % 8];
+          __syncwarp();
+          continue;
+        }
+        tc::fence_async_smem();
+        __syncwarp();
+        if (lane == 0) {
+          if (!sums(KIND)) tc::tile_s2g(&map_out, bx, (int)m0, box);
+          else if (w.add) tc::tile_add_s2g(&map_out, bx, s.part * w.slot_rows + (int)m0, box);
+          else tc::tile_s2g(&map_out, bx, s.part * w.slot_rows + (int)m0, box);
+          tc::bulk_commit();
         }
       }
       tc::tc_fence_before();
       __syncwarp();
-      if (lane == 0) tc::mbar_arrive(&sh.acc_empty[buf]);
+      if (lane == 0) tc::mbar_arrive_cluster(empty_bar[buf]);
       ++n_acc;
-      if (KIND == kStats && last && live)
-        w.partial[(walk.unit_split() * 2 + half) * w.M + m] = make_float2(top, sum);
+      if (KIND == kStats && s.last && live)
+        w.partial[((int64_t)s.part * 2 + half) * w.M + m] = make_float2(top, sum);
     }
+    if (KIND != kStats && lane == 0) tc::bulk_wait();
   }
+  __syncwarp();
   tc::tc_fence_before();
   __syncthreads();
+  tc::cluster_sync();  // no CTA leaves while its pair may still signal or read it
   tc::tc_fence_after();
-  if (warp == 2) tc::tmem_dealloc(tmem, 512);
+  if (warp == 2) tc::tmem_dealloc_pair(tmem, 512);
 }
 
-// Joins a row's partial statistics: one warp per row.
+// Joins a row's partial statistics: one warp per row.  The sum's logarithm
+// and the differences are taken in 64 bits: lse and the target's logit are
+// several times the loss, and each would lose half an ulp of its own size.
 __global__ void __launch_bounds__(256)
 join_kernel(const float2* partial, int parts, const float* own, const int64_t* targets,
             int64_t ignore, int64_t rows, int64_t vocab, float* loss, float* lse, int* status) {
@@ -460,8 +552,6 @@ join_kernel(const float2* partial, int parts, const float* own, const int64_t* t
     const float ot = __shfl_xor_sync(0xffffffffu, top, k);
     const float os = __shfl_xor_sync(0xffffffffu, sum, k);
     const float now = fmaxf(top, ot), ref = now == -INFINITY ? 0.f : now;
-    // the same two terms on both sides of the exchange: commutative, so the
-    // order is the same in every lane
     sum = sum * tc::ex2(top - ref) + os * tc::ex2(ot - ref);
     top = now;
   }
@@ -471,45 +561,41 @@ join_kernel(const float2* partial, int parts, const float* own, const int64_t* t
     loss[n] = lse[n] = 0.f;
     return;
   }
-  const float l = fmaf(top, kLn2, logf(sum));
-  const float r = y >= 0 && y < vocab ? l - own[n] : NAN;
-  lse[n] = l;
+  const double l = (double)top * kLn2 + log((double)sum);
+  const float r = y >= 0 && y < vocab ? (float)(l - (double)own[n]) : NAN;
+  lse[n] = (float)l;
   loss[n] = isfinite(r) ? r : NAN;
   if (!isfinite(r)) atomicCAS(status, 0, SOMA_ERR_NONFINITE);
 }
 
-// Per row: what it takes part with, and a copy of h in rows of a multiple of
-// eight elements with the rows that take no part zeroed (their h may hold
-// anything, and 0 * NaN would reach demb).
+// Per row, one warp: what it takes part with, and a copy of h in rows of a
+// multiple of eight elements with the rows that take no part zeroed (their h
+// may hold anything, and 0 * NaN would reach demb).
 template <typename T>
-__global__ void __launch_bounds__(128)
-rows_kernel(const T* h, int64_t hs, int64_t dim, const int64_t* targets, int64_t ignore,
-            int64_t vocab, const float* lse, const float* dloss, RowInfo* info, T* copy,
-            int64_t cs, float* top) {
-  const int64_t n = blockIdx.x;
+__global__ void __launch_bounds__(256)
+rows_kernel(const T* h, soma_linear_ce_dims d, const int64_t* targets, int64_t ignore,
+            const float* lse, const float* dloss, RowInfo* info, T* copy, int64_t cs, float* top) {
+  const int64_t n = (int64_t)blockIdx.x * 8 + threadIdx.x / 32;
+  if (n >= d.rows) return;
+  const int lane = threadIdx.x % 32;
   const int64_t y = targets[n];
   const float l = lse[n];
-  const bool live = y != ignore && y >= 0 && y < vocab && isfinite(l);
-  if (threadIdx.x == 0) {
-    const float g = live ? dloss[n] : 0.f;
-    info[n] = {l * kLog2e, g, live ? y : -1};
-    // non-negative floats order as their bits do
-    if (top && isfinite(g)) atomicMax(reinterpret_cast<int*>(top), __float_as_int(fabsf(g)));
+  const bool live = y != ignore && y >= 0 && y < d.vocab && isfinite(l);
+  const bool vec = d.h_stride % 8 == 0;
+  for (int64_t j = lane * 8; j < cs; j += 256)
+    *reinterpret_cast<uint4*>(copy + n * cs + j) =
+        live ? row_piece(h + n * d.h_stride, j, d.dim, vec) : make_uint4(0u, 0u, 0u, 0u);
+  if (lane) return;
+  RowInfo r = {l * kLog2e, 0.f, 0.f, -1};
+  if (live) {
+    r.g = dloss[n];
+    r.y = (int32_t)y;
+    // non-negative floats order as their bits do; most rows need no atomic
+    const int bits = __float_as_int(fabsf(r.g));
+    if (top && isfinite(r.g) && bits > *reinterpret_cast<volatile int*>(top))
+      atomicMax(reinterpret_cast<int*>(top), bits);
   }
-  const bool vec = hs % 8 == 0;
-  for (int64_t j = threadIdx.x * 8; j < cs; j += 128 * 8) {
-    uint4 v = make_uint4(0u, 0u, 0u, 0u);
-    if (live) {
-      if (vec && j + 8 <= dim) {
-        v = *reinterpret_cast<const uint4*>(h + n * hs + j);
-      } else {
-        T t[8];
-        for (int k = 0; k < 8; ++k) t[k] = j + k < dim ? h[n * hs + j + k] : from_f32<T>(0.f);
-        memcpy(&v, t, 16);
-      }
-    }
-    *reinterpret_cast<uint4*>(copy + n * cs + j) = v;
-  }
+  info[n] = r;
 }
 
 // A matrix whose row stride is no multiple of eight, copied to rows that are.
@@ -521,26 +607,44 @@ pack_kernel(const T* x, int64_t xs, int64_t dim, T* copy, int64_t cs) {
     copy[n * cs + j] = j < dim ? x[n * xs + j] : from_f32<T>(0.f);
 }
 
-// dh from the fp32 sums: the slots of a row's tile in order.
+// The rows of dh (info) or demb (no info) from their fp32 sums, the slots in
+// order.  used = 0: the slots that the row's tile has (w's shares).
 template <typename T>
 __global__ void __launch_bounds__(128)
-dh_kernel(const float* acc, int64_t acc_stride, int64_t slot_stride, int slots, int per_tile,
-          Work w, int64_t dim, const RowInfo* info, const float* top, T* dh, int64_t ds) {
+sums_kernel(const float* acc, int64_t acc_stride, int used, const __grid_constant__ Work w,
+            const RowInfo* info, T* out, int64_t stride, int vec) {
   const int64_t n = blockIdx.x;
-  const bool live = info[n].y >= 0;
-  const float unscale = 1.f / g_scale<T>(*top);
-  const int64_t total = (int64_t)w.m_tiles * w.n_tiles * w.k_stages;
-  for (int64_t j = threadIdx.x; j < dim; j += 128) {
-    int used = slots;
-    if (per_tile) {  // one piece: only the slots that its tile has were written
-      const int64_t tile = n / kM * w.n_tiles + j / kN;
-      used = (int)(share_owner((tile + 1) * w.k_stages - 1, total, w.ctas) -
-                   share_owner(tile * w.k_stages, total, w.ctas)) + 1;
+  const float f = 1.f / g_scale<T>(*w.top);
+  if (!used) {
+    const int64_t total = (int64_t)w.m_tiles * w.k_stages, begin = n / kTile * w.k_stages;
+    used = (int)(share_owner(begin + w.k_stages - 1, total, w.groups) -
+                 share_owner(begin, total, w.groups)) + 1;
+  }
+  RowInfo r = {0.f, 0.f, 0.f, 0};
+  if (info) r = info[n];
+  const T* e = static_cast<const T*>(w.emb) + (r.y < 0 ? 0 : r.y) * w.emb_stride;
+  for (int64_t j = threadIdx.x * 4; j < w.N; j += 512) {
+    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (r.y >= 0) {
+      for (int k = 0; k < used; ++k) {
+        const float4 v = *reinterpret_cast<const float4*>(
+            acc + ((int64_t)k * w.slot_rows + n) * acc_stride + j);
+        x = make_float4(x.x + v.x, x.y + v.y, x.z + v.z, x.w + v.w);
+      }
+      if (info) {
+        float* o = &x.x;
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          if (j + k < w.N) o[k] = fmaf(r.rest, to_f32(e[j + k]), o[k]);
+      }
     }
-    float x = 0.f;
-    if (live)
-      for (int k = 0; k < used; ++k) x += acc[k * slot_stride + n * acc_stride + j];
-    dh[n * ds + j] = from_f32<T>(x * unscale);
+    T* p = out + n * stride + j;
+    if (vec && j + 4 <= w.N) {
+      *reinterpret_cast<uint2*>(p) = make_uint2(pack2<T>(x.x * f, x.y * f), pack2<T>(x.z * f, x.w * f));
+    } else {
+      const float v[4] = {x.x, x.y, x.z, x.w};
+      for (int k = 0; k < 4 && j + k < w.N; ++k) p[k] = from_f32<T>(v[k] * f);
+    }
   }
 }
 
@@ -557,32 +661,94 @@ bool dims_ok(const soma_linear_ce_dims& d) {
          (d.dtype == SOMA_BF16 || d.dtype == SOMA_FP16);
 }
 
-struct Plan {
-  int32_t splits;              // forward
-  int64_t piece;               // backward: vocabulary entries of one piece
-  int64_t g_stride, acc_stride, slots;
-  size_t h, emb, partial, own; // offsets; h, emb: copies (emb only where its stride asks for it)
-  size_t g, info, acc, top, total;
-};
+// Times of the backward call's parts, in units of a pair's stage (about 0.4 us
+// at the rate of a large product): what a launch costs besides its stages, and
+// the fp32 bytes that one unit reads or writes.
+constexpr int64_t kLaunchStages = 18;
+constexpr int64_t kBytesPerStage = 2700000;
 
-// Shares of the depth of dh's tiles.
-void share_plan(const soma_linear_ce_dims& d, int64_t width, Work* w) {
-  w->m_tiles = (int32_t)ceil_div(d.rows, kM);
-  w->n_tiles = (int32_t)ceil_div(d.dim, kN);
-  w->k_stages = (int32_t)ceil_div(width, tc::kDepth);
-  const int64_t total = (int64_t)w->m_tiles * w->n_tiles * w->k_stages;
-  w->ctas = (int32_t)(total < kSms ? total : kSms);
+// M x N sums over a depth, cut into shares.
+Work shares(int64_t M, int64_t N, int64_t depth) {
+  Work w = {};
+  w.M = M;
+  w.N = N;
+  w.m_tiles = (int32_t)ceil_div(M, kTile);
+  w.n_tiles = (int32_t)ceil_div(N, kTile);
+  w.k_stages = (int32_t)ceil_div(depth, tc::kDepth);
+  w.columns = w.n_tiles < kPairs ? w.n_tiles : kPairs;
+  const int64_t total = (int64_t)w.m_tiles * w.k_stages;
+  w.groups = (int32_t)(total < kPairs / w.columns ? total : kPairs / w.columns);
+  w.pairs = w.groups * w.columns;
+  w.slot_rows = w.m_tiles * kTile;
+  return w;
 }
 
 // Slots that a tile can need: its depth touches at most this many shares.
 int64_t slots_of(const Work& w) {
-  const int64_t total = (int64_t)w.m_tiles * w.n_tiles * w.k_stages;
-  const int64_t share = total / w.ctas;
+  const int64_t share = (int64_t)w.m_tiles * w.k_stages / w.groups;
   const int64_t n = ceil_div(w.k_stages, share) + 1;
-  return n < w.ctas ? n : w.ctas;
+  return n < w.groups ? n : w.groups;
 }
 
-Plan plan(const soma_linear_ce_dims& d, bool backward) {
+int64_t sums_cost(const Work& w, bool add) {
+  const int64_t bytes = (int64_t)w.M * w.N * 4;
+  return ceil_div((int64_t)w.m_tiles * w.k_stages, w.groups) * ceil_div(w.n_tiles, w.columns) +
+         kLaunchStages + bytes * (add ? 2 : 1) / kBytesPerStage;
+}
+int64_t tiles_cost(int64_t M, int64_t N, int64_t depth) {
+  return ceil_div(ceil_div(M, kTile) * ceil_div(N, kTile), kPairs) * ceil_div(depth, tc::kDepth) +
+         kLaunchStages;
+}
+
+struct Plan {
+  int32_t splits;                // forward
+  int64_t piece;                 // backward: vocabulary entries of one piece
+  bool dh_sums, demb_sums;       // which kernels the products take
+  int64_t g_stride, acc_stride, dh_slots, demb_slots;
+  size_t h, emb, partial, own;   // offsets; h, emb: copies (emb only where its stride asks for it)
+  size_t g, info, dh_acc, demb_acc, top, total;
+};
+
+// The backward call's pieces: as few as G's share of the workspace allows, or
+// somewhat more where the tiles then fill the last round of pairs better.
+void plan_pieces(const soma_linear_ce_dims& d, Plan* p) {
+  int64_t most = (int64_t)(kPieceBytes / 2) / d.rows / kTile * kTile;
+  if (most < kTile) most = kTile;
+  const int64_t fewest = ceil_div(d.vocab, most);
+  int64_t best = INT64_MAX;
+  for (int64_t n = fewest; n < fewest + 24; ++n) {
+    int64_t width = n == 1 ? d.vocab : ceil_div(ceil_div(d.vocab, n), kTile) * kTile;
+    if (width > d.vocab) width = d.vocab;
+    const int64_t full = d.vocab / width, rest = d.vocab % width;
+    const bool one = full == 1 && !rest;
+    int64_t cost = 0;
+    bool dh_sums = true, demb_sums = false;
+    for (int64_t w : {width, rest}) {
+      if (!w) continue;
+      const int64_t dh_by_sums =
+          sums_cost(shares(d.rows, d.dim, w), !one) + (one ? kLaunchStages : 0);
+      const int64_t dh_by_tiles = tiles_cost(d.rows, d.dim, w);
+      int64_t demb = tiles_cost(w, d.dim, d.rows);
+      if (one) {
+        dh_sums = dh_by_sums < dh_by_tiles;
+        const int64_t by_sums = sums_cost(shares(w, d.dim, d.rows), false) + kLaunchStages;
+        demb_sums = by_sums < demb;
+        if (demb_sums) demb = by_sums;
+      }
+      cost += (w == width ? full : 1) *
+              (tiles_cost(d.rows, w, d.dim) + demb + (dh_sums ? dh_by_sums : dh_by_tiles));
+    }
+    if (cost < best) {
+      best = cost;
+      p->piece = width;
+      p->dh_sums = dh_sums;
+      p->demb_sums = demb_sums;
+    }
+    if (width == kTile) break;
+  }
+}
+
+Plan plan(soma_linear_ce_dims d, bool backward) {
   Plan p = {};
   size_t at = 0;
   const auto take = [&](size_t bytes) {
@@ -590,39 +756,40 @@ Plan plan(const soma_linear_ce_dims& d, bool backward) {
     at += round256(bytes);
     return o;
   };
-  const int64_t rows = d.rows ? d.rows : 1;
-  if (backward || d.h_stride % 8) p.h = take((size_t)rows * round8(d.dim) * 2);
+  if (!d.rows) d.rows = 1;
+  if (backward || d.h_stride % 8) p.h = take((size_t)d.rows * round8(d.dim) * 2);
   if (d.emb_stride % 8) p.emb = take((size_t)d.vocab * round8(d.dim) * 2);
-  const int64_t mt = ceil_div(rows, kM), vt = ceil_div(d.vocab, kN);
   if (!backward) {
-    // rounds of CTAs times the tiles of a unit, least first
+    // rounds of pairs times the tiles of a unit, least first
+    const int64_t mt = ceil_div(d.rows, kTile), vt = ceil_div(d.vocab, kTile);
     int64_t best = INT64_MAX;
-    for (int64_t s = 1; s <= vt && s <= 4 * kSms; ++s) {
-      const int64_t cost = ceil_div(mt * s, kSms) * ceil_div(vt, s);
+    for (int64_t s = 1; s <= vt && s <= 4 * kPairs; ++s) {
+      const int64_t cost = ceil_div(mt * s, kPairs) * ceil_div(vt, s);
       if (cost < best) {
         best = cost;
         p.splits = (int32_t)s;
       }
     }
-    p.partial = take((size_t)rows * 2 * p.splits * sizeof(float2));
-    p.own = take((size_t)rows * 4);
+    p.partial = take((size_t)d.rows * 2 * p.splits * sizeof(float2));
+    p.own = take((size_t)d.rows * 4);
   } else {
-    p.piece = (int64_t)(kPieceBytes / 2) / rows / kN * kN;
-    if (p.piece < kN) p.piece = kN;
-    if (p.piece > d.vocab) p.piece = d.vocab;
-    p.g_stride = ceil_div(p.piece, kN) * kN;
+    plan_pieces(d, &p);
+    p.g_stride = round8(p.piece);
     p.acc_stride = ceil_div(d.dim, 4) * 4;
-    p.g = take((size_t)rows * p.g_stride * 2);
-    p.info = take((size_t)rows * sizeof(RowInfo));
-    soma_linear_ce_dims one = d;
-    one.rows = rows;
-    Work w = {};
-    for (int64_t width : {p.piece, d.vocab - (d.vocab - 1) / p.piece * p.piece}) {
-      share_plan(one, width, &w);
-      const int64_t n = slots_of(w);
-      if (n > p.slots) p.slots = n;
+    p.g = take((size_t)d.rows * p.g_stride * 2);
+    p.info = take((size_t)d.rows * sizeof(RowInfo));
+    if (p.dh_sums) {
+      for (int64_t width : {p.piece, d.vocab % p.piece}) {
+        if (!width) continue;
+        const int64_t n = slots_of(shares(d.rows, d.dim, width));
+        if (n > p.dh_slots) p.dh_slots = n;
+      }
+      p.dh_acc = take((size_t)p.dh_slots * ceil_div(d.rows, kTile) * kTile * p.acc_stride * 4);
     }
-    p.acc = take((size_t)p.slots * rows * p.acc_stride * 4);
+    if (p.demb_sums) {
+      p.demb_slots = slots_of(shares(d.vocab, d.dim, d.rows));
+      p.demb_acc = take((size_t)p.demb_slots * ceil_div(d.vocab, kTile) * kTile * p.acc_stride * 4);
+    }
     p.top = take(4);
   }
   p.total = at;
@@ -631,19 +798,20 @@ Plan plan(const soma_linear_ce_dims& d, bool backward) {
 
 bool aligned(const void* p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
 
+template <typename T>
+constexpr int dtype_of() { return std::is_same<T, __half>::value ? SOMA_FP16 : SOMA_BF16; }
+
+// A launch of `units` units, or of w.pairs pairs (sums).
 template <int KIND, typename T>
-cudaError_t launch(const CUtensorMap& a, const CUtensorMap& b, Work w, int64_t units, int* status,
-                   cudaStream_t st) {
+cudaError_t launch(const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& out, Work w,
+                   int64_t units, int* status, cudaStream_t st) {
   const cudaError_t ready = cudaFuncSetAttribute(
       product_kernel<KIND, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem);
   if (ready != cudaSuccess) return ready;
-  if (KIND != kDh) w.ctas = (int32_t)(units < kSms ? units : kSms);
-  product_kernel<KIND, T><<<w.ctas, kThreads, kSmem, st>>>(a, b, w, status);
+  if (!sums(KIND)) w.pairs = (int32_t)(units < kPairs ? units : kPairs);
+  product_kernel<KIND, T><<<2 * w.pairs, kThreads, kSmem, st>>>(a, b, out, w, status);
   return cudaGetLastError();
 }
-
-template <typename T>
-constexpr bool is_bf16() { return !std::is_same<T, __half>::value; }
 
 template <typename T>
 cudaError_t forward(const T* h, const T* emb, const soma_linear_ce_dims& d, const int64_t* targets,
@@ -664,12 +832,12 @@ cudaError_t forward(const T* h, const T* emb, const soma_linear_ce_dims& d, cons
     es = round8(d.dim);
   }
   CUtensorMap ma, mb;
-  if (!make_tile_map(&ma, h, is_bf16<T>(), d.rows, d.dim, hs, kM) ||
-      !make_tile_map(&mb, emb, is_bf16<T>(), d.vocab, d.dim, es, kN))
+  if (!make_tile_map(&ma, h, dtype_of<T>(), d.rows, d.dim, hs, kHalf) ||
+      !make_tile_map(&mb, emb, dtype_of<T>(), d.vocab, d.dim, es, kHalf))
     return cudaErrorInvalidValue;
   Work w = {};
-  w.m_tiles = (int32_t)ceil_div(d.rows, kM);
-  w.n_tiles = (int32_t)ceil_div(d.vocab, kN);
+  w.m_tiles = (int32_t)ceil_div(d.rows, kTile);
+  w.n_tiles = (int32_t)ceil_div(d.vocab, kTile);
   w.k_stages = (int32_t)ceil_div(d.dim, tc::kDepth);
   w.splits = p.splits;
   w.M = d.rows;
@@ -678,7 +846,7 @@ cudaError_t forward(const T* h, const T* emb, const soma_linear_ce_dims& d, cons
   w.partial = reinterpret_cast<float2*>(ws + p.partial);
   w.own = reinterpret_cast<float*>(ws + p.own);
   const cudaError_t e =
-      launch<kStats, T>(ma, mb, w, (int64_t)w.m_tiles * w.splits, status, st);
+      launch<kStats, T>(ma, mb, ma, w, (int64_t)w.m_tiles * w.splits, status, st);
   if (e != cudaSuccess) return e;
   join_kernel<<<(unsigned)ceil_div(d.rows, 8), 256, 0, st>>>(w.partial, 2 * p.splits, w.own,
                                                              targets, ignore, d.rows, d.vocab,
@@ -694,18 +862,19 @@ cudaError_t backward(const T* h, const T* emb, const soma_linear_ce_dims& d,
   if (d.rows == 0)
     return cudaMemset2DAsync(demb, des * 2, 0, d.dim * 2, d.vocab, st);
   const Plan p = plan(d, true);
+  constexpr int dtype = dtype_of<T>();
   RowInfo* info = reinterpret_cast<RowInfo*>(ws + p.info);
   T* copy = reinterpret_cast<T*>(ws + p.h);
   T* G = reinterpret_cast<T*>(ws + p.g);
   float* top = reinterpret_cast<float*>(ws + p.top);
-  float* acc = reinterpret_cast<float*>(ws + p.acc);
+  float* dh_acc = reinterpret_cast<float*>(ws + p.dh_acc);
+  float* demb_acc = reinterpret_cast<float*>(ws + p.demb_acc);
   const int64_t cs = round8(d.dim);
   int64_t es = d.emb_stride;
   cudaError_t e = cudaMemsetAsync(top, 0, 4, st);
   if (e != cudaSuccess) return e;
-  rows_kernel<T><<<(unsigned)d.rows, 128, 0, st>>>(h, d.h_stride, d.dim, targets, ignore, d.vocab,
-                                                   lse, dloss, info, copy, cs,
-                                                   is_bf16<T>() ? nullptr : top);
+  rows_kernel<T><<<(unsigned)ceil_div(d.rows, 8), 256, 0, st>>>(
+      h, d, targets, ignore, lse, dloss, info, copy, cs, dtype == SOMA_FP16 ? top : nullptr);
   if (es % 8) {
     T* packed = reinterpret_cast<T*>(ws + p.emb);
     pack_kernel<T><<<(unsigned)d.vocab, 128, 0, st>>>(emb, es, d.dim, packed, cs);
@@ -713,69 +882,91 @@ cudaError_t backward(const T* h, const T* emb, const soma_linear_ce_dims& d,
     es = cs;
   }
   const bool many = p.piece < d.vocab;
+  const bool dh_tiled = dhs % 8 == 0 && aligned(dh, 16);
+  const bool demb_tiled = des % 8 == 0 && aligned(demb, 16);
+  CUtensorMap h_k, h_mn, e_k, e_mn, dh_out, demb_sum;
+  bool ok = make_tile_map(&h_k, copy, dtype, d.rows, d.dim, cs, kHalf) &&
+            make_tile_map(&h_mn, copy, dtype, d.rows, d.dim, cs, 64) &&
+            make_tile_map(&e_k, emb, dtype, d.vocab, d.dim, es, kHalf) &&
+            make_tile_map(&e_mn, emb, dtype, d.vocab, d.dim, es, 64);
+  if (p.dh_sums)
+    ok = ok && make_tile_map(&dh_out, dh_acc, SOMA_FP32,
+                             p.dh_slots * ceil_div(d.rows, kTile) * kTile, p.acc_stride,
+                             p.acc_stride, 32);
+  else if (dh_tiled)
+    ok = ok && make_tile_map(&dh_out, dh, dtype, d.rows, d.dim, dhs, 32);
+  else
+    dh_out = h_k;  // not used
+  if (p.demb_sums)
+    ok = ok && make_tile_map(&demb_sum, demb_acc, SOMA_FP32,
+                             p.demb_slots * ceil_div(d.vocab, kTile) * kTile, p.acc_stride,
+                             p.acc_stride, 32);
+  if (!ok) return cudaErrorInvalidValue;
   if (many) {
-    e = cudaMemsetAsync(acc, 0, (size_t)p.slots * d.rows * p.acc_stride * 4, st);
+    e = cudaMemsetAsync(dh_acc, 0,
+                        (size_t)p.dh_slots * ceil_div(d.rows, kTile) * kTile * p.acc_stride * 4, st);
     if (e != cudaSuccess) return e;
   }
-  CUtensorMap h_k, h_mn, e_k, e_mn;
-  if (!make_tile_map(&h_k, copy, is_bf16<T>(), d.rows, d.dim, cs, kM) ||
-      !make_tile_map(&h_mn, copy, is_bf16<T>(), d.rows, d.dim, cs, 64) ||
-      !make_tile_map(&e_k, emb, is_bf16<T>(), d.vocab, d.dim, es, kN) ||
-      !make_tile_map(&e_mn, emb, is_bf16<T>(), d.vocab, d.dim, es, 64))
-    return cudaErrorInvalidValue;
-  Work dhw = {};
   for (int64_t v0 = 0; v0 < d.vocab; v0 += p.piece) {
     const int64_t width = d.vocab - v0 < p.piece ? d.vocab - v0 : p.piece;
-    CUtensorMap g_k, g_mn;
-    if (!make_tile_map(&g_k, G, is_bf16<T>(), d.rows, width, p.g_stride, kM) ||
-        !make_tile_map(&g_mn, G, is_bf16<T>(), d.rows, width, p.g_stride, 64))
+    CUtensorMap g_k, g_mn, g_out, demb_out = h_k;
+    if (!make_tile_map(&g_k, G, dtype, d.rows, width, p.g_stride, kHalf) ||
+        !make_tile_map(&g_mn, G, dtype, d.rows, width, p.g_stride, 64) ||
+        !make_tile_map(&g_out, G, dtype, d.rows, width, p.g_stride, 32) ||
+        (demb_tiled && !p.demb_sums &&
+         !make_tile_map(&demb_out, demb + v0 * des, dtype, width, d.dim, des, 32)))
       return cudaErrorInvalidValue;
     Work w = {};
-    w.m_tiles = (int32_t)ceil_div(d.rows, kM);
-    w.n_tiles = (int32_t)ceil_div(width, kN);
-    w.k_stages = (int32_t)ceil_div(d.dim, tc::kDepth);
     w.M = d.rows;
     w.N = width;
+    w.m_tiles = (int32_t)ceil_div(w.M, kTile);
+    w.n_tiles = (int32_t)ceil_div(w.N, kTile);
+    w.k_stages = (int32_t)ceil_div(d.dim, tc::kDepth);
     w.y_b = (int32_t)v0;
     w.info = info;
-    w.out = G;
-    w.out_stride = p.g_stride;
     w.v0 = v0;
     w.top = top;
-    e = launch<kGrad, T>(h_k, e_k, w, (int64_t)w.m_tiles * w.n_tiles, status, st);
+    e = launch<kGrad, T>(h_k, e_k, g_out, w, (int64_t)w.m_tiles * w.n_tiles, status, st);
     if (e != cudaSuccess) return e;
 
-    w = {};
-    share_plan(d, width, &w);
-    w.M = d.rows;
-    w.N = d.dim;
+    w = shares(d.rows, d.dim, width);
     w.y_b = (int32_t)v0;
-    w.acc = acc;
-    w.acc_stride = p.acc_stride;
-    w.slot_stride = d.rows * p.acc_stride;
-    w.add = many;
+    w.info = info;
+    w.emb = emb;
+    w.emb_stride = es;
     w.top = top;
-    dhw = w;
-    e = launch<kDh, T>(g_k, e_mn, w, 0, status, st);
+    if (p.dh_sums) {
+      w.add = many;
+      e = launch<kDhSums, T>(g_k, e_mn, dh_out, w, 0, status, st);
+      if (e == cudaSuccess && v0 + width == d.vocab) {
+        sums_kernel<T><<<(unsigned)d.rows, 128, 0, st>>>(
+            dh_acc, p.acc_stride, many ? (int)p.dh_slots : 0, w, info, dh, dhs,
+            dhs % 4 == 0 && aligned(dh, 8));
+        e = cudaGetLastError();
+      }
+    } else {
+      w.out = dh_tiled ? nullptr : dh;
+      w.out_stride = dhs;
+      e = launch<kDh, T>(g_k, e_mn, dh_out, w, (int64_t)w.m_tiles * w.n_tiles, status, st);
+    }
     if (e != cudaSuccess) return e;
 
-    w = {};
-    w.m_tiles = (int32_t)ceil_div(width, kM);
-    w.n_tiles = (int32_t)ceil_div(d.dim, kN);
-    w.k_stages = (int32_t)ceil_div(d.rows, tc::kDepth);
-    w.M = width;
-    w.N = d.dim;
-    w.out = demb + v0 * des;
-    w.out_stride = des;
-    w.vec = des % 8 == 0 && aligned(demb, 16);
+    w = shares(width, d.dim, d.rows);
     w.top = top;
-    e = launch<kDemb, T>(g_mn, h_mn, w, (int64_t)w.m_tiles * w.n_tiles, status, st);
+    if (p.demb_sums) {
+      e = launch<kDembSums, T>(g_mn, h_mn, demb_sum, w, 0, status, st);
+      if (e != cudaSuccess) return e;
+      sums_kernel<T><<<(unsigned)d.vocab, 128, 0, st>>>(demb_acc, p.acc_stride, 0, w, nullptr,
+                                                        demb, des, des % 4 == 0 && aligned(demb, 8));
+      e = cudaGetLastError();
+    } else {
+      w.out = demb_tiled ? nullptr : demb + v0 * des;
+      w.out_stride = des;
+      e = launch<kDemb, T>(g_mn, h_mn, demb_out, w, (int64_t)w.m_tiles * w.n_tiles, status, st);
+    }
     if (e != cudaSuccess) return e;
   }
-  dh_kernel<T><<<(unsigned)d.rows, 128, 0, st>>>(acc, p.acc_stride, d.rows * p.acc_stride,
-                                                 (int)p.slots, !many, dhw, d.dim, info, top, dh,
-                                                 dhs);
-  return cudaGetLastError();
+  return cudaSuccess;
 }
 
 }  // namespace

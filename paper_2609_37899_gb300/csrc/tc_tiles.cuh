@@ -5,8 +5,8 @@
 // A stage of an operand is made of boxes of 64 columns (128 bytes) by some
 // rows of the matrix in memory, each row 128 bytes further, the 16-byte pieces
 // of a row permuted by the row's index modulo 8 (the 128-byte swizzle).
-//  - K-major (the columns are the product's depth): one box of 128 or 256
-//    rows; eight rows lie 1024 bytes apart from the next eight.
+//  - K-major (the columns are the product's depth): one box of 128 rows; eight
+//    rows lie 1024 bytes apart from the next eight.
 //  - MN-major (the columns are the operand's rows): one box of 64 rows per 64
 //    columns; the depth runs over the box's rows.
 #pragma once
@@ -24,14 +24,107 @@ constexpr int kBoxCols = 64;                // 16-bit elements of one swizzled r
 constexpr int kDepth = 64;                  // depth of one stage
 constexpr uint32_t kBoxBytes = 64 * 128;    // an MN-major box
 
-// 2-D tiled copy of one box at (x, y) = (column, row).
-__device__ __forceinline__ void tile_g2s(void* smem_dst, const CUtensorMap* map, int x, int y,
-                                         uint64_t* bar) {
+// ---- CTA pairs ------------------------------------------------------------
+// Two CTAs of a cluster multiply one 256-row tile: each stages 128 rows of A
+// and half of B's rows, the even one issues the products for both, and each
+// accumulates its own 128 rows.
+__device__ __forceinline__ uint32_t pair_rank() {
+  uint32_t r;
+  asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+
+// Cluster address of the even CTA's shared variable at the same place as *p.
+__device__ __forceinline__ uint32_t leader_addr(const void* p) {
+  uint32_t r;
+  asm("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(smem_u32(p)));
+  return r;
+}
+
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.aligned;\n barrier.cluster.wait.aligned;" ::: "memory");
+}
+
+// Arrives on a barrier given by its cluster address.
+__device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar) {
+  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar)
+               : "memory");
+}
+
+// 2-D tiled copy of one box at (x, y) = (column, row) into this CTA's shared
+// memory; the bytes are counted on the barrier at the cluster address `bar`.
+__device__ __forceinline__ void tile_g2s_pair(void* smem_dst, const CUtensorMap* map, int x, int y,
+                                              uint32_t bar) {
   asm volatile(
-      "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
-      " [%0], [%1, {%2, %3}], [%4];" ::"r"(smem_u32(smem_dst)),
-      "l"(map), "r"(x), "r"(y), "r"(smem_u32(bar))
+      "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile"
+      ".mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(smem_u32(smem_dst)),
+      "l"(map), "r"(x), "r"(y), "r"(bar)
       : "memory");
+}
+
+__device__ __forceinline__ void tmem_alloc_pair(uint32_t* slot, uint32_t ncols) {
+  asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(
+                   smem_u32(slot)),
+               "r"(ncols)
+               : "memory");
+  asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+}
+
+__device__ __forceinline__ void tmem_dealloc_pair(uint32_t taddr, uint32_t ncols) {
+  asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(taddr), "r"(ncols)
+               : "memory");
+}
+
+// D[tmem of both] (+)= A * B^T with operands in both CTAs' shared memory.
+__device__ __forceinline__ void mma_f16_ss_pair(uint32_t d_tmem, uint32_t a_lo, uint32_t b_lo,
+                                                uint32_t desc_hi, uint32_t idesc,
+                                                uint32_t accumulate) {
+  asm volatile(
+      "{\n .reg .pred p;\n .reg .b64 da, db;\n setp.ne.b32 p, %5, 0;\n"
+      " mov.b64 da, {%1, %3};\n mov.b64 db, {%2, %3};\n"
+      " tcgen05.mma.cta_group::2.kind::f16 [%0], da, db, %4, p;\n}" ::"r"(d_tmem),
+      "r"(a_lo), "r"(b_lo), "r"(desc_hi), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+
+// Arrive on *bar of both CTAs once every tcgen05.mma of this thread so far
+// has completed.
+__device__ __forceinline__ void mma_commit_pair(uint64_t* bar) {
+  asm volatile(
+      "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64"
+      " [%0], %1;" ::"r"(smem_u32(bar)),
+      "h"((uint16_t)3)
+      : "memory");
+}
+
+// ---- tiled stores ---------------------------------------------------------
+__device__ __forceinline__ void tile_s2g(const CUtensorMap* map, int x, int y, const void* src) {
+  asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];" ::
+                   "l"(map),
+               "r"(x), "r"(y), "r"(smem_u32(src))
+               : "memory");
+}
+
+// Adds the fp32 box to memory.
+__device__ __forceinline__ void tile_add_s2g(const CUtensorMap* map, int x, int y,
+                                             const void* src) {
+  asm volatile(
+      "cp.reduce.async.bulk.tensor.2d.global.shared::cta.add.tile.bulk_group [%0, {%1, %2}], "
+      "[%3];" ::"l"(map),
+      "r"(x), "r"(y), "r"(smem_u32(src))
+      : "memory");
+}
+
+__device__ __forceinline__ void bulk_commit() {
+  asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+}
+// This thread's committed stores have read their shared memory.
+__device__ __forceinline__ void bulk_wait_read() {
+  asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+}
+// ... and have been made.
+__device__ __forceinline__ void bulk_wait() {
+  asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
 }
 
 __device__ __forceinline__ void prefetch_map(const CUtensorMap* map) {
@@ -82,11 +175,11 @@ __device__ __forceinline__ float ex2(float x) {
 
 }  // namespace tc
 
-// Tensor map of a row-major 16-bit matrix [rows][cols], `stride` elements
-// between rows, read in boxes of 64 columns by box_rows rows.  The address
-// must be 16-byte aligned and the stride a multiple of 8.  What lies outside
-// the matrix reads as zero.
-bool make_tile_map(CUtensorMap* map, const void* base, bool bf16, int64_t rows, int64_t cols,
+// Tensor map of a row-major matrix [rows][cols] of a soma_dtype, `stride`
+// elements between rows, in boxes of 128 bytes of columns by box_rows rows.
+// The address must be 16-byte aligned and the stride a multiple of 16 bytes.
+// What lies outside the matrix reads as zero and is not written.
+bool make_tile_map(CUtensorMap* map, const void* base, int dtype, int64_t rows, int64_t cols,
                    int64_t stride, int box_rows);
 
 }  // namespace soma
