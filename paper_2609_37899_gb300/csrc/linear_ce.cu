@@ -69,7 +69,7 @@ constexpr size_t kSmem =                      // and what aligns the stages
     kStages * kStageBytes + kEpilogueWarps * kOutBytes + 1024;
 constexpr size_t kPieceBytes = (size_t)256 << 20;  // of G of one piece, at most
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr double kLn2 = 0.69314718055994530942;
+constexpr float kLn2 = 0.6931471805599453f;
 
 enum Kind { kStats, kGrad, kDemb, kDh, kDembSums, kDhSums };
 __host__ __device__ constexpr bool a_mn(int kind) { return kind == kDemb || kind == kDembSums; }
@@ -215,14 +215,14 @@ struct Shared {
   volatile int abort;
 };
 
-// A bounded wait; on running out it records the timeout and raises the CTA's
-// abort flag.
+// A bounded wait of a whole warp, with one answer for all its lanes; on
+// running out it records the timeout and raises the CTA's abort flag.
 __device__ __forceinline__ bool wait_or_abort(uint64_t* bar, uint32_t parity, Shared* sh,
                                               int* status, uint32_t max_polls = 1u << 22) {
-  if (sh->abort) return false;
-  if (tc::mbar_wait(bar, parity, max_polls)) return true;
+  const bool ok = !sh->abort && tc::mbar_wait(bar, parity, max_polls);
+  if (__all_sync(0xffffffffu, ok)) return true;
+  if (!sh->abort) atomicCAS(status, 0, SOMA_ERR_TIMEOUT);
   sh->abort = 1;
-  atomicCAS(status, 0, SOMA_ERR_TIMEOUT);
   return false;
 }
 
@@ -295,44 +295,41 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
   Span s;
 
   if (warp == 0) {
-    // loader: this CTA's halves of A and B; both CTAs' bytes count on the even
-    // CTA's barrier
-    if (lane == 0) {
-      uint32_t it = 0;
-      bool ok = true;
-      while (ok && walk.next(s, pair)) {
-        const int m0 = s.m * kTile + (int)rank * kHalf, n0 = s.n * kTile + (int)rank * kHalf;
-        for (int k = s.k0; k < s.k1; ++k, ++it) {
-          const uint32_t slot = it % kStages, round = it / kStages;
-          if (!wait_or_abort(&sh.empty[slot], (round & 1) ^ 1, &sh, status)) {
-            ok = false;
-            break;
-          }
-          uint8_t* a = stages + slot * kStageBytes;
-          uint8_t* b = a + kOperandBytes;
-          if (rank == 0) tc::mbar_arrive_expect_tx(&sh.full[slot], 2 * kStageBytes);
-          const uint32_t bar = tc::leader_addr(&sh.full[slot]);
+    // loader: lanes 0 and 1 copy this CTA's half of A, lanes 2 and 3 that of B,
+    // in one instruction (boxes of several lanes are fetched at once, those of
+    // consecutive instructions one after another).  A K-major half is one box
+    // (two of 64 rows took 10% longer), an MN-major one two.  Both CTAs' bytes
+    // count on the even CTA's barrier.
+    const bool is_b = lane >= 2;
+    const int sub = (lane & 1) * 64;
+    const CUtensorMap* map = is_b ? &map_b : &map_a;
+    const bool mn = is_b ? b_mn(KIND) : a_mn(KIND);
+    const bool copies = lane < 4 && (mn || !sub);
+    const int y0 = is_b ? w.y_b : 0;
+    uint32_t it = 0;
+    bool ok = true;
+    while (ok && walk.next(s, pair)) {
+      const int r0 = (is_b ? s.n : s.m) * kTile + (int)rank * kHalf + sub;
+      for (int k = s.k0; k < s.k1; ++k, ++it) {
+        const uint32_t slot = it % kStages, round = it / kStages;
+        if (!wait_or_abort(&sh.empty[slot], (round & 1) ^ 1, &sh, status)) {
+          ok = false;
+          break;
+        }
+        if (rank == 0 && lane == 0) tc::mbar_arrive_expect_tx(&sh.full[slot], 2 * kStageBytes);
+        __syncwarp();
+        if (copies) {
           const int kx = k * tc::kDepth;
-          if (a_mn(KIND)) {
-            for (int j = 0; j < kHalf / 64; ++j)
-              tc::tile_g2s_pair(a + j * tc::kBoxBytes, &map_a, m0 + j * 64, kx, bar);
-          } else {
-            tc::tile_g2s_pair(a, &map_a, kx, m0, bar);
-          }
-          if (b_mn(KIND)) {
-            for (int j = 0; j < kHalf / 64; ++j)
-              tc::tile_g2s_pair(b + j * tc::kBoxBytes, &map_b, n0 + j * 64, w.y_b + kx, bar);
-          } else {
-            tc::tile_g2s_pair(b, &map_b, kx, w.y_b + n0, bar);
-          }
+          tc::tile_g2s_pair(stages + slot * kStageBytes + lane * tc::kBoxBytes, map,
+                            mn ? r0 : kx, y0 + (mn ? kx : r0), tc::leader_addr(&sh.full[slot]));
         }
       }
-      // an aborting CTA leaves only after its copies have landed (the even
-      // CTA's barriers count both CTAs' copies)
-      if (!ok && rank == 0)
-        for (uint32_t j = it > kStages ? it - kStages : 0; j < it; ++j)
-          tc::mbar_wait(&sh.full[j % kStages], (j / kStages) & 1);
     }
+    // an aborting CTA leaves only after its copies have landed (the even
+    // CTA's barriers count both CTAs' copies)
+    if (!ok && rank == 0)
+      for (uint32_t j = it > kStages ? it - kStages : 0; j < it; ++j)
+        tc::mbar_wait(&sh.full[j % kStages], (j / kStages) & 1);
   } else if (warp == 1 && rank == 0) {
     // MMA issuer of the pair: the whole warp waits, one elected thread issues
     constexpr uint32_t idesc =
@@ -423,36 +420,37 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             for (int j = 0; j < 32; ++j)
               if (n + j >= w.N) x[j] = -INFINITY;
           }
-          float mx = x[0];
+          // four chains each: one would wait for itself
+          float mx[4] = {x[0], x[1], x[2], x[3]};
 #pragma unroll
-          for (int j = 1; j < 32; ++j) mx = fmaxf(mx, x[j]);
-          const float now = fmaxf(top, mx * kLog2e);
+          for (int j = 4; j < 32; ++j) mx[j % 4] = fmaxf(mx[j % 4], x[j]);
+          const float now =
+              fmaxf(top, fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * kLog2e);
           const float ref = now == -INFINITY ? 0.f : now;
-          float t = 0.f;
+          float t[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int j = 0; j < 32; ++j) t += tc::ex2(fmaf(x[j], kLog2e, -ref));
-          sum = fmaf(sum, tc::ex2(top - ref), t);
+          for (int j = 0; j < 32; ++j) t[j % 4] += tc::ex2(fmaf(x[j], kLog2e, -ref));
+          sum = fmaf(sum, tc::ex2(top - ref), (t[0] + t[1]) + (t[2] + t[3]));
           top = now;
           continue;
-        }
-        // the last box has been read before this one is written
-        const bool new_box = sums(KIND) || c % 64 == 0;
-        if (new_box) {
-          if (lane == 0) tc::bulk_wait_read();
-          __syncwarp();
         }
         if (KIND == kGrad) {
           if (info.y >= 0) {
             const int64_t hit = info.y - w.v0 - n;
             const float g = scale * info.g;
-#pragma unroll
-            for (int j = 0; j < 32; ++j)
-              x[j] = g * (tc::ex2(fmaf(x[j], kLog2e, -info.lse2)) - (j == hit ? 1.f : 0.f));
             if (hit >= 0 && hit < 32) {
-              float v = 0.f;
+              const int at = (int)hit;
+              float rest = 0.f;
 #pragma unroll
-              for (int j = 0; j < 32; ++j) v = j == hit ? x[j] : v;
-              w.info[m].rest = v - to_f32(from_f32<T>(v));
+              for (int j = 0; j < 32; ++j) {
+                const float p = tc::ex2(fmaf(x[j], kLog2e, -info.lse2));
+                x[j] = g * (j == at ? p - 1.f : p);
+                rest = j == at ? x[j] - to_f32(from_f32<T>(x[j])) : rest;
+              }
+              w.info[m].rest = rest;
+            } else {
+#pragma unroll
+              for (int j = 0; j < 32; ++j) x[j] = g * tc::ex2(fmaf(x[j], kLog2e, -info.lse2));
             }
           } else {
 #pragma unroll
@@ -479,6 +477,10 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
               o = info.y >= 0 ? scale * fmaf(info.rest, to_f32(v.t[k]), o) : 0.f;
             }
           }
+        }
+        if (sums(KIND) || c % 64 == 0) {  // the last box has been read before this is written
+          if (lane == 0) tc::bulk_wait_read();
+          __syncwarp();
         }
         if (sums(KIND)) {
 #pragma unroll
@@ -531,9 +533,9 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
   if (warp == 2) tc::tmem_dealloc_pair(tmem, 512);
 }
 
-// Joins a row's partial statistics: one warp per row.  The sum's logarithm
-// and the differences are taken in 64 bits: lse and the target's logit are
-// several times the loss, and each would lose half an ulp of its own size.
+// Joins a row's partial statistics: one warp per row.  lse and the target's
+// logit are several times the loss: their difference is taken before the small
+// terms are added, so that it does not lose half an ulp of their size.
 __global__ void __launch_bounds__(256)
 join_kernel(const float2* partial, int parts, const float* own, const int64_t* targets,
             int64_t ignore, int64_t rows, int64_t vocab, float* loss, float* lse, int* status) {
@@ -561,15 +563,15 @@ join_kernel(const float2* partial, int parts, const float* own, const int64_t* t
     loss[n] = lse[n] = 0.f;
     return;
   }
-  const double l = (double)top * kLn2 + log((double)sum);
-  const float r = y >= 0 && y < vocab ? (float)(l - (double)own[n]) : NAN;
-  lse[n] = (float)l;
+  const float hi = top * kLn2, lo = fmaf(top, kLn2, -hi) + logf(sum);
+  const float r = y >= 0 && y < vocab ? (hi - own[n]) + lo : NAN;
+  lse[n] = hi + lo;
   loss[n] = isfinite(r) ? r : NAN;
   if (!isfinite(r)) atomicCAS(status, 0, SOMA_ERR_NONFINITE);
 }
 
 // Per row, one warp: what it takes part with, and a copy of h in rows of a
-// multiple of eight elements with the rows that take no part zeroed (their h
+// multiple of 64 elements with the rows that take no part zeroed (their h
 // may hold anything, and 0 * NaN would reach demb).
 template <typename T>
 __global__ void __launch_bounds__(256)
@@ -598,13 +600,15 @@ rows_kernel(const T* h, soma_linear_ce_dims d, const int64_t* targets, int64_t i
   info[n] = r;
 }
 
-// A matrix whose row stride is no multiple of eight, copied to rows that are.
+// A matrix copied to rows of cs elements, zeros after the first dim; eight
+// elements per thread.
 template <typename T>
-__global__ void __launch_bounds__(128)
-pack_kernel(const T* x, int64_t xs, int64_t dim, T* copy, int64_t cs) {
-  const int64_t n = blockIdx.x;
-  for (int64_t j = threadIdx.x; j < cs; j += 128)
-    copy[n * cs + j] = j < dim ? x[n * xs + j] : from_f32<T>(0.f);
+__global__ void __launch_bounds__(256)
+pack_kernel(const T* x, int64_t xs, int64_t rows, int64_t dim, T* copy, int64_t cs) {
+  const int64_t at = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8;
+  const int64_t n = at / cs, j = at - n * cs;
+  if (n < rows)
+    *reinterpret_cast<uint4*>(copy + at) = row_piece(x + n * xs, j, dim, xs % 8 == 0);
 }
 
 // The rows of dh (info) or demb (no info) from their fp32 sums, the slots in
@@ -653,6 +657,7 @@ sums_kernel(const float* acc, int64_t acc_stride, int used, const __grid_constan
 size_t round256(size_t x) { return (x + 255) / 256 * 256; }
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 int64_t round8(int64_t x) { return (x + 7) / 8 * 8; }
+int64_t round64(int64_t x) { return (x + 63) / 64 * 64; }
 
 bool dims_ok(const soma_linear_ce_dims& d) {
   return d.rows >= 0 && d.rows <= (1 << 30) && d.vocab >= 1 && d.vocab <= (1 << 30) &&
@@ -700,12 +705,25 @@ int64_t tiles_cost(int64_t M, int64_t N, int64_t depth) {
          kLaunchStages;
 }
 
+// Whether a matrix of `copied` rows is copied to rows of a multiple of 64
+// elements before `rows` rows are multiplied by it: a stride that is no
+// multiple of 8 cannot be read in boxes at all, and one that is no multiple of
+// 16 puts a box's 128-byte rows across five 32-byte sectors, which makes the
+// products take 1.35 times as long (3001 x 50021 x 680 forward: 182 us at a
+// stride of 680 or 712, 133 us at 704).  The copy is worth its time (4 bytes
+// per element moved) from about 2000 rows in the forward call, and a third of
+// that in the backward call with its three products.
+bool copied(int64_t stride, int64_t rows, bool backward) {
+  return stride % 8 != 0 || (stride % 16 != 0 && rows >= (backward ? 700 : 2000));
+}
+
 struct Plan {
   int32_t splits;                // forward
   int64_t piece;                 // backward: vocabulary entries of one piece
   bool dh_sums, demb_sums;       // which kernels the products take
   int64_t g_stride, acc_stride, dh_slots, demb_slots;
-  size_t h, emb, partial, own;   // offsets; h, emb: copies (emb only where its stride asks for it)
+  bool copy_h, copy_emb;
+  size_t h, emb, partial, own;   // offsets; h, emb: copies
   size_t g, info, dh_acc, demb_acc, top, total;
 };
 
@@ -757,8 +775,10 @@ Plan plan(soma_linear_ce_dims d, bool backward) {
     return o;
   };
   if (!d.rows) d.rows = 1;
-  if (backward || d.h_stride % 8) p.h = take((size_t)d.rows * round8(d.dim) * 2);
-  if (d.emb_stride % 8) p.emb = take((size_t)d.vocab * round8(d.dim) * 2);
+  p.copy_h = backward || copied(d.h_stride, d.rows, false);
+  p.copy_emb = copied(d.emb_stride, d.rows, backward);
+  if (p.copy_h) p.h = take((size_t)d.rows * round64(d.dim) * 2);
+  if (p.copy_emb) p.emb = take((size_t)d.vocab * round64(d.dim) * 2);
   if (!backward) {
     // rounds of pairs times the tiles of a unit, least first
     const int64_t mt = ceil_div(d.rows, kTile), vt = ceil_div(d.vocab, kTile);
@@ -801,6 +821,16 @@ bool aligned(const void* p, size_t to) { return (reinterpret_cast<uintptr_t>(p) 
 template <typename T>
 constexpr int dtype_of() { return std::is_same<T, __half>::value ? SOMA_FP16 : SOMA_BF16; }
 
+// x copied to rows of a multiple of 64 elements; *stride becomes theirs.
+template <typename T>
+const T* pack(const T* x, int64_t rows, int64_t dim, int64_t* stride, T* copy, cudaStream_t st) {
+  const int64_t cs = round64(dim);
+  pack_kernel<T><<<(unsigned)ceil_div(rows * cs, 256 * 8), 256, 0, st>>>(x, *stride, rows, dim,
+                                                                       copy, cs);
+  *stride = cs;
+  return copy;
+}
+
 // A launch of `units` units, or of w.pairs pairs (sums).
 template <int KIND, typename T>
 cudaError_t launch(const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& out, Work w,
@@ -819,18 +849,8 @@ cudaError_t forward(const T* h, const T* emb, const soma_linear_ce_dims& d, cons
                     cudaStream_t st) {
   const Plan p = plan(d, false);
   int64_t hs = d.h_stride, es = d.emb_stride;
-  if (hs % 8) {
-    T* copy = reinterpret_cast<T*>(ws + p.h);
-    pack_kernel<T><<<(unsigned)d.rows, 128, 0, st>>>(h, hs, d.dim, copy, round8(d.dim));
-    h = copy;
-    hs = round8(d.dim);
-  }
-  if (es % 8) {
-    T* copy = reinterpret_cast<T*>(ws + p.emb);
-    pack_kernel<T><<<(unsigned)d.vocab, 128, 0, st>>>(emb, es, d.dim, copy, round8(d.dim));
-    emb = copy;
-    es = round8(d.dim);
-  }
+  if (p.copy_h) h = pack(h, d.rows, d.dim, &hs, reinterpret_cast<T*>(ws + p.h), st);
+  if (p.copy_emb) emb = pack(emb, d.vocab, d.dim, &es, reinterpret_cast<T*>(ws + p.emb), st);
   CUtensorMap ma, mb;
   if (!make_tile_map(&ma, h, dtype_of<T>(), d.rows, d.dim, hs, kHalf) ||
       !make_tile_map(&mb, emb, dtype_of<T>(), d.vocab, d.dim, es, kHalf))
@@ -869,18 +889,13 @@ cudaError_t backward(const T* h, const T* emb, const soma_linear_ce_dims& d,
   float* top = reinterpret_cast<float*>(ws + p.top);
   float* dh_acc = reinterpret_cast<float*>(ws + p.dh_acc);
   float* demb_acc = reinterpret_cast<float*>(ws + p.demb_acc);
-  const int64_t cs = round8(d.dim);
+  const int64_t cs = round64(d.dim);
   int64_t es = d.emb_stride;
   cudaError_t e = cudaMemsetAsync(top, 0, 4, st);
   if (e != cudaSuccess) return e;
   rows_kernel<T><<<(unsigned)ceil_div(d.rows, 8), 256, 0, st>>>(
       h, d, targets, ignore, lse, dloss, info, copy, cs, dtype == SOMA_FP16 ? top : nullptr);
-  if (es % 8) {
-    T* packed = reinterpret_cast<T*>(ws + p.emb);
-    pack_kernel<T><<<(unsigned)d.vocab, 128, 0, st>>>(emb, es, d.dim, packed, cs);
-    emb = packed;
-    es = cs;
-  }
+  if (p.copy_emb) emb = pack(emb, d.vocab, d.dim, &es, reinterpret_cast<T*>(ws + p.emb), st);
   const bool many = p.piece < d.vocab;
   const bool dh_tiled = dhs % 8 == 0 && aligned(dh, 16);
   const bool demb_tiled = des % 8 == 0 && aligned(demb, 16);
