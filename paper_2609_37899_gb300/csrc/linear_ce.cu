@@ -18,6 +18,7 @@
 #define SOMA_CHECK_FILE 10
 #include "checked.cuh"
 #include "numeric.cuh"
+#include "pdl.cuh"
 #include "soma_api.h"
 #include "soma_launch.h"
 #include "tc_tiles.cuh"
@@ -101,7 +102,7 @@ struct Work {
   int32_t y_b;                // first row of B (the piece's place in emb)
   // stats
   const int64_t* targets;
-  float2* partial;            // [2 splits][M]: maximum (powers of two), sum
+  float2* partial;            // [M][2 splits]: maximum (powers of two), sum
   float* own;                 // [M] logit of the target
   // grad, dh
   RowInfo* info;
@@ -284,11 +285,13 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     tc::prefetch_map(&map_b);
     if (KIND != kStats) tc::prefetch_map(&map_out);
   }
+  admit_successor();
   if (warp == 2) tc::tmem_alloc_pair(&sh.tmem, 512);
   tc::tc_fence_before();
   __syncthreads();
   tc::cluster_sync();
   tc::tc_fence_after();
+  after_predecessor();
   const uint32_t tmem = sh.tmem;
 
   Walk<KIND> walk(w, pair);
@@ -401,12 +404,18 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
       tc::tc_fence_after();
       const uint32_t src = tmem + buf * kTile + half * kHalf + ((uint32_t)(quarter * 32) << 16);
       const int64_t n0 = (int64_t)s.n * kTile + half * kHalf;
+      // 32 columns at a time, the next ones on their way while these are used
+      float next[32];
+      if (n0 < w.N && m0 < w.M) tc::tmem_ld32_nowait(src, next);
+#pragma unroll
       for (int c = 0; c < kHalf; c += 32) {
         const int64_t n = n0 + c;
         if (n >= w.N || m0 >= w.M) break;  // nothing there (the whole warp)
+        tc::tmem_wait_ld32(next);
         float x[32];
-        tc::tmem_ld32_nowait(src + c, x);
-        tc::tmem_wait_ld();
+#pragma unroll
+        for (int j = 0; j < 32; ++j) x[j] = next[j];
+        if (c + 32 < kHalf && n + 32 < w.N) tc::tmem_ld32_nowait(src + c + 32, next);
         if (KIND == kStats) {
           const int64_t hit = y - n;
           if (hit >= 0 && hit < 32) {
@@ -521,7 +530,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
       if (lane == 0) tc::mbar_arrive_cluster(empty_bar[buf]);
       ++n_acc;
       if (KIND == kStats && s.last && live)
-        w.partial[((int64_t)s.part * 2 + half) * w.M + m] = make_float2(top, sum);
+        w.partial[m * 2 * w.splits + 2 * s.part + half] = make_float2(top, sum);
     }
     if (KIND != kStats && lane == 0) tc::bulk_wait();
   }
@@ -539,12 +548,14 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
 __global__ void __launch_bounds__(256)
 join_kernel(const float2* partial, int parts, const float* own, const int64_t* targets,
             int64_t ignore, int64_t rows, int64_t vocab, float* loss, float* lse, int* status) {
+  admit_successor();
+  after_predecessor();
   const int64_t n = (int64_t)blockIdx.x * 8 + threadIdx.x / 32;
   if (n >= rows) return;
   const int lane = threadIdx.x % 32;
   float top = -INFINITY, sum = 0.f;
   for (int j = lane; j < parts; j += 32) {
-    const float2 p = partial[(int64_t)j * rows + n];
+    const float2 p = partial[n * parts + j];
     const float now = fmaxf(top, p.x), ref = now == -INFINITY ? 0.f : now;
     sum = sum * tc::ex2(top - ref) + p.y * tc::ex2(p.x - ref);
     top = now;
@@ -577,27 +588,37 @@ template <typename T>
 __global__ void __launch_bounds__(256)
 rows_kernel(const T* h, soma_linear_ce_dims d, const int64_t* targets, int64_t ignore,
             const float* lse, const float* dloss, RowInfo* info, T* copy, int64_t cs, float* top) {
+  __shared__ int largest;
+  if (threadIdx.x == 0) largest = 0;
+  __syncthreads();
+  admit_successor();
+  after_predecessor();
   const int64_t n = (int64_t)blockIdx.x * 8 + threadIdx.x / 32;
-  if (n >= d.rows) return;
   const int lane = threadIdx.x % 32;
-  const int64_t y = targets[n];
-  const float l = lse[n];
-  const bool live = y != ignore && y >= 0 && y < d.vocab && isfinite(l);
-  const bool vec = d.h_stride % 8 == 0;
-  for (int64_t j = lane * 8; j < cs; j += 256)
-    *reinterpret_cast<uint4*>(copy + n * cs + j) =
-        live ? row_piece(h + n * d.h_stride, j, d.dim, vec) : make_uint4(0u, 0u, 0u, 0u);
-  if (lane) return;
-  RowInfo r = {l * kLog2e, 0.f, 0.f, -1};
-  if (live) {
-    r.g = dloss[n];
-    r.y = (int32_t)y;
-    // non-negative floats order as their bits do; most rows need no atomic
-    const int bits = __float_as_int(fabsf(r.g));
-    if (top && isfinite(r.g) && bits > *reinterpret_cast<volatile int*>(top))
-      atomicMax(reinterpret_cast<int*>(top), bits);
+  if (n < d.rows) {
+    const int64_t y = targets[n];
+    const float l = lse[n];
+    const bool live = y != ignore && y >= 0 && y < d.vocab && isfinite(l);
+    const bool vec = d.h_stride % 8 == 0;
+    for (int64_t j = lane * 8; j < cs; j += 256)
+      *reinterpret_cast<uint4*>(copy + n * cs + j) =
+          live ? row_piece(h + n * d.h_stride, j, d.dim, vec) : make_uint4(0u, 0u, 0u, 0u);
+    if (lane == 0) {
+      RowInfo r = {l * kLog2e, 0.f, 0.f, -1};
+      if (live) {
+        r.g = dloss[n];
+        r.y = (int32_t)y;
+        // non-negative floats order as their bits do
+        if (top && isfinite(r.g)) atomicMax(&largest, __float_as_int(fabsf(r.g)));
+      }
+      info[n] = r;
+    }
   }
-  info[n] = r;
+  if (!top) return;
+  __syncthreads();
+  // one atomic per block, and none where it would change nothing
+  if (threadIdx.x == 0 && largest > *reinterpret_cast<volatile int*>(top))
+    atomicMax(reinterpret_cast<int*>(top), largest);
 }
 
 // A matrix copied to rows of cs elements, zeros after the first dim; eight
@@ -605,6 +626,8 @@ rows_kernel(const T* h, soma_linear_ce_dims d, const int64_t* targets, int64_t i
 template <typename T>
 __global__ void __launch_bounds__(256)
 pack_kernel(const T* x, int64_t xs, int64_t rows, int64_t dim, T* copy, int64_t cs) {
+  admit_successor();
+  after_predecessor();
   const int64_t at = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8;
   const int64_t n = at / cs, j = at - n * cs;
   if (n < rows)
@@ -617,6 +640,8 @@ template <typename T>
 __global__ void __launch_bounds__(128)
 sums_kernel(const float* acc, int64_t acc_stride, int used, const __grid_constant__ Work w,
             const RowInfo* info, T* out, int64_t stride, int vec) {
+  admit_successor();
+  after_predecessor();
   const int64_t n = blockIdx.x;
   const float f = 1.f / g_scale<T>(*w.top);
   if (!used) {
@@ -825,10 +850,10 @@ constexpr int dtype_of() { return std::is_same<T, __half>::value ? SOMA_FP16 : S
 template <typename T>
 const T* pack(const T* x, int64_t rows, int64_t dim, int64_t* stride, T* copy, cudaStream_t st) {
   const int64_t cs = round64(dim);
-  pack_kernel<T><<<(unsigned)ceil_div(rows * cs, 256 * 8), 256, 0, st>>>(x, *stride, rows, dim,
-                                                                       copy, cs);
+  const cudaError_t e = launch_overlapped(pack_kernel<T>, (unsigned)ceil_div(rows * cs, 256 * 8),
+                                          256, 0, st, x, *stride, rows, dim, copy, cs);
   *stride = cs;
-  return copy;
+  return e == cudaSuccess ? copy : nullptr;
 }
 
 // A launch of `units` units, or of w.pairs pairs (sums).
@@ -839,8 +864,8 @@ cudaError_t launch(const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap
       product_kernel<KIND, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem);
   if (ready != cudaSuccess) return ready;
   if (!sums(KIND)) w.pairs = (int32_t)(units < kPairs ? units : kPairs);
-  product_kernel<KIND, T><<<2 * w.pairs, kThreads, kSmem, st>>>(a, b, out, w, status);
-  return cudaGetLastError();
+  return launch_overlapped(product_kernel<KIND, T>, 2 * w.pairs, kThreads, kSmem, st, a, b, out, w,
+                           status);
 }
 
 template <typename T>
@@ -851,6 +876,7 @@ cudaError_t forward(const T* h, const T* emb, const soma_linear_ce_dims& d, cons
   int64_t hs = d.h_stride, es = d.emb_stride;
   if (p.copy_h) h = pack(h, d.rows, d.dim, &hs, reinterpret_cast<T*>(ws + p.h), st);
   if (p.copy_emb) emb = pack(emb, d.vocab, d.dim, &es, reinterpret_cast<T*>(ws + p.emb), st);
+  if (!h || !emb) return cudaErrorLaunchFailure;
   CUtensorMap ma, mb;
   if (!make_tile_map(&ma, h, dtype_of<T>(), d.rows, d.dim, hs, kHalf) ||
       !make_tile_map(&mb, emb, dtype_of<T>(), d.vocab, d.dim, es, kHalf))
@@ -868,10 +894,8 @@ cudaError_t forward(const T* h, const T* emb, const soma_linear_ce_dims& d, cons
   const cudaError_t e =
       launch<kStats, T>(ma, mb, ma, w, (int64_t)w.m_tiles * w.splits, status, st);
   if (e != cudaSuccess) return e;
-  join_kernel<<<(unsigned)ceil_div(d.rows, 8), 256, 0, st>>>(w.partial, 2 * p.splits, w.own,
-                                                             targets, ignore, d.rows, d.vocab,
-                                                             loss, lse, status);
-  return cudaGetLastError();
+  return launch_overlapped(join_kernel, (unsigned)ceil_div(d.rows, 8), 256, 0, st, w.partial,
+                           2 * p.splits, w.own, targets, ignore, d.rows, d.vocab, loss, lse, status);
 }
 
 template <typename T>
@@ -891,11 +915,17 @@ cudaError_t backward(const T* h, const T* emb, const soma_linear_ce_dims& d,
   float* demb_acc = reinterpret_cast<float*>(ws + p.demb_acc);
   const int64_t cs = round64(d.dim);
   int64_t es = d.emb_stride;
-  cudaError_t e = cudaMemsetAsync(top, 0, 4, st);
+  cudaError_t e = cudaSuccess;
+  if (dtype == SOMA_FP16) e = cudaMemsetAsync(top, 0, 4, st);
+  if (p.dh_sums && p.piece < d.vocab && e == cudaSuccess)
+    e = cudaMemsetAsync(dh_acc, 0,
+                        (size_t)p.dh_slots * ceil_div(d.rows, kTile) * kTile * p.acc_stride * 4, st);
+  if (e == cudaSuccess)
+    e = launch_overlapped(rows_kernel<T>, (unsigned)ceil_div(d.rows, 8), 256, 0, st, h, d, targets,
+                          ignore, lse, dloss, info, copy, cs, dtype == SOMA_FP16 ? top : nullptr);
   if (e != cudaSuccess) return e;
-  rows_kernel<T><<<(unsigned)ceil_div(d.rows, 8), 256, 0, st>>>(
-      h, d, targets, ignore, lse, dloss, info, copy, cs, dtype == SOMA_FP16 ? top : nullptr);
   if (p.copy_emb) emb = pack(emb, d.vocab, d.dim, &es, reinterpret_cast<T*>(ws + p.emb), st);
+  if (!emb) return cudaErrorLaunchFailure;
   const bool many = p.piece < d.vocab;
   const bool dh_tiled = dhs % 8 == 0 && aligned(dh, 16);
   const bool demb_tiled = des % 8 == 0 && aligned(demb, 16);
@@ -917,11 +947,6 @@ cudaError_t backward(const T* h, const T* emb, const soma_linear_ce_dims& d,
                              p.demb_slots * ceil_div(d.vocab, kTile) * kTile, p.acc_stride,
                              p.acc_stride, 32);
   if (!ok) return cudaErrorInvalidValue;
-  if (many) {
-    e = cudaMemsetAsync(dh_acc, 0,
-                        (size_t)p.dh_slots * ceil_div(d.rows, kTile) * kTile * p.acc_stride * 4, st);
-    if (e != cudaSuccess) return e;
-  }
   for (int64_t v0 = 0; v0 < d.vocab; v0 += p.piece) {
     const int64_t width = d.vocab - v0 < p.piece ? d.vocab - v0 : p.piece;
     CUtensorMap g_k, g_mn, g_out, demb_out = h_k;
@@ -953,12 +978,10 @@ cudaError_t backward(const T* h, const T* emb, const soma_linear_ce_dims& d,
     if (p.dh_sums) {
       w.add = many;
       e = launch<kDhSums, T>(g_k, e_mn, dh_out, w, 0, status, st);
-      if (e == cudaSuccess && v0 + width == d.vocab) {
-        sums_kernel<T><<<(unsigned)d.rows, 128, 0, st>>>(
-            dh_acc, p.acc_stride, many ? (int)p.dh_slots : 0, w, info, dh, dhs,
-            dhs % 4 == 0 && aligned(dh, 8));
-        e = cudaGetLastError();
-      }
+      if (e == cudaSuccess && v0 + width == d.vocab)
+        e = launch_overlapped(sums_kernel<T>, (unsigned)d.rows, 128, 0, st, dh_acc, p.acc_stride,
+                              many ? (int)p.dh_slots : 0, w, info, dh, dhs,
+                              dhs % 4 == 0 && aligned(dh, 8));
     } else {
       w.out = dh_tiled ? nullptr : dh;
       w.out_stride = dhs;
@@ -970,10 +993,10 @@ cudaError_t backward(const T* h, const T* emb, const soma_linear_ce_dims& d,
     w.top = top;
     if (p.demb_sums) {
       e = launch<kDembSums, T>(g_mn, h_mn, demb_sum, w, 0, status, st);
-      if (e != cudaSuccess) return e;
-      sums_kernel<T><<<(unsigned)d.vocab, 128, 0, st>>>(demb_acc, p.acc_stride, 0, w, nullptr,
-                                                        demb, des, des % 4 == 0 && aligned(demb, 8));
-      e = cudaGetLastError();
+      if (e == cudaSuccess)
+        e = launch_overlapped(sums_kernel<T>, (unsigned)d.vocab, 128, 0, st, demb_acc,
+                              p.acc_stride, 0, w, nullptr, demb, des,
+                              des % 4 == 0 && aligned(demb, 8));
     } else {
       w.out = demb_tiled ? nullptr : demb + v0 * des;
       w.out_stride = des;
