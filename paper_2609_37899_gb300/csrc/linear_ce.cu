@@ -25,36 +25,6 @@
 
 namespace soma {
 
-bool make_tile_map(CUtensorMap* map, const void* base, int dtype, int64_t rows, int64_t cols,
-                   int64_t stride, int box_rows) {
-  using Encode = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*,
-                              const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
-                              const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
-                              CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-  static const Encode encode = [] {
-    void* f = nullptr;
-    cudaDriverEntryPointQueryResult found;
-    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault,
-                                         &found) != cudaSuccess ||
-        found != cudaDriverEntryPointSuccess)
-      f = nullptr;
-    return reinterpret_cast<Encode>(f);
-  }();
-  if (!encode) return false;
-  const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
-  const int width = dtype == SOMA_FP32 ? 4 : 2;
-  const cuuint64_t strides[1] = {(cuuint64_t)stride * width};
-  const cuuint32_t box[2] = {128u / width, (cuuint32_t)box_rows};
-  const cuuint32_t step[2] = {1, 1};
-  const CUtensorMapDataType type = dtype == SOMA_FP32   ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
-                                   : dtype == SOMA_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16
-                                                        : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
-  return encode(map, type, 2, const_cast<void*>(base), dims, strides, box, step,
-                CU_TENSOR_MAP_INTERLEAVE_NONE,
-                CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
 namespace {
 
 constexpr int kPairs = 76;                    // CTA pairs that are resident: 152 SMs

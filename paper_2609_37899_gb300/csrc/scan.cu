@@ -6,16 +6,21 @@
 // the time axis is cut into segments of kSegment steps: every warp turns its
 // segment's gates into f and u in registers, the (A, B) of the segments are
 // joined, and each warp runs its steps again from the state that reaches it.
-// The gates are read once.  A warp holds 32 lanes' channels of one segment; a
-// CTA's warps hold consecutive segments, a cluster's CTAs consecutive groups of
-// them, and the cluster walks the sequence, its next gates on their way while
-// it joins (through shared memory and distributed shared memory).  Backward is
-// the same with r_t = f_t (dh_t o_t tanh'(c_t) + r_{t+1}) from the right, the
-// states of a segment run again from the forward call's checkpoint.
+// The gates are read once.  A CTA's warps hold consecutive segments, a
+// cluster's CTAs consecutive groups of them, and the cluster walks the
+// sequence, joining through shared memory and distributed shared memory.
+// Backward is the same with r_t = f_t (dh_t o_t tanh'(c_t) + r_{t+1}) from the
+// right, the states of a segment run again from the forward call's checkpoint.
+//
+// Tiled kernels: a lane holds two channels in packed fp32 arithmetic, the gates
+// come as TMA boxes into a ring of shared-memory stages.  Plain kernels: one
+// channel per lane and loads of single elements, for tensors that a tensor map
+// cannot describe.
 //
 // Bytes bound it: per element of 16 bits 8 read and 2 written forward, 10 read
-// and 8 written backward, next to 6 (10) operations of the special function
-// unit.
+// and 8 written backward.  The instructions come close: 113 per element (one
+// channel at a time, a 64-bit address and a bounds check per load) took 2.7
+// times the bytes' time.
 #define SOMA_CHECK_FILE 9
 #include "checked.cuh"
 #include "numeric.cuh"
@@ -82,6 +87,76 @@ __device__ __forceinline__ void tanh_slope(float x, float& y, float& dy) {
                                         0x1.111112p-3f), s, -0x1.555556p-2f), s, 1.f);
   y = fabsf(x) < 0.3f ? near : copysignf((1.f - e) * r, x);
   dy = 4.f * e * r * r;
+}
+
+// Two fp32 values in a register pair, for the packed instructions.
+struct Two {
+  unsigned long long v;
+};
+__device__ __forceinline__ Two two(float a, float b) {
+  Two r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ Two two(float a) { return two(a, a); }
+__device__ __forceinline__ void split(Two x, float& a, float& b) {
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(x.v));
+}
+__device__ __forceinline__ Two operator*(Two a, Two b) {
+  Two r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+__device__ __forceinline__ Two operator+(Two a, Two b) {
+  Two r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+__device__ __forceinline__ Two fma2(Two a, Two b, Two c) {
+  Two r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+  return r;
+}
+template <typename F>
+__device__ __forceinline__ Two each(Two x, F f) {
+  float a, b;
+  split(x, a, b);
+  return two(f(a), f(b));
+}
+__device__ __forceinline__ Two rcp2(Two x) {
+  return each(x, [](float y) { return rcp(y); });
+}
+__device__ __forceinline__ Two ex22(Two x) {
+  return each(x, [](float y) { return tc::ex2(y); });
+}
+__device__ __forceinline__ Two one_exp2(Two x) { return ex22(x * two(-kLog2e)) + two(1.f); }
+__device__ __forceinline__ void tanh_parts2(Two x, Two& num, Two& den) {
+  x = each(x, [](float y) { return min_nan(max_nan(y, -8.7f), 8.7f); });
+  const Two s = x * x;
+  num = x * fma2(fma2(fma2(fma2(two(0x1.dd859ep-27f), s, two(0x1.60381ep-16f)), s,
+                           two(0x1.cd359ap-9f)), s, two(0x1.12710ep-3f)), s, two(1.f));
+  den = fma2(fma2(fma2(fma2(two(0x1.ad4ff2p-21f), s, two(0x1.5c82aep-12f)), s,
+                       two(0x1.a968bap-6f)), s, two(0x1.de8dd4p-2f)), s, two(1.f));
+}
+// sigmoid and y (1 - y): the derivative good to 1 u of 1.
+__device__ __forceinline__ void sigmoid_slope2(Two x, Two& y, Two& dy) {
+  y = rcp2(one_exp2(x));
+  dy = fma2(y * two(-1.f), y, y);
+}
+// tanh by e = exp(-2 |x|), which gives the derivative 4 e / (1 + e)^2 good
+// relative to its size, and below 0.1 by the Taylor series to x^5 (6e-8).
+__device__ __forceinline__ void tanh_slope2(Two x, Two& y, Two& dy) {
+  const Two e = each(x, [](float z) { return tc::ex2(-2.f * kLog2e * fabsf(z)); });
+  const Two r = rcp2(e + two(1.f));
+  const Two s = x * x;
+  const Two near = x * fma2(fma2(two(0x1.111112p-3f), s, two(-0x1.555556p-2f)), s, two(1.f));
+  const Two far = fma2(e, two(-1.f), two(1.f)) * r;
+  float x0, x1, n0, n1, f0, f1;
+  split(x, x0, x1);
+  split(near, n0, n1);
+  split(far, f0, f1);
+  y = two(fabsf(x0) < 0.1f ? n0 : copysignf(f0, x0), fabsf(x1) < 0.1f ? n1 : copysignf(f1, x1));
+  dy = (e * two(4.f)) * (r * r);
 }
 
 struct Scan {
@@ -443,6 +518,336 @@ scan_backward_kernel(const T* __restrict__ gates, const __grid_constant__ Scan s
   }
 }
 
+// ---- tiled ----------------------------------------------------------------
+constexpr int kDepth = 3;          // stages of the ring
+constexpr int kBackwardWarps = 4;  // of a CTA: its registers allow three such on an SM
+constexpr int kBlock = 64;         // channels of a CTA: 32 lanes of two
+
+// The tensors of a call as boxes of 64 channels by the CTA's steps: one map
+// per gate, then dh.
+struct Maps {
+  CUtensorMap in[5], out[4];
+  int32_t t_inner;  // whether steps are the second dimension of the maps, sequences the third
+};
+
+__device__ __forceinline__ void box_g2s(void* dst, const CUtensorMap* map, int x, int y, int z,
+                                        uint64_t* bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
+      " [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(tc::smem_u32(dst)),
+      "l"(map), "r"(x), "r"(y), "r"(z), "r"(tc::smem_u32(bar))
+      : "memory");
+}
+__device__ __forceinline__ void box_s2g(const CUtensorMap* map, int x, int y, int z,
+                                        const void* src) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%1, %2, %3}], [%4];" ::"l"(
+          map),
+      "r"(x), "r"(y), "r"(z), "r"(tc::smem_u32(src))
+      : "memory");
+}
+
+// A lane's two channels in shared memory.
+__device__ __forceinline__ Two load_two(const float* p) {
+  const float2 x = *reinterpret_cast<const float2*>(p);
+  return two(x.x, x.y);
+}
+__device__ __forceinline__ Two load_two(const __nv_bfloat16* p) {
+  const uint32_t x = *reinterpret_cast<const uint32_t*>(p);
+  return two(__uint_as_float(x << 16), __uint_as_float(x & 0xFFFF0000u));
+}
+__device__ __forceinline__ Two load_two(const __half* p) {
+  const float2 x = __half22float2(*reinterpret_cast<const __half2*>(p));
+  return two(x.x, x.y);
+}
+__device__ __forceinline__ void store_two(float* p, Two x) {
+  float a, b;
+  split(x, a, b);
+  *reinterpret_cast<float2*>(p) = make_float2(a, b);
+}
+__device__ __forceinline__ void store_two(__nv_bfloat16* p, Two x) {
+  float a, b;
+  split(x, a, b);
+  *reinterpret_cast<__nv_bfloat162*>(p) = __floats2bfloat162_rn(a, b);
+}
+__device__ __forceinline__ void store_two(__half* p, Two x) {
+  float a, b;
+  split(x, a, b);
+  *reinterpret_cast<__half2*>(p) = __floats2half2_rn(a, b);
+}
+
+__device__ __forceinline__ Two apply2(Two a, Two b, Two c) {
+  float a0, a1, b0, b1, c0, c1;
+  split(a, a0, a1);
+  split(b, b0, b1);
+  split(c, c0, c1);
+  return two(apply(a0, b0, c0), apply(a1, b1, c1));
+}
+
+struct Ring {
+  uint64_t full[kDepth];
+  volatile int abort;
+};
+
+__device__ __forceinline__ void ring_wait(Ring& r, int stage, uint32_t parity, int* status) {
+  if (r.abort || tc::mbar_wait(&r.full[stage], parity)) return;
+  r.abort = 1;
+  atomicCAS(status, 0, SOMA_ERR_TIMEOUT);
+}
+
+// RAGGED: lengths or resets are given.  h is written directly: a row of a
+// warp's store is 128 bytes.
+template <typename T, bool RAGGED>
+__global__ void __launch_bounds__(32 * kMaxWarps, 2)
+scan_forward_tiled_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Scan s,
+                          T* __restrict__ h, int* status) {
+  extern __shared__ uint8_t raw[];
+  __shared__ Joint<2> sh;
+  __shared__ Ring ring;
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, warps = blockDim.x / 32;
+  const int C = s.cluster;
+  const uint32_t rank = C > 1 ? tc::pair_rank() : 0;
+  const int rows = warps * kSegment;                // steps of the CTA's round
+  const int64_t span = (int64_t)C * rows;           // ... of the cluster's
+  const int64_t marks = (s.d.steps + kSegment - 1) / kSegment;
+  const int stage_elems = 4 * rows * kBlock;
+  T* const stages = reinterpret_cast<T*>(raw + (128 - (tc::smem_u32(raw) & 127)) % 128);
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < kDepth; ++i) tc::mbar_init(&ring.full[i], 1);
+    tc::mbar_fence_init();
+    ring.abort = 0;
+  }
+  __syncthreads();
+  uint32_t filled = 0, used = 0;  // stages so far
+  for (int64_t item = blockIdx.x / C; item < s.d.batch * s.blocks; item += gridDim.x / C) {
+    const int64_t b = item / s.blocks;
+    const int ch0 = (int)(item % s.blocks) * kBlock;
+    const int64_t ch = ch0 + 2 * lane;
+    const bool on = ch < s.d.dim;
+    const int64_t n = length_of(s, b);
+    const int64_t rounds = (n + span - 1) / span;
+    float c[2] = {0.f, 0.f};
+    if (on && s.c0) c[0] = s.c0[b * s.d.dim + ch], c[1] = s.c0[b * s.d.dim + ch + 1];
+
+    const auto fill = [&](int64_t round) {  // warp 0
+      const int st = filled++ % kDepth;
+      if (lane == 0) tc::mbar_arrive_expect_tx(&ring.full[st], stage_elems * sizeof(T));
+      __syncwarp();
+      if (lane < 4) {
+        const int t = (int)(round * span) + (int)rank * rows;
+        box_g2s(stages + (size_t)st * stage_elems + lane * rows * kBlock, &maps.in[lane], ch0,
+                maps.t_inner ? t : (int)b, maps.t_inner ? (int)b : t, &ring.full[st]);
+      }
+    };
+    if (warp == 0)
+      for (int64_t q = 0; q < kDepth && q < rounds; ++q) fill(q);
+
+    int64_t t0 = (int64_t)(rank * warps + warp) * kSegment;
+    for (int64_t round = 0; round < rounds; ++round, t0 += span) {
+      const int st = used % kDepth;
+      ring_wait(ring, st, (used / kDepth) & 1, status);
+      ++used;
+      const T* p = stages + (size_t)st * stage_elems + warp * kSegment * kBlock + 2 * lane;
+      const int gate = rows * kBlock;
+      Two f[kSegment], u[kSegment], o[kSegment];
+      Two A = two(1.f), B = two(0.f);
+      const bool whole = t0 + kSegment <= n;  // no step past the end (the whole warp)
+#pragma unroll
+      for (int j = 0; j < kSegment; ++j) {
+        const Two ai = load_two(p + j * kBlock), af = load_two(p + gate + j * kBlock);
+        const Two ag = load_two(p + 2 * gate + j * kBlock);
+        o[j] = load_two(p + 3 * gate + j * kBlock);
+        Two num, den;
+        tanh_parts2(ag, num, den);
+        u[j] = num * rcp2(den * one_exp2(ai));
+        f[j] = rcp2(one_exp2(af));
+        if (RAGGED && s.resets && t0 + j < n && s.resets[b * s.d.steps + t0 + j]) f[j] = two(0.f);
+        if (!whole && t0 + j >= n) f[j] = two(1.f), u[j] = two(0.f);
+        B = RAGGED ? apply2(f[j], u[j], B) : fma2(f[j], B, u[j]);
+        A = A * f[j];
+      }
+      Map<2> m;
+      split(A, m.a[0], m.a[1]);
+      split(B, m.b[0], m.b[1]);
+      float in[2];
+      join<2, false>(sh, m, (int)(used & 1), C, rank, c, in);
+      // every warp has read the stage
+      if (warp == 0 && round + kDepth < rounds) fill(round + kDepth);
+      if (on) {
+        if (s.marks && t0 < s.d.steps)
+          *reinterpret_cast<float2*>(s.marks + (b * marks + t0 / kSegment) * s.d.dim + ch) =
+              make_float2(in[0], in[1]);
+        T* q = h + b * s.hs.b + t0 * s.hs.t + ch;
+        Two x = two(in[0], in[1]);
+#pragma unroll
+        for (int j = 0; j < kSegment; ++j) {
+          x = RAGGED ? apply2(f[j], u[j], x) : fma2(f[j], x, u[j]);
+          Two num, den;
+          tanh_parts2(x, num, den);
+          const Two y = num * rcp2(den * one_exp2(o[j]));
+          if (whole || t0 + j < n) store_two(q, y);
+          else if (t0 + j < s.d.steps) store_two(q, two(0.f));
+          q += s.hs.t;
+        }
+      }
+      __syncwarp();
+    }
+    // rounds past the sequence's end
+    if (RAGGED && on)
+      for (; t0 < s.d.steps; t0 += span)
+        for (int j = 0; j < kSegment && t0 + j < s.d.steps; ++j)
+          store_two(h + b * s.hs.b + (t0 + j) * s.hs.t + ch, two(0.f));
+    __syncwarp();
+    if (s.c_last && on && rank == 0 && warp == 0)
+      s.c_last[b * s.d.dim + ch] = c[0], s.c_last[b * s.d.dim + ch + 1] = c[1];
+  }
+}
+
+// The gradients of the gates take their places in the stage and are stored
+// from there as boxes.
+template <typename T, bool RAGGED>
+__global__ void __launch_bounds__(32 * kBackwardWarps, 3)
+scan_backward_tiled_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Scan s,
+                           const float* __restrict__ dc_last, float* __restrict__ dc0,
+                           int* status) {
+  extern __shared__ uint8_t raw[];
+  __shared__ Joint<2> sh;
+  __shared__ Ring ring;
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, warps = blockDim.x / 32;
+  const int C = s.cluster;
+  const uint32_t rank = C > 1 ? tc::pair_rank() : 0;
+  const int rows = warps * kSegment;
+  const int64_t span = (int64_t)C * rows;
+  const int64_t marks = (s.d.steps + kSegment - 1) / kSegment;
+  const int stage_elems = 5 * rows * kBlock;
+  T* const stages = reinterpret_cast<T*>(raw + (128 - (tc::smem_u32(raw) & 127)) % 128);
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < kDepth; ++i) tc::mbar_init(&ring.full[i], 1);
+    tc::mbar_fence_init();
+    ring.abort = 0;
+  }
+  __syncthreads();
+  uint32_t filled = 0, used = 0;
+  for (int64_t item = blockIdx.x / C; item < s.d.batch * s.blocks; item += gridDim.x / C) {
+    const int64_t b = item / s.blocks;
+    const int ch0 = (int)(item % s.blocks) * kBlock;
+    const int64_t ch = ch0 + 2 * lane;
+    const bool on = ch < s.d.dim;
+    const int64_t n = length_of(s, b);
+    const int64_t rounds = (s.d.steps + span - 1) / span;  // the last ones may be past the end
+    float r[2] = {0.f, 0.f};
+    if (on && dc_last) r[0] = dc_last[b * s.d.dim + ch], r[1] = dc_last[b * s.d.dim + ch + 1];
+
+    // warp 0; of the stores that this thread has made, the newest may still read
+    // its stage: the stage filled here is an older one, except at an item's start
+    const auto fill = [&](int64_t round, bool start) {
+      const int st = filled++ % kDepth;
+      if (lane == 0) {
+        if (start) tc::bulk_wait_read();
+        else asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+        tc::mbar_arrive_expect_tx(&ring.full[st], stage_elems * sizeof(T));
+      }
+      __syncwarp();
+      if (lane < 5) {
+        const int t = (int)(round * span) + (int)rank * rows;
+        box_g2s(stages + (size_t)st * stage_elems + lane * rows * kBlock, &maps.in[lane], ch0,
+                maps.t_inner ? t : (int)b, maps.t_inner ? (int)b : t, &ring.full[st]);
+      }
+    };
+    // one stage less in flight than there are: the newest is being stored
+    if (warp == 0)
+      for (int64_t q = 0; q < kDepth - 1 && q < rounds; ++q) fill(rounds - 1 - q, true);
+
+    int64_t t0 = (rounds - 1) * span + (int64_t)(rank * warps + warp) * kSegment;
+    for (int64_t round = rounds - 1; round >= 0; --round, t0 -= span) {
+      const int st = used % kDepth;
+      float mark[2] = {0.f, 0.f};
+      if (on && t0 < n) {
+        const float2 x = *reinterpret_cast<const float2*>(
+            s.marks + (b * marks + t0 / kSegment) * s.d.dim + ch);
+        mark[0] = x.x, mark[1] = x.y;
+      }
+      ring_wait(ring, st, (used / kDepth) & 1, status);
+      ++used;
+      T* p = stages + (size_t)st * stage_elems + warp * kSegment * kBlock + 2 * lane;
+      const int gate = rows * kBlock;
+      // what each step adds to r, its f, and the factors that turn the gradient
+      // of its state into those of i, f and g
+      Two add[kSegment], f[kSegment], ki[kSegment], kf[kSegment], kg[kSegment];
+      Two c = two(mark[0], mark[1]);
+      const bool whole = t0 + kSegment <= n;
+#pragma unroll
+      for (int j = 0; j < kSegment; ++j) {
+        const Two ai = load_two(p + j * kBlock), af = load_two(p + gate + j * kBlock);
+        const Two ag = load_two(p + 2 * gate + j * kBlock);
+        const Two ao = load_two(p + 3 * gate + j * kBlock);
+        const Two y = load_two(p + 4 * gate + j * kBlock);
+        Two i, di, fg, df, g, dg, o, d_o, th, dth;
+        sigmoid_slope2(ai, i, di);
+        sigmoid_slope2(af, fg, df);
+        tanh_slope2(ag, g, dg);
+        sigmoid_slope2(ao, o, d_o);
+        const bool reset =
+            RAGGED && s.resets && t0 + j < n && s.resets[b * s.d.steps + t0 + j] != 0;
+        const Two prev = reset ? two(0.f) : c;
+        c = fma2(fg, prev, i * g);
+        tanh_slope2(c, th, dth);
+        add[j] = y * o * dth;
+        f[j] = reset ? two(0.f) : fg;
+        ki[j] = g * di;
+        kf[j] = prev * df;
+        kg[j] = i * dg;
+        Two od = y * th * d_o;
+        if (!whole && t0 + j >= n) {
+          add[j] = ki[j] = kf[j] = kg[j] = od = two(0.f);
+          f[j] = two(1.f);
+        }
+        store_two(p + 3 * gate + j * kBlock, od);
+      }
+      Two A = two(1.f), B = two(0.f);
+#pragma unroll
+      for (int j = kSegment - 1; j >= 0; --j) {
+        B = RAGGED ? apply2(f[j], f[j] * add[j], B) : f[j] * (add[j] + B);
+        A = A * f[j];
+      }
+      Map<2> m;
+      split(A, m.a[0], m.a[1]);
+      split(B, m.b[0], m.b[1]);
+      float in[2];
+      join<2, true>(sh, m, (int)(used & 1), C, rank, r, in);
+      Two x = two(in[0], in[1]);
+#pragma unroll
+      for (int j = kSegment - 1; j >= 0; --j) {
+        const Two dc = add[j] + x;
+        const bool dead = !whole && t0 + j >= n;
+        store_two(p + j * kBlock, dead ? two(0.f) : dc * ki[j]);
+        store_two(p + gate + j * kBlock, dead ? two(0.f) : dc * kf[j]);
+        store_two(p + 2 * gate + j * kBlock, dead ? two(0.f) : dc * kg[j]);
+        x = RAGGED ? apply2(f[j], two(0.f), dc) : f[j] * dc;
+      }
+      tc::fence_async_smem();
+      __syncthreads();
+      if (warp == 0) {
+        if (lane == 0) {
+          const int t = (int)(round * span) + (int)rank * rows;
+          if (t < s.d.steps) {
+            for (int k = 0; k < 4; ++k)
+              box_s2g(&maps.out[k], ch0, maps.t_inner ? t : (int)b, maps.t_inner ? (int)b : t,
+                      stages + (size_t)st * stage_elems + k * gate);
+          }
+          tc::bulk_commit();
+        }
+        __syncwarp();
+        if (round >= kDepth - 1) fill(round - (kDepth - 1), false);
+      }
+    }
+    if (dc0 && on && rank == 0 && warp == 0)
+      dc0[b * s.d.dim + ch] = r[0], dc0[b * s.d.dim + ch + 1] = r[1];
+    __syncwarp();
+  }
+  if (threadIdx.x == 0) tc::bulk_wait();
+}
+
 template <typename T, int V>
 __global__ void __launch_bounds__(128)
 scan_step_kernel(const T* __restrict__ gates, const __grid_constant__ Scan s,
@@ -498,14 +903,14 @@ struct Shape {
 
 // Warps of a CTA cover the steps as far as they go; CTAs are put together
 // along the time axis while the channels alone leave SMs without work.
-Shape shape(Scan* s, int V) {
+Shape shape(Scan* s, int V, int most_warps, int resident) {
   s->blocks = (s->d.dim + 32 * V - 1) / (32 * V);
   const int64_t items = s->d.batch * s->blocks;
   Shape f;
   f.warps = 1;
-  while (f.warps < kMaxWarps && f.warps * kSegment < s->d.steps) f.warps *= 2;
+  while (f.warps < most_warps && f.warps * kSegment < s->d.steps) f.warps *= 2;
   s->cluster = 1;
-  while (s->cluster < kMaxCluster && items * s->cluster < 2 * 152 &&
+  while (s->cluster < kMaxCluster && items * s->cluster < resident * 152 &&
          (int64_t)s->cluster * f.warps * kSegment < s->d.steps)
     s->cluster *= 2;
   const int64_t most = 1 << 20;
@@ -514,7 +919,12 @@ Shape shape(Scan* s, int V) {
 }
 
 template <typename K, typename... A>
-cudaError_t launch(K kernel, const Shape& f, int cluster, cudaStream_t st, A... args) {
+cudaError_t launch(K kernel, const Shape& f, int cluster, size_t smem, cudaStream_t st, A... args) {
+  if (smem) {
+    const cudaError_t e =
+        cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e != cudaSuccess) return e;
+  }
   cudaLaunchAttribute attr;
   attr.id = cudaLaunchAttributeClusterDimension;
   attr.val.clusterDim.x = (unsigned)cluster;
@@ -522,28 +932,112 @@ cudaError_t launch(K kernel, const Shape& f, int cluster, cudaStream_t st, A... 
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(f.grid);
   cfg.blockDim = dim3(32u * f.warps);
+  cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
   cfg.attrs = &attr;
   cfg.numAttrs = 1;
   return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
-template <typename T, int V>
-cudaError_t forward(const void* gates, Scan s, void* h, cudaStream_t st) {
-  const Shape f = shape(&s, V);
-  const bool ragged = s.lengths || s.resets;
-  return launch(ragged ? scan_forward_kernel<T, V, true> : scan_forward_kernel<T, V, false>, f,
-                s.cluster, st, static_cast<const T*>(gates), s, static_cast<T*>(h));
+// A [batch][steps][dim] tensor as a tensor map: its steps inside the sequences
+// (t_inner) or the other way round.
+struct Layout3 {
+  int64_t size[3], stride[2];
+};
+
+bool layout(const soma_scan_dims& d, const soma_scan_strides& s, bool t_inner, int dtype,
+            Layout3* l) {
+  const int64_t unit = dtype == SOMA_FP32 ? 4 : 8;  // elements of 16 bytes
+  const int64_t n1 = t_inner ? d.steps : d.batch, n2 = t_inner ? d.batch : d.steps;
+  int64_t s1 = t_inner ? s.t : s.b, s2 = t_inner ? s.b : s.t;
+  if (n1 == 1) s1 = (d.dim + unit - 1) / unit * unit;  // never stepped over
+  if (n2 == 1) s2 = n1 * s1;
+  *l = {{d.dim, n1, n2}, {s1, s2}};
+  return s1 % unit == 0 && s2 % unit == 0 && s1 >= d.dim && s2 >= n1 * s1 && s2 % s1 == 0 &&
+         s1 < ((int64_t)1 << 37) && s2 < ((int64_t)1 << 37);
 }
 
-template <typename T, int V>
-cudaError_t backward(const void* gates, Scan s, const void* dh, const float* dc_last,
-                     void* dgates, float* dc0, cudaStream_t st) {
-  const Shape f = shape(&s, V);
+bool mappable(const void* p, const soma_scan_dims& d, const soma_scan_strides& s, bool gates,
+              bool t_inner, int dtype) {
+  const int64_t unit = dtype == SOMA_FP32 ? 4 : 8;
+  Layout3 l;
+  return aligned(p, 16) && (!gates || s.g % unit == 0) && layout(d, s, t_inner, dtype, &l);
+}
+
+// Maps of one tensor's gates (or of the tensor itself), boxes of 64 channels
+// by `rows` steps of one sequence.
+bool map_all(CUtensorMap* maps, int count, const void* p, const soma_scan_dims& d,
+             const soma_scan_strides& s, bool t_inner, int dtype, int rows) {
+  Layout3 l;
+  if (!layout(d, s, t_inner, dtype, &l)) return false;
+  const int box[3] = {kBlock, t_inner ? rows : 1, t_inner ? 1 : rows};
+  for (int k = 0; k < count; ++k)
+    if (!make_box_map(&maps[k], static_cast<const uint8_t*>(p) + k * s.g * (int64_t)width(dtype),
+                      dtype, l.size, l.stride, box))
+      return false;
+  return true;
+}
+
+template <typename T>
+constexpr int dtype_of() {
+  return std::is_same<T, float>::value ? SOMA_FP32
+         : std::is_same<T, __half>::value ? SOMA_FP16 : SOMA_BF16;
+}
+
+template <typename T>
+size_t ring_bytes(int boxes, int warps) {
+  return (size_t)kDepth * boxes * warps * kSegment * kBlock * sizeof(T) + 128;
+}
+
+template <typename T>
+cudaError_t forward(const void* gates, Scan s, void* h, int* status, cudaStream_t st) {
+  constexpr int dtype = dtype_of<T>();
   const bool ragged = s.lengths || s.resets;
-  return launch(ragged ? scan_backward_kernel<T, V, true> : scan_backward_kernel<T, V, false>, f,
-                s.cluster, st, static_cast<const T*>(gates), s, static_cast<const T*>(dh), dc_last,
-                static_cast<T*>(dgates), dc0);
+  // h and the checkpoints are written two channels at a time
+  const bool direct = s.d.dim % 2 == 0 && aligned(h, 2 * sizeof(T)) && s.hs.b % 2 == 0 &&
+                      s.hs.t % 2 == 0 && aligned(s.marks, 8);
+  for (const bool t_inner : {true, false}) {
+    if (s.d.steps < 1 || !direct || !mappable(gates, s.d, s.gs, true, t_inner, dtype)) continue;
+    const Shape f = shape(&s, 2, sizeof(T) == 4 ? 4 : kMaxWarps, 2);
+    Maps maps;
+    maps.t_inner = t_inner;
+    if (!map_all(maps.in, 4, gates, s.d, s.gs, t_inner, dtype, f.warps * kSegment))
+      return cudaErrorInvalidValue;
+    return launch(ragged ? scan_forward_tiled_kernel<T, true> : scan_forward_tiled_kernel<T, false>,
+                  f, s.cluster, ring_bytes<T>(4, f.warps), st, maps, s, static_cast<T*>(h), status);
+  }
+  const Shape f = shape(&s, 1, kMaxWarps, 2);
+  return launch(ragged ? scan_forward_kernel<T, 1, true> : scan_forward_kernel<T, 1, false>, f,
+                s.cluster, 0, st, static_cast<const T*>(gates), s, static_cast<T*>(h));
+}
+
+template <typename T>
+cudaError_t backward(const void* gates, Scan s, const void* dh, const float* dc_last,
+                     void* dgates, float* dc0, int* status, cudaStream_t st) {
+  constexpr int dtype = dtype_of<T>();
+  const bool ragged = s.lengths || s.resets;
+  for (const bool t_inner : {true, false}) {
+    if (s.d.steps < 1 || s.d.dim % 2 || !aligned(s.marks, 8) ||
+        !mappable(gates, s.d, s.gs, true, t_inner, dtype) ||
+        !mappable(dh, s.d, s.hs, false, t_inner, dtype) ||
+        !mappable(dgates, s.d, s.ds, true, t_inner, dtype))
+      continue;
+    const Shape f = shape(&s, 2, sizeof(T) == 4 ? 2 : kBackwardWarps, 3);
+    const int rows = f.warps * kSegment;
+    Maps maps;
+    maps.t_inner = t_inner;
+    if (!map_all(maps.in, 4, gates, s.d, s.gs, t_inner, dtype, rows) ||
+        !map_all(maps.in + 4, 1, dh, s.d, s.hs, t_inner, dtype, rows) ||
+        !map_all(maps.out, 4, dgates, s.d, s.ds, t_inner, dtype, rows))
+      return cudaErrorInvalidValue;
+    return launch(
+        ragged ? scan_backward_tiled_kernel<T, true> : scan_backward_tiled_kernel<T, false>, f,
+        s.cluster, ring_bytes<T>(5, f.warps), st, maps, s, dc_last, dc0, status);
+  }
+  const Shape f = shape(&s, 1, kMaxWarps, 1);
+  return launch(ragged ? scan_backward_kernel<T, 1, true> : scan_backward_kernel<T, 1, false>, f,
+                s.cluster, 0, st, static_cast<const T*>(gates), s, static_cast<const T*>(dh),
+                dc_last, static_cast<T*>(dgates), dc0);
 }
 
 template <typename T, int V>
@@ -582,14 +1076,12 @@ int soma_scan_forward(const void* gates, soma_scan_strides gate_strides, int dty
   const Scan s = {d,       gate_strides, h_strides, {0, 0, 0},   c0,
                   lengths, resets,       c_last,    checkpoints, 0, 1};
   const cudaStream_t st = (cudaStream_t)stream;
-  const bool two = d.dim % 2 == 0 && pairs(gates, gate_strides) && pairs(h, h_strides);
+  int* status = status_ptr();
+  if (!status) return SOMA_ERR_CUDA;
   trace_begin(SOMA_TRACE_GATE, st);
-  cudaError_t e;
-  if (dtype == SOMA_FP32) e = forward<float, 1>(gates, s, h, st);
-  else if (dtype == SOMA_BF16)
-    e = two ? forward<__nv_bfloat16, 2>(gates, s, h, st) : forward<__nv_bfloat16, 1>(gates, s, h, st);
-  else
-    e = two ? forward<__half, 2>(gates, s, h, st) : forward<__half, 1>(gates, s, h, st);
+  const cudaError_t e = dtype == SOMA_FP32   ? forward<float>(gates, s, h, status, st)
+                        : dtype == SOMA_BF16 ? forward<__nv_bfloat16>(gates, s, h, status, st)
+                                             : forward<__half>(gates, s, h, status, st);
   trace_end(SOMA_TRACE_GATE, st);
   return e == cudaSuccess ? SOMA_OK : SOMA_ERR_CUDA;
 }
@@ -612,17 +1104,13 @@ int soma_scan_backward(const void* gates, soma_scan_strides gate_strides, int dt
                   nullptr, lengths,      resets,     nullptr,
                   const_cast<float*>(checkpoints), 0, 1};
   const cudaStream_t st = (cudaStream_t)stream;
-  const bool two = d.dim % 2 == 0 && pairs(gates, gate_strides) && pairs(dh, dh_strides) &&
-                   pairs(dgates, dgate_strides);
+  int* status = status_ptr();
+  if (!status) return SOMA_ERR_CUDA;
   trace_begin(SOMA_TRACE_GATE, st);
-  cudaError_t e;
-  if (dtype == SOMA_FP32) e = backward<float, 1>(gates, s, dh, dc_last, dgates, dc0, st);
-  else if (dtype == SOMA_BF16)
-    e = two ? backward<__nv_bfloat16, 2>(gates, s, dh, dc_last, dgates, dc0, st)
-            : backward<__nv_bfloat16, 1>(gates, s, dh, dc_last, dgates, dc0, st);
-  else
-    e = two ? backward<__half, 2>(gates, s, dh, dc_last, dgates, dc0, st)
-            : backward<__half, 1>(gates, s, dh, dc_last, dgates, dc0, st);
+  const cudaError_t e =
+      dtype == SOMA_FP32   ? backward<float>(gates, s, dh, dc_last, dgates, dc0, status, st)
+      : dtype == SOMA_BF16 ? backward<__nv_bfloat16>(gates, s, dh, dc_last, dgates, dc0, status, st)
+                           : backward<__half>(gates, s, dh, dc_last, dgates, dc0, status, st);
   trace_end(SOMA_TRACE_GATE, st);
   return e == cudaSuccess ? SOMA_OK : SOMA_ERR_CUDA;
 }

@@ -184,4 +184,11 @@ __device__ __forceinline__ float ex2(float x) {
 bool make_tile_map(CUtensorMap* map, const void* base, int dtype, int64_t rows, int64_t cols,
                    int64_t stride, int box_rows);
 
+// Tensor map of a 3-D tensor, the first dimension adjacent and `stride`
+// elements between neighbours of the other two, in plain boxes (no swizzle).
+// The address must be 16-byte aligned, the strides multiples of 16 bytes, the
+// second a multiple of the first and neither shorter than what it steps over.
+bool make_box_map(CUtensorMap* map, const void* base, int dtype, const int64_t (&size)[3],
+                  const int64_t (&stride)[2], const int (&box_size)[3]);
+
 }  // namespace soma
