@@ -232,9 +232,9 @@ __device__ __forceinline__ void apply(const Map<V>& m, float (&c)[V]) {
   for (int v = 0; v < V; ++v) c[v] = apply(m.a[v], m.b[v], c[v]);
 }
 
-template <int V>
+template <int V, int WARPS>
 struct Joint {
-  Map<V> warp[2][kMaxWarps][32];
+  Map<V> warp[2][WARPS][32];
   Map<V> cta[2][kMaxCluster][32];
 };
 
@@ -242,8 +242,8 @@ struct Joint {
 // last to the first).  c: in, what reaches the cluster's first (last) segment,
 // the same in all its warps; out, what leaves its last (first).  `in` becomes
 // what reaches this warp's.
-template <int V, bool REVERSE>
-__device__ __forceinline__ void join(Joint<V>& sh, const Map<V>& mine, int round, int cluster,
+template <bool REVERSE, int V, int WARPS>
+__device__ __forceinline__ void join(Joint<V, WARPS>& sh, const Map<V>& mine, int round, int cluster,
                                      uint32_t rank, float (&c)[V], float (&in)[V]) {
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, warps = blockDim.x / 32;
   const int buf = round & 1;
@@ -306,7 +306,7 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2)
 scan_forward_kernel(const T* __restrict__ gates, const __grid_constant__ Scan s,
                     T* __restrict__ h) {
   using B = typename Bits<T, V>::type;
-  __shared__ Joint<V> sh;
+  __shared__ Joint<V, kMaxWarps> sh;
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, warps = blockDim.x / 32;
   const int C = s.cluster;
   const uint32_t rank = C > 1 ? tc::pair_rank() : 0;
@@ -365,7 +365,7 @@ scan_forward_kernel(const T* __restrict__ gates, const __grid_constant__ Scan s,
       }
       fetch(t0 + span);
       float in[V];
-      join<V, false>(sh, m, round, C, rank, c, in);
+      join<false>(sh, m, round, C, rank, c, in);
       if (!on) continue;
       if (s.marks && t0 < s.d.steps) {
         float* p = s.marks + (b * marks + t0 / kSegment) * s.d.dim + ch;
@@ -400,7 +400,7 @@ scan_backward_kernel(const T* __restrict__ gates, const __grid_constant__ Scan s
                      const T* __restrict__ dh, const float* __restrict__ dc_last,
                      T* __restrict__ dgates, float* __restrict__ dc0) {
   using B = typename Bits<T, V>::type;
-  __shared__ Joint<V> sh;
+  __shared__ Joint<V, kMaxWarps> sh;
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, warps = blockDim.x / 32;
   const int C = s.cluster;
   const uint32_t rank = C > 1 ? tc::pair_rank() : 0;
@@ -491,7 +491,7 @@ scan_backward_kernel(const T* __restrict__ gates, const __grid_constant__ Scan s
         }
       fetch(t0 - span);
       float in[V];
-      join<V, true>(sh, m, round, C, rank, r, in);
+      join<true>(sh, m, round, C, rank, r, in);
       if (!on) continue;
 #pragma unroll
       for (int j = kSegment - 1; j >= 0; --j) {
@@ -602,7 +602,7 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2)
 scan_forward_tiled_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Scan s,
                           T* __restrict__ h, int* status) {
   extern __shared__ uint8_t raw[];
-  __shared__ Joint<2> sh;
+  __shared__ Joint<2, kMaxWarps> sh;
   __shared__ Ring ring;
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, warps = blockDim.x / 32;
   const int C = s.cluster;
@@ -651,7 +651,9 @@ scan_forward_tiled_kernel(const __grid_constant__ Maps maps, const __grid_consta
       const int gate = rows * kBlock;
       Two f[kSegment], u[kSegment], o[kSegment];
       Two A = two(1.f), B = two(0.f);
-      const bool whole = t0 + kSegment <= n;  // no step past the end (the whole warp)
+      // steps of this segment that exist: nearly always all of them, and the
+      // whole warp takes the branch without their checks
+      const int live = n - t0 >= kSegment ? kSegment : n > t0 ? (int)(n - t0) : 0;
 #pragma unroll
       for (int j = 0; j < kSegment; ++j) {
         const Two ai = load_two(p + j * kBlock), af = load_two(p + gate + j * kBlock);
@@ -661,8 +663,19 @@ scan_forward_tiled_kernel(const __grid_constant__ Maps maps, const __grid_consta
         tanh_parts2(ag, num, den);
         u[j] = num * rcp2(den * one_exp2(ai));
         f[j] = rcp2(one_exp2(af));
-        if (RAGGED && s.resets && t0 + j < n && s.resets[b * s.d.steps + t0 + j]) f[j] = two(0.f);
-        if (!whole && t0 + j >= n) f[j] = two(1.f), u[j] = two(0.f);
+      }
+      if (RAGGED && s.resets) {
+#pragma unroll
+        for (int j = 0; j < kSegment; ++j)
+          if (j < live && s.resets[b * s.d.steps + t0 + j]) f[j] = two(0.f);
+      }
+      if (live < kSegment) {
+#pragma unroll
+        for (int j = 0; j < kSegment; ++j)
+          if (j >= live) f[j] = two(1.f), u[j] = two(0.f);
+      }
+#pragma unroll
+      for (int j = 0; j < kSegment; ++j) {
         B = RAGGED ? apply2(f[j], u[j], B) : fma2(f[j], B, u[j]);
         A = A * f[j];
       }
@@ -670,7 +683,7 @@ scan_forward_tiled_kernel(const __grid_constant__ Maps maps, const __grid_consta
       split(A, m.a[0], m.a[1]);
       split(B, m.b[0], m.b[1]);
       float in[2];
-      join<2, false>(sh, m, (int)(used & 1), C, rank, c, in);
+      join<false>(sh, m, (int)(used & 1), C, rank, c, in);
       // every warp has read the stage
       if (warp == 0 && round + kDepth < rounds) fill(round + kDepth);
       if (on) {
@@ -685,8 +698,8 @@ scan_forward_tiled_kernel(const __grid_constant__ Maps maps, const __grid_consta
           Two num, den;
           tanh_parts2(x, num, den);
           const Two y = num * rcp2(den * one_exp2(o[j]));
-          if (whole || t0 + j < n) store_two(q, y);
-          else if (t0 + j < s.d.steps) store_two(q, two(0.f));
+          if (live == kSegment) store_two(q, y);
+          else if (t0 + j < s.d.steps) store_two(q, j < live ? y : two(0.f));
           q += s.hs.t;
         }
       }
@@ -711,7 +724,7 @@ scan_backward_tiled_kernel(const __grid_constant__ Maps maps, const __grid_const
                            const float* __restrict__ dc_last, float* __restrict__ dc0,
                            int* status) {
   extern __shared__ uint8_t raw[];
-  __shared__ Joint<2> sh;
+  __shared__ Joint<2, kBackwardWarps> sh;
   __shared__ Ring ring;
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, warps = blockDim.x / 32;
   const int C = s.cluster;
@@ -775,7 +788,7 @@ scan_backward_tiled_kernel(const __grid_constant__ Maps maps, const __grid_const
       // of its state into those of i, f and g
       Two add[kSegment], f[kSegment], ki[kSegment], kf[kSegment], kg[kSegment];
       Two c = two(mark[0], mark[1]);
-      const bool whole = t0 + kSegment <= n;
+      const int live = n - t0 >= kSegment ? kSegment : n > t0 ? (int)(n - t0) : 0;
 #pragma unroll
       for (int j = 0; j < kSegment; ++j) {
         const Two ai = load_two(p + j * kBlock), af = load_two(p + gate + j * kBlock);
@@ -788,7 +801,7 @@ scan_backward_tiled_kernel(const __grid_constant__ Maps maps, const __grid_const
         tanh_slope2(ag, g, dg);
         sigmoid_slope2(ao, o, d_o);
         const bool reset =
-            RAGGED && s.resets && t0 + j < n && s.resets[b * s.d.steps + t0 + j] != 0;
+            RAGGED && s.resets && j < live && s.resets[b * s.d.steps + t0 + j] != 0;
         const Two prev = reset ? two(0.f) : c;
         c = fma2(fg, prev, i * g);
         tanh_slope2(c, th, dth);
@@ -797,12 +810,16 @@ scan_backward_tiled_kernel(const __grid_constant__ Maps maps, const __grid_const
         ki[j] = g * di;
         kf[j] = prev * df;
         kg[j] = i * dg;
-        Two od = y * th * d_o;
-        if (!whole && t0 + j >= n) {
-          add[j] = ki[j] = kf[j] = kg[j] = od = two(0.f);
-          f[j] = two(1.f);
-        }
-        store_two(p + 3 * gate + j * kBlock, od);
+        store_two(p + 3 * gate + j * kBlock, y * th * d_o);
+      }
+      if (live < kSegment) {
+#pragma unroll
+        for (int j = 0; j < kSegment; ++j)
+          if (j >= live) {
+            add[j] = ki[j] = kf[j] = kg[j] = two(0.f);
+            f[j] = two(1.f);
+            store_two(p + 3 * gate + j * kBlock, two(0.f));
+          }
       }
       Two A = two(1.f), B = two(0.f);
 #pragma unroll
@@ -814,16 +831,21 @@ scan_backward_tiled_kernel(const __grid_constant__ Maps maps, const __grid_const
       split(A, m.a[0], m.a[1]);
       split(B, m.b[0], m.b[1]);
       float in[2];
-      join<2, true>(sh, m, (int)(used & 1), C, rank, r, in);
+      join<true>(sh, m, (int)(used & 1), C, rank, r, in);
       Two x = two(in[0], in[1]);
 #pragma unroll
       for (int j = kSegment - 1; j >= 0; --j) {
         const Two dc = add[j] + x;
-        const bool dead = !whole && t0 + j >= n;
-        store_two(p + j * kBlock, dead ? two(0.f) : dc * ki[j]);
-        store_two(p + gate + j * kBlock, dead ? two(0.f) : dc * kf[j]);
-        store_two(p + 2 * gate + j * kBlock, dead ? two(0.f) : dc * kg[j]);
+        store_two(p + j * kBlock, dc * ki[j]);
+        store_two(p + gate + j * kBlock, dc * kf[j]);
+        store_two(p + 2 * gate + j * kBlock, dc * kg[j]);
         x = RAGGED ? apply2(f[j], two(0.f), dc) : f[j] * dc;
+      }
+      if (live < kSegment) {  // an infinite dc times 0 is no gradient
+#pragma unroll
+        for (int j = 0; j < kSegment; ++j)
+          if (j >= live)
+            for (int k = 0; k < 3; ++k) store_two(p + k * gate + j * kBlock, two(0.f));
       }
       tc::fence_async_smem();
       __syncthreads();
