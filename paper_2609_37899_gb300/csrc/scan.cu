@@ -21,6 +21,9 @@
 // and 8 written backward.  The instructions come close: 113 per element (one
 // channel at a time, a 64-bit address and a bounds check per load) took 2.7
 // times the bytes' time.
+#include <cmath>
+#include <initializer_list>
+
 #define SOMA_CHECK_FILE 9
 #include "checked.cuh"
 #include "numeric.cuh"
@@ -34,7 +37,7 @@ namespace {
 
 constexpr int kSegment = 8;     // steps of a warp, and between two checkpoints
 constexpr int kMaxWarps = 8;    // of a CTA
-constexpr int kMaxCluster = 8;
+constexpr int kMaxCluster = 16;
 constexpr float kLog2e = 1.4426950408889634f;
 
 __device__ __forceinline__ float rcp(float x) {
@@ -217,7 +220,7 @@ __device__ __forceinline__ typename Bits<T, V>::type pack(const float (&x)[V]) {
 
 // The map c -> a c + b.
 template <int V>
-struct Map {
+struct __align__(8 * V) Map {
   float a[V], b[V];
 };
 
@@ -226,52 +229,70 @@ __device__ __forceinline__ float apply(float a, float b, float c) {
   return a == 0.f ? b : fmaf(a, c, b);
 }
 
-template <int V>
+template <bool RAGGED, int V>
 __device__ __forceinline__ void apply(const Map<V>& m, float (&c)[V]) {
 #pragma unroll
-  for (int v = 0; v < V; ++v) c[v] = apply(m.a[v], m.b[v], c[v]);
+  for (int v = 0; v < V; ++v)
+    c[v] = RAGGED ? apply(m.a[v], m.b[v], c[v]) : fmaf(m.a[v], c[v], m.b[v]);
 }
 
-template <int V, int WARPS>
+// Where the maps are exchanged: [2][warps][32] of this CTA, and in clusters
+// [2][CTAs][32] that every CTA writes into all of them.
+template <int V>
 struct Joint {
-  Map<V> warp[2][WARPS][32];
-  Map<V> cta[2][kMaxCluster][32];
+  Map<V>* warp;
+  Map<V>* cta;
 };
 
-// Joins the maps of a cluster's segments (in time order; `reverse`: from the
+template <int V>
+__host__ __device__ constexpr size_t joint_bytes(int warps, int cluster) {
+  return sizeof(Map<V>) * 64 * (warps + (cluster > 1 ? cluster : 0));
+}
+
+template <int V>
+__device__ __forceinline__ Joint<V> joint_at(void* p, int warps) {
+  Map<V>* const m = static_cast<Map<V>*>(p);
+  return {m, m + 64 * warps};
+}
+
+// Joins the maps of a cluster's segments (in time order; REVERSE: from the
 // last to the first).  c: in, what reaches the cluster's first (last) segment,
 // the same in all its warps; out, what leaves its last (first).  `in` becomes
 // what reaches this warp's.
-template <bool REVERSE, int V, int WARPS>
-__device__ __forceinline__ void join(Joint<V, WARPS>& sh, const Map<V>& mine, int round, int cluster,
-                                     uint32_t rank, float (&c)[V], float (&in)[V]) {
+template <bool REVERSE, bool RAGGED, int WARPS, int V>
+__device__ __forceinline__ void join(const Joint<V>& sh, const Map<V>& mine, int round,
+                                     int cluster, uint32_t rank, float (&c)[V], float (&in)[V]) {
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, warps = blockDim.x / 32;
-  const int buf = round & 1;
+  Map<V>* const of_warp = sh.warp + (round & 1) * warps * 32 + lane;
+  Map<V>* const of_cta = sh.cta + (round & 1) * cluster * 32 + lane;
   __syncwarp();  // lanes past the last channel left the round early
-  sh.warp[buf][warp][lane] = mine;
+  of_warp[warp * 32] = mine;
   __syncthreads();
   const auto at = [](int j, int n) { return REVERSE ? n - 1 - j : j; };
   if (cluster > 1) {
-    Map<V> all = sh.warp[buf][at(0, warps)][lane];
-    for (int j = 1; j < warps; ++j) {
-      const Map<V> m = sh.warp[buf][at(j, warps)][lane];
+    if (warp < cluster) {
+      Map<V> all = of_warp[at(0, warps) * 32];
 #pragma unroll
-      for (int v = 0; v < V; ++v) {
-        all.b[v] = apply(m.a[v], m.b[v], all.b[v]);
-        all.a[v] *= m.a[v];
+      for (int j = 1; j < WARPS; ++j) {
+        if (j >= warps) break;
+        const Map<V> m = of_warp[at(j, warps) * 32];
+        apply<RAGGED>(m, all.b);
+#pragma unroll
+        for (int v = 0; v < V; ++v) all.a[v] *= m.a[v];
       }
-    }
-    for (int to = warp; to < cluster; to += warps) {
-      uint32_t addr;
-      asm("mapa.shared::cluster.u32 %0, %1, %2;"
-          : "=r"(addr)
-          : "r"(tc::smem_u32(&sh.cta[buf][rank][lane])), "r"(to));
-#pragma unroll
-      for (int v = 0; v < V; ++v) {
-        asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(addr + 4 * v), "f"(all.a[v])
-                     : "memory");
-        asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(addr + 4 * (V + v)), "f"(all.b[v])
-                     : "memory");
+      for (int to = warp; to < cluster; to += warps) {
+        uint32_t addr;
+        asm("mapa.shared::cluster.u32 %0, %1, %2;"
+            : "=r"(addr)
+            : "r"(tc::smem_u32(of_cta + rank * 32)), "r"(to));
+        if (V == 2)
+          asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(addr),
+                       "f"(all.a[0]), "f"(all.a[V - 1]), "f"(all.b[0]), "f"(all.b[V - 1])
+                       : "memory");
+        else
+          asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(addr), "f"(all.a[0]),
+                       "f"(all.b[0])
+                       : "memory");
       }
     }
     tc::cluster_sync();
@@ -281,21 +302,24 @@ __device__ __forceinline__ void join(Joint<V, WARPS>& sh, const Map<V>& mine, in
 #pragma unroll
         for (int v = 0; v < V; ++v) in[v] = c[v];
       }
-      apply(sh.cta[buf][r][lane], c);
+      apply<RAGGED>(of_cta[r * 32], c);
     }
-    for (int j = 0; j < warps; ++j) {
+#pragma unroll
+    for (int j = 0; j < WARPS - 1; ++j) {
       const int w = at(j, warps);
-      if (w == warp) break;
-      apply(sh.warp[buf][w][lane], in);
+      if (j >= warps || w == warp) break;
+      apply<RAGGED>(of_warp[w * 32], in);
     }
   } else {
-    for (int j = 0; j < warps; ++j) {
+#pragma unroll
+    for (int j = 0; j < WARPS; ++j) {
       const int w = at(j, warps);
+      if (j >= warps) break;
       if (w == warp) {
 #pragma unroll
         for (int v = 0; v < V; ++v) in[v] = c[v];
       }
-      apply(sh.warp[buf][w][lane], c);
+      apply<RAGGED>(of_warp[w * 32], c);
     }
   }
 }
@@ -306,10 +330,11 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2)
 scan_forward_kernel(const T* __restrict__ gates, const __grid_constant__ Scan s,
                     T* __restrict__ h) {
   using B = typename Bits<T, V>::type;
-  __shared__ Joint<V, kMaxWarps> sh;
+  extern __shared__ __align__(16) uint8_t raw[];
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, warps = blockDim.x / 32;
   const int C = s.cluster;
   const uint32_t rank = C > 1 ? tc::pair_rank() : 0;
+  const Joint<V> sh = joint_at<V>(raw, warps);
   const int64_t span = (int64_t)C * warps * kSegment;  // steps of the cluster's round
   const int64_t marks = (s.d.steps + kSegment - 1) / kSegment;
   int round = 0;
@@ -365,7 +390,7 @@ scan_forward_kernel(const T* __restrict__ gates, const __grid_constant__ Scan s,
       }
       fetch(t0 + span);
       float in[V];
-      join<false>(sh, m, round, C, rank, c, in);
+      join<false, RAGGED, kMaxWarps>(sh, m, round, C, rank, c, in);
       if (!on) continue;
       if (s.marks && t0 < s.d.steps) {
         float* p = s.marks + (b * marks + t0 / kSegment) * s.d.dim + ch;
@@ -400,10 +425,11 @@ scan_backward_kernel(const T* __restrict__ gates, const __grid_constant__ Scan s
                      const T* __restrict__ dh, const float* __restrict__ dc_last,
                      T* __restrict__ dgates, float* __restrict__ dc0) {
   using B = typename Bits<T, V>::type;
-  __shared__ Joint<V, kMaxWarps> sh;
+  extern __shared__ __align__(16) uint8_t raw[];
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, warps = blockDim.x / 32;
   const int C = s.cluster;
   const uint32_t rank = C > 1 ? tc::pair_rank() : 0;
+  const Joint<V> sh = joint_at<V>(raw, warps);
   const int64_t span = (int64_t)C * warps * kSegment;
   const int64_t marks = (s.d.steps + kSegment - 1) / kSegment;
   int round = 0;
@@ -491,7 +517,7 @@ scan_backward_kernel(const T* __restrict__ gates, const __grid_constant__ Scan s
         }
       fetch(t0 - span);
       float in[V];
-      join<true>(sh, m, round, C, rank, r, in);
+      join<true, RAGGED, kMaxWarps>(sh, m, round, C, rank, r, in);
       if (!on) continue;
 #pragma unroll
       for (int j = kSegment - 1; j >= 0; --j) {
@@ -519,9 +545,14 @@ scan_backward_kernel(const T* __restrict__ gates, const __grid_constant__ Scan s
 }
 
 // ---- tiled ----------------------------------------------------------------
-constexpr int kDepth = 3;          // stages of the ring
-constexpr int kBackwardWarps = 4;  // of a CTA: its registers allow three such on an SM
-constexpr int kBlock = 64;         // channels of a CTA: 32 lanes of two
+constexpr int kBlock = 64;  // channels of a CTA: 32 lanes of two
+// Stages of the ring.  Forward, one is read to the end of its round; backward,
+// one more is being stored.
+constexpr int kForwardDepth = 2;
+constexpr int kBackwardDepth = 3;
+// CTAs of so many warps that an SM's registers hold.
+constexpr int forward_resident(int warps) { return 20 / warps; }
+constexpr int backward_resident(int warps) { return 12 / warps; }
 
 // The tensors of a call as boxes of 64 channels by the CTA's steps: one map
 // per gate, then dh.
@@ -585,7 +616,7 @@ __device__ __forceinline__ Two apply2(Two a, Two b, Two c) {
 }
 
 struct Ring {
-  uint64_t full[kDepth];
+  uint64_t full[kBackwardDepth];
   volatile int abort;
 };
 
@@ -597,12 +628,12 @@ __device__ __forceinline__ void ring_wait(Ring& r, int stage, uint32_t parity, i
 
 // RAGGED: lengths or resets are given.  h is written directly: a row of a
 // warp's store is 128 bytes.
-template <typename T, bool RAGGED>
-__global__ void __launch_bounds__(32 * kMaxWarps, 2)
+template <typename T, bool RAGGED, int WARPS>
+__global__ void __launch_bounds__(32 * WARPS, forward_resident(WARPS))
 scan_forward_tiled_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Scan s,
                           T* __restrict__ h, int* status) {
   extern __shared__ uint8_t raw[];
-  __shared__ Joint<2, kMaxWarps> sh;
+  constexpr int kDepth = kForwardDepth;
   __shared__ Ring ring;
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, warps = blockDim.x / 32;
   const int C = s.cluster;
@@ -612,6 +643,7 @@ scan_forward_tiled_kernel(const __grid_constant__ Maps maps, const __grid_consta
   const int64_t marks = (s.d.steps + kSegment - 1) / kSegment;
   const int stage_elems = 4 * rows * kBlock;
   T* const stages = reinterpret_cast<T*>(raw + (128 - (tc::smem_u32(raw) & 127)) % 128);
+  const Joint<2> sh = joint_at<2>(stages + (size_t)kDepth * stage_elems, warps);
   if (threadIdx.x == 0) {
     for (int i = 0; i < kDepth; ++i) tc::mbar_init(&ring.full[i], 1);
     tc::mbar_fence_init();
@@ -626,6 +658,7 @@ scan_forward_tiled_kernel(const __grid_constant__ Maps maps, const __grid_consta
     const bool on = ch < s.d.dim;
     const int64_t n = length_of(s, b);
     const int64_t rounds = (n + span - 1) / span;
+    if (item >= gridDim.x / C) __syncthreads();  // the last item's stages have been read
     float c[2] = {0.f, 0.f};
     if (on && s.c0) c[0] = s.c0[b * s.d.dim + ch], c[1] = s.c0[b * s.d.dim + ch + 1];
 
@@ -639,8 +672,10 @@ scan_forward_tiled_kernel(const __grid_constant__ Maps maps, const __grid_consta
                 maps.t_inner ? t : (int)b, maps.t_inner ? (int)b : t, &ring.full[st]);
       }
     };
+    // one stage less in flight than there are: the newest is read to the end of
+    // its round
     if (warp == 0)
-      for (int64_t q = 0; q < kDepth && q < rounds; ++q) fill(q);
+      for (int64_t q = 0; q < kDepth - 1 && q < rounds; ++q) fill(q);
 
     int64_t t0 = (int64_t)(rank * warps + warp) * kSegment;
     for (int64_t round = 0; round < rounds; ++round, t0 += span) {
@@ -649,7 +684,7 @@ scan_forward_tiled_kernel(const __grid_constant__ Maps maps, const __grid_consta
       ++used;
       const T* p = stages + (size_t)st * stage_elems + warp * kSegment * kBlock + 2 * lane;
       const int gate = rows * kBlock;
-      Two f[kSegment], u[kSegment], o[kSegment];
+      Two f[kSegment], u[kSegment];
       Two A = two(1.f), B = two(0.f);
       // steps of this segment that exist: nearly always all of them, and the
       // whole warp takes the branch without their checks
@@ -658,7 +693,6 @@ scan_forward_tiled_kernel(const __grid_constant__ Maps maps, const __grid_consta
       for (int j = 0; j < kSegment; ++j) {
         const Two ai = load_two(p + j * kBlock), af = load_two(p + gate + j * kBlock);
         const Two ag = load_two(p + 2 * gate + j * kBlock);
-        o[j] = load_two(p + 3 * gate + j * kBlock);
         Two num, den;
         tanh_parts2(ag, num, den);
         u[j] = num * rcp2(den * one_exp2(ai));
@@ -683,9 +717,9 @@ scan_forward_tiled_kernel(const __grid_constant__ Maps maps, const __grid_consta
       split(A, m.a[0], m.a[1]);
       split(B, m.b[0], m.b[1]);
       float in[2];
-      join<false>(sh, m, (int)(used & 1), C, rank, c, in);
-      // every warp has read the stage
-      if (warp == 0 && round + kDepth < rounds) fill(round + kDepth);
+      join<false, RAGGED, WARPS>(sh, m, (int)(used & 1), C, rank, c, in);
+      // every warp is through with the stage of the round before
+      if (warp == 0 && round + kDepth - 1 < rounds) fill(round + kDepth - 1);
       if (on) {
         if (s.marks && t0 < s.d.steps)
           *reinterpret_cast<float2*>(s.marks + (b * marks + t0 / kSegment) * s.d.dim + ch) =
@@ -697,7 +731,7 @@ scan_forward_tiled_kernel(const __grid_constant__ Maps maps, const __grid_consta
           x = RAGGED ? apply2(f[j], u[j], x) : fma2(f[j], x, u[j]);
           Two num, den;
           tanh_parts2(x, num, den);
-          const Two y = num * rcp2(den * one_exp2(o[j]));
+          const Two y = num * rcp2(den * one_exp2(load_two(p + 3 * gate + j * kBlock)));
           if (live == kSegment) store_two(q, y);
           else if (t0 + j < s.d.steps) store_two(q, j < live ? y : two(0.f));
           q += s.hs.t;
@@ -718,13 +752,13 @@ scan_forward_tiled_kernel(const __grid_constant__ Maps maps, const __grid_consta
 
 // The gradients of the gates take their places in the stage and are stored
 // from there as boxes.
-template <typename T, bool RAGGED>
-__global__ void __launch_bounds__(32 * kBackwardWarps, 3)
+template <typename T, bool RAGGED, int WARPS>
+__global__ void __launch_bounds__(32 * WARPS, backward_resident(WARPS))
 scan_backward_tiled_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Scan s,
                            const float* __restrict__ dc_last, float* __restrict__ dc0,
                            int* status) {
   extern __shared__ uint8_t raw[];
-  __shared__ Joint<2, kBackwardWarps> sh;
+  constexpr int kDepth = kBackwardDepth;
   __shared__ Ring ring;
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, warps = blockDim.x / 32;
   const int C = s.cluster;
@@ -734,6 +768,7 @@ scan_backward_tiled_kernel(const __grid_constant__ Maps maps, const __grid_const
   const int64_t marks = (s.d.steps + kSegment - 1) / kSegment;
   const int stage_elems = 5 * rows * kBlock;
   T* const stages = reinterpret_cast<T*>(raw + (128 - (tc::smem_u32(raw) & 127)) % 128);
+  const Joint<2> sh = joint_at<2>(stages + (size_t)kDepth * stage_elems, warps);
   if (threadIdx.x == 0) {
     for (int i = 0; i < kDepth; ++i) tc::mbar_init(&ring.full[i], 1);
     tc::mbar_fence_init();
@@ -831,7 +866,7 @@ scan_backward_tiled_kernel(const __grid_constant__ Maps maps, const __grid_const
       split(A, m.a[0], m.a[1]);
       split(B, m.b[0], m.b[1]);
       float in[2];
-      join<true>(sh, m, (int)(used & 1), C, rank, r, in);
+      join<true, RAGGED, WARPS>(sh, m, (int)(used & 1), C, rank, r, in);
       Two x = two(in[0], in[1]);
 #pragma unroll
       for (int j = kSegment - 1; j >= 0; --j) {
@@ -919,34 +954,53 @@ bool pairs(const void* p, const soma_scan_strides& s) {
 }
 
 struct Shape {
-  int warps;
+  int warps, most;  // of a CTA, and of the kernel compiled for it
   unsigned grid;
 };
 
-// Warps of a CTA cover the steps as far as they go; CTAs are put together
-// along the time axis while the channels alone leave SMs without work.
-Shape shape(Scan* s, int V, int most_warps, int resident) {
+// How the work is cut: CTAs of up to `most` warps (resident[k] of `most >> k`
+// fit an SM) along the steps, and CTAs of a cluster.  All CTAs of a call
+// together on the GPU finish soonest: 704 items (32 x 2048 x 1376) in CTAs of
+// eight warps are 2.3 waves of 304 and took three (222 us forward), in CTAs of
+// four they are one of 760.  What is left is the SM with the most CTAs, too
+// few warps to fill an SM, and the price of a cluster's barrier (clusters of
+// eight of the same work, 18.5 waves: 290 us).
+Shape shape(Scan* s, int V, int most, std::initializer_list<int> resident) {
   s->blocks = (s->d.dim + 32 * V - 1) / (32 * V);
   const int64_t items = s->d.batch * s->blocks;
-  Shape f;
-  f.warps = 1;
-  while (f.warps < most_warps && f.warps * kSegment < s->d.steps) f.warps *= 2;
-  s->cluster = 1;
-  while (s->cluster < kMaxCluster && items * s->cluster < resident * 152 &&
-         (int64_t)s->cluster * f.warps * kSegment < s->d.steps)
-    s->cluster *= 2;
-  const int64_t most = 1 << 20;
-  f.grid = (unsigned)((items < most ? items : most) * s->cluster);
-  return f;
+  Shape best = {1, 1, 1};
+  double least = 1e300;
+  for (const int fit : resident) {
+    int warps = 1;
+    while (warps < most && warps * kSegment < s->d.steps) warps *= 2;
+    for (int c = 1; c <= kMaxCluster; c *= 2) {
+      if (c > 1 && (int64_t)c / 2 * warps * kSegment >= s->d.steps) break;
+      const double n = (double)items * c, slots = 152.0 * fit;
+      const double waves = n > slots ? std::ceil(n / slots) * slots / n
+                                     : std::ceil(n / 152) * 152 / n;
+      const double held = (n < slots ? n : slots) * warps / 152;
+      const double cost = waves * (held < 10 ? 10 / held : 1) * (c > 1 ? 1.4 : 1);
+      if (cost < least * 0.98) {
+        least = cost;
+        best.warps = warps;
+        best.most = most;
+        s->cluster = c;
+      }
+    }
+    most /= 2;
+  }
+  const int64_t cap = 1 << 20;
+  best.grid = (unsigned)((items < cap ? items : cap) * s->cluster);
+  return best;
 }
 
 template <typename K, typename... A>
 cudaError_t launch(K kernel, const Shape& f, int cluster, size_t smem, cudaStream_t st, A... args) {
-  if (smem) {
-    const cudaError_t e =
-        cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-    if (e != cudaSuccess) return e;
-  }
+  cudaError_t e =
+      cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  if (e == cudaSuccess && cluster > 8)
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+  if (e != cudaSuccess) return e;
   cudaLaunchAttribute attr;
   attr.id = cudaLaunchAttributeClusterDimension;
   attr.val.clusterDim.x = (unsigned)cluster;
@@ -1007,8 +1061,9 @@ constexpr int dtype_of() {
 }
 
 template <typename T>
-size_t ring_bytes(int boxes, int warps) {
-  return (size_t)kDepth * boxes * warps * kSegment * kBlock * sizeof(T) + 128;
+size_t tiled_bytes(int depth, int boxes, int warps, int cluster) {
+  return (size_t)depth * boxes * warps * kSegment * kBlock * sizeof(T) + 128 +
+         joint_bytes<2>(warps, cluster);
 }
 
 template <typename T>
@@ -1020,17 +1075,25 @@ cudaError_t forward(const void* gates, Scan s, void* h, int* status, cudaStream_
                       s.hs.t % 2 == 0 && aligned(s.marks, 8);
   for (const bool t_inner : {true, false}) {
     if (s.d.steps < 1 || !direct || !mappable(gates, s.d, s.gs, true, t_inner, dtype)) continue;
-    const Shape f = shape(&s, 2, sizeof(T) == 4 ? 4 : kMaxWarps, 2);
+    // eight warps' stages of fp32 fit an SM only once
+    const Shape f = sizeof(T) == 4 ? shape(&s, 2, 4, {3, 5}) : shape(&s, 2, 8, {2, 5});
     Maps maps;
     maps.t_inner = t_inner;
     if (!map_all(maps.in, 4, gates, s.d, s.gs, t_inner, dtype, f.warps * kSegment))
       return cudaErrorInvalidValue;
-    return launch(ragged ? scan_forward_tiled_kernel<T, true> : scan_forward_tiled_kernel<T, false>,
-                  f, s.cluster, ring_bytes<T>(4, f.warps), st, maps, s, static_cast<T*>(h), status);
+    const auto kernel = f.most == 8   ? ragged ? scan_forward_tiled_kernel<T, true, 8>
+                                               : scan_forward_tiled_kernel<T, false, 8>
+                        : f.most == 4 ? ragged ? scan_forward_tiled_kernel<T, true, 4>
+                                               : scan_forward_tiled_kernel<T, false, 4>
+                                      : ragged ? scan_forward_tiled_kernel<T, true, 2>
+                                               : scan_forward_tiled_kernel<T, false, 2>;
+    return launch(kernel, f, s.cluster, tiled_bytes<T>(kForwardDepth, 4, f.warps, s.cluster), st,
+                  maps, s, static_cast<T*>(h), status);
   }
-  const Shape f = shape(&s, 1, kMaxWarps, 2);
+  const Shape f = shape(&s, 1, kMaxWarps, {2});
   return launch(ragged ? scan_forward_kernel<T, 1, true> : scan_forward_kernel<T, 1, false>, f,
-                s.cluster, 0, st, static_cast<const T*>(gates), s, static_cast<T*>(h));
+                s.cluster, joint_bytes<1>(f.warps, s.cluster), st, static_cast<const T*>(gates), s,
+                static_cast<T*>(h));
 }
 
 template <typename T>
@@ -1044,7 +1107,7 @@ cudaError_t backward(const void* gates, Scan s, const void* dh, const float* dc_
         !mappable(dh, s.d, s.hs, false, t_inner, dtype) ||
         !mappable(dgates, s.d, s.ds, true, t_inner, dtype))
       continue;
-    const Shape f = shape(&s, 2, sizeof(T) == 4 ? 2 : kBackwardWarps, 3);
+    const Shape f = sizeof(T) == 4 ? shape(&s, 2, 2, {3, 6}) : shape(&s, 2, 4, {3, 6});
     const int rows = f.warps * kSegment;
     Maps maps;
     maps.t_inner = t_inner;
@@ -1052,13 +1115,18 @@ cudaError_t backward(const void* gates, Scan s, const void* dh, const float* dc_
         !map_all(maps.in + 4, 1, dh, s.d, s.hs, t_inner, dtype, rows) ||
         !map_all(maps.out, 4, dgates, s.d, s.ds, t_inner, dtype, rows))
       return cudaErrorInvalidValue;
-    return launch(
-        ragged ? scan_backward_tiled_kernel<T, true> : scan_backward_tiled_kernel<T, false>, f,
-        s.cluster, ring_bytes<T>(5, f.warps), st, maps, s, dc_last, dc0, status);
+    const auto kernel = f.most == 4   ? ragged ? scan_backward_tiled_kernel<T, true, 4>
+                                               : scan_backward_tiled_kernel<T, false, 4>
+                        : f.most == 2 ? ragged ? scan_backward_tiled_kernel<T, true, 2>
+                                               : scan_backward_tiled_kernel<T, false, 2>
+                                      : ragged ? scan_backward_tiled_kernel<T, true, 1>
+                                               : scan_backward_tiled_kernel<T, false, 1>;
+    return launch(kernel, f, s.cluster, tiled_bytes<T>(kBackwardDepth, 5, f.warps, s.cluster), st,
+                  maps, s, dc_last, dc0, status);
   }
-  const Shape f = shape(&s, 1, kMaxWarps, 1);
+  const Shape f = shape(&s, 1, kMaxWarps, {1});
   return launch(ragged ? scan_backward_kernel<T, 1, true> : scan_backward_kernel<T, 1, false>, f,
-                s.cluster, 0, st, static_cast<const T*>(gates), s, static_cast<const T*>(dh),
+                s.cluster, joint_bytes<1>(f.warps, s.cluster), st, static_cast<const T*>(gates), s, static_cast<const T*>(dh),
                 dc_last, static_cast<T*>(dgates), dc0);
 }
 
