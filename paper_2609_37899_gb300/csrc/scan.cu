@@ -37,7 +37,7 @@ namespace {
 
 constexpr int kSegment = 8;     // steps of a warp, and between two checkpoints
 constexpr int kMaxWarps = 8;    // of a CTA
-constexpr int kMaxCluster = 16;
+constexpr int kMaxCluster = 8;
 constexpr float kLog2e = 1.4426950408889634f;
 
 __device__ __forceinline__ float rcp(float x) {
@@ -92,34 +92,19 @@ __device__ __forceinline__ void tanh_slope(float x, float& y, float& dy) {
   dy = 4.f * e * r * r;
 }
 
-// Two fp32 values in a register pair, for the packed instructions.
+// Two fp32 values for the packed instructions.
 struct Two {
-  unsigned long long v;
+  float2 v;
 };
-__device__ __forceinline__ Two two(float a, float b) {
-  Two r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(a), "f"(b));
-  return r;
-}
+__device__ __forceinline__ Two two(float a, float b) { return {make_float2(a, b)}; }
 __device__ __forceinline__ Two two(float a) { return two(a, a); }
 __device__ __forceinline__ void split(Two x, float& a, float& b) {
-  asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(x.v));
+  a = x.v.x;
+  b = x.v.y;
 }
-__device__ __forceinline__ Two operator*(Two a, Two b) {
-  Two r;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
-  return r;
-}
-__device__ __forceinline__ Two operator+(Two a, Two b) {
-  Two r;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
-  return r;
-}
-__device__ __forceinline__ Two fma2(Two a, Two b, Two c) {
-  Two r;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
-  return r;
-}
+__device__ __forceinline__ Two operator*(Two a, Two b) { return {__fmul2_rn(a.v, b.v)}; }
+__device__ __forceinline__ Two operator+(Two a, Two b) { return {__fadd2_rn(a.v, b.v)}; }
+__device__ __forceinline__ Two fma2(Two a, Two b, Two c) { return {__ffma2_rn(a.v, b.v, c.v)}; }
 template <typename F>
 __device__ __forceinline__ Two each(Two x, F f) {
   float a, b;
@@ -172,6 +157,7 @@ struct Scan {
   float* marks;      // [batch][ceil(steps / kSegment)][dim]: the state before each segment
   int64_t blocks;    // blocks of 32 V channels
   int32_t cluster;   // CTAs along the time axis
+  int32_t depth;     // stages of the ring
 };
 
 __device__ __forceinline__ int64_t length_of(const Scan& s, int64_t b) {
@@ -546,10 +532,10 @@ scan_backward_kernel(const T* __restrict__ gates, const __grid_constant__ Scan s
 
 // ---- tiled ----------------------------------------------------------------
 constexpr int kBlock = 64;  // channels of a CTA: 32 lanes of two
-// Stages of the ring.  Forward, one is read to the end of its round; backward,
-// one more is being stored.
-constexpr int kForwardDepth = 2;
-constexpr int kBackwardDepth = 3;
+// Stages of the ring: one is read to the end of its round (forward) or being
+// stored (backward), so one less is in flight.  A call whose CTAs have an SM to
+// themselves takes more of them, as nothing else covers a copy's latency.
+constexpr int kMaxDepth = 4;
 // CTAs of so many warps that an SM's registers hold.
 constexpr int forward_resident(int warps) { return 20 / warps; }
 constexpr int backward_resident(int warps) { return 12 / warps; }
@@ -616,7 +602,7 @@ __device__ __forceinline__ Two apply2(Two a, Two b, Two c) {
 }
 
 struct Ring {
-  uint64_t full[kBackwardDepth];
+  uint64_t full[kMaxDepth];
   volatile int abort;
 };
 
@@ -633,7 +619,7 @@ __global__ void __launch_bounds__(32 * WARPS, forward_resident(WARPS))
 scan_forward_tiled_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Scan s,
                           T* __restrict__ h, int* status) {
   extern __shared__ uint8_t raw[];
-  constexpr int kDepth = kForwardDepth;
+  const int depth = s.depth;
   __shared__ Ring ring;
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, warps = blockDim.x / 32;
   const int C = s.cluster;
@@ -643,14 +629,15 @@ scan_forward_tiled_kernel(const __grid_constant__ Maps maps, const __grid_consta
   const int64_t marks = (s.d.steps + kSegment - 1) / kSegment;
   const int stage_elems = 4 * rows * kBlock;
   T* const stages = reinterpret_cast<T*>(raw + (128 - (tc::smem_u32(raw) & 127)) % 128);
-  const Joint<2> sh = joint_at<2>(stages + (size_t)kDepth * stage_elems, warps);
+  const Joint<2> sh = joint_at<2>(stages + (size_t)depth * stage_elems, warps);
   if (threadIdx.x == 0) {
-    for (int i = 0; i < kDepth; ++i) tc::mbar_init(&ring.full[i], 1);
+    for (int i = 0; i < depth; ++i) tc::mbar_init(&ring.full[i], 1);
     tc::mbar_fence_init();
     ring.abort = 0;
   }
   __syncthreads();
-  uint32_t filled = 0, used = 0;  // stages so far
+  int filled = 0, st = 0;          // the next stage to fill, and to use
+  uint32_t parity = 0, turn = 0;
   for (int64_t item = blockIdx.x / C; item < s.d.batch * s.blocks; item += gridDim.x / C) {
     const int64_t b = item / s.blocks;
     const int ch0 = (int)(item % s.blocks) * kBlock;
@@ -663,7 +650,8 @@ scan_forward_tiled_kernel(const __grid_constant__ Maps maps, const __grid_consta
     if (on && s.c0) c[0] = s.c0[b * s.d.dim + ch], c[1] = s.c0[b * s.d.dim + ch + 1];
 
     const auto fill = [&](int64_t round) {  // warp 0
-      const int st = filled++ % kDepth;
+      const int st = filled;
+      filled = filled + 1 == depth ? 0 : filled + 1;
       if (lane == 0) tc::mbar_arrive_expect_tx(&ring.full[st], stage_elems * sizeof(T));
       __syncwarp();
       if (lane < 4) {
@@ -675,13 +663,11 @@ scan_forward_tiled_kernel(const __grid_constant__ Maps maps, const __grid_consta
     // one stage less in flight than there are: the newest is read to the end of
     // its round
     if (warp == 0)
-      for (int64_t q = 0; q < kDepth - 1 && q < rounds; ++q) fill(q);
+      for (int64_t q = 0; q < depth - 1 && q < rounds; ++q) fill(q);
 
     int64_t t0 = (int64_t)(rank * warps + warp) * kSegment;
     for (int64_t round = 0; round < rounds; ++round, t0 += span) {
-      const int st = used % kDepth;
-      ring_wait(ring, st, (used / kDepth) & 1, status);
-      ++used;
+      ring_wait(ring, st, parity, status);
       const T* p = stages + (size_t)st * stage_elems + warp * kSegment * kBlock + 2 * lane;
       const int gate = rows * kBlock;
       Two f[kSegment], u[kSegment];
@@ -717,9 +703,9 @@ scan_forward_tiled_kernel(const __grid_constant__ Maps maps, const __grid_consta
       split(A, m.a[0], m.a[1]);
       split(B, m.b[0], m.b[1]);
       float in[2];
-      join<false, RAGGED, WARPS>(sh, m, (int)(used & 1), C, rank, c, in);
+      join<false, RAGGED, WARPS>(sh, m, (int)(turn & 1), C, rank, c, in);
       // every warp is through with the stage of the round before
-      if (warp == 0 && round + kDepth - 1 < rounds) fill(round + kDepth - 1);
+      if (warp == 0 && round + depth - 1 < rounds) fill(round + depth - 1);
       if (on) {
         if (s.marks && t0 < s.d.steps)
           *reinterpret_cast<float2*>(s.marks + (b * marks + t0 / kSegment) * s.d.dim + ch) =
@@ -738,6 +724,8 @@ scan_forward_tiled_kernel(const __grid_constant__ Maps maps, const __grid_consta
         }
       }
       __syncwarp();
+      if (++st == depth) st = 0, parity ^= 1;
+      ++turn;
     }
     // rounds past the sequence's end
     if (RAGGED && on)
@@ -758,7 +746,7 @@ scan_backward_tiled_kernel(const __grid_constant__ Maps maps, const __grid_const
                            const float* __restrict__ dc_last, float* __restrict__ dc0,
                            int* status) {
   extern __shared__ uint8_t raw[];
-  constexpr int kDepth = kBackwardDepth;
+  const int depth = s.depth;
   __shared__ Ring ring;
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, warps = blockDim.x / 32;
   const int C = s.cluster;
@@ -768,14 +756,15 @@ scan_backward_tiled_kernel(const __grid_constant__ Maps maps, const __grid_const
   const int64_t marks = (s.d.steps + kSegment - 1) / kSegment;
   const int stage_elems = 5 * rows * kBlock;
   T* const stages = reinterpret_cast<T*>(raw + (128 - (tc::smem_u32(raw) & 127)) % 128);
-  const Joint<2> sh = joint_at<2>(stages + (size_t)kDepth * stage_elems, warps);
+  const Joint<2> sh = joint_at<2>(stages + (size_t)depth * stage_elems, warps);
   if (threadIdx.x == 0) {
-    for (int i = 0; i < kDepth; ++i) tc::mbar_init(&ring.full[i], 1);
+    for (int i = 0; i < depth; ++i) tc::mbar_init(&ring.full[i], 1);
     tc::mbar_fence_init();
     ring.abort = 0;
   }
   __syncthreads();
-  uint32_t filled = 0, used = 0;
+  int filled = 0, st = 0;
+  uint32_t parity = 0, turn = 0;
   for (int64_t item = blockIdx.x / C; item < s.d.batch * s.blocks; item += gridDim.x / C) {
     const int64_t b = item / s.blocks;
     const int ch0 = (int)(item % s.blocks) * kBlock;
@@ -789,7 +778,8 @@ scan_backward_tiled_kernel(const __grid_constant__ Maps maps, const __grid_const
     // warp 0; of the stores that this thread has made, the newest may still read
     // its stage: the stage filled here is an older one, except at an item's start
     const auto fill = [&](int64_t round, bool start) {
-      const int st = filled++ % kDepth;
+      const int st = filled;
+      filled = filled + 1 == depth ? 0 : filled + 1;
       if (lane == 0) {
         if (start) tc::bulk_wait_read();
         else asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
@@ -804,25 +794,26 @@ scan_backward_tiled_kernel(const __grid_constant__ Maps maps, const __grid_const
     };
     // one stage less in flight than there are: the newest is being stored
     if (warp == 0)
-      for (int64_t q = 0; q < kDepth - 1 && q < rounds; ++q) fill(rounds - 1 - q, true);
+      for (int64_t q = 0; q < depth - 1 && q < rounds; ++q) fill(rounds - 1 - q, true);
 
+    const auto mark_at = [&](int64_t t) {
+      float2 x = make_float2(0.f, 0.f);
+      if (on && t >= 0 && t < n)
+        x = *reinterpret_cast<const float2*>(s.marks + (b * marks + t / kSegment) * s.d.dim + ch);
+      return two(x.x, x.y);
+    };
     int64_t t0 = (rounds - 1) * span + (int64_t)(rank * warps + warp) * kSegment;
+    Two next_mark = mark_at(t0);
     for (int64_t round = rounds - 1; round >= 0; --round, t0 -= span) {
-      const int st = used % kDepth;
-      float mark[2] = {0.f, 0.f};
-      if (on && t0 < n) {
-        const float2 x = *reinterpret_cast<const float2*>(
-            s.marks + (b * marks + t0 / kSegment) * s.d.dim + ch);
-        mark[0] = x.x, mark[1] = x.y;
-      }
-      ring_wait(ring, st, (used / kDepth) & 1, status);
-      ++used;
+      const Two mark = next_mark;
+      next_mark = mark_at(t0 - span);
+      ring_wait(ring, st, parity, status);
       T* p = stages + (size_t)st * stage_elems + warp * kSegment * kBlock + 2 * lane;
       const int gate = rows * kBlock;
       // what each step adds to r, its f, and the factors that turn the gradient
       // of its state into those of i, f and g
       Two add[kSegment], f[kSegment], ki[kSegment], kf[kSegment], kg[kSegment];
-      Two c = two(mark[0], mark[1]);
+      Two c = mark;
       const int live = n - t0 >= kSegment ? kSegment : n > t0 ? (int)(n - t0) : 0;
 #pragma unroll
       for (int j = 0; j < kSegment; ++j) {
@@ -866,7 +857,7 @@ scan_backward_tiled_kernel(const __grid_constant__ Maps maps, const __grid_const
       split(A, m.a[0], m.a[1]);
       split(B, m.b[0], m.b[1]);
       float in[2];
-      join<true, RAGGED, WARPS>(sh, m, (int)(used & 1), C, rank, r, in);
+      join<true, RAGGED, WARPS>(sh, m, (int)(turn & 1), C, rank, r, in);
       Two x = two(in[0], in[1]);
 #pragma unroll
       for (int j = kSegment - 1; j >= 0; --j) {
@@ -895,8 +886,10 @@ scan_backward_tiled_kernel(const __grid_constant__ Maps maps, const __grid_const
           tc::bulk_commit();
         }
         __syncwarp();
-        if (round >= kDepth - 1) fill(round - (kDepth - 1), false);
+        if (round >= depth - 1) fill(round - (depth - 1), false);
       }
+      if (++st == depth) st = 0, parity ^= 1;
+      ++turn;
     }
     if (dc0 && on && rank == 0 && warp == 0)
       dc0[b * s.d.dim + ch] = r[0], dc0[b * s.d.dim + ch + 1] = r[1];
@@ -956,6 +949,7 @@ bool pairs(const void* p, const soma_scan_strides& s) {
 struct Shape {
   int warps, most;  // of a CTA, and of the kernel compiled for it
   unsigned grid;
+  bool alone;       // no SM has two CTAs
 };
 
 // How the work is cut: CTAs of up to `most` warps (resident[k] of `most >> k`
@@ -968,7 +962,7 @@ struct Shape {
 Shape shape(Scan* s, int V, int most, std::initializer_list<int> resident) {
   s->blocks = (s->d.dim + 32 * V - 1) / (32 * V);
   const int64_t items = s->d.batch * s->blocks;
-  Shape best = {1, 1, 1};
+  Shape best = {1, 1, 1, false};
   double least = 1e300;
   for (const int fit : resident) {
     int warps = 1;
@@ -991,6 +985,7 @@ Shape shape(Scan* s, int V, int most, std::initializer_list<int> resident) {
   }
   const int64_t cap = 1 << 20;
   best.grid = (unsigned)((items < cap ? items : cap) * s->cluster);
+  best.alone = best.grid <= 152;
   return best;
 }
 
@@ -998,8 +993,6 @@ template <typename K, typename... A>
 cudaError_t launch(K kernel, const Shape& f, int cluster, size_t smem, cudaStream_t st, A... args) {
   cudaError_t e =
       cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-  if (e == cudaSuccess && cluster > 8)
-    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
   if (e != cudaSuccess) return e;
   cudaLaunchAttribute attr;
   attr.id = cudaLaunchAttributeClusterDimension;
@@ -1087,8 +1080,9 @@ cudaError_t forward(const void* gates, Scan s, void* h, int* status, cudaStream_
                                                : scan_forward_tiled_kernel<T, false, 4>
                                       : ragged ? scan_forward_tiled_kernel<T, true, 2>
                                                : scan_forward_tiled_kernel<T, false, 2>;
-    return launch(kernel, f, s.cluster, tiled_bytes<T>(kForwardDepth, 4, f.warps, s.cluster), st,
-                  maps, s, static_cast<T*>(h), status);
+    s.depth = f.alone ? 4 : 2;
+    return launch(kernel, f, s.cluster, tiled_bytes<T>(s.depth, 4, f.warps, s.cluster), st, maps, s,
+                  static_cast<T*>(h), status);
   }
   const Shape f = shape(&s, 1, kMaxWarps, {2});
   return launch(ragged ? scan_forward_kernel<T, 1, true> : scan_forward_kernel<T, 1, false>, f,
@@ -1121,8 +1115,9 @@ cudaError_t backward(const void* gates, Scan s, const void* dh, const float* dc_
                                                : scan_backward_tiled_kernel<T, false, 2>
                                       : ragged ? scan_backward_tiled_kernel<T, true, 1>
                                                : scan_backward_tiled_kernel<T, false, 1>;
-    return launch(kernel, f, s.cluster, tiled_bytes<T>(kBackwardDepth, 5, f.warps, s.cluster), st,
-                  maps, s, dc_last, dc0, status);
+    s.depth = f.alone ? 4 : 3;
+    return launch(kernel, f, s.cluster, tiled_bytes<T>(s.depth, 5, f.warps, s.cluster), st, maps, s,
+                  dc_last, dc0, status);
   }
   const Shape f = shape(&s, 1, kMaxWarps, {1});
   return launch(ragged ? scan_backward_kernel<T, 1, true> : scan_backward_kernel<T, 1, false>, f,
@@ -1164,7 +1159,7 @@ int soma_scan_forward(const void* gates, soma_scan_strides gate_strides, int dty
   if (d.steps > 0 && (!gates || !h)) return SOMA_ERR_INVALID_ARG;
   h_strides.g = 0;
   const Scan s = {d,       gate_strides, h_strides, {0, 0, 0},   c0,
-                  lengths, resets,       c_last,    checkpoints, 0, 1};
+                  lengths, resets,       c_last,    checkpoints, 0, 1, 2};
   const cudaStream_t st = (cudaStream_t)stream;
   int* status = status_ptr();
   if (!status) return SOMA_ERR_CUDA;
@@ -1192,7 +1187,7 @@ int soma_scan_backward(const void* gates, soma_scan_strides gate_strides, int dt
   dh_strides.g = 0;
   const Scan s = {d,       gate_strides, dh_strides, dgate_strides,
                   nullptr, lengths,      resets,     nullptr,
-                  const_cast<float*>(checkpoints), 0, 1};
+                  const_cast<float*>(checkpoints), 0, 1, 2};
   const cudaStream_t st = (cudaStream_t)stream;
   int* status = status_ptr();
   if (!status) return SOMA_ERR_CUDA;
@@ -1216,7 +1211,7 @@ int soma_scan_step(const void* gates, soma_scan_strides gate_strides, int dtype,
   if (!gates || !c || !h) return SOMA_ERR_INVALID_ARG;
   gate_strides.t = h_strides.t = h_strides.g = 0;
   const Scan s = {d,       gate_strides, h_strides, {0, 0, 0}, nullptr,
-                  nullptr, nullptr,      nullptr,   nullptr,   0, 1};
+                  nullptr, nullptr,      nullptr,   nullptr,   0, 1, 2};
   const cudaStream_t st = (cudaStream_t)stream;
   const bool two = dim % 2 == 0 && pairs(gates, gate_strides) && pairs(h, h_strides);
   trace_begin(SOMA_TRACE_GATE, st);
