@@ -495,18 +495,23 @@ typedef struct soma_scan_strides {
  * soma_scan_backward (states at regular steps); -1 if the sizes are invalid. */
 int64_t soma_scan_checkpoint_count(soma_scan_dims d);
 
+/* Bytes of workspace that the forward and the backward call need, 0 for most
+ * sizes (few channels and many steps take some); -1 if the sizes are invalid. */
+int64_t soma_scan_workspace_bytes(soma_scan_dims d);
+
 /*   gates        [batch][steps][4][dim] by gate_strides
  *   c0           fp32 [batch][dim] or NULL for 0
  *   lengths      int32 [batch] or NULL;  resets: uint8 [batch][steps] or NULL
  *   h            [batch][steps][dim] by h_strides (g unused)
  *   c_last       fp32 [batch][dim], the state after the last step, or NULL;
- *                may be c0
+ *                not c0
  *   checkpoints  fp32 [soma_scan_checkpoint_count()], or NULL when no
  *                backward call follows */
 int soma_scan_forward(const void* gates, soma_scan_strides gate_strides, int dtype,
                       soma_scan_dims d, const float* c0, const int32_t* lengths,
                       const uint8_t* resets, void* h, soma_scan_strides h_strides,
-                      float* c_last, float* checkpoints, void* stream);
+                      float* c_last, float* checkpoints, void* workspace, size_t workspace_bytes,
+                      void* stream);
 
 /* The gradients, from dh and dc_last (fp32, the gradient of c_last; NULL: 0):
  *   dc_t = dh_t o (1 - tanh(c_t)^2) + f_{t+1} dc_{t+1}
@@ -518,7 +523,7 @@ int soma_scan_backward(const void* gates, soma_scan_strides gate_strides, int dt
                        soma_scan_dims d, const float* checkpoints, const int32_t* lengths,
                        const uint8_t* resets, const void* dh, soma_scan_strides dh_strides,
                        const float* dc_last, void* dgates, soma_scan_strides dgate_strides,
-                       float* dc0, void* stream);
+                       float* dc0, void* workspace, size_t workspace_bytes, void* stream);
 
 /* One token of each of `batch` running sequences: gates [batch][4][dim] and
  * h [batch][dim] by their strides (t unused); c [batch][dim] is updated. */

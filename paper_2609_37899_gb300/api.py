@@ -176,9 +176,11 @@ def _open(path: str):
                                          soma_adamw_config, vp, vp])
         sd, ss = soma_scan_dims, soma_scan_strides
         _sig(L, "soma_scan_checkpoint_count", i64, [sd])
-        _sig(L, "soma_scan_forward", i32, [vp, ss, i32, sd, vp, vp, vp, vp, ss, vp, vp, vp])
+        _sig(L, "soma_scan_workspace_bytes", i64, [sd])
+        _sig(L, "soma_scan_forward", i32, [vp, ss, i32, sd, vp, vp, vp, vp, ss, vp, vp, vp, sz,
+                                           vp])
         _sig(L, "soma_scan_backward", i32, [vp, ss, i32, sd, vp, vp, vp, vp, ss, vp, vp, ss, vp,
-                                            vp])
+                                            vp, sz, vp])
         _sig(L, "soma_scan_step", i32, [vp, ss, i32, i64, i64, vp, vp, ss, vp])
         cd = soma_linear_ce_dims
         _sig(L, "soma_linear_ce_workspace_bytes", sz, [cd, i32])
@@ -635,31 +637,54 @@ def scan_alloc_checkpoints(batch: int, steps: int, dim: int, device="cuda") -> t
     return torch.empty(n, dtype=torch.float32, device=device)
 
 
+def scan_workspace_bytes(batch: int, steps: int, dim: int) -> int:
+    return int(lib().soma_scan_workspace_bytes(soma_scan_dims(batch, steps, dim)))
+
+
+def _scan_workspace(d: soma_scan_dims, workspace, device, stream):
+    """(pointer, bytes, the tensor) of the caller's workspace, or of one from
+    torch's allocator where the sizes need any and none is given."""
+    if workspace is None:
+        n = int(lib().soma_scan_workspace_bytes(d))
+        if n <= 0:
+            return None, 0, None
+        workspace = torch.empty(n, dtype=torch.uint8, device=device)
+        if stream is not None:
+            # torch's allocator orders it by the current stream: keep it from
+            # being handed out again before `stream` is through with it
+            stream.wait_stream(torch.cuda.current_stream())
+            workspace.record_stream(stream)
+    return _dev(workspace, torch.uint8, "workspace"), workspace.numel(), workspace
+
+
 def scan_forward(gates: torch.Tensor, h: torch.Tensor, c_last: torch.Tensor | None = None,
                  c0: torch.Tensor | None = None, lengths: torch.Tensor | None = None,
                  resets: torch.Tensor | None = None, checkpoints: torch.Tensor | None = None,
-                 stream=None):
+                 workspace: torch.Tensor | None = None, stream=None):
     """The gated linear recurrence over gates [B, T, 4, D] (pre-activations in
     the order i, f, g, o) into h [B, T, D]; c0 and c_last fp32 [B, D], lengths
     int32 [B], resets uint8 [B, T], checkpoints of scan_alloc_checkpoints for
-    a scan_backward call."""
+    a scan_backward call, workspace uint8 of scan_workspace_bytes (taken from
+    torch's allocator if not given)."""
     B, T, _, D = gates.shape
     dt, d = _gate_dtype(gates), soma_scan_dims(B, T, D)
     gp, gs = _rows(gates, "gates", (B, T, 4, D), gates.dtype)
     hp, hs = _rows(h, "h", (B, T, D), gates.dtype)
     f32 = torch.float32
+    wp, wn, _keep = _scan_workspace(d, workspace, gates.device, stream)
     _check(lib().soma_scan_forward(
         gp, soma_scan_strides(*gs[:3]), dt, d, _opt(c0, f32, "c0", B * D),
         _opt(lengths, torch.int32, "lengths", B), _opt(resets, torch.uint8, "resets", B * T), hp,
         soma_scan_strides(hs[0], hs[1], 0), _opt(c_last, f32, "c_last", B * D),
         _opt(checkpoints, f32, "checkpoints", None if checkpoints is None else
-             lib().soma_scan_checkpoint_count(d)), _stream(stream)), "soma_scan_forward")
+             lib().soma_scan_checkpoint_count(d)), wp, wn, _stream(stream)), "soma_scan_forward")
 
 
 def scan_backward(gates: torch.Tensor, checkpoints: torch.Tensor, dh: torch.Tensor,
                   dgates: torch.Tensor, dc0: torch.Tensor | None = None,
                   dc_last: torch.Tensor | None = None, lengths: torch.Tensor | None = None,
-                  resets: torch.Tensor | None = None, stream=None):
+                  resets: torch.Tensor | None = None, workspace: torch.Tensor | None = None,
+                  stream=None):
     """Gradients of scan_forward: dgates [B, T, 4, D] and dc0 [B, D] from dh
     [B, T, D] and dc_last [B, D], with that call's checkpoints."""
     B, T, _, D = gates.shape
@@ -668,12 +693,13 @@ def scan_backward(gates: torch.Tensor, checkpoints: torch.Tensor, dh: torch.Tens
     hp, hs = _rows(dh, "dh", (B, T, D), gates.dtype)
     dp, ds = _rows(dgates, "dgates", (B, T, 4, D), gates.dtype)
     f32 = torch.float32
+    wp, wn, _keep = _scan_workspace(d, workspace, gates.device, stream)
     _check(lib().soma_scan_backward(
         gp, soma_scan_strides(*gs[:3]), dt, d,
         _dev(checkpoints, f32, "checkpoints", lib().soma_scan_checkpoint_count(d)),
         _opt(lengths, torch.int32, "lengths", B), _opt(resets, torch.uint8, "resets", B * T), hp,
         soma_scan_strides(hs[0], hs[1], 0), _opt(dc_last, f32, "dc_last", B * D), dp,
-        soma_scan_strides(*ds[:3]), _opt(dc0, f32, "dc0", B * D), _stream(stream)),
+        soma_scan_strides(*ds[:3]), _opt(dc0, f32, "dc0", B * D), wp, wn, _stream(stream)),
         "soma_scan_backward")
 
 

@@ -47,32 +47,43 @@ def test_adamw_refusals(soma):
 def test_scan_refusals(soma):
     L, dims, st = soma.lib(), soma.soma_scan_dims, soma.soma_scan_strides
     ok, s, odd = dims(2, 3, 8), st(96, 32, 8), ctypes.c_void_p(0x10001)
-    assert L.soma_scan_checkpoint_count(ok) == 16
-    assert L.soma_scan_checkpoint_count(dims(2, 17, 8)) == 32
+
+    def fwd(gates=FAKE, gs=s, dtype=0, d=ok, c0=None, lengths=None, h=FAKE, ws=None, n=0):
+        return L.soma_scan_forward(gates, gs, dtype, d, c0, lengths, None, h, s, None, None, ws, n,
+                                   None)
+
+    def bwd(marks=FAKE, d=ok, dgates=FAKE, ws=None, n=0):
+        return L.soma_scan_backward(FAKE, s, 0, d, marks, None, None, FAKE, s, None, dgates, s,
+                                    None, ws, n, None)
+
+    assert L.soma_scan_checkpoint_count(ok) == 8 * 2
+    assert L.soma_scan_checkpoint_count(dims(2, 17, 8)) == 8 * 2 * 3
+    assert L.soma_scan_workspace_bytes(ok) == 0
     for bad in (dims(-1, 3, 8), dims(2, -3, 8), dims(2, 3, -8), dims(1 << 31, 3, 8),
                 dims(2, 1 << 31, 8), dims(2, 3, (1 << 24) + 1), dims(1 << 30, 1, 1 << 20)):
         assert L.soma_scan_checkpoint_count(bad) == -1
-        assert L.soma_scan_forward(FAKE, s, 0, bad, None, None, None, FAKE, s, None, None, None) == 2
-        assert L.soma_scan_backward(FAKE, s, 0, bad, FAKE, None, None, FAKE, s, None, FAKE, s, None,
-                                    None) == 2
+        assert L.soma_scan_workspace_bytes(bad) == -1
+        assert fwd(d=bad) == 2 and bwd(d=bad) == 2
     assert L.soma_scan_step(FAKE, s, 0, -1, 8, FAKE, FAKE, s, None) == 2
-    assert L.soma_scan_forward(FAKE, s, 3, ok, None, None, None, FAKE, s, None, None, None) == 1
-    assert L.soma_scan_forward(FAKE, st(-96, 32, 8), 0, ok, None, None, None, FAKE, s, None, None,
-                               None) == 1
-    assert L.soma_scan_forward(None, s, 0, ok, None, None, None, FAKE, s, None, None, None) == 1
-    assert L.soma_scan_forward(FAKE, s, 0, ok, None, None, None, None, s, None, None, None) == 1
-    assert L.soma_scan_forward(odd, s, 1, ok, None, None, None, FAKE, s, None, None, None) == 1
-    assert L.soma_scan_forward(FAKE, s, 0, ok, odd, None, None, FAKE, s, None, None, None) == 1
-    assert L.soma_scan_forward(FAKE, s, 0, ok, None, odd, None, FAKE, s, None, None, None) == 1
-    assert L.soma_scan_backward(FAKE, s, 0, ok, None, None, None, FAKE, s, None, FAKE, s, None,
-                                None) == 1
-    assert L.soma_scan_backward(FAKE, s, 0, ok, FAKE, None, None, FAKE, s, None, None, s, None,
-                                None) == 1
+    assert fwd(dtype=3) == 1
+    assert fwd(gs=st(-96, 32, 8)) == 1
+    assert fwd(gates=None) == 1
+    assert fwd(h=None) == 1
+    assert fwd(gates=odd, dtype=1) == 1
+    assert fwd(c0=odd) == 1
+    assert fwd(lengths=odd) == 1
+    assert bwd(marks=None) == 1
+    assert bwd(dgates=None) == 1
     assert L.soma_scan_step(FAKE, s, 0, 2, 8, None, FAKE, s, None) == 1
     assert L.soma_scan_step(FAKE, s, 7, 2, 8, FAKE, FAKE, s, None) == 1
     # nothing to do is fine without pointers
-    assert L.soma_scan_forward(None, s, 0, dims(0, 3, 8), None, None, None, None, s, None, None,
-                               None) == 0
+    assert fwd(gates=None, d=dims(0, 3, 8), h=None) == 0
+    # few channels, many steps: a workspace
+    long = dims(1, 1 << 16, 64)
+    need = L.soma_scan_workspace_bytes(long)
+    assert need > 0
+    assert fwd(d=long) == 3 and bwd(d=long) == 3
+    assert fwd(d=long, ws=odd, n=need) == 3 and bwd(d=long, ws=FAKE, n=7) == 3
 
 
 def test_linear_ce_refusals(soma):
