@@ -36,39 +36,68 @@ backward_kernel(const T* __restrict__ gates, const __grid_constant__ Scan s,
     Map<1> total = identity<1>();
     if (!MAPS) over_chunks<true, RAGGED, kWarps>(s, b, ch, on, k + 1, s.chunks, shared, turn++, r);
 
+    const int64_t stop = n < end ? n : end;
+    const int64_t at_ch = on ? ch : s.d.dim - 1;  // lanes past the last channel read along
     const int64_t rounds = (end - begin + rows - 1) / rows;
     int64_t t0 = begin + (rounds - 1) * rows + warp * kSegment;
+    T next[kSegment][5];
+    float next_mark;
+    const auto fetch = [&](int64_t t) {
+      const T* p = gates + b * s.gs.b + t * s.gs.t + at_ch;
+      const T* q = dh + b * s.hs.b + t * s.hs.t + at_ch;
+      if (t >= begin && t + kSegment <= stop) {
+#pragma unroll
+        for (int j = 0; j < kSegment; ++j, p += s.gs.t, q += s.hs.t) {
+#pragma unroll
+          for (int g = 0; g < 4; ++g) next[j][g] = p[g * s.gs.g];
+          next[j][4] = *q;
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < kSegment; ++j) {
+          const bool there = t >= begin && t + j < stop;
+#pragma unroll
+          for (int g = 0; g < 4; ++g)
+            next[j][g] = there ? p[j * s.gs.t + g * s.gs.g] : from_f32<T>(0.f);
+          next[j][4] = there ? q[j * s.hs.t] : from_f32<T>(0.f);
+        }
+      }
+      next_mark = t >= begin && t < stop
+                      ? s.marks[(b * marks + t / kSegment) * s.d.dim + at_ch] : 0.f;
+    };
+    fetch(t0);
     for (int64_t left = rounds; left > 0; --left, t0 -= rows) {
-      float add[kSegment], f[kSegment], ki[kSegment], kf[kSegment], kg[kSegment];
-      float c = on && t0 < n && t0 < end ? s.marks[(b * marks + t0 / kSegment) * s.d.dim + ch] : 0.f;
-      const T* p = gates + b * s.gs.b + t0 * s.gs.t + ch;
-      const T* q = dh + b * s.hs.b + t0 * s.hs.t + ch;
-      T* w = dgates + b * s.ds.b + t0 * s.ds.t + ch;
+      float add[kSegment], f[kSegment], ki[kSegment], kf[kSegment], kg[kSegment], od[kSegment];
+      float c = next_mark;
+      const int live = stop - t0 >= kSegment ? kSegment : stop > t0 ? (int)(stop - t0) : 0;
 #pragma unroll
       for (int j = 0; j < kSegment; ++j) {
-        const bool live = on && t0 + j < n && t0 + j < end;
-        float a[4] = {0.f, 0.f, 0.f, 0.f}, y = 0.f;
-        if (live) {
-#pragma unroll
-          for (int g = 0; g < 4; ++g) a[g] = to_f32(p[j * s.gs.t + g * s.gs.g]);
-          y = to_f32(q[j * s.hs.t]);
-        }
-        const bool reset = RAGGED && s.resets && live && s.resets[b * s.d.steps + t0 + j] != 0;
+        const float y = to_f32(next[j][4]);
+        const bool reset =
+            RAGGED && s.resets && j < live && s.resets[b * s.d.steps + t0 + j] != 0;
         float i, di, fg, df, g, dg, o, d_o, th, dth;
-        sigmoid_slope(a[0], i, di);
-        sigmoid_slope(a[1], fg, df);
-        tanh_slope(a[2], g, dg);
-        sigmoid_slope(a[3], o, d_o);
+        sigmoid_slope(to_f32(next[j][0]), i, di);
+        sigmoid_slope(to_f32(next[j][1]), fg, df);
+        tanh_slope(to_f32(next[j][2]), g, dg);
+        sigmoid_slope(to_f32(next[j][3]), o, d_o);
         const float prev = reset ? 0.f : c;
         c = fmaf(fg, prev, i * g);
         tanh_slope(c, th, dth);
-        add[j] = live ? y * o * dth : 0.f;
-        f[j] = live ? (reset ? 0.f : fg) : 1.f;
-        ki[j] = live ? g * di : 0.f;
-        kf[j] = live ? prev * df : 0.f;
-        kg[j] = live ? i * dg : 0.f;
-        if (!MAPS && on && t0 + j < end)
-          w[j * s.ds.t + 3 * s.ds.g] = from_f32<T>(live ? y * th * d_o : 0.f);
+        add[j] = y * o * dth;
+        f[j] = reset ? 0.f : fg;
+        ki[j] = g * di;
+        kf[j] = prev * df;
+        kg[j] = i * dg;
+        od[j] = y * th * d_o;
+      }
+      fetch(t0 - rows);
+      if (live < kSegment) {
+#pragma unroll
+        for (int j = 0; j < kSegment; ++j)
+          if (j >= live) {
+            add[j] = ki[j] = kf[j] = kg[j] = od[j] = 0.f;
+            f[j] = 1.f;
+          }
       }
       Map<1> m = identity<1>();
 #pragma unroll
@@ -84,16 +113,17 @@ backward_kernel(const T* __restrict__ gates, const __grid_constant__ Scan s,
       float in[1];
       join<true, RAGGED, kWarps>(shared, m, turn++, r, in);
       if (!on) continue;
+      T* w = dgates + b * s.ds.b + (t0 + kSegment - 1) * s.ds.t + ch;
 #pragma unroll
-      for (int j = kSegment - 1; j >= 0; --j) {
+      for (int j = kSegment - 1; j >= 0; --j, w -= s.ds.t) {
         const float dc = add[j] + in[0];
-        const bool live = t0 + j < n;
-        if (t0 + j < end) {
-          w[j * s.ds.t] = from_f32<T>(live ? dc * ki[j] : 0.f);
-          w[j * s.ds.t + s.ds.g] = from_f32<T>(live ? dc * kf[j] : 0.f);
-          w[j * s.ds.t + 2 * s.ds.g] = from_f32<T>(live ? dc * kg[j] : 0.f);
-        }
         in[0] = RAGGED ? apply(f[j], 0.f, dc) : f[j] * dc;
+        if (live < kSegment && t0 + j >= end) continue;
+        const bool dead = live < kSegment && j >= live;  // an infinite dc times 0 is no gradient
+        w[0] = from_f32<T>(dead ? 0.f : dc * ki[j]);
+        w[s.ds.g] = from_f32<T>(dead ? 0.f : dc * kf[j]);
+        w[2 * s.ds.g] = from_f32<T>(dead ? 0.f : dc * kg[j]);
+        w[3 * s.ds.g] = from_f32<T>(od[j]);
       }
     }
     __syncwarp();

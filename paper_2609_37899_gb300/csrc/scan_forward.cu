@@ -25,6 +25,7 @@ forward_kernel(const T* __restrict__ gates, const __grid_constant__ Scan s, T* _
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, warps = blockDim.x / 32;
   const int rows = warps * kSegment;  // steps of a round
   const int64_t marks = (s.d.steps + kSegment - 1) / kSegment;
+  constexpr int kGates = MAPS ? 3 : 4;
   uint32_t turn = 0;
   after_predecessor();
   for (int64_t at = blockIdx.x; at < s.d.batch * s.blocks * s.chunks; at += gridDim.x) {
@@ -37,37 +38,55 @@ forward_kernel(const T* __restrict__ gates, const __grid_constant__ Scan s, T* _
     Map<1> total = identity<1>();
     if (!MAPS) over_chunks<false, RAGGED, kWarps>(s, b, ch, on, 0, k, shared, turn++, c);
 
-    int64_t t0 = k * s.chunk + warp * kSegment;
-    T next[kSegment][4];
+    const int64_t begin = k * s.chunk, stop = n < end ? n : end;
+    const int64_t at_ch = on ? ch : s.d.dim - 1;  // lanes past the last channel read along
+    int64_t t0 = begin + warp * kSegment;
+    T next[kSegment][kGates];
     const auto fetch = [&](int64_t t) {
-      const T* p = gates + b * s.gs.b + t * s.gs.t + ch;
+      const T* p = gates + b * s.gs.b + t * s.gs.t + at_ch;
+      if (t + kSegment <= stop) {
 #pragma unroll
-      for (int j = 0; j < kSegment; ++j)
+        for (int j = 0; j < kSegment; ++j, p += s.gs.t)
 #pragma unroll
-        for (int g = 0; g < (MAPS ? 3 : 4); ++g) {
-          next[j][g] = from_f32<T>(0.f);
-          if (on && t + j < end && t + j < n) next[j][g] = p[j * s.gs.t + g * s.gs.g];
-        }
+          for (int g = 0; g < kGates; ++g) next[j][g] = p[g * s.gs.g];
+      } else {
+#pragma unroll
+        for (int j = 0; j < kSegment; ++j)
+#pragma unroll
+          for (int g = 0; g < kGates; ++g)
+            next[j][g] = t + j < stop ? p[j * s.gs.t + g * s.gs.g] : from_f32<T>(0.f);
+      }
     };
     fetch(t0);
-    for (int64_t start = k * s.chunk; start < end; start += rows, t0 += rows) {
+    for (int64_t start = begin; start < end; start += rows, t0 += rows) {
       float f[kSegment], u[kSegment];
       T o[kSegment];
       Map<1> m = identity<1>();
+      const int live = stop - t0 >= kSegment ? kSegment : stop > t0 ? (int)(stop - t0) : 0;
 #pragma unroll
       for (int j = 0; j < kSegment; ++j) {
-        o[j] = next[j][3];
-        const bool live = t0 + j < n && t0 + j < end;
+        o[j] = next[j][kGates - 1];
         float num, den;
         tanh_parts(to_f32(next[j][2]), num, den);
         u[j] = num * rcp(den * one_exp(to_f32(next[j][0])));
         f[j] = rcp(one_exp(to_f32(next[j][1])));
-        if (RAGGED && s.resets && live && s.resets[b * s.d.steps + t0 + j]) f[j] = 0.f;
-        if (!live) f[j] = 1.f, u[j] = 0.f;
+      }
+      fetch(t0 + rows);
+      if (RAGGED && s.resets) {
+#pragma unroll
+        for (int j = 0; j < kSegment; ++j)
+          if (j < live && s.resets[b * s.d.steps + t0 + j]) f[j] = 0.f;
+      }
+      if (live < kSegment) {
+#pragma unroll
+        for (int j = 0; j < kSegment; ++j)
+          if (j >= live) f[j] = 1.f, u[j] = 0.f;
+      }
+#pragma unroll
+      for (int j = 0; j < kSegment; ++j) {
         m.b[0] = RAGGED ? apply(f[j], u[j], m.b[0]) : fmaf(f[j], m.b[0], u[j]);
         m.a[0] *= f[j];
       }
-      fetch(t0 + rows);
       if (MAPS) {
         join_total<false, RAGGED, kWarps>(shared, m, turn++, total);
         continue;
@@ -78,12 +97,13 @@ forward_kernel(const T* __restrict__ gates, const __grid_constant__ Scan s, T* _
       if (s.marks && t0 < end) s.marks[(b * marks + t0 / kSegment) * s.d.dim + ch] = in[0];
       T* p = h + b * s.hs.b + t0 * s.hs.t + ch;
 #pragma unroll
-      for (int j = 0; j < kSegment; ++j) {
+      for (int j = 0; j < kSegment; ++j, p += s.hs.t) {
         in[0] = RAGGED ? apply(f[j], u[j], in[0]) : fmaf(f[j], in[0], u[j]);
         float num, den;
         tanh_parts(in[0], num, den);
-        const float y = num * rcp(den * one_exp(to_f32(o[j])));
-        if (t0 + j < end) p[j * s.hs.t] = from_f32<T>(t0 + j < n ? y : 0.f);
+        const T y = from_f32<T>(num * rcp(den * one_exp(to_f32(o[j]))));
+        if (live == kSegment) *p = y;
+        else if (t0 + j < end) *p = j < live ? y : from_f32<T>(0.f);
       }
     }
     __syncwarp();
