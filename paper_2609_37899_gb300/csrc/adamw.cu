@@ -1,12 +1,13 @@
 // adamw.cu -- AdamW over many tensors in one launch, moments in 32 bits or in
 // 8 (soma_adamw_step in include/soma_api.h has the formulas).
 //
-// Work is cut into chunks of kChunk elements of one tensor; a persistent grid
-// takes them in turn and finds a chunk's tensor by bisection over the first
-// chunks, a table in the kernel's parameters.  A thread owns eight consecutive
-// elements, so every stream is read and written in 8- to 32-byte pieces, and
-// a warp owns 256: exactly one block of the 8-bit state, whose new scale is
-// the warp's maximum.
+// Work is cut into chunks of one or four times kRow elements of one tensor; a
+// persistent grid takes them in turn and finds a chunk's tensor by bisection
+// over the first chunks, a table in the kernel's parameters (bisecting for
+// every kRow elements cost a ninth of the 8-bit kernel's instructions).  A
+// thread owns eight consecutive elements at a time, so every stream is read and
+// written in 8- to 32-byte pieces, and a warp owns 256: exactly one block of
+// the 8-bit state, whose new scale is the warp's maximum.
 #include <cmath>
 #include <cuda_fp8.h>
 
@@ -23,7 +24,7 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kGroup = 8;                          // elements of one thread
 constexpr int kBlock8 = 256;                       // elements that share a scale
-constexpr int kChunk = kThreads * kGroup;          // elements of one CTA's turn
+constexpr int kRow = kThreads * kGroup;            // elements of one pass of a CTA
 constexpr int kMaxTensors = 360;                   // table rows of one launch
 static_assert(kBlock8 == 32 * kGroup, "a warp owns one block of the 8-bit state");
 
@@ -57,47 +58,73 @@ struct Args {
   float b1, c1, b2, c2;  // beta and 1 - beta
   float lr, s2, eps;     // lr / (1 - beta1^t), 1 / sqrt(1 - beta2^t)
   uint32_t k0, k1, t;    // Philox key, update
+  int32_t passes;        // of kRow elements in a chunk
 };
 
-// One value's e4m3 neighbour, up or down at random.  y = |x| / scale lies in
-// [0, 448]; adding 16 random bits right below the last kept mantissa bit and
-// cutting the rest off rounds up with the odds of the cut-off part.  Below
-// the smallest normal value the grid has the step 2^-9, which is the step of
-// [2^-6, 2^-5): the value is moved there and back.
-__device__ __forceinline__ float round_e4m3(float y, uint32_t bits16) {
+// The two rounding forms of y = |x| / scale in [0, 448] to its e4m3 neighbour,
+// up or down at random.  Adding 16 random bits (here at their place) right below
+// the last kept mantissa bit and cutting the rest off rounds up with the odds
+// of the cut-off part.
+__device__ __forceinline__ uint32_t round_normal(float y, uint32_t random) {
+  return (__float_as_uint(y) + random) & 0xFFF00000u;
+}
+// Below the smallest normal value the grid has the step 2^-9, which is the
+// step of [2^-6, 2^-5): the value is moved there and back.  `floor`: what is
+// above zero stays above zero.
+__device__ __forceinline__ uint32_t round_any(float y, uint32_t random, bool floor) {
   const float low = y < kE4M3Normal ? kE4M3Normal : 0.f;
-  const uint32_t u = (__float_as_uint(__fadd_rn(y, low)) + (bits16 << 4)) & 0xFFF00000u;
-  return __fsub_rn(__uint_as_float(u), low);
+  float r = __fsub_rn(__uint_as_float(round_normal(__fadd_rn(y, low), random)), low);
+  if (floor && y > 0.f) r = fmaxf(r, kE4M3Least);
+  return __float_as_uint(r);
 }
 
 // Rounds the warp's 256 values x and returns this lane's eight bytes; the
-// scale goes to *scale.  `floor`: what is above zero stays above zero.
-__device__ __forceinline__ uint2 pack_block(const float (&x)[8], const uint4& rnd, bool floor,
+// scale goes to *scale.  FLOOR: the values are roots, none is negative, and
+// what is above zero stays above zero.
+template <bool FLOOR>
+__device__ __forceinline__ uint2 pack_block(const float (&x)[8], const uint32_t (&random)[8],
                                             float* scale) {
   float top = 0.f;
 #pragma unroll
   for (int j = 0; j < 8; ++j) top = fmaxf(top, fabsf(x[j]));
-#pragma unroll
-  for (int s = 16; s; s >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, s));
+  // non-negative floats order as their bits do
+  top = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(top)));
   // below 2^-100 the reciprocal could overflow: such a block is zero
   const bool some = top > 0x1p-100f;
   const float inv = some ? __fdiv_rn(kE4M3Max, top) : 0.f;
   if ((threadIdx.x & 31) == 0) *scale = some ? __fdiv_rn(top, kE4M3Max) : 0.f;
-  float z[8];
+  float y[8], z[8], least = kE4M3Max;
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
-    const uint32_t w = word_of(rnd, j >> 1);
-    const float y = fminf(__fmul_rn(fabsf(x[j]), inv), kE4M3Max);
-    float r = round_e4m3(y, (j & 1) ? w >> 16 : w & 0xFFFFu);
-    if (floor && y > 0.f) r = fmaxf(r, kE4M3Least);
-    z[j] = x[j] < 0.f ? -r : r;
+    y[j] = __fmul_rn(fabsf(x[j]), inv);
+    least = fminf(least, y[j]);
   }
-  // z is on the e4m3 grid: the conversion is exact
+  // one value in ten thousand of a normal distribution is below the normal
+  // ones: the others do without its steps
+  if (least >= kE4M3Normal) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) z[j] = __uint_as_float(round_normal(y[j], random[j]));
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) z[j] = __uint_as_float(round_any(y[j], random[j], FLOOR));
+  }
+  if (!FLOOR)
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      z[j] = __uint_as_float(__float_as_uint(z[j]) | (__float_as_uint(x[j]) & 0x80000000u));
+  // z is on the e4m3 grid, or the step above it where the product was rounded
+  // above 448: the conversion is exact or saturates
   uint32_t h[4];
 #pragma unroll
   for (int j = 0; j < 4; ++j)
     h[j] = __nv_cvt_float2_to_fp8x2(make_float2(z[2 * j], z[2 * j + 1]), __NV_SATFINITE, __NV_E4M3);
   return make_uint2(h[0] | (h[1] << 16), h[2] | (h[3] << 16));
+}
+
+__device__ __forceinline__ float rcp_approx(float x) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
 }
 
 __device__ __forceinline__ void unpack8(const uint2& b, float scale, float (&x)[8]) {
@@ -151,16 +178,39 @@ __device__ __forceinline__ void store_bytes(uint8_t* p, bool vec, int n, const u
   }
 }
 
+// The eight elements' new moments (r: the second one's root) and parameters.
+// Each operation of the moments is rounded by itself, which makes the 8-bit
+// states a matter of the formulas alone.  The parameter's quotient is one of
+// the special function unit in the 8-bit form (good to 2^-23), where
+// instructions are scarce.
+template <bool EIGHT>
+__device__ __forceinline__ void update(const Args& a, float decay, float gs, const float (&g)[8],
+                                       float (&w)[8], float (&m)[8], float (&v)[8],
+                                       float (&r)[8]) {
+#pragma unroll
+  for (int j = 0; j < kGroup; ++j) {
+    const float x = __fmul_rn(g[j], gs);
+    if (EIGHT) v[j] = __fmul_rn(r[j], r[j]);
+    m[j] = __fadd_rn(__fmul_rn(m[j], a.b1), __fmul_rn(x, a.c1));
+    v[j] = __fadd_rn(__fmul_rn(v[j], a.b2), __fmul_rn(__fmul_rn(x, x), a.c2));
+    r[j] = __fsqrt_rn(v[j]);
+    float step;
+    if (EIGHT) step = m[j] * rcp_approx(fmaf(r[j], a.s2, a.eps));
+    else step = __fdiv_rn(m[j], __fadd_rn(__fmul_rn(r[j], a.s2), a.eps));
+    // w - decay w in one rounding: 1 - decay would be rounded before the product
+    w[j] = __fmaf_rn(-step, a.lr, __fmaf_rn(-w[j], decay, w[j]));
+  }
+}
+
 template <typename P, typename G, bool MASTER, bool EIGHT>
-__global__ void __launch_bounds__(kThreads)
-adamw_kernel(const __grid_constant__ Table tab, Args a, const float* __restrict__ grad_scale,
-             int* status) {
+__global__ void __launch_bounds__(kThreads, 4)
+adamw_kernel(const __grid_constant__ Table tab, const __grid_constant__ Args a,
+             const float* __restrict__ grad_scale, int* status) {
   const float gs = grad_scale ? *grad_scale : 1.f;
   if (!isfinite(gs)) {
     if (blockIdx.x == 0 && threadIdx.x == 0) atomicCAS(status, 0, SOMA_ERR_NONFINITE);
     return;
   }
-  bool bad = false;
   for (int64_t chunk = blockIdx.x; chunk < tab.chunks; chunk += gridDim.x) {
     int lo = 0, hi = tab.rows - 1;  // the last row whose first chunk is <= chunk
     while (lo < hi) {
@@ -168,60 +218,75 @@ adamw_kernel(const __grid_constant__ Table tab, Args a, const float* __restrict_
       if (tab.row[mid].first <= chunk) lo = mid; else hi = mid - 1;
     }
     const Row& t = tab.row[lo];
-    const int64_t base = (chunk - t.first) * kChunk;
-    const int64_t i = base + (int64_t)threadIdx.x * kGroup;
-    if (i - (threadIdx.x & 31) * kGroup >= t.n) continue;  // the whole warp is past the end
-    const int n = i >= t.n ? 0 : (int)(t.n - i < kGroup ? t.n - i : kGroup);
     const bool vec = t.vec != 0;
+    int64_t i = (chunk - t.first) * a.passes * kRow + (int64_t)threadIdx.x * kGroup;
+    for (int pass = 0; pass < a.passes; ++pass, i += kRow) {
+      if (i - (threadIdx.x & 31) * kGroup >= t.n) break;  // the whole warp is past the end
+      const int n = i >= t.n ? 0 : (int)(t.n - i < kGroup ? t.n - i : kGroup);
 
-    float g[8], w[8], m[8], v[8], r[8];
-    load_n(static_cast<const G*>(t.g) + i, vec, n, g);
-    if (MASTER) load_n(t.master + i, vec, n, w);
-    else load_n(static_cast<const P*>(t.p) + i, vec, n, w);
-    if (EIGHT) {
-      unpack8(load_bytes(static_cast<const uint8_t*>(t.m) + i, vec, n), t.ms[i / kBlock8], m);
-      unpack8(load_bytes(static_cast<const uint8_t*>(t.v) + i, vec, n), t.vs[i / kBlock8], r);
-    } else {
-      load_n(static_cast<const float*>(t.m) + i, vec, n, m);
-      load_n(static_cast<const float*>(t.v) + i, vec, n, v);
-    }
+      float g[8], w[8], m[8], v[8], r[8];
+      const auto load_state = [&] {
+        if (MASTER) load_n(t.master + i, vec, n, w);
+        else load_n(static_cast<const P*>(t.p) + i, vec, n, w);
+        if (EIGHT) {
+          const uint2 bm = load_bytes(static_cast<const uint8_t*>(t.m) + i, vec, n);
+          const uint2 bv = load_bytes(static_cast<const uint8_t*>(t.v) + i, vec, n);
+          const float ms = t.ms[i / kBlock8], vs = t.vs[i / kBlock8];
+          unpack8(bm, ms, m);
+          unpack8(bv, vs, r);
+        } else {
+          load_n(static_cast<const float*>(t.m) + i, vec, n, m);
+          load_n(static_cast<const float*>(t.v) + i, vec, n, v);
+        }
+      };
+      load_n(static_cast<const G*>(t.g) + i, vec, n, g);
+      load_state();
+      update<EIGHT>(a, t.decay, gs, g, w, m, v, r);
+      float check = 0.f;  // NaN if any new moment is not finite
 #pragma unroll
-    for (int j = 0; j < kGroup; ++j) {
-      if (EIGHT) v[j] = __fmul_rn(r[j], r[j]);
-      const float x = __fmul_rn(g[j], gs);
-      const float m1 = __fadd_rn(__fmul_rn(m[j], a.b1), __fmul_rn(x, a.c1));
-      const float v1 = __fadd_rn(__fmul_rn(v[j], a.b2), __fmul_rn(__fmul_rn(x, x), a.c2));
-      const float r1 = __fsqrt_rn(v1);
-      const float step = __fdiv_rn(m1, __fadd_rn(__fmul_rn(r1, a.s2), a.eps));
-      if (isfinite(m1) && isfinite(v1)) {
-        // w - decay w in one rounding: 1 - decay would be rounded before the product
-        w[j] = __fmaf_rn(-step, a.lr, __fmaf_rn(-w[j], t.decay, w[j]));
-        m[j] = m1;
-        v[j] = v1;
-        r[j] = r1;
+      for (int j = 0; j < kGroup; ++j) check = fmaf(m[j], 0.f, fmaf(v[j], 0.f, check));
+      if (check != 0.f) {  // those elements keep what they had
+        uint32_t keep = 0;
+#pragma unroll
+        for (int j = 0; j < kGroup; ++j)
+          if (!(isfinite(m[j]) && isfinite(v[j]))) keep |= 1u << j;
+        float new_w[8], new_m[8], new_v[8], new_r[8];
+#pragma unroll
+        for (int j = 0; j < kGroup; ++j)
+          new_w[j] = w[j], new_m[j] = m[j], new_v[j] = v[j], new_r[j] = r[j];
+        load_state();
+#pragma unroll
+        for (int j = 0; j < kGroup; ++j)
+          if (!((keep >> j) & 1u))
+            w[j] = new_w[j], m[j] = new_m[j], v[j] = new_v[j], r[j] = new_r[j];
+        atomicCAS(status, 0, SOMA_ERR_NONFINITE);
+      }
+      __syncwarp();
+      if (MASTER) store_n(t.master + i, vec, n, w);
+      store_n(static_cast<P*>(t.p) + i, vec, n, w);
+      if (EIGHT) {
+        const uint64_t q = (uint64_t)i / kGroup;
+        const uint4 rnd = philox4x32_10(
+            make_uint4((uint32_t)q, (uint32_t)t.index, a.t, 0x80000002u), a.k0, a.k1);
+        uint32_t random[8];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          random[2 * j] = (word_of(rnd, j) << 4) & 0xFFFF0u;
+          random[2 * j + 1] = (word_of(rnd, j) >> 12) & 0xFFFF0u;
+        }
+        const uint2 bm = pack_block<false>(m, random, t.ms + i / kBlock8);
+        const uint2 bv = pack_block<true>(r, random, t.vs + i / kBlock8);
+        store_bytes(static_cast<uint8_t*>(t.m) + i, vec, n, bm);
+        store_bytes(static_cast<uint8_t*>(t.v) + i, vec, n, bv);
       } else {
-        bad = true;
+        store_n(static_cast<float*>(t.m) + i, vec, n, m);
+        store_n(static_cast<float*>(t.v) + i, vec, n, v);
       }
     }
-    if (MASTER) store_n(t.master + i, vec, n, w);
-    store_n(static_cast<P*>(t.p) + i, vec, n, w);
-    if (EIGHT) {
-      const uint64_t q = (uint64_t)i / kGroup;
-      const uint4 rnd = philox4x32_10(
-          make_uint4((uint32_t)q, (uint32_t)t.index, a.t, 0x80000002u), a.k0, a.k1);
-      const uint2 bm = pack_block(m, rnd, false, t.ms + i / kBlock8);
-      const uint2 bv = pack_block(r, rnd, true, t.vs + i / kBlock8);
-      store_bytes(static_cast<uint8_t*>(t.m) + i, vec, n, bm);
-      store_bytes(static_cast<uint8_t*>(t.v) + i, vec, n, bv);
-    } else {
-      store_n(static_cast<float*>(t.m) + i, vec, n, m);
-      store_n(static_cast<float*>(t.v) + i, vec, n, v);
-    }
   }
-  if (bad) atomicCAS(status, 0, SOMA_ERR_NONFINITE);
 }
 
-using Kernel = void (*)(const Table, Args, const float*, int*);
+using Kernel = void (*)(const Table, const Args, const float*, int*);
 
 template <typename P, typename G>
 Kernel pick(bool master, bool eight) {
@@ -294,6 +359,11 @@ extern "C" int soma_adamw_step(const soma_adamw_tensor* tensors, int n_tensors,
   a.k1 = (uint32_t)(cfg.seed >> 32);
   a.t = (uint32_t)cfg.t;
   const Kernel kernel = pick(cfg.param_dtype, cfg.grad_dtype, master, eight);
+  // four passes a chunk where that leaves enough chunks for every SM
+  int64_t total = 0;
+  for (int j = 0; j < n_tensors; ++j) total += tensors[j].count;
+  const int64_t resident = 152 * 4;
+  a.passes = eight && total >= 4 * resident * kRow * 4 ? 4 : 1;
 
   Table tab;
   int k = 0;
@@ -317,10 +387,9 @@ extern "C" int soma_adamw_step(const soma_adamw_tensor* tensors, int n_tensors,
       r.first = tab.chunks;
       r.vec = aligned(t.param, 16) && aligned(t.grad, 16) && aligned(t.m, eight ? 8 : 16) &&
               aligned(t.v, eight ? 8 : 16) && aligned(t.master, 16);
-      tab.chunks += (t.count + kChunk - 1) / kChunk;
+      tab.chunks += (t.count + (int64_t)a.passes * kRow - 1) / ((int64_t)a.passes * kRow);
     }
     if (!tab.rows) break;
-    const int64_t resident = 152 * 4;
     const unsigned grid = (unsigned)(tab.chunks < resident ? tab.chunks : resident);
     trace_begin(SOMA_TRACE_UPDATE, (cudaStream_t)stream);
     kernel<<<grid, kThreads, 0, (cudaStream_t)stream>>>(tab, a, grad_scale, status);
