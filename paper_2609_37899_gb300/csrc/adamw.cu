@@ -57,7 +57,7 @@ static_assert(sizeof(Table) + 256 <= 32764, "kernel parameter space");
 struct Args {
   float b1, c1, b2, c2;  // beta and 1 - beta
   float lr, s2, eps;     // lr / (1 - beta1^t), 1 / sqrt(1 - beta2^t)
-  uint32_t k0, k1, t;    // Philox key, update
+  uint32_t key[20], t;   // the ten Philox rounds' keys, update
   int32_t passes;        // of kRow elements in a chunk
 };
 
@@ -78,17 +78,23 @@ __device__ __forceinline__ uint32_t round_any(float y, uint32_t random, bool flo
   return __float_as_uint(r);
 }
 
-// Rounds the warp's 256 values x and returns this lane's eight bytes; the
-// scale goes to *scale.  FLOOR: the values are roots, none is negative, and
-// what is above zero stays above zero.
-template <bool FLOOR>
-__device__ __forceinline__ uint2 pack_block(const float (&x)[8], const uint32_t (&random)[8],
-                                            float* scale) {
-  float top = 0.f;
+// philox4x32_10 with the rounds' keys given.
+__device__ __forceinline__ uint4 random_block(uint4 ctr, const uint32_t (&key)[20]) {
 #pragma unroll
-  for (int j = 0; j < 8; ++j) top = fmaxf(top, fabsf(x[j]));
-  // non-negative floats order as their bits do
-  top = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(top)));
+  for (int r = 0; r < 10; ++r) {
+    const uint64_t p = (uint64_t)0xD2511F53u * ctr.x, q = (uint64_t)0xCD9E8D57u * ctr.z;
+    ctr = make_uint4((uint32_t)(q >> 32) ^ ctr.y ^ key[2 * r], (uint32_t)q,
+                     (uint32_t)(p >> 32) ^ ctr.w ^ key[2 * r + 1], (uint32_t)p);
+  }
+  return ctr;
+}
+
+// Rounds the warp's 256 values x, the largest magnitude of which is `top`, and
+// returns this lane's eight bytes; the scale goes to *scale.  FLOOR: the values
+// are roots, none is negative, and what is above zero stays above zero.
+template <bool FLOOR>
+__device__ __forceinline__ uint2 pack_block(const float (&x)[8], float top,
+                                            const uint32_t (&random)[8], float* scale) {
   // below 2^-100 the reciprocal could overflow: such a block is zero
   const bool some = top > 0x1p-100f;
   const float inv = some ? __fdiv_rn(kE4M3Max, top) : 0.f;
@@ -138,9 +144,11 @@ __device__ __forceinline__ void unpack8(const uint2& b, float scale, float (&x)[
   }
 }
 
-template <typename T>
-__device__ __forceinline__ void load_n(const T* p, bool vec, int n, float (&x)[8]) {
-  if (vec && n == kGroup) {
+// The eight elements from p, or the first n of them one by one (FULL: all, by
+// wide accesses).
+template <bool FULL, typename T>
+__device__ __forceinline__ void load_n(const T* p, int n, float (&x)[8]) {
+  if (FULL) {
     load8(p, x);
   } else {
 #pragma unroll
@@ -148,9 +156,9 @@ __device__ __forceinline__ void load_n(const T* p, bool vec, int n, float (&x)[8
   }
 }
 
-template <typename T>
-__device__ __forceinline__ void store_n(T* p, bool vec, int n, const float (&x)[8]) {
-  if (vec && n == kGroup) {
+template <bool FULL, typename T>
+__device__ __forceinline__ void store_n(T* p, int n, const float (&x)[8]) {
+  if (FULL) {
     store8(p, x);
   } else {
 #pragma unroll
@@ -159,8 +167,9 @@ __device__ __forceinline__ void store_n(T* p, bool vec, int n, const float (&x)[
   }
 }
 
-__device__ __forceinline__ uint2 load_bytes(const uint8_t* p, bool vec, int n) {
-  if (vec && n == kGroup) return *reinterpret_cast<const uint2*>(p);
+template <bool FULL>
+__device__ __forceinline__ uint2 load_bytes(const uint8_t* p, int n) {
+  if (FULL) return *reinterpret_cast<const uint2*>(p);
   uint32_t w[2] = {0u, 0u};
 #pragma unroll
   for (int j = 0; j < kGroup; ++j)
@@ -168,8 +177,9 @@ __device__ __forceinline__ uint2 load_bytes(const uint8_t* p, bool vec, int n) {
   return make_uint2(w[0], w[1]);
 }
 
-__device__ __forceinline__ void store_bytes(uint8_t* p, bool vec, int n, const uint2& b) {
-  if (vec && n == kGroup) {
+template <bool FULL>
+__device__ __forceinline__ void store_bytes(uint8_t* p, int n, const uint2& b) {
+  if (FULL) {
     *reinterpret_cast<uint2*>(p) = b;
   } else {
 #pragma unroll
@@ -184,22 +194,107 @@ __device__ __forceinline__ void store_bytes(uint8_t* p, bool vec, int n, const u
 // the special function unit in the 8-bit form (good to 2^-23), where
 // instructions are scarce.
 template <bool EIGHT>
-__device__ __forceinline__ void update(const Args& a, float decay, float gs, const float (&g)[8],
-                                       float (&w)[8], float (&m)[8], float (&v)[8],
-                                       float (&r)[8]) {
+__device__ __forceinline__ void update_one(const Args& a, float decay, float x, float& w, float& m,
+                                           float& v, float& r) {
+  if (EIGHT) v = __fmul_rn(r, r);
+  m = __fadd_rn(__fmul_rn(m, a.b1), __fmul_rn(x, a.c1));
+  v = __fadd_rn(__fmul_rn(v, a.b2), __fmul_rn(__fmul_rn(x, x), a.c2));
+  r = __fsqrt_rn(v);
+  float step;
+  if (EIGHT) step = m * rcp_approx(fmaf(r, a.s2, a.eps));
+  else step = __fdiv_rn(m, __fadd_rn(__fmul_rn(r, a.s2), a.eps));
+  // w - decay w in one rounding: 1 - decay would be rounded before the product
+  w = __fmaf_rn(-step, a.lr, __fmaf_rn(-w, decay, w));
+}
+
+// The thread's eight elements from i on, n of which exist.  FULL: all of the
+// warp's exist and are aligned.  Returns whether an element's new moments were
+// not finite: it keeps what it had.
+template <typename P, typename G, bool MASTER, bool EIGHT, bool FULL>
+__device__ __forceinline__ bool eight_elements(const Row& t, const Args& a, float gs, int64_t i,
+                                               int n) {
+  const int64_t block = (int64_t)((uint64_t)i / kBlock8);
+  float g[8], w[8], m[8], v[8], r[8];
+  const auto load_state = [&] {
+    if (MASTER) load_n<FULL>(t.master + i, n, w);
+    else load_n<FULL>(static_cast<const P*>(t.p) + i, n, w);
+    if (EIGHT) {
+      const uint2 bm = load_bytes<FULL>(static_cast<const uint8_t*>(t.m) + i, n);
+      const uint2 bv = load_bytes<FULL>(static_cast<const uint8_t*>(t.v) + i, n);
+      const float ms = t.ms[block], vs = t.vs[block];
+      unpack8(bm, ms, m);
+      unpack8(bv, vs, r);
+    } else {
+      load_n<FULL>(static_cast<const float*>(t.m) + i, n, m);
+      load_n<FULL>(static_cast<const float*>(t.v) + i, n, v);
+    }
+  };
+  load_n<FULL>(static_cast<const G*>(t.g) + i, n, g);
+  load_state();
+  bool bad = false;
+  float top_m = 0.f, top_r = 0.f;
+  if (EIGHT) {
 #pragma unroll
-  for (int j = 0; j < kGroup; ++j) {
-    const float x = __fmul_rn(g[j], gs);
-    if (EIGHT) v[j] = __fmul_rn(r[j], r[j]);
-    m[j] = __fadd_rn(__fmul_rn(m[j], a.b1), __fmul_rn(x, a.c1));
-    v[j] = __fadd_rn(__fmul_rn(v[j], a.b2), __fmul_rn(__fmul_rn(x, x), a.c2));
-    r[j] = __fsqrt_rn(v[j]);
-    float step;
-    if (EIGHT) step = m[j] * rcp_approx(fmaf(r[j], a.s2, a.eps));
-    else step = __fdiv_rn(m[j], __fadd_rn(__fmul_rn(r[j], a.s2), a.eps));
-    // w - decay w in one rounding: 1 - decay would be rounded before the product
-    w[j] = __fmaf_rn(-step, a.lr, __fmaf_rn(-w[j], decay, w[j]));
+    for (int j = 0; j < kGroup; ++j)
+      update_one<true>(a, t.decay, __fmul_rn(g[j], gs), w[j], m[j], v[j], r[j]);
+    // The bits of non-negative floats order as the floats do, NaN above all:
+    // one reduction gives the scale and whether all roots are finite.  A first
+    // moment that is not comes with a second one that is not: the square of a
+    // gradient overflows long before the gradient does.
+    const auto largest = [](const float (&x)[8]) {
+      uint32_t top = 0u;
+#pragma unroll
+      for (int j = 0; j < kGroup; ++j) top = max(top, __float_as_uint(x[j]) & 0x7FFFFFFFu);
+      return __reduce_max_sync(0xffffffffu, top);
+    };
+    uint32_t bits = largest(r);
+    if (bits >= 0x7F800000u) {  // the whole warp
+      uint32_t keep = 0;
+      float new_w[8], new_m[8], new_r[8];
+#pragma unroll
+      for (int j = 0; j < kGroup; ++j) {
+        if (!isfinite(r[j]) || !isfinite(m[j])) keep |= 1u << j;
+        new_w[j] = w[j], new_m[j] = m[j], new_r[j] = r[j];
+      }
+      load_state();
+#pragma unroll
+      for (int j = 0; j < kGroup; ++j)
+        if (!((keep >> j) & 1u)) w[j] = new_w[j], m[j] = new_m[j], r[j] = new_r[j];
+      bad = keep != 0;
+      bits = largest(r);
+    }
+    top_r = __uint_as_float(bits);
+    top_m = __uint_as_float(largest(m));
+  } else {
+#pragma unroll
+    for (int j = 0; j < kGroup; ++j) {
+      float w1 = w[j], m1 = m[j], v1 = v[j];
+      update_one<false>(a, t.decay, __fmul_rn(g[j], gs), w1, m1, v1, r[j]);
+      if (isfinite(m1) && isfinite(v1)) w[j] = w1, m[j] = m1, v[j] = v1;
+      else bad = true;
+    }
   }
+  if (MASTER) store_n<FULL>(t.master + i, n, w);
+  store_n<FULL>(static_cast<P*>(t.p) + i, n, w);
+  if (EIGHT) {
+    const uint64_t q = (uint64_t)i / kGroup;
+    const uint4 rnd =
+        random_block(make_uint4((uint32_t)q, (uint32_t)t.index, a.t, 0x80000002u), a.key);
+    uint32_t random[8];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      random[2 * j] = (word_of(rnd, j) << 4) & 0xFFFF0u;
+      random[2 * j + 1] = (word_of(rnd, j) >> 12) & 0xFFFF0u;
+    }
+    const uint2 bm = pack_block<false>(m, top_m, random, t.ms + block);
+    const uint2 bv = pack_block<true>(r, top_r, random, t.vs + block);
+    store_bytes<FULL>(static_cast<uint8_t*>(t.m) + i, n, bm);
+    store_bytes<FULL>(static_cast<uint8_t*>(t.v) + i, n, bv);
+  } else {
+    store_n<FULL>(static_cast<float*>(t.m) + i, n, m);
+    store_n<FULL>(static_cast<float*>(t.v) + i, n, v);
+  }
+  return bad;
 }
 
 template <typename P, typename G, bool MASTER, bool EIGHT>
@@ -211,6 +306,7 @@ adamw_kernel(const __grid_constant__ Table tab, const __grid_constant__ Args a,
     if (blockIdx.x == 0 && threadIdx.x == 0) atomicCAS(status, 0, SOMA_ERR_NONFINITE);
     return;
   }
+  bool bad = false;
   for (int64_t chunk = blockIdx.x; chunk < tab.chunks; chunk += gridDim.x) {
     int lo = 0, hi = tab.rows - 1;  // the last row whose first chunk is <= chunk
     while (lo < hi) {
@@ -218,72 +314,19 @@ adamw_kernel(const __grid_constant__ Table tab, const __grid_constant__ Args a,
       if (tab.row[mid].first <= chunk) lo = mid; else hi = mid - 1;
     }
     const Row& t = tab.row[lo];
-    const bool vec = t.vec != 0;
     int64_t i = (chunk - t.first) * a.passes * kRow + (int64_t)threadIdx.x * kGroup;
     for (int pass = 0; pass < a.passes; ++pass, i += kRow) {
-      if (i - (threadIdx.x & 31) * kGroup >= t.n) break;  // the whole warp is past the end
-      const int n = i >= t.n ? 0 : (int)(t.n - i < kGroup ? t.n - i : kGroup);
-
-      float g[8], w[8], m[8], v[8], r[8];
-      const auto load_state = [&] {
-        if (MASTER) load_n(t.master + i, vec, n, w);
-        else load_n(static_cast<const P*>(t.p) + i, vec, n, w);
-        if (EIGHT) {
-          const uint2 bm = load_bytes(static_cast<const uint8_t*>(t.m) + i, vec, n);
-          const uint2 bv = load_bytes(static_cast<const uint8_t*>(t.v) + i, vec, n);
-          const float ms = t.ms[i / kBlock8], vs = t.vs[i / kBlock8];
-          unpack8(bm, ms, m);
-          unpack8(bv, vs, r);
-        } else {
-          load_n(static_cast<const float*>(t.m) + i, vec, n, m);
-          load_n(static_cast<const float*>(t.v) + i, vec, n, v);
-        }
-      };
-      load_n(static_cast<const G*>(t.g) + i, vec, n, g);
-      load_state();
-      update<EIGHT>(a, t.decay, gs, g, w, m, v, r);
-      float check = 0.f;  // NaN if any new moment is not finite
-#pragma unroll
-      for (int j = 0; j < kGroup; ++j) check = fmaf(m[j], 0.f, fmaf(v[j], 0.f, check));
-      if (check != 0.f) {  // those elements keep what they had
-        uint32_t keep = 0;
-#pragma unroll
-        for (int j = 0; j < kGroup; ++j)
-          if (!(isfinite(m[j]) && isfinite(v[j]))) keep |= 1u << j;
-        float new_w[8], new_m[8], new_v[8], new_r[8];
-#pragma unroll
-        for (int j = 0; j < kGroup; ++j)
-          new_w[j] = w[j], new_m[j] = m[j], new_v[j] = v[j], new_r[j] = r[j];
-        load_state();
-#pragma unroll
-        for (int j = 0; j < kGroup; ++j)
-          if (!((keep >> j) & 1u))
-            w[j] = new_w[j], m[j] = new_m[j], v[j] = new_v[j], r[j] = new_r[j];
-        atomicCAS(status, 0, SOMA_ERR_NONFINITE);
-      }
-      __syncwarp();
-      if (MASTER) store_n(t.master + i, vec, n, w);
-      store_n(static_cast<P*>(t.p) + i, vec, n, w);
-      if (EIGHT) {
-        const uint64_t q = (uint64_t)i / kGroup;
-        const uint4 rnd = philox4x32_10(
-            make_uint4((uint32_t)q, (uint32_t)t.index, a.t, 0x80000002u), a.k0, a.k1);
-        uint32_t random[8];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          random[2 * j] = (word_of(rnd, j) << 4) & 0xFFFF0u;
-          random[2 * j + 1] = (word_of(rnd, j) >> 12) & 0xFFFF0u;
-        }
-        const uint2 bm = pack_block<false>(m, random, t.ms + i / kBlock8);
-        const uint2 bv = pack_block<true>(r, random, t.vs + i / kBlock8);
-        store_bytes(static_cast<uint8_t*>(t.m) + i, vec, n, bm);
-        store_bytes(static_cast<uint8_t*>(t.v) + i, vec, n, bv);
+      const int64_t warp_i = i - (threadIdx.x & 31) * kGroup;
+      if (warp_i >= t.n) break;
+      if (t.vec && warp_i + 32 * kGroup <= t.n) {
+        bad |= eight_elements<P, G, MASTER, EIGHT, true>(t, a, gs, i, kGroup);
       } else {
-        store_n(static_cast<float*>(t.m) + i, vec, n, m);
-        store_n(static_cast<float*>(t.v) + i, vec, n, v);
+        const int n = i >= t.n ? 0 : (int)(t.n - i < kGroup ? t.n - i : kGroup);
+        bad |= eight_elements<P, G, MASTER, EIGHT, false>(t, a, gs, i, n);
       }
     }
   }
+  if (bad) atomicCAS(status, 0, SOMA_ERR_NONFINITE);
 }
 
 using Kernel = void (*)(const Table, const Args, const float*, int*);
@@ -355,8 +398,10 @@ extern "C" int soma_adamw_step(const soma_adamw_tensor* tensors, int n_tensors,
   a.lr = (float)(cfg.lr / (1.0 - std::pow(cfg.beta1, (double)cfg.t)));
   a.s2 = (float)(1.0 / std::sqrt(1.0 - std::pow(cfg.beta2, (double)cfg.t)));
   a.eps = (float)cfg.eps;
-  a.k0 = (uint32_t)cfg.seed;
-  a.k1 = (uint32_t)(cfg.seed >> 32);
+  for (uint32_t r = 0; r < 10; ++r) {  // the key advances by the Weyl constants (philox4x32_10)
+    a.key[2 * r] = (uint32_t)cfg.seed + r * 0x9E3779B9u;
+    a.key[2 * r + 1] = (uint32_t)(cfg.seed >> 32) + r * 0xBB67AE85u;
+  }
   a.t = (uint32_t)cfg.t;
   const Kernel kernel = pick(cfg.param_dtype, cfg.grad_dtype, master, eight);
   // four passes a chunk where that leaves enough chunks for every SM
