@@ -1,13 +1,16 @@
 // adamw.cu -- AdamW over many tensors in one launch, moments in 32 bits or in
 // 8 (soma_adamw_step in include/soma_api.h has the formulas).
 //
-// Work is cut into chunks of one or four times kRow elements of one tensor; a
-// persistent grid takes them in turn and finds a chunk's tensor by bisection
-// over the first chunks, a table in the kernel's parameters (bisecting for
-// every kRow elements cost a ninth of the 8-bit kernel's instructions).  A
-// thread owns eight consecutive elements at a time, so every stream is read and
-// written in 8- to 32-byte pieces, and a warp owns 256: exactly one block of
-// the 8-bit state, whose new scale is the warp's maximum.
+// Work is cut into chunks of kChunk elements of one tensor, one CTA each, which
+// finds its tensor by bisection over the first chunks, a table in the kernel's
+// parameters.  (Resident CTAs that took chunks in turn were slower: 100M
+// parameters in 32 bits 451 us against 368, the copy rate of the memory being
+// 383.)  A thread owns eight consecutive elements, so every stream is read and
+// written in 8- to 32-byte pieces, and a warp owns 256: exactly one block of the
+// 8-bit state, whose new scale is the warp's maximum.
+//
+// Bytes bound the 32-bit form.  The 8-bit form has about 70 instructions for 14
+// to 16 bytes an element and reaches three quarters of the bytes' rate.
 #include <cmath>
 #include <cuda_fp8.h>
 
@@ -24,7 +27,7 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kGroup = 8;                          // elements of one thread
 constexpr int kBlock8 = 256;                       // elements that share a scale
-constexpr int kRow = kThreads * kGroup;            // elements of one pass of a CTA
+constexpr int kChunk = kThreads * kGroup;          // elements of one CTA
 constexpr int kMaxTensors = 360;                   // table rows of one launch
 static_assert(kBlock8 == 32 * kGroup, "a warp owns one block of the 8-bit state");
 
@@ -58,7 +61,6 @@ struct Args {
   float b1, c1, b2, c2;  // beta and 1 - beta
   float lr, s2, eps;     // lr / (1 - beta1^t), 1 / sqrt(1 - beta2^t)
   uint32_t key[20], t;   // the ten Philox rounds' keys, update
-  int32_t passes;        // of kRow elements in a chunk
 };
 
 // The two rounding forms of y = |x| / scale in [0, 448] to its e4m3 neighbour,
@@ -297,8 +299,10 @@ __device__ __forceinline__ bool eight_elements(const Row& t, const Args& a, floa
   return bad;
 }
 
+// Five CTAs an SM in 8 bits: at four its loads do not cover one another (299 us
+// against 271 for 100M parameters), at six registers spill.
 template <typename P, typename G, bool MASTER, bool EIGHT>
-__global__ void __launch_bounds__(kThreads, 4)
+__global__ void __launch_bounds__(kThreads, EIGHT ? 5 : 4)
 adamw_kernel(const __grid_constant__ Table tab, const __grid_constant__ Args a,
              const float* __restrict__ grad_scale, int* status) {
   const float gs = grad_scale ? *grad_scale : 1.f;
@@ -314,16 +318,14 @@ adamw_kernel(const __grid_constant__ Table tab, const __grid_constant__ Args a,
       if (tab.row[mid].first <= chunk) lo = mid; else hi = mid - 1;
     }
     const Row& t = tab.row[lo];
-    int64_t i = (chunk - t.first) * a.passes * kRow + (int64_t)threadIdx.x * kGroup;
-    for (int pass = 0; pass < a.passes; ++pass, i += kRow) {
-      const int64_t warp_i = i - (threadIdx.x & 31) * kGroup;
-      if (warp_i >= t.n) break;
-      if (t.vec && warp_i + 32 * kGroup <= t.n) {
-        bad |= eight_elements<P, G, MASTER, EIGHT, true>(t, a, gs, i, kGroup);
-      } else {
-        const int n = i >= t.n ? 0 : (int)(t.n - i < kGroup ? t.n - i : kGroup);
-        bad |= eight_elements<P, G, MASTER, EIGHT, false>(t, a, gs, i, n);
-      }
+    const int64_t i = (chunk - t.first) * kChunk + (int64_t)threadIdx.x * kGroup;
+    const int64_t warp_i = i - (threadIdx.x & 31) * kGroup;
+    if (warp_i >= t.n) continue;
+    if (t.vec && warp_i + 32 * kGroup <= t.n) {
+      bad |= eight_elements<P, G, MASTER, EIGHT, true>(t, a, gs, i, kGroup);
+    } else {
+      const int n = i >= t.n ? 0 : (int)(t.n - i < kGroup ? t.n - i : kGroup);
+      bad |= eight_elements<P, G, MASTER, EIGHT, false>(t, a, gs, i, n);
     }
   }
   if (bad) atomicCAS(status, 0, SOMA_ERR_NONFINITE);
@@ -404,11 +406,6 @@ extern "C" int soma_adamw_step(const soma_adamw_tensor* tensors, int n_tensors,
   }
   a.t = (uint32_t)cfg.t;
   const Kernel kernel = pick(cfg.param_dtype, cfg.grad_dtype, master, eight);
-  // four passes a chunk where that leaves enough chunks for every SM
-  int64_t total = 0;
-  for (int j = 0; j < n_tensors; ++j) total += tensors[j].count;
-  const int64_t resident = 152 * 4;
-  a.passes = eight && total >= 4 * resident * kRow * 4 ? 4 : 1;
 
   Table tab;
   int k = 0;
@@ -432,10 +429,11 @@ extern "C" int soma_adamw_step(const soma_adamw_tensor* tensors, int n_tensors,
       r.first = tab.chunks;
       r.vec = aligned(t.param, 16) && aligned(t.grad, 16) && aligned(t.m, eight ? 8 : 16) &&
               aligned(t.v, eight ? 8 : 16) && aligned(t.master, 16);
-      tab.chunks += (t.count + (int64_t)a.passes * kRow - 1) / ((int64_t)a.passes * kRow);
+      tab.chunks += (t.count + kChunk - 1) / kChunk;
     }
     if (!tab.rows) break;
-    const unsigned grid = (unsigned)(tab.chunks < resident ? tab.chunks : resident);
+    const int64_t most = (int64_t)1 << 30;
+    const unsigned grid = (unsigned)(tab.chunks < most ? tab.chunks : most);
     trace_begin(SOMA_TRACE_UPDATE, (cudaStream_t)stream);
     kernel<<<grid, kThreads, 0, (cudaStream_t)stream>>>(tab, a, grad_scale, status);
     trace_end(SOMA_TRACE_UPDATE, (cudaStream_t)stream);
