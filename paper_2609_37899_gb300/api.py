@@ -206,8 +206,14 @@ def _check(code: int, what: str):
         raise SomaError(code, what)
 
 
+# the current stream's handle without a torch.cuda.Stream object around it
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream(stream) -> ctypes.c_void_p:
     if stream is None:
+        if _raw_stream is not None:
+            return ctypes.c_void_p(_raw_stream(torch.cuda.current_device()))
         stream = torch.cuda.current_stream()
     return ctypes.c_void_p(stream.cuda_stream)
 
@@ -816,6 +822,9 @@ class AdamW:
             if masters is not None:
                 row.master = _dev(masters[k], torch.float32, f"masters[{k}]", size).value
             row.count, row.weight_decay = size, float(decay[k])
+        self._sizes = [p.numel() for p in params]
+        self._addresses = [p.data_ptr() for p in params]
+        self._in_table = [0] * n  # the gradients' addresses in the table
 
     @staticmethod
     def zero_state(params, bits: int = 32) -> dict:
@@ -840,10 +849,14 @@ class AdamW:
         dtype = grads[0].dtype if grads else torch.float32
         if dtype not in DTYPES:
             raise ValueError(f"grads: unsupported dtype {dtype}")
-        for k, (g, p, row) in enumerate(zip(grads, params, self._table)):
-            row.grad = _dev(g, dtype, f"grads[{k}]", row.count).value
-            if p.data_ptr() != (row.param or 0):
-                raise ValueError(f"params[{k}] was given other memory since the table was made")
+        if [p.data_ptr() for p in params] != self._addresses:
+            raise ValueError("params were given other memory since the table was made")
+        for k, (g, size) in enumerate(zip(grads, self._sizes)):
+            if not g.is_cuda or g.dtype != dtype or g.numel() != size or not g.is_contiguous():
+                _dev(g, dtype, f"grads[{k}]", size)  # says which it is
+            at = g.data_ptr()
+            if at != self._in_table[k]:
+                self._table[k].grad = self._in_table[k] = at
         cfg = soma_adamw_config(lr, beta1, beta2, eps, seed & (2 ** 64 - 1), t,
                                 DTYPES[self.param_dtype], DTYPES[dtype], self.bits)
         _check(lib().soma_adamw_step(
