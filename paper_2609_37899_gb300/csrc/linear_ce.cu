@@ -512,17 +512,48 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
   if (warp == 2) tc::tmem_dealloc_pair(tmem, 512);
 }
 
-// Joins a row's partial statistics: one warp per row.  lse and the target's
-// logit are several times the loss: their difference is taken before the small
-// terms are added, so that it does not lose half an ulp of their size.
+// Joins a row's partial statistics: one warp per row.
+//
+// The tensor cores cut an fp32 sum off instead of rounding it, so a logit comes
+// out short by about 1e-8 of itself for every 16 of its depth.  That matters
+// for the target's, which is large and enters the loss twice (960 deep: the
+// loss was off by 1.2e-6 of itself): it is computed here once more by fp32
+// multiply-adds and takes the other one's place in the sum and in the loss.
+// lse and the target's logit are several times the loss: their difference is
+// taken before the small terms are added.
+template <typename T>
 __global__ void __launch_bounds__(256)
-join_kernel(const float2* partial, int parts, const float* own, const int64_t* targets,
-            int64_t ignore, int64_t rows, int64_t vocab, float* loss, float* lse, int* status) {
+join_kernel(const float2* partial, int parts, const float* own, const T* h, int64_t hs,
+            const T* emb, int64_t es, const int64_t* targets, int64_t ignore, int64_t rows,
+            int64_t vocab, int64_t dim, float* loss, float* lse, int* status) {
   admit_successor();
   after_predecessor();
   const int64_t n = (int64_t)blockIdx.x * 8 + threadIdx.x / 32;
   if (n >= rows) return;
   const int lane = threadIdx.x % 32;
+  const int64_t y = targets[n];
+  if (y == ignore) {
+    if (lane == 0) loss[n] = lse[n] = 0.f;
+    return;
+  }
+  const bool has_target = y >= 0 && y < vocab;
+  float logit = 0.f;
+  if (has_target) {
+    const T* a = h + n * hs;
+    const T* b = emb + y * es;
+    for (int64_t j = lane * 8; j < dim; j += 256) {
+      union {
+        uint4 u;
+        T t[8];
+      } p, q;
+      p.u = row_piece(a, j, dim, true);
+      q.u = row_piece(b, j, dim, true);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) logit = fmaf(to_f32(p.t[k]), to_f32(q.t[k]), logit);
+    }
+#pragma unroll
+    for (int k = 16; k; k >>= 1) logit += __shfl_xor_sync(0xffffffffu, logit, k);
+  }
   float top = -INFINITY, sum = 0.f;
   for (int j = lane; j < parts; j += 32) {
     const float2 p = partial[n * parts + j];
@@ -539,13 +570,13 @@ join_kernel(const float2* partial, int parts, const float* own, const int64_t* t
     top = now;
   }
   if (lane) return;
-  const int64_t y = targets[n];
-  if (y == ignore) {
-    loss[n] = lse[n] = 0.f;
-    return;
+  if (has_target) {
+    const float instead =
+        tc::ex2(fmaf(logit, kLog2e, -top)) - tc::ex2(fmaf(own[n], kLog2e, -top));
+    sum += instead;
   }
   const float hi = top * kLn2, lo = fmaf(top, kLn2, -hi) + logf(sum);
-  const float r = y >= 0 && y < vocab ? (hi - own[n]) + lo : NAN;
+  const float r = has_target ? (hi - logit) + lo : NAN;
   lse[n] = hi + lo;
   loss[n] = isfinite(r) ? r : NAN;
   if (!isfinite(r)) atomicCAS(status, 0, SOMA_ERR_NONFINITE);
@@ -864,8 +895,9 @@ cudaError_t forward(const T* h, const T* emb, const soma_linear_ce_dims& d, cons
   const cudaError_t e =
       launch<kStats, T>(ma, mb, ma, w, (int64_t)w.m_tiles * w.splits, status, st);
   if (e != cudaSuccess) return e;
-  return launch_overlapped(join_kernel, (unsigned)ceil_div(d.rows, 8), 256, 0, st, w.partial,
-                           2 * p.splits, w.own, targets, ignore, d.rows, d.vocab, loss, lse, status);
+  return launch_overlapped(join_kernel<T>, (unsigned)ceil_div(d.rows, 8), 256, 0, st, w.partial,
+                           2 * p.splits, w.own, h, hs, emb, es, targets, ignore, d.rows, d.vocab,
+                           d.dim, loss, lse, status);
 }
 
 template <typename T>
