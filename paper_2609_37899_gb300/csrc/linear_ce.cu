@@ -65,6 +65,7 @@ struct __align__(16) RowInfo {
 // group, and a tile that several groups share is summed in as many slots.
 struct Work {
   int32_t m_tiles, n_tiles, k_stages;
+  int32_t tile_n;             // columns of a tile: kTile, or fewer (stats, grad)
   int32_t splits;             // stats
   int32_t pairs;              // of the grid
   int32_t columns, groups;    // sums
@@ -278,18 +279,21 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     const CUtensorMap* map = is_b ? &map_b : &map_a;
     const bool mn = is_b ? b_mn(KIND) : a_mn(KIND);
     const bool copies = lane < 4 && (mn || !sub);
+    const int half_n = w.tile_n / 2;  // rows of B that one CTA stages
+    const uint32_t bytes = 2 * (kOperandBytes + half_n * 128);
     const int y0 = is_b ? w.y_b : 0;
     uint32_t it = 0;
     bool ok = true;
     while (ok && walk.next(s, pair)) {
-      const int r0 = (is_b ? s.n : s.m) * kTile + (int)rank * kHalf + sub;
+      const int r0 = (is_b ? s.n * w.tile_n + (int)rank * half_n
+                           : s.m * kTile + (int)rank * kHalf) + sub;
       for (int k = s.k0; k < s.k1; ++k, ++it) {
         const uint32_t slot = it % kStages, round = it / kStages;
         if (!wait_or_abort(&sh.empty[slot], (round & 1) ^ 1, &sh, status)) {
           ok = false;
           break;
         }
-        if (rank == 0 && lane == 0) tc::mbar_arrive_expect_tx(&sh.full[slot], 2 * kStageBytes);
+        if (rank == 0 && lane == 0) tc::mbar_arrive_expect_tx(&sh.full[slot], bytes);
         __syncwarp();
         if (copies) {
           const int kx = k * tc::kDepth;
@@ -305,8 +309,8 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         tc::mbar_wait(&sh.full[j % kStages], (j / kStages) & 1);
   } else if (warp == 1 && rank == 0) {
     // MMA issuer of the pair: the whole warp waits, one elected thread issues
-    constexpr uint32_t idesc =
-        tc::idesc_16(kTile, kTile, !std::is_same<T, __half>::value, a_mn(KIND), b_mn(KIND));
+    const uint32_t idesc =
+        tc::idesc_16(kTile, w.tile_n, !std::is_same<T, __half>::value, a_mn(KIND), b_mn(KIND));
     uint32_t it = 0, n_acc = 0;
     bool ok = true;
     while (ok && walk.next(s, pair)) {
@@ -368,36 +372,52 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         info = {0.f, 0.f, 0.f, -1};
         if (live) info = w.info[m];
       }
+      // dh: the target's row of emb, 32 columns ahead of their use
+      const T* e_row = nullptr;
+      uint4 e_next[4];
+      const auto fetch_e = [&](int64_t n) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          e_next[j] = make_uint4(0u, 0u, 0u, 0u);
+          if (info.y >= 0 && n + 8 * j < w.N) e_next[j] = row_piece(e_row, n + 8 * j, w.N, true);
+        }
+      };
+      if (KIND == kDh) {
+        e_row = static_cast<const T*>(w.emb) + (info.y < 0 ? 0 : info.y) * w.emb_stride;
+        fetch_e((int64_t)s.n * w.tile_n + half * (w.tile_n / 2));
+      }
       const uint32_t buf = n_acc & 1;
       // a tile's whole depth may lie before this: allow it more time
       if (!wait_or_abort(&sh.acc_full[buf], (n_acc >> 1) & 1, &sh, status, 1u << 27)) break;
       tc::tc_fence_after();
-      const uint32_t src = tmem + buf * kTile + half * kHalf + ((uint32_t)(quarter * 32) << 16);
-      const int64_t n0 = (int64_t)s.n * kTile + half * kHalf;
+      const int half_n = w.tile_n / 2;
+      const uint32_t src = tmem + buf * kTile + half * half_n + ((uint32_t)(quarter * 32) << 16);
+      const int64_t n0 = (int64_t)s.n * w.tile_n + half * half_n;
+      const int64_t n_end = n0 + half_n < w.N ? n0 + half_n : w.N;
       // 32 columns at a time, the next ones on their way while these are used
       float next[32];
-      if (n0 < w.N && m0 < w.M) tc::tmem_ld32_nowait(src, next);
+      if (n0 < n_end && m0 < w.M) tc::tmem_ld32_nowait(src, next);
 #pragma unroll
       for (int c = 0; c < kHalf; c += 32) {
         const int64_t n = n0 + c;
-        if (n >= w.N || m0 >= w.M) break;  // nothing there (the whole warp)
+        if (n >= n_end || m0 >= w.M) break;  // nothing there (the whole warp)
         tc::tmem_wait_ld32(next);
         float x[32];
 #pragma unroll
         for (int j = 0; j < 32; ++j) x[j] = next[j];
-        if (c + 32 < kHalf && n + 32 < w.N) tc::tmem_ld32_nowait(src + c + 32, next);
+        if (c + 32 < kHalf && n + 32 < n_end) tc::tmem_ld32_nowait(src + c + 32, next);
         if (KIND == kStats) {
           const int64_t hit = y - n;
           if (hit >= 0 && hit < 32) {
             float v = 0.f;
 #pragma unroll
             for (int j = 0; j < 32; ++j) v = j == hit ? x[j] : v;
-            if (y < w.N) w.own[m] = v;
+            if (y < n_end) w.own[m] = v;
           }
-          if (n + 32 > w.N) {
+          if (n + 32 > n_end) {
 #pragma unroll
             for (int j = 0; j < 32; ++j)
-              if (n + j >= w.N) x[j] = -INFINITY;
+              if (n + j >= n_end) x[j] = -INFINITY;
           }
           // four chains each: one would wait for itself
           float mx[4] = {x[0], x[1], x[2], x[3]};
@@ -441,15 +461,17 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
           for (int j = 0; j < 32; ++j) x[j] *= scale;
         }
         if (KIND == kDh) {
-          const T* e = static_cast<const T*>(w.emb) + (info.y < 0 ? 0 : info.y) * w.emb_stride;
+          uint4 e[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) e[j] = e_next[j];
+          if (c + 32 < kHalf) fetch_e(n + 32);
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
             union {
               uint4 u;
               T t[8];
             } v;
-            v.u = make_uint4(0u, 0u, 0u, 0u);
-            if (info.y >= 0) v.u = row_piece(e, n + 8 * j, w.N, true);
+            v.u = e[j];
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
               float& o = x[8 * j + k];
@@ -475,7 +497,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                            pack2<T>(x[8 * j + 4], x[8 * j + 5]),
                            pack2<T>(x[8 * j + 6], x[8 * j + 7]));
         }
-        if (!sums(KIND) && c % 64 == 0 && n + 32 < w.N) continue;  // half a box so far
+        if (!sums(KIND) && c % 64 == 0 && n + 32 < n_end) continue;  // half a box so far
         const int bx = (int)(sums(KIND) ? n : n - c % 64);
         if (!sums(KIND) && w.out) {
           __syncwarp();
@@ -704,6 +726,7 @@ Work shares(int64_t M, int64_t N, int64_t depth) {
   w.M = M;
   w.N = N;
   w.m_tiles = (int32_t)ceil_div(M, kTile);
+  w.tile_n = kTile;
   w.n_tiles = (int32_t)ceil_div(N, kTile);
   w.k_stages = (int32_t)ceil_div(depth, tc::kDepth);
   w.columns = w.n_tiles < kPairs ? w.n_tiles : kPairs;
@@ -731,6 +754,14 @@ int64_t tiles_cost(int64_t M, int64_t N, int64_t depth) {
          kLaunchStages;
 }
 
+// Stats and grad take tiles of half the columns where those occupy the GPU
+// better: 8192 x 256 x 960 is 32 whole tiles or 64 half ones for 76 pairs (grad
+// 14 -> 12 us).  A half tile's stage takes 0.7 of a whole one's: its copies,
+// half of which are A's, not its products.  Widths in between were tried where
+// they divide the vocabulary evenly among the pairs (64 x 32768 in 147 tiles of
+// 224) and were slower, 19.7 us against 18.4.
+constexpr double kHalfTile = 0.7;
+
 // Whether a matrix of `copied` rows is copied to rows of a multiple of 64
 // elements before `rows` rows are multiplied by it: a stride that is no
 // multiple of 8 cannot be read in boxes at all, and one that is no multiple of
@@ -744,7 +775,7 @@ bool copied(int64_t stride, int64_t rows, bool backward) {
 }
 
 struct Plan {
-  int32_t splits;                // forward
+  int32_t splits, tile_n;        // forward
   int64_t piece;                 // backward: vocabulary entries of one piece
   bool dh_sums, demb_sums;       // which kernels the products take
   int64_t g_stride, acc_stride, dh_slots, demb_slots;
@@ -807,13 +838,18 @@ Plan plan(soma_linear_ce_dims d, bool backward) {
   if (p.copy_emb) p.emb = take((size_t)d.vocab * round64(d.dim) * 2);
   if (!backward) {
     // rounds of pairs times the tiles of a unit, least first
-    const int64_t mt = ceil_div(d.rows, kTile), vt = ceil_div(d.vocab, kTile);
-    int64_t best = INT64_MAX;
-    for (int64_t s = 1; s <= vt && s <= 4 * kPairs; ++s) {
-      const int64_t cost = ceil_div(mt * s, kPairs) * ceil_div(vt, s);
-      if (cost < best) {
-        best = cost;
-        p.splits = (int32_t)s;
+    const int64_t mt = ceil_div(d.rows, kTile);
+    double best = 1e300;
+    for (const int tile_n : {kTile, kTile / 2}) {
+      const int64_t vt = ceil_div(d.vocab, tile_n);
+      for (int64_t s = 1; s <= vt && s <= 4 * kPairs; ++s) {
+        const double cost = (double)(ceil_div(mt * s, kPairs) * ceil_div(vt, s)) *
+                            (tile_n == kTile ? 1 : kHalfTile);
+        if (cost < best * 0.995) {
+          best = cost;
+          p.splits = (int32_t)s;
+          p.tile_n = tile_n;
+        }
       }
     }
     p.partial = take((size_t)d.rows * 2 * p.splits * sizeof(float2));
@@ -880,11 +916,12 @@ cudaError_t forward(const T* h, const T* emb, const soma_linear_ce_dims& d, cons
   if (!h || !emb) return cudaErrorLaunchFailure;
   CUtensorMap ma, mb;
   if (!make_tile_map(&ma, h, dtype_of<T>(), d.rows, d.dim, hs, kHalf) ||
-      !make_tile_map(&mb, emb, dtype_of<T>(), d.vocab, d.dim, es, kHalf))
+      !make_tile_map(&mb, emb, dtype_of<T>(), d.vocab, d.dim, es, p.tile_n / 2))
     return cudaErrorInvalidValue;
   Work w = {};
   w.m_tiles = (int32_t)ceil_div(d.rows, kTile);
-  w.n_tiles = (int32_t)ceil_div(d.vocab, kTile);
+  w.tile_n = p.tile_n;
+  w.n_tiles = (int32_t)ceil_div(d.vocab, p.tile_n);
   w.k_stages = (int32_t)ceil_div(d.dim, tc::kDepth);
   w.splits = p.splits;
   w.M = d.rows;
@@ -931,10 +968,11 @@ cudaError_t backward(const T* h, const T* emb, const soma_linear_ce_dims& d,
   const bool many = p.piece < d.vocab;
   const bool dh_tiled = dhs % 8 == 0 && aligned(dh, 16);
   const bool demb_tiled = des % 8 == 0 && aligned(demb, 16);
-  CUtensorMap h_k, h_mn, e_k, e_mn, dh_out, demb_sum;
+  CUtensorMap h_k, h_mn, e_k, e_k_half, e_mn, dh_out, demb_sum;
   bool ok = make_tile_map(&h_k, copy, dtype, d.rows, d.dim, cs, kHalf) &&
             make_tile_map(&h_mn, copy, dtype, d.rows, d.dim, cs, 64) &&
             make_tile_map(&e_k, emb, dtype, d.vocab, d.dim, es, kHalf) &&
+            make_tile_map(&e_k_half, emb, dtype, d.vocab, d.dim, es, kHalf / 2) &&
             make_tile_map(&e_mn, emb, dtype, d.vocab, d.dim, es, 64);
   if (p.dh_sums)
     ok = ok && make_tile_map(&dh_out, dh_acc, SOMA_FP32,
@@ -962,13 +1000,17 @@ cudaError_t backward(const T* h, const T* emb, const soma_linear_ce_dims& d,
     w.M = d.rows;
     w.N = width;
     w.m_tiles = (int32_t)ceil_div(w.M, kTile);
-    w.n_tiles = (int32_t)ceil_div(w.N, kTile);
+    const auto rounds = [&](int64_t tile_n) {
+      return (double)ceil_div(w.m_tiles * ceil_div(width, tile_n), kPairs);
+    };
+    w.tile_n = kHalfTile * rounds(kTile / 2) < rounds(kTile) ? kTile / 2 : kTile;
+    w.n_tiles = (int32_t)ceil_div(w.N, w.tile_n);
     w.k_stages = (int32_t)ceil_div(d.dim, tc::kDepth);
     w.y_b = (int32_t)v0;
     w.info = info;
     w.v0 = v0;
     w.top = top;
-    e = launch<kGrad, T>(h_k, e_k, g_out, w, (int64_t)w.m_tiles * w.n_tiles, status, st);
+    e = launch<kGrad, T>(h_k, w.tile_n == kTile ? e_k : e_k_half, g_out, w, (int64_t)w.m_tiles * w.n_tiles, status, st);
     if (e != cudaSuccess) return e;
 
     w = shares(d.rows, d.dim, width);
