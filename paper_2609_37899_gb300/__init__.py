@@ -5,4 +5,4 @@ a C ABI, declared in ``include/soma_api.h``); ``api`` is its thin ctypes
 binding.  Importing this package loads nothing: ``api`` loads the library on
 first use and raises if it is missing.
 """
-__all__ = ["api", "inputs"]
+__all__ = ["api", "first_order", "inputs"]
