@@ -167,16 +167,10 @@ backward_tiled_kernel(const __grid_constant__ Maps maps, const __grid_constant__
     // the last rounds may be past the sequence's end: their gradients are zeros
     const int64_t rounds = (end - begin + rows - 1) / rows;
 
-    // warp 0; of the stores that this thread has made, the newest may still read
-    // its stage: the stage filled here is an older one, except at a chunk's start
-    const auto fill = [&](int64_t round, bool start) {
+    const auto fill = [&](int64_t round) {  // warp 0
       const int to = filled;
       filled = filled + 1 == depth ? 0 : filled + 1;
-      if (lane == 0) {
-        if (start || depth == 2) tc::bulk_wait_read();
-        else asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
-        tc::mbar_arrive_expect_tx(&ring.full[to], stage_elems * sizeof(T));
-      }
+      if (lane == 0) tc::mbar_arrive_expect_tx(&ring.full[to], stage_elems * sizeof(T));
       __syncwarp();
       if (lane < 5) {
         const int t = (int)(begin + round * rows);
@@ -186,7 +180,7 @@ backward_tiled_kernel(const __grid_constant__ Maps maps, const __grid_constant__
     };
     // one stage less in flight than there are: the newest is being stored
     if (warp == 0)
-      for (int64_t q = 0; q < depth - 1 && q < rounds; ++q) fill(rounds - 1 - q, true);
+      for (int64_t q = 0; q < depth - 1 && q < rounds; ++q) fill(rounds - 1 - q);
     float r[2] = {0.f, 0.f};
     if (on && dc_last) r[0] = dc_last[b * s.d.dim + ch], r[1] = dc_last[b * s.d.dim + ch + 1];
     Map<2> total = identity<2>();
@@ -254,11 +248,16 @@ backward_tiled_kernel(const __grid_constant__ Maps maps, const __grid_constant__
       Map<2> m;
       split(A, m.a[0], m.a[1]);
       split(B, m.b[0], m.b[1]);
+      float in[2];
       if (MAPS) {
         join_total<true, RAGGED, kWarps>(shared, m, turn++, total);
       } else {
-        float in[2];
+        if (lane == 0) tc::bulk_wait_read();  // this warp's stores of the round before
         join<true, RAGGED, kWarps>(shared, m, turn++, r, in);
+      }
+      // every warp is through with the stage of the round before
+      if (warp == 0 && round >= depth - 1) fill(round - (depth - 1));
+      if (!MAPS) {
         Two x = two(in[0], in[1]);
 #pragma unroll
         for (int j = kSegment - 1; j >= 0; --j) {
@@ -274,19 +273,15 @@ backward_tiled_kernel(const __grid_constant__ Maps maps, const __grid_constant__
             if (j >= live)
               for (int g = 0; g < 3; ++g) store_two(p + g * gate + j * kBlock, two(0.f));
         }
+        // each warp stores its own steps: no barrier of the CTA
         tc::fence_async_smem();
-        __syncthreads();
-      }
-      if (warp == 0) {
-        if (!MAPS && lane == 0) {
-          const int t = (int)(begin + round * rows);
+        __syncwarp();
+        if (lane == 0 && t0 < end) {
           for (int g = 0; g < 4; ++g)
-            box_s2g(&maps.out[g], ch0, maps.t_inner ? t : (int)b, maps.t_inner ? (int)b : t,
-                    stages + (size_t)st * stage_elems + g * gate);
+            box_s2g(&maps.out[g], ch0, maps.t_inner ? (int)t0 : (int)b,
+                    maps.t_inner ? (int)b : (int)t0, p - 2 * lane + g * gate);
           tc::bulk_commit();
         }
-        __syncwarp();
-        if (round >= depth - 1) fill(round - (depth - 1), false);
       }
       if (++st == depth) st = 0, parity ^= 1;
     }
@@ -296,10 +291,11 @@ backward_tiled_kernel(const __grid_constant__ Maps maps, const __grid_constant__
     } else if (dc0 && on && k == 0 && warp == 0) {
       dc0[b * s.d.dim + ch] = r[0], dc0[b * s.d.dim + ch + 1] = r[1];
     }
-    __syncthreads();
+    if (!MAPS && lane == 0) tc::bulk_wait_read();
+    __syncthreads();  // the stages are free
   }
   admit_successor();
-  if (!MAPS && threadIdx.x == 0) tc::bulk_wait();
+  if (!MAPS && lane == 0) tc::bulk_wait();
 }
 
 // ------------------------------------------------------------------- host --
@@ -327,7 +323,7 @@ cudaError_t backward(const void* gates, Scan s, const void* dh, const float* dc_
     maps.t_inner = t_inner;
     if (!map_all(maps.in, 4, gates, s.d, s.gs, t_inner, dtype, rows) ||
         !map_all(maps.in + 4, 1, dh, s.d, s.hs, t_inner, dtype, rows) ||
-        !map_all(maps.out, 4, dgates, s.d, s.ds, t_inner, dtype, rows))
+        !map_all(maps.out, 4, dgates, s.d, s.ds, t_inner, dtype, kSegment))
       return cudaErrorInvalidValue;
     s.depth = sizeof(T) == 4 ? 2 : 3;
     const size_t smem = tiled_bytes<T>(s.depth, 5, f.warps);

@@ -24,7 +24,8 @@
 #pragma once
 
 #include <cmath>
-#include <initializer_list>
+#include <cstring>
+#include <type_traits>
 
 #include "checked.cuh"
 #include "numeric.cuh"
@@ -349,19 +350,27 @@ __device__ __forceinline__ void box_s2g(const CUtensorMap* map, int x, int y, in
       : "memory");
 }
 
-// A lane's two channels in shared memory.
-__device__ __forceinline__ Two load_two(const float* p) {
-  const float2 x = *reinterpret_cast<const float2*>(p);
-  return two(x.x, x.y);
+// A lane's two channels in shared memory, as they are and as fp32.
+__device__ __forceinline__ float2 load_raw(const float* p) {
+  return *reinterpret_cast<const float2*>(p);
 }
-__device__ __forceinline__ Two load_two(const __nv_bfloat16* p) {
-  const uint32_t x = *reinterpret_cast<const uint32_t*>(p);
-  return two(__uint_as_float(x << 16), __uint_as_float(x & 0xFFFF0000u));
+template <typename T>
+__device__ __forceinline__ uint32_t load_raw(const T* p) {
+  return *reinterpret_cast<const uint32_t*>(p);
 }
-__device__ __forceinline__ Two load_two(const __half* p) {
-  const float2 x = __half22float2(*reinterpret_cast<const __half2*>(p));
-  return two(x.x, x.y);
+template <typename T>
+__device__ __forceinline__ Two widen(float2 x) { return two(x.x, x.y); }
+template <typename T>
+__device__ __forceinline__ Two widen(uint32_t x) {
+  if (std::is_same<T, __nv_bfloat16>::value)
+    return two(__uint_as_float(x << 16), __uint_as_float(x & 0xFFFF0000u));
+  __half2 h;
+  memcpy(&h, &x, 4);
+  const float2 f = __half22float2(h);
+  return two(f.x, f.y);
 }
+template <typename T>
+__device__ __forceinline__ Two load_two(const T* p) { return widen<T>(load_raw(p)); }
 __device__ __forceinline__ void store_two(float* p, Two x) {
   float a, b;
   split(x, a, b);

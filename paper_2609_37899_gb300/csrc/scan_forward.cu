@@ -157,10 +157,8 @@ forward_tiled_kernel(const __grid_constant__ Maps maps, const __grid_constant__ 
                 maps.t_inner ? t : (int)b, maps.t_inner ? (int)b : t, &ring.full[to]);
       }
     };
-    // one stage less in flight than there are: the newest is read to the end of
-    // its round
     if (warp == 0)
-      for (int64_t q = 0; q < depth - 1 && q < rounds; ++q) fill(q);
+      for (int64_t q = 0; q < depth && q < rounds; ++q) fill(q);
     float c[2] = {0.f, 0.f};
     if (on && s.c0) c[0] = s.c0[b * s.d.dim + ch], c[1] = s.c0[b * s.d.dim + ch + 1];
     Map<2> total = identity<2>();
@@ -171,6 +169,7 @@ forward_tiled_kernel(const __grid_constant__ Maps maps, const __grid_constant__ 
       ring_wait(ring, st, parity, status);
       const T* p = stages + (size_t)st * stage_elems + warp * kSegment * kBlock + 2 * lane;
       Two f[kSegment], u[kSegment];
+      decltype(load_raw(p)) o[kSegment];  // kept, so that the stage is free after the join
       Two A = two(1.f), B = two(0.f);
       // steps of this segment that exist: nearly always all of them, and the
       // whole warp takes the branch without their checks
@@ -179,6 +178,7 @@ forward_tiled_kernel(const __grid_constant__ Maps maps, const __grid_constant__ 
       for (int j = 0; j < kSegment; ++j) {
         const Two ai = load_two(p + j * kBlock), af = load_two(p + gate + j * kBlock);
         const Two ag = load_two(p + 2 * gate + j * kBlock);
+        if (!MAPS) o[j] = load_raw(p + 3 * gate + j * kBlock);
         Two num, den;
         tanh_parts2(ag, num, den);
         u[j] = num * rcp2(den * one_exp2(ai));
@@ -205,8 +205,8 @@ forward_tiled_kernel(const __grid_constant__ Maps maps, const __grid_constant__ 
       float in[2];
       if (MAPS) join_total<false, RAGGED, kWarps>(shared, m, turn++, total);
       else join<false, RAGGED, kWarps>(shared, m, turn++, c, in);
-      // every warp is through with the stage of the round before
-      if (warp == 0 && round + depth - 1 < rounds) fill(round + depth - 1);
+      // every warp has read the stage
+      if (warp == 0 && round + depth < rounds) fill(round + depth);
       if (!MAPS && on) {
         if (s.marks && t0 < end)
           *reinterpret_cast<float2*>(s.marks + (b * marks + t0 / kSegment) * s.d.dim + ch) =
@@ -218,7 +218,7 @@ forward_tiled_kernel(const __grid_constant__ Maps maps, const __grid_constant__ 
           x = RAGGED ? apply2(f[j], u[j], x) : fma2(f[j], x, u[j]);
           Two num, den;
           tanh_parts2(x, num, den);
-          const Two y = num * rcp2(den * one_exp2(load_two(p + 3 * gate + j * kBlock)));
+          const Two y = num * rcp2(den * one_exp2(widen<T>(o[j])));
           if (live == kSegment) store_two(q, y);
           else if (t0 + j < end) store_two(q, j < live ? y : two(0.f));
           q += s.hs.t;
