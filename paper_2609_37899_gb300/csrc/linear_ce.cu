@@ -13,6 +13,7 @@
 //   demb_sums, dh_sums    fp32 sums over pieces, or over parts of the depth where
 //                         there are too few tiles to occupy the GPU otherwise;
 //                         sums_kernel rounds them
+#include <atomic>
 #include <cmath>
 
 #define SOMA_CHECK_FILE 10
@@ -38,7 +39,10 @@ constexpr uint32_t kOutBytes = 32 * 128;      // a warp's output box: 32 rows of
 constexpr int kThreads = 128 + 32 * kEpilogueWarps;
 constexpr size_t kSmem =                      // and what aligns the stages
     kStages * kStageBytes + kEpilogueWarps * kOutBytes + 1024;
-constexpr size_t kPieceBytes = (size_t)256 << 20;  // of G of one piece, at most
+// Of G of one piece, at most.  Smaller pieces would stay in the 129 MB L2 but
+// make dh's sums and the launches more (8192 x 131072 x 1024, both calls: 6.4 ms
+// at 48 MB, 5.6 at 96, 5.25 at 256, 5.5 at 512).
+constexpr size_t kPieceBytes = (size_t)256 << 20;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
@@ -66,6 +70,7 @@ struct __align__(16) RowInfo {
 struct Work {
   int32_t m_tiles, n_tiles, k_stages;
   int32_t tile_n;             // columns of a tile: kTile, or fewer (stats, grad)
+  int32_t rows_a;             // rows of A's box; fewer than 128: the odd CTA has none
   int32_t splits;             // stats
   int32_t pairs;              // of the grid
   int32_t columns, groups;    // sums
@@ -278,9 +283,13 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     const int sub = (lane & 1) * 64;
     const CUtensorMap* map = is_b ? &map_b : &map_a;
     const bool mn = is_b ? b_mn(KIND) : a_mn(KIND);
-    const bool copies = lane < 4 && (mn || !sub);
+    // Few rows (K-major A): the box ends with them, as boxes that reach past a
+    // matrix's end are slow, and the odd CTA copies none.  What the products
+    // make of the stage's other rows is not read.
+    const bool few = !a_mn(KIND) && w.rows_a < kHalf;
+    const bool copies = lane < 4 && (mn || !sub) && !(few && !is_b && rank);
     const int half_n = w.tile_n / 2;  // rows of B that one CTA stages
-    const uint32_t bytes = 2 * (kOperandBytes + half_n * 128);
+    const uint32_t bytes = (few ? w.rows_a * 128 : 2 * kOperandBytes) + 2 * half_n * 128;
     const int y0 = is_b ? w.y_b : 0;
     uint32_t it = 0;
     bool ok = true;
@@ -720,6 +729,9 @@ bool dims_ok(const soma_linear_ce_dims& d) {
 constexpr int64_t kLaunchStages = 18;
 constexpr int64_t kBytesPerStage = 2700000;
 
+// Rows of the boxes of a K-major A of M rows.
+int box_rows(int64_t M) { return M <= kHalf - 8 ? (int)round8(M) : kHalf; }
+
 // M x N sums over a depth, cut into shares.
 Work shares(int64_t M, int64_t N, int64_t depth) {
   Work w = {};
@@ -727,6 +739,7 @@ Work shares(int64_t M, int64_t N, int64_t depth) {
   w.N = N;
   w.m_tiles = (int32_t)ceil_div(M, kTile);
   w.tile_n = kTile;
+  w.rows_a = box_rows(M);
   w.n_tiles = (int32_t)ceil_div(N, kTile);
   w.k_stages = (int32_t)ceil_div(depth, tc::kDepth);
   w.columns = w.n_tiles < kPairs ? w.n_tiles : kPairs;
@@ -791,7 +804,8 @@ void plan_pieces(const soma_linear_ce_dims& d, Plan* p) {
   if (most < kTile) most = kTile;
   const int64_t fewest = ceil_div(d.vocab, most);
   int64_t best = INT64_MAX;
-  for (int64_t n = fewest; n < fewest + 24; ++n) {
+  // one piece has no sums over pieces, and then more would only add launches
+  for (int64_t n = fewest; n < fewest + (fewest == 1 ? 1 : 24); ++n) {
     int64_t width = n == 1 ? d.vocab : ceil_div(ceil_div(d.vocab, n), kTile) * kTile;
     if (width > d.vocab) width = d.vocab;
     const int64_t full = d.vocab / width, rest = d.vocab % width;
@@ -842,14 +856,19 @@ Plan plan(soma_linear_ce_dims d, bool backward) {
     double best = 1e300;
     for (const int tile_n : {kTile, kTile / 2}) {
       const int64_t vt = ceil_div(d.vocab, tile_n);
-      for (int64_t s = 1; s <= vt && s <= 4 * kPairs; ++s) {
-        const double cost = (double)(ceil_div(mt * s, kPairs) * ceil_div(vt, s)) *
-                            (tile_n == kTile ? 1 : kHalfTile);
+      // as many splits as fit r rounds of the pairs
+      for (int64_t r = ceil_div(mt, kPairs), tried = 0; tried < 64; ++r, ++tried) {
+        const int64_t fit = r * kPairs / mt;
+        const int64_t s = fit < vt ? fit : vt;
+        if (tried && s > 4 * kPairs) break;
+        const double cost =
+            (double)(r * ceil_div(vt, s)) * (tile_n == kTile ? 1 : kHalfTile);
         if (cost < best * 0.995) {
           best = cost;
           p.splits = (int32_t)s;
           p.tile_n = tile_n;
         }
+        if (s == vt) break;
       }
     }
     p.partial = take((size_t)d.rows * 2 * p.splits * sizeof(float2));
@@ -897,30 +916,39 @@ const T* pack(const T* x, int64_t rows, int64_t dim, int64_t* stride, T* copy, c
 template <int KIND, typename T>
 cudaError_t launch(const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& out, Work w,
                    int64_t units, int* status, cudaStream_t st) {
-  const cudaError_t ready = cudaFuncSetAttribute(
-      product_kernel<KIND, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem);
-  if (ready != cudaSuccess) return ready;
+  // the attribute stays with the kernel: asked for once per device
+  static std::atomic<uint64_t> ready{0};
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  const uint64_t bit = dev < 64 ? (uint64_t)1 << dev : 0;
+  if (!(ready.load(std::memory_order_relaxed) & bit) || !bit) {
+    e = cudaFuncSetAttribute(product_kernel<KIND, T>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                             (int)kSmem);
+    if (e != cudaSuccess) return e;
+    ready.fetch_or(bit, std::memory_order_relaxed);
+  }
   if (!sums(KIND)) w.pairs = (int32_t)(units < kPairs ? units : kPairs);
   return launch_overlapped(product_kernel<KIND, T>, 2 * w.pairs, kThreads, kSmem, st, a, b, out, w,
                            status);
 }
 
 template <typename T>
-cudaError_t forward(const T* h, const T* emb, const soma_linear_ce_dims& d, const int64_t* targets,
-                    int64_t ignore, float* loss, float* lse, uint8_t* ws, int* status,
-                    cudaStream_t st) {
-  const Plan p = plan(d, false);
+cudaError_t forward(const Plan& p, const T* h, const T* emb, const soma_linear_ce_dims& d,
+                    const int64_t* targets, int64_t ignore, float* loss, float* lse, uint8_t* ws,
+                    int* status, cudaStream_t st) {
   int64_t hs = d.h_stride, es = d.emb_stride;
   if (p.copy_h) h = pack(h, d.rows, d.dim, &hs, reinterpret_cast<T*>(ws + p.h), st);
   if (p.copy_emb) emb = pack(emb, d.vocab, d.dim, &es, reinterpret_cast<T*>(ws + p.emb), st);
   if (!h || !emb) return cudaErrorLaunchFailure;
   CUtensorMap ma, mb;
-  if (!make_tile_map(&ma, h, dtype_of<T>(), d.rows, d.dim, hs, kHalf) ||
+  if (!make_tile_map(&ma, h, dtype_of<T>(), d.rows, d.dim, hs, box_rows(d.rows)) ||
       !make_tile_map(&mb, emb, dtype_of<T>(), d.vocab, d.dim, es, p.tile_n / 2))
     return cudaErrorInvalidValue;
   Work w = {};
   w.m_tiles = (int32_t)ceil_div(d.rows, kTile);
   w.tile_n = p.tile_n;
+  w.rows_a = box_rows(d.rows);
   w.n_tiles = (int32_t)ceil_div(d.vocab, p.tile_n);
   w.k_stages = (int32_t)ceil_div(d.dim, tc::kDepth);
   w.splits = p.splits;
@@ -938,13 +966,12 @@ cudaError_t forward(const T* h, const T* emb, const soma_linear_ce_dims& d, cons
 }
 
 template <typename T>
-cudaError_t backward(const T* h, const T* emb, const soma_linear_ce_dims& d,
+cudaError_t backward(const Plan& p, const T* h, const T* emb, const soma_linear_ce_dims& d,
                      const int64_t* targets, int64_t ignore, const float* lse, const float* dloss,
                      T* dh, int64_t dhs, T* demb, int64_t des, uint8_t* ws, int* status,
                      cudaStream_t st) {
   if (d.rows == 0)
     return cudaMemset2DAsync(demb, des * 2, 0, d.dim * 2, d.vocab, st);
-  const Plan p = plan(d, true);
   constexpr int dtype = dtype_of<T>();
   RowInfo* info = reinterpret_cast<RowInfo*>(ws + p.info);
   T* copy = reinterpret_cast<T*>(ws + p.h);
@@ -969,7 +996,7 @@ cudaError_t backward(const T* h, const T* emb, const soma_linear_ce_dims& d,
   const bool dh_tiled = dhs % 8 == 0 && aligned(dh, 16);
   const bool demb_tiled = des % 8 == 0 && aligned(demb, 16);
   CUtensorMap h_k, h_mn, e_k, e_k_half, e_mn, dh_out, demb_sum;
-  bool ok = make_tile_map(&h_k, copy, dtype, d.rows, d.dim, cs, kHalf) &&
+  bool ok = make_tile_map(&h_k, copy, dtype, d.rows, d.dim, cs, box_rows(d.rows)) &&
             make_tile_map(&h_mn, copy, dtype, d.rows, d.dim, cs, 64) &&
             make_tile_map(&e_k, emb, dtype, d.vocab, d.dim, es, kHalf) &&
             make_tile_map(&e_k_half, emb, dtype, d.vocab, d.dim, es, kHalf / 2) &&
@@ -990,7 +1017,7 @@ cudaError_t backward(const T* h, const T* emb, const soma_linear_ce_dims& d,
   for (int64_t v0 = 0; v0 < d.vocab; v0 += p.piece) {
     const int64_t width = d.vocab - v0 < p.piece ? d.vocab - v0 : p.piece;
     CUtensorMap g_k, g_mn, g_out, demb_out = h_k;
-    if (!make_tile_map(&g_k, G, dtype, d.rows, width, p.g_stride, kHalf) ||
+    if (!make_tile_map(&g_k, G, dtype, d.rows, width, p.g_stride, box_rows(d.rows)) ||
         !make_tile_map(&g_mn, G, dtype, d.rows, width, p.g_stride, 64) ||
         !make_tile_map(&g_out, G, dtype, d.rows, width, p.g_stride, 32) ||
         (demb_tiled && !p.demb_sums &&
@@ -999,6 +1026,7 @@ cudaError_t backward(const T* h, const T* emb, const soma_linear_ce_dims& d,
     Work w = {};
     w.M = d.rows;
     w.N = width;
+    w.rows_a = box_rows(d.rows);
     w.m_tiles = (int32_t)ceil_div(w.M, kTile);
     const auto rounds = [&](int64_t tile_n) {
       return (double)ceil_div(w.m_tiles * ceil_div(width, tile_n), kPairs);
@@ -1072,7 +1100,8 @@ int soma_linear_ce_forward(const void* h, const void* emb, soma_linear_ce_dims d
   if (!h || !emb || !targets || !loss || !lse || !aligned(h, 16) || !aligned(emb, 16) ||
       !aligned(targets, 8) || !aligned(loss, 4) || !aligned(lse, 4))
     return SOMA_ERR_INVALID_ARG;
-  if (!workspace || !aligned(workspace, 16) || workspace_bytes < plan(d, false).total)
+  const Plan p = plan(d, false);
+  if (!workspace || !aligned(workspace, 16) || workspace_bytes < p.total)
     return SOMA_ERR_WORKSPACE;
   int* status = status_ptr();
   if (!status) return SOMA_ERR_CUDA;
@@ -1081,9 +1110,9 @@ int soma_linear_ce_forward(const void* h, const void* emb, soma_linear_ce_dims d
   trace_begin(SOMA_TRACE_HEAD, st);
   const cudaError_t e =
       d.dtype == SOMA_BF16
-          ? forward(static_cast<const __nv_bfloat16*>(h), static_cast<const __nv_bfloat16*>(emb),
+          ? forward(p, static_cast<const __nv_bfloat16*>(h), static_cast<const __nv_bfloat16*>(emb),
                     d, targets, ignore_index, loss, lse, ws, status, st)
-          : forward(static_cast<const __half*>(h), static_cast<const __half*>(emb), d, targets,
+          : forward(p, static_cast<const __half*>(h), static_cast<const __half*>(emb), d, targets,
                     ignore_index, loss, lse, ws, status, st);
   trace_end(SOMA_TRACE_HEAD, st);
   return e == cudaSuccess ? SOMA_OK : SOMA_ERR_CUDA;
@@ -1100,7 +1129,8 @@ int soma_linear_ce_backward(const void* h, const void* emb, soma_linear_ce_dims 
       dh_stride < d.dim || demb_stride < d.dim || dh_stride > ((int64_t)1 << 32) ||
       demb_stride > ((int64_t)1 << 32) || (d.rows && (!h || !targets || !lse || !dloss || !dh)))
     return SOMA_ERR_INVALID_ARG;
-  if (!workspace || !aligned(workspace, 16) || workspace_bytes < plan(d, true).total)
+  const Plan p = plan(d, true);
+  if (!workspace || !aligned(workspace, 16) || workspace_bytes < p.total)
     return SOMA_ERR_WORKSPACE;
   int* status = status_ptr();
   if (!status) return SOMA_ERR_CUDA;
@@ -1109,10 +1139,10 @@ int soma_linear_ce_backward(const void* h, const void* emb, soma_linear_ce_dims 
   trace_begin(SOMA_TRACE_HEAD, st);
   const cudaError_t e =
       d.dtype == SOMA_BF16
-          ? backward(static_cast<const __nv_bfloat16*>(h), static_cast<const __nv_bfloat16*>(emb),
+          ? backward(p, static_cast<const __nv_bfloat16*>(h), static_cast<const __nv_bfloat16*>(emb),
                      d, targets, ignore_index, lse, dloss, static_cast<__nv_bfloat16*>(dh),
                      dh_stride, static_cast<__nv_bfloat16*>(demb), demb_stride, ws, status, st)
-          : backward(static_cast<const __half*>(h), static_cast<const __half*>(emb), d, targets,
+          : backward(p, static_cast<const __half*>(h), static_cast<const __half*>(emb), d, targets,
                      ignore_index, lse, dloss, static_cast<__half*>(dh), dh_stride,
                      static_cast<__half*>(demb), demb_stride, ws, status, st);
   trace_end(SOMA_TRACE_HEAD, st);

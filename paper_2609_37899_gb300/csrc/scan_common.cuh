@@ -498,9 +498,11 @@ inline void put(const Shape& f, Scan* s) {
 
 template <typename K, typename... A>
 cudaError_t launch(K kernel, const Shape& f, size_t smem, cudaStream_t st, A... args) {
-  const cudaError_t e =
-      cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-  if (e != cudaSuccess) return e;
+  if (smem > (48 << 10)) {  // more than a kernel has unasked
+    const cudaError_t e =
+        cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e != cudaSuccess) return e;
+  }
   return launch_overlapped(kernel, dim3(f.grid), 32 * f.warps, smem, st, args...);
 }
 
