@@ -80,13 +80,14 @@ struct Work {
   const int64_t* targets;
   float2* partial;            // [M][2 splits]: maximum (powers of two), sum
   float* own;                 // [M] logit of the target
+  int32_t low;                // grad: rows to where G's second half goes, or 0
   // grad, dh
   RowInfo* info;
   const void* emb;            // dh: 16-byte aligned rows of emb
   int64_t emb_stride;
   int64_t v0;                 // first vocabulary entry of the piece
   const float* top;           // largest |dloss|
-  // demb, dh: where its rows are not 16-byte aligned, or null
+  // demb, dh: where its rows are not 16-byte aligned, or null; grad: G
   void* out;
   int64_t out_stride;
   // sums
@@ -231,6 +232,30 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
   w.t[0] = from_f32<T>(a);
   w.t[1] = from_f32<T>(b);
   return w.u;
+}
+
+// The first `cols` of 64 columns of a box's rows to memory that a tiled store
+// cannot address: a warp writes a row at a time, a 4-byte word per lane.  Where
+// a row starts between two words (odd), a lane's word is made of its own lower
+// half and its neighbour's upper one, and the row's ends go by themselves.
+template <typename T>
+__device__ __forceinline__ void store_box(T* out, int64_t stride, uint8_t* box, int rows, int cols,
+                                          int lane) {
+  uint16_t* q = reinterpret_cast<uint16_t*>(out) + 2 * lane;  // this lane's first column
+#pragma unroll 4
+  for (int r = 0; r < rows; ++r, q += stride) {
+    const uint32_t own =
+        *reinterpret_cast<const uint32_t*>(reinterpret_cast<uint8_t*>(box_piece(box, r, lane / 4)) +
+                                           (lane % 4) * 4);
+    const uint32_t before = __shfl_up_sync(0xffffffffu, own, 1);
+    const int odd = (int)(reinterpret_cast<uintptr_t>(q) >> 1) & 1;
+    const int first = 2 * lane - odd, last = cols - 1;
+    if (first >= 0 && first < last)
+      *reinterpret_cast<uint32_t*>(q - odd) = odd ? __funnelshift_r(before, own, 16) : own;
+    if (first < 0) q[0] = (uint16_t)own;
+    if (((cols ^ odd) & 1) && lane == last / 2)
+      q[last & 1] = (uint16_t)(last & 1 ? own >> 16 : own);
+  }
 }
 
 template <int KIND, typename T>
@@ -488,6 +513,21 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             }
           }
         }
+        if (KIND == kGrad && w.low) {
+          // few rows: what the rounding takes off each entry, for demb, right away
+          // (32 columns, 64 bytes a row, at a time)
+          if (live) {
+            T* q = static_cast<T*>(w.out) + (m + w.low) * w.out_stride + n;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              float rest[8];
+#pragma unroll
+              for (int k = 0; k < 8; ++k)
+                rest[k] = x[8 * j + k] - to_f32(from_f32<T>(x[8 * j + k]));
+              if (n + 8 * j < w.N) store8(q + 8 * j, rest);
+            }
+          }
+        }
         if (sums(KIND) || c % 64 == 0) {  // the last box has been read before this is written
           if (lane == 0) tc::bulk_wait_read();
           __syncwarp();
@@ -508,12 +548,12 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         }
         if (!sums(KIND) && c % 64 == 0 && n + 32 < n_end) continue;  // half a box so far
         const int bx = (int)(sums(KIND) ? n : n - c % 64);
-        if (!sums(KIND) && w.out) {
+        if (!sums(KIND) && KIND != kGrad && w.out) {
           __syncwarp();
-          for (int r = 0; r < 32 && m0 + r < w.M; ++r)
-            for (int j = lane; j < 64 && bx + j < w.N; j += 32)
-              static_cast<T*>(w.out)[(m0 + r) * w.out_stride + bx + j] =
-                  reinterpret_cast<const T*>(box_piece(box, r, j / 8))[j % 8];
+          const int rows = w.M - m0 < 32 ? (int)(w.M - m0) : 32;
+          const int cols = n_end - bx < 64 ? (int)(n_end - bx) : 64;
+          store_box(static_cast<T*>(w.out) + m0 * w.out_stride + bx, w.out_stride, box, rows, cols,
+                    lane);
           __syncwarp();
           continue;
         }
@@ -572,6 +612,7 @@ join_kernel(const float2* partial, int parts, const float* own, const T* h, int6
   if (has_target) {
     const T* a = h + n * hs;
     const T* b = emb + y * es;
+#pragma unroll 4
     for (int64_t j = lane * 8; j < dim; j += 256) {
       union {
         uint4 u;
@@ -586,6 +627,7 @@ join_kernel(const float2* partial, int parts, const float* own, const T* h, int6
     for (int k = 16; k; k >>= 1) logit += __shfl_xor_sync(0xffffffffu, logit, k);
   }
   float top = -INFINITY, sum = 0.f;
+#pragma unroll 4
   for (int j = lane; j < parts; j += 32) {
     const float2 p = partial[n * parts + j];
     const float now = fmaxf(top, p.x), ref = now == -INFINITY ? 0.f : now;
@@ -619,7 +661,8 @@ join_kernel(const float2* partial, int parts, const float* own, const T* h, int6
 template <typename T>
 __global__ void __launch_bounds__(256)
 rows_kernel(const T* h, soma_linear_ce_dims d, const int64_t* targets, int64_t ignore,
-            const float* lse, const float* dloss, RowInfo* info, T* copy, int64_t cs, float* top) {
+            const float* lse, const float* dloss, RowInfo* info, T* copy, int64_t cs, int halves,
+            float* top) {
   __shared__ int largest;
   if (threadIdx.x == 0) largest = 0;
   __syncthreads();
@@ -632,9 +675,12 @@ rows_kernel(const T* h, soma_linear_ce_dims d, const int64_t* targets, int64_t i
     const float l = lse[n];
     const bool live = y != ignore && y >= 0 && y < d.vocab && isfinite(l);
     const bool vec = d.h_stride % 8 == 0;
-    for (int64_t j = lane * 8; j < cs; j += 256)
-      *reinterpret_cast<uint4*>(copy + n * cs + j) =
+    for (int64_t j = lane * 8; j < cs; j += 256) {
+      const uint4 v =
           live ? row_piece(h + n * d.h_stride, j, d.dim, vec) : make_uint4(0u, 0u, 0u, 0u);
+      *reinterpret_cast<uint4*>(copy + n * cs + j) = v;
+      if (halves == 2) *reinterpret_cast<uint4*>(copy + (d.rows + n) * cs + j) = v;
+    }
     if (lane == 0) {
       RowInfo r = {l * kLog2e, 0.f, 0.f, -1};
       if (live) {
@@ -684,9 +730,11 @@ sums_kernel(const float* acc, int64_t acc_stride, int used, const __grid_constan
   RowInfo r = {0.f, 0.f, 0.f, 0};
   if (info) r = info[n];
   const T* e = static_cast<const T*>(w.emb) + (r.y < 0 ? 0 : r.y) * w.emb_stride;
-  for (int64_t j = threadIdx.x * 4; j < w.N; j += 512) {
+  const int64_t j = ((int64_t)blockIdx.y * 128 + threadIdx.x) * 4;
+  if (j < w.N) {
     float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
     if (r.y >= 0) {
+#pragma unroll 8
       for (int k = 0; k < used; ++k) {
         const float4 v = *reinterpret_cast<const float4*>(
             acc + ((int64_t)k * w.slot_rows + n) * acc_stride + j);
@@ -728,6 +776,13 @@ bool dims_ok(const soma_linear_ce_dims& d) {
 // the fp32 bytes that one unit reads or writes.
 constexpr int64_t kLaunchStages = 18;
 constexpr int64_t kBytesPerStage = 2700000;
+
+// With no more rows than this, the rounding of G to 16 bits does not average
+// out in demb (a row of it may be a single entry times a single state: its norm
+// was off by up to 1.6 times what rounding the result costs).  G is stored in
+// two halves then, what the rounding took off as further rows that meet h's
+// rows once more.  demb is bound by its own bytes at such sizes.
+constexpr int64_t kFewRows = 128;
 
 // Rows of the boxes of a K-major A of M rows.
 int box_rows(int64_t M) { return M <= kHalf - 8 ? (int)round8(M) : kHalf; }
@@ -791,6 +846,7 @@ struct Plan {
   int32_t splits, tile_n;        // forward
   int64_t piece;                 // backward: vocabulary entries of one piece
   bool dh_sums, demb_sums;       // which kernels the products take
+  int64_t halves;                // rows of G and of h's copy per row: 2 with G's second half
   int64_t g_stride, acc_stride, dh_slots, demb_slots;
   bool copy_h, copy_emb;
   size_t h, emb, partial, own;   // offsets; h, emb: copies
@@ -800,7 +856,7 @@ struct Plan {
 // The backward call's pieces: as few as G's share of the workspace allows, or
 // somewhat more where the tiles then fill the last round of pairs better.
 void plan_pieces(const soma_linear_ce_dims& d, Plan* p) {
-  int64_t most = (int64_t)(kPieceBytes / 2) / d.rows / kTile * kTile;
+  int64_t most = (int64_t)(kPieceBytes / 2) / (d.rows * p->halves) / kTile * kTile;
   if (most < kTile) most = kTile;
   const int64_t fewest = ceil_div(d.vocab, most);
   int64_t best = INT64_MAX;
@@ -817,10 +873,11 @@ void plan_pieces(const soma_linear_ce_dims& d, Plan* p) {
       const int64_t dh_by_sums =
           sums_cost(shares(d.rows, d.dim, w), !one) + (one ? kLaunchStages : 0);
       const int64_t dh_by_tiles = tiles_cost(d.rows, d.dim, w);
-      int64_t demb = tiles_cost(w, d.dim, d.rows);
+      int64_t demb = tiles_cost(w, d.dim, d.rows * p->halves);
       if (one) {
         dh_sums = dh_by_sums < dh_by_tiles;
-        const int64_t by_sums = sums_cost(shares(w, d.dim, d.rows), false) + kLaunchStages;
+        const int64_t by_sums =
+            sums_cost(shares(w, d.dim, d.rows * p->halves), false) + kLaunchStages;
         demb_sums = by_sums < demb;
         if (demb_sums) demb = by_sums;
       }
@@ -846,9 +903,10 @@ Plan plan(soma_linear_ce_dims d, bool backward) {
     return o;
   };
   if (!d.rows) d.rows = 1;
+  p.halves = backward && d.rows <= kFewRows ? 2 : 1;
   p.copy_h = backward || copied(d.h_stride, d.rows, false);
   p.copy_emb = copied(d.emb_stride, d.rows, backward);
-  if (p.copy_h) p.h = take((size_t)d.rows * round64(d.dim) * 2);
+  if (p.copy_h) p.h = take((size_t)d.rows * p.halves * round64(d.dim) * 2);
   if (p.copy_emb) p.emb = take((size_t)d.vocab * round64(d.dim) * 2);
   if (!backward) {
     // rounds of pairs times the tiles of a unit, least first
@@ -877,7 +935,7 @@ Plan plan(soma_linear_ce_dims d, bool backward) {
     plan_pieces(d, &p);
     p.g_stride = round8(p.piece);
     p.acc_stride = ceil_div(d.dim, 4) * 4;
-    p.g = take((size_t)d.rows * p.g_stride * 2);
+    p.g = take((size_t)d.rows * p.halves * p.g_stride * 2);
     p.info = take((size_t)d.rows * sizeof(RowInfo));
     if (p.dh_sums) {
       for (int64_t width : {p.piece, d.vocab % p.piece}) {
@@ -888,7 +946,7 @@ Plan plan(soma_linear_ce_dims d, bool backward) {
       p.dh_acc = take((size_t)p.dh_slots * ceil_div(d.rows, kTile) * kTile * p.acc_stride * 4);
     }
     if (p.demb_sums) {
-      p.demb_slots = slots_of(shares(d.vocab, d.dim, d.rows));
+      p.demb_slots = slots_of(shares(d.vocab, d.dim, d.rows * p.halves));
       p.demb_acc = take((size_t)p.demb_slots * ceil_div(d.vocab, kTile) * kTile * p.acc_stride * 4);
     }
     p.top = take(4);
@@ -988,7 +1046,8 @@ cudaError_t backward(const Plan& p, const T* h, const T* emb, const soma_linear_
                         (size_t)p.dh_slots * ceil_div(d.rows, kTile) * kTile * p.acc_stride * 4, st);
   if (e == cudaSuccess)
     e = launch_overlapped(rows_kernel<T>, (unsigned)ceil_div(d.rows, 8), 256, 0, st, h, d, targets,
-                          ignore, lse, dloss, info, copy, cs, dtype == SOMA_FP16 ? top : nullptr);
+                          ignore, lse, dloss, info, copy, cs, (int)p.halves,
+                          dtype == SOMA_FP16 ? top : nullptr);
   if (e != cudaSuccess) return e;
   if (p.copy_emb) emb = pack(emb, d.vocab, d.dim, &es, reinterpret_cast<T*>(ws + p.emb), st);
   if (!emb) return cudaErrorLaunchFailure;
@@ -997,7 +1056,7 @@ cudaError_t backward(const Plan& p, const T* h, const T* emb, const soma_linear_
   const bool demb_tiled = des % 8 == 0 && aligned(demb, 16);
   CUtensorMap h_k, h_mn, e_k, e_k_half, e_mn, dh_out, demb_sum;
   bool ok = make_tile_map(&h_k, copy, dtype, d.rows, d.dim, cs, box_rows(d.rows)) &&
-            make_tile_map(&h_mn, copy, dtype, d.rows, d.dim, cs, 64) &&
+            make_tile_map(&h_mn, copy, dtype, d.rows * p.halves, d.dim, cs, 64) &&
             make_tile_map(&e_k, emb, dtype, d.vocab, d.dim, es, kHalf) &&
             make_tile_map(&e_k_half, emb, dtype, d.vocab, d.dim, es, kHalf / 2) &&
             make_tile_map(&e_mn, emb, dtype, d.vocab, d.dim, es, 64);
@@ -1018,7 +1077,7 @@ cudaError_t backward(const Plan& p, const T* h, const T* emb, const soma_linear_
     const int64_t width = d.vocab - v0 < p.piece ? d.vocab - v0 : p.piece;
     CUtensorMap g_k, g_mn, g_out, demb_out = h_k;
     if (!make_tile_map(&g_k, G, dtype, d.rows, width, p.g_stride, box_rows(d.rows)) ||
-        !make_tile_map(&g_mn, G, dtype, d.rows, width, p.g_stride, 64) ||
+        !make_tile_map(&g_mn, G, dtype, d.rows * p.halves, width, p.g_stride, 64) ||
         !make_tile_map(&g_out, G, dtype, d.rows, width, p.g_stride, 32) ||
         (demb_tiled && !p.demb_sums &&
          !make_tile_map(&demb_out, demb + v0 * des, dtype, width, d.dim, des, 32)))
@@ -1038,7 +1097,11 @@ cudaError_t backward(const Plan& p, const T* h, const T* emb, const soma_linear_
     w.info = info;
     w.v0 = v0;
     w.top = top;
-    e = launch<kGrad, T>(h_k, w.tile_n == kTile ? e_k : e_k_half, g_out, w, (int64_t)w.m_tiles * w.n_tiles, status, st);
+    w.out = G;
+    w.out_stride = p.g_stride;
+    w.low = p.halves == 2 ? (int32_t)d.rows : 0;
+    e = launch<kGrad, T>(h_k, w.tile_n == kTile ? e_k : e_k_half, g_out, w,
+                         (int64_t)w.m_tiles * w.n_tiles, status, st);
     if (e != cudaSuccess) return e;
 
     w = shares(d.rows, d.dim, width);
@@ -1051,7 +1114,8 @@ cudaError_t backward(const Plan& p, const T* h, const T* emb, const soma_linear_
       w.add = many;
       e = launch<kDhSums, T>(g_k, e_mn, dh_out, w, 0, status, st);
       if (e == cudaSuccess && v0 + width == d.vocab)
-        e = launch_overlapped(sums_kernel<T>, (unsigned)d.rows, 128, 0, st, dh_acc, p.acc_stride,
+        e = launch_overlapped(sums_kernel<T>, dim3((unsigned)d.rows, (unsigned)ceil_div(d.dim, 512)),
+                              128, 0, st, dh_acc, p.acc_stride,
                               many ? (int)p.dh_slots : 0, w, info, dh, dhs,
                               dhs % 4 == 0 && aligned(dh, 8));
     } else {
@@ -1061,12 +1125,13 @@ cudaError_t backward(const Plan& p, const T* h, const T* emb, const soma_linear_
     }
     if (e != cudaSuccess) return e;
 
-    w = shares(width, d.dim, d.rows);
+    w = shares(width, d.dim, d.rows * p.halves);
     w.top = top;
     if (p.demb_sums) {
       e = launch<kDembSums, T>(g_mn, h_mn, demb_sum, w, 0, status, st);
       if (e == cudaSuccess)
-        e = launch_overlapped(sums_kernel<T>, (unsigned)d.vocab, 128, 0, st, demb_acc,
+        e = launch_overlapped(sums_kernel<T>, dim3((unsigned)d.vocab, (unsigned)ceil_div(d.dim, 512)),
+                              128, 0, st, demb_acc,
                               p.acc_stride, 0, w, nullptr, demb, des,
                               des % 4 == 0 && aligned(demb, 8));
     } else {
