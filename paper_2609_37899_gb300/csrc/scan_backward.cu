@@ -39,7 +39,9 @@ backward_kernel(const T* __restrict__ gates, const __grid_constant__ Scan s,
     const int64_t stop = n < end ? n : end;
     const int64_t at_ch = on ? ch : s.d.dim - 1;  // lanes past the last channel read along
     const int64_t rounds = (end - begin + rows - 1) / rows;
-    int64_t t0 = begin + (rounds - 1) * rows + warp * kSegment;
+    // maps: from the chunk's first round to its last
+    const int64_t step = MAPS ? rows : -rows;
+    int64_t t0 = begin + (MAPS ? 0 : rounds - 1) * rows + warp * kSegment;
     T next[kSegment][5];
     float next_mark;
     const auto fetch = [&](int64_t t) {
@@ -66,7 +68,7 @@ backward_kernel(const T* __restrict__ gates, const __grid_constant__ Scan s,
                       ? s.marks[(b * marks + t / kSegment) * s.d.dim + at_ch] : 0.f;
     };
     fetch(t0);
-    for (int64_t left = rounds; left > 0; --left, t0 -= rows) {
+    for (int64_t left = rounds; left > 0; --left, t0 += step) {
       float add[kSegment], f[kSegment], ki[kSegment], kf[kSegment], kg[kSegment], od[kSegment];
       float c = next_mark;
       const int live = stop - t0 >= kSegment ? kSegment : stop > t0 ? (int)(stop - t0) : 0;
@@ -90,7 +92,7 @@ backward_kernel(const T* __restrict__ gates, const __grid_constant__ Scan s,
         kg[j] = i * dg;
         od[j] = y * th * d_o;
       }
-      fetch(t0 - rows);
+      fetch(t0 + step);
       if (live < kSegment) {
 #pragma unroll
         for (int j = 0; j < kSegment; ++j)
@@ -173,7 +175,7 @@ backward_tiled_kernel(const __grid_constant__ Maps maps, const __grid_constant__
       if (lane == 0) tc::mbar_arrive_expect_tx(&ring.full[to], stage_elems * sizeof(T));
       __syncwarp();
       if (lane < 5) {
-        const int t = (int)(begin + round * rows);
+        const int t = (int)(begin + (MAPS ? rounds - 1 - round : round) * rows);
         box_g2s(stages + (size_t)to * stage_elems + lane * gate, &maps.in[lane], ch0,
                 maps.t_inner ? t : (int)b, maps.t_inner ? (int)b : t, &ring.full[to]);
       }
@@ -192,11 +194,13 @@ backward_tiled_kernel(const __grid_constant__ Maps maps, const __grid_constant__
         x = *reinterpret_cast<const float2*>(s.marks + (b * marks + t / kSegment) * s.d.dim + ch);
       return two(x.x, x.y);
     };
-    int64_t t0 = begin + (rounds - 1) * rows + warp * kSegment;
+    // maps: from the first round to the last
+    const int64_t step = MAPS ? rows : -rows;
+    int64_t t0 = begin + (MAPS ? 0 : rounds - 1) * rows + warp * kSegment;
     Two next_mark = mark_at(t0);
-    for (int64_t round = rounds - 1; round >= 0; --round, t0 -= rows) {
+    for (int64_t round = rounds - 1; round >= 0; --round, t0 += step) {
       const Two mark = next_mark;
-      next_mark = mark_at(t0 - rows);
+      next_mark = mark_at(t0 + step);
       ring_wait(ring, st, parity, status);
       T* p = stages + (size_t)st * stage_elems + warp * kSegment * kBlock + 2 * lane;
       // what each step adds to r, its f, and the factors that turn the gradient

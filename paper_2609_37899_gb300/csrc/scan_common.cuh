@@ -15,7 +15,9 @@
 // Where the channels alone do not occupy the GPU, the steps are cut into
 // chunks as well: one launch forms the chunks' maps (it reads what the maps
 // need and writes nothing else), and in the next each CTA applies the maps of
-// the chunks before its own to the state that enters and runs its chunk.
+// the chunks before its own to the state that enters and runs its chunk.  The
+// first of the two goes through a chunk the other way round: what it read last
+// is what the second wants first, and still in L2.
 //
 // Tiled kernels: a lane holds two channels in packed fp32 arithmetic, the gates
 // come as TMA boxes into a ring of shared-memory stages.  Plain kernels: one
@@ -266,8 +268,8 @@ __device__ __forceinline__ void join(Map<V>* shared, const Map<V>& mine, uint32_
   }
 }
 
-// The same for a CTA that forms its chunk's map: all of its warps' maps follow
-// `total`.
+// The same for a CTA that forms its chunk's map, from its end (REVERSE: from
+// its beginning) on: all of its warps' maps go before `total`.
 template <bool REVERSE, bool RAGGED, int WARPS, int V>
 __device__ __forceinline__ void join_total(Map<V>* shared, const Map<V>& mine, uint32_t turn,
                                            Map<V>& total) {
@@ -279,7 +281,9 @@ __device__ __forceinline__ void join_total(Map<V>* shared, const Map<V>& mine, u
 #pragma unroll
   for (int j = 0; j < WARPS; ++j) {
     if (j >= warps) break;
-    follow<RAGGED>(total, of_warp[(REVERSE ? warps - 1 - j : j) * 32]);
+    Map<V> m = of_warp[(REVERSE ? j : warps - 1 - j) * 32];
+    follow<RAGGED>(m, total);
+    total = m;
   }
 }
 

@@ -40,11 +40,13 @@ forward_kernel(const T* __restrict__ gates, const __grid_constant__ Scan s, T* _
 
     const int64_t begin = k * s.chunk, stop = n < end ? n : end;
     const int64_t at_ch = on ? ch : s.d.dim - 1;  // lanes past the last channel read along
-    int64_t t0 = begin + warp * kSegment;
+    // maps: from the chunk's last round to its first
+    const int64_t step = MAPS ? -rows : rows;
+    int64_t t0 = begin + warp * kSegment + (MAPS ? (end - begin - 1) / rows * rows : 0);
     T next[kSegment][kGates];
     const auto fetch = [&](int64_t t) {
       const T* p = gates + b * s.gs.b + t * s.gs.t + at_ch;
-      if (t + kSegment <= stop) {
+      if ((!MAPS || t >= begin) && t + kSegment <= stop) {
 #pragma unroll
         for (int j = 0; j < kSegment; ++j, p += s.gs.t)
 #pragma unroll
@@ -54,11 +56,12 @@ forward_kernel(const T* __restrict__ gates, const __grid_constant__ Scan s, T* _
         for (int j = 0; j < kSegment; ++j)
 #pragma unroll
           for (int g = 0; g < kGates; ++g)
-            next[j][g] = t + j < stop ? p[j * s.gs.t + g * s.gs.g] : from_f32<T>(0.f);
+            next[j][g] = (!MAPS || t >= begin) && t + j < stop ? p[j * s.gs.t + g * s.gs.g]
+                                                               : from_f32<T>(0.f);
       }
     };
     fetch(t0);
-    for (int64_t start = begin; start < end; start += rows, t0 += rows) {
+    for (int64_t start = begin; start < end; start += rows, t0 += step) {
       float f[kSegment], u[kSegment];
       T o[kSegment];
       Map<1> m = identity<1>();
@@ -71,7 +74,7 @@ forward_kernel(const T* __restrict__ gates, const __grid_constant__ Scan s, T* _
         u[j] = num * rcp(den * one_exp(to_f32(next[j][0])));
         f[j] = rcp(one_exp(to_f32(next[j][1])));
       }
-      fetch(t0 + rows);
+      fetch(t0 + step);
       if (RAGGED && s.resets) {
 #pragma unroll
         for (int j = 0; j < kSegment; ++j)
@@ -152,7 +155,7 @@ forward_tiled_kernel(const __grid_constant__ Maps maps, const __grid_constant__ 
       if (lane == 0) tc::mbar_arrive_expect_tx(&ring.full[to], stage_elems * sizeof(T));
       __syncwarp();
       if (lane < kGates) {
-        const int t = (int)(begin + round * rows);
+        const int t = (int)(begin + (MAPS ? rounds - 1 - round : round) * rows);
         box_g2s(stages + (size_t)to * stage_elems + lane * gate, &maps.in[lane], ch0,
                 maps.t_inner ? t : (int)b, maps.t_inner ? (int)b : t, &ring.full[to]);
       }
@@ -164,8 +167,9 @@ forward_tiled_kernel(const __grid_constant__ Maps maps, const __grid_constant__ 
     Map<2> total = identity<2>();
     if (!MAPS) over_chunks<false, RAGGED, kWarps>(s, b, ch, on, 0, k, shared, turn++, c);
 
-    int64_t t0 = begin + warp * kSegment;
-    for (int64_t round = 0; round < rounds; ++round, t0 += rows) {
+    // maps: from the last round to the first
+    int64_t t0 = begin + warp * kSegment + (MAPS ? (rounds - 1) * rows : 0);
+    for (int64_t round = 0; round < rounds; ++round, t0 += MAPS ? -rows : rows) {
       ring_wait(ring, st, parity, status);
       const T* p = stages + (size_t)st * stage_elems + warp * kSegment * kBlock + 2 * lane;
       Two f[kSegment], u[kSegment];
