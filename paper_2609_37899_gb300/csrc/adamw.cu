@@ -13,8 +13,6 @@
 #include <cmath>
 #include <cuda_fp8.h>
 
-#define SOMA_CHECK_FILE 8
-#include "checked.cuh"
 #include "numeric.cuh"
 #include "soma_api.h"
 #include "soma_launch.h"

@@ -16,8 +16,6 @@
 #include <atomic>
 #include <cmath>
 
-#define SOMA_CHECK_FILE 10
-#include "checked.cuh"
 #include "numeric.cuh"
 #include "pdl.cuh"
 #include "soma_api.h"

@@ -3,7 +3,6 @@
 //
 // Per element of 16 bits 10 bytes read, 8 written and half a byte of the
 // checkpoints.
-#define SOMA_CHECK_FILE 11
 #include "scan_common.cuh"
 
 namespace soma {

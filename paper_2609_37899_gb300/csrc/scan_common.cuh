@@ -29,7 +29,6 @@
 #include <cstring>
 #include <type_traits>
 
-#include "checked.cuh"
 #include "numeric.cuh"
 #include "pdl.cuh"
 #include "soma_api.h"

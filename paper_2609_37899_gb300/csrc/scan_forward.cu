@@ -5,7 +5,6 @@
 // and half a byte for the checkpoints.  The instructions come close: 113 per
 // element (one channel at a time, a 64-bit address and a bounds check per
 // load) took 2.7 times the bytes' time.
-#define SOMA_CHECK_FILE 9
 #include "scan_common.cuh"
 
 namespace soma {

@@ -20,7 +20,6 @@
 namespace soma {
 namespace tc {
 
-constexpr int kBoxCols = 64;                // 16-bit elements of one swizzled row
 constexpr int kDepth = 64;                  // depth of one stage
 constexpr uint32_t kBoxBytes = 64 * 128;    // an MN-major box
 
