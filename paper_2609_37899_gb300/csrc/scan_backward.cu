@@ -10,8 +10,9 @@ namespace scan {
 
 namespace {
 
-constexpr int kWarps = 2;     // of a CTA
-constexpr int kResident = 6;  // such CTAs fit an SM
+constexpr int kWarps = 4;     // of a CTA, at most
+constexpr int kResident = 3;  // such CTAs fit an SM
+constexpr double kJoin = 0.2; // steps that joining a chunk's map is worth
 
 template <typename T, bool RAGGED, bool MAPS>
 __global__ void __launch_bounds__(32 * kWarps, kResident)
@@ -303,10 +304,18 @@ backward_tiled_kernel(const __grid_constant__ Maps maps, const __grid_constant__
 
 // ------------------------------------------------------------------- host --
 
-Shape tiled_shape(const soma_scan_dims& d, size_t width) {
-  return shape(d, 2, kWarps, width == 4 ? 5 : kResident);  // fp32: as many as shared memory holds
+// CTAs of two warps, or of four and half as many: the larger ones take fewer
+// chunks (1 x 32768 x 960: 183 us with two warps, 167 with four) and keep an SM
+// full where two-warp ones are too few to (32 x 2048 x 1376: 348 and 325);
+// elsewhere the smaller ones spread better (4 x 4096 x 960: 89 and 98).
+Shape shape_of(const soma_scan_dims& d, int V, int fit) {
+  const Shape a = shape(d, V, kWarps / 2, fit, kJoin), b = shape(d, V, kWarps, fit / 2, kJoin);
+  return b.cost < 0.98 * a.cost ? b : a;
 }
-Shape plain_shape(const soma_scan_dims& d) { return shape(d, 1, kWarps, kResident); }
+Shape tiled_shape(const soma_scan_dims& d, size_t width) {
+  return shape_of(d, 2, width == 4 ? 5 : 2 * kResident);  // fp32: as many as shared memory holds
+}
+Shape plain_shape(const soma_scan_dims& d) { return shape_of(d, 1, 2 * kResident); }
 
 template <typename T>
 cudaError_t backward(const void* gates, Scan s, const void* dh, const float* dc_last,

@@ -442,42 +442,45 @@ struct Shape {
   int warps;                     // of a CTA
   int64_t blocks, chunks, chunk; // of the channels, of the steps; steps of a chunk
   unsigned grid;
+  double cost;                   // estimated time, relative to other cuts of the same call
 };
 
 // CTAs of up to `most` warps, `fit` of which an SM holds, each over V * 32
 // channels.  The time is that of the SM with the most of them, longer where
 // their warps do not fill it; with chunks, half as much again for the launch
-// that forms the maps (it reads 6 bytes of 10 forward, 10 of 18 backward).
+// that forms the maps (it reads 6 bytes of 10 forward, 10 of 18 backward), and
+// what it takes to join them: as long as `join` steps for each of the chunks.
 // The alternative for 1 x 32768 x 960 (15 blocks), clusters of eight CTAs that
 // joined over distributed shared memory every round, took 170 us forward and
 // 350 us backward.
 // No CTA of the next launch is admitted before the end of the present ones:
 // early ones would sit where there is room and leave the rest badly spread.
-inline Shape shape(const soma_scan_dims& d, int V, int most, int fit) {
+inline Shape shape(const soma_scan_dims& d, int V, int most, int fit, double join) {
   Shape f;
   f.blocks = (d.dim + 32 * V - 1) / (32 * V);
   f.warps = 1;
   while (f.warps < most && f.warps * kSegment < d.steps) f.warps *= 2;
   const int64_t items = d.batch * f.blocks, rows = f.warps * kSegment;
   const int64_t slots = (int64_t)kSms * fit;
-  const auto cost = [&](int64_t chunks) {
+  const auto cost = [&](int64_t chunks, int64_t chunk) {
     const double n = (double)items * chunks;
     const double waves = n > slots ? std::ceil(n / slots) * slots / n
                                    : std::ceil(n / kSms) * kSms / n;
     const double held = (n < slots ? n : slots) * f.warps / kSms;
     const double enough = fit * f.warps < 16 ? fit * f.warps : 16;
-    return waves * (held < enough ? enough / held : 1) * (chunks > 1 ? 1.5 : 1);
+    return waves * (held < enough ? enough / held : 1) *
+           (chunks > 1 ? 1.5 + join * (double)chunks / (double)chunk : 1);
   };
   f.chunks = 1;
   f.chunk = d.steps > 0 ? d.steps : 1;
-  double least = cost(1);
+  f.cost = cost(1, f.chunk);
   // two rounds a chunk at least, and no more chunks than are quickly joined
   for (int64_t n = 2; n <= 256 && n * 2 * rows <= d.steps && items * n <= 2 * slots; ++n) {
     const int64_t chunk = (d.steps + n * rows - 1) / (n * rows) * rows;
     const int64_t chunks = (d.steps + chunk - 1) / chunk;
-    const double c = cost(chunks) * (double)(chunk * chunks) / (double)d.steps;
-    if (c < least * 0.98) {
-      least = c;
+    const double c = cost(chunks, chunk) * (double)(chunk * chunks) / (double)d.steps;
+    if (c < f.cost * 0.98) {
+      f.cost = c;
       f.chunks = chunks;
       f.chunk = chunk;
     }
