@@ -90,7 +90,8 @@ struct Work {
   const void* emb;            // dh: 16-byte aligned rows of emb
   int64_t emb_stride;
   int64_t v0;                 // first vocabulary entry of the piece
-  const float* top;           // largest |dloss|
+  float* top;                 // largest |dloss|; after it those of rows_kernel's blocks (fp16)
+  int32_t tops;               // grad: how many
   // demb, dh: where its rows are not 16-byte aligned, or null; grad: G
   void* out;
   int64_t out_stride;
@@ -396,7 +397,15 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     int64_t y = -1;
     RowInfo info = {0.f, 0.f, 0.f, -1};
     float scale = 1.f;
-    if (KIND == kGrad) scale = g_scale<T>(*w.top);
+    if (KIND == kGrad && std::is_same<T, __half>::value) {
+      int largest = 0;  // non-negative floats order as their bits do
+#pragma unroll 8
+      for (int j = lane; j < w.tops; j += 32)
+        largest = max(largest, __float_as_int(w.top[1 + j]));
+      const float g = __int_as_float(__reduce_max_sync(0xffffffffu, largest));
+      scale = g_scale<T>(g);
+      if (blockIdx.x == 0 && warp == 4 && lane == 0) *w.top = g;  // for the kernels that follow
+    }
     if (KIND == kDemb || KIND == kDh) scale = 1.f / g_scale<T>(*w.top);
     while (walk.next(s, pair)) {
       const int64_t m0 = (int64_t)s.m * kTile + m_in, m = m0 + lane;
@@ -672,9 +681,8 @@ rows_kernel(const T* h, soma_linear_ce_dims d, const int64_t* targets, int64_t i
   __syncthreads();
   admit_successor();
   after_predecessor();
-  const int64_t n = (int64_t)blockIdx.x * 8 + threadIdx.x / 32;
   const int lane = threadIdx.x % 32;
-  if (n < d.rows) {
+  for (int64_t n = (int64_t)blockIdx.x * 8 + threadIdx.x / 32; n < d.rows; n += 8 * gridDim.x) {
     const int64_t y = targets[n];
     const float l = lse[n];
     const bool live = y != ignore && y >= 0 && y < d.vocab && isfinite(l);
@@ -698,9 +706,7 @@ rows_kernel(const T* h, soma_linear_ce_dims d, const int64_t* targets, int64_t i
   }
   if (!top) return;
   __syncthreads();
-  // one atomic per block, and none where it would change nothing
-  if (threadIdx.x == 0 && largest > *reinterpret_cast<volatile int*>(top))
-    atomicMax(reinterpret_cast<int*>(top), largest);
+  if (threadIdx.x == 0) top[1 + blockIdx.x] = __int_as_float(largest);
 }
 
 // A matrix copied to rows of cs elements, zeros after the first dim; eight
@@ -846,6 +852,14 @@ bool copied(int64_t stride, int64_t rows, bool backward) {
   return stride % 8 != 0 || (stride % 16 != 0 && rows >= (backward ? 700 : 2000));
 }
 
+// Blocks of rows_kernel.  In fp16 each leaves its largest |dloss|, and every
+// epilogue warp of grad reads them all while its first products run.
+constexpr int64_t kMostTops = 1024;
+unsigned row_blocks(const soma_linear_ce_dims& d) {
+  const int64_t n = ceil_div(d.rows, 8);
+  return (unsigned)(d.dtype == SOMA_FP16 && n > kMostTops ? kMostTops : n);
+}
+
 struct Plan {
   int32_t splits, tile_n;        // forward
   int64_t piece;                 // backward: vocabulary entries of one piece
@@ -953,7 +967,7 @@ Plan plan(soma_linear_ce_dims d, bool backward) {
       p.demb_slots = slots_of(shares(d.vocab, d.dim, d.rows * p.halves));
       p.demb_acc = take((size_t)p.demb_slots * ceil_div(d.vocab, kTile) * kTile * p.acc_stride * 4);
     }
-    p.top = take(4);
+    p.top = take((1 + kMostTops) * 4);
   }
   p.total = at;
   return p;
@@ -1044,13 +1058,12 @@ cudaError_t backward(const Plan& p, const T* h, const T* emb, const soma_linear_
   const int64_t cs = round64(d.dim);
   int64_t es = d.emb_stride;
   cudaError_t e = cudaSuccess;
-  if (dtype == SOMA_FP16) e = cudaMemsetAsync(top, 0, 4, st);
   if (p.dh_sums && p.piece < d.vocab && e == cudaSuccess)
     e = cudaMemsetAsync(dh_acc, 0,
                         (size_t)p.dh_slots * ceil_div(d.rows, kTile) * kTile * p.acc_stride * 4, st);
   if (e == cudaSuccess)
-    e = launch_overlapped(rows_kernel<T>, (unsigned)ceil_div(d.rows, 8), 256, 0, st, h, d, targets,
-                          ignore, lse, dloss, info, copy, cs, (int)p.halves,
+    e = launch_overlapped(rows_kernel<T>, row_blocks(d), 256, 0, st, h, d, targets, ignore, lse,
+                          dloss, info, copy, cs, (int)p.halves,
                           dtype == SOMA_FP16 ? top : nullptr);
   if (e != cudaSuccess) return e;
   if (p.copy_emb) emb = pack(emb, d.vocab, d.dim, &es, reinterpret_cast<T*>(ws + p.emb), st);
@@ -1103,6 +1116,7 @@ cudaError_t backward(const Plan& p, const T* h, const T* emb, const soma_linear_
     w.top = top;
     w.out = G;
     w.out_stride = p.g_stride;
+    w.tops = (int32_t)row_blocks(d);
     w.low = p.halves == 2 ? (int32_t)d.rows : 0;
     e = launch<kGrad, T>(h_k, w.tile_n == kTile ? e_k : e_k_half, g_out, w,
                          (int64_t)w.m_tiles * w.n_tiles, status, st);
