@@ -540,8 +540,8 @@ int soma_scan_step(const void* gates, soma_scan_strides gate_strides, int dtype,
  * (demb with dloss = 1/(BT) is the decoder-path rule of the paper's seed run,
  * Eq. delta).  h, emb and their gradients are of one 16-bit soma_dtype;
  * products accumulate in fp32, losses are fp32.  G is rounded to the 16-bit
- * type before it meets emb and h (fp16: scaled by a power of two so that the
- * largest |dloss| lies in [2^13, 2^14)).
+ * type before it meets emb and h, scaled so that the largest |dloss| is 1
+ * (fp16: 2^14).
  *
  * A row whose target is ignore_index has loss 0, lse 0 and no gradient; its h
  * is never used, whatever it holds.  A row with a target outside 0 .. vocab - 1

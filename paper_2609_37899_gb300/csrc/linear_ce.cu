@@ -18,7 +18,7 @@
 // TFLOP/s, the rate that the power limit lets a long run keep), 8192 x 131072 x
 // 1024 forward and backward 5.5 ms (1600).  emb's bytes bound few rows (64 x
 // 32768 x 960 forward: 21 us, 3 TB/s), the launches small sizes (8192 x 256 x
-// 960 forward and backward: 72 us).
+// 960 forward and backward: 68 us).
 #include <atomic>
 #include <cmath>
 
@@ -90,7 +90,7 @@ struct Work {
   const void* emb;            // dh: 16-byte aligned rows of emb
   int64_t emb_stride;
   int64_t v0;                 // first vocabulary entry of the piece
-  float* top;                 // largest |dloss|; after it those of rows_kernel's blocks (fp16)
+  float* top;                 // largest |dloss|; after it those of rows_kernel's blocks
   int32_t tops;               // grad: how many
   // demb, dh: where its rows are not 16-byte aligned, or null; grad: G
   void* out;
@@ -182,14 +182,15 @@ struct Walk {
   }
 };
 
-// The power of two that the 16-bit G is scaled by.
+// What the 16-bit G is scaled by: the largest |dloss| becomes 1, or 2^14 in fp16.
+// Most calls have one dloss for all rows; -dloss (1 - p) is then next to a power
+// of two and exact for small p.  Without the scaling those entries were all off
+// by the same up to 2^-8 of themselves in bf16, and demb with them (1.5 times
+// the error that its own rounding has).
 template <typename T>
-__device__ __forceinline__ float g_scale(float) { return 1.f; }
-template <>
-__device__ __forceinline__ float g_scale<__half>(float top) {
-  int e = 0;
-  frexpf(top, &e);  // top in [2^(e-1), 2^e)
-  return top > 0.f ? exp2f((float)(14 - e)) : 1.f;
+__device__ __forceinline__ float g_scale(float top) {
+  const float to = std::is_same<T, __half>::value ? 16384.f : 1.f;
+  return to / fminf(fmaxf(top, 0x1p-100f), 0x1p126f);
 }
 
 struct Shared {
@@ -397,7 +398,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     int64_t y = -1;
     RowInfo info = {0.f, 0.f, 0.f, -1};
     float scale = 1.f;
-    if (KIND == kGrad && std::is_same<T, __half>::value) {
+    if (KIND == kGrad) {
       int largest = 0;  // non-negative floats order as their bits do
 #pragma unroll 8
       for (int j = lane; j < w.tops; j += 32)
@@ -699,12 +700,11 @@ rows_kernel(const T* h, soma_linear_ce_dims d, const int64_t* targets, int64_t i
         r.g = dloss[n];
         r.y = (int32_t)y;
         // non-negative floats order as their bits do
-        if (top && isfinite(r.g)) atomicMax(&largest, __float_as_int(fabsf(r.g)));
+        if (isfinite(r.g)) atomicMax(&largest, __float_as_int(fabsf(r.g)));
       }
       info[n] = r;
     }
   }
-  if (!top) return;
   __syncthreads();
   if (threadIdx.x == 0) top[1 + blockIdx.x] = __int_as_float(largest);
 }
@@ -852,12 +852,12 @@ bool copied(int64_t stride, int64_t rows, bool backward) {
   return stride % 8 != 0 || (stride % 16 != 0 && rows >= (backward ? 700 : 2000));
 }
 
-// Blocks of rows_kernel.  In fp16 each leaves its largest |dloss|, and every
-// epilogue warp of grad reads them all while its first products run.
+// Blocks of rows_kernel.  Each leaves its largest |dloss|, and every epilogue
+// warp of grad reads them all while its first products run.
 constexpr int64_t kMostTops = 1024;
 unsigned row_blocks(const soma_linear_ce_dims& d) {
   const int64_t n = ceil_div(d.rows, 8);
-  return (unsigned)(d.dtype == SOMA_FP16 && n > kMostTops ? kMostTops : n);
+  return (unsigned)(n < kMostTops ? n : kMostTops);
 }
 
 struct Plan {
@@ -1063,8 +1063,7 @@ cudaError_t backward(const Plan& p, const T* h, const T* emb, const soma_linear_
                         (size_t)p.dh_slots * ceil_div(d.rows, kTile) * kTile * p.acc_stride * 4, st);
   if (e == cudaSuccess)
     e = launch_overlapped(rows_kernel<T>, row_blocks(d), 256, 0, st, h, d, targets, ignore, lse,
-                          dloss, info, copy, cs, (int)p.halves,
-                          dtype == SOMA_FP16 ? top : nullptr);
+                          dloss, info, copy, cs, (int)p.halves, top);
   if (e != cudaSuccess) return e;
   if (p.copy_emb) emb = pack(emb, d.vocab, d.dim, &es, reinterpret_cast<T*>(ws + p.emb), st);
   if (!emb) return cudaErrorLaunchFailure;

@@ -34,3 +34,20 @@ def test_several_pieces():
     """So large a vocabulary that both halves of G take several pieces."""
     s = _case(100, 700001, 24, "bf16", seed=4, ignored=0.1)
     _check(s, _run(s))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("N,V,d", [(200, 20000, 64), (625, 30000, 72), (1000, 20000, 65)])
+def test_one_gradient_for_all_rows(N, V, d, dtype):
+    """With one dloss for all rows, G's entries at the targets are just below a power of two and
+    off by at most half of what rounding can cost, evenly: hu / 2 / sqrt(3) = 0.29 hu.  demb's own
+    rounding is off by hu / sqrt(3) times 0.72, the mean over the values' mantissas: 0.42 hu.
+    Together 1.22 times the latter (for entries all off by the same up to hu: 2.6); 1.4 is allowed."""
+    s = _case(N, V, d, dtype, seed=N, spread=0.5)
+    s["dloss"] = torch.full_like(s["dloss"], 1 / 3)
+    got = _run(s)
+    _check(s, got)
+    want = _reference(s)[0]["demb"]
+    rounding = (want.to(got["demb"].dtype).double() - want).norm().item()
+    off = (got["demb"].double() - want).norm().item()
+    assert off <= 1.4 * rounding + 1e-5 * want.norm().item()
