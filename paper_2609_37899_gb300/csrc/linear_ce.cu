@@ -616,6 +616,14 @@ join_kernel(const float2* partial, int parts, const float* own, const T* h, int6
   const int64_t n = (int64_t)blockIdx.x * 8 + threadIdx.x / 32;
   if (n >= rows) return;
   const int lane = threadIdx.x % 32;
+  // what does not depend on the target is on its way before it is known
+  constexpr int kAhead = 4;
+  float2 ahead[kAhead];
+#pragma unroll
+  for (int i = 0; i < kAhead; ++i)
+    ahead[i] = lane + 32 * i < parts ? partial[n * parts + lane + 32 * i]
+                                     : make_float2(-INFINITY, 0.f);
+  const float was = own[n];
   const int64_t y = targets[n];
   if (y == ignore) {
     if (lane == 0) loss[n] = lse[n] = 0.f;
@@ -626,23 +634,38 @@ join_kernel(const float2* partial, int parts, const float* own, const T* h, int6
   if (has_target) {
     const T* a = h + n * hs;
     const T* b = emb + y * es;
-#pragma unroll 4
-    for (int64_t j = lane * 8; j < dim; j += 256) {
+    const int64_t whole = dim / 8 * 8;
+    for (int64_t j0 = lane * 8; j0 < whole; j0 += 1024) {
       union {
         uint4 u;
         T t[8];
-      } p, q;
-      p.u = row_piece(a, j, dim, true);
-      q.u = row_piece(b, j, dim, true);
+      } p[4], q[4];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) logit = fmaf(to_f32(p.t[k]), to_f32(q.t[k]), logit);
+      for (int i = 0; i < 4; ++i) {
+        const bool there = j0 + 256 * i < whole;
+        p[i].u = q[i].u = make_uint4(0u, 0u, 0u, 0u);
+        if (there) p[i].u = *reinterpret_cast<const uint4*>(a + j0 + 256 * i);
+        if (there) q[i].u = *reinterpret_cast<const uint4*>(b + j0 + 256 * i);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) logit = fmaf(to_f32(p[i].t[k]), to_f32(q[i].t[k]), logit);
     }
+    if (whole + lane < dim) logit = fmaf(to_f32(a[whole + lane]), to_f32(b[whole + lane]), logit);
 #pragma unroll
     for (int k = 16; k; k >>= 1) logit += __shfl_xor_sync(0xffffffffu, logit, k);
   }
-  float top = -INFINITY, sum = 0.f;
+  float top = ahead[0].x, sum = 0.f;
+#pragma unroll
+  for (int i = 1; i < kAhead; ++i) top = fmaxf(top, ahead[i].x);
+  {
+    const float ref = top == -INFINITY ? 0.f : top;
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) sum = fmaf(ahead[i].y, tc::ex2(ahead[i].x - ref), sum);
+  }
 #pragma unroll 4
-  for (int j = lane; j < parts; j += 32) {
+  for (int j = lane + 32 * kAhead; j < parts; j += 32) {
     const float2 p = partial[n * parts + j];
     const float now = fmaxf(top, p.x), ref = now == -INFINITY ? 0.f : now;
     sum = sum * tc::ex2(top - ref) + p.y * tc::ex2(p.x - ref);
@@ -659,7 +682,7 @@ join_kernel(const float2* partial, int parts, const float* own, const T* h, int6
   if (lane) return;
   if (has_target) {
     const float instead =
-        tc::ex2(fmaf(logit, kLog2e, -top)) - tc::ex2(fmaf(own[n], kLog2e, -top));
+        tc::ex2(fmaf(logit, kLog2e, -top)) - tc::ex2(fmaf(was, kLog2e, -top));
     sum += instead;
   }
   const float hi = top * kLn2, lo = fmaf(top, kLn2, -hi) + logf(sum);
