@@ -54,6 +54,12 @@ enum Kind { kStats, kGrad, kDemb, kDh, kDembSums, kDhSums };
 __host__ __device__ constexpr bool a_mn(int kind) { return kind == kDemb || kind == kDembSums; }
 __host__ __device__ constexpr bool b_mn(int kind) { return kind >= kDemb; }
 __host__ __device__ constexpr bool sums(int kind) { return kind >= kDembSums; }
+// demb's product reads nothing of dh's, which is launched right before it: it
+// starts on the SMs that dh's last tiles leave and waits for dh's end at its own.
+// What both read is complete by then, as dh's kernels admit their successor
+// after their own wait (8192 x 256 x 960: dh's 128 tiles on 76 pairs).
+__host__ __device__ constexpr bool is_demb(int kind) { return kind == kDemb || kind == kDembSums; }
+__host__ __device__ constexpr bool before_demb(int kind) { return kind == kDh || kind == kDhSums; }
 
 // What a row of the backward call takes part with; y = -1: no part.  The
 // entry of G at the target is by far the row's largest, and its rounding to 16
@@ -292,13 +298,14 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     tc::prefetch_map(&map_b);
     if (KIND != kStats) tc::prefetch_map(&map_out);
   }
-  admit_successor();
+  if (!before_demb(KIND)) admit_successor();
   if (warp == 2) tc::tmem_alloc_pair(&sh.tmem, 512);
   tc::tc_fence_before();
   __syncthreads();
   tc::cluster_sync();
   tc::tc_fence_after();
-  after_predecessor();
+  if (!is_demb(KIND)) after_predecessor();
+  if (before_demb(KIND)) admit_successor();
   const uint32_t tmem = sh.tmem;
 
   Walk<KIND> walk(w, pair);
@@ -407,7 +414,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
       scale = g_scale<T>(g);
       if (blockIdx.x == 0 && warp == 4 && lane == 0) *w.top = g;  // for the kernels that follow
     }
-    if (KIND == kDemb || KIND == kDh) scale = 1.f / g_scale<T>(*w.top);
+    if (KIND == kDemb || KIND == kDh) scale = 1.f / g_scale<T>(__ldcg(w.top));
     while (walk.next(s, pair)) {
       const int64_t m0 = (int64_t)s.m * kTile + m_in, m = m0 + lane;
       const bool live = m < w.M;
@@ -590,6 +597,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     if (KIND != kStats && lane == 0) tc::bulk_wait();
   }
   __syncwarp();
+  if (is_demb(KIND)) after_predecessor();
   tc::tc_fence_before();
   __syncthreads();
   tc::cluster_sync();  // no CTA leaves while its pair may still signal or read it
@@ -751,8 +759,8 @@ template <typename T>
 __global__ void __launch_bounds__(128)
 sums_kernel(const float* acc, int64_t acc_stride, int used, const __grid_constant__ Work w,
             const RowInfo* info, T* out, int64_t stride, int vec) {
-  admit_successor();
   after_predecessor();
+  admit_successor();  // only now: the product of demb may follow
   const int64_t n = blockIdx.x;
   const float f = 1.f / g_scale<T>(*w.top);
   if (!used) {
