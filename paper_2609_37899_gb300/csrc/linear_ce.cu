@@ -16,9 +16,10 @@
 //
 // The tensor cores bound large sizes: 16385 x 32768 x 1376 forward 860 us (1720
 // TFLOP/s, the rate that the power limit lets a long run keep), 8192 x 131072 x
-// 1024 forward and backward 5.5 ms (1600).  emb's bytes bound few rows (64 x
-// 32768 x 960 forward: 21 us, 3 TB/s), the launches small sizes (8192 x 256 x
-// 960 forward and backward: 68 us).
+// 1024 forward and backward 5.5 ms (1600); the tensor pipe is 91% busy in stats
+// and 77 to 80% in the others at 4096 x 65536 x 1024.  emb's bytes bound few
+// rows (64 x 32768 x 960 forward: 18 us, 3.4 TB/s), the launches small sizes
+// (8192 x 256 x 960 forward and backward: 64 us).
 #include <atomic>
 #include <cmath>
 
@@ -59,7 +60,10 @@ __host__ __device__ constexpr bool sums(int kind) { return kind >= kDembSums; }
 // What both read is complete by then, as dh's kernels admit their successor
 // after their own wait (8192 x 256 x 960: dh's 128 tiles on 76 pairs).
 __host__ __device__ constexpr bool is_demb(int kind) { return kind == kDemb || kind == kDembSums; }
-__host__ __device__ constexpr bool before_demb(int kind) { return kind == kDh || kind == kDhSums; }
+// The successors of these rely on all that came before.
+__host__ __device__ constexpr bool admits_late(int kind) {
+  return kind == kDh || kind == kDhSums || kind == kStats;
+}
 
 // What a row of the backward call takes part with; y = -1: no part.  The
 // entry of G at the target is by far the row's largest, and its rounding to 16
@@ -298,14 +302,14 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     tc::prefetch_map(&map_b);
     if (KIND != kStats) tc::prefetch_map(&map_out);
   }
-  if (!before_demb(KIND)) admit_successor();
+  if (!admits_late(KIND)) admit_successor();
   if (warp == 2) tc::tmem_alloc_pair(&sh.tmem, 512);
   tc::tc_fence_before();
   __syncthreads();
   tc::cluster_sync();
   tc::tc_fence_after();
   if (!is_demb(KIND)) after_predecessor();
-  if (before_demb(KIND)) admit_successor();
+  if (admits_late(KIND)) admit_successor();
   const uint32_t tmem = sh.tmem;
 
   Walk<KIND> walk(w, pair);
@@ -620,24 +624,14 @@ join_kernel(const float2* partial, int parts, const float* own, const T* h, int6
             const T* emb, int64_t es, const int64_t* targets, int64_t ignore, int64_t rows,
             int64_t vocab, int64_t dim, float* loss, float* lse, int* status) {
   admit_successor();
-  after_predecessor();
   const int64_t n = (int64_t)blockIdx.x * 8 + threadIdx.x / 32;
   if (n >= rows) return;
   const int lane = threadIdx.x % 32;
-  // what does not depend on the target is on its way before it is known
-  constexpr int kAhead = 4;
-  float2 ahead[kAhead];
-#pragma unroll
-  for (int i = 0; i < kAhead; ++i)
-    ahead[i] = lane + 32 * i < parts ? partial[n * parts + lane + 32 * i]
-                                     : make_float2(-INFINITY, 0.f);
-  const float was = own[n];
-  const int64_t y = targets[n];
-  if (y == ignore) {
-    if (lane == 0) loss[n] = lse[n] = 0.f;
-    return;
-  }
-  const bool has_target = y >= 0 && y < vocab;
+  // the call's inputs are there since before stats: it admits this kernel after
+  // its own wait, and CTAs that find room next to it compute this meanwhile
+  // (from L2, where what earlier kernels wrote is)
+  const int64_t y = __ldcg(reinterpret_cast<const long long*>(targets) + n);
+  const bool has_target = y != ignore && y >= 0 && y < vocab;
   float logit = 0.f;
   if (has_target) {
     const T* a = h + n * hs;
@@ -652,18 +646,31 @@ join_kernel(const float2* partial, int parts, const float* own, const T* h, int6
       for (int i = 0; i < 4; ++i) {
         const bool there = j0 + 256 * i < whole;
         p[i].u = q[i].u = make_uint4(0u, 0u, 0u, 0u);
-        if (there) p[i].u = *reinterpret_cast<const uint4*>(a + j0 + 256 * i);
-        if (there) q[i].u = *reinterpret_cast<const uint4*>(b + j0 + 256 * i);
+        if (there) p[i].u = __ldcg(reinterpret_cast<const uint4*>(a + j0 + 256 * i));
+        if (there) q[i].u = __ldcg(reinterpret_cast<const uint4*>(b + j0 + 256 * i));
       }
 #pragma unroll
       for (int i = 0; i < 4; ++i)
 #pragma unroll
         for (int k = 0; k < 8; ++k) logit = fmaf(to_f32(p[i].t[k]), to_f32(q[i].t[k]), logit);
     }
-    if (whole + lane < dim) logit = fmaf(to_f32(a[whole + lane]), to_f32(b[whole + lane]), logit);
+    if (whole + lane < dim)
+      logit = fmaf(to_f32(__ldcg(a + whole + lane)), to_f32(__ldcg(b + whole + lane)), logit);
 #pragma unroll
     for (int k = 16; k; k >>= 1) logit += __shfl_xor_sync(0xffffffffu, logit, k);
   }
+  after_predecessor();  // no CTA ends before stats has
+  if (y == ignore) {
+    if (lane == 0) loss[n] = lse[n] = 0.f;
+    return;
+  }
+  constexpr int kAhead = 4;
+  float2 ahead[kAhead];
+#pragma unroll
+  for (int i = 0; i < kAhead; ++i)
+    ahead[i] = lane + 32 * i < parts ? partial[n * parts + lane + 32 * i]
+                                     : make_float2(-INFINITY, 0.f);
+  const float was = own[n];
   float top = ahead[0].x, sum = 0.f;
 #pragma unroll
   for (int i = 1; i < kAhead; ++i) top = fmaxf(top, ahead[i].x);
