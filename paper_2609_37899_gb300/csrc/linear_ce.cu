@@ -58,7 +58,8 @@ __host__ __device__ constexpr bool sums(int kind) { return kind >= kDembSums; }
 // demb's product reads nothing of dh's, which is launched right before it: it
 // starts on the SMs that dh's last tiles leave and waits for dh's end at its own.
 // What both read is complete by then, as dh's kernels admit their successor
-// after their own wait (8192 x 256 x 960: dh's 128 tiles on 76 pairs).
+// after their own wait (8192 x 256 x 960, dh's 128 tiles on 76 pairs: both calls
+// 68 us where demb waits, 65 so).
 __host__ __device__ constexpr bool is_demb(int kind) { return kind == kDemb || kind == kDembSums; }
 // The successors of these rely on all that came before.
 __host__ __device__ constexpr bool admits_late(int kind) {
