@@ -267,6 +267,13 @@ int soma_debug_probe(uint64_t seed, uint64_t step, int expert, int pert, int pro
  *   returns; the context stays usable.  This is the path every kernel of the
  *   library takes when one of its waits runs out. */
 int soma_debug_wait_timeout(uint32_t max_polls, void* stream);
+/* soma_debug_scan_timeout: the same for the stages of the gated linear
+ *   recurrence's kernels, with a copy under way.  One stage is filled from src
+ *   (device fp32 [1024], 16-byte aligned), another is waited for that nothing
+ *   fills.  The kernel records SOMA_ERR_TIMEOUT, refuses to fill a further
+ *   stage, waits for its copy and writes what arrived to out[0 .. 1023] and
+ *   the number of stages that it filled (1) to out[1024]. */
+int soma_debug_scan_timeout(const float* src, float* out, uint32_t max_polls, void* stream);
 /* soma_debug_tc_gemm: d[128][n] = a[128][k] * b[n][k]^T (fp16 inputs as
  *   uint16 bit patterns, row-major; fp32 output) through the same shared-
  *   memory descriptors, tcgen05.mma and tensor-memory read-back as the

@@ -160,6 +160,7 @@ def _open(path: str):
                                                  ctypes.POINTER(soma_estimate_options), f32, u64,
                                                  u64, vp, i32, i32, vp, vp, vp, sz, vp])
         _sig(L, "soma_debug_wait_timeout", i32, [ctypes.c_uint32, vp])
+        _sig(L, "soma_debug_scan_timeout", i32, [vp, vp, ctypes.c_uint32, vp])
         bd = soma_body_dims
         _sig(L, "soma_body_param_count", i64, [bd])
         _sig(L, "soma_body_workspace_bytes", sz, [bd, i32, i32, i32, i32])
@@ -400,6 +401,16 @@ def debug_probe(seed: int, step: int, expert: int, probe: int, kind: str, p0: in
 def debug_wait_timeout(max_polls: int, stream=None):
     """Launch a kernel whose bounded wait runs out (see soma_api.h)."""
     _check(lib().soma_debug_wait_timeout(max_polls, _stream(stream)), "soma_debug_wait_timeout")
+
+
+def debug_scan_timeout(src: torch.Tensor, max_polls: int, stream=None) -> torch.Tensor:
+    """A stage of the recurrence's kernels that is never filled (see soma_api.h): what arrived of
+    src fp32 [1024], and the number of stages filled, as one tensor of 1025."""
+    out = torch.full((1025,), float("nan"), device=src.device)
+    _check(lib().soma_debug_scan_timeout(_dev(src, torch.float32, "src", 1024),
+                                         ctypes.c_void_p(out.data_ptr()), max_polls,
+                                         _stream(stream)), "soma_debug_scan_timeout")
+    return out
 
 
 def debug_tc_gemm(a: torch.Tensor, b: torch.Tensor, stream=None,

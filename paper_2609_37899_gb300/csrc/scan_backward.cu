@@ -158,7 +158,7 @@ backward_tiled_kernel(const __grid_constant__ Maps maps, const __grid_constant__
   Map<2>* const shared = reinterpret_cast<Map<2>*>(stages + (size_t)depth * stage_elems);
   ring_init(ring, depth);
   int filled = 0, st = 0;
-  uint32_t parity = 0, turn = 0;
+  uint32_t parity = 0, turn = 0, fills = 0;
   after_predecessor();
   for (int64_t at = blockIdx.x; at < s.d.batch * s.blocks * s.chunks; at += gridDim.x) {
     const int64_t item = at / s.chunks, k = at % s.chunks;
@@ -173,6 +173,8 @@ backward_tiled_kernel(const __grid_constant__ Maps maps, const __grid_constant__
     const int64_t rounds = (end - begin + rows - 1) / rows;
 
     const auto fill = [&](int64_t round) {  // warp 0
+      if (!ring_may_fill(ring)) return;
+      ++fills;
       const int to = filled;
       filled = filled + 1 == depth ? 0 : filled + 1;
       if (lane == 0) tc::mbar_arrive_expect_tx(&ring.full[to], stage_elems * sizeof(T));
@@ -301,6 +303,7 @@ backward_tiled_kernel(const __grid_constant__ Maps maps, const __grid_constant__
     if (!MAPS && lane == 0) tc::bulk_wait_read();
     __syncthreads();  // the stages are free
   }
+  if (threadIdx.x == 0) ring_drain(ring, depth, fills);
   admit_successor();
   if (!MAPS && lane == 0) tc::bulk_wait();
 }

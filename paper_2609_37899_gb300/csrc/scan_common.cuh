@@ -412,10 +412,32 @@ __device__ __forceinline__ void ring_init(Ring& r, int depth) {
   __syncthreads();
 }
 
-__device__ __forceinline__ void ring_wait(Ring& r, int stage, uint32_t parity, int* status) {
-  if (r.abort || tc::mbar_wait(&r.full[stage], parity)) return;
+// A wait that runs out records the timeout and raises the abort flag: from
+// then on no stage is filled and no wait is made, and the rest of the CTA's
+// work runs through on whatever the stages hold.
+__device__ __forceinline__ void ring_wait(Ring& r, int stage, uint32_t parity, int* status,
+                                          uint32_t max_polls = 1u << 22) {
+  if (r.abort || tc::mbar_wait(&r.full[stage], parity, max_polls)) return;
   r.abort = 1;
   atomicCAS(status, 0, SOMA_ERR_TIMEOUT);
+}
+
+// Whether the loading warp (all of it) may arm another stage: after an abort
+// the stage's last copy may still be on its way, and its barrier not free.
+__device__ __forceinline__ bool ring_may_fill(const Ring& r) {
+  return !__any_sync(0xffffffffu, r.abort);
+}
+
+// One thread, at the end of a CTA: after an abort the copies on their way land
+// before the CTA leaves its shared memory to another.  fills: the stages filled
+// in all, one after another around the ring, so that stage i's last copy
+// completes phase (its number of fills) - 1.
+__device__ __forceinline__ void ring_drain(Ring& r, int depth, uint32_t fills) {
+  if (!r.abort) return;
+  for (int i = 0; i < depth; ++i) {
+    const uint32_t n = (fills + depth - 1 - i) / depth;
+    if (n) tc::mbar_wait(&r.full[i], (n - 1) & 1);
+  }
 }
 
 // ------------------------------------------------------------------- host --

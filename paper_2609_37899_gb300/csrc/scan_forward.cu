@@ -23,6 +23,8 @@ constexpr int kResident = 5;  // such CTAs fit an SM
 constexpr double kJoin = 0.8; // steps that joining a chunk's map is worth (8 x 1024 x 480 in fp32:
                               // 25.0 us with 0, 23.2 with this)
 
+constexpr int kRingTest = 1024;  // floats of a stage of ring_timeout_kernel
+
 // RAGGED: lengths or resets are given.  MAPS: the chunks' maps instead of h.
 template <typename T, bool RAGGED, bool MAPS>
 __global__ void __launch_bounds__(32 * kWarps, kResident)
@@ -143,7 +145,7 @@ forward_tiled_kernel(const __grid_constant__ Maps maps, const __grid_constant__ 
   Map<2>* const shared = reinterpret_cast<Map<2>*>(stages + (size_t)depth * stage_elems);
   ring_init(ring, depth);
   int filled = 0, st = 0;  // the next stage to fill, and to use
-  uint32_t parity = 0, turn = 0;
+  uint32_t parity = 0, turn = 0, fills = 0;
   after_predecessor();
   for (int64_t at = blockIdx.x; at < s.d.batch * s.blocks * s.chunks; at += gridDim.x) {
     const int64_t item = at / s.chunks, k = at % s.chunks;
@@ -157,6 +159,8 @@ forward_tiled_kernel(const __grid_constant__ Maps maps, const __grid_constant__ 
     const int64_t rounds = stop > begin ? (stop - begin + rows - 1) / rows : 0;
 
     const auto fill = [&](int64_t round) {  // warp 0
+      if (!ring_may_fill(ring)) return;
+      ++fills;
       const int to = filled;
       filled = filled + 1 == depth ? 0 : filled + 1;
       if (lane == 0) tc::mbar_arrive_expect_tx(&ring.full[to], stage_elems * sizeof(T));
@@ -251,7 +255,35 @@ forward_tiled_kernel(const __grid_constant__ Maps maps, const __grid_constant__ 
     }
     __syncthreads();  // the stages have been read
   }
+  if (threadIdx.x == 0) ring_drain(ring, depth, fills);
   admit_successor();
+}
+
+// A wait of the ring that runs out, with a copy under way: stage 0 is filled
+// from src, stage 1 is waited for and never filled.  out: stage 0 as it is
+// when the CTA would leave, then the stages filled (a fill after the timeout is
+// refused).
+__global__ void __launch_bounds__(64)
+ring_timeout_kernel(const float* src, float* out, uint32_t max_polls, int* status) {
+  __shared__ __align__(128) float stages[2][kRingTest];
+  __shared__ Ring ring;
+  uint32_t fills = 0;
+  ring_init(ring, 2);
+  const auto fill = [&](int to) {
+    if (!ring_may_fill(ring)) return;
+    ++fills;
+    if (threadIdx.x) return;
+    tc::mbar_arrive_expect_tx(&ring.full[to], sizeof(stages[0]));
+    tc::bulk_g2s(stages[to], src, sizeof(stages[0]), &ring.full[to]);
+  };
+  if (threadIdx.x < 32) fill(0);
+  ring_wait(ring, 1, 0, status, max_polls);
+  __syncthreads();
+  if (threadIdx.x < 32) fill(1);
+  if (threadIdx.x == 0) ring_drain(ring, 2, fills);
+  __syncthreads();
+  for (int i = threadIdx.x; i < kRingTest; i += 64) out[i] = stages[0][i];
+  if (threadIdx.x == 0) out[kRingTest] = (float)fills;
 }
 
 template <typename T, int V>
@@ -434,6 +466,16 @@ int soma_scan_step(const void* gates, soma_scan_strides gate_strides, int dtype,
     e = two ? step<__half, 2>(gates, s, c, h, st) : step<__half, 1>(gates, s, c, h, st);
   trace_end(SOMA_TRACE_GATE, st);
   return e == cudaSuccess ? SOMA_OK : SOMA_ERR_CUDA;
+}
+
+int soma_debug_scan_timeout(const float* src, float* out, uint32_t max_polls, void* stream) {
+  if (!src || !out || !aligned(src, 16) || !aligned(out, 4) || max_polls < 1 ||
+      max_polls > (1u << 22))
+    return SOMA_ERR_INVALID_ARG;
+  int* status = status_ptr();
+  if (!status) return SOMA_ERR_CUDA;
+  ring_timeout_kernel<<<1, 64, 0, (cudaStream_t)stream>>>(src, out, max_polls, status);
+  return cudaGetLastError() == cudaSuccess ? SOMA_OK : SOMA_ERR_CUDA;
 }
 
 }  // extern "C"
