@@ -74,6 +74,7 @@ backward_kernel(const T* __restrict__ gates, const __grid_constant__ Scan s,
     for (int64_t left = rounds; left > 0; --left, t0 += step) {
       float add[kSegment], f[kSegment], ki[kSegment], kf[kSegment], kg[kSegment], od[kSegment];
       float c = next_mark;
+      bool cut = false;  // a reset in the segment
       const int live = stop - t0 >= kSegment ? kSegment : stop > t0 ? (int)(stop - t0) : 0;
 #pragma unroll
       for (int j = 0; j < kSegment; ++j) {
@@ -85,6 +86,7 @@ backward_kernel(const T* __restrict__ gates, const __grid_constant__ Scan s,
         sigmoid_slope(to_f32(next[j][1]), fg, df);
         tanh_slope(to_f32(next[j][2]), g, dg);
         sigmoid_slope(to_f32(next[j][3]), o, d_o);
+        cut |= reset;
         const float prev = reset ? 0.f : c;
         c = fmaf(fg, prev, i * g);
         tanh_slope(c, th, dth);
@@ -107,10 +109,11 @@ backward_kernel(const T* __restrict__ gates, const __grid_constant__ Scan s,
       Map<1> m = identity<1>();
 #pragma unroll
       for (int j = kSegment - 1; j >= 0; --j) {
-        const float x = f[j] * add[j];
-        m.b[0] = RAGGED ? apply(f[j], x, m.b[0]) : fmaf(f[j], m.b[0], x);
+        // past a reset nothing goes on, not a NaN of its own document either
+        m.b[0] = RAGGED ? apply(f[j], 0.f, add[j] + m.b[0]) : fmaf(f[j], m.b[0], f[j] * add[j]);
         m.a[0] *= f[j];
       }
+      if (RAGGED && cut) m.a[0] = 0.f;
       if (MAPS) {
         join_total<true, RAGGED, kWarps>(shared, m, turn++, total);
         continue;
@@ -212,6 +215,7 @@ backward_tiled_kernel(const __grid_constant__ Maps maps, const __grid_constant__
       // of its state into those of i, f and g
       Two add[kSegment], f[kSegment], ki[kSegment], kf[kSegment], kg[kSegment];
       Two c = mark;
+      bool cut = false;  // a reset in the segment
       const int live = stop - t0 >= kSegment ? kSegment : stop > t0 ? (int)(stop - t0) : 0;
 #pragma unroll
       for (int j = 0; j < kSegment; ++j) {
@@ -226,6 +230,7 @@ backward_tiled_kernel(const __grid_constant__ Maps maps, const __grid_constant__
         sigmoid_slope2(ao, o, d_o);
         const bool reset =
             RAGGED && s.resets && j < live && s.resets[b * s.d.steps + t0 + j] != 0;
+        cut |= reset;
         const Two prev = reset ? two(0.f) : c;
         c = fma2(fg, prev, i * g);
         tanh_slope2(c, th, dth);
@@ -251,9 +256,11 @@ backward_tiled_kernel(const __grid_constant__ Maps maps, const __grid_constant__
       Two A = two(1.f), B = two(0.f);
 #pragma unroll
       for (int j = kSegment - 1; j >= 0; --j) {
-        B = RAGGED ? apply2(f[j], f[j] * add[j], B) : f[j] * (add[j] + B);
+        // past a reset nothing goes on, not a NaN of its own document either
+        B = RAGGED ? apply2(f[j], two(0.f), add[j] + B) : f[j] * (add[j] + B);
         A = A * f[j];
       }
+      if (RAGGED && cut) A = two(0.f);
       Map<2> m;
       split(A, m.a[0], m.a[1]);
       split(B, m.b[0], m.b[1]);

@@ -216,6 +216,8 @@ struct __align__(8 * V) Map {
 };
 
 // A map applied; a = 0 forgets the state altogether, a NaN one too (resets).
+// So a map with a reset among its steps has a = 0, whatever the product of its
+// other gates is (NaN * 0 is not): a document that is not finite ends with it.
 __device__ __forceinline__ float apply(float a, float b, float c) {
   return a == 0.f ? b : fmaf(a, c, b);
 }
@@ -232,7 +234,8 @@ template <bool RAGGED, int V>
 __device__ __forceinline__ void follow(Map<V>& m, const Map<V>& later) {
   apply<RAGGED>(later, m.b);
 #pragma unroll
-  for (int v = 0; v < V; ++v) m.a[v] *= later.a[v];
+  for (int v = 0; v < V; ++v)
+    m.a[v] = RAGGED && (m.a[v] == 0.f || later.a[v] == 0.f) ? 0.f : m.a[v] * later.a[v];
 }
 
 template <int V>

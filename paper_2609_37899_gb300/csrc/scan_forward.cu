@@ -84,10 +84,11 @@ forward_kernel(const T* __restrict__ gates, const __grid_constant__ Scan s, T* _
         f[j] = rcp(one_exp(to_f32(next[j][1])));
       }
       fetch(t0 + step);
+      bool cut = false;  // a reset in the segment
       if (RAGGED && s.resets) {
 #pragma unroll
         for (int j = 0; j < kSegment; ++j)
-          if (j < live && s.resets[b * s.d.steps + t0 + j]) f[j] = 0.f;
+          if (j < live && s.resets[b * s.d.steps + t0 + j]) f[j] = 0.f, cut = true;
       }
       if (live < kSegment) {
 #pragma unroll
@@ -99,6 +100,7 @@ forward_kernel(const T* __restrict__ gates, const __grid_constant__ Scan s, T* _
         m.b[0] = RAGGED ? apply(f[j], u[j], m.b[0]) : fmaf(f[j], m.b[0], u[j]);
         m.a[0] *= f[j];
       }
+      if (RAGGED && cut) m.a[0] = 0.f;
       if (MAPS) {
         join_total<false, RAGGED, kWarps>(shared, m, turn++, total);
         continue;
@@ -199,10 +201,11 @@ forward_tiled_kernel(const __grid_constant__ Maps maps, const __grid_constant__ 
         u[j] = num * rcp2(den * one_exp2(ai));
         f[j] = rcp2(one_exp2(af));
       }
+      bool cut = false;  // a reset in the segment
       if (RAGGED && s.resets) {
 #pragma unroll
         for (int j = 0; j < kSegment; ++j)
-          if (j < live && s.resets[b * s.d.steps + t0 + j]) f[j] = two(0.f);
+          if (j < live && s.resets[b * s.d.steps + t0 + j]) f[j] = two(0.f), cut = true;
       }
       if (live < kSegment) {
 #pragma unroll
@@ -214,6 +217,7 @@ forward_tiled_kernel(const __grid_constant__ Maps maps, const __grid_constant__ 
         B = RAGGED ? apply2(f[j], u[j], B) : fma2(f[j], B, u[j]);
         A = A * f[j];
       }
+      if (RAGGED && cut) A = two(0.f);
       Map<2> m;
       split(A, m.a[0], m.a[1]);
       split(B, m.b[0], m.b[1]);
