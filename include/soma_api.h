@@ -486,7 +486,9 @@ int soma_adamw_step(const soma_adamw_tensor* tensors, int n_tensors, soma_adamw_
  * are not read, leave the state as it is and have h = 0 and gradient 0.  A
  * step with resets[b][t] != 0 starts a document: it takes c_{t-1} = 0 and
  * passes no gradient on, whatever is not finite on either side.
- * Any size may be 0.  A state that is not finite is passed on as it is. */
+ * Any size may be 0.  A state that is not finite is passed on as it is (an
+ * infinite one stays infinite, however small the forget gates): forget gates
+ * are taken as at least 2^-149, the least fp32 number. */
 typedef struct soma_scan_dims {
   int64_t batch; /* 0 .. 2^31 - 1 */
   int64_t steps; /* 0 .. 2^31 - 1 */

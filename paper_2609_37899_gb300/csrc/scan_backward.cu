@@ -84,6 +84,7 @@ backward_kernel(const T* __restrict__ gates, const __grid_constant__ Scan s,
         float i, di, fg, df, g, dg, o, d_o, th, dth;
         sigmoid_slope(to_f32(next[j][0]), i, di);
         sigmoid_slope(to_f32(next[j][1]), fg, df);
+        fg = open(fg);
         tanh_slope(to_f32(next[j][2]), g, dg);
         sigmoid_slope(to_f32(next[j][3]), o, d_o);
         cut |= reset;
@@ -113,7 +114,7 @@ backward_kernel(const T* __restrict__ gates, const __grid_constant__ Scan s,
         m.b[0] = RAGGED ? apply(f[j], 0.f, add[j] + m.b[0]) : fmaf(f[j], m.b[0], f[j] * add[j]);
         m.a[0] *= f[j];
       }
-      if (RAGGED && cut) m.a[0] = 0.f;
+      m.a[0] = RAGGED && cut ? 0.f : fmaxf(m.a[0], kLeast);
       if (MAPS) {
         join_total<true, RAGGED, kWarps>(shared, m, turn++, total);
         continue;
@@ -226,6 +227,7 @@ backward_tiled_kernel(const __grid_constant__ Maps maps, const __grid_constant__
         Two i, di, fg, df, g, dg, o, d_o, th, dth;
         sigmoid_slope2(ai, i, di);
         sigmoid_slope2(af, fg, df);
+        fg = open2(fg);
         tanh_slope2(ag, g, dg);
         sigmoid_slope2(ao, o, d_o);
         const bool reset =
@@ -260,9 +262,10 @@ backward_tiled_kernel(const __grid_constant__ Maps maps, const __grid_constant__
         B = RAGGED ? apply2(f[j], two(0.f), add[j] + B) : f[j] * (add[j] + B);
         A = A * f[j];
       }
-      if (RAGGED && cut) A = two(0.f);
       Map<2> m;
       split(A, m.a[0], m.a[1]);
+#pragma unroll
+      for (int v = 0; v < 2; ++v) m.a[v] = RAGGED && cut ? 0.f : fmaxf(m.a[v], kLeast);
       split(B, m.b[0], m.b[1]);
       float in[2];
       if (MAPS) {

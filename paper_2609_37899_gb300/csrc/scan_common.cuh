@@ -63,6 +63,14 @@ __device__ __forceinline__ float max_nan(float a, float b) {
 // 1 + exp(-x): its reciprocal is sigmoid(x).
 __device__ __forceinline__ float one_exp(float x) { return 1.f + tc::ex2(-kLog2e * x); }
 
+// Forget gates, and products of them, are never taken as less than this, the
+// least fp32 number: 0 times a state that is infinite would be NaN, and which
+// products underflow depends on how the steps are cut.  Of a finite state it
+// leaves less than 2^-21 (2^-49 of one up to 2^100).  So 0 stands for a reset
+// alone.
+constexpr float kLeast = 0x1p-149f;
+__device__ __forceinline__ float open(float f) { return max_nan(f, kLeast); }
+
 // tanh(x) = num / den, a rational function of degrees 9 and 8 fitted to
 // tanh(x)/x in x^2 by iteratively reweighted least squares of the relative
 // error on [0, 8.7] (1.5e-8; in fp32 with the division 3.2e-7, also near 0,
@@ -150,6 +158,10 @@ __device__ __forceinline__ void tanh_slope2(Two x, Two& y, Two& dy) {
   dy = (e * two(4.f)) * (r * r);
 }
 
+__device__ __forceinline__ Two open2(Two f) {
+  return each(f, [](float x) { return open(x); });
+}
+
 struct Scan {
   soma_scan_dims d;
   soma_scan_strides gs, hs, ds;
@@ -218,6 +230,7 @@ struct __align__(8 * V) Map {
 // A map applied; a = 0 forgets the state altogether, a NaN one too (resets).
 // So a map with a reset among its steps has a = 0, whatever the product of its
 // other gates is (NaN * 0 is not): a document that is not finite ends with it.
+// Without one a is at least kLeast, also where a gate is NaN: b is NaN then.
 __device__ __forceinline__ float apply(float a, float b, float c) {
   return a == 0.f ? b : fmaf(a, c, b);
 }
@@ -235,7 +248,8 @@ __device__ __forceinline__ void follow(Map<V>& m, const Map<V>& later) {
   apply<RAGGED>(later, m.b);
 #pragma unroll
   for (int v = 0; v < V; ++v)
-    m.a[v] = RAGGED && (m.a[v] == 0.f || later.a[v] == 0.f) ? 0.f : m.a[v] * later.a[v];
+    m.a[v] = RAGGED && (m.a[v] == 0.f || later.a[v] == 0.f)
+                 ? 0.f : fmaxf(m.a[v] * later.a[v], kLeast);
 }
 
 template <int V>

@@ -81,7 +81,7 @@ forward_kernel(const T* __restrict__ gates, const __grid_constant__ Scan s, T* _
         float num, den;
         tanh_parts(to_f32(next[j][2]), num, den);
         u[j] = num * rcp(den * one_exp(to_f32(next[j][0])));
-        f[j] = rcp(one_exp(to_f32(next[j][1])));
+        f[j] = open(rcp(one_exp(to_f32(next[j][1]))));
       }
       fetch(t0 + step);
       bool cut = false;  // a reset in the segment
@@ -100,7 +100,7 @@ forward_kernel(const T* __restrict__ gates, const __grid_constant__ Scan s, T* _
         m.b[0] = RAGGED ? apply(f[j], u[j], m.b[0]) : fmaf(f[j], m.b[0], u[j]);
         m.a[0] *= f[j];
       }
-      if (RAGGED && cut) m.a[0] = 0.f;
+      m.a[0] = RAGGED && cut ? 0.f : fmaxf(m.a[0], kLeast);
       if (MAPS) {
         join_total<false, RAGGED, kWarps>(shared, m, turn++, total);
         continue;
@@ -199,7 +199,7 @@ forward_tiled_kernel(const __grid_constant__ Maps maps, const __grid_constant__ 
         Two num, den;
         tanh_parts2(ag, num, den);
         u[j] = num * rcp2(den * one_exp2(ai));
-        f[j] = rcp2(one_exp2(af));
+        f[j] = open2(rcp2(one_exp2(af)));
       }
       bool cut = false;  // a reset in the segment
       if (RAGGED && s.resets) {
@@ -217,9 +217,10 @@ forward_tiled_kernel(const __grid_constant__ Maps maps, const __grid_constant__ 
         B = RAGGED ? apply2(f[j], u[j], B) : fma2(f[j], B, u[j]);
         A = A * f[j];
       }
-      if (RAGGED && cut) A = two(0.f);
       Map<2> m;
       split(A, m.a[0], m.a[1]);
+#pragma unroll
+      for (int v = 0; v < 2; ++v) m.a[v] = RAGGED && cut ? 0.f : fmaxf(m.a[v], kLeast);
       split(B, m.b[0], m.b[1]);
       float in[2];
       if (MAPS) join_total<false, RAGGED, kWarps>(shared, m, turn++, total);
@@ -309,7 +310,7 @@ scan_step_kernel(const T* __restrict__ gates, const __grid_constant__ Scan s,
   for (int v = 0; v < V; ++v) {
     float num, den;
     tanh_parts(a[2][v], num, den);
-    x[v] = fmaf(rcp(one_exp(a[1][v])), c[at + v], num * rcp(den * one_exp(a[0][v])));
+    x[v] = fmaf(open(rcp(one_exp(a[1][v]))), c[at + v], num * rcp(den * one_exp(a[0][v])));
     tanh_parts(x[v], num, den);
     y[v] = num * rcp(den * one_exp(a[3][v]));
   }
