@@ -137,10 +137,14 @@ __device__ __forceinline__ void tanh_parts2(Two x, Two& num, Two& den) {
   den = fma2(fma2(fma2(fma2(two(0x1.ad4ff2p-21f), s, two(0x1.5c82aep-12f)), s,
                        two(0x1.a968bap-6f)), s, two(0x1.de8dd4p-2f)), s, two(1.f));
 }
-// sigmoid and y (1 - y): the derivative good to 1 u of 1.
+// sigmoid and its derivative e / (1 + e)^2 with e = exp(-x), both good relative
+// to their size on either side: y - y^2 would be good to half an ulp of 1 only,
+// and a saturated gate's is far below.  e stays finite (0 times infinity); the
+// reciprocal of 2^127 is flushed to 0.
 __device__ __forceinline__ void sigmoid_slope2(Two x, Two& y, Two& dy) {
-  y = rcp2(one_exp2(x));
-  dy = fma2(y * two(-1.f), y, y);
+  const Two e = each(x * two(-kLog2e), [](float z) { return tc::ex2(min_nan(z, 127.f)); });
+  y = rcp2(e + two(1.f));
+  dy = (e * y) * y;
 }
 // tanh by e = exp(-2 |x|), which gives the derivative 4 e / (1 + e)^2 good
 // relative to its size, and below 0.1 by the Taylor series to x^5 (6e-8).
