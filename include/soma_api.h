@@ -439,10 +439,11 @@ typedef enum soma_dtype {
  *   block with key (seed halves) and counter (q, k, t, 0x80000002): a
  *   domain disjoint from the probes' and the initialisation's.  A root above
  *   zero is never rounded to zero.
- * An element whose new moments would not be finite keeps its parameter and
- * moments (up to their rounding to 8 bits), and SOMA_ERR_NONFINITE is
- * recorded; a grad_scale that is not finite skips the whole step the same
- * way. */
+ * An element whose new moments would not be finite, by its gradient or by what
+ * is stored of it, keeps its parameter and moments (up to their rounding to 8
+ * bits), and SOMA_ERR_NONFINITE is recorded; a grad_scale that is not finite
+ * skips the whole step the same way.  In 8 bits a scale that is not finite is
+ * that of 256 such elements. */
 typedef struct soma_adamw_tensor {
   void* param;         /* [count] of param_dtype, updated */
   const void* grad;    /* [count] of grad_dtype */

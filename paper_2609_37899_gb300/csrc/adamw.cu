@@ -212,6 +212,15 @@ __device__ __forceinline__ void update_one(const Args& a, float decay, float x, 
   w = __fmaf_rn(-step, a.lr, __fmaf_rn(-w, decay, w));
 }
 
+// A thread's eight bytes of the 8-bit state with those set to e4m3's NaN whose
+// moments are NaN and stay it.
+__device__ __forceinline__ uint2 with_nan(uint2 b, uint32_t which) {
+#pragma unroll
+  for (int j = 0; j < kGroup; ++j)
+    if ((which >> j) & 1u) (j < 4 ? b.x : b.y) |= 0x7Fu << (8 * (j & 3));
+  return b;
+}
+
 // The thread's eight elements from i on, n of which exist.  FULL: all of the
 // warp's exist and are aligned.  Returns whether an element's new moments were
 // not finite: it keeps what it had.
@@ -237,24 +246,41 @@ __device__ __forceinline__ bool eight_elements(const Row& t, const Args& a, floa
   load_n<FULL>(static_cast<const G*>(t.g) + i, n, g);
   load_state();
   bool bad = false;
-  float top_m = 0.f, top_r = 0.f;
   if (EIGHT) {
 #pragma unroll
     for (int j = 0; j < kGroup; ++j)
       update_one<true>(a, t.decay, __fmul_rn(g[j], gs), w[j], m[j], v[j], r[j]);
     // The bits of non-negative floats order as the floats do, NaN above all:
-    // one reduction gives the scale and whether all roots are finite.  A first
-    // moment that is not comes with a second one that is not: the square of a
-    // gradient overflows long before the gradient does.
+    // one reduction gives the scale and whether all of the block are finite.
     const auto largest = [](const float (&x)[8]) {
       uint32_t top = 0u;
 #pragma unroll
       for (int j = 0; j < kGroup; ++j) top = max(top, __float_as_uint(x[j]) & 0x7FFFFFFFu);
       return __reduce_max_sync(0xffffffffu, top);
     };
-    uint32_t bits = largest(r);
-    if (bits >= 0x7F800000u) {  // the whole warp
-      uint32_t keep = 0;
+    uint32_t top_r = largest(r), top_m = largest(m);
+    // lost: elements whose stored moment is NaN, eight bits for m and eight for r
+    const auto store_all = [&](uint32_t lost) {
+      if (MASTER) store_n<FULL>(t.master + i, n, w);
+      store_n<FULL>(static_cast<P*>(t.p) + i, n, w);
+      const uint64_t q = (uint64_t)i / kGroup;
+      const uint4 rnd =
+          random_block(make_uint4((uint32_t)q, (uint32_t)t.index, a.t, 0x80000002u), a.key);
+      uint32_t random[8];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        random[2 * j] = (word_of(rnd, j) << 4) & 0xFFFF0u;
+        random[2 * j + 1] = (word_of(rnd, j) >> 12) & 0xFFFF0u;
+      }
+      const uint2 bm = pack_block<false>(m, __uint_as_float(top_m), random, t.ms + block);
+      const uint2 bv = pack_block<true>(r, __uint_as_float(top_r), random, t.vs + block);
+      store_bytes<FULL>(static_cast<uint8_t*>(t.m) + i, n, with_nan(bm, lost));
+      store_bytes<FULL>(static_cast<uint8_t*>(t.v) + i, n, with_nan(bv, lost >> 8));
+    };
+    if (max(top_r, top_m) >= 0x7F800000u) {  // the whole warp
+      // a gradient that is not finite, or whose square is not, or a stored moment
+      if (!isfinite(t.ms[block]) || !isfinite(t.vs[block])) return true;  // no element has moments
+      uint32_t keep = 0, lost = 0;
       float new_w[8], new_m[8], new_r[8];
 #pragma unroll
       for (int j = 0; j < kGroup; ++j) {
@@ -263,13 +289,18 @@ __device__ __forceinline__ bool eight_elements(const Row& t, const Args& a, floa
       }
       load_state();
 #pragma unroll
-      for (int j = 0; j < kGroup; ++j)
+      for (int j = 0; j < kGroup; ++j) {
         if (!((keep >> j) & 1u)) w[j] = new_w[j], m[j] = new_m[j], r[j] = new_r[j];
-      bad = keep != 0;
-      bits = largest(r);
+        // the scales are those of the others
+        if (!isfinite(m[j])) lost |= 1u << j, m[j] = 0.f;
+        if (!isfinite(r[j])) lost |= 256u << j, r[j] = 0.f;
+      }
+      top_r = largest(r);
+      top_m = largest(m);
+      store_all(lost);  // apart, so that the common path holds no `lost`
+      return keep != 0;
     }
-    top_r = __uint_as_float(bits);
-    top_m = __uint_as_float(largest(m));
+    store_all(0u);
   } else {
 #pragma unroll
     for (int j = 0; j < kGroup; ++j) {
@@ -278,24 +309,8 @@ __device__ __forceinline__ bool eight_elements(const Row& t, const Args& a, floa
       if (isfinite(m1) && isfinite(v1)) w[j] = w1, m[j] = m1, v[j] = v1;
       else bad = true;
     }
-  }
-  if (MASTER) store_n<FULL>(t.master + i, n, w);
-  store_n<FULL>(static_cast<P*>(t.p) + i, n, w);
-  if (EIGHT) {
-    const uint64_t q = (uint64_t)i / kGroup;
-    const uint4 rnd =
-        random_block(make_uint4((uint32_t)q, (uint32_t)t.index, a.t, 0x80000002u), a.key);
-    uint32_t random[8];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      random[2 * j] = (word_of(rnd, j) << 4) & 0xFFFF0u;
-      random[2 * j + 1] = (word_of(rnd, j) >> 12) & 0xFFFF0u;
-    }
-    const uint2 bm = pack_block<false>(m, top_m, random, t.ms + block);
-    const uint2 bv = pack_block<true>(r, top_r, random, t.vs + block);
-    store_bytes<FULL>(static_cast<uint8_t*>(t.m) + i, n, bm);
-    store_bytes<FULL>(static_cast<uint8_t*>(t.v) + i, n, bv);
-  } else {
+    if (MASTER) store_n<FULL>(t.master + i, n, w);
+    store_n<FULL>(static_cast<P*>(t.p) + i, n, w);
     store_n<FULL>(static_cast<float*>(t.m) + i, n, m);
     store_n<FULL>(static_cast<float*>(t.v) + i, n, v);
   }
