@@ -460,7 +460,7 @@ typedef struct soma_adamw_config {
   double lr;    /* finite */
   double beta1; /* in [0, 1) */
   double beta2; /* in [0, 1) */
-  double eps;   /* > 0, finite, and not 0 in fp32 */
+  double eps;   /* > 0, finite, and not 0 in fp32; 8 bits: at least 2^-126 */
   uint64_t seed; /* of the random rounding (8 bits) */
   int32_t t;     /* 1-based update count */
   int32_t param_dtype, grad_dtype; /* soma_dtype, the same for all tensors */

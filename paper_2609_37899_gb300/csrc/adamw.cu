@@ -12,6 +12,7 @@
 // tensors, 26 bytes each, take 733 us (7.1 TB/s).  The 8-bit form has about 70
 // instructions for 14 to 16 bytes an element and comes to 0.85 of the copy rate:
 // 150M bf16 parameters with masters in 120 tensors 418 us (5.7 TB/s).
+#include <cfloat>
 #include <cmath>
 #include <cuda_fp8.h>
 
@@ -394,6 +395,9 @@ extern "C" int soma_adamw_step(const soma_adamw_tensor* tensors, int n_tensors,
       !std::isfinite((float)cfg.eps) || !aligned(grad_scale, 4))
     return SOMA_ERR_INVALID_ARG;
   const bool eight = cfg.state_bits == 8;
+  // the 8-bit form's reciprocal takes a subnormal denominator for 0, and an
+  // element with zero moments would get 0 times infinity
+  if (eight && (float)cfg.eps < FLT_MIN) return SOMA_ERR_INVALID_ARG;
   const int pw = width(cfg.param_dtype), gw = width(cfg.grad_dtype), sw = eight ? 1 : 4;
   bool master = false, plain = false;
   for (int k = 0; k < n_tensors; ++k) {
