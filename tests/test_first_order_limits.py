@@ -1,4 +1,6 @@
 """Host-side limits of the first-order entry points: no launch is made."""
+import ctypes
+
 import pytest
 
 
@@ -16,3 +18,12 @@ def test_eight_bit_eps_is_a_normal_number(soma, eps):
         **{k: 0x10000 for k in ("param", "grad", "m", "v", "m_scale", "v_scale")}, count=10))
     cfg = soma.soma_adamw_config(1e-3, 0.9, 0.999, eps, 0, 1, 0, 0, 8)
     assert soma.lib().soma_adamw_step(row, 1, cfg, None, None) == 1
+
+
+def test_structures_have_the_sizes_of_the_abi(soma):
+    """Seven pointers, a 64-bit count and a double; four doubles, a 64-bit seed, four 32-bit
+    words; and so on."""
+    for name, size in (("soma_adamw_tensor", 72), ("soma_adamw_config", 56),
+                       ("soma_scan_dims", 24), ("soma_scan_strides", 24),
+                       ("soma_linear_ce_dims", 48)):
+        assert ctypes.sizeof(getattr(soma, name)) == size
