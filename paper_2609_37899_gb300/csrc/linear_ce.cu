@@ -73,7 +73,8 @@ __host__ __device__ constexpr bool admits_late(int kind) {
 struct __align__(16) RowInfo {
   float lse2;  // lse in powers of two
   float g;     // gradient of the loss
-  float rest;  // of the (scaled) entry of G at the target; written by grad
+  float rest;  // p - 1 of the target, by fp32 multiply-adds (rows_kernel); from
+               // grad on, what its rounding took off the (scaled) entry of G
   int32_t y;
 };
 
@@ -503,7 +504,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
 #pragma unroll
               for (int j = 0; j < 32; ++j) {
                 const float p = tc::ex2(fmaf(x[j], kLog2e, -info.lse2));
-                x[j] = g * (j == at ? p - 1.f : p);
+                x[j] = g * (j == at ? info.rest : p);
                 rest = j == at ? x[j] - to_f32(from_f32<T>(x[j])) : rest;
               }
               w.info[m].rest = rest;
@@ -613,7 +614,8 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
 // Joins a row's partial statistics: one warp per row.
 //
 // The tensor cores cut an fp32 sum off instead of rounding it, so a logit comes
-// out short by about 1e-8 of itself for every 16 of its depth.  That matters
+// out short by about 1e-8 of itself for every 16 of its depth, several times
+// that where its products are of one sign, as the target's are.  That matters
 // for the target's, which is large and enters the loss twice (960 deep: the
 // loss was off by 1.2e-6 of itself): it is computed here once more by fp32
 // multiply-adds and takes the other one's place in the sum and in the loss.
@@ -711,9 +713,15 @@ join_kernel(const float2* partial, int parts, const float* own, const T* h, int6
 // Per row, one warp: what it takes part with, and a copy of h in rows of a
 // multiple of 64 elements with the rows that take no part zeroed (their h
 // may hold anything, and 0 * NaN would reach demb).
+//
+// The target's p - 1 is taken from the logit that is in lse, which is not the
+// tensor cores' (join_kernel): that one is short by so much that a row sure of
+// its target would get several times its gradient, always the same way (960
+// deep at a logit of 22: p short by 5e-5 in bf16, 1.3e-4 in fp16, where the
+// loss is 1.5e-5).
 template <typename T>
 __global__ void __launch_bounds__(256)
-rows_kernel(const T* h, soma_linear_ce_dims d, const int64_t* targets, int64_t ignore,
+rows_kernel(const T* h, const T* emb, soma_linear_ce_dims d, const int64_t* targets, int64_t ignore,
             const float* lse, const float* dloss, RowInfo* info, T* copy, int64_t cs, int halves,
             float* top) {
   __shared__ int largest;
@@ -726,16 +734,30 @@ rows_kernel(const T* h, soma_linear_ce_dims d, const int64_t* targets, int64_t i
     const int64_t y = targets[n];
     const float l = lse[n];
     const bool live = y != ignore && y >= 0 && y < d.vocab && isfinite(l);
-    const bool vec = d.h_stride % 8 == 0;
+    const bool vec = d.h_stride % 8 == 0, vec_e = d.emb_stride % 8 == 0;
+    const T* e = emb + (live ? y : 0) * d.emb_stride;
+    float logit = 0.f;
     for (int64_t j = lane * 8; j < cs; j += 256) {
-      const uint4 v =
-          live ? row_piece(h + n * d.h_stride, j, d.dim, vec) : make_uint4(0u, 0u, 0u, 0u);
-      *reinterpret_cast<uint4*>(copy + n * cs + j) = v;
-      if (halves == 2) *reinterpret_cast<uint4*>(copy + (d.rows + n) * cs + j) = v;
+      union {
+        uint4 u;
+        T t[8];
+      } v, w;
+      v.u = w.u = make_uint4(0u, 0u, 0u, 0u);
+      if (live) {
+        v.u = row_piece(h + n * d.h_stride, j, d.dim, vec);
+        w.u = row_piece(e, j, d.dim, vec_e);
+      }
+      *reinterpret_cast<uint4*>(copy + n * cs + j) = v.u;
+      if (halves == 2) *reinterpret_cast<uint4*>(copy + (d.rows + n) * cs + j) = v.u;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) logit = fmaf(to_f32(v.t[k]), to_f32(w.t[k]), logit);
     }
+#pragma unroll
+    for (int k = 16; k; k >>= 1) logit += __shfl_xor_sync(0xffffffffu, logit, k);
     if (lane == 0) {
       RowInfo r = {l * kLog2e, 0.f, 0.f, -1};
       if (live) {
+        r.rest = expm1f(logit - l);
         r.g = dloss[n];
         r.y = (int32_t)y;
         // non-negative floats order as their bits do
@@ -1101,8 +1123,8 @@ cudaError_t backward(const Plan& p, const T* h, const T* emb, const soma_linear_
     e = cudaMemsetAsync(dh_acc, 0,
                         (size_t)p.dh_slots * ceil_div(d.rows, kTile) * kTile * p.acc_stride * 4, st);
   if (e == cudaSuccess)
-    e = launch_overlapped(rows_kernel<T>, row_blocks(d), 256, 0, st, h, d, targets, ignore, lse,
-                          dloss, info, copy, cs, (int)p.halves, top);
+    e = launch_overlapped(rows_kernel<T>, row_blocks(d), 256, 0, st, h, emb, d, targets, ignore,
+                          lse, dloss, info, copy, cs, (int)p.halves, top);
   if (e != cudaSuccess) return e;
   if (p.copy_emb) emb = pack(emb, d.vocab, d.dim, &es, reinterpret_cast<T*>(ws + p.emb), st);
   if (!emb) return cudaErrorLaunchFailure;
