@@ -515,7 +515,7 @@ int64_t soma_scan_workspace_bytes(soma_scan_dims d);
  *   lengths      int32 [batch] or NULL;  resets: uint8 [batch][steps] or NULL
  *   h            [batch][steps][dim] by h_strides (g unused)
  *   c_last       fp32 [batch][dim], the state after the last step, or NULL;
- *                not c0
+ *                must not overlap c0 (SOMA_ERR_INVALID_ARG)
  *   checkpoints  fp32 [soma_scan_checkpoint_count()], or NULL when no
  *                backward call follows */
 int soma_scan_forward(const void* gates, soma_scan_strides gate_strides, int dtype,
@@ -528,7 +528,8 @@ int soma_scan_forward(const void* gates, soma_scan_strides gate_strides, int dty
  *   dc_t = dh_t o (1 - tanh(c_t)^2) + f_{t+1} dc_{t+1}
  *   d a_i = dc g i (1 - i);  d a_f = dc c_{t-1} f (1 - f);
  *   d a_g = dc i (1 - g^2);  d a_o = dh tanh(c) o (1 - o)
- *   dgates  as gates, by dgate_strides;  dc0: fp32 [batch][dim] or NULL
+ *   dgates  as gates, by dgate_strides;  dc0: fp32 [batch][dim] or NULL, must
+ *           not overlap dc_last (SOMA_ERR_INVALID_ARG)
  * gates, lengths, resets: as in the forward call that wrote checkpoints. */
 int soma_scan_backward(const void* gates, soma_scan_strides gate_strides, int dtype,
                        soma_scan_dims d, const float* checkpoints, const int32_t* lengths,

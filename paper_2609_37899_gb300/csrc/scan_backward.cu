@@ -411,6 +411,7 @@ extern "C" int soma_scan_backward(const void* gates, soma_scan_strides gate_stri
     return SOMA_ERR_INVALID_ARG;
   if (d.batch == 0 || d.dim == 0) return SOMA_OK;
   if (d.steps > 0 && (!gates || !dh || !dgates || !checkpoints)) return SOMA_ERR_INVALID_ARG;
+  if (overlap(dc_last, dc0, d)) return SOMA_ERR_INVALID_ARG;
   const size_t need = backward_workspace(d);
   if (need && (!workspace || !aligned(workspace, 16) || workspace_bytes < need))
     return SOMA_ERR_WORKSPACE;

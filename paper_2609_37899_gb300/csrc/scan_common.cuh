@@ -478,6 +478,15 @@ inline bool aligned(const void* p, size_t to) {
   return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0;
 }
 
+// Whether two states [batch][dim] share memory (null pointers: no).  A call
+// reads one all along its chunks and writes the other as soon as its first or
+// last chunk is done.
+inline bool overlap(const float* p, const float* q, const soma_scan_dims& d) {
+  if (!p || !q) return false;
+  const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
+  return (a < b ? b - a : a - b) < (uintptr_t)(d.batch * d.dim) * sizeof(float);
+}
+
 inline size_t width(int dtype) { return dtype == SOMA_FP32 ? 4 : 2; }
 
 // How a call is cut.

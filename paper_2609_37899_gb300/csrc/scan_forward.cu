@@ -421,6 +421,7 @@ int soma_scan_forward(const void* gates, soma_scan_strides gate_strides, int dty
     return SOMA_ERR_INVALID_ARG;
   if (d.batch == 0 || d.dim == 0) return SOMA_OK;
   if (d.steps > 0 && (!gates || !h)) return SOMA_ERR_INVALID_ARG;
+  if (overlap(c0, c_last, d)) return SOMA_ERR_INVALID_ARG;
   const size_t need = forward_workspace(d);
   if (need && (!workspace || !aligned(workspace, 16) || workspace_bytes < need))
     return SOMA_ERR_WORKSPACE;

@@ -27,3 +27,17 @@ def test_structures_have_the_sizes_of_the_abi(soma):
                        ("soma_scan_dims", 24), ("soma_scan_strides", 24),
                        ("soma_linear_ce_dims", 48)):
         assert ctypes.sizeof(getattr(soma, name)) == size
+
+
+def test_states_of_the_recurrence_must_not_overlap(soma):
+    """c_last in the place of c0 (or of a part of it) would hold what the sizes make of it: some are cut
+    into chunks that still read c0 when the last one is done.  The same of dc0 and dc_last."""
+    L, st = soma.lib(), soma.soma_scan_strides(96, 32, 8)
+    fake, at = ctypes.c_void_p(0x10000), lambda n: ctypes.c_void_p(0x20000 + 4 * n)
+    for dims, far in (((2, 3, 8), 16), ((1, 1 << 16, 64), 64)):
+        d = soma.soma_scan_dims(*dims)
+        for off in (0, 1, far - 1, 1 - far):
+            assert L.soma_scan_forward(fake, st, 0, d, at(0), None, None, fake, st, at(off), None,
+                                       fake, 1 << 40, None) == 1
+            assert L.soma_scan_backward(fake, st, 0, d, fake, None, None, fake, st, at(0), fake, st,
+                                        at(off), fake, 1 << 40, None) == 1
