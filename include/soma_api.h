@@ -248,6 +248,22 @@ int soma_trace_enable(int enable);
 /* reset != 0 also forgets the records that were read. */
 int soma_trace_read(soma_kernel_times* out, int reset);
 
+/* The first-order entry points (below) are classes of their own, which are not
+ * in soma_kernel_times.  A call is bracketed as a whole, as its launches
+ * overlap. */
+enum {
+  SOMA_TRACE_LINEAR_CE = 5, /* soma_linear_ce_forward, soma_linear_ce_backward */
+  SOMA_TRACE_SCAN = 6,      /* soma_scan_forward, soma_scan_backward, soma_scan_step */
+  SOMA_TRACE_ADAMW = 7,     /* soma_adamw_step, each of its launches */
+  SOMA_TRACE_FIRST_ORDER = 3
+};
+typedef struct soma_first_order_times {
+  double ms[SOMA_TRACE_FIRST_ORDER];     /* summed device time, in the order above */
+  int64_t calls[SOMA_TRACE_FIRST_ORDER];
+} soma_first_order_times;
+/* As soma_trace_read, for these. */
+int soma_trace_read_first_order(soma_first_order_times* out, int reset);
+
 /* Test exports (bit-exactness of the generator the kernels use).
  * soma_debug_philox: out4[j] = Philox4x32-10(ctr4[j], key = seed halves) for
  *   j < count; ctr4 and out4 are device uint32 [count][4].

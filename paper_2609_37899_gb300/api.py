@@ -37,6 +37,7 @@ class soma_dims(ctypes.Structure):
 
 
 TRACE_KINDS = ("gate", "head", "reduce", "update", "prep")
+TRACE_FIRST_ORDER = ("linear_ce", "scan", "adamw")
 
 
 class soma_body_dims(ctypes.Structure):
@@ -87,6 +88,10 @@ MAX_ACCUM = 64
 
 class soma_kernel_times(ctypes.Structure):
     _fields_ = [("ms", ctypes.c_double * 5), ("launches", ctypes.c_int64 * 5)]
+
+
+class soma_first_order_times(ctypes.Structure):
+    _fields_ = [("ms", ctypes.c_double * 3), ("calls", ctypes.c_int64 * 3)]
 
 
 def _sig(lib, name, res, args):
@@ -142,6 +147,7 @@ def _open(path: str):
         _sig(L, "soma_status_string", ctypes.c_char_p, [i32])
         _sig(L, "soma_trace_enable", i32, [i32])
         _sig(L, "soma_trace_read", i32, [ctypes.POINTER(soma_kernel_times), i32])
+        _sig(L, "soma_trace_read_first_order", i32, [ctypes.POINTER(soma_first_order_times), i32])
         _sig(L, "soma_debug_philox", i32, [u64, vp, vp, i32, vp])
         _sig(L, "soma_debug_rademacher", i32, [u64, u64, i32, i32, i64, i64, vp, vp])
         _sig(L, "soma_debug_tc_gemm", i32, [vp, vp, vp, i32, i32, vp])
@@ -364,6 +370,14 @@ def trace_read(reset: bool = True) -> dict:
     t = soma_kernel_times()
     _check(lib().soma_trace_read(ctypes.byref(t), 1 if reset else 0), "soma_trace_read")
     return {k: (t.ms[j], int(t.launches[j])) for j, k in enumerate(TRACE_KINDS)}
+
+
+def trace_read_first_order(reset: bool = True) -> dict:
+    """{kind: (total_ms, calls)} of the traced first-order calls (waits for them)."""
+    t = soma_first_order_times()
+    _check(lib().soma_trace_read_first_order(ctypes.byref(t), 1 if reset else 0),
+           "soma_trace_read_first_order")
+    return {k: (t.ms[j], int(t.calls[j])) for j, k in enumerate(TRACE_FIRST_ORDER)}
 
 
 def get_status(stream=None) -> int:

@@ -466,9 +466,9 @@ extern "C" int soma_adamw_step(const soma_adamw_tensor* tensors, int n_tensors,
     }
     const int64_t most = (int64_t)1 << 30;
     const unsigned grid = (unsigned)(tab.chunks < most ? tab.chunks : most);
-    trace_begin(SOMA_TRACE_UPDATE, (cudaStream_t)stream);
+    trace_begin(SOMA_TRACE_ADAMW, (cudaStream_t)stream);
     kernel<<<grid, kThreads, 0, (cudaStream_t)stream>>>(tab, a, grad_scale, status);
-    trace_end(SOMA_TRACE_UPDATE, (cudaStream_t)stream);
+    trace_end(SOMA_TRACE_ADAMW, (cudaStream_t)stream);
     if (cudaGetLastError() != cudaSuccess) return SOMA_ERR_CUDA;
   }
   return SOMA_OK;

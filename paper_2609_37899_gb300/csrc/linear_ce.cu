@@ -1250,14 +1250,14 @@ int soma_linear_ce_forward(const void* h, const void* emb, soma_linear_ce_dims d
   if (!status) return SOMA_ERR_CUDA;
   uint8_t* ws = static_cast<uint8_t*>(workspace);
   const cudaStream_t st = (cudaStream_t)stream;
-  trace_begin(SOMA_TRACE_HEAD, st);
+  trace_begin(SOMA_TRACE_LINEAR_CE, st);
   const cudaError_t e =
       d.dtype == SOMA_BF16
           ? forward(p, static_cast<const __nv_bfloat16*>(h), static_cast<const __nv_bfloat16*>(emb),
                     d, targets, ignore_index, loss, lse, ws, status, st)
           : forward(p, static_cast<const __half*>(h), static_cast<const __half*>(emb), d, targets,
                     ignore_index, loss, lse, ws, status, st);
-  trace_end(SOMA_TRACE_HEAD, st);
+  trace_end(SOMA_TRACE_LINEAR_CE, st);
   return e == cudaSuccess ? SOMA_OK : SOMA_ERR_CUDA;
 }
 
@@ -1279,7 +1279,7 @@ int soma_linear_ce_backward(const void* h, const void* emb, soma_linear_ce_dims 
   if (!status) return SOMA_ERR_CUDA;
   uint8_t* ws = static_cast<uint8_t*>(workspace);
   const cudaStream_t st = (cudaStream_t)stream;
-  trace_begin(SOMA_TRACE_HEAD, st);
+  trace_begin(SOMA_TRACE_LINEAR_CE, st);
   const cudaError_t e =
       d.dtype == SOMA_BF16
           ? backward(p, static_cast<const __nv_bfloat16*>(h), static_cast<const __nv_bfloat16*>(emb),
@@ -1288,7 +1288,7 @@ int soma_linear_ce_backward(const void* h, const void* emb, soma_linear_ce_dims 
           : backward(p, static_cast<const __half*>(h), static_cast<const __half*>(emb), d, targets,
                      ignore_index, lse, dloss, static_cast<__half*>(dh), dh_stride,
                      static_cast<__half*>(demb), demb_stride, ws, status, st);
-  trace_end(SOMA_TRACE_HEAD, st);
+  trace_end(SOMA_TRACE_LINEAR_CE, st);
   return e == cudaSuccess ? SOMA_OK : SOMA_ERR_CUDA;
 }
 

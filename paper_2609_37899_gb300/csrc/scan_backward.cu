@@ -428,11 +428,11 @@ extern "C" int soma_scan_backward(const void* gates, soma_scan_strides gate_stri
   const cudaStream_t st = (cudaStream_t)stream;
   int* status = status_ptr();
   if (!status) return SOMA_ERR_CUDA;
-  trace_begin(SOMA_TRACE_GATE, st);
+  trace_begin(SOMA_TRACE_SCAN, st);
   const cudaError_t e =
       dtype == SOMA_FP32   ? backward<float>(gates, s, dh, dc_last, dgates, dc0, status, st)
       : dtype == SOMA_BF16 ? backward<__nv_bfloat16>(gates, s, dh, dc_last, dgates, dc0, status, st)
                            : backward<__half>(gates, s, dh, dc_last, dgates, dc0, status, st);
-  trace_end(SOMA_TRACE_GATE, st);
+  trace_end(SOMA_TRACE_SCAN, st);
   return e == cudaSuccess ? SOMA_OK : SOMA_ERR_CUDA;
 }

@@ -439,11 +439,11 @@ int soma_scan_forward(const void* gates, soma_scan_strides gate_strides, int dty
   const cudaStream_t st = (cudaStream_t)stream;
   int* status = status_ptr();
   if (!status) return SOMA_ERR_CUDA;
-  trace_begin(SOMA_TRACE_GATE, st);
+  trace_begin(SOMA_TRACE_SCAN, st);
   const cudaError_t e = dtype == SOMA_FP32   ? forward<float>(gates, s, h, status, st)
                         : dtype == SOMA_BF16 ? forward<__nv_bfloat16>(gates, s, h, status, st)
                                              : forward<__half>(gates, s, h, status, st);
-  trace_end(SOMA_TRACE_GATE, st);
+  trace_end(SOMA_TRACE_SCAN, st);
   return e == cudaSuccess ? SOMA_OK : SOMA_ERR_CUDA;
 }
 
@@ -463,14 +463,14 @@ int soma_scan_step(const void* gates, soma_scan_strides gate_strides, int dtype,
   s.hs = h_strides;
   const cudaStream_t st = (cudaStream_t)stream;
   const bool two = dim % 2 == 0 && pairs(gates, gate_strides) && pairs(h, h_strides);
-  trace_begin(SOMA_TRACE_GATE, st);
+  trace_begin(SOMA_TRACE_SCAN, st);
   cudaError_t e;
   if (dtype == SOMA_FP32) e = step<float, 1>(gates, s, c, h, st);
   else if (dtype == SOMA_BF16)
     e = two ? step<__nv_bfloat16, 2>(gates, s, c, h, st) : step<__nv_bfloat16, 1>(gates, s, c, h, st);
   else
     e = two ? step<__half, 2>(gates, s, c, h, st) : step<__half, 1>(gates, s, c, h, st);
-  trace_end(SOMA_TRACE_GATE, st);
+  trace_end(SOMA_TRACE_SCAN, st);
   return e == cudaSuccess ? SOMA_OK : SOMA_ERR_CUDA;
 }
 

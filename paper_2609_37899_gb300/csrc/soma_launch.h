@@ -15,7 +15,8 @@ namespace soma {
 // position word of the checked build; nullptr if it cannot be found.
 int* status_ptr();
 
-// Tracing hooks: bracket one kernel launch of class `kind` (SOMA_TRACE_*).
+// Tracing hooks: bracket one kernel launch (first-order operators: one call) of
+// class `kind` (SOMA_TRACE_*).
 void trace_begin(int kind, cudaStream_t stream);
 void trace_end(int kind, cudaStream_t stream);
 

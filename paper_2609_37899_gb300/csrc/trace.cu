@@ -1,6 +1,7 @@
 // trace.cu -- optional per-kernel-class timing with CUDA events recorded on
-// the launching stream around every kernel of soma_spsa_step / soma_eval_loss
-// (soma_trace_enable / soma_trace_read in include/soma_api.h).
+// the launching stream around every kernel of soma_spsa_step / soma_eval_loss,
+// and around every call of the first-order entry points (soma_trace_enable /
+// soma_trace_read / soma_trace_read_first_order in include/soma_api.h).
 #include <mutex>
 #include <vector>
 
@@ -31,6 +32,42 @@ cudaEvent_t take_event() {
   cudaEvent_t e = nullptr;
   if (cudaEventCreate(&e) != cudaSuccess) return nullptr;
   return e;
+}
+
+// Sums the records of the classes [first, first + count).  Under g_mu.
+int read_kinds(int first, int count, double* ms, int64_t* launches, int reset) {
+  for (int k = 0; k < count; ++k) {
+    ms[k] = 0.0;
+    launches[k] = 0;
+  }
+  int rc = SOMA_OK;
+  for (const Record& r : g_pending) {
+    if (r.kind < first || r.kind >= first + count) continue;
+    if (cudaEventSynchronize(r.stop) != cudaSuccess) {
+      rc = SOMA_ERR_CUDA;
+      continue;
+    }
+    float t = 0.f;
+    if (cudaEventElapsedTime(&t, r.start, r.stop) != cudaSuccess) {
+      rc = SOMA_ERR_CUDA;
+      continue;
+    }
+    ms[r.kind - first] += t;
+    launches[r.kind - first] += 1;
+  }
+  if (reset) {
+    std::vector<Record> others;
+    for (const Record& r : g_pending) {
+      if (r.kind < first || r.kind >= first + count) {
+        others.push_back(r);
+        continue;
+      }
+      g_pool.push_back(r.start);
+      g_pool.push_back(r.stop);
+    }
+    g_pending.swap(others);
+  }
+  return rc;
 }
 
 }  // namespace
@@ -67,34 +104,13 @@ int soma_trace_enable(int enable) {
 int soma_trace_read(soma_kernel_times* out, int reset) {
   if (!out) return SOMA_ERR_INVALID_ARG;
   std::lock_guard<std::mutex> lk(g_mu);
-  for (int k = 0; k < SOMA_TRACE_KINDS; ++k) {
-    out->ms[k] = 0.0;
-    out->launches[k] = 0;
-  }
-  int rc = SOMA_OK;
-  for (const Record& r : g_pending) {
-    if (cudaEventSynchronize(r.stop) != cudaSuccess) {
-      rc = SOMA_ERR_CUDA;
-      continue;
-    }
-    float ms = 0.f;
-    if (cudaEventElapsedTime(&ms, r.start, r.stop) != cudaSuccess) {
-      rc = SOMA_ERR_CUDA;
-      continue;
-    }
-    if (r.kind >= 0 && r.kind < SOMA_TRACE_KINDS) {
-      out->ms[r.kind] += ms;
-      out->launches[r.kind] += 1;
-    }
-  }
-  if (reset) {
-    for (const Record& r : g_pending) {
-      g_pool.push_back(r.start);
-      g_pool.push_back(r.stop);
-    }
-    g_pending.clear();
-  }
-  return rc;
+  return read_kinds(0, SOMA_TRACE_KINDS, out->ms, out->launches, reset);
+}
+
+int soma_trace_read_first_order(soma_first_order_times* out, int reset) {
+  if (!out) return SOMA_ERR_INVALID_ARG;
+  std::lock_guard<std::mutex> lk(g_mu);
+  return read_kinds(SOMA_TRACE_LINEAR_CE, SOMA_TRACE_FIRST_ORDER, out->ms, out->calls, reset);
 }
 
 }  // extern "C"
