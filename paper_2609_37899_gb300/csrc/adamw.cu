@@ -16,6 +16,8 @@
 #include <cmath>
 #include <cuda_fp8.h>
 
+#define SOMA_CHECK_FILE 11
+#include "checked.cuh"
 #include "numeric.cuh"
 #include "soma_api.h"
 #include "soma_launch.h"
@@ -340,15 +342,20 @@ adamw_kernel(const __grid_constant__ Table tab, const __grid_constant__ Args a,
       const int mid = (lo + hi + 1) >> 1;
       if (tab.row[mid].first <= chunk) lo = mid; else hi = mid - 1;
     }
+    if (!SOMA_CHECK(bucket < kBuckets && lo >= 0 && lo < tab.rows && tab.row[lo].first <= chunk,
+                    status))
+      continue;
     const Row& t = tab.row[lo];
     const int64_t i = (chunk - t.first) * kChunk + (int64_t)threadIdx.x * kGroup;
     const int64_t warp_i = i - (threadIdx.x & 31) * kGroup;
     if (warp_i >= t.n) continue;
+    if (!SOMA_CHECK(warp_i >= 0 && warp_i % kBlock8 == 0, status)) continue;
     if (t.vec && warp_i + 32 * kGroup <= t.n) {
       bad |= eight_elements<P, G, MASTER, EIGHT, true>(t, a, gs, i, kGroup);
     } else {
       const int n = i >= t.n ? 0 : (int)(t.n - i < kGroup ? t.n - i : kGroup);
-      bad |= eight_elements<P, G, MASTER, EIGHT, false>(t, a, gs, i, n);
+      const bool in = SOMA_CHECK(n >= 0 && n <= kGroup && (n == 0 || i + n <= t.n), status);
+      bad |= eight_elements<P, G, MASTER, EIGHT, false>(t, a, gs, i, in ? n : 0);
     }
   }
   if (bad) atomicCAS(status, 0, SOMA_ERR_NONFINITE);

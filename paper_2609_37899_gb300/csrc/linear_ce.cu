@@ -23,6 +23,8 @@
 #include <atomic>
 #include <cmath>
 
+#define SOMA_CHECK_FILE 8
+#include "checked.cuh"
 #include "numeric.cuh"
 #include "pdl.cuh"
 #include "soma_api.h"
@@ -65,6 +67,10 @@ __host__ __device__ constexpr bool is_demb(int kind) { return kind == kDemb || k
 __host__ __device__ constexpr bool admits_late(int kind) {
   return kind == kDh || kind == kDhSums || kind == kStats;
 }
+
+// rows_kernel leaves the largest |dloss| of each of its blocks, and every
+// epilogue warp of grad reads them all while its first products run.
+constexpr int64_t kMostTops = 1024;
 
 // What a row of the backward call takes part with; y = -1: no part.  The
 // entry of G at the target is by far the row's largest, and its rounding to 16
@@ -348,8 +354,14 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         }
         if (rank == 0 && lane == 0) tc::mbar_arrive_expect_tx(&sh.full[slot], bytes);
         __syncwarp();
-        if (copies) {
-          const int kx = k * tc::kDepth;
+        const int kx = k * tc::kDepth;
+        // a box starts inside its matrix's tiles, on 16 bytes, and fits the stage
+        if (copies &&
+            SOMA_CHECK(r0 % 8 == 0 && r0 >= 0 && kx >= 0 && k < w.k_stages &&
+                           s.m < w.m_tiles && s.n < w.n_tiles &&
+                           slot * kStageBytes + lane * tc::kBoxBytes +
+                                   (mn ? tc::kBoxBytes : kOperandBytes) <= kStages * kStageBytes,
+                       status)) {
           tc::tile_g2s_pair(stages + slot * kStageBytes + lane * tc::kBoxBytes, map,
                             mn ? r0 : kx, y0 + (mn ? kx : r0), tc::leader_addr(&sh.full[slot]));
         }
@@ -381,7 +393,10 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         const uint32_t a = tc::smem_u32(stages + slot * kStageBytes);
         const uint32_t a_lo = tc::desc_lo(a, a_mn(KIND));
         const uint32_t b_lo = tc::desc_lo(a + kOperandBytes, b_mn(KIND));
-        if (tc::elect_one()) {
+        if (tc::elect_one() &&
+            SOMA_CHECK(buf * kTile + w.tile_n <= 512 &&
+                           (slot + 1) * kStageBytes <= kStages * kStageBytes,
+                       status)) {
 #pragma unroll
           for (int j = 0; j < tc::kDepth / 16; ++j)
             tc::mma_f16_ss_pair(d, a_lo + j * tc::desc_step(a_mn(KIND)),
@@ -427,7 +442,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
       if (KIND == kStats && s.first) {
         top = -INFINITY;
         sum = 0.f;
-        y = live ? w.targets[m] : -1;
+        y = live && SOMA_CHECK(m >= 0, status) ? w.targets[m] : -1;
       }
       if (KIND == kGrad || KIND == kDh) {
         info = {0.f, 0.f, 0.f, -1};
@@ -444,6 +459,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         }
       };
       if (KIND == kDh) {
+        if (!SOMA_CHECK(info.y < (int64_t)w.k_stages * tc::kDepth, status)) info.y = -1;
         e_row = static_cast<const T*>(w.emb) + (info.y < 0 ? 0 : info.y) * w.emb_stride;
         fetch_e((int64_t)s.n * w.tile_n + half * (w.tile_n / 2));
       }
@@ -462,6 +478,9 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
       for (int c = 0; c < kHalf; c += 32) {
         const int64_t n = n0 + c;
         if (n >= n_end || m0 >= w.M) break;  // nothing there (the whole warp)
+        if (!SOMA_CHECK(buf * kTile + half * half_n + c + 32 <= 512 && quarter * 32 + 32 <= 128,
+                        status))
+          break;
         tc::tmem_wait_ld32(next);
         float x[32];
 #pragma unroll
@@ -473,7 +492,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             float v = 0.f;
 #pragma unroll
             for (int j = 0; j < 32; ++j) v = j == hit ? x[j] : v;
-            if (y < n_end) w.own[m] = v;
+            if (y < n_end && SOMA_CHECK(m >= 0 && m < w.M, status)) w.own[m] = v;
           }
           if (n + 32 > n_end) {
 #pragma unroll
@@ -507,7 +526,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                 x[j] = g * (j == at ? info.rest : p);
                 rest = j == at ? x[j] - to_f32(from_f32<T>(x[j])) : rest;
               }
-              w.info[m].rest = rest;
+              if (SOMA_CHECK(m >= 0 && m < w.M, status)) w.info[m].rest = rest;
             } else {
 #pragma unroll
               for (int j = 0; j < 32; ++j) x[j] = g * tc::ex2(fmaf(x[j], kLog2e, -info.lse2));
@@ -551,7 +570,9 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
 #pragma unroll
               for (int k = 0; k < 8; ++k)
                 rest[k] = x[8 * j + k] - to_f32(from_f32<T>(x[8 * j + k]));
-              if (n + 8 * j < w.N) store8(q + 8 * j, rest);
+              if (n + 8 * j < w.N &&
+                  SOMA_CHECK(n + 8 * j + 8 <= w.out_stride && m < w.low, status))
+                store8(q + 8 * j, rest);
             }
           }
         }
@@ -579,6 +600,10 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
           __syncwarp();
           const int rows = w.M - m0 < 32 ? (int)(w.M - m0) : 32;
           const int cols = n_end - bx < 64 ? (int)(n_end - bx) : 64;
+          if (!SOMA_CHECK(m0 >= 0 && rows >= 0 && m0 + rows <= w.M && bx >= 0 && cols >= 0 &&
+                              bx + cols <= w.N,
+                          status))
+            continue;
           store_box(static_cast<T*>(w.out) + m0 * w.out_stride + bx, w.out_stride, box, rows, cols,
                     lane);
           __syncwarp();
@@ -586,7 +611,10 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         }
         tc::fence_async_smem();
         __syncwarp();
-        if (lane == 0) {
+        if (lane == 0 &&
+            SOMA_CHECK(m0 >= 0 && m0 < w.M && bx >= 0 && bx < w.N && bx % 8 == 0 &&
+                           (!sums(KIND) || (s.part >= 0 && s.part < w.groups)),
+                       status)) {
           if (!sums(KIND)) tc::tile_s2g(&map_out, bx, (int)m0, box);
           else if (w.add) tc::tile_add_s2g(&map_out, bx, s.part * w.slot_rows + (int)m0, box);
           else tc::tile_s2g(&map_out, bx, s.part * w.slot_rows + (int)m0, box);
@@ -597,7 +625,8 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
       __syncwarp();
       if (lane == 0) tc::mbar_arrive_cluster(empty_bar[buf]);
       ++n_acc;
-      if (KIND == kStats && s.last && live)
+      if (KIND == kStats && s.last && live &&
+          SOMA_CHECK(m >= 0 && m < w.M && s.part >= 0 && s.part < w.splits, status))
         w.partial[m * 2 * w.splits + 2 * s.part + half] = make_float2(top, sum);
     }
     if (KIND != kStats && lane == 0) tc::bulk_wait();
@@ -634,7 +663,8 @@ join_kernel(const float2* partial, int parts, const float* own, const T* h, int6
   // its own wait, and CTAs that find room next to it compute this meanwhile
   // (from L2, where what earlier kernels wrote is)
   const int64_t y = __ldcg(reinterpret_cast<const long long*>(targets) + n);
-  const bool has_target = y != ignore && y >= 0 && y < vocab;
+  const bool has_target = y != ignore && y >= 0 && y < vocab &&
+                          SOMA_CHECK(hs >= dim && es >= dim && hs % 8 == 0 && es % 8 == 0, status);
   float logit = 0.f;
   if (has_target) {
     const T* a = h + n * hs;
@@ -723,7 +753,7 @@ template <typename T>
 __global__ void __launch_bounds__(256)
 rows_kernel(const T* h, const T* emb, soma_linear_ce_dims d, const int64_t* targets, int64_t ignore,
             const float* lse, const float* dloss, RowInfo* info, T* copy, int64_t cs, int halves,
-            float* top) {
+            float* top, int* status) {
   __shared__ int largest;
   if (threadIdx.x == 0) largest = 0;
   __syncthreads();
@@ -738,6 +768,7 @@ rows_kernel(const T* h, const T* emb, soma_linear_ce_dims d, const int64_t* targ
     const T* e = emb + (live ? y : 0) * d.emb_stride;
     float logit = 0.f;
     for (int64_t j = lane * 8; j < cs; j += 256) {
+      if (!SOMA_CHECK(j + 8 <= cs && n >= 0 && n < d.rows, status)) break;
       union {
         uint4 u;
         T t[8];
@@ -767,19 +798,20 @@ rows_kernel(const T* h, const T* emb, soma_linear_ce_dims d, const int64_t* targ
     }
   }
   __syncthreads();
-  if (threadIdx.x == 0) top[1 + blockIdx.x] = __int_as_float(largest);
+  if (threadIdx.x == 0 && SOMA_CHECK(blockIdx.x < kMostTops, status))
+    top[1 + blockIdx.x] = __int_as_float(largest);
 }
 
 // A matrix copied to rows of cs elements, zeros after the first dim; eight
 // elements per thread.
 template <typename T>
 __global__ void __launch_bounds__(256)
-pack_kernel(const T* x, int64_t xs, int64_t rows, int64_t dim, T* copy, int64_t cs) {
+pack_kernel(const T* x, int64_t xs, int64_t rows, int64_t dim, T* copy, int64_t cs, int* status) {
   admit_successor();
   after_predecessor();
   const int64_t at = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8;
   const int64_t n = at / cs, j = at - n * cs;
-  if (n < rows)
+  if (n < rows && SOMA_CHECK(at >= 0 && at + 8 <= rows * cs && j + 8 <= cs, status))
     *reinterpret_cast<uint4*>(copy + at) = row_piece(x + n * xs, j, dim, xs % 8 == 0);
 }
 
@@ -788,7 +820,7 @@ pack_kernel(const T* x, int64_t xs, int64_t rows, int64_t dim, T* copy, int64_t 
 template <typename T>
 __global__ void __launch_bounds__(128)
 sums_kernel(const float* acc, int64_t acc_stride, int used, const __grid_constant__ Work w,
-            const RowInfo* info, T* out, int64_t stride, int vec) {
+            const RowInfo* info, T* out, int64_t stride, int vec, int* status) {
   after_predecessor();
   admit_successor();  // only now: the product of demb may follow
   const int64_t n = blockIdx.x;
@@ -802,6 +834,9 @@ sums_kernel(const float* acc, int64_t acc_stride, int used, const __grid_constan
   if (info) r = info[n];
   const T* e = static_cast<const T*>(w.emb) + (r.y < 0 ? 0 : r.y) * w.emb_stride;
   const int64_t j = ((int64_t)blockIdx.y * 128 + threadIdx.x) * 4;
+  if (!SOMA_CHECK(n < w.M && used >= 1 && used <= kPairs && (j >= w.N || j + 4 <= acc_stride),
+                  status))
+    return;
   if (j < w.N) {
     float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
     if (r.y >= 0) {
@@ -913,9 +948,7 @@ bool copied(int64_t stride, int64_t rows, bool backward) {
   return stride % 8 != 0 || (stride % 16 != 0 && rows >= (backward ? 700 : 2000));
 }
 
-// Blocks of rows_kernel.  Each leaves its largest |dloss|, and every epilogue
-// warp of grad reads them all while its first products run.
-constexpr int64_t kMostTops = 1024;
+// Blocks of rows_kernel.
 unsigned row_blocks(const soma_linear_ce_dims& d) {
   const int64_t n = ceil_div(d.rows, 8);
   return (unsigned)(n < kMostTops ? n : kMostTops);
@@ -930,6 +963,7 @@ struct Plan {
   bool copy_h, copy_emb;
   size_t h, emb, partial, own;   // offsets; h, emb: copies
   size_t g, info, dh_acc, demb_acc, top, total;
+  Gaps gaps;                     // of the checked build
 };
 
 // The backward call's pieces: as few as G's share of the workspace allows, or
@@ -977,8 +1011,9 @@ Plan plan(soma_linear_ce_dims d, bool backward) {
   Plan p = {};
   size_t at = 0;
   const auto take = [&](size_t bytes) {
-    const size_t o = at;
-    at += round256(bytes);
+    p.gaps.off[p.gaps.n++] = at;
+    const size_t o = at + kGuard;
+    at = o + round256(bytes);
     return o;
   };
   if (!d.rows) d.rows = 1;
@@ -1030,7 +1065,8 @@ Plan plan(soma_linear_ce_dims d, bool backward) {
     }
     p.top = take((1 + kMostTops) * 4);
   }
-  p.total = at;
+  p.gaps.off[p.gaps.n++] = at;
+  p.total = at + kGuard;
   return p;
 }
 
@@ -1041,10 +1077,11 @@ constexpr int dtype_of() { return std::is_same<T, __half>::value ? SOMA_FP16 : S
 
 // x copied to rows of a multiple of 64 elements; *stride becomes theirs.
 template <typename T>
-const T* pack(const T* x, int64_t rows, int64_t dim, int64_t* stride, T* copy, cudaStream_t st) {
+const T* pack(const T* x, int64_t rows, int64_t dim, int64_t* stride, T* copy, int* status,
+              cudaStream_t st) {
   const int64_t cs = round64(dim);
   const cudaError_t e = launch_overlapped(pack_kernel<T>, (unsigned)ceil_div(rows * cs, 256 * 8),
-                                          256, 0, st, x, *stride, rows, dim, copy, cs);
+                                          256, 0, st, x, *stride, rows, dim, copy, cs, status);
   *stride = cs;
   return e == cudaSuccess ? copy : nullptr;
 }
@@ -1075,8 +1112,9 @@ cudaError_t forward(const Plan& p, const T* h, const T* emb, const soma_linear_c
                     const int64_t* targets, int64_t ignore, float* loss, float* lse, uint8_t* ws,
                     int* status, cudaStream_t st) {
   int64_t hs = d.h_stride, es = d.emb_stride;
-  if (p.copy_h) h = pack(h, d.rows, d.dim, &hs, reinterpret_cast<T*>(ws + p.h), st);
-  if (p.copy_emb) emb = pack(emb, d.vocab, d.dim, &es, reinterpret_cast<T*>(ws + p.emb), st);
+  if (p.copy_h) h = pack(h, d.rows, d.dim, &hs, reinterpret_cast<T*>(ws + p.h), status, st);
+  if (p.copy_emb)
+    emb = pack(emb, d.vocab, d.dim, &es, reinterpret_cast<T*>(ws + p.emb), status, st);
   if (!h || !emb) return cudaErrorLaunchFailure;
   CUtensorMap ma, mb;
   if (!make_tile_map(&ma, h, dtype_of<T>(), d.rows, d.dim, hs, box_rows(d.rows)) ||
@@ -1124,9 +1162,10 @@ cudaError_t backward(const Plan& p, const T* h, const T* emb, const soma_linear_
                         (size_t)p.dh_slots * ceil_div(d.rows, kTile) * kTile * p.acc_stride * 4, st);
   if (e == cudaSuccess)
     e = launch_overlapped(rows_kernel<T>, row_blocks(d), 256, 0, st, h, emb, d, targets, ignore,
-                          lse, dloss, info, copy, cs, (int)p.halves, top);
+                          lse, dloss, info, copy, cs, (int)p.halves, top, status);
   if (e != cudaSuccess) return e;
-  if (p.copy_emb) emb = pack(emb, d.vocab, d.dim, &es, reinterpret_cast<T*>(ws + p.emb), st);
+  if (p.copy_emb)
+    emb = pack(emb, d.vocab, d.dim, &es, reinterpret_cast<T*>(ws + p.emb), status, st);
   if (!emb) return cudaErrorLaunchFailure;
   const bool many = p.piece < d.vocab;
   const bool dh_tiled = dhs % 8 == 0 && aligned(dh, 16);
@@ -1195,7 +1234,7 @@ cudaError_t backward(const Plan& p, const T* h, const T* emb, const soma_linear_
         e = launch_overlapped(sums_kernel<T>, dim3((unsigned)d.rows, (unsigned)ceil_div(d.dim, 512)),
                               128, 0, st, dh_acc, p.acc_stride,
                               many ? (int)p.dh_slots : 0, w, info, dh, dhs,
-                              dhs % 4 == 0 && aligned(dh, 8));
+                              dhs % 4 == 0 && aligned(dh, 8), status);
     } else {
       w.out = dh_tiled ? nullptr : dh;
       w.out_stride = dhs;
@@ -1211,7 +1250,7 @@ cudaError_t backward(const Plan& p, const T* h, const T* emb, const soma_linear_
         e = launch_overlapped(sums_kernel<T>, dim3((unsigned)d.vocab, (unsigned)ceil_div(d.dim, 512)),
                               128, 0, st, demb_acc,
                               p.acc_stride, 0, w, nullptr, demb, des,
-                              des % 4 == 0 && aligned(demb, 8));
+                              des % 4 == 0 && aligned(demb, 8), status);
     } else {
       w.out = demb_tiled ? nullptr : demb + v0 * des;
       w.out_stride = des;
@@ -1250,14 +1289,16 @@ int soma_linear_ce_forward(const void* h, const void* emb, soma_linear_ce_dims d
   if (!status) return SOMA_ERR_CUDA;
   uint8_t* ws = static_cast<uint8_t*>(workspace);
   const cudaStream_t st = (cudaStream_t)stream;
+  if (gaps_fill(p.gaps, ws, st) != cudaSuccess) return SOMA_ERR_CUDA;
   trace_begin(SOMA_TRACE_LINEAR_CE, st);
-  const cudaError_t e =
+  cudaError_t e =
       d.dtype == SOMA_BF16
           ? forward(p, static_cast<const __nv_bfloat16*>(h), static_cast<const __nv_bfloat16*>(emb),
                     d, targets, ignore_index, loss, lse, ws, status, st)
           : forward(p, static_cast<const __half*>(h), static_cast<const __half*>(emb), d, targets,
                     ignore_index, loss, lse, ws, status, st);
   trace_end(SOMA_TRACE_LINEAR_CE, st);
+  if (e == cudaSuccess) e = gaps_check(p.gaps, ws, status, st);
   return e == cudaSuccess ? SOMA_OK : SOMA_ERR_CUDA;
 }
 
@@ -1279,8 +1320,9 @@ int soma_linear_ce_backward(const void* h, const void* emb, soma_linear_ce_dims 
   if (!status) return SOMA_ERR_CUDA;
   uint8_t* ws = static_cast<uint8_t*>(workspace);
   const cudaStream_t st = (cudaStream_t)stream;
+  if (gaps_fill(p.gaps, ws, st) != cudaSuccess) return SOMA_ERR_CUDA;
   trace_begin(SOMA_TRACE_LINEAR_CE, st);
-  const cudaError_t e =
+  cudaError_t e =
       d.dtype == SOMA_BF16
           ? backward(p, static_cast<const __nv_bfloat16*>(h), static_cast<const __nv_bfloat16*>(emb),
                      d, targets, ignore_index, lse, dloss, static_cast<__nv_bfloat16*>(dh),
@@ -1289,6 +1331,7 @@ int soma_linear_ce_backward(const void* h, const void* emb, soma_linear_ce_dims 
                      ignore_index, lse, dloss, static_cast<__half*>(dh), dh_stride,
                      static_cast<__half*>(demb), demb_stride, ws, status, st);
   trace_end(SOMA_TRACE_LINEAR_CE, st);
+  if (e == cudaSuccess) e = gaps_check(p.gaps, ws, status, st);
   return e == cudaSuccess ? SOMA_OK : SOMA_ERR_CUDA;
 }
 

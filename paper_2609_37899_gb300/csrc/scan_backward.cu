@@ -6,6 +6,8 @@
 // segment's factors take and so at most 12 warps an SM: 32 x 2048 x 1376 in
 // bf16 takes 325 us (5.1 TB/s), 1 x 32768 x 960, read twice, 167 us.  With 128
 // registers (16 warps) they spill: 371 and 240 us.
+#define SOMA_CHECK_FILE 10
+#include "checked.cuh"
 #include "scan_common.cuh"
 
 namespace soma {
@@ -53,6 +55,7 @@ backward_kernel(const T* __restrict__ gates, const __grid_constant__ Scan s,
       if (t >= begin && t + kSegment <= stop) {
 #pragma unroll
         for (int j = 0; j < kSegment; ++j, p += s.gs.t, q += s.hs.t) {
+          if (!SOMA_CHECK(inside(s, b, t + j, 1, at_ch, 1), s.status)) continue;
 #pragma unroll
           for (int g = 0; g < 4; ++g) next[j][g] = p[g * s.gs.g];
           next[j][4] = *q;
@@ -60,14 +63,16 @@ backward_kernel(const T* __restrict__ gates, const __grid_constant__ Scan s,
       } else {
 #pragma unroll
         for (int j = 0; j < kSegment; ++j) {
-          const bool there = t >= begin && t + j < stop;
+          const bool there = t >= begin && t + j < stop &&
+                             SOMA_CHECK(inside(s, b, t + j, 1, at_ch, 1), s.status);
 #pragma unroll
           for (int g = 0; g < 4; ++g)
             next[j][g] = there ? p[j * s.gs.t + g * s.gs.g] : from_f32<T>(0.f);
           next[j][4] = there ? q[j * s.hs.t] : from_f32<T>(0.f);
         }
       }
-      next_mark = t >= begin && t < stop
+      next_mark = t >= begin && t < stop &&
+                          SOMA_CHECK(t % kSegment == 0 && inside(s, b, t, 1, at_ch, 1), s.status)
                       ? s.marks[(b * marks + t / kSegment) * s.d.dim + at_ch] : 0.f;
     };
     fetch(t0);
@@ -128,6 +133,7 @@ backward_kernel(const T* __restrict__ gates, const __grid_constant__ Scan s,
         const float dc = add[j] + in[0];
         in[0] = RAGGED ? apply(f[j], 0.f, dc) : f[j] * dc;
         if (live < kSegment && t0 + j >= end) continue;
+        if (!SOMA_CHECK(inside(s, b, t0 + j, 1, ch, 1), s.status)) continue;
         const bool dead = live < kSegment && j >= live;  // an infinite dc times 0 is no gradient
         w[0] = from_f32<T>(dead ? 0.f : dc * ki[j]);
         w[s.ds.g] = from_f32<T>(dead ? 0.f : dc * kf[j]);
@@ -178,13 +184,18 @@ backward_tiled_kernel(const __grid_constant__ Maps maps, const __grid_constant__
 
     const auto fill = [&](int64_t round) {  // warp 0
       if (!ring_may_fill(ring)) return;
+      const int t = (int)(begin + (MAPS ? rounds - 1 - round : round) * rows);
+      if (!SOMA_CHECK(ch0 % kBlock == 0 && inside(s, b, t, 1, ch0, 1) && filled < depth &&
+                          in_dynamic(raw, stages + (size_t)filled * stage_elems,
+                                     stage_elems * sizeof(T)),
+                      s.status))
+        return;
       ++fills;
       const int to = filled;
       filled = filled + 1 == depth ? 0 : filled + 1;
       if (lane == 0) tc::mbar_arrive_expect_tx(&ring.full[to], stage_elems * sizeof(T));
       __syncwarp();
       if (lane < 5) {
-        const int t = (int)(begin + (MAPS ? rounds - 1 - round : round) * rows);
         box_g2s(stages + (size_t)to * stage_elems + lane * gate, &maps.in[lane], ch0,
                 maps.t_inner ? t : (int)b, maps.t_inner ? (int)b : t, &ring.full[to]);
       }
@@ -199,7 +210,8 @@ backward_tiled_kernel(const __grid_constant__ Maps maps, const __grid_constant__
 
     const auto mark_at = [&](int64_t t) {
       float2 x = make_float2(0.f, 0.f);
-      if (on && t >= begin && t < stop)
+      if (on && t >= begin && t < stop &&
+          SOMA_CHECK(t % kSegment == 0 && inside(s, b, t, 1, ch, 2), s.status))
         x = *reinterpret_cast<const float2*>(s.marks + (b * marks + t / kSegment) * s.d.dim + ch);
       return two(x.x, x.y);
     };
@@ -295,7 +307,11 @@ backward_tiled_kernel(const __grid_constant__ Maps maps, const __grid_constant__
         // each warp stores its own steps: no barrier of the CTA
         tc::fence_async_smem();
         __syncwarp();
-        if (lane == 0 && t0 < end) {
+        if (lane == 0 && t0 < end &&
+            SOMA_CHECK(inside(s, b, t0, 1, ch0, 1) &&
+                           in_dynamic(raw, p - 2 * lane, 3 * (size_t)gate * sizeof(T) +
+                                                             kSegment * kBlock * sizeof(T)),
+                       s.status)) {
           for (int g = 0; g < 4; ++g)
             box_s2g(&maps.out[g], ch0, maps.t_inner ? (int)t0 : (int)b,
                     maps.t_inner ? (int)b : (int)t0, p - 2 * lane + g * gate);
@@ -413,7 +429,7 @@ extern "C" int soma_scan_backward(const void* gates, soma_scan_strides gate_stri
   if (d.steps > 0 && (!gates || !dh || !dgates || !checkpoints)) return SOMA_ERR_INVALID_ARG;
   if (overlap(dc_last, dc0, d)) return SOMA_ERR_INVALID_ARG;
   const size_t need = backward_workspace(d);
-  if (need && (!workspace || !aligned(workspace, 16) || workspace_bytes < need))
+  if (need && (!workspace || !aligned(workspace, 16) || workspace_bytes < guarded(need)))
     return SOMA_ERR_WORKSPACE;
   dh_strides.g = 0;
   Scan s = {};
@@ -424,15 +440,17 @@ extern "C" int soma_scan_backward(const void* gates, soma_scan_strides gate_stri
   s.lengths = lengths;
   s.resets = resets;
   s.marks = const_cast<float*>(checkpoints);
-  s.maps = static_cast<float2*>(workspace);
+  if (need) s.maps = reinterpret_cast<float2*>(static_cast<uint8_t*>(workspace) + kGuard);
   const cudaStream_t st = (cudaStream_t)stream;
-  int* status = status_ptr();
+  int* status = s.status = status_ptr();
   if (!status) return SOMA_ERR_CUDA;
+  if (need && gaps_fill(gaps_around(need), workspace, st) != cudaSuccess) return SOMA_ERR_CUDA;
   trace_begin(SOMA_TRACE_SCAN, st);
-  const cudaError_t e =
+  cudaError_t e =
       dtype == SOMA_FP32   ? backward<float>(gates, s, dh, dc_last, dgates, dc0, status, st)
       : dtype == SOMA_BF16 ? backward<__nv_bfloat16>(gates, s, dh, dc_last, dgates, dc0, status, st)
                            : backward<__half>(gates, s, dh, dc_last, dgates, dc0, status, st);
   trace_end(SOMA_TRACE_SCAN, st);
+  if (need && e == cudaSuccess) e = gaps_check(gaps_around(need), workspace, status, st);
   return e == cudaSuccess ? SOMA_OK : SOMA_ERR_CUDA;
 }

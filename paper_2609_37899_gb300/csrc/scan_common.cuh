@@ -178,6 +178,7 @@ struct Scan {
   int64_t chunks;    // of the steps, `chunk` steps each
   int64_t chunk;
   float2* maps;      // [batch][chunks][dim]: (A, B) of the chunks
+  int* status;
   int32_t depth;     // stages of the ring (tiled)
 };
 
@@ -185,6 +186,13 @@ __device__ __forceinline__ int64_t length_of(const Scan& s, int64_t b) {
   if (!s.lengths) return s.d.steps;
   const int64_t n = s.lengths[b];
   return n < 0 ? 0 : (n < s.d.steps ? n : s.d.steps);
+}
+
+// What the checked build asks of an access: steps [t, t + n) of sequence b,
+// channels [ch, ch + v).
+__device__ __forceinline__ bool inside(const Scan& s, int64_t b, int64_t t, int64_t n, int64_t ch,
+                                       int v) {
+  return b >= 0 && b < s.d.batch && t >= 0 && t + n <= s.d.steps && ch >= 0 && ch + v <= s.d.dim;
 }
 
 // V adjacent elements as one register of bits.
@@ -324,7 +332,7 @@ __device__ __forceinline__ void over_chunks(const Scan& s, int64_t b, int64_t ch
   for (int64_t j = first; j < last; ++j) {
     const int64_t k = REVERSE ? to - 1 - j : from + j;
     Map<V> x = identity<V>();
-    if (on) {
+    if (on && SOMA_CHECK(k >= 0 && k < s.chunks && inside(s, b, 0, 0, ch, V), s.status)) {
       const float2* p = s.maps + (b * s.chunks + k) * s.d.dim + ch;
 #pragma unroll
       for (int v = 0; v < V; ++v) {
@@ -342,6 +350,7 @@ __device__ __forceinline__ void over_chunks(const Scan& s, int64_t b, int64_t ch
 template <int V>
 __device__ __forceinline__ void write_map(const Scan& s, int64_t b, int64_t k, int64_t ch,
                                           const Map<V>& m) {
+  if (!SOMA_CHECK(k >= 0 && k < s.chunks && inside(s, b, 0, 0, ch, V), s.status)) return;
   float2* p = s.maps + (b * s.chunks + k) * s.d.dim + ch;
 #pragma unroll
   for (int v = 0; v < V; ++v) p[v] = make_float2(m.a[v], m.b[v]);
@@ -417,6 +426,13 @@ __device__ __forceinline__ Two apply2(Two a, Two b, Two c) {
   split(b, b0, b1);
   split(c, c0, c1);
   return two(apply(a0, b0, c0), apply(a1, b1, c1));
+}
+
+// The bytes [at, at + n) of the CTA's dynamic shared memory.
+__device__ __forceinline__ bool in_dynamic(const void* raw, const void* at, size_t n) {
+  uint32_t size;
+  asm("mov.u32 %0, %%dynamic_smem_size;" : "=r"(size));
+  return tc::smem_u32(at) >= tc::smem_u32(raw) && tc::smem_u32(at) + n <= tc::smem_u32(raw) + size;
 }
 
 struct Ring {
@@ -543,10 +559,16 @@ inline Shape shape(const soma_scan_dims& d, int V, int most, int fit, double joi
   return f;
 }
 
-// Workspace of a call cut like this: its chunks' maps.
+// Workspace of a call cut like this: its chunks' maps (the checked build's
+// canary gaps go around it).
 inline size_t maps_bytes(const soma_scan_dims& d, const Shape& f) {
   return f.chunks > 1 ? (size_t)d.batch * f.chunks * d.dim * sizeof(float2) : 0;
 }
+
+inline size_t guarded(size_t need) {
+  return need && kGuard ? (need + 255) / 256 * 256 + 2 * kGuard : need;
+}
+inline Gaps gaps_around(size_t need) { return {2, {0, guarded(need) - kGuard}}; }
 
 inline void put(const Shape& f, Scan* s) {
   s->blocks = f.blocks;

@@ -11,6 +11,8 @@
 // Warps of a CTA and CTAs of an SM, those two sizes: 4 and 5 186 and 103 us,
 // 3 and 7 213 and 108, 4 and 6 202 and 108, 5 and 5 229 and 113, 6 and 4 212
 // and 115, 8 and 3 196 and 112.
+#define SOMA_CHECK_FILE 9
+#include "checked.cuh"
 #include "scan_common.cuh"
 
 namespace soma {
@@ -59,14 +61,16 @@ forward_kernel(const T* __restrict__ gates, const __grid_constant__ Scan s, T* _
 #pragma unroll
         for (int j = 0; j < kSegment; ++j, p += s.gs.t)
 #pragma unroll
-          for (int g = 0; g < kGates; ++g) next[j][g] = p[g * s.gs.g];
+          for (int g = 0; g < kGates; ++g)
+            if (SOMA_CHECK(inside(s, b, t + j, 1, at_ch, 1), s.status)) next[j][g] = p[g * s.gs.g];
       } else {
 #pragma unroll
         for (int j = 0; j < kSegment; ++j)
 #pragma unroll
           for (int g = 0; g < kGates; ++g)
-            next[j][g] = (!MAPS || t >= begin) && t + j < stop ? p[j * s.gs.t + g * s.gs.g]
-                                                               : from_f32<T>(0.f);
+            next[j][g] = (!MAPS || t >= begin) && t + j < stop &&
+                                 SOMA_CHECK(inside(s, b, t + j, 1, at_ch, 1), s.status)
+                             ? p[j * s.gs.t + g * s.gs.g] : from_f32<T>(0.f);
       }
     };
     fetch(t0);
@@ -108,7 +112,9 @@ forward_kernel(const T* __restrict__ gates, const __grid_constant__ Scan s, T* _
       float in[1];
       join<false, RAGGED, kWarps>(shared, m, turn++, c, in);
       if (!on) continue;
-      if (s.marks && t0 < end) s.marks[(b * marks + t0 / kSegment) * s.d.dim + ch] = in[0];
+      if (s.marks && t0 < end &&
+          SOMA_CHECK(t0 % kSegment == 0 && inside(s, b, t0, 1, ch, 1), s.status))
+        s.marks[(b * marks + t0 / kSegment) * s.d.dim + ch] = in[0];
       T* p = h + b * s.hs.b + t0 * s.hs.t + ch;
 #pragma unroll
       for (int j = 0; j < kSegment; ++j, p += s.hs.t) {
@@ -116,6 +122,7 @@ forward_kernel(const T* __restrict__ gates, const __grid_constant__ Scan s, T* _
         float num, den;
         tanh_parts(in[0], num, den);
         const T y = from_f32<T>(num * rcp(den * one_exp(to_f32(o[j]))));
+        if (t0 + j < end && !SOMA_CHECK(inside(s, b, t0 + j, 1, ch, 1), s.status)) continue;
         if (live == kSegment) *p = y;
         else if (t0 + j < end) *p = j < live ? y : from_f32<T>(0.f);
       }
@@ -162,13 +169,18 @@ forward_tiled_kernel(const __grid_constant__ Maps maps, const __grid_constant__ 
 
     const auto fill = [&](int64_t round) {  // warp 0
       if (!ring_may_fill(ring)) return;
+      const int t = (int)(begin + (MAPS ? rounds - 1 - round : round) * rows);
+      if (!SOMA_CHECK(ch0 % kBlock == 0 && inside(s, b, t, 1, ch0, 1) && filled < depth &&
+                          in_dynamic(raw, stages + (size_t)filled * stage_elems,
+                                     stage_elems * sizeof(T)),
+                      s.status))
+        return;
       ++fills;
       const int to = filled;
       filled = filled + 1 == depth ? 0 : filled + 1;
       if (lane == 0) tc::mbar_arrive_expect_tx(&ring.full[to], stage_elems * sizeof(T));
       __syncwarp();
       if (lane < kGates) {
-        const int t = (int)(begin + (MAPS ? rounds - 1 - round : round) * rows);
         box_g2s(stages + (size_t)to * stage_elems + lane * gate, &maps.in[lane], ch0,
                 maps.t_inner ? t : (int)b, maps.t_inner ? (int)b : t, &ring.full[to]);
       }
@@ -228,7 +240,8 @@ forward_tiled_kernel(const __grid_constant__ Maps maps, const __grid_constant__ 
       // every warp has read the stage
       if (warp == 0 && round + depth < rounds) fill(round + depth);
       if (!MAPS && on) {
-        if (s.marks && t0 < end)
+        if (s.marks && t0 < end &&
+            SOMA_CHECK(t0 % kSegment == 0 && inside(s, b, t0, 1, ch, 2), s.status))
           *reinterpret_cast<float2*>(s.marks + (b * marks + t0 / kSegment) * s.d.dim + ch) =
               make_float2(in[0], in[1]);
         T* q = h + b * s.hs.b + t0 * s.hs.t + ch;
@@ -239,6 +252,7 @@ forward_tiled_kernel(const __grid_constant__ Maps maps, const __grid_constant__ 
           Two num, den;
           tanh_parts2(x, num, den);
           const Two y = num * rcp2(den * one_exp2(widen<T>(o[j])));
+          if (t0 + j < end && !SOMA_CHECK(inside(s, b, t0 + j, 1, ch, 2), s.status)) continue;
           if (live == kSegment) store_two(q, y);
           else if (t0 + j < end) store_two(q, j < live ? y : two(0.f));
           q += s.hs.t;
@@ -251,7 +265,8 @@ forward_tiled_kernel(const __grid_constant__ Maps maps, const __grid_constant__ 
     if (RAGGED && !MAPS && on)
       for (; t0 < end; t0 += rows)
         for (int j = 0; j < kSegment && t0 + j < end; ++j)
-          store_two(h + b * s.hs.b + (t0 + j) * s.hs.t + ch, two(0.f));
+          if (SOMA_CHECK(inside(s, b, t0 + j, 1, ch, 2), s.status))
+            store_two(h + b * s.hs.b + (t0 + j) * s.hs.t + ch, two(0.f));
     __syncwarp();
     if (MAPS) {
       if (on && warp == 0) write_map(s, b, k, ch, total);
@@ -301,6 +316,7 @@ scan_step_kernel(const T* __restrict__ gates, const __grid_constant__ Scan s,
   const int64_t at = ((int64_t)blockIdx.x * 128 + threadIdx.x) * V;
   if (at >= s.d.batch * s.d.dim) return;
   const int64_t b = at / s.d.dim, ch = at % s.d.dim;
+  if (!SOMA_CHECK(inside(s, b, 0, 1, ch, V), s.status)) return;
   const T* p = gates + b * s.gs.b + ch;
   float a[4][V], x[V], y[V];
 #pragma unroll
@@ -406,7 +422,7 @@ int64_t soma_scan_workspace_bytes(soma_scan_dims d) {
   if (!dims_ok(d)) return -1;
   if (d.batch == 0 || d.dim == 0) return 0;
   const size_t f = forward_workspace(d), b = backward_workspace(d);
-  return (int64_t)(f > b ? f : b);
+  return (int64_t)guarded(f > b ? f : b);
 }
 
 int soma_scan_forward(const void* gates, soma_scan_strides gate_strides, int dtype,
@@ -423,7 +439,7 @@ int soma_scan_forward(const void* gates, soma_scan_strides gate_strides, int dty
   if (d.steps > 0 && (!gates || !h)) return SOMA_ERR_INVALID_ARG;
   if (overlap(c0, c_last, d)) return SOMA_ERR_INVALID_ARG;
   const size_t need = forward_workspace(d);
-  if (need && (!workspace || !aligned(workspace, 16) || workspace_bytes < need))
+  if (need && (!workspace || !aligned(workspace, 16) || workspace_bytes < guarded(need)))
     return SOMA_ERR_WORKSPACE;
   h_strides.g = 0;
   Scan s = {};
@@ -435,15 +451,17 @@ int soma_scan_forward(const void* gates, soma_scan_strides gate_strides, int dty
   s.resets = resets;
   s.c_last = c_last;
   s.marks = checkpoints;
-  s.maps = static_cast<float2*>(workspace);
+  if (need) s.maps = reinterpret_cast<float2*>(static_cast<uint8_t*>(workspace) + kGuard);
   const cudaStream_t st = (cudaStream_t)stream;
-  int* status = status_ptr();
+  int* status = s.status = status_ptr();
   if (!status) return SOMA_ERR_CUDA;
+  if (need && gaps_fill(gaps_around(need), workspace, st) != cudaSuccess) return SOMA_ERR_CUDA;
   trace_begin(SOMA_TRACE_SCAN, st);
-  const cudaError_t e = dtype == SOMA_FP32   ? forward<float>(gates, s, h, status, st)
-                        : dtype == SOMA_BF16 ? forward<__nv_bfloat16>(gates, s, h, status, st)
-                                             : forward<__half>(gates, s, h, status, st);
+  cudaError_t e = dtype == SOMA_FP32   ? forward<float>(gates, s, h, status, st)
+                  : dtype == SOMA_BF16 ? forward<__nv_bfloat16>(gates, s, h, status, st)
+                                       : forward<__half>(gates, s, h, status, st);
   trace_end(SOMA_TRACE_SCAN, st);
+  if (need && e == cudaSuccess) e = gaps_check(gaps_around(need), workspace, status, st);
   return e == cudaSuccess ? SOMA_OK : SOMA_ERR_CUDA;
 }
 
@@ -461,6 +479,8 @@ int soma_scan_step(const void* gates, soma_scan_strides gate_strides, int dtype,
   s.d = d;
   s.gs = gate_strides;
   s.hs = h_strides;
+  s.status = status_ptr();
+  if (!s.status) return SOMA_ERR_CUDA;
   const cudaStream_t st = (cudaStream_t)stream;
   const bool two = dim % 2 == 0 && pairs(gates, gate_strides) && pairs(h, h_strides);
   trace_begin(SOMA_TRACE_SCAN, st);

@@ -35,58 +35,10 @@ int* soma::status_ptr() {
   return g_status_ptr[dev];
 }
 
+#ifdef SOMA_CHECKED
 namespace {
 
-constexpr int kMaxPert = 12 * 1024;  // coefficients of one expert staged in shared memory
-
-bool dims_ok(const soma_dims& d) {
-  return d.vocab == kVocab && d.embed >= 1 && d.embed <= 1024 && d.hidden >= 1 &&
-         d.hidden <= 4096;
-}
-
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
-constexpr size_t kAlign = 256;
-size_t round_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
-
-// Workspace layout: regions in order, each rounded up to 256 bytes.  The
-// checked build puts a 256-byte canary gap before every region and after
-// the last; the gaps are filled before a step and checked after it.
-#ifdef SOMA_CHECKED
-constexpr size_t kGuard = 256;
-#else
-constexpr size_t kGuard = 0;
-#endif
-constexpr int kMaxRegions = 12;
-
-struct Regions {
-  int n;
-  size_t off[kMaxRegions];
-  size_t end;
-  size_t add(size_t bytes) {
-    off[n] = end + kGuard;
-    end = off[n] + round_up(bytes);
-    return off[n++];
-  }
-  size_t total() const { return end + kGuard; }
-};
-
-#ifdef SOMA_CHECKED
 constexpr uint32_t kCanaryWord = 0x5A17C0DEu;
-
-// The canary gaps of a workspace: before each region and after the last.
-struct Gaps {
-  int n;
-  size_t off[kMaxRegions + 1];
-};
-
-Gaps gaps_of(const Regions& r) {
-  Gaps g;
-  g.n = r.n + 1;
-  for (int i = 0; i < r.n; ++i) g.off[i] = r.off[i] - kGuard;
-  g.off[r.n] = r.end;
-  return g;
-}
 
 __global__ void canary_fill_kernel(uint32_t* ws, Gaps g) {
   for (int j = threadIdx.x; j < g.n * (int)(kGuard / 4); j += blockDim.x) {
@@ -106,26 +58,75 @@ __global__ void canary_check_kernel(const uint32_t* ws, Gaps g, int* status) {
     }
   }
 }
+
+}  // namespace
 #endif
 
-cudaError_t canary_fill(const Regions& r, void* ws, cudaStream_t st) {
+cudaError_t soma::gaps_fill(const Gaps& g, void* ws, cudaStream_t st) {
 #ifdef SOMA_CHECKED
-  canary_fill_kernel<<<1, 256, 0, st>>>(static_cast<uint32_t*>(ws), gaps_of(r));
+  canary_fill_kernel<<<1, 256, 0, st>>>(static_cast<uint32_t*>(ws), g);
   return cudaGetLastError();
 #else
-  (void)r, (void)ws, (void)st;
+  (void)g, (void)ws, (void)st;
   return cudaSuccess;
 #endif
 }
 
-cudaError_t canary_check(const Regions& r, const void* ws, int* status, cudaStream_t st) {
+cudaError_t soma::gaps_check(const Gaps& g, const void* ws, int* status, cudaStream_t st) {
 #ifdef SOMA_CHECKED
-  canary_check_kernel<<<1, 256, 0, st>>>(static_cast<const uint32_t*>(ws), gaps_of(r), status);
+  canary_check_kernel<<<1, 256, 0, st>>>(static_cast<const uint32_t*>(ws), g, status);
   return cudaGetLastError();
 #else
-  (void)r, (void)ws, (void)status, (void)st;
+  (void)g, (void)ws, (void)status, (void)st;
   return cudaSuccess;
 #endif
+}
+
+namespace {
+
+constexpr int kMaxPert = 12 * 1024;  // coefficients of one expert staged in shared memory
+
+bool dims_ok(const soma_dims& d) {
+  return d.vocab == kVocab && d.embed >= 1 && d.embed <= 1024 && d.hidden >= 1 &&
+         d.hidden <= 4096;
+}
+
+bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+constexpr size_t kAlign = 256;
+size_t round_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
+
+// Workspace layout: regions in order, each rounded up to 256 bytes, with the
+// checked build's gaps (kGuard) around them.
+constexpr int kMaxRegions = kMaxGaps - 1;
+
+struct Regions {
+  int n;
+  size_t off[kMaxRegions];
+  size_t end;
+  size_t add(size_t bytes) {
+    off[n] = end + kGuard;
+    end = off[n] + round_up(bytes);
+    return off[n++];
+  }
+  size_t total() const { return end + kGuard; }
+};
+
+// The canary gaps of a workspace: before each region and after the last.
+Gaps gaps_of(const Regions& r) {
+  Gaps g;
+  g.n = r.n + 1;
+  for (int i = 0; i < r.n; ++i) g.off[i] = r.off[i] - kGuard;
+  g.off[r.n] = r.end;
+  return g;
+}
+
+cudaError_t canary_fill(const Regions& r, void* ws, cudaStream_t st) {
+  return gaps_fill(gaps_of(r), ws, st);
+}
+
+cudaError_t canary_check(const Regions& r, const void* ws, int* status, cudaStream_t st) {
+  return gaps_check(gaps_of(r), ws, status, st);
 }
 
 // Workspace of one sweep with `n_pert` probes and `n_sign` signs.  Small

@@ -20,6 +20,21 @@ int* status_ptr();
 void trace_begin(int kind, cudaStream_t stream);
 void trace_end(int kind, cudaStream_t stream);
 
+// The checked build puts a 256-byte canary gap before every region of a
+// workspace and after the last; the gaps are filled before a call and checked
+// after it.  In the default build a gap has no bytes and the two do nothing.
+#ifdef SOMA_CHECKED
+constexpr size_t kGuard = 256;
+#else
+constexpr size_t kGuard = 0;
+#endif
+constexpr int kMaxGaps = 13;
+struct Gaps {
+  int n;
+  size_t off[kMaxGaps];  // multiples of 4 bytes
+};
+cudaError_t gaps_fill(const Gaps& g, void* ws, cudaStream_t st);
+cudaError_t gaps_check(const Gaps& g, const void* ws, int* status, cudaStream_t st);
 
 // ---- tensor-core path ------------------------------------------------------
 // Geometry of one sweep on the tensor cores.  K of the gate GEMM is
