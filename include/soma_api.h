@@ -483,7 +483,12 @@ typedef struct soma_adamw_config {
   int32_t state_bits;              /* 32 or 8 */
 } soma_adamw_config;
 
-/* tensors: HOST array [n_tensors], read before the call returns; grad_scale:
+/* The configuration, t and seed among it, and the table of tensors are values of
+ * the launch: a captured step replays update t with the same random bits, so a
+ * graph serves one update.  What may change between replays is what the
+ * pointers hold.
+ *
+ * tensors: HOST array [n_tensors], read before the call returns; grad_scale:
  * device fp32 [1], or NULL for 1.  Tensors must not overlap.  No workspace.
  * One launch per 360 non-empty tensors. */
 int soma_adamw_step(const soma_adamw_tensor* tensors, int n_tensors, soma_adamw_config cfg,
@@ -509,7 +514,7 @@ int soma_adamw_step(const soma_adamw_tensor* tensors, int n_tensors, soma_adamw_
 typedef struct soma_scan_dims {
   int64_t batch; /* 0 .. 2^31 - 1 */
   int64_t steps; /* 0 .. 2^31 - 1 */
-  int64_t dim;   /* 0 .. 2^24 */
+  int64_t dim;   /* 0 .. 2^24, batch * dim up to 2^36 */
 } soma_scan_dims;
 
 /* Elements between neighbouring sequences, steps and (gate tensors) gates;
@@ -569,7 +574,12 @@ int soma_scan_step(const void* gates, soma_scan_strides gate_strides, int dtype,
  * Eq. delta).  h, emb and their gradients are of one 16-bit soma_dtype;
  * products accumulate in fp32, losses are fp32.  G is rounded to the 16-bit
  * type before it meets emb and h, scaled so that the largest |dloss| is 1
- * (fp16: 2^14).
+ * (fp16: 2^14): an entry is good to half an ulp of its type, and in fp16 to
+ * 2^-39 of the largest |dloss| where that is more, so that rows whose dloss is
+ * smaller by many powers of two have less accurate gradients.  With 128 rows or
+ * fewer demb takes what that rounding took off, too, and dh always does at the
+ * target.  Logits are the tensor cores' sums, which are cut off rather than
+ * rounded, but for the target's, which is one of fp32 multiply-adds.
  *
  * A row whose target is ignore_index has loss 0, lse 0 and no gradient; its h
  * is never used, whatever it holds.  A row with a target outside 0 .. vocab - 1

@@ -14,12 +14,12 @@
 //                         there are too few tiles to occupy the GPU otherwise;
 //                         sums_kernel rounds them
 //
-// The tensor cores bound large sizes: 16385 x 32768 x 1376 forward 860 us (1720
+// The tensor cores bound large sizes: 16385 x 32768 x 1376 forward 865 us (1710
 // TFLOP/s, the rate that the power limit lets a long run keep), 8192 x 131072 x
-// 1024 forward and backward 5.5 ms (1600); the tensor pipe is 91% busy in stats
+// 1024 forward and backward 5.6 ms (1575); the tensor pipe is 91% busy in stats
 // and 77 to 80% in the others at 4096 x 65536 x 1024.  emb's bytes bound few
 // rows (64 x 32768 x 960 forward: 18 us, 3.4 TB/s), the launches small sizes
-// (8192 x 256 x 960 forward and backward: 64 us).
+// (8192 x 256 x 960 forward and backward: 63 us).
 #include <atomic>
 #include <cmath>
 
@@ -46,9 +46,10 @@ constexpr uint32_t kOutBytes = 32 * 128;      // a warp's output box: 32 rows of
 constexpr int kThreads = 128 + 32 * kEpilogueWarps;
 constexpr size_t kSmem =                      // and what aligns the stages
     kStages * kStageBytes + kEpilogueWarps * kOutBytes + 1024;
-// Of G of one piece, at most.  Smaller pieces would stay in the 129 MB L2 but
-// make dh's sums and the launches more (8192 x 131072 x 1024, both calls: 6.4 ms
-// at 48 MB, 5.6 at 96, 5.25 at 256, 5.5 at 512).
+// Of G of one piece, at most, while a piece has kTile vocabulary entries at
+// least: above 524,288 rows G takes 512 bytes a row.  Smaller pieces would stay
+// in the 129 MB L2 but make dh's sums and the launches more (8192 x 131072 x
+// 1024, both calls: 6.4 ms at 48 MB, 5.6 at 96, 5.25 at 256, 5.5 at 512).
 constexpr size_t kPieceBytes = (size_t)256 << 20;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
@@ -204,7 +205,9 @@ struct Walk {
 // Most calls have one dloss for all rows; -dloss (1 - p) is then next to a power
 // of two and exact for small p.  Without the scaling those entries were all off
 // by the same up to 2^-8 of themselves in bf16, and demb with them (1.5 times
-// the error that its own rounding has).
+// the error that its own rounding has).  One scale serves all rows, as demb adds
+// over them: in fp16 a row whose |dloss| is far below the largest has its small
+// entries among the subnormals, 2^-39 of the largest |dloss| off at most.
 template <typename T>
 __device__ __forceinline__ float g_scale(float top) {
   const float to = std::is_same<T, __half>::value ? 16384.f : 1.f;

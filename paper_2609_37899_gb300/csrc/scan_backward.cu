@@ -4,8 +4,10 @@
 // Per element of 16 bits 10 bytes read, 8 written and half a byte of the
 // checkpoints.  Instructions bound it, with the 168 registers a thread that a
 // segment's factors take and so at most 12 warps an SM: 32 x 2048 x 1376 in
-// bf16 takes 325 us (5.1 TB/s), 1 x 32768 x 960, read twice, 167 us.  With 128
-// registers (16 warps) they spill: 371 and 240 us.
+// bf16 takes 339 us (4.9 TB/s), 1 x 32768 x 960, read twice, 172 us.  Before
+// forget gates were kept above zero and sigmoid' good relative to its size,
+// which cost 4%, with 128 registers (16 warps), where they spill: 371 and 240 us
+// against 325 and 167.
 #define SOMA_CHECK_FILE 10
 #include "checked.cuh"
 #include "scan_common.cuh"
@@ -339,7 +341,8 @@ backward_tiled_kernel(const __grid_constant__ Maps maps, const __grid_constant__
 // CTAs of two warps, or of four and half as many: the larger ones take fewer
 // chunks (1 x 32768 x 960: 183 us with two warps, 167 with four) and keep an SM
 // full where two-warp ones are too few to (32 x 2048 x 1376: 348 and 325);
-// elsewhere the smaller ones spread better (4 x 4096 x 960: 89 and 98).
+// elsewhere the smaller ones spread better (4 x 4096 x 960: 89 and 98).  All of
+// these are some 3% more now, as said at the top.
 Shape shape_of(const soma_scan_dims& d, int V, int fit) {
   const Shape a = shape(d, V, kWarps / 2, fit, kJoin), b = shape(d, V, kWarps, fit / 2, kJoin);
   return b.cost < 0.98 * a.cost ? b : a;

@@ -43,6 +43,9 @@ constexpr int kBlock = 64;   // channels of a tiled CTA: 32 lanes of two
 constexpr int kSms = 152;
 constexpr float kLog2e = 1.4426950408889634f;
 
+// The special function unit's reciprocal and power of two: within an ulp or two
+// of the rounded ones.  h, the states and the gradients are allowed 32 half
+// ulps of their terms per step for all of it.
 __device__ __forceinline__ float rcp(float x) {
   float y;
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
