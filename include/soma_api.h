@@ -264,6 +264,19 @@ typedef struct soma_first_order_times {
 /* As soma_trace_read, for these. */
 int soma_trace_read_first_order(soma_first_order_times* out, int reset);
 
+/* And the operators of the attention expert and of answering. */
+enum {
+  SOMA_TRACE_LINEAR_ATTN = 8, /* soma_linear_attn_forward, _backward and _step */
+  SOMA_TRACE_DROPOUT = 9,
+  SOMA_TRACE_SAMPLE = 10,
+  SOMA_TRACE_SEQUENCE = 3
+};
+typedef struct soma_sequence_times {
+  double ms[SOMA_TRACE_SEQUENCE];
+  int64_t calls[SOMA_TRACE_SEQUENCE];
+} soma_sequence_times;
+int soma_trace_read_sequence(soma_sequence_times* out, int reset);
+
 /* Test exports (bit-exactness of the generator the kernels use).
  * soma_debug_philox: out4[j] = Philox4x32-10(ctr4[j], key = seed halves) for
  *   j < count; ctr4 and out4 are device uint32 [count][4].
@@ -615,6 +628,151 @@ int soma_linear_ce_backward(const void* h, const void* emb, soma_linear_ce_dims 
                             const float* dloss, void* dh, int64_t dh_stride, void* demb,
                             int64_t demb_stride, void* workspace, size_t workspace_bytes,
                             void* stream);
+
+/* Linear attention with a decay for each head: the recurrence with a matrix for
+ * a state.  For sequence b, head h and step t, with the decay l_h =
+ * exp(log_decay[h]):
+ *   S_t = l_h S_{t-1} + k_t v_t^T  [key_dim][value_dim];   o_t = scale S_t^T q_t
+ * and so o_t = scale (sum_{j<=t} l^{t-j} <q_t, k_j> v_j + l^{t+1} S_{-1}^T q_t).
+ * States are fp32 [batch][heads][key_dim][value_dim]; q, k, v, o and their
+ * gradients are of one soma_dtype.  log_decay: fp32 [heads], each at most 0 and
+ * given, not learned (-infinity: a step sees itself alone); a head whose decay
+ * is above 0 or NaN has NaN outputs, and SOMA_ERR_NONFINITE is recorded.
+ *
+ * lengths and resets are as in the gated linear recurrence: sequence b ends
+ * after lengths[b] steps (clamped to 0 .. steps), later steps are not read,
+ * leave the state as it is and have o = 0 and gradient 0; a step with
+ * resets[b][t] != 0 starts a document, which sees nothing before it.  Any size
+ * may be 0, but the widths.  A q, k or v that is not finite may reach every
+ * output of its sequence and head, earlier ones and other documents' too.
+ *
+ * 16-bit types run on the tensor cores where rows allow tiled copies: addresses
+ * and strides that are multiples of 16 bytes, and widths of 8 elements.  There
+ * scale l^{i-j} <q_i, k_j>, the state that a chunk of 128 steps starts from and
+ * the decayed v of a chunk are rounded to the type for the products that they
+ * enter (states that are in memory take what the rounding of v takes off, too);
+ * sums and states are fp32.  fp16: those three are scaled by powers of two to the
+ * range of the type.  Other layouts, and fp32, take kernels of fp32 arithmetic. */
+typedef struct soma_attn_dims {
+  int64_t batch; /* 0 .. 2^31 - 1 */
+  int64_t steps; /* 0 .. 2^31 - 1 */
+  int64_t heads; /* 0 .. 2^16, batch * heads up to 2^29 */
+  int32_t key_dim, value_dim; /* 1 .. 128 */
+} soma_attn_dims;
+
+/* Elements between neighbouring sequences, steps and heads; the elements of a
+ * head are adjacent.  Negative strides are invalid.  Inputs may repeat (stride
+ * 0: heads that share k and v); gradients are those of each head. */
+typedef struct soma_attn_strides {
+  int64_t b, t, h;
+} soma_attn_strides;
+
+/* Bytes of workspace of the forward (backward = 0) or the backward call (1), 0
+ * for many sizes; -1 if the sizes are invalid.  One workspace of the larger size
+ * serves both. */
+int64_t soma_linear_attn_workspace_bytes(soma_attn_dims d, int dtype, int backward);
+
+/*   q, k          [batch][steps][heads][key_dim] by q_strides, k_strides
+ *   v, o          [batch][steps][heads][value_dim] by v_strides, o_strides
+ *   s0            the state before the first step, or NULL for 0
+ *   lengths       int32 [batch] or NULL;  resets: uint8 [batch][steps] or NULL
+ *   s_last        the state after the last step, or NULL; must not overlap s0
+ *                 (SOMA_ERR_INVALID_ARG)
+ * o must not overlap an input. */
+int soma_linear_attn_forward(const void* q, soma_attn_strides q_strides, const void* k,
+                             soma_attn_strides k_strides, const void* v,
+                             soma_attn_strides v_strides, int dtype, soma_attn_dims d,
+                             const float* log_decay, float scale, const float* s0,
+                             const int32_t* lengths, const uint8_t* resets, void* o,
+                             soma_attn_strides o_strides, float* s_last, void* workspace,
+                             size_t workspace_bytes, void* stream);
+
+/* The gradients, from do (d_out) and ds_last (the gradient of s_last; NULL: 0):
+ *   dq_i = scale (sum_{j<=i} l^{i-j} <do_i, v_j> k_j + l^{i+1} S_{-1} do_i)
+ *   dk_j = scale sum_{i>=j} l^{i-j} <do_i, v_j> q_i + l^{n-1-j} dS_{n-1} v_j
+ *   dv_j = scale sum_{i>=j} l^{i-j} <q_i, k_j> do_i + l^{n-1-j} dS_{n-1}^T k_j
+ *   dS_{-1} = l^n dS_{n-1} + scale sum_i l^{i+1} q_i do_i^T
+ * within each document.  ds0 (the gradient of s0) or NULL; it must not overlap
+ * s0 or ds_last.  No gradient may overlap an input or another one. */
+int soma_linear_attn_backward(const void* q, soma_attn_strides q_strides, const void* k,
+                              soma_attn_strides k_strides, const void* v,
+                              soma_attn_strides v_strides, int dtype, soma_attn_dims d,
+                              const float* log_decay, float scale, const float* s0,
+                              const int32_t* lengths, const uint8_t* resets, const void* d_out,
+                              soma_attn_strides do_strides, const float* ds_last, void* dq,
+                              soma_attn_strides dq_strides, void* dk,
+                              soma_attn_strides dk_strides, void* dv,
+                              soma_attn_strides dv_strides, float* ds0, void* workspace,
+                              size_t workspace_bytes, void* stream);
+
+/* One token of each of d.batch running sequences (d.steps and the strides' t are
+ * unused); the states s are updated. */
+int soma_linear_attn_step(const void* q, soma_attn_strides q_strides, const void* k,
+                          soma_attn_strides k_strides, const void* v,
+                          soma_attn_strides v_strides, int dtype, soma_attn_dims d,
+                          const float* log_decay, float scale, float* s, void* o,
+                          soma_attn_strides o_strides, void* stream);
+
+/* Dropout, with the residual's addition, from the counter-based generator; no
+ * mask is stored.  For element e = row * cols + column:
+ *   y_e = residual_e + (kept_e ? x_e / (1 - p') : 0),   p' = round(65536 p) / 65536
+ * in fp32, rounded once (residual NULL: 0).  Element e takes 16 bits, half e % 2
+ * of word (e / 2) % 4 of the Philox4x32-10 block with key (seed halves) and
+ * counter (e / 8, call & 0xffffffff, call >> 32, 0x80000003), a domain disjoint
+ * from the library's others; it is kept where they are at least 65536 p'.  So the
+ * mask depends on the element's place, the seed and the call alone, not on
+ * strides or types.  call = offset + (counter ? counter[0] : 0): every call of a
+ * training step has an offset of its own, and a counter on the device, which the
+ * caller advances, gives each replay of a captured graph other masks.
+ *
+ * The gradient of x is the same call on the gradient of y without a residual (the
+ * residual's is that of y itself).  What is dropped may be anything, NaN too.
+ *   x, y, residual  [rows][cols] of a soma_dtype, rows x_stride, y_stride and
+ *                   residual_stride elements apart (>= cols); y may be x or
+ *                   residual itself, but not overlap them otherwise
+ *   rows, cols      >= 0, rows * cols up to 2^34
+ *   p               0 .. 1
+ *   counter         device uint64 [1] or NULL */
+int soma_dropout(const void* x, int64_t x_stride, const void* residual, int64_t residual_stride,
+                 void* y, int64_t y_stride, int dtype, int64_t rows, int64_t cols, double p,
+                 uint64_t seed, uint64_t offset, const uint64_t* counter, void* stream);
+
+/* Sampling: one token per row of logits, from given random numbers.  For a row
+ * with largest logit m, token v has the weight w_v = rint(2^40 exp((l_v - m) / T)),
+ * a whole number of 64 bits, so that sums of weights are exact and results do
+ * not depend on the order of additions.  Tokens are ranked by logit, equal ones
+ * by index.  Of the tokens remain, in this order,
+ *   top-k   the first top_k of the ranking (0 or less: all);
+ *   top-p   the shortest beginning of the ranking that has at least top_p of the
+ *           weight that is left, the first always (1 or more: all);
+ *   min-p   those with w_v >= min_p 2^40 (min_p above 1 counts as 1).
+ * The answer is the first token, by index, up to which the remaining weights sum
+ * to more than floor(u W), W being the sum of all that remain; logprob is
+ * log(w_v / W), to fp32, of that token.  T = 0 (and below 2^-100) gives the first
+ * token of the ranking, with logprob 0.
+ *
+ * Logits of -infinity, or so low that their weight is 0, are never chosen.  A row
+ * without an answer has token -1 and logprob NaN: one of -infinities alone (a mask
+ * that leaves nothing), and, with SOMA_ERR_NONFINITE recorded, one that holds NaN
+ * or +infinity or whose T is negative or NaN, whose top_p or min_p is NaN, or whose
+ * u is outside [0, 1).  T above 2^100 counts as 2^100. */
+typedef struct soma_sample_config {
+  float temperature; /* for all rows where the row's own are not given */
+  float top_p, min_p;
+  int32_t top_k;
+  const float* temperatures; /* device fp32 [rows] or NULL */
+  const float* top_ps;       /* device fp32 [rows] or NULL */
+  const float* min_ps;       /* device fp32 [rows] or NULL */
+  const int32_t* top_ks;     /* device int32 [rows] or NULL */
+} soma_sample_config;
+
+/*   logits   [rows][vocab] of a soma_dtype, rows `stride` elements apart (>= vocab)
+ *   u        device fp32 [rows]
+ *   tokens   device int64 [rows];  logprobs: device fp32 [rows] or NULL
+ *   rows     0 .. 2^24, vocab 1 .. 2^20.  No workspace. */
+int soma_sample(const void* logits, int64_t stride, int dtype, int64_t rows, int64_t vocab,
+                soma_sample_config cfg, const float* u, int64_t* tokens, float* logprobs,
+                void* stream);
 
 #ifdef __cplusplus
 }

@@ -38,6 +38,7 @@ class soma_dims(ctypes.Structure):
 
 TRACE_KINDS = ("gate", "head", "reduce", "update", "prep")
 TRACE_FIRST_ORDER = ("linear_ce", "scan", "adamw")
+TRACE_SEQUENCE = ("linear_attn", "dropout", "sample")
 
 
 class soma_body_dims(ctypes.Structure):
@@ -81,6 +82,21 @@ class soma_linear_ce_dims(ctypes.Structure):
                                               "emb_stride")] + [("dtype", ctypes.c_int32)]
 
 
+class soma_attn_dims(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int64) for n in ("batch", "steps", "heads")] + \
+               [(n, ctypes.c_int32) for n in ("key_dim", "value_dim")]
+
+
+class soma_attn_strides(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int64) for n in ("b", "t", "h")]
+
+
+class soma_sample_config(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_float) for n in ("temperature", "top_p", "min_p")] + \
+               [("top_k", ctypes.c_int32)] + \
+               [(n, ctypes.c_void_p) for n in ("temperatures", "top_ps", "min_ps", "top_ks")]
+
+
 DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 PROBE_KINDS = {"dense": 0, "sparse": 1}
 MAX_ACCUM = 64
@@ -91,6 +107,10 @@ class soma_kernel_times(ctypes.Structure):
 
 
 class soma_first_order_times(ctypes.Structure):
+    _fields_ = [("ms", ctypes.c_double * 3), ("calls", ctypes.c_int64 * 3)]
+
+
+class soma_sequence_times(ctypes.Structure):
     _fields_ = [("ms", ctypes.c_double * 3), ("calls", ctypes.c_int64 * 3)]
 
 
@@ -194,6 +214,19 @@ def _open(path: str):
         _sig(L, "soma_linear_ce_forward", i32, [vp, vp, cd, vp, i64, vp, vp, vp, sz, vp])
         _sig(L, "soma_linear_ce_backward", i32, [vp, vp, cd, vp, i64, vp, vp, vp, i64, vp, i64,
                                                  vp, sz, vp])
+        ad, at = soma_attn_dims, soma_attn_strides
+        _sig(L, "soma_linear_attn_workspace_bytes", i64, [ad, i32, i32])
+        _sig(L, "soma_linear_attn_forward", i32, [vp, at, vp, at, vp, at, i32, ad, vp, f32, vp, vp,
+                                                  vp, vp, at, vp, vp, sz, vp])
+        _sig(L, "soma_linear_attn_backward", i32, [vp, at, vp, at, vp, at, i32, ad, vp, f32, vp, vp,
+                                                   vp, vp, at, vp, vp, at, vp, at, vp, at, vp, vp,
+                                                   sz, vp])
+        _sig(L, "soma_linear_attn_step", i32, [vp, at, vp, at, vp, at, i32, ad, vp, f32, vp, vp, at,
+                                               vp])
+        _sig(L, "soma_dropout", i32, [vp, i64, vp, i64, vp, i64, i32, i64, i64, ctypes.c_double,
+                                      u64, u64, vp, vp])
+        _sig(L, "soma_sample", i32, [vp, i64, i32, i64, i64, soma_sample_config, vp, vp, vp, vp])
+        _sig(L, "soma_trace_read_sequence", i32, [ctypes.POINTER(soma_sequence_times), i32])
         _sig(L, "soma_checked_build", i32, [])
         _sig(L, "soma_debug_check_line", i32, [vp])
         _sig(L, "soma_debug_check_fail", i32, [vp])
@@ -378,6 +411,14 @@ def trace_read_first_order(reset: bool = True) -> dict:
     _check(lib().soma_trace_read_first_order(ctypes.byref(t), 1 if reset else 0),
            "soma_trace_read_first_order")
     return {k: (t.ms[j], int(t.calls[j])) for j, k in enumerate(TRACE_FIRST_ORDER)}
+
+
+def trace_read_sequence(reset: bool = True) -> dict:
+    """{kind: (total_ms, calls)} of the traced linear attention, dropout and sampling calls."""
+    t = soma_sequence_times()
+    _check(lib().soma_trace_read_sequence(ctypes.byref(t), 1 if reset else 0),
+           "soma_trace_read_sequence")
+    return {k: (t.ms[j], int(t.calls[j])) for j, k in enumerate(TRACE_SEQUENCE)}
 
 
 def get_status(stream=None) -> int:
@@ -888,3 +929,198 @@ class AdamW:
             self._table, len(params), cfg,
             _dev(grad_scale, torch.float32, "grad_scale", 1) if grad_scale is not None else None,
             _stream(stream)), "soma_adamw_step")
+
+
+# ---------------------------------------------------------------------------
+# Linear attention with a decay for each head, dropout, sampling.
+# ---------------------------------------------------------------------------
+
+def _here(**tensors):
+    """Refuses tensors of another device than the current one, whose stream the call goes to."""
+    index = torch.cuda.current_device()
+    for name, t in tensors.items():
+        if t is not None and t.is_cuda and t.device.index != index:
+            raise ValueError(f"{name}: on {t.device}, but the current device is cuda:{index}")
+
+
+def _attn_dims(q, v) -> soma_attn_dims:
+    if q.dim() != 4 or v.dim() != 4:
+        raise ValueError("q and v: expected [batch, steps, heads, width] tensors")
+    return soma_attn_dims(*q.shape, v.shape[3])
+
+
+def _attn_tensor(t, name, shape, dtype) -> tuple:
+    p, strides = _rows(t, name, shape, dtype)
+    return p, soma_attn_strides(*strides[:3])
+
+
+def _attn_dtype(q) -> int:
+    if q.dtype not in DTYPES:
+        raise ValueError(f"q: unsupported dtype {q.dtype}")
+    return DTYPES[q.dtype]
+
+
+def linear_attn_workspace_bytes(batch: int, steps: int, heads: int, key_dim: int, value_dim: int,
+                                dtype: torch.dtype, backward: bool = True) -> int:
+    """Bytes that linear_attn_forward needs, and linear_attn_backward with `backward`."""
+    d = soma_attn_dims(batch, steps, heads, key_dim, value_dim)
+    return max(int(lib().soma_linear_attn_workspace_bytes(d, DTYPES.get(dtype, -1), k))
+               for k in range(1 + bool(backward)))
+
+
+def linear_attn_alloc_workspace(batch, steps, heads, key_dim, value_dim, dtype, backward=True,
+                                device="cuda") -> torch.Tensor:
+    n = linear_attn_workspace_bytes(batch, steps, heads, key_dim, value_dim, dtype, backward)
+    if n < 0:
+        raise ValueError("invalid sizes or dtype for the workspace")
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def _attn_workspace(d, dtype, backward, workspace, device, stream):
+    """(pointer, bytes, the tensor) of the caller's workspace, or of one from
+    torch's allocator where the sizes need any and none is given."""
+    if workspace is None:
+        n = int(lib().soma_linear_attn_workspace_bytes(d, dtype, backward))
+        if n <= 0:
+            return None, 0, None
+        workspace = torch.empty(n, dtype=torch.uint8, device=device)
+        if stream is not None:
+            # torch's allocator orders it by the current stream: keep it from
+            # being handed out again before `stream` is through with it
+            stream.wait_stream(torch.cuda.current_stream())
+            workspace.record_stream(stream)
+    return _dev(workspace, torch.uint8, "workspace"), workspace.numel(), workspace
+
+
+def linear_attn_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
+                        log_decay: torch.Tensor, o: torch.Tensor,
+                        s_last: torch.Tensor | None = None, s0: torch.Tensor | None = None,
+                        lengths: torch.Tensor | None = None, resets: torch.Tensor | None = None,
+                        scale: float = 1.0, workspace: torch.Tensor | None = None, stream=None):
+    """Linear attention of q, k [B, T, H, dk] and v [B, T, H, dv] into o [B, T, H, dv] with the
+    decay exp(log_decay [H]) of each head; states s0 and s_last fp32 [B, H, dk, dv], lengths int32
+    [B], resets uint8 [B, T], workspace uint8 of linear_attn_workspace_bytes (taken from torch's
+    allocator if not given)."""
+    d, dt = _attn_dims(q, v), _attn_dtype(q)
+    B, T, H, dk, dv = d.batch, d.steps, d.heads, d.key_dim, d.value_dim
+    _here(q=q, k=k, v=v, log_decay=log_decay, o=o, s_last=s_last, s0=s0, lengths=lengths,
+          resets=resets, workspace=workspace)
+    f32, states = torch.float32, B * H * dk * dv
+    qp, qs = _attn_tensor(q, "q", (B, T, H, dk), q.dtype)
+    kp, ks = _attn_tensor(k, "k", (B, T, H, dk), q.dtype)
+    vp, vs = _attn_tensor(v, "v", (B, T, H, dv), q.dtype)
+    op, os_ = _attn_tensor(o, "o", (B, T, H, dv), q.dtype)
+    wp, wn, _keep = _attn_workspace(d, dt, 0, workspace, q.device, stream)
+    _check(lib().soma_linear_attn_forward(
+        qp, qs, kp, ks, vp, vs, dt, d, _dev(log_decay, f32, "log_decay", H), scale,
+        _opt(s0, f32, "s0", states), _opt(lengths, torch.int32, "lengths", B),
+        _opt(resets, torch.uint8, "resets", B * T), op, os_, _opt(s_last, f32, "s_last", states),
+        wp, wn, _stream(stream)), "soma_linear_attn_forward")
+
+
+def linear_attn_backward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
+                         log_decay: torch.Tensor, do: torch.Tensor, dq: torch.Tensor,
+                         dk: torch.Tensor, dv: torch.Tensor, s0: torch.Tensor | None = None,
+                         ds_last: torch.Tensor | None = None, ds0: torch.Tensor | None = None,
+                         lengths: torch.Tensor | None = None, resets: torch.Tensor | None = None,
+                         scale: float = 1.0, workspace: torch.Tensor | None = None, stream=None):
+    """Gradients of linear_attn_forward: dq, dk, dv (and ds0) from do and ds_last (the gradient of
+    s_last), with that call's inputs."""
+    d, dt = _attn_dims(q, v), _attn_dtype(q)
+    B, T, H, kd, vd = d.batch, d.steps, d.heads, d.key_dim, d.value_dim
+    _here(q=q, k=k, v=v, log_decay=log_decay, do=do, dq=dq, dk=dk, dv=dv, s0=s0, ds_last=ds_last,
+          ds0=ds0, lengths=lengths, resets=resets, workspace=workspace)
+    f32, states = torch.float32, B * H * kd * vd
+    keys, values = (B, T, H, kd), (B, T, H, vd)
+    qp, qs = _attn_tensor(q, "q", keys, q.dtype)
+    kp, ks = _attn_tensor(k, "k", keys, q.dtype)
+    vp, vs = _attn_tensor(v, "v", values, q.dtype)
+    dop, dos = _attn_tensor(do, "do", values, q.dtype)
+    dqp, dqs = _attn_tensor(dq, "dq", keys, q.dtype)
+    dkp, dks = _attn_tensor(dk, "dk", keys, q.dtype)
+    dvp, dvs = _attn_tensor(dv, "dv", values, q.dtype)
+    wp, wn, _keep = _attn_workspace(d, dt, 1, workspace, q.device, stream)
+    _check(lib().soma_linear_attn_backward(
+        qp, qs, kp, ks, vp, vs, dt, d, _dev(log_decay, f32, "log_decay", H), scale,
+        _opt(s0, f32, "s0", states), _opt(lengths, torch.int32, "lengths", B),
+        _opt(resets, torch.uint8, "resets", B * T), dop, dos, _opt(ds_last, f32, "ds_last", states),
+        dqp, dqs, dkp, dks, dvp, dvs, _opt(ds0, f32, "ds0", states), wp, wn, _stream(stream)),
+        "soma_linear_attn_backward")
+
+
+def linear_attn_step(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_decay: torch.Tensor,
+                     s: torch.Tensor, o: torch.Tensor, scale: float = 1.0, stream=None):
+    """One token: q, k [B, H, dk], v and o [B, H, dv], states s fp32 [B, H, dk, dv] (updated)."""
+    if q.dim() != 3 or v.dim() != 3:
+        raise ValueError("q and v: expected [batch, heads, width] tensors")
+    (B, H, dk), dv, dt = q.shape, v.shape[2], _attn_dtype(q)
+    _here(q=q, k=k, v=v, log_decay=log_decay, s=s, o=o)
+
+    def tensor(t, name, width):
+        p, st = _rows(t, name, (B, H, width), q.dtype)
+        return p, soma_attn_strides(st[0], 0, st[1])
+
+    (qp, qs), (kp, ks) = tensor(q, "q", dk), tensor(k, "k", dk)
+    (vp, vs), (op, os_) = tensor(v, "v", dv), tensor(o, "o", dv)
+    _check(lib().soma_linear_attn_step(
+        qp, qs, kp, ks, vp, vs, dt, soma_attn_dims(B, 1, H, dk, dv),
+        _dev(log_decay, torch.float32, "log_decay", H), scale,
+        _dev(s, torch.float32, "s", B * H * dk * dv), op, os_, _stream(stream)),
+        "soma_linear_attn_step")
+
+
+def _matrix(t: torch.Tensor, name: str, shape, dtype) -> tuple:
+    """(pointer, elements between rows) of a matrix, or of a contiguous tensor of other
+    dimensions as one of its last dimension's rows."""
+    p, strides = _rows(t, name, shape, dtype)
+    if t.dim() == 2:
+        return p, _row_stride(t)
+    if not t.is_contiguous():
+        raise ValueError(f"{name}: a tensor of {t.dim()} dimensions must be contiguous")
+    return p, max(t.shape[-1], 1) if t.dim() else 1
+
+
+def dropout(x: torch.Tensor, y: torch.Tensor, p: float, seed: int, offset: int = 0,
+            residual: torch.Tensor | None = None, counter: torch.Tensor | None = None,
+            stream=None):
+    """y = residual + x * mask / (1 - p), the mask from (seed, offset + counter) and the elements'
+    places; x, y and residual of one shape and dtype, counter int64 [1] on the device.  The
+    gradient of x is dropout(dy, dx, p, seed, offset, counter=counter)."""
+    if x.dtype not in DTYPES:
+        raise ValueError(f"x: unsupported dtype {x.dtype}")
+    if x.dim() == 0:
+        raise ValueError("x: expected a tensor of one dimension or more")
+    _here(x=x, y=y, residual=residual, counter=counter)
+    (xp, xs), (yp, ys) = _matrix(x, "x", x.shape, x.dtype), _matrix(y, "y", x.shape, x.dtype)
+    rp, rs = (None, 0) if residual is None else _matrix(residual, "residual", x.shape, x.dtype)
+    cols = x.shape[-1]
+    _check(lib().soma_dropout(
+        xp, xs, rp, rs, yp, ys, DTYPES[x.dtype], x.numel() // cols if cols else 0, cols, p,
+        seed & (2 ** 64 - 1), offset & (2 ** 64 - 1), _opt(counter, torch.int64, "counter", 1),
+        _stream(stream)), "soma_dropout")
+
+
+def sample(logits: torch.Tensor, u: torch.Tensor, tokens: torch.Tensor, temperature=1.0, top_k=0,
+           top_p=1.0, min_p=0.0, logprob: torch.Tensor | None = None, stream=None):
+    """One token per row of logits [R, V] into tokens [R] int64, from uniform numbers u [R] fp32;
+    logprob [R] fp32 gets its log probability among the tokens that remained.  temperature, top_p
+    and min_p are numbers or fp32 [R] on the device, top_k a number or int32 [R]."""
+    if logits.dim() != 2 or logits.dtype not in DTYPES:
+        raise ValueError(f"logits: expected a matrix of fp32, bf16 or fp16, got {logits.dtype} "
+                         f"{tuple(logits.shape)}")
+    R = logits.shape[0]
+    cfg, own = soma_sample_config(1.0, 1.0, 0.0, 0), {}
+    for name, x, dtype in (("temperature", temperature, torch.float32),
+                           ("top_p", top_p, torch.float32), ("min_p", min_p, torch.float32),
+                           ("top_k", top_k, torch.int32)):
+        if torch.is_tensor(x):
+            own[name] = x
+            setattr(cfg, name + "s", _dev(x, dtype, name, R).value)
+        else:
+            setattr(cfg, name, x)
+    _here(logits=logits, u=u, tokens=tokens, logprob=logprob, **own)
+    lp, _ = _rows(logits, "logits", logits.shape, logits.dtype)
+    _check(lib().soma_sample(
+        lp, _row_stride(logits), DTYPES[logits.dtype], R, logits.shape[1], cfg,
+        _dev(u, torch.float32, "u", R), _dev(tokens, torch.int64, "tokens", R),
+        _opt(logprob, torch.float32, "logprob", R), _stream(stream)), "soma_sample")

@@ -1,0 +1,679 @@
+// sample.cu -- one token per row of logits by temperature, top-k, top-p and min-p
+// from given random numbers (soma_sample in include/soma_api.h).
+//
+// A cluster of up to eight CTAs shares a row, each with a part of the vocabulary
+// that stays in L2 over the passes.  The ranking is never made: top-k and top-p
+// each need one cut in it, which is found as a radix selection finds it, by
+// counts (or weights) per bin, the bin that the cut lies in, then finer bins of
+// that one.  The first bins are equal steps of (max - l) / T: there the weights
+// of a bin differ by a known factor, so that counts alone say which few bins
+// can hold the cut by weight, and only their weights are added up by bin.
+//
+// Weights are whole numbers, so sums do not depend on their order and every CTA
+// of a cluster comes to the same cut by itself.
+#include <cmath>
+
+#define SOMA_CHECK_FILE 13
+#include "checked.cuh"
+#include "numeric.cuh"
+#include "pdl.cuh"
+#include "soma_api.h"
+#include "soma_launch.h"
+#include "tc_tiles.cuh"
+
+namespace soma {
+
+namespace {
+
+using u64 = unsigned long long;
+
+constexpr int kBins = 2048;
+constexpr int kMaxCluster = 8;
+constexpr int64_t kMaxPart = 1 << 17;      // elements of a CTA: sums of 14-bit parts fit 32 bits
+constexpr float kDeepest = 28.5f;          // 2^40 exp(-28.42) = 1/2: weights further down are 0
+constexpr float kStep = kDeepest / kBins;
+constexpr float kLeastTemperature = 0x1p-100f, kMostTemperature = 0x1p100f;
+
+// 2^(-j/64) as the sum of two fp32 numbers.
+__device__ const float2 kRoots[64] = {
+    {1.f, 0.f}, {0.98922801f, 3.01636316e-09f}, {0.978572071f, -8.51090221e-09f},
+    {0.96803087f, 2.67853615e-08f}, {0.957603276f, 4.92266405e-09f}, {0.947287977f, 1.40516923e-08f},
+    {0.93708384f, -2.33150281e-08f}, {0.926989555f, 7.18280591e-09f}, {0.917004049f, -5.61963898e-09f},
+    {0.907126069f, 1.86812912e-08f}, {0.897354543f, -5.70752245e-09f}, {0.88768822f, 2.67159894e-08f},
+    {0.878126085f, -4.61788519e-09f}, {0.868666947f, -2.92511171e-08f}, {0.859309673f, -2.4248088e-08f},
+    {0.850053191f, -1.43257362e-08f}, {0.840896428f, -1.23776633e-08f}, {0.83183831f, -1.96014938e-08f},
+    {0.822877765f, -2.56248605e-08f}, {0.81401372f, -8.63004157e-09f}, {0.805245161f, 4.91810859e-09f},
+    {0.796571076f, -2.45156839e-10f}, {0.787990451f, -2.83051271e-08f}, {0.779502213f, -1.28823325e-08f},
+    {0.771105409f, 4.03545242e-09f}, {0.762799084f, -8.81428441e-09f}, {0.754582226f, -1.24796866e-08f},
+    {0.746453881f, -1.71181007e-08f}, {0.738413095f, -2.25044943e-08f}, {0.730458915f, -1.81432878e-08f},
+    {0.722590387f, 1.66209997e-08f}, {0.714806676f, -6.71496458e-09f}, {0.707106769f, 1.21016175e-08f},
+    {0.699489832f, 4.34471703e-09f}, {0.69195497f, -2.93778868e-08f}, {0.684501231f, -1.92294092e-08f},
+    {0.677127779f, -5.06167463e-09f}, {0.669833779f, -1.73083698e-08f}, {0.662618339f, -1.74818666e-08f},
+    {0.655480623f, -1.74828578e-08f}, {0.648419797f, -2.00949977e-08f}, {0.641435027f, -1.90831084e-08f},
+    {0.634525478f, 7.09666659e-10f}, {0.627690375f, 3.66111874e-09f}, {0.620928884f, 2.24841905e-08f},
+    {0.614240289f, -2.06810018e-08f}, {0.607623696f, -1.63369744e-08f}, {0.601078391f, -2.53487826e-08f},
+    {0.594603539f, 1.89881764e-08f}, {0.588198483f, 1.28348754e-08f}, {0.58186245f, -2.02572075e-08f},
+    {0.575594604f, 1.09611413e-08f}, {0.56939429f, 2.69311116e-08f}, {0.563260794f, 1.56182072e-08f},
+    {0.557193398f, -2.71777001e-08f}, {0.55119127f, 2.130251e-08f}, {0.545253873f, -6.53876997e-09f},
+    {0.539380372f, 2.73079728e-08f}, {0.53357023f, -2.96687599e-08f}, {0.527822614f, -2.45358471e-08f},
+    {0.522136867f, 2.41673508e-08f}, {0.516512454f, -1.40454466e-08f}, {0.510948598f, -2.40577993e-08f},
+    {0.505444646f, -2.85580271e-09f}};
+
+// The weight of a token whose logit l is at most kDeepest temperatures below
+// max; inv = 1 / T as the sum of two fp32 numbers.  x = (l - max) / T is split
+// into -k ln2/64 + r with |r| < 0.0055, and exp(x) = 2^-(k/64) (1 + r + r^2/2 +
+// ...), with what fp32 rounds off the large terms carried along: good to a few
+// units of the 2^-40 it is rounded to.
+__device__ __forceinline__ u64 weight(float l, float max, float2 inv, const float2* roots) {
+  // l - max = d + e (Knuth's two-sum), times inv
+  const float d = __fsub_rn(l, max), b = __fsub_rn(d, l);
+  const float e = __fsub_rn(__fsub_rn(l, __fsub_rn(d, b)), __fadd_rn(max, b));
+  const float xh = __fmul_rn(d, inv.x);
+  const float xl = fmaf(d, inv.y, fmaf(e, inv.x, fmaf(d, inv.x, -xh)));
+  // ln2 / 64 in parts of 12 bits, whose products with k (12 bits) are exact
+  const float k = fminf(rintf(-xh * 92.3324826f), 4095.f);
+  const float r = fmaf(k, 0x1.62ep-7f, xh);
+  const float m = __fmul_rn(k, 0x1.0bep-21f);
+  const float rh = __fadd_rn(r, m);
+  const float rl = __fadd_rn(__fsub_rn(m, __fsub_rn(rh, r)), fmaf(k, 0x1.be8e7cp-33f, xl));
+  const float q = fmaf(rh * rh, fmaf(rh, fmaf(rh, 1.f / 24, 1.f / 6), 0.5f),
+                       fmaf(rl, rh, rl));
+  const int n = (int)k;
+  const float2 t = roots[n & 63];
+  const float p = __fmul_rn(t.x, rh);
+  const float s = __fadd_rn(t.x, p);
+  const float lo = __fadd_rn(__fsub_rn(p, __fsub_rn(s, t.x)),
+                             fmaf(t.x, q, fmaf(t.x, rh, -p)) + fmaf(t.y, rh, t.y));
+  // to units of 2^-40, the upper 20 bits apart
+  const float up = __fmul_rn(s, 0x1p20f);
+  const int whole = (int)up;
+  const float rest = __fsub_rn(up, (float)whole);
+  const long long w = ((long long)whole << 20) +
+                      (int)rintf(__fmul_rn(fmaf(lo, 0x1p20f, rest), 0x1p20f));
+  const int shift = n >> 6;
+  return shift ? (u64)(w + (1ll << (shift - 1))) >> shift : (u64)w;
+}
+
+// A number that orders as the logits do, and the logit of such a number.
+// 16-bit types have at most 19 significant bits in it, which 22 hold.
+template <typename T>
+constexpr int kKeyBits = sizeof(T) == 4 ? 32 : 22;
+template <typename T>
+__device__ __forceinline__ uint32_t key_of(float l) {
+  const uint32_t b = __float_as_uint(__fadd_rn(l, 0.f));  // -0 as 0
+  return (b >> 31 ? ~b : b | 0x80000000u) >> (32 - kKeyBits<T>);
+}
+template <typename T>
+__device__ __forceinline__ float logit_of(uint32_t key) {
+  const uint32_t b = key << (32 - kKeyBits<T>);
+  const uint32_t low = (1u << (32 - kKeyBits<T>)) - 1;
+  return __uint_as_float(b >> 31 ? b & 0x7fffffffu : ~(b | low));
+}
+
+struct Sample {
+  int64_t stride, rows;
+  int32_t vocab;
+  int32_t part;  // elements of a CTA
+  soma_sample_config cfg;
+  const float* u;
+  int64_t* tokens;
+  float* logprobs;
+};
+
+template <int THREADS>
+struct Shared {
+  uint32_t hist[2][3][kBins];  // two, so that one is read while the other is filled
+  float2 roots[64];
+  u64 slot[12][3];             // sums of this CTA, for the others
+  u64 part[3][THREADS / 32];
+  float fpart[2][THREADS / 32];
+  float2 inv;
+  u64 found[3];
+  int lo, hi;
+};
+
+__device__ __forceinline__ uint32_t cluster_size() {
+  uint32_t n;
+  asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(n));
+  return n;
+}
+__device__ __forceinline__ uint32_t at_rank(const void* p, uint32_t rank) {
+  uint32_t a;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(tc::smem_u32(p)), "r"(rank));
+  return a;
+}
+__device__ __forceinline__ uint32_t remote32(const uint32_t* p, uint32_t rank) {
+  uint32_t v;
+  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(at_rank(p, rank)) : "memory");
+  return v;
+}
+__device__ __forceinline__ u64 remote64(const u64* p, uint32_t rank) {
+  u64 v;
+  asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(at_rank(p, rank)) : "memory");
+  return v;
+}
+
+// One row's work in one CTA.
+template <typename T, int THREADS>
+struct Row {
+  using S = Shared<THREADS>;
+  static constexpr int kWarps = THREADS / 32;
+  static constexpr int kOwn = kBins / THREADS;  // bins of a thread
+  S& sh;
+  const T* row;        // 16-byte aligned, `shift` elements before the first logit
+  int shift, end;      // end: one behind the last logit, counted from `row`
+  int first, stop;     // this thread's
+  uint32_t rank, ranks;
+  int slots = 0, buf = 0;
+  float max = 0.f, inv = 0.f;
+  float2 inv2 = {0.f, 0.f};
+  uint32_t cut = 0;    // what is ranked above this key remains, and ...
+  u64 ties = 0;        // ... so many of this key
+
+  __device__ Row(S& s) : sh(s) {}
+
+  // f(logit, index from `row`) for this thread's logits in order.
+  template <typename F>
+  __device__ __forceinline__ void each(F f) const {
+    for (int i = first; i < stop; i += 8) {
+      if (i + 8 <= shift) continue;
+      float v[8];
+      if (i >= shift && i + 8 <= end) {
+        load8(row + i, v);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) f(v[j], i + j);
+      } else {
+        for (int j = 0; j < 8; ++j)
+          if (i + j >= shift && i + j < end) f(to_f32(row[i + j]), i + j);
+      }
+    }
+  }
+  // f(logit, index, depth) for those whose weight may be above 0; the depth
+  // orders as the logits do.
+  template <typename F>
+  __device__ __forceinline__ void each_weighted(F f) const {
+    each([&](float l, int i) {
+      const float depth = __fmul_rn(__fsub_rn(max, l), inv);
+      if (depth < kDeepest) f(l, i, depth);
+    });
+  }
+  __device__ __forceinline__ static int bin_of(float depth) {
+    return min((int)__fmul_rn(depth, 1.f / kStep), kBins - 1);
+  }
+  __device__ __forceinline__ u64 weight_of(float l) const {
+    return weight(l, max, inv2, sh.roots);
+  }
+
+  __device__ __forceinline__ static u64 warp_sum(u64 v) {
+#pragma unroll
+    for (int k = 16; k; k >>= 1) v += __shfl_xor_sync(0xffffffffu, v, k);
+    return v;
+  }
+  // Sums over the row's CTAs.  Every slot is used once.
+  template <int N>
+  __device__ void sum(u64 (&v)[N]) {
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      v[j] = warp_sum(v[j]);
+      if (threadIdx.x % 32 == 0) sh.part[j][threadIdx.x / 32] = v[j];
+    }
+    __syncthreads();
+    if (threadIdx.x < N) {
+      u64 t = 0;
+      for (int w = 0; w < kWarps; ++w) t += sh.part[threadIdx.x][w];
+      sh.slot[slots][threadIdx.x] = t;
+    }
+    tc::cluster_sync();
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      v[j] = 0;
+      for (uint32_t r = 0; r < ranks; ++r) v[j] += remote64(&sh.slot[slots][j], r);
+    }
+    ++slots;
+  }
+  // The largest over the row's CTAs.
+  __device__ u64 largest(u64 v) {
+#pragma unroll
+    for (int k = 16; k; k >>= 1) {
+      const u64 o = __shfl_xor_sync(0xffffffffu, v, k);
+      v = o > v ? o : v;
+    }
+    if (threadIdx.x % 32 == 0) sh.part[0][threadIdx.x / 32] = v;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+      for (int w = 1; w < kWarps; ++w) v = sh.part[0][w] > v ? sh.part[0][w] : v;
+      sh.slot[slots][0] = v;
+    }
+    tc::cluster_sync();
+    v = 0;
+    for (uint32_t r = 0; r < ranks; ++r) {
+      const u64 o = remote64(&sh.slot[slots][0], r);
+      v = o > v ? o : v;
+    }
+    ++slots;
+    return v;
+  }
+
+  // ---- bins ----
+  __device__ void clear(int arrays) {
+    buf ^= 1;
+    for (int a = 0; a < arrays; ++a)
+      for (int b = threadIdx.x; b < kBins; b += THREADS) sh.hist[buf][a][b] = 0;
+    __syncthreads();
+  }
+  __device__ __forceinline__ void count(int b) { atomicAdd(&sh.hist[buf][0][b], 1u); }
+  // weights go by 14 bits: sums of kMaxPart such numbers fit 32 bits
+  __device__ __forceinline__ void add(int b, u64 w) {
+    atomicAdd(&sh.hist[buf][0][b], (uint32_t)w & 0x3fffu);
+    atomicAdd(&sh.hist[buf][1][b], (uint32_t)(w >> 14) & 0x3fffu);
+    atomicAdd(&sh.hist[buf][2][b], (uint32_t)(w >> 28));
+  }
+  template <bool WEIGHTS>
+  __device__ __forceinline__ u64 in_bin(int b) const {
+    u64 t = 0;
+    for (uint32_t r = 0; r < ranks; ++r) {
+      t += remote32(&sh.hist[buf][0][b], r);
+      if (WEIGHTS) {
+        t += (u64)remote32(&sh.hist[buf][1][b], r) << 14;
+        t += (u64)remote32(&sh.hist[buf][2][b], r) << 28;
+      }
+    }
+    return t;
+  }
+  // The bin where the running sum over the row's bins reaches `need` (at least
+  // 1), the sum before it and what it holds; false if none does.
+  template <bool WEIGHTS>
+  __device__ bool find(u64 need, int* bin, u64* before, u64* held) {
+    if (threadIdx.x == 0) sh.found[0] = ~0ull;
+    tc::cluster_sync();
+    u64 own[kOwn], total = 0;
+#pragma unroll
+    for (int j = 0; j < kOwn; ++j) total += own[j] = in_bin<WEIGHTS>(threadIdx.x * kOwn + j);
+    u64 run = total;
+    const int lane = threadIdx.x % 32;
+#pragma unroll
+    for (int k = 1; k < 32; k <<= 1) {
+      const u64 o = __shfl_up_sync(0xffffffffu, run, k);
+      if (lane >= k) run += o;
+    }
+    if (lane == 31) sh.part[0][threadIdx.x / 32] = run;
+    __syncthreads();
+    run -= total;
+    for (int w = 0; w < (int)threadIdx.x / 32; ++w) run += sh.part[0][w];
+#pragma unroll
+    for (int j = 0; j < kOwn; ++j) {
+      if (run < need && run + own[j] >= need) {
+        sh.found[0] = threadIdx.x * kOwn + j;
+        sh.found[1] = run;
+        sh.found[2] = own[j];
+      }
+      run += own[j];
+    }
+    __syncthreads();
+    *bin = (int)sh.found[0];
+    *before = sh.found[1];
+    *held = sh.found[2];
+    return sh.found[0] != ~0ull;
+  }
+  // From counts per bin of depth: the bins [lo, hi] one of which is where the
+  // sum of weights reaches `need`.  The slack is for the roundings of depths,
+  // of these sums (1e-4) and of small weights to whole numbers (2e-6 of the
+  // largest weight, over 2^20 tokens).
+  __device__ void band(u64 need, int* lo, int* hi) {
+    if (threadIdx.x == 0) {
+      sh.lo = kBins - 1;
+      sh.hi = kBins - 1;
+    }
+    tc::cluster_sync();
+    float most[kOwn], total = 0.f;
+#pragma unroll
+    for (int j = 0; j < kOwn; ++j) {
+      const int b = threadIdx.x * kOwn + j;
+      total += most[j] = (float)in_bin<false>(b) * __expf(-kStep * b);
+    }
+    float run = total;
+    const int lane = threadIdx.x % 32;
+#pragma unroll
+    for (int k = 1; k < 32; k <<= 1) {
+      const float o = __shfl_up_sync(0xffffffffu, run, k);
+      if (lane >= k) run += o;
+    }
+    if (lane == 31) sh.fpart[0][threadIdx.x / 32] = run;
+    __syncthreads();
+    run -= total;
+    for (int w = 0; w < (int)threadIdx.x / 32; ++w) run += sh.fpart[0][w];
+    const float want = (float)need * 0x1p-40f;
+    const float least = __expf(-kStep);  // the lowest weight of a bin by its highest
+    int first_most = kBins, first_least = kBins;
+#pragma unroll
+    for (int j = 0; j < kOwn; ++j) {
+      run += most[j];
+      if (first_most == kBins && fmaf(run, 1.0001f, 2e-6f) >= want)
+        first_most = threadIdx.x * kOwn + j;
+      if (first_least == kBins && fmaf(run * least, 0.9999f, -2e-6f) >= want)
+        first_least = threadIdx.x * kOwn + j;
+    }
+    if (first_most < kBins) atomicMin(&sh.lo, first_most);
+    if (first_least < kBins) atomicMin(&sh.hi, first_least);
+    __syncthreads();
+    *lo = sh.lo;
+    *hi = sh.hi;
+  }
+  // The key in bin `bin` of depth at which the running count (or weight) of the
+  // bin reaches `need`; what is left of `need` at that key is returned.
+  template <bool WEIGHTS>
+  __device__ u64 refine(int bin, u64 need, uint32_t* key) {
+    uint32_t prefix = 0;
+    int left = kKeyBits<T>;
+    while (left > 0) {
+      const int bits = left < 11 ? left : 11;
+      const uint32_t mask = (1u << bits) - 1;
+      clear(WEIGHTS ? 3 : 1);
+      each_weighted([&](float l, int, float depth) {
+        if (bin_of(depth) != bin) return;
+        const uint32_t k = key_of<T>(l);
+        if (k <= cut || (left < kKeyBits<T> && k >> left != prefix)) return;
+        const int b = (int)(mask - (k >> (left - bits) & mask));  // larger keys first
+        if (WEIGHTS) add(b, weight_of(l));
+        else count(b);
+      });
+      int at;
+      u64 before, held;
+      find<WEIGHTS>(need, &at, &before, &held);
+      need -= before;
+      prefix = prefix << bits | (mask - (uint32_t)at);
+      left -= bits;
+    }
+    *key = prefix;
+    return need;
+  }
+
+  // ---- the two cuts ----
+  __device__ void top_k(u64 k) {
+    clear(1);
+    each_weighted([&](float, int, float depth) { count(bin_of(depth)); });
+    int bin;
+    u64 before, held;
+    if (!find<false>(k, &bin, &before, &held)) return;  // fewer have a weight at all
+    uint32_t key;
+    ties = refine<false>(bin, k - before, &key);
+    cut = key;
+  }
+  __device__ void top_p(float p) {
+    clear(1);
+    u64 v[1] = {0};
+    each_weighted([&](float l, int, float depth) {
+      if (key_of<T>(l) <= cut) return;
+      count(bin_of(depth));
+      v[0] += weight_of(l);
+    });
+    sum(v);
+    const u64 tie = ties ? weight_of(logit_of<T>(cut)) : 0;
+    if (threadIdx.x == 0) {
+      const double want = ceil((double)p * (double)(v[0] + ties * tie));
+      sh.found[0] = want < 1.0 ? 1 : (u64)want;
+    }
+    __syncthreads();
+    u64 need = sh.found[0];
+    __syncthreads();
+    if (need > v[0]) {  // the cut stays at the key of the first one
+      if (tie) ties = min(ties, (need - v[0] + tie - 1) / tie);
+      return;
+    }
+    int lo, hi;
+    band(need, &lo, &hi);
+    clear(3);
+    u64 above[1] = {0};
+    each_weighted([&](float l, int, float depth) {
+      const int b = bin_of(depth);
+      if (b > hi || key_of<T>(l) <= cut) return;
+      const u64 w = weight_of(l);
+      if (b < lo) above[0] += w;
+      else add(b, w);
+    });
+    sum(above);
+    int bin;
+    u64 before, held;
+    if (!find<true>(need - above[0], &bin, &before, &held)) return;
+    uint32_t key;
+    need = refine<true>(bin, need - above[0] - before, &key);
+    const u64 w = weight_of(logit_of<T>(key));
+    cut = key;
+    ties = w ? (need + w - 1) / w : 0;
+  }
+};
+
+template <typename T, int THREADS>
+__global__ void __launch_bounds__(THREADS)
+sample_kernel(const T* logits, const Sample s, int* status) {
+  extern __shared__ __align__(16) uint8_t raw[];
+  auto& sh = *reinterpret_cast<Shared<THREADS>*>(raw);
+  Row<T, THREADS> r(sh);
+  r.ranks = cluster_size();
+  r.rank = tc::pair_rank();
+  const int64_t n = blockIdx.x / r.ranks;
+  if (threadIdx.x < 64) sh.roots[threadIdx.x] = kRoots[threadIdx.x];
+  admit_successor();
+  after_predecessor();
+
+  const float temperature = s.cfg.temperatures ? s.cfg.temperatures[n] : s.cfg.temperature;
+  const float top_p = s.cfg.top_ps ? s.cfg.top_ps[n] : s.cfg.top_p;
+  const float min_p = s.cfg.min_ps ? s.cfg.min_ps[n] : s.cfg.min_p;
+  const int top_k = s.cfg.top_ks ? s.cfg.top_ks[n] : s.cfg.top_k;
+  const float u = s.u[n];
+  const T* row = logits + n * s.stride;
+  r.shift = (int)((reinterpret_cast<uintptr_t>(row) & 15) / sizeof(T));
+  r.row = row - r.shift;
+  r.end = r.shift + s.vocab;
+  const int part_end = min(r.end, (int)(r.rank + 1) * s.part);
+  const int each = (s.part / THREADS + 8) / 8 * 8;
+  r.first = (int)r.rank * s.part + (int)threadIdx.x * each;
+  r.stop = min(r.first + each, part_end);
+
+  // the largest logit, as an ordered number; NaN above all
+  u64 top = 0;
+  r.each([&](float l, int) {
+    const uint32_t b = __float_as_uint(__fadd_rn(l, 0.f));
+    const u64 k = isnan(l) ? 0xffffffffu : (b >> 31 ? ~b : b | 0x80000000u);
+    top = k > top ? k : top;
+  });
+  top = r.largest(top);
+  const uint32_t lowest = ~0xff800000u;  // of -infinity
+  const bool nothing = top <= lowest;
+  const bool bad = top >= (0x7f800000u | 0x80000000u) || !(temperature >= 0.f) || isnan(top_p) ||
+                   isnan(min_p) || !(u >= 0.f && u < 1.f);
+  if (bad || nothing) {  // the whole cluster
+    if (r.rank == 0 && threadIdx.x == 0) {
+      s.tokens[n] = -1;
+      if (s.logprobs) s.logprobs[n] = NAN;
+      if (bad) atomicCAS(status, 0, SOMA_ERR_NONFINITE);
+    }
+    tc::cluster_sync();
+    return;
+  }
+  r.max = __uint_as_float(top >> 31 ? (uint32_t)top & 0x7fffffffu : ~(uint32_t)top);
+
+  if (temperature < kLeastTemperature) {
+    u64 at = 0;  // the first of the largest: the largest of 2^32 - index
+    r.each([&](float l, int i) {
+      if (l == r.max) at = max(at, (1ull << 32) - (u64)i);
+    });
+    at = r.largest(at);
+    if (r.rank == 0 && threadIdx.x == 0) {
+      s.tokens[n] = (int64_t)((1ull << 32) - at) - r.shift;
+      if (s.logprobs) s.logprobs[n] = 0.f;
+    }
+    tc::cluster_sync();
+    return;
+  }
+
+  if (threadIdx.x == 0) {
+    const double inv = 1.0 / (double)fminf(temperature, kMostTemperature);
+    const float hi = (float)inv;
+    sh.inv = make_float2(hi, (float)(inv - (double)hi));
+  }
+  __syncthreads();
+  r.inv2 = sh.inv;
+  r.inv = r.inv2.x;
+  if (top_k > 0 && top_k < s.vocab) r.top_k((u64)top_k);
+  if (top_p < 1.f) r.top_p(top_p);
+
+  // what remains, in the order of the indexes
+  const u64 least = min_p > 0.f ? (u64)ceil((double)fminf(min_p, 1.f) * 0x1p40) : 0;
+  const u64 tie = r.ties ? r.weight_of(logit_of<T>(r.cut)) : 0;
+  const bool tied = r.ties && tie >= least;
+  u64 own = 0, equal = 0;
+  r.each_weighted([&](float l, int, float) {
+    const uint32_t k = key_of<T>(l);
+    if (k > r.cut) {
+      const u64 w = r.weight_of(l);
+      if (w >= least) own += w;
+    } else if (tied && k == r.cut) {
+      ++equal;
+    }
+  });
+  // equal ones before this thread's, in the CTA and in the CTAs before it
+  const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+  const auto scan = [&](u64 v, int which) {  // sum of the threads before this one
+    u64 run = v;
+#pragma unroll
+    for (int k = 1; k < 32; k <<= 1) {
+      const u64 o = __shfl_up_sync(0xffffffffu, run, k);
+      if (lane >= k) run += o;
+    }
+    if (lane == 31) sh.part[which][warp] = run;
+    __syncthreads();
+    run -= v;
+    for (int w = 0; w < warp; ++w) run += sh.part[which][w];
+    return run;
+  };
+  __syncthreads();
+  u64 equal_before = scan(equal, 0);
+  if (threadIdx.x == THREADS - 1) sh.slot[r.slots][0] = equal_before + equal;
+  tc::cluster_sync();
+  for (uint32_t k = 0; k < r.rank; ++k) equal_before += remote64(&sh.slot[r.slots][0], k);
+  u64 room = r.ties > equal_before ? r.ties - equal_before : 0;
+  if (!tied) room = 0;
+  own += min(room, equal) * tie;
+  u64 before = scan(own, 1);
+  if (threadIdx.x == THREADS - 1) sh.slot[r.slots][1] = before + own;
+  tc::cluster_sync();
+  u64 total = 0;
+  for (uint32_t k = 0; k < r.ranks; ++k) {
+    const u64 v = remote64(&sh.slot[r.slots][1], k);
+    total += v;
+    if (k < r.rank) before += v;
+  }
+  u64 at = (u64)((double)u * (double)total);
+  if (at >= total) at = total - 1;
+  if (at >= before && at - before < own) {
+    // the token is this thread's
+    u64 run = before;
+    int token = -1;
+    float chosen = 0.f;
+    r.each_weighted([&](float l, int i, float) {
+      if (token >= 0) return;
+      const uint32_t k = key_of<T>(l);
+      u64 w = 0;
+      if (k > r.cut) {
+        w = r.weight_of(l);
+        if (w < least) w = 0;
+      } else if (k == r.cut && room) {
+        w = tie;
+        --room;
+      }
+      run += w;
+      if (run > at) {
+        token = i - r.shift;
+        chosen = l;
+      }
+    });
+    s.tokens[n] = token;
+    if (s.logprobs)
+      s.logprobs[n] = (float)(((double)chosen - (double)r.max) /
+                                  (double)fminf(temperature, kMostTemperature) -
+                              log((double)total * 0x1p-40));
+  }
+  tc::cluster_sync();  // no CTA leaves while another may read its sums
+}
+
+// CTAs of a row: as many as fill the GPU three times over, if each keeps 2048
+// logits or more.
+int cluster_of(int64_t rows, int64_t vocab) {
+  int n = 1;
+  while (n < kMaxCluster && (vocab / n > kMaxPart - 8 ||
+                             (rows * n < 3 * 152 && vocab / (2 * n) >= 2048)))
+    n *= 2;
+  return n;
+}
+
+template <typename T, int THREADS>
+cudaError_t launch(const void* logits, Sample s, int* status, cudaStream_t st) {
+  const int n = cluster_of(s.rows, s.vocab);
+  const auto kernel = sample_kernel<T, THREADS>;
+  // up to 16 / width - 1 elements come before the first logit
+  s.part = (int32_t)(((s.vocab + 7 + n - 1) / n + 7) / 8 * 8);
+  const size_t smem = sizeof(Shared<THREADS>);
+  static const cudaError_t set =
+      cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  if (set != cudaSuccess) return set;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = (unsigned)n;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(s.rows * n));
+  cfg.blockDim = dim3(THREADS);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  return cudaLaunchKernelEx(&cfg, kernel, static_cast<const T*>(logits), (const Sample)s, status);
+}
+
+template <typename T>
+cudaError_t run(const void* logits, const Sample& s, int* status, cudaStream_t st) {
+  return s.vocab <= 2048 ? launch<T, 128>(logits, s, status, st)
+                         : launch<T, 512>(logits, s, status, st);
+}
+
+bool aligned(const void* p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
+
+}  // namespace
+}  // namespace soma
+
+using namespace soma;
+
+extern "C" int soma_sample(const void* logits, int64_t stride, int dtype, int64_t rows,
+                           int64_t vocab, soma_sample_config cfg, const float* u, int64_t* tokens,
+                           float* logprobs, void* stream) {
+  if (rows < 0 || rows > (1 << 24) || vocab < 1 || vocab > (1 << 20)) return SOMA_ERR_UNSUPPORTED;
+  if (dtype != SOMA_FP32 && dtype != SOMA_BF16 && dtype != SOMA_FP16) return SOMA_ERR_INVALID_ARG;
+  if (stride < vocab || !aligned(logits, dtype == SOMA_FP32 ? 4 : 2) || !aligned(u, 4) ||
+      !aligned(tokens, 8) || !aligned(logprobs, 4) || !aligned(cfg.temperatures, 4) ||
+      !aligned(cfg.top_ps, 4) || !aligned(cfg.min_ps, 4) || !aligned(cfg.top_ks, 4) ||
+      (!cfg.temperatures && !(cfg.temperature >= 0.f)) ||
+      (!cfg.top_ps && std::isnan(cfg.top_p)) || (!cfg.min_ps && std::isnan(cfg.min_p)))
+    return SOMA_ERR_INVALID_ARG;
+  if (rows == 0) return SOMA_OK;
+  if (!logits || !u || !tokens) return SOMA_ERR_INVALID_ARG;
+  int* status = status_ptr();
+  if (!status) return SOMA_ERR_CUDA;
+  Sample s = {};
+  s.stride = stride;
+  s.rows = rows;
+  s.vocab = (int32_t)vocab;
+  s.cfg = cfg;
+  s.u = u;
+  s.tokens = tokens;
+  s.logprobs = logprobs;
+  const cudaStream_t st = (cudaStream_t)stream;
+  trace_begin(SOMA_TRACE_SAMPLE, st);
+  const cudaError_t e = dtype == SOMA_FP32   ? run<float>(logits, s, status, st)
+                        : dtype == SOMA_BF16 ? run<__nv_bfloat16>(logits, s, status, st)
+                                             : run<__half>(logits, s, status, st);
+  trace_end(SOMA_TRACE_SAMPLE, st);
+  return e == cudaSuccess ? SOMA_OK : SOMA_ERR_CUDA;
+}

@@ -1,7 +1,8 @@
 // trace.cu -- optional per-kernel-class timing with CUDA events recorded on
 // the launching stream around every kernel of soma_spsa_step / soma_eval_loss,
 // and around every call of the first-order entry points (soma_trace_enable /
-// soma_trace_read / soma_trace_read_first_order in include/soma_api.h).
+// soma_trace_read / soma_trace_read_first_order / soma_trace_read_sequence in
+// include/soma_api.h).
 #include <mutex>
 #include <vector>
 
@@ -111,6 +112,12 @@ int soma_trace_read_first_order(soma_first_order_times* out, int reset) {
   if (!out) return SOMA_ERR_INVALID_ARG;
   std::lock_guard<std::mutex> lk(g_mu);
   return read_kinds(SOMA_TRACE_LINEAR_CE, SOMA_TRACE_FIRST_ORDER, out->ms, out->calls, reset);
+}
+
+int soma_trace_read_sequence(soma_sequence_times* out, int reset) {
+  if (!out) return SOMA_ERR_INVALID_ARG;
+  std::lock_guard<std::mutex> lk(g_mu);
+  return read_kinds(SOMA_TRACE_LINEAR_ATTN, SOMA_TRACE_SEQUENCE, out->ms, out->calls, reset);
 }
 
 }  // extern "C"
