@@ -19,6 +19,25 @@ constexpr int kRows = 16;       // rows of the state that a thread holds, in fou
 constexpr int kCols = 4;        // and columns
 constexpr int kStepThreads = 256;
 
+// exp(g) by fp32 numbers that have it as their mean: `up` is due `share` / 2^32 of
+// the steps, `low` in the others.  The nearest fp32 number would be off by up to
+// 2^-25 every time in the same direction, 3e-5 after a thousand steps.
+struct Decay {
+  float low, up;
+  uint32_t share;
+  __device__ __forceinline__ float at(int64_t step) const {
+    return (uint32_t)(step + 1) * share < share ? up : low;
+  }
+};
+__device__ Decay split_decay(float g) {
+  const double l = exp((double)g);
+  Decay d;
+  d.low = __double2float_rd(l);
+  d.up = __double2float_ru(l);
+  d.share = d.up > d.low ? (uint32_t)((l - d.low) / ((double)d.up - d.low) * 4294967295.0) : 0;
+  return d;
+}
+
 // The recurrence step by step in fp32: one CTA per problem, sequence and head,
 // the state in registers, 16 x 4 of it per thread.  Threads of `groups`
 // neighbouring lanes hold the rows of the same columns.
@@ -32,7 +51,8 @@ plain_kernel(const __grid_constant__ Call call, int groups) {
   const Problem& p = call.p[blockIdx.x / rows_all];
   const int64_t bh = blockIdx.x % rows_all, b = bh / call.heads, h = bh % call.heads;
   const int64_t len = length_of(call, b);
-  const float g = decay_of(call, h), decay = expf(g);
+  __shared__ Decay decay;
+  if (threadIdx.x == 0) decay = split_decay(decay_of(call, h));
   const int rows = groups * kRows, cols = (p.c + kCols - 1) / kCols * kCols;
   float* sx = smem;
   float* sy = sx + kTile * rows;
@@ -75,7 +95,7 @@ plain_kernel(const __grid_constant__ Call call, int groups) {
     }
     if ((int)threadIdx.x < n) {
       const int64_t t = step_of(threadIdx.x);
-      float m = decay;
+      float m = decay.at(n0 + threadIdx.x);
       if (p.reversed) {
         if (t == len - 1) m = 1.f;
         else if (resets && resets[t + 1]) m = 0.f;
@@ -128,7 +148,7 @@ plain_kernel(const __grid_constant__ Call call, int groups) {
   for (int64_t e = len * p.c + threadIdx.x; e < call.steps * p.c; e += blockDim.x)
     out[e / p.c * p.os.t + e % p.c] = from_f32<T>(0.f);
   if (!p.s_out || !holds) return;
-  const float last = !p.reversed || len == 0 ? 1.f : resets && resets[0] ? 0.f : decay;
+  const float last = !p.reversed || len == 0 ? 1.f : resets && resets[0] ? 0.f : decay.at(len);
 #pragma unroll
   for (int r = 0; r < kRows; ++r)
 #pragma unroll
@@ -177,7 +197,11 @@ step_kernel(const __grid_constant__ Call call, int lanes) {
     sx[i] = to_f32(x[i]);
     sy[i] = to_f32(y[i]);
   }
-  const float decay = expf(decay_of(call, h));
+  // exp(g) as a sum whose error is 2^-24 of 1 - exp(g), not of exp(g): over the
+  // steps that a state lasts it stays 2^-24
+  const float g = decay_of(call, h);
+  const bool slow = g > -0.5f;
+  const float keep = slow ? 1.f : expf(g), change = slow ? expm1f(g) : 0.f;
   float zc[V], o[V];
 #pragma unroll
   for (int j = 0; j < V; ++j) {
@@ -195,8 +219,8 @@ step_kernel(const __grid_constant__ Call call, int lanes) {
 #pragma unroll
         for (int j = 0; j < V; ++j) {
           // a decay of 0 keeps nothing, whatever it is
-          const float kept = decay == 0.f ? 0.f : decay * v[k][j];
-          v[k][j] = fmaf(sy[r], zc[j], kept);
+          const float new_part = sy[r] * zc[j];
+          v[k][j] = keep == 0.f ? new_part : fmaf(keep, v[k][j], fmaf(change, v[k][j], new_part));
           o[j] = fmaf(sx[r], v[k][j], o[j]);
         }
         float* at = s + r * p.c + col;
@@ -269,7 +293,64 @@ cudaError_t step(const Call& call, cudaStream_t st) {
   return launch_overlapped(step_kernel<T, 1>, grid, kStepThreads, 0, st, call, kStepThreads / p.c);
 }
 
-cudaError_t run(const Call& call, int dtype, cudaStream_t st) {
+// Whether the tensor-core kernels can read and write a tensor.
+bool tiled(const void* p, const soma_attn_strides& s) {
+  return aligned(p, 16) && s.b % 8 == 0 && s.t % 8 == 0 && s.h % 8 == 0;
+}
+
+// The cut with the least estimated time, in chunks of one CTA: states of all
+// segments but the last first (half the work of a chunk), then the outputs.
+Cut cut_of(const soma_attn_dims& d, int dtype, int problems) {
+  Cut best = {};
+  best.segments = 1;
+  best.chunks = (d.steps + kChunk - 1) / kChunk;
+  if (dtype == SOMA_FP32 || d.key_dim % 8 || d.value_dim % 8) return best;
+  const int64_t rows = d.batch * d.heads * problems, chunks = best.chunks;
+  const int64_t resident = d.key_dim <= 64 && d.value_dim <= 64 ? 304 : 152;
+  const auto waves = [&](int64_t n) { return (double)((n + resident - 1) / resident); };
+  double least = waves(rows) * (chunks + 2);
+  for (int64_t n = 2; n <= chunks && n <= 1024; ++n) {
+    const int64_t each = (chunks + n - 1) / n;
+    if ((chunks + each - 1) / each != n) continue;
+    const double cost =
+        waves(rows * n) * (each + 2) + waves(rows * (n - 1)) * (0.5 * each + 2) + 4;
+    if (cost < least) {
+      least = cost;
+      best.segments = (int32_t)n;
+      best.chunks = each;
+    }
+  }
+  return best;
+}
+
+// Where a cut's parts lie in the workspace, with the checked build's gaps.
+struct Parts {
+  size_t starts, fades, bytes;
+  Gaps gaps;
+};
+Parts parts_of(const soma_attn_dims& d, const Cut& cut, int problems) {
+  Parts p = {};
+  if (cut.segments < 2) return p;
+  const size_t n = (size_t)(d.batch * d.heads) * problems * cut.segments;
+  p.starts = kGuard;
+  p.fades = p.starts + (n * d.key_dim * d.value_dim * sizeof(float) + 15) / 16 * 16 + kGuard;
+  p.bytes = p.fades + (n * sizeof(float2) + 15) / 16 * 16 + kGuard;
+  p.gaps.n = 3;
+  p.gaps.off[0] = 0;
+  p.gaps.off[1] = p.fades - kGuard;
+  p.gaps.off[2] = p.bytes - kGuard;
+  return p;
+}
+
+cudaError_t run(const Call& call, const Cut& cut, int dtype, cudaStream_t st) {
+  bool chunked = dtype != SOMA_FP32 && call.steps > 0;
+  for (int k = 0; k < call.problems; ++k) {
+    const Problem& p = call.p[k];
+    chunked = chunked && p.a % 8 == 0 && p.c % 8 == 0 && tiled(p.x, p.xs) && tiled(p.y, p.ys) &&
+              tiled(p.z, p.zs) && tiled(p.out, p.os);
+  }
+  cudaError_t e;
+  if (chunked && launch_chunks(call, cut, dtype, st, &e)) return e;
   return dtype == SOMA_FP32   ? plain<float>(call, st)
          : dtype == SOMA_BF16 ? plain<__nv_bfloat16>(call, st)
                               : plain<__half>(call, st);
@@ -287,6 +368,23 @@ Call make_call(const soma_attn_dims& d, const float* log_decay, const int32_t* l
   c.resets = resets;
   c.status = status;
   return c;
+}
+
+void put_workspace(Cut* cut, const Parts& parts, void* workspace) {
+  if (!parts.bytes) return;
+  uint8_t* ws = static_cast<uint8_t*>(workspace);
+  cut->starts = reinterpret_cast<float*>(ws + parts.starts);
+  cut->fades = reinterpret_cast<float2*>(ws + parts.fades);
+}
+
+int traced(const Call& call, const Cut& cut, const Parts& parts, int dtype, void* workspace,
+           cudaStream_t st) {
+  if (parts.bytes && gaps_fill(parts.gaps, workspace, st) != cudaSuccess) return SOMA_ERR_CUDA;
+  trace_begin(SOMA_TRACE_LINEAR_ATTN, st);
+  cudaError_t e = run(call, cut, dtype, st);
+  trace_end(SOMA_TRACE_LINEAR_ATTN, st);
+  if (parts.bytes && e == cudaSuccess) e = gaps_check(parts.gaps, workspace, call.status, st);
+  return e == cudaSuccess ? SOMA_OK : SOMA_ERR_CUDA;
 }
 
 // States are [key_dim][value_dim]; `turned`: the problem's rows are its columns.
@@ -308,7 +406,8 @@ extern "C" {
 
 int64_t soma_linear_attn_workspace_bytes(soma_attn_dims d, int dtype, int backward) {
   if (!dims_ok(d) || !dtype_ok(dtype) || (backward != 0 && backward != 1)) return -1;
-  return 0;
+  const int problems = backward ? 3 : 1;
+  return (int64_t)parts_of(d, cut_of(d, dtype, problems), problems).bytes;
 }
 
 int soma_linear_attn_forward(const void* q, soma_attn_strides q_strides, const void* k,
@@ -327,8 +426,11 @@ int soma_linear_attn_forward(const void* q, soma_attn_strides q_strides, const v
   if (d.batch == 0 || d.heads == 0) return SOMA_OK;
   if (!log_decay || (d.steps > 0 && (!q || !k || !v || !o))) return SOMA_ERR_INVALID_ARG;
   if (overlap(s0, s_last, d.batch * d.heads * d.key_dim * d.value_dim)) return SOMA_ERR_INVALID_ARG;
-  (void)workspace;
-  (void)workspace_bytes;
+  Cut cut = cut_of(d, dtype, 1);
+  const Parts parts = parts_of(d, cut, 1);
+  if (parts.bytes && (!workspace || !aligned(workspace, 16) || workspace_bytes < parts.bytes))
+    return SOMA_ERR_WORKSPACE;
+  put_workspace(&cut, parts, workspace);
   int* status = status_ptr();
   if (!status) return SOMA_ERR_CUDA;
   Call call = make_call(d, log_decay, lengths, resets, status);
@@ -338,11 +440,7 @@ int soma_linear_attn_forward(const void* q, soma_attn_strides q_strides, const v
   p.f = 1.f;
   p.g = scale;
   put_states(&p, d, false, s0, s_last);
-  const cudaStream_t st = (cudaStream_t)stream;
-  trace_begin(SOMA_TRACE_LINEAR_ATTN, st);
-  const cudaError_t e = run(call, dtype, st);
-  trace_end(SOMA_TRACE_LINEAR_ATTN, st);
-  return e == cudaSuccess ? SOMA_OK : SOMA_ERR_CUDA;
+  return traced(call, cut, parts, dtype, workspace, (cudaStream_t)stream);
 }
 
 int soma_linear_attn_backward(const void* q, soma_attn_strides q_strides, const void* k,
@@ -367,8 +465,11 @@ int soma_linear_attn_backward(const void* q, soma_attn_strides q_strides, const 
     return SOMA_ERR_INVALID_ARG;
   const int64_t states = d.batch * d.heads * d.key_dim * d.value_dim;
   if (overlap(s0, ds0, states) || overlap(ds_last, ds0, states)) return SOMA_ERR_INVALID_ARG;
-  (void)workspace;
-  (void)workspace_bytes;
+  Cut cut = cut_of(d, dtype, 3);
+  const Parts parts = parts_of(d, cut, 3);
+  if (parts.bytes && (!workspace || !aligned(workspace, 16) || workspace_bytes < parts.bytes))
+    return SOMA_ERR_WORKSPACE;
+  put_workspace(&cut, parts, workspace);
   int* status = status_ptr();
   if (!status) return SOMA_ERR_CUDA;
   Call call = make_call(d, log_decay, lengths, resets, status);
@@ -383,11 +484,7 @@ int soma_linear_attn_backward(const void* q, soma_attn_strides q_strides, const 
   put_states(&pq, d, true, s0, nullptr);
   put_states(&pk, d, true, ds_last, nullptr);
   put_states(&pv, d, false, ds_last, ds0);
-  const cudaStream_t st = (cudaStream_t)stream;
-  trace_begin(SOMA_TRACE_LINEAR_ATTN, st);
-  const cudaError_t e = run(call, dtype, st);
-  trace_end(SOMA_TRACE_LINEAR_ATTN, st);
-  return e == cudaSuccess ? SOMA_OK : SOMA_ERR_CUDA;
+  return traced(call, cut, parts, dtype, workspace, (cudaStream_t)stream);
 }
 
 int soma_linear_attn_step(const void* q, soma_attn_strides q_strides, const void* k,

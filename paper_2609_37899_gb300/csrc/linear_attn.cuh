@@ -51,6 +51,22 @@ struct Call {
   int* status;
 };
 
+// Steps of a chunk of the tensor-core kernels, and how the steps of a call are
+// cut into segments of whole chunks.
+constexpr int kChunk = 128;
+struct Cut {
+  int32_t segments;
+  int32_t launched;  // segments of the launch
+  int64_t chunks;    // of a segment
+  float* starts;     // [batch * heads][problems][segments] states; where segments > 1
+  float2* fades;     // ... what a segment keeps of the state before it
+};
+
+// The recurrences of a call on the tensor cores (16-bit types; widths, strides
+// and addresses of whole 16-byte pieces; steps > 0).  False, and nothing is
+// launched, if the strides do not nest as a tensor map wants it.
+bool launch_chunks(const Call& call, const Cut& cut, int dtype, cudaStream_t st, cudaError_t* e);
+
 __device__ __forceinline__ int64_t length_of(const Call& c, int64_t b) {
   if (!c.lengths) return c.steps;
   const int64_t n = c.lengths[b];

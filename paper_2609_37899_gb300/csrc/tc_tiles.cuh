@@ -190,4 +190,10 @@ bool make_tile_map(CUtensorMap* map, const void* base, int dtype, int64_t rows, 
 bool make_box_map(CUtensorMap* map, const void* base, int dtype, const int64_t (&size)[3],
                   const int64_t (&stride)[2], const int (&box_size)[3]);
 
+// Tensor map of a 4-D tensor of a 16-bit type, the first dimension adjacent and
+// `stride` elements between neighbours of the others, in boxes of 64 columns
+// (128 bytes, swizzled).  As make_box_map, each stride a multiple of the last.
+bool make_swizzled_map(CUtensorMap* map, const void* base, int dtype, const int64_t (&size)[4],
+                       const int64_t (&stride)[3], const int (&box_size)[4]);
+
 }  // namespace soma

@@ -66,4 +66,22 @@ bool make_box_map(CUtensorMap* map, const void* base, int dtype, const int64_t (
                 CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+bool make_swizzled_map(CUtensorMap* map, const void* base, int dtype, const int64_t (&size)[4],
+                       const int64_t (&stride)[3], const int (&box_size)[4]) {
+  const Encode encode = encoder();
+  if (!encode) return false;
+  cuuint64_t dims[4], strides[3];
+  cuuint32_t box[4];
+  for (int i = 0; i < 4; ++i) {
+    dims[i] = (cuuint64_t)size[i];
+    box[i] = (cuuint32_t)box_size[i];
+    if (i < 3) strides[i] = (cuuint64_t)stride[i] * 2;
+  }
+  const cuuint32_t step[4] = {1, 1, 1, 1};
+  return encode(map, type_of(dtype), 4, const_cast<void*>(base), dims, strides, box, step,
+                CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 }  // namespace soma
