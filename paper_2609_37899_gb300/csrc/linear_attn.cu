@@ -8,6 +8,7 @@
 #include "linear_attn.cuh"
 #include "numeric.cuh"
 #include "pdl.cuh"
+#include "tc_primitives.cuh"
 
 namespace soma {
 namespace attn {
@@ -15,8 +16,9 @@ namespace attn {
 namespace {
 
 constexpr int kTile = 16;       // steps that are staged at once
-constexpr int kRows = 16;       // rows of the state that a thread holds, in four runs of four
+constexpr int kAtOnce = 2;      // and gone through in one go
 constexpr int kCols = 4;        // and columns
+constexpr int kLoaders = 128;   // threads that stage the next steps meanwhile
 constexpr int kStepThreads = 256;
 
 // exp(g) by fp32 numbers that have it as their mean: `up` is due `share` / 2^32 of
@@ -38,117 +40,256 @@ __device__ Decay split_decay(float g) {
   return d;
 }
 
-// The recurrence step by step in fp32: one CTA per problem, sequence and head,
-// the state in registers, 16 x 4 of it per thread.  Threads of `groups`
-// neighbouring lanes hold the rows of the same columns.
-template <typename T>
-__global__ void __launch_bounds__(256)
-plain_kernel(const __grid_constant__ Call call, int groups) {
+// Threads that an SM's registers are shared among: two CTAs where heads are narrow.
+__host__ __device__ constexpr int most_threads(int runs) { return runs == 4 ? 512 : 640; }
+
+// Shared memory of the plain kernel: three tiles of steps, two of them on their way.
+constexpr int kTiles = 3;
+struct Tile {
+  int rows, cols;
+  float* at;
+  __device__ float* x(int buf) const { return at + buf * kTile * (2 * rows + cols); }
+  __device__ float* y(int buf) const { return x(buf) + kTile * rows; }
+  __device__ float* z(int buf) const { return y(buf) + kTile * rows; }
+};
+
+// The recurrence step by step in fp32: one CTA per problem, segment, sequence and
+// head, the state in registers, RUNS runs of four rows by four columns per thread.  Threads of `groups`
+// neighbouring lanes hold the rows of the same columns.  A few steps at a
+// time: what they read and the sums over their rows do not wait for one another, only
+// the state itself does.  The last kLoaders threads stage the next tile.
+// Instruction issue bounds it: three fp32 instructions per element of the state and
+// step.  Packed pairs (fma.rn.f32x2) issue at half the rate here and need moves:
+// 16 x 2048 x 8 heads of 128 x 128 took 1000 us.
+template <typename T, int RUNS, bool OUT>
+__global__ void __launch_bounds__(most_threads(RUNS))
+plain_kernel(const __grid_constant__ Call call, const __grid_constant__ Cut cut, int groups) {
+  constexpr int kRows = 4 * RUNS;
   extern __shared__ __align__(16) float smem[];
+  __shared__ Decay decay;
+  __shared__ float multiplier[kTiles][kTile];
   admit_successor();
   after_predecessor();
-  const int64_t rows_all = call.batch * call.heads;
-  const Problem& p = call.p[blockIdx.x / rows_all];
-  const int64_t bh = blockIdx.x % rows_all, b = bh / call.heads, h = bh % call.heads;
+  const int workers = blockDim.x - kLoaders;
+  const bool loads = (int)threadIdx.x >= workers;
+  const Problem& p = call.p[blockIdx.x % call.problems];
+  const int64_t rest = blockIdx.x / call.problems;
+  const int seg = (int)(rest % cut.launched);
+  const int64_t bh = rest / cut.launched, b = bh / call.heads, h = bh % call.heads;
+  const int64_t which = bh * call.problems + blockIdx.x % call.problems;
   const int64_t len = length_of(call, b);
-  __shared__ Decay decay;
-  if (threadIdx.x == 0) decay = split_decay(decay_of(call, h));
-  const int rows = groups * kRows, cols = (p.c + kCols - 1) / kCols * kCols;
-  float* sx = smem;
-  float* sy = sx + kTile * rows;
-  float* sz = sy + kTile * rows;
-  float* sm = sz + kTile * cols;
-  const int group = threadIdx.x % groups, c0 = threadIdx.x / groups * kCols;
-  const bool holds = c0 < cols;
-  const T* x = static_cast<const T*>(p.x) + b * p.xs.b + h * p.xs.h;
-  const T* y = static_cast<const T*>(p.y) + b * p.ys.b + h * p.ys.h;
-  const T* z = static_cast<const T*>(p.z) + b * p.zs.b + h * p.zs.h;
-  T* out = static_cast<T*>(p.out) + b * p.os.b + h * p.os.h;
+  const float g = decay_of(call, h);
+  if (threadIdx.x == 0) decay = split_decay(g);
+  // this segment's steps [first, last) in time, and how many of the sequence come
+  // before them in the recurrence's order
+  const int place = p.reversed ? cut.segments - 1 - seg : seg;
+  const int64_t first = min(len, place * cut.steps);
+  const int64_t last = min(len, (place + 1) * cut.steps);
+  const int64_t count = last - first, done = p.reversed ? len - last : first;
+  const Tile tile = {groups * kRows, (p.c + kCols - 1) / kCols * kCols, smem};
   const uint8_t* resets = call.resets ? call.resets + b * call.steps : nullptr;
+  const auto step_of = [&](int64_t k) { return p.reversed ? last - 1 - k : first + k; };
+
+  // steps k0 .. of the segment, rows and columns and steps past the end as zeros
+  bool fresh = false;  // a document started in what this thread has seen
+  const auto stage = [&](int64_t k0, int buf) {
+    const int thread = (int)threadIdx.x - workers;
+    const T* x = static_cast<const T*>(p.x) + b * p.xs.b + h * p.xs.h;
+    const T* y = static_cast<const T*>(p.y) + b * p.ys.b + h * p.ys.h;
+    const T* z = static_cast<const T*>(p.z) + b * p.zs.b + h * p.zs.h;
+    const int n = count - k0 < kTile ? (int)(count - k0) : kTile;
+    const auto copy = [&](const T* from, int64_t stride, int width, int wide, float* to) {
+      if (std::is_same<T, float>::value) {
+        // asynchronous: whole tiles are on their way
+        const bool pieces = width % 4 == 0 && stride % 4 == 0 &&
+                            (reinterpret_cast<uintptr_t>(from) & 15) == 0;
+        const int each = pieces ? 4 : 1, across = wide / each;
+        const int i = thread % across * each, per = kLoaders / across;
+        if (thread >= per * across) return;
+        for (int k = thread / across; k < kTile; k += per) {
+          const bool there = k < n && i < width;
+          const T* src = there ? from + step_of(k0 + k) * stride + i : from;
+          const uint32_t dst = tc::smem_u32(to + k * wide + i);
+          if (pieces)
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src),
+                         "r"(there ? 16 : 0)
+                         : "memory");
+          else
+            asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src),
+                         "r"(there ? 4 : 0)
+                         : "memory");
+        }
+      } else {
+        // 16 loads are on their way before the first is stored
+        constexpr int kAhead = 16;
+        const int i = thread % wide, per = kLoaders / wide;
+        if (thread >= per * wide) return;
+        for (int k = thread / wide; k < kTile; k += per * kAhead) {
+          T v[kAhead];
+#pragma unroll
+          for (int u = 0; u < kAhead; ++u) {
+            const int s = k + u * per;
+            v[u] = from[s < n && i < width ? step_of(k0 + s) * stride + i : 0];
+          }
+#pragma unroll
+          for (int u = 0; u < kAhead; ++u) {
+            const int s = k + u * per;
+            if (s < kTile) to[s * wide + i] = s < n && i < width ? to_f32(v[u]) : 0.f;
+          }
+        }
+      }
+    };
+    if (OUT) copy(x, p.xs.t, p.a, tile.rows, tile.x(buf));
+    copy(y, p.ys.t, p.a, tile.rows, tile.y(buf));
+    copy(z, p.zs.t, p.c, tile.cols, tile.z(buf));
+    if (thread < kTile) {
+      float m = 1.f;
+      if (thread < n) {
+        const int64_t t = step_of(k0 + thread);
+        m = decay.at(done + k0 + thread);
+        if (p.reversed) {
+          if (t == len - 1) m = 1.f;
+          else if (resets && resets[t + 1]) m = 0.f;
+        } else if (resets && resets[t]) {
+          m = 0.f;
+        }
+        fresh = fresh || m == 0.f;
+      }
+      multiplier[buf][thread] = m;
+    }
+  };
 
   // row of register r: runs of four, `groups` runs apart
+  const int group = threadIdx.x % groups, c0 = threadIdx.x / groups * kCols;
+  const bool holds = !loads && c0 < tile.cols;
   const auto row_of = [&](int r) { return (r / 4 * groups + group) * 4 + r % 4; };
+  const bool joined = cut.segments > 1 && seg > 0;
+  const float* from = joined ? cut.starts + (which * cut.segments + seg) * call.state
+                      : p.s_in ? p.s_in + bh * call.state : nullptr;
+  if (!OUT) from = nullptr;  // what the segment adds
+  const int64_t from_row = joined ? p.c : p.in_row, from_col = joined ? 1 : p.in_col;
   float S[kRows][kCols];
 #pragma unroll
   for (int r = 0; r < kRows; ++r)
 #pragma unroll
     for (int j = 0; j < kCols; ++j) {
       const int i = row_of(r), c = c0 + j;
-      S[r][j] = p.s_in && i < p.a && c < p.c
-                    ? p.s_in[bh * call.state + i * p.in_row + c * p.in_col]
-                    : 0.f;
+      S[r][j] = from && holds && i < p.a && c < p.c ? from[i * from_row + c * from_col] : 0.f;
     }
+  // of the columns, lane `group` stores those that leave `group` by `groups`
+  bool stores[kCols];
+#pragma unroll
+  for (int j = 0; j < kCols; ++j) stores[j] = holds && j % groups == group && c0 + j < p.c;
 
-  for (int64_t n0 = 0; n0 < len; n0 += kTile) {
-    const int n = len - n0 < kTile ? (int)(len - n0) : kTile;
-    const auto step_of = [&](int k) { return p.reversed ? len - 1 - n0 - k : n0 + k; };
-    __syncthreads();
-    for (int e = threadIdx.x; e < n * rows; e += blockDim.x) {
-      const int k = e / rows, i = e % rows;
-      const int64_t t = step_of(k);
-      sx[e] = i < p.a ? to_f32(x[t * p.xs.t + i]) : 0.f;
-      sy[e] = i < p.a ? to_f32(y[t * p.ys.t + i]) : 0.f;
-    }
-    for (int e = threadIdx.x; e < n * cols; e += blockDim.x) {
-      const int k = e / cols, i = e % cols;
-      sz[e] = i < p.c ? p.f * to_f32(z[step_of(k) * p.zs.t + i]) : 0.f;
-    }
-    if ((int)threadIdx.x < n) {
-      const int64_t t = step_of(threadIdx.x);
-      float m = decay.at(n0 + threadIdx.x);
-      if (p.reversed) {
-        if (t == len - 1) m = 1.f;
-        else if (resets && resets[t + 1]) m = 0.f;
-      } else if (resets && resets[t]) {
-        m = 0.f;
-      }
-      sm[threadIdx.x] = m;
-    }
-    __syncthreads();
-    for (int k = 0; k < n; ++k) {
-      const float m = sm[k];
-      float o[kCols] = {0.f, 0.f, 0.f, 0.f};
-      if (holds) {
-        const float4 v4 = *reinterpret_cast<const float4*>(sz + k * cols + c0);
-        const float v[kCols] = {v4.x, v4.y, v4.z, v4.w};
-        if (m == 0.f) {  // nothing passes, whatever it is
-#pragma unroll
-          for (int r = 0; r < kRows; ++r)
-#pragma unroll
-            for (int j = 0; j < kCols; ++j) S[r][j] = 0.f;
-        }
-#pragma unroll
-        for (int q = 0; q < kRows / 4; ++q) {
-          const int at = k * rows + (q * groups + group) * 4;
-          const float4 y4 = *reinterpret_cast<const float4*>(sy + at);
-          const float4 x4 = *reinterpret_cast<const float4*>(sx + at);
-          const float yr[4] = {y4.x, y4.y, y4.z, y4.w}, xr[4] = {x4.x, x4.y, x4.z, x4.w};
-#pragma unroll
-          for (int r = 0; r < 4; ++r)
-#pragma unroll
-            for (int j = 0; j < kCols; ++j) {
-              float& s = S[4 * q + r][j];
-              s = fmaf(m, s, yr[r] * v[j]);
-              o[j] = fmaf(xr[r], s, o[j]);
-            }
-        }
-      }
-      for (int s = 1; s < groups; s <<= 1)
-#pragma unroll
-        for (int j = 0; j < kCols; ++j) o[j] += __shfl_xor_sync(0xffffffffu, o[j], s);
-      if (holds) {
-        T* to = out + step_of(k) * p.os.t + c0;
-#pragma unroll
-        for (int j = 0; j < kCols; ++j)
-          if (j % groups == group && c0 + j < p.c) to[j] = from_f32<T>(p.g * o[j]);
-      }
-    }
+  __syncthreads();  // the decay
+  T* out = static_cast<T*>(p.out) + b * p.os.b + h * p.os.h;
+  const auto arrived = [&](bool all) {  // this thread's copies, but those of the last tile
+    if (all) asm volatile("cp.async.wait_all;" ::: "memory");
+    else asm volatile("cp.async.wait_group 1;" ::: "memory");
+  };
+  const auto stage_next = [&](int64_t k0, int buf) {
+    if (k0 < count) stage(k0, buf);
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  if (loads) {
+    stage_next(0, 0);
+    stage_next(kTile, 1);
+    arrived(false);
   }
-  // past the end
-  for (int64_t e = len * p.c + threadIdx.x; e < call.steps * p.c; e += blockDim.x)
-    out[e / p.c * p.os.t + e % p.c] = from_f32<T>(0.f);
-  if (!p.s_out || !holds) return;
-  const float last = !p.reversed || len == 0 ? 1.f : resets && resets[0] ? 0.f : decay.at(len);
+  __syncthreads();
+  int buf = 0;
+  for (int64_t k0 = 0; k0 < count; k0 += kTile) {
+    if (loads) {
+      stage_next(k0 + 2 * kTile, (buf + 2) % kTiles);
+      arrived(false);
+    } else {
+      const int n = count - k0 < kTile ? (int)(count - k0) : kTile;
+      for (int k = 0; k < n; k += kAtOnce) {
+        float o[kAtOnce][kCols];
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+          const float m = multiplier[buf][k + u];
+          const float4 v4 = holds ? *reinterpret_cast<const float4*>(tile.z(buf) + (k + u) * tile.cols + c0)
+                                  : make_float4(0.f, 0.f, 0.f, 0.f);
+          const float v[kCols] = {p.f * v4.x, p.f * v4.y, p.f * v4.z, p.f * v4.w};
+          if (m == 0.f) {  // nothing passes, whatever it is
+#pragma unroll
+            for (int r = 0; r < kRows; ++r)
+#pragma unroll
+              for (int j = 0; j < kCols; ++j) S[r][j] = 0.f;
+          }
+#pragma unroll
+          for (int j = 0; j < kCols; ++j) o[u][j] = 0.f;
+#pragma unroll
+          for (int q = 0; q < RUNS; ++q) {
+            const int at = (k + u) * tile.rows + (q * groups + group) * 4;
+            const float4 y4 = *reinterpret_cast<const float4*>(tile.y(buf) + at);
+            const float yr[4] = {y4.x, y4.y, y4.z, y4.w};
+            float xr[4];
+            if (OUT) {
+              const float4 x4 = *reinterpret_cast<const float4*>(tile.x(buf) + at);
+              xr[0] = x4.x; xr[1] = x4.y; xr[2] = x4.z; xr[3] = x4.w;
+            }
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+              for (int j = 0; j < kCols; ++j) {
+                float& s = S[4 * q + r][j];
+                s = fmaf(m, s, yr[r] * v[j]);
+                if (OUT) o[u][j] = fmaf(xr[r], s, o[u][j]);
+              }
+          }
+        }
+        if (OUT) {
+          for (int s = 1; s < groups; s <<= 1)
+#pragma unroll
+            for (int u = 0; u < kAtOnce; ++u)
+#pragma unroll
+              for (int j = 0; j < kCols; ++j) o[u][j] += __shfl_xor_sync(0xffffffffu, o[u][j], s);
+#pragma unroll
+          for (int u = 0; u < kAtOnce; ++u) {
+            T* to = out + step_of(k0 + k + u) * p.os.t + c0;
+#pragma unroll
+            for (int j = 0; j < kCols; ++j)
+              if (stores[j] && k + u < n) to[j] = from_f32<T>(p.g * o[u][j]);
+          }
+        }
+      }
+    }
+    __syncthreads();
+    buf = (buf + 1) % kTiles;
+  }
+  if (loads) arrived(true);
+
+  if (!OUT) {
+    // what the segment adds, and what it leaves of the state before it: the
+    // reversed recurrence's decays come one step later
+    const bool any = __syncthreads_or(fresh) != 0;
+    float* to = cut.starts + (which * cut.segments + seg + 1) * call.state;
+    if (threadIdx.x == 0) {
+      const int64_t decays = p.reversed && last == len && count > 0 ? count - 1 : count;
+      const Fade f = fade_of(g, (float)decays);
+      cut.fades[which * cut.segments + seg] = any ? make_float2(0.f, 0.f)
+                                                  : make_float2(f.keep, f.change);
+    }
+    if (holds)
+#pragma unroll
+      for (int r = 0; r < kRows; ++r)
+#pragma unroll
+        for (int j = 0; j < kCols; ++j) {
+          const int i = row_of(r), c = c0 + j;
+          if (i < p.a && c < p.c && SOMA_CHECK(seg + 1 < cut.segments, call.status))
+            to[i * p.c + c] = S[r][j];
+        }
+    return;
+  }
+  // past the end, this segment's share
+  const int64_t begin = max(len, place * cut.steps);
+  const int64_t end = min(call.steps, (place + 1) * cut.steps);
+  for (int64_t e = threadIdx.x; e < (end - begin) * p.c; e += blockDim.x)
+    out[(begin + e / p.c) * p.os.t + e % p.c] = from_f32<T>(0.f);
+  if (!p.s_out || !holds || seg != cut.segments - 1) return;
+  const float left = !p.reversed || len == 0 ? 1.f : resets && resets[0] ? 0.f : decay.at(len);
 #pragma unroll
   for (int r = 0; r < kRows; ++r)
 #pragma unroll
@@ -156,8 +297,38 @@ plain_kernel(const __grid_constant__ Call call, int groups) {
       const int i = row_of(r), c = c0 + j;
       if (i < p.a && c < p.c)
         p.s_out[bh * call.state + i * p.out_row + c * p.out_col] =
-            last == 0.f ? 0.f : last * S[r][j];
+            left == 0.f ? 0.f : left * S[r][j];
     }
+}
+
+// Turns the segments' states into those that they start from, in place: state
+// s + 1 is what segment s adds to what it leaves of state s.
+__global__ void __launch_bounds__(256)
+join_kernel(const __grid_constant__ Call call, const __grid_constant__ Cut cut) {
+  admit_successor();
+  after_predecessor();
+  const int64_t which = blockIdx.y, bh = which / call.problems;
+  const Problem& p = call.p[which % call.problems];
+  const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (e >= call.state) return;
+  const int64_t i = e / p.c, c = e % p.c;
+  float s = p.s_in ? p.s_in[bh * call.state + i * p.in_row + c * p.in_col] : 0.f;
+  float* at = cut.starts + which * cut.segments * call.state + e;
+  const float2* fades = cut.fades + which * cut.segments;
+  constexpr int kAhead = 8;
+  for (int k0 = 1; k0 < cut.segments; k0 += kAhead) {
+    float add[kAhead];
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j)
+      add[j] = k0 + j < cut.segments ? at[(k0 + j) * call.state] : 0.f;
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j)
+      if (k0 + j < cut.segments) {
+        const float2 f = fades[k0 + j - 1];
+        s = f.x == 0.f ? add[j] : fmaf(f.x, s, fmaf(f.y, s, add[j]));
+        at[(k0 + j) * call.state] = s;
+      }
+  }
 }
 
 // One token: a CTA per sequence and head, V adjacent columns per thread, the rows
@@ -267,20 +438,57 @@ bool overlap(const float* p, const float* q, int64_t count) {
   return (a < b ? b - a : a - b) < (uintptr_t)count * sizeof(float);
 }
 
-template <typename T>
-cudaError_t plain(const Call& call, cudaStream_t st) {
-  int widest = 0, wide_c = 0;
-  for (int k = 0; k < call.problems; ++k) {
-    if (call.p[k].a > widest) widest = call.p[k].a;
-    if (call.p[k].c > wide_c) wide_c = call.p[k].c;
+// Threads of a CTA of the plain kernel: `groups` of them share columns, each with
+// `runs` runs of four rows, as few as hold all rows.
+struct Spread {
+  int groups, runs, cols;
+};
+Spread spread_of(int rows, int columns) {
+  Spread s = {1, 0, (columns + kCols - 1) / kCols * kCols};
+  while (s.groups * 16 < rows) s.groups *= 2;
+  s.runs = (rows + 4 * s.groups - 1) / (4 * s.groups);
+  return s;
+}
+int threads_of(const Spread& s) { return (s.groups * (s.cols / kCols) + 31) / 32 * 32 + kLoaders; }
+
+template <typename T, int RUNS>
+cudaError_t plain(const Call& call, Cut cut, const Spread& s, cudaStream_t st) {
+  const size_t smem = sizeof(float) * kTiles * kTile * (2 * s.groups * 4 * RUNS + s.cols);
+  constexpr int most = sizeof(float) * kTiles * kTile * (2 * 128 + 128);
+  static const cudaError_t set = [] {
+    const cudaError_t e = cudaFuncSetAttribute(plain_kernel<T, RUNS, true>,
+                                               cudaFuncAttributeMaxDynamicSharedMemorySize, most);
+    return e != cudaSuccess ? e
+                            : cudaFuncSetAttribute(plain_kernel<T, RUNS, false>,
+                                                   cudaFuncAttributeMaxDynamicSharedMemorySize, most);
+  }();
+  if (set != cudaSuccess) return set;
+  const int64_t rows = call.problems * call.batch * call.heads;
+  if (cut.segments > 1) {
+    cut.launched = cut.segments - 1;
+    cudaError_t e = launch_overlapped(plain_kernel<T, RUNS, false>,
+                                      dim3((unsigned)(rows * cut.launched)), threads_of(s), smem, st,
+                                      call, cut, s.groups);
+    if (e == cudaSuccess) e = launch_join(call, cut, st);
+    if (e != cudaSuccess) return e;
   }
-  int groups = 1;
-  while (groups * kRows < widest) groups *= 2;
-  const int cols = (wide_c + kCols - 1) / kCols * kCols;
-  const int threads = (groups * (cols / kCols) + 31) / 32 * 32;
-  const size_t smem = sizeof(float) * (kTile * (2 * groups * kRows + cols) + kTile);
-  return launch_overlapped(plain_kernel<T>, dim3((unsigned)(call.problems * call.batch * call.heads)),
-                           threads, smem, st, call, groups);
+  cut.launched = cut.segments;
+  return launch_overlapped(plain_kernel<T, RUNS, true>, dim3((unsigned)(rows * cut.segments)),
+                           threads_of(s), smem, st, call, cut, s.groups);
+}
+
+template <typename T>
+cudaError_t plain(const Call& call, const Cut& cut, cudaStream_t st) {
+  int rows = 0, columns = 0;
+  for (int k = 0; k < call.problems; ++k) {
+    if (call.p[k].a > rows) rows = call.p[k].a;
+    if (call.p[k].c > columns) columns = call.p[k].c;
+  }
+  const Spread s = spread_of(rows, columns);
+  return s.runs == 1   ? plain<T, 1>(call, cut, s, st)
+         : s.runs == 2 ? plain<T, 2>(call, cut, s, st)
+         : s.runs == 3 ? plain<T, 3>(call, cut, s, st)
+                       : plain<T, 4>(call, cut, s, st);
 }
 
 template <typename T>
@@ -298,26 +506,36 @@ bool tiled(const void* p, const soma_attn_strides& s) {
   return aligned(p, 16) && s.b % 8 == 0 && s.t % 8 == 0 && s.h % 8 == 0;
 }
 
-// The cut with the least estimated time, in chunks of one CTA: states of all
-// segments but the last first (half the work of a chunk), then the outputs.
+// The cut with the least estimated time, in units of one CTA's work: a chunk on
+// the tensor cores, a tile of steps elsewhere.  The states of all segments but
+// the last come first (half the work), then the outputs; a CTA's begin and end
+// take about two units, the join between the launches as much.
 Cut cut_of(const soma_attn_dims& d, int dtype, int problems) {
+  const bool chunked = dtype != SOMA_FP32 && d.key_dim % 8 == 0 && d.value_dim % 8 == 0;
+  const int unit = chunked ? kChunk : kTile, ends = 2;
+  int64_t resident = 152;
+  if (chunked) {
+    if (d.key_dim <= 64 && d.value_dim <= 64) resident = 304;
+  } else {
+    const int wide = d.key_dim > d.value_dim ? d.key_dim : d.value_dim;
+    const Spread s = spread_of(problems > 1 ? wide : d.key_dim, problems > 1 ? wide : d.value_dim);
+    resident *= most_threads(s.runs) / threads_of(s);
+  }
   Cut best = {};
   best.segments = 1;
-  best.chunks = (d.steps + kChunk - 1) / kChunk;
-  if (dtype == SOMA_FP32 || d.key_dim % 8 || d.value_dim % 8) return best;
-  const int64_t rows = d.batch * d.heads * problems, chunks = best.chunks;
-  const int64_t resident = d.key_dim <= 64 && d.value_dim <= 64 ? 304 : 152;
+  const int64_t rows = d.batch * d.heads * problems, units = (d.steps + unit - 1) / unit;
+  best.steps = units * unit;
   const auto waves = [&](int64_t n) { return (double)((n + resident - 1) / resident); };
-  double least = waves(rows) * (chunks + 2);
-  for (int64_t n = 2; n <= chunks && n <= 1024; ++n) {
-    const int64_t each = (chunks + n - 1) / n;
-    if ((chunks + each - 1) / each != n) continue;
+  double least = waves(rows) * (units + ends);
+  for (int64_t n = 2; n <= units && n <= 1024; ++n) {
+    const int64_t each = (units + n - 1) / n;
+    if ((units + each - 1) / each != n) continue;
     const double cost =
-        waves(rows * n) * (each + 2) + waves(rows * (n - 1)) * (0.5 * each + 2) + 4;
+        waves(rows * n) * (each + ends) + waves(rows * (n - 1)) * (0.5 * each + ends) + 2 * ends;
     if (cost < least) {
       least = cost;
       best.segments = (int32_t)n;
-      best.chunks = each;
+      best.steps = each * unit;
     }
   }
   return best;
@@ -351,9 +569,9 @@ cudaError_t run(const Call& call, const Cut& cut, int dtype, cudaStream_t st) {
   }
   cudaError_t e;
   if (chunked && launch_chunks(call, cut, dtype, st, &e)) return e;
-  return dtype == SOMA_FP32   ? plain<float>(call, st)
-         : dtype == SOMA_BF16 ? plain<__nv_bfloat16>(call, st)
-                              : plain<__half>(call, st);
+  return dtype == SOMA_FP32   ? plain<float>(call, cut, st)
+         : dtype == SOMA_BF16 ? plain<__nv_bfloat16>(call, cut, st)
+                              : plain<__half>(call, cut, st);
 }
 
 Call make_call(const soma_attn_dims& d, const float* log_decay, const int32_t* lengths,
@@ -396,6 +614,13 @@ void put_states(Problem* p, const soma_attn_dims& d, bool turned, const float* i
 }
 
 }  // namespace
+
+cudaError_t launch_join(const Call& call, const Cut& cut, cudaStream_t st) {
+  const unsigned rows = (unsigned)(call.batch * call.heads * call.problems);
+  return launch_overlapped(join_kernel, dim3((unsigned)((call.state + 255) / 256), rows), 256, 0, st,
+                           call, cut);
+}
+
 }  // namespace attn
 }  // namespace soma
 

@@ -52,15 +52,36 @@ struct Call {
 };
 
 // Steps of a chunk of the tensor-core kernels, and how the steps of a call are
-// cut into segments of whole chunks.
+// cut into segments (there, of whole chunks).
 constexpr int kChunk = 128;
 struct Cut {
   int32_t segments;
   int32_t launched;  // segments of the launch
-  int64_t chunks;    // of a segment
+  int64_t steps;     // of a segment
   float* starts;     // [batch * heads][problems][segments] states; where segments > 1
   float2* fades;     // ... what a segment keeps of the state before it
 };
+
+// exp(e g) with the product's rounding carried along.
+__device__ __forceinline__ float power_of(float g, float e) {
+  if (e == 0.f) return 1.f;
+  const float y = g * e;
+  if (y < -104.f) return 0.f;
+  return expf(y) * (1.f + fmaf(g, e, -y));
+}
+// S times exp(e g) is keep S + change S, so written that its error is 2^-24 of
+// what is taken off where that is little: over many chunks it adds up.
+struct Fade {
+  float keep, change;
+};
+__device__ __forceinline__ Fade fade_of(float g, float e) {
+  const float y = g * e;
+  if (!(y > -0.5f)) return {power_of(g, e), 0.f};
+  return {1.f, expm1f(y) + fmaf(g, e, -y)};
+}
+
+// Joins the segments' states of `call` (after the launch that made them).
+cudaError_t launch_join(const Call& call, const Cut& cut, cudaStream_t st);
 
 // The recurrences of a call on the tensor cores (16-bit types; widths, strides
 // and addresses of whole 16-byte pieces; steps > 0).  False, and nothing is

@@ -55,8 +55,8 @@ struct Layout {
   // Registers of a thread, of each kind of warps.  All were launched with `launched`
   // (what ptxas takes from the launch bounds), and the sums must not exceed that.
   static constexpr int launched = W == 64 ? 80 : 96;
-  static constexpr int out_regs = 96, state_regs = W == 64 ? 104 : 128;
-  static constexpr int rest_regs = W == 64 ? 40 : 32;
+  static constexpr int out_regs = W == 64 ? 80 : 88, state_regs = W == 64 ? 112 : 128;
+  static constexpr int rest_regs = W == 64 ? 48 : 40;
   static_assert(32 * (group * (out_regs + state_regs) + 4 * rest_regs) <= threads * launched,
                 "setmaxnreg would wait for registers that the CTA does not have");
   // Columns of the state of a thread of the states' group.  64 rows fill half of
@@ -202,24 +202,6 @@ __device__ __forceinline__ float reciprocal(float scale) {  // of a power of two
   return __uint_as_float((254u << 23) - __float_as_uint(scale));
 }
 
-// exp(e g) with the product's rounding carried along.
-__device__ __forceinline__ float power_of(float g, float e) {
-  if (e == 0.f) return 1.f;
-  const float y = g * e;
-  if (y < -104.f) return 0.f;
-  return expf(y) * (1.f + fmaf(g, e, -y));
-}
-// S times exp(e g) is keep S + change S, so written that its error is 2^-24 of
-// what is taken off where that is little: over many chunks it adds up.
-struct Fade {
-  float keep, change;
-};
-__device__ __forceinline__ Fade fade_of(float g, float e) {
-  const float y = g * e;
-  if (!(y > -0.5f)) return {power_of(g, e), 0.f};
-  return {1.f, expm1f(y) + fmaf(g, e, -y)};
-}
-
 // Which steps of a chunk start a document, as bits.
 struct Starts {
   uint32_t m[4];
@@ -307,8 +289,8 @@ chunk_kernel(const __grid_constant__ Sources sources, const __grid_constant__ Ca
   // this segment's chunks [first, last) in time
   const int place = reversed ? cut.segments - 1 - seg : seg;
   const int all = (int)(((int64_t)len + kChunk - 1) / kChunk);
-  const int first = min(all, place * (int)cut.chunks);
-  const int last = min(all, first + (int)cut.chunks);
+  const int chunks = (int)(cut.steps / kChunk);
+  const int first = min(all, place * chunks), last = min(all, first + chunks);
   const int count = last - first;
   const bool final_one = seg == cut.segments - 1;
   // whether the state after the segment is wanted; of each chunk but the last it is
@@ -341,7 +323,7 @@ chunk_kernel(const __grid_constant__ Sources sources, const __grid_constant__ Ca
 
   if (warp < L::group) {
     // ---- outputs -------------------------------------------------------------
-    more_registers<L::out_regs>();
+    fewer_registers<L::out_regs>();
     // No worker leaves early, as they meet at named barriers.
     if (OUT) {
       const int quarter = warp % 4, half = warp / 4;
@@ -472,42 +454,39 @@ chunk_kernel(const __grid_constant__ Sources sources, const __grid_constant__ Ca
         tc::tc_fence_after();
         T* const to = out + (t0 + row) * p.os.t + half * kCols;
 #pragma unroll
-        for (int c = 0; c < kCols; c += 32) {
+        for (int c = 0; c < kCols; c += 16) {
           const int col = half * kCols + c;
-          float v0[32], v1[32];
-          uint32_t u0[16];
-          tc::tmem_ld32_nowait(lanes + L::o1 + col, v0);
-          tc::tmem_ld32_nowait(lanes + L::o2 + col, v1);
-          tc::tmem_wait_ld32(v0);
-          tc::tmem_wait_ld32(v1);
+          float o1[16], o2[16];
+          tc::tmem_ld16(lanes + L::o1 + col, o1);
+          tc::tmem_ld16(lanes + L::o2 + col, o2);
+          uint32_t u[8];
 #pragma unroll
-          for (int j = 0; j < 32; ++j) {
-            const float own = kHalfType ? v1[j] * back : v1[j];
-            v0[j] = sees ? fmaf(r, v0[j], own) : own;
-          }
-          pack(1.f, v0, u0);
-          if (row < n && SOMA_CHECK(t0 + row < call.steps && p.c % 8 == 0, status))
+          for (int j = 0; j < 8; ++j) {
+            float v[2];
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-              const uint32_t u[8] = {u0[8 * i],     u0[8 * i + 1], u0[8 * i + 2], u0[8 * i + 3],
-                                     u0[8 * i + 4], u0[8 * i + 5], u0[8 * i + 6], u0[8 * i + 7]};
-              const int from = col + 16 * i;
-              T* at = to + c + 16 * i;
-              if (wide && from + 16 <= p.c) {
-                store32(at, u);
-              } else {
-                if (from + 8 <= p.c)
-                  *reinterpret_cast<uint4*>(at) = make_uint4(u[0], u[1], u[2], u[3]);
-                if (from + 16 <= p.c)
-                  *reinterpret_cast<uint4*>(at + 8) = make_uint4(u[4], u[5], u[6], u[7]);
-              }
+              const float own = kHalfType ? o2[2 * j + i] * back : o2[2 * j + i];
+              v[i] = sees ? fmaf(r, o1[2 * j + i], own) : own;
             }
+            u[j] = pack2<T>(v[0], v[1]);
+          }
+          if (row < n && SOMA_CHECK(t0 + row < call.steps && p.c % 8 == 0, status)) {
+            T* at = to + c;
+            if (wide && col + 16 <= p.c) {
+              store32(at, u);
+            } else {
+              if (col + 8 <= p.c)
+                *reinterpret_cast<uint4*>(at) = make_uint4(u[0], u[1], u[2], u[3]);
+              if (col + 16 <= p.c)
+                *reinterpret_cast<uint4*>(at + 8) = make_uint4(u[4], u[5], u[6], u[7]);
+            }
+          }
         }
         tc::tc_fence_before();
         arrive(&sh.o_free);
       }
       // rows past the sequence's end, this segment's share of them
-      const int64_t share = cut.chunks * kChunk;
+      const int64_t share = cut.steps;
       const int64_t from_step = max((int64_t)len, place * share);
       const int64_t to_step = min(call.steps, (place + 1) * share);
       const int per = p.c / 8;
@@ -842,36 +821,6 @@ chunk_kernel(const __grid_constant__ Sources sources, const __grid_constant__ Ca
   if (warp == L::issuer) tc::tmem_dealloc(tmem, L::columns);
 }
 
-// Turns the segments' states into those that they start from, in place: state
-// s + 1 is what segment s adds to what it leaves of state s.
-__global__ void __launch_bounds__(256)
-join_kernel(const __grid_constant__ Call call, const __grid_constant__ Cut cut) {
-  admit_successor();
-  after_predecessor();
-  const int64_t which = blockIdx.y, bh = which / call.problems;
-  const Problem& p = call.p[which % call.problems];
-  const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (e >= call.state) return;
-  const int64_t i = e / p.c, c = e % p.c;
-  float s = p.s_in ? p.s_in[bh * call.state + i * p.in_row + c * p.in_col] : 0.f;
-  float* at = cut.starts + which * cut.segments * call.state + e;
-  const float2* fades = cut.fades + which * cut.segments;
-  constexpr int kAhead = 8;
-  for (int k0 = 1; k0 < cut.segments; k0 += kAhead) {
-    float add[kAhead];
-#pragma unroll
-    for (int j = 0; j < kAhead; ++j)
-      add[j] = k0 + j < cut.segments ? at[(k0 + j) * call.state] : 0.f;
-#pragma unroll
-    for (int j = 0; j < kAhead; ++j)
-      if (k0 + j < cut.segments) {
-        const float2 f = fades[k0 + j - 1];
-        s = f.x == 0.f ? add[j] : fmaf(f.x, s, fmaf(f.y, s, add[j]));
-        at[(k0 + j) * call.state] = s;
-      }
-  }
-}
-
 // ------------------------------------------------------------------- host --
 
 // The tensor map of a tensor, if one of the forms describes it: strides are
@@ -942,8 +891,7 @@ cudaError_t launch(const Sources& sources, const Call& call, Cut cut, cudaStream
     cudaError_t e = launch_overlapped(chunk_kernel<T, W, false>, dim3((unsigned)(rows * cut.launched)),
                                       Layout<W>::threads, smem, st, sources, call, cut);
     if (e != cudaSuccess) return e;
-    e = launch_overlapped(join_kernel, dim3((unsigned)((call.state + 255) / 256), (unsigned)rows), 256,
-                          0, st, call, cut);
+    e = launch_join(call, cut, st);
     if (e != cudaSuccess) return e;
   } else {
     cut.starts = nullptr;
