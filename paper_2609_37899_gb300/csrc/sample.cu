@@ -2,7 +2,8 @@
 // from given random numbers (soma_sample in include/soma_api.h).
 //
 // A cluster of up to eight CTAs shares a row, each with a part of the vocabulary
-// that stays in L2 over the passes.  The ranking is never made: top-k and top-p
+// in its shared memory, so that the logits are read once (above 131,064 of them,
+// from L2 or memory in every pass).  The ranking is never made: top-k and top-p
 // each need one cut in it, which is found as a radix selection finds it, by
 // counts (or weights) per bin, the bin that the cut lies in, then finer bins of
 // that one.  The first bins are equal steps of (max - l) / T: there the weights
@@ -30,6 +31,8 @@ using u64 = unsigned long long;
 constexpr int kBins = 2048;
 constexpr int kMaxCluster = 8;
 constexpr int64_t kMaxPart = 1 << 17;      // elements of a CTA: sums of 14-bit parts fit 32 bits
+constexpr int kSlots = 24;                 // exchanges between the CTAs of a row
+constexpr int kHeld = 32;                  // logits of a thread that shared memory holds
 constexpr float kDeepest = 28.5f;          // 2^40 exp(-28.42) = 1/2: weights further down are 0
 constexpr float kStep = kDeepest / kBins;
 constexpr float kLeastTemperature = 0x1p-100f, kMostTemperature = 0x1p100f;
@@ -120,13 +123,18 @@ struct Sample {
   float* logprobs;
 };
 
+// Logits of a thread: neighbouring ones, in eights.
+__host__ __device__ constexpr int each_of(int part, int threads) {
+  return (part + 8 * threads - 1) / (8 * threads) * 8;
+}
+
 template <int THREADS>
-struct Shared {
-  uint32_t hist[2][3][kBins];  // two, so that one is read while the other is filled
+struct __align__(16) Shared {
+  uint32_t hist[3][kBins];
   float2 roots[64];
-  u64 slot[12][3];             // sums of this CTA, for the others
+  u64 slot[kSlots][3];         // sums of this CTA, for the others
   u64 part[3][THREADS / 32];
-  float fpart[2][THREADS / 32];
+  float fpart[THREADS / 32];
   float2 inv;
   u64 found[3];
   int lo, hi;
@@ -147,6 +155,9 @@ __device__ __forceinline__ uint32_t remote32(const uint32_t* p, uint32_t rank) {
   asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(at_rank(p, rank)) : "memory");
   return v;
 }
+__device__ __forceinline__ void set_remote64(u64* p, uint32_t rank, u64 v) {
+  asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(at_rank(p, rank)), "l"(v) : "memory");
+}
 __device__ __forceinline__ u64 remote64(const u64* p, uint32_t rank) {
   u64 v;
   asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(at_rank(p, rank)) : "memory");
@@ -154,7 +165,7 @@ __device__ __forceinline__ u64 remote64(const u64* p, uint32_t rank) {
 }
 
 // One row's work in one CTA.
-template <typename T, int THREADS>
+template <typename T, int THREADS, bool HELD>
 struct Row {
   using S = Shared<THREADS>;
   static constexpr int kWarps = THREADS / 32;
@@ -164,7 +175,7 @@ struct Row {
   int shift, end;      // end: one behind the last logit, counted from `row`
   int first, stop;     // this thread's
   uint32_t rank, ranks;
-  int slots = 0, buf = 0;
+  int slots = 0;
   float max = 0.f, inv = 0.f;
   float2 inv2 = {0.f, 0.f};
   uint32_t cut = 0;    // what is ranked above this key remains, and ...
@@ -172,20 +183,73 @@ struct Row {
 
   __device__ Row(S& s) : sh(s) {}
 
+  // Eight logits in shared memory: 16-byte pieces of neighbouring threads side by
+  // side.  What lies outside the row is -infinity.
+  static constexpr int kPieces = sizeof(T) / 2;
+  uint4* held;
+  __device__ __forceinline__ void hold(int group, const float (&v)[8]) {
+    union {
+      T t[8];
+      uint4 u[kPieces];
+    } w;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) w.t[j] = from_f32<T>(v[j]);  // exact
+#pragma unroll
+    for (int k = 0; k < kPieces; ++k)
+      held[(group * kPieces + k) * THREADS + threadIdx.x] = w.u[k];
+  }
+  __device__ __forceinline__ void load(int i, float (&v)[8]) const {
+    if (HELD) {
+      union {
+        T t[8];
+        uint4 u[kPieces];
+      } w;
+      const int group = (i - first) / 8;
+#pragma unroll
+      for (int k = 0; k < kPieces; ++k)
+        w.u[k] = held[(group * kPieces + k) * THREADS + threadIdx.x];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = to_f32(w.t[j]);
+    } else {
+      fetch(i, v);
+    }
+  }
+  __device__ __forceinline__ void fetch(int i, float (&v)[8]) const {
+    if (i >= shift && i + 8 <= end) {
+      load8(row + i, v);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        v[j] = i + j >= shift && i + j < end ? to_f32(row[i + j]) : -INFINITY;
+    }
+  }
   // f(logit, index from `row`) for this thread's logits in order.
   template <typename F>
   __device__ __forceinline__ void each(F f) const {
     for (int i = first; i < stop; i += 8) {
-      if (i + 8 <= shift) continue;
       float v[8];
-      if (i >= shift && i + 8 <= end) {
-        load8(row + i, v);
+      load(i, v);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) f(v[j], i + j);
-      } else {
-        for (int j = 0; j < 8; ++j)
-          if (i + j >= shift && i + j < end) f(to_f32(row[i + j]), i + j);
-      }
+      for (int j = 0; j < 8; ++j) f(v[j], i + j);
+    }
+  }
+  // The first pass: the same over the logits in memory, which shared memory holds
+  // from then on.
+  template <typename F>
+  __device__ __forceinline__ void first_pass(F f) {
+#pragma unroll
+    for (int g = 0; g < kHeld / 8; g += 2) {
+      float v[2][8];
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+        if (first + 8 * (g + u) < stop) fetch(first + 8 * (g + u), v[u]);
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+        if (first + 8 * (g + u) < stop) {
+          hold(g + u, v[u]);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) f(v[u][j], 0);
+        }
     }
   }
   // f(logit, index, depth) for those whose weight may be above 0; the depth
@@ -254,65 +318,93 @@ struct Row {
     return v;
   }
 
-  // ---- bins ----
+  // ---- bins: those of all CTAs have been read when find() or band() returns ----
   __device__ void clear(int arrays) {
-    buf ^= 1;
     for (int a = 0; a < arrays; ++a)
-      for (int b = threadIdx.x; b < kBins; b += THREADS) sh.hist[buf][a][b] = 0;
+      for (int b = threadIdx.x; b < kBins; b += THREADS) sh.hist[a][b] = 0;
     __syncthreads();
   }
-  __device__ __forceinline__ void count(int b) { atomicAdd(&sh.hist[buf][0][b], 1u); }
+  __device__ __forceinline__ void count(int b) { atomicAdd(&sh.hist[0][b], 1u); }
   // weights go by 14 bits: sums of kMaxPart such numbers fit 32 bits
   __device__ __forceinline__ void add(int b, u64 w) {
-    atomicAdd(&sh.hist[buf][0][b], (uint32_t)w & 0x3fffu);
-    atomicAdd(&sh.hist[buf][1][b], (uint32_t)(w >> 14) & 0x3fffu);
-    atomicAdd(&sh.hist[buf][2][b], (uint32_t)(w >> 28));
+    atomicAdd(&sh.hist[0][b], (uint32_t)w & 0x3fffu);
+    atomicAdd(&sh.hist[1][b], (uint32_t)(w >> 14) & 0x3fffu);
+    atomicAdd(&sh.hist[2][b], (uint32_t)(w >> 28));
   }
   template <bool WEIGHTS>
   __device__ __forceinline__ u64 in_bin(int b) const {
     u64 t = 0;
     for (uint32_t r = 0; r < ranks; ++r) {
-      t += remote32(&sh.hist[buf][0][b], r);
+      t += remote32(&sh.hist[0][b], r);
       if (WEIGHTS) {
-        t += (u64)remote32(&sh.hist[buf][1][b], r) << 14;
-        t += (u64)remote32(&sh.hist[buf][2][b], r) << 28;
+        t += (u64)remote32(&sh.hist[1][b], r) << 14;
+        t += (u64)remote32(&sh.hist[2][b], r) << 28;
       }
     }
     return t;
   }
+  // Every CTA adds up a slice of the bins over all of them.  A thread's bins of it:
+  __device__ __forceinline__ int slice_bins() const {  // 0: none
+    const int per = kBins / (int)ranks;
+    return per >= THREADS ? per / THREADS : (int)threadIdx.x < per ? 1 : 0;
+  }
+  __device__ __forceinline__ int slice_first() const {
+    const int per = kBins / (int)ranks;
+    return (int)rank * per + (int)threadIdx.x * (per >= THREADS ? per / THREADS : 1);
+  }
+  // The sum of `v` over the threads before this one; *all: over all of them.
+  template <typename V>
+  __device__ __forceinline__ V before_me(V v, V* parts, V* all) {
+    V run = v;
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+#pragma unroll
+    for (int k = 1; k < 32; k <<= 1) {
+      const V o = __shfl_up_sync(0xffffffffu, run, k);
+      if (lane >= k) run += o;
+    }
+    if (lane == 31) parts[warp] = run;
+    __syncthreads();
+    run -= v;
+    V total = 0;
+    for (int w = 0; w < kWarps; ++w) {
+      if (w < warp) run += parts[w];
+      total += parts[w];
+    }
+    *all = total;
+    return run;
+  }
   // The bin where the running sum over the row's bins reaches `need` (at least
   // 1), the sum before it and what it holds; false if none does.
   template <bool WEIGHTS>
-  __device__ bool find(u64 need, int* bin, u64* before, u64* held) {
+  __device__ bool find(u64 need, int* bin, u64* before, u64* held_there) {
     if (threadIdx.x == 0) sh.found[0] = ~0ull;
     tc::cluster_sync();
-    u64 own[kOwn], total = 0;
-#pragma unroll
-    for (int j = 0; j < kOwn; ++j) total += own[j] = in_bin<WEIGHTS>(threadIdx.x * kOwn + j);
-    u64 run = total;
-    const int lane = threadIdx.x % 32;
-#pragma unroll
-    for (int k = 1; k < 32; k <<= 1) {
-      const u64 o = __shfl_up_sync(0xffffffffu, run, k);
-      if (lane >= k) run += o;
-    }
-    if (lane == 31) sh.part[0][threadIdx.x / 32] = run;
-    __syncthreads();
-    run -= total;
-    for (int w = 0; w < (int)threadIdx.x / 32; ++w) run += sh.part[0][w];
+    const int bins = slice_bins(), b0 = slice_first();
+    u64 own[kOwn], total = 0, all;
 #pragma unroll
     for (int j = 0; j < kOwn; ++j) {
-      if (run < need && run + own[j] >= need) {
-        sh.found[0] = threadIdx.x * kOwn + j;
-        sh.found[1] = run;
-        sh.found[2] = own[j];
-      }
+      own[j] = j < bins ? in_bin<WEIGHTS>(b0 + j) : 0;
+      total += own[j];
+    }
+    u64 run = before_me(total, sh.part[0], &all);
+    if (threadIdx.x == 0) sh.slot[slots][0] = all;
+    tc::cluster_sync();
+    for (uint32_t r = 0; r < rank; ++r) run += remote64(&sh.slot[slots][0], r);
+    ++slots;
+#pragma unroll
+    for (int j = 0; j < kOwn; ++j) {
+      if (j < bins && run < need && run + own[j] >= need)
+        for (uint32_t r = 0; r < ranks; ++r) {
+          set_remote64(&sh.found[0], r, (u64)(b0 + j));
+          set_remote64(&sh.found[1], r, run);
+          set_remote64(&sh.found[2], r, own[j]);
+        }
       run += own[j];
     }
-    __syncthreads();
+    tc::cluster_sync();
     *bin = (int)sh.found[0];
     *before = sh.found[1];
-    *held = sh.found[2];
+    *held_there = sh.found[2];
     return sh.found[0] != ~0ull;
   }
   // From counts per bin of depth: the bins [lo, hi] one of which is where the
@@ -325,39 +417,42 @@ struct Row {
       sh.hi = kBins - 1;
     }
     tc::cluster_sync();
-    float most[kOwn], total = 0.f;
+    const int bins = slice_bins(), b0 = slice_first();
+    float most[kOwn], total = 0.f, all;
 #pragma unroll
     for (int j = 0; j < kOwn; ++j) {
-      const int b = threadIdx.x * kOwn + j;
-      total += most[j] = (float)in_bin<false>(b) * __expf(-kStep * b);
+      most[j] = j < bins ? (float)in_bin<false>(b0 + j) * __expf(-kStep * (b0 + j)) : 0.f;
+      total += most[j];
     }
-    float run = total;
-    const int lane = threadIdx.x % 32;
-#pragma unroll
-    for (int k = 1; k < 32; k <<= 1) {
-      const float o = __shfl_up_sync(0xffffffffu, run, k);
-      if (lane >= k) run += o;
-    }
-    if (lane == 31) sh.fpart[0][threadIdx.x / 32] = run;
-    __syncthreads();
-    run -= total;
-    for (int w = 0; w < (int)threadIdx.x / 32; ++w) run += sh.fpart[0][w];
+    float run = before_me(total, sh.fpart, &all);
+    if (threadIdx.x == 0) sh.slot[slots][0] = __float_as_uint(all);
+    tc::cluster_sync();
+    for (uint32_t r = 0; r < rank; ++r)
+      run += __uint_as_float((uint32_t)remote64(&sh.slot[slots][0], r));
+    ++slots;
     const float want = (float)need * 0x1p-40f;
     const float least = __expf(-kStep);  // the lowest weight of a bin by its highest
-    int first_most = kBins, first_least = kBins;
+    int first_most = kBins - 1, first_least = kBins - 1;
 #pragma unroll
-    for (int j = 0; j < kOwn; ++j) {
-      run += most[j];
-      if (first_most == kBins && fmaf(run, 1.0001f, 2e-6f) >= want)
-        first_most = threadIdx.x * kOwn + j;
-      if (first_least == kBins && fmaf(run * least, 0.9999f, -2e-6f) >= want)
-        first_least = threadIdx.x * kOwn + j;
+    for (int j = kOwn - 1; j >= 0; --j) {
+      float upto = run;
+#pragma unroll
+      for (int i = 0; i <= j; ++i) upto += most[i];
+      if (j < bins && fmaf(upto, 1.0001f, 2e-6f) >= want) first_most = b0 + j;
+      if (j < bins && fmaf(upto * least, 0.9999f, -2e-6f) >= want) first_least = b0 + j;
     }
-    if (first_most < kBins) atomicMin(&sh.lo, first_most);
-    if (first_least < kBins) atomicMin(&sh.hi, first_least);
+    atomicMin(&sh.lo, first_most);
+    atomicMin(&sh.hi, first_least);
     __syncthreads();
-    *lo = sh.lo;
-    *hi = sh.hi;
+    if (threadIdx.x == 0) sh.slot[slots][0] = (u64)sh.lo << 32 | (u64)sh.hi;
+    tc::cluster_sync();
+    *lo = *hi = kBins - 1;
+    for (uint32_t r = 0; r < ranks; ++r) {
+      const u64 v = remote64(&sh.slot[slots][0], r);
+      *lo = min(*lo, (int)(v >> 32));
+      *hi = min(*hi, (int)(uint32_t)v);
+    }
+    ++slots;
   }
   // The key in bin `bin` of depth at which the running count (or weight) of the
   // bin reaches `need`; what is left of `need` at that key is returned.
@@ -443,12 +538,13 @@ struct Row {
   }
 };
 
-template <typename T, int THREADS>
-__global__ void __launch_bounds__(THREADS)
+template <typename T, int THREADS, bool HELD>
+__global__ void __launch_bounds__(THREADS, 1024 / THREADS)
 sample_kernel(const T* logits, const Sample s, int* status) {
   extern __shared__ __align__(16) uint8_t raw[];
   auto& sh = *reinterpret_cast<Shared<THREADS>*>(raw);
-  Row<T, THREADS> r(sh);
+  Row<T, THREADS, HELD> r(sh);
+  r.held = reinterpret_cast<uint4*>(raw + sizeof(Shared<THREADS>));
   r.ranks = cluster_size();
   r.rank = tc::pair_rank();
   const int64_t n = blockIdx.x / r.ranks;
@@ -466,18 +562,20 @@ sample_kernel(const T* logits, const Sample s, int* status) {
   r.row = row - r.shift;
   r.end = r.shift + s.vocab;
   const int part_end = min(r.end, (int)(r.rank + 1) * s.part);
-  const int each = (s.part / THREADS + 8) / 8 * 8;
+  const int each = each_of(s.part, THREADS);
   r.first = (int)r.rank * s.part + (int)threadIdx.x * each;
   r.stop = min(r.first + each, part_end);
 
   // the largest logit, as an ordered number; NaN above all
-  u64 top = 0;
-  r.each([&](float l, int) {
+  uint32_t own_top = 0;
+  const auto upper = [&](float l, int) {
     const uint32_t b = __float_as_uint(__fadd_rn(l, 0.f));
-    const u64 k = isnan(l) ? 0xffffffffu : (b >> 31 ? ~b : b | 0x80000000u);
-    top = k > top ? k : top;
-  });
-  top = r.largest(top);
+    const uint32_t k = isnan(l) ? 0xffffffffu : (b >> 31 ? ~b : b | 0x80000000u);
+    own_top = max(own_top, k);
+  };
+  if (HELD) r.first_pass(upper);
+  else r.each(upper);
+  const u64 top = r.largest(own_top);
   const uint32_t lowest = ~0xff800000u;  // of -infinity
   const bool nothing = top <= lowest;
   const bool bad = top >= (0x7f800000u | 0x80000000u) || !(temperature >= 0.f) || isnan(top_p) ||
@@ -533,30 +631,18 @@ sample_kernel(const T* logits, const Sample s, int* status) {
     }
   });
   // equal ones before this thread's, in the CTA and in the CTAs before it
-  const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
-  const auto scan = [&](u64 v, int which) {  // sum of the threads before this one
-    u64 run = v;
-#pragma unroll
-    for (int k = 1; k < 32; k <<= 1) {
-      const u64 o = __shfl_up_sync(0xffffffffu, run, k);
-      if (lane >= k) run += o;
-    }
-    if (lane == 31) sh.part[which][warp] = run;
-    __syncthreads();
-    run -= v;
-    for (int w = 0; w < warp; ++w) run += sh.part[which][w];
-    return run;
-  };
-  __syncthreads();
-  u64 equal_before = scan(equal, 0);
-  if (threadIdx.x == THREADS - 1) sh.slot[r.slots][0] = equal_before + equal;
-  tc::cluster_sync();
-  for (uint32_t k = 0; k < r.rank; ++k) equal_before += remote64(&sh.slot[r.slots][0], k);
-  u64 room = r.ties > equal_before ? r.ties - equal_before : 0;
-  if (!tied) room = 0;
-  own += min(room, equal) * tie;
-  u64 before = scan(own, 1);
-  if (threadIdx.x == THREADS - 1) sh.slot[r.slots][1] = before + own;
+  u64 all;
+  u64 room = 0;
+  if (tied) {
+    u64 equal_before = r.before_me(equal, sh.part[0], &all);
+    if (threadIdx.x == 0) sh.slot[r.slots][0] = all;
+    tc::cluster_sync();
+    for (uint32_t k = 0; k < r.rank; ++k) equal_before += remote64(&sh.slot[r.slots][0], k);
+    room = r.ties > equal_before ? r.ties - equal_before : 0;
+    own += min(room, equal) * tie;
+  }
+  u64 before = r.before_me(own, sh.part[1], &all);
+  if (threadIdx.x == 0) sh.slot[r.slots][1] = all;
   tc::cluster_sync();
   u64 total = 0;
   for (uint32_t k = 0; k < r.ranks; ++k) {
@@ -597,25 +683,28 @@ sample_kernel(const T* logits, const Sample s, int* status) {
   tc::cluster_sync();  // no CTA leaves while another may read its sums
 }
 
-// CTAs of a row: as many as fill the GPU three times over, if each keeps 2048
-// logits or more.
-int cluster_of(int64_t rows, int64_t vocab) {
+// Logits of one of n CTAs; `before`: elements that may come before a row's first
+// one, as rows are read from 16-byte boundaries.
+int part_of(int64_t vocab, int before, int n) {
+  return (int)(((vocab + before + n - 1) / n + 7) / 8 * 8);
+}
+
+// CTAs of a row: as many as hold its logits in shared memory; twice as many while
+// that leaves SMs idle and each 2048 logits or more.
+int cluster_of(int64_t rows, int64_t vocab, int before) {
   int n = 1;
-  while (n < kMaxCluster && (vocab / n > kMaxPart - 8 ||
-                             (rows * n < 3 * 152 && vocab / (2 * n) >= 2048)))
+  while (n < kMaxCluster && (each_of(part_of(vocab, before, n), 512) > kHeld ||
+                             (rows * n < 152 && vocab / (2 * n) >= 2048)))
     n *= 2;
   return n;
 }
 
-template <typename T, int THREADS>
-cudaError_t launch(const void* logits, Sample s, int* status, cudaStream_t st) {
-  const int n = cluster_of(s.rows, s.vocab);
-  const auto kernel = sample_kernel<T, THREADS>;
-  // up to 16 / width - 1 elements come before the first logit
-  s.part = (int32_t)(((s.vocab + 7 + n - 1) / n + 7) / 8 * 8);
-  const size_t smem = sizeof(Shared<THREADS>);
+template <typename T, int THREADS, bool HELD>
+cudaError_t launch(const void* logits, Sample s, int n, int* status, cudaStream_t st) {
+  const auto kernel = sample_kernel<T, THREADS, HELD>;
+  constexpr int most = sizeof(Shared<THREADS>) + (HELD ? THREADS * kHeld * sizeof(T) : 0);
   static const cudaError_t set =
-      cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+      cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
   if (set != cudaSuccess) return set;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -626,20 +715,27 @@ cudaError_t launch(const void* logits, Sample s, int* status, cudaStream_t st) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(s.rows * n));
   cfg.blockDim = dim3(THREADS);
-  cfg.dynamicSmemBytes = smem;
+  cfg.dynamicSmemBytes = most;
   cfg.stream = st;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
   return cudaLaunchKernelEx(&cfg, kernel, static_cast<const T*>(logits), (const Sample)s, status);
 }
 
+bool aligned(const void* p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
+
 template <typename T>
-cudaError_t run(const void* logits, const Sample& s, int* status, cudaStream_t st) {
-  return s.vocab <= 2048 ? launch<T, 128>(logits, s, status, st)
-                         : launch<T, 512>(logits, s, status, st);
+cudaError_t run(const void* logits, Sample s, int* status, cudaStream_t st) {
+  constexpr int piece = 16 / sizeof(T);
+  const int before = aligned(logits, 16) && (s.rows == 1 || s.stride % piece == 0) ? 0 : piece - 1;
+  const bool few = s.vocab <= 2048;
+  const int n = few ? 1 : cluster_of(s.rows, s.vocab, before);
+  s.part = part_of(s.vocab, before, n);
+  if (few) return launch<T, 128, true>(logits, s, n, status, st);
+  return each_of(s.part, 512) <= kHeld ? launch<T, 512, true>(logits, s, n, status, st)
+                                       : launch<T, 512, false>(logits, s, n, status, st);
 }
 
-bool aligned(const void* p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
 
 }  // namespace
 }  // namespace soma
