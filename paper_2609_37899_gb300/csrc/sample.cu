@@ -30,7 +30,6 @@ using u64 = unsigned long long;
 
 constexpr int kBins = 2048;
 constexpr int kMaxCluster = 8;
-constexpr int64_t kMaxPart = 1 << 17;      // elements of a CTA: sums of 14-bit parts fit 32 bits
 constexpr int kSlots = 24;                 // exchanges between the CTAs of a row
 constexpr int kHeld = 32;                  // logits of a thread that shared memory holds
 constexpr float kDeepest = 28.5f;          // 2^40 exp(-28.42) = 1/2: weights further down are 0
@@ -123,6 +122,9 @@ struct Sample {
   float* logprobs;
 };
 
+// Logits that one CTA finishes alone.
+__host__ __device__ constexpr int list_of(int threads) { return 2 * threads; }
+
 // Logits of a thread: neighbouring ones, in eights.
 __host__ __device__ constexpr int each_of(int part, int threads) {
   return (part + 8 * threads - 1) / (8 * threads) * 8;
@@ -137,6 +139,9 @@ struct __align__(16) Shared {
   float fpart[THREADS / 32];
   float2 inv;
   u64 found[3];
+  u64 list[list_of(THREADS)];     // rank 0's: key and index, sorted
+  u64 weights[list_of(THREADS)];  // running sums of the list's weights
+  uint32_t listed;
   int lo, hi;
 };
 
@@ -164,12 +169,30 @@ __device__ __forceinline__ u64 remote64(const u64* p, uint32_t rank) {
   return v;
 }
 
+// The same variable of all CTAs, on their way together; the sum, or that of the
+// CTAs before this one.
+__device__ __forceinline__ void remote_all(const u64* p, uint32_t ranks, u64 (&v)[kMaxCluster]) {
+#pragma unroll
+  for (uint32_t r = 0; r < kMaxCluster; ++r) v[r] = remote64(p, min(r, ranks - 1));
+#pragma unroll
+  for (uint32_t r = 0; r < kMaxCluster; ++r)
+    if (r >= ranks) v[r] = 0;
+}
+__device__ __forceinline__ u64 remote_sum(const u64* p, uint32_t ranks, uint32_t upto) {
+  u64 v[kMaxCluster], t = 0;
+  remote_all(p, ranks, v);
+#pragma unroll
+  for (uint32_t r = 0; r < kMaxCluster; ++r) t += r < upto ? v[r] : 0;
+  return t;
+}
+
 // One row's work in one CTA.
 template <typename T, int THREADS, bool HELD>
 struct Row {
   using S = Shared<THREADS>;
   static constexpr int kWarps = THREADS / 32;
   static constexpr int kOwn = kBins / THREADS;  // bins of a thread
+  static constexpr int kList = list_of(THREADS);
   S& sh;
   const T* row;        // 16-byte aligned, `shift` elements before the first logit
   int shift, end;      // end: one behind the last logit, counted from `row`
@@ -180,6 +203,8 @@ struct Row {
   float2 inv2 = {0.f, 0.f};
   uint32_t cut = 0;    // what is ranked above this key remains, and ...
   u64 ties = 0;        // ... so many of this key
+  int lo = 0;          // of this thread's logits, those in bins of depth below this
+  u64 surely = 0;      // ... remain, and weigh so much
 
   __device__ Row(S& s) : sh(s) {}
 
@@ -252,17 +277,21 @@ struct Row {
         }
     }
   }
-  // f(logit, index, depth) for those whose weight may be above 0; the depth
-  // orders as the logits do.
+  // f(logit, index, depth) for those whose weight may be above 0.  The depth, in
+  // bins, orders as the logits do: bin b has those of [b, b + 1).
   template <typename F>
   __device__ __forceinline__ void each_weighted(F f) const {
     each([&](float l, int i) {
-      const float depth = __fmul_rn(__fsub_rn(max, l), inv);
-      if (depth < kDeepest) f(l, i, depth);
+      const float depth = __fmul_rn(__fmul_rn(__fsub_rn(max, l), inv), 1.f / kStep);
+      if (depth < kBins) f(l, i, depth);
     });
   }
-  __device__ __forceinline__ static int bin_of(float depth) {
-    return min((int)__fmul_rn(depth, 1.f / kStep), kBins - 1);
+  __device__ __forceinline__ static bool in(float depth, int bin) {
+    return depth >= bin && depth < bin + 1;
+  }
+  // whether a top-k cut leaves it, but for those at the cut itself
+  __device__ __forceinline__ bool above_cut(float l) const {
+    return cut == 0 || key_of<T>(l) > cut;
   }
   __device__ __forceinline__ u64 weight_of(float l) const {
     return weight(l, max, inv2, sh.roots);
@@ -289,10 +318,7 @@ struct Row {
     }
     tc::cluster_sync();
 #pragma unroll
-    for (int j = 0; j < N; ++j) {
-      v[j] = 0;
-      for (uint32_t r = 0; r < ranks; ++r) v[j] += remote64(&sh.slot[slots][j], r);
-    }
+    for (int j = 0; j < N; ++j) v[j] = remote_sum(&sh.slot[slots][j], ranks, ranks);
     ++slots;
   }
   // The largest over the row's CTAs.
@@ -309,11 +335,10 @@ struct Row {
       sh.slot[slots][0] = v;
     }
     tc::cluster_sync();
-    v = 0;
-    for (uint32_t r = 0; r < ranks; ++r) {
-      const u64 o = remote64(&sh.slot[slots][0], r);
-      v = o > v ? o : v;
-    }
+    u64 o[kMaxCluster];
+    remote_all(&sh.slot[slots][0], ranks, o);
+#pragma unroll
+    for (uint32_t r = 0; r < kMaxCluster; ++r) v = r == 0 || o[r] > v ? o[r] : v;
     ++slots;
     return v;
   }
@@ -333,14 +358,18 @@ struct Row {
   }
   template <bool WEIGHTS>
   __device__ __forceinline__ u64 in_bin(int b) const {
+    uint32_t v[kMaxCluster][WEIGHTS ? 3 : 1];
+#pragma unroll
+    for (uint32_t r = 0; r < kMaxCluster; ++r)
+#pragma unroll
+      for (int a = 0; a < (WEIGHTS ? 3 : 1); ++a) v[r][a] = remote32(&sh.hist[a][b], min(r, ranks - 1));
     u64 t = 0;
-    for (uint32_t r = 0; r < ranks; ++r) {
-      t += remote32(&sh.hist[0][b], r);
-      if (WEIGHTS) {
-        t += (u64)remote32(&sh.hist[1][b], r) << 14;
-        t += (u64)remote32(&sh.hist[2][b], r) << 28;
+#pragma unroll
+    for (uint32_t r = 0; r < kMaxCluster; ++r)
+      if (r < ranks) {
+        t += v[r][0];
+        if (WEIGHTS) t += ((u64)v[r][WEIGHTS ? 1 : 0] << 14) + ((u64)v[r][WEIGHTS ? 2 : 0] << 28);
       }
-    }
     return t;
   }
   // Every CTA adds up a slice of the bins over all of them.  A thread's bins of it:
@@ -389,7 +418,7 @@ struct Row {
     u64 run = before_me(total, sh.part[0], &all);
     if (threadIdx.x == 0) sh.slot[slots][0] = all;
     tc::cluster_sync();
-    for (uint32_t r = 0; r < rank; ++r) run += remote64(&sh.slot[slots][0], r);
+    run += remote_sum(&sh.slot[slots][0], ranks, rank);
     ++slots;
 #pragma unroll
     for (int j = 0; j < kOwn; ++j) {
@@ -427,8 +456,11 @@ struct Row {
     float run = before_me(total, sh.fpart, &all);
     if (threadIdx.x == 0) sh.slot[slots][0] = __float_as_uint(all);
     tc::cluster_sync();
-    for (uint32_t r = 0; r < rank; ++r)
-      run += __uint_as_float((uint32_t)remote64(&sh.slot[slots][0], r));
+    u64 others[kMaxCluster];
+    remote_all(&sh.slot[slots][0], ranks, others);
+#pragma unroll
+    for (uint32_t r = 0; r < kMaxCluster; ++r)
+      if (r < rank) run += __uint_as_float((uint32_t)others[r]);
     ++slots;
     const float want = (float)need * 0x1p-40f;
     const float least = __expf(-kStep);  // the lowest weight of a bin by its highest
@@ -446,18 +478,117 @@ struct Row {
     __syncthreads();
     if (threadIdx.x == 0) sh.slot[slots][0] = (u64)sh.lo << 32 | (u64)sh.hi;
     tc::cluster_sync();
+    remote_all(&sh.slot[slots][0], ranks, others);
     *lo = *hi = kBins - 1;
-    for (uint32_t r = 0; r < ranks; ++r) {
-      const u64 v = remote64(&sh.slot[slots][0], r);
-      *lo = min(*lo, (int)(v >> 32));
-      *hi = min(*hi, (int)(uint32_t)v);
-    }
+#pragma unroll
+    for (uint32_t r = 0; r < kMaxCluster; ++r)
+      if (r < ranks) {
+        *lo = min(*lo, (int)(others[r] >> 32));
+        *hi = min(*hi, (int)(uint32_t)others[r]);
+      }
     ++slots;
   }
+  // ---- a list of few logits in rank 0 ----
+  // Those for which f says so, kList at most, sorted by logit and index.
+  template <typename F>
+  __device__ void gather(F f) {
+    if (threadIdx.x == 0) sh.listed = 0;
+    tc::cluster_sync();
+    each_weighted([&](float l, int i, float depth) {
+      if (!f(l, depth)) return;
+      uint32_t at;
+      asm volatile("atom.shared::cluster.add.u32 %0, [%1], 1;"
+                   : "=r"(at)
+                   : "r"(at_rank(&sh.listed, 0))
+                   : "memory");
+      if (at < kList) set_remote64(&sh.list[at], 0, (u64)key_of<T>(l) << 32 | (~(uint32_t)i));
+    });
+    tc::cluster_sync();
+    if (rank == 0) sort((int)min(sh.listed, (uint32_t)kList));
+  }
+  // Sorts rank 0's list downwards: bitonic, past its end zeros.
+  __device__ void sort(int count) {
+    int n = 2;
+    while (n < count) n *= 2;
+    for (int i = count + threadIdx.x; i < n; i += THREADS) sh.list[i] = 0;
+    __syncthreads();
+    for (int size = 2; size <= n; size *= 2)
+      for (int step = size / 2; step > 0; step /= 2) {
+        for (int t = threadIdx.x; t < n / 2; t += THREADS) {
+          const int a = 2 * t - (t & (step - 1)), b = a + step;
+          const u64 x = sh.list[a], y = sh.list[b];
+          if ((x < y) == ((a & size) == 0)) {
+            sh.list[a] = y;
+            sh.list[b] = x;
+          }
+        }
+        __syncthreads();
+      }
+  }
+  // Running sums over f(position) of the list into sh.weights.
+  template <typename F>
+  __device__ u64 run_over(int count, F f) {
+    constexpr int kEach = (kList + THREADS - 1) / THREADS;
+    u64 own[kEach], total = 0, all;
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) {
+      const int i = threadIdx.x * kEach + j;
+      total += own[j] = i < count ? f(i) : 0;
+    }
+    u64 run = before_me(total, sh.part[0], &all);
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) {
+      run += own[j];
+      if (threadIdx.x * kEach + j < kList) sh.weights[threadIdx.x * kEach + j] = run;
+    }
+    __syncthreads();
+    return all;
+  }
+  // The first of `count` positions whose running sum is at least `need`, or count.
+  __device__ int reaches(int count, u64 need) {
+    if (threadIdx.x == 0) sh.lo = count;
+    __syncthreads();
+    for (int i = threadIdx.x; i < count; i += THREADS)
+      if (sh.weights[i] >= need && (i == 0 || sh.weights[i - 1] < need)) sh.lo = i;
+    __syncthreads();
+    const int at = sh.lo;
+    __syncthreads();
+    return at;
+  }
+  __device__ __forceinline__ uint32_t listed_key(int i) const { return (uint32_t)(sh.list[i] >> 32); }
+
   // The key in bin `bin` of depth at which the running count (or weight) of the
-  // bin reaches `need`; what is left of `need` at that key is returned.
+  // bin, which has `held_there` of it, reaches `need`; what is left of `need` at
+  // that key is returned.
   template <bool WEIGHTS>
-  __device__ u64 refine(int bin, u64 need, uint32_t* key) {
+  __device__ u64 refine(int bin, u64 held_there, u64 need, uint32_t* key) {
+    // a bin's weights are known to 1.4%, and their roundings to whole numbers to
+    // 1.3% where they are 40 or more: how many they are at most
+    const float deep = kStep * (bin + 1);
+    const float most = WEIGHTS ? (float)held_there * 0x1p-40f * __expf(deep) * 1.03f + 2.f
+                               : (float)held_there;
+    if (most <= kList && (!WEIGHTS || deep < 24.f)) {
+      gather([&](float l, float depth) { return in(depth, bin) && above_cut(l); });
+      if (rank == 0) {
+        const int n = (int)min(sh.listed, (uint32_t)kList);
+        run_over(n, [&](int i) { return WEIGHTS ? weight_of(logit_of<T>(listed_key(i))) : 1ull; });
+        const int at = min(reaches(n, need), n - 1);
+        // back to the first of this key
+        if (threadIdx.x == 0) {
+          int first_equal = at;
+          while (first_equal > 0 && listed_key(first_equal - 1) == listed_key(at)) --first_equal;
+          const u64 left = need - (first_equal ? sh.weights[first_equal - 1] : 0);
+          for (uint32_t r = 0; r < ranks; ++r) {
+            set_remote64(&sh.found[0], r, listed_key(at));
+            set_remote64(&sh.found[1], r, left);
+          }
+        }
+      }
+      tc::cluster_sync();
+      *key = (uint32_t)sh.found[0];
+      return sh.found[1];
+    }
+    // many, of few keys as a rule: by digits of the keys
     uint32_t prefix = 0;
     int left = kKeyBits<T>;
     while (left > 0) {
@@ -465,7 +596,7 @@ struct Row {
       const uint32_t mask = (1u << bits) - 1;
       clear(WEIGHTS ? 3 : 1);
       each_weighted([&](float l, int, float depth) {
-        if (bin_of(depth) != bin) return;
+        if (!in(depth, bin)) return;
         const uint32_t k = key_of<T>(l);
         if (k <= cut || (left < kKeyBits<T> && k >> left != prefix)) return;
         const int b = (int)(mask - (k >> (left - bits) & mask));  // larger keys first
@@ -473,8 +604,8 @@ struct Row {
         else count(b);
       });
       int at;
-      u64 before, held;
-      find<WEIGHTS>(need, &at, &before, &held);
+      u64 before, held_now;
+      find<WEIGHTS>(need, &at, &before, &held_now);
       need -= before;
       prefix = prefix << bits | (mask - (uint32_t)at);
       left -= bits;
@@ -484,30 +615,83 @@ struct Row {
   }
 
   // ---- the two cuts ----
-  __device__ void top_k(u64 k) {
-    clear(1);
-    each_weighted([&](float, int, float depth) { count(bin_of(depth)); });
-    int bin;
-    u64 before, held;
-    if (!find<false>(k, &bin, &before, &held)) return;  // fewer have a weight at all
-    uint32_t key;
-    ties = refine<false>(bin, k - before, &key);
-    cut = key;
+  // Few logits are left by top-k (the first `count` of the ranking hold it): rank 0
+  // does the rest alone.  The answer's index, or -1, in rank 0.
+  struct Answer {
+    int token;
+    float logit;
+    u64 total;
+  };
+  __device__ Answer finish(int count, u64 k, float top_p, u64 least, float u) {
+    int n = (int)min((u64)count, k);
+    u64 total = run_over(n, [&](int i) { return weight_of(logit_of<T>(listed_key(i))); });
+    if (top_p < 1.f) {
+      if (threadIdx.x == 0) sh.found[0] = share_of(top_p, total);
+      __syncthreads();
+      const u64 need = sh.found[0];
+      __syncthreads();
+      n = min(n, reaches(n, need) + 1);
+    }
+    if (least) {  // weights fall: those from some place on are out
+      if (threadIdx.x == 0) sh.hi = n;
+      __syncthreads();
+      for (int i = threadIdx.x; i < n; i += THREADS)
+        if (sh.weights[i] - (i ? sh.weights[i - 1] : 0) < least) atomicMin(&sh.hi, i);
+      __syncthreads();
+      n = min(n, sh.hi);
+    }
+    total = sh.weights[n - 1];
+    __syncthreads();
+    // by index, their order for the choice
+    for (int i = threadIdx.x; i < n; i += THREADS) {
+      const u64 e = sh.list[i];
+      sh.list[i] = e << 32 | e >> 32;
+    }
+    __syncthreads();
+    sort(n);
+    run_over(n, [&](int i) { return weight_of(logit_of<T>((uint32_t)sh.list[i])); });
+    if (threadIdx.x == 0) {
+      const u64 at = (u64)((double)u * (double)total);
+      sh.found[0] = (at >= total ? total - 1 : at) + 1;
+    }
+    __syncthreads();
+    const int at = min(reaches(n, sh.found[0]), n - 1);
+    const u64 e = sh.list[at];
+    return {(int)~(uint32_t)(e >> 32), logit_of<T>((uint32_t)e), total};
   }
-  __device__ void top_p(float p) {
+  __device__ __forceinline__ static u64 share_of(float p, u64 total) {
+    const double want = ceil((double)p * (double)total);
+    return want < 1.0 ? 1 : (u64)want;
+  }
+
+  // True if few logits hold the first k: they are in rank 0's list then.
+  __device__ bool top_k(u64 k, int* few) {
+    clear(1);
+    each_weighted([&](float, int, float depth) { count((int)depth); });
+    int bin;
+    u64 before, held_there;
+    if (!find<false>(k, &bin, &before, &held_there)) return false;  // fewer have a weight at all
+    if (before + held_there <= kList) {
+      *few = (int)(before + held_there);
+      gather([&](float, float depth) { return depth < bin + 1; });
+      return true;
+    }
+    uint32_t key;
+    ties = refine<false>(bin, held_there, k - before, &key);
+    cut = key;
+    return false;
+  }
+  __device__ void top_p(float p, u64 least) {
     clear(1);
     u64 v[1] = {0};
     each_weighted([&](float l, int, float depth) {
-      if (key_of<T>(l) <= cut) return;
-      count(bin_of(depth));
+      if (!above_cut(l)) return;
+      count((int)depth);
       v[0] += weight_of(l);
     });
     sum(v);
     const u64 tie = ties ? weight_of(logit_of<T>(cut)) : 0;
-    if (threadIdx.x == 0) {
-      const double want = ceil((double)p * (double)(v[0] + ties * tie));
-      sh.found[0] = want < 1.0 ? 1 : (u64)want;
-    }
+    if (threadIdx.x == 0) sh.found[0] = share_of(p, v[0] + ties * tie);
     __syncthreads();
     u64 need = sh.found[0];
     __syncthreads();
@@ -515,23 +699,26 @@ struct Row {
       if (tie) ties = min(ties, (need - v[0] + tie - 1) / tie);
       return;
     }
-    int lo, hi;
+    int hi;
     band(need, &lo, &hi);
     clear(3);
     u64 above[1] = {0};
     each_weighted([&](float l, int, float depth) {
-      const int b = bin_of(depth);
-      if (b > hi || key_of<T>(l) <= cut) return;
+      if (depth >= hi + 1 || !above_cut(l)) return;
       const u64 w = weight_of(l);
-      if (b < lo) above[0] += w;
-      else add(b, w);
+      if (depth < lo) {
+        above[0] += w;
+        surely += w >= least ? w : 0;
+      } else {
+        add((int)depth, w);
+      }
     });
     sum(above);
     int bin;
-    u64 before, held;
-    if (!find<true>(need - above[0], &bin, &before, &held)) return;
+    u64 before, held_there;
+    if (!find<true>(need - above[0], &bin, &before, &held_there)) return;
     uint32_t key;
-    need = refine<true>(bin, need - above[0] - before, &key);
+    need = refine<true>(bin, held_there, need - above[0] - before, &key);
     const u64 w = weight_of(logit_of<T>(key));
     cut = key;
     ties = w ? (need + w - 1) / w : 0;
@@ -613,15 +800,30 @@ sample_kernel(const T* logits, const Sample s, int* status) {
   __syncthreads();
   r.inv2 = sh.inv;
   r.inv = r.inv2.x;
-  if (top_k > 0 && top_k < s.vocab) r.top_k((u64)top_k);
-  if (top_p < 1.f) r.top_p(top_p);
+  const auto logprob = [&](float l, u64 total) {
+    return (float)(((double)l - (double)r.max) / (double)fminf(temperature, kMostTemperature) -
+                   log((double)total * 0x1p-40));
+  };
+  const u64 least = min_p > 0.f ? (u64)ceil((double)fminf(min_p, 1.f) * 0x1p40) : 0;
+  int few;
+  if (top_k > 0 && top_k < s.vocab && r.top_k((u64)top_k, &few)) {
+    if (r.rank == 0) {
+      const auto a = r.finish(few, (u64)top_k, top_p, least, u);
+      if (threadIdx.x == 0) {
+        s.tokens[n] = a.token - r.shift;
+        if (s.logprobs) s.logprobs[n] = logprob(a.logit, a.total);
+      }
+    }
+    return;  // the others' last access to its memory was before its last meeting
+  }
+  if (top_p < 1.f) r.top_p(top_p, least);
 
   // what remains, in the order of the indexes
-  const u64 least = min_p > 0.f ? (u64)ceil((double)fminf(min_p, 1.f) * 0x1p40) : 0;
   const u64 tie = r.ties ? r.weight_of(logit_of<T>(r.cut)) : 0;
   const bool tied = r.ties && tie >= least;
-  u64 own = 0, equal = 0;
-  r.each_weighted([&](float l, int, float) {
+  u64 own = r.surely, equal = 0;
+  r.each_weighted([&](float l, int, float depth) {
+    if (depth < r.lo) return;
     const uint32_t k = key_of<T>(l);
     if (k > r.cut) {
       const u64 w = r.weight_of(l);
@@ -637,19 +839,15 @@ sample_kernel(const T* logits, const Sample s, int* status) {
     u64 equal_before = r.before_me(equal, sh.part[0], &all);
     if (threadIdx.x == 0) sh.slot[r.slots][0] = all;
     tc::cluster_sync();
-    for (uint32_t k = 0; k < r.rank; ++k) equal_before += remote64(&sh.slot[r.slots][0], k);
+    equal_before += remote_sum(&sh.slot[r.slots][0], r.ranks, r.rank);
     room = r.ties > equal_before ? r.ties - equal_before : 0;
     own += min(room, equal) * tie;
   }
   u64 before = r.before_me(own, sh.part[1], &all);
   if (threadIdx.x == 0) sh.slot[r.slots][1] = all;
   tc::cluster_sync();
-  u64 total = 0;
-  for (uint32_t k = 0; k < r.ranks; ++k) {
-    const u64 v = remote64(&sh.slot[r.slots][1], k);
-    total += v;
-    if (k < r.rank) before += v;
-  }
+  before += remote_sum(&sh.slot[r.slots][1], r.ranks, r.rank);
+  const u64 total = remote_sum(&sh.slot[r.slots][1], r.ranks, r.ranks);
   u64 at = (u64)((double)u * (double)total);
   if (at >= total) at = total - 1;
   if (at >= before && at - before < own) {
@@ -675,10 +873,7 @@ sample_kernel(const T* logits, const Sample s, int* status) {
       }
     });
     s.tokens[n] = token;
-    if (s.logprobs)
-      s.logprobs[n] = (float)(((double)chosen - (double)r.max) /
-                                  (double)fminf(temperature, kMostTemperature) -
-                              log((double)total * 0x1p-40));
+    if (s.logprobs) s.logprobs[n] = logprob(chosen, total);
   }
   tc::cluster_sync();  // no CTA leaves while another may read its sums
 }
