@@ -5,10 +5,9 @@
 // in its shared memory, so that the logits are read once (above 131,064 of them,
 // from L2 or memory in every pass).  The ranking is never made: top-k and top-p
 // each need one cut in it, which is found as a radix selection finds it, by
-// counts (or weights) per bin, the bin that the cut lies in, then finer bins of
-// that one.  The first bins are equal steps of (max - l) / T: there the weights
-// of a bin differ by a known factor, so that counts alone say which few bins
-// can hold the cut by weight, and only their weights are added up by bin.
+// counts (or weights) per bin, the bin that the cut lies in, then the logits of
+// that one: sorted in a list where they are few, by finer bins where not (equal
+// logits, as a rule).  The first bins are equal steps of (max - l) / T.
 //
 // Weights are whole numbers, so sums do not depend on their order and every CTA
 // of a cluster comes to the same cut by itself.
@@ -136,9 +135,8 @@ struct __align__(16) Shared {
   float2 roots[64];
   u64 slot[kSlots][3];         // sums of this CTA, for the others
   u64 part[3][THREADS / 32];
-  float fpart[THREADS / 32];
   float2 inv;
-  u64 found[3];
+  u64 found[3], need;
   u64 list[list_of(THREADS)];     // rank 0's: key and index, sorted
   u64 weights[list_of(THREADS)];  // running sums of the list's weights
   uint32_t listed;
@@ -169,21 +167,14 @@ __device__ __forceinline__ u64 remote64(const u64* p, uint32_t rank) {
   return v;
 }
 
-// The same variable of all CTAs, on their way together; the sum, or that of the
-// CTAs before this one.
-__device__ __forceinline__ void remote_all(const u64* p, uint32_t ranks, u64 (&v)[kMaxCluster]) {
+// The same variable of all CTAs (at most N), on their way together.
+template <int N>
+__device__ __forceinline__ void remote_all(const u64* p, uint32_t ranks, u64 (&v)[N]) {
 #pragma unroll
-  for (uint32_t r = 0; r < kMaxCluster; ++r) v[r] = remote64(p, min(r, ranks - 1));
+  for (uint32_t r = 0; r < N; ++r) v[r] = remote64(p, min(r, ranks - 1));
 #pragma unroll
-  for (uint32_t r = 0; r < kMaxCluster; ++r)
+  for (uint32_t r = 0; r < N; ++r)
     if (r >= ranks) v[r] = 0;
-}
-__device__ __forceinline__ u64 remote_sum(const u64* p, uint32_t ranks, uint32_t upto) {
-  u64 v[kMaxCluster], t = 0;
-  remote_all(p, ranks, v);
-#pragma unroll
-  for (uint32_t r = 0; r < kMaxCluster; ++r) t += r < upto ? v[r] : 0;
-  return t;
 }
 
 // One row's work in one CTA.
@@ -193,6 +184,7 @@ struct Row {
   static constexpr int kWarps = THREADS / 32;
   static constexpr int kOwn = kBins / THREADS;  // bins of a thread
   static constexpr int kList = list_of(THREADS);
+  static constexpr int kMost = THREADS < 512 ? 1 : kMaxCluster;  // CTAs of a row
   S& sh;
   const T* row;        // 16-byte aligned, `shift` elements before the first logit
   int shift, end;      // end: one behind the last logit, counted from `row`
@@ -203,10 +195,17 @@ struct Row {
   float2 inv2 = {0.f, 0.f};
   uint32_t cut = 0;    // what is ranked above this key remains, and ...
   u64 ties = 0;        // ... so many of this key
-  int lo = 0;          // of this thread's logits, those in bins of depth below this
-  u64 surely = 0;      // ... remain, and weigh so much
 
   __device__ Row(S& s) : sh(s) {}
+
+  // The sum of a variable over the CTAs before `upto`.
+  __device__ __forceinline__ u64 remote_sum(const u64* p, uint32_t upto) const {
+    u64 v[kMost], t = 0;
+    remote_all(p, ranks, v);
+#pragma unroll
+    for (uint32_t r = 0; r < kMost; ++r) t += r < upto ? v[r] : 0;
+    return t;
+  }
 
   // Eight logits in shared memory: 16-byte pieces of neighbouring threads side by
   // side.  What lies outside the row is -infinity.
@@ -297,30 +296,6 @@ struct Row {
     return weight(l, max, inv2, sh.roots);
   }
 
-  __device__ __forceinline__ static u64 warp_sum(u64 v) {
-#pragma unroll
-    for (int k = 16; k; k >>= 1) v += __shfl_xor_sync(0xffffffffu, v, k);
-    return v;
-  }
-  // Sums over the row's CTAs.  Every slot is used once.
-  template <int N>
-  __device__ void sum(u64 (&v)[N]) {
-#pragma unroll
-    for (int j = 0; j < N; ++j) {
-      v[j] = warp_sum(v[j]);
-      if (threadIdx.x % 32 == 0) sh.part[j][threadIdx.x / 32] = v[j];
-    }
-    __syncthreads();
-    if (threadIdx.x < N) {
-      u64 t = 0;
-      for (int w = 0; w < kWarps; ++w) t += sh.part[threadIdx.x][w];
-      sh.slot[slots][threadIdx.x] = t;
-    }
-    tc::cluster_sync();
-#pragma unroll
-    for (int j = 0; j < N; ++j) v[j] = remote_sum(&sh.slot[slots][j], ranks, ranks);
-    ++slots;
-  }
   // The largest over the row's CTAs.
   __device__ u64 largest(u64 v) {
 #pragma unroll
@@ -335,10 +310,10 @@ struct Row {
       sh.slot[slots][0] = v;
     }
     tc::cluster_sync();
-    u64 o[kMaxCluster];
+    u64 o[kMost];
     remote_all(&sh.slot[slots][0], ranks, o);
 #pragma unroll
-    for (uint32_t r = 0; r < kMaxCluster; ++r) v = r == 0 || o[r] > v ? o[r] : v;
+    for (uint32_t r = 0; r < kMost; ++r) v = r == 0 || o[r] > v ? o[r] : v;
     ++slots;
     return v;
   }
@@ -358,14 +333,14 @@ struct Row {
   }
   template <bool WEIGHTS>
   __device__ __forceinline__ u64 in_bin(int b) const {
-    uint32_t v[kMaxCluster][WEIGHTS ? 3 : 1];
+    uint32_t v[kMost][WEIGHTS ? 3 : 1];
 #pragma unroll
-    for (uint32_t r = 0; r < kMaxCluster; ++r)
+    for (uint32_t r = 0; r < kMost; ++r)
 #pragma unroll
       for (int a = 0; a < (WEIGHTS ? 3 : 1); ++a) v[r][a] = remote32(&sh.hist[a][b], min(r, ranks - 1));
     u64 t = 0;
 #pragma unroll
-    for (uint32_t r = 0; r < kMaxCluster; ++r)
+    for (uint32_t r = 0; r < kMost; ++r)
       if (r < ranks) {
         t += v[r][0];
         if (WEIGHTS) t += ((u64)v[r][WEIGHTS ? 1 : 0] << 14) + ((u64)v[r][WEIGHTS ? 2 : 0] << 28);
@@ -402,10 +377,11 @@ struct Row {
     *all = total;
     return run;
   }
-  // The bin where the running sum over the row's bins reaches `need` (at least
-  // 1), the sum before it and what it holds; false if none does.
-  template <bool WEIGHTS>
-  __device__ bool find(u64 need, int* bin, u64* before, u64* held_there) {
+  // The bin where the running sum over the row's bins reaches need_of(the sum of
+  // all), which is at least 1; the sum before it and what it holds.  False if none
+  // does.
+  template <bool WEIGHTS, typename F>
+  __device__ bool find(F need_of, int* bin, u64* need, u64* before, u64* held_there) {
     if (threadIdx.x == 0) sh.found[0] = ~0ull;
     tc::cluster_sync();
     const int bins = slice_bins(), b0 = slice_first();
@@ -418,11 +394,14 @@ struct Row {
     u64 run = before_me(total, sh.part[0], &all);
     if (threadIdx.x == 0) sh.slot[slots][0] = all;
     tc::cluster_sync();
-    run += remote_sum(&sh.slot[slots][0], ranks, rank);
+    run += remote_sum(&sh.slot[slots][0], rank);
+    if (threadIdx.x == 0) sh.need = need_of(remote_sum(&sh.slot[slots][0], ranks));
+    __syncthreads();
+    *need = sh.need;
     ++slots;
 #pragma unroll
     for (int j = 0; j < kOwn; ++j) {
-      if (j < bins && run < need && run + own[j] >= need)
+      if (j < bins && run < *need && run + own[j] >= *need)
         for (uint32_t r = 0; r < ranks; ++r) {
           set_remote64(&sh.found[0], r, (u64)(b0 + j));
           set_remote64(&sh.found[1], r, run);
@@ -435,58 +414,6 @@ struct Row {
     *before = sh.found[1];
     *held_there = sh.found[2];
     return sh.found[0] != ~0ull;
-  }
-  // From counts per bin of depth: the bins [lo, hi] one of which is where the
-  // sum of weights reaches `need`.  The slack is for the roundings of depths,
-  // of these sums (1e-4) and of small weights to whole numbers (2e-6 of the
-  // largest weight, over 2^20 tokens).
-  __device__ void band(u64 need, int* lo, int* hi) {
-    if (threadIdx.x == 0) {
-      sh.lo = kBins - 1;
-      sh.hi = kBins - 1;
-    }
-    tc::cluster_sync();
-    const int bins = slice_bins(), b0 = slice_first();
-    float most[kOwn], total = 0.f, all;
-#pragma unroll
-    for (int j = 0; j < kOwn; ++j) {
-      most[j] = j < bins ? (float)in_bin<false>(b0 + j) * __expf(-kStep * (b0 + j)) : 0.f;
-      total += most[j];
-    }
-    float run = before_me(total, sh.fpart, &all);
-    if (threadIdx.x == 0) sh.slot[slots][0] = __float_as_uint(all);
-    tc::cluster_sync();
-    u64 others[kMaxCluster];
-    remote_all(&sh.slot[slots][0], ranks, others);
-#pragma unroll
-    for (uint32_t r = 0; r < kMaxCluster; ++r)
-      if (r < rank) run += __uint_as_float((uint32_t)others[r]);
-    ++slots;
-    const float want = (float)need * 0x1p-40f;
-    const float least = __expf(-kStep);  // the lowest weight of a bin by its highest
-    int first_most = kBins - 1, first_least = kBins - 1;
-#pragma unroll
-    for (int j = kOwn - 1; j >= 0; --j) {
-      float upto = run;
-#pragma unroll
-      for (int i = 0; i <= j; ++i) upto += most[i];
-      if (j < bins && fmaf(upto, 1.0001f, 2e-6f) >= want) first_most = b0 + j;
-      if (j < bins && fmaf(upto * least, 0.9999f, -2e-6f) >= want) first_least = b0 + j;
-    }
-    atomicMin(&sh.lo, first_most);
-    atomicMin(&sh.hi, first_least);
-    __syncthreads();
-    if (threadIdx.x == 0) sh.slot[slots][0] = (u64)sh.lo << 32 | (u64)sh.hi;
-    tc::cluster_sync();
-    remote_all(&sh.slot[slots][0], ranks, others);
-    *lo = *hi = kBins - 1;
-#pragma unroll
-    for (uint32_t r = 0; r < kMaxCluster; ++r)
-      if (r < ranks) {
-        *lo = min(*lo, (int)(others[r] >> 32));
-        *hi = min(*hi, (int)(uint32_t)others[r]);
-      }
-    ++slots;
   }
   // ---- a list of few logits in rank 0 ----
   // Those for which f says so, kList at most, sorted by logit and index.
@@ -605,7 +532,8 @@ struct Row {
       });
       int at;
       u64 before, held_now;
-      find<WEIGHTS>(need, &at, &before, &held_now);
+      const u64 wanted = need;
+      find<WEIGHTS>([&](u64) { return wanted; }, &at, &need, &before, &held_now);
       need -= before;
       prefix = prefix << bits | (mask - (uint32_t)at);
       left -= bits;
@@ -669,8 +597,8 @@ struct Row {
     clear(1);
     each_weighted([&](float, int, float depth) { count((int)depth); });
     int bin;
-    u64 before, held_there;
-    if (!find<false>(k, &bin, &before, &held_there)) return false;  // fewer have a weight at all
+    u64 need, before, held_there;
+    if (!find<false>([&](u64) { return k; }, &bin, &need, &before, &held_there)) return false;  // fewer have a weight at all
     if (before + held_there <= kList) {
       *few = (int)(before + held_there);
       gather([&](float, float depth) { return depth < bin + 1; });
@@ -681,44 +609,25 @@ struct Row {
     cut = key;
     return false;
   }
-  __device__ void top_p(float p, u64 least) {
-    clear(1);
-    u64 v[1] = {0};
+  __device__ void top_p(float p) {
+    clear(3);
     each_weighted([&](float l, int, float depth) {
-      if (!above_cut(l)) return;
-      count((int)depth);
-      v[0] += weight_of(l);
+      if (above_cut(l)) add((int)depth, weight_of(l));
     });
-    sum(v);
-    const u64 tie = ties ? weight_of(logit_of<T>(cut)) : 0;
-    if (threadIdx.x == 0) sh.found[0] = share_of(p, v[0] + ties * tie);
-    __syncthreads();
-    u64 need = sh.found[0];
-    __syncthreads();
-    if (need > v[0]) {  // the cut stays at the key of the first one
-      if (tie) ties = min(ties, (need - v[0] + tie - 1) / tie);
+    const u64 tie = ties ? weight_of(logit_of<T>(cut)) : 0, tied = ties * tie;
+    int bin;
+    u64 need, before, held_there;
+    if (!find<true>([&](u64 all) { return share_of(p, all + tied); }, &bin, &need, &before,
+                    &held_there)) {
+      // the cut stays at the key of the first one, with as many of that key as it takes
+      if (tie) {
+        const u64 over = remote_sum(&sh.slot[slots - 1][0], ranks);
+        ties = min(ties, (need - over + tie - 1) / tie);
+      }
       return;
     }
-    int hi;
-    band(need, &lo, &hi);
-    clear(3);
-    u64 above[1] = {0};
-    each_weighted([&](float l, int, float depth) {
-      if (depth >= hi + 1 || !above_cut(l)) return;
-      const u64 w = weight_of(l);
-      if (depth < lo) {
-        above[0] += w;
-        surely += w >= least ? w : 0;
-      } else {
-        add((int)depth, w);
-      }
-    });
-    sum(above);
-    int bin;
-    u64 before, held_there;
-    if (!find<true>(need - above[0], &bin, &before, &held_there)) return;
     uint32_t key;
-    need = refine<true>(bin, held_there, need - above[0] - before, &key);
+    need = refine<true>(bin, held_there, need - before, &key);
     const u64 w = weight_of(logit_of<T>(key));
     cut = key;
     ties = w ? (need + w - 1) / w : 0;
@@ -816,14 +725,13 @@ sample_kernel(const T* logits, const Sample s, int* status) {
     }
     return;  // the others' last access to its memory was before its last meeting
   }
-  if (top_p < 1.f) r.top_p(top_p, least);
+  if (top_p < 1.f) r.top_p(top_p);
 
   // what remains, in the order of the indexes
   const u64 tie = r.ties ? r.weight_of(logit_of<T>(r.cut)) : 0;
   const bool tied = r.ties && tie >= least;
-  u64 own = r.surely, equal = 0;
-  r.each_weighted([&](float l, int, float depth) {
-    if (depth < r.lo) return;
+  u64 own = 0, equal = 0;
+  r.each_weighted([&](float l, int, float) {
     const uint32_t k = key_of<T>(l);
     if (k > r.cut) {
       const u64 w = r.weight_of(l);
@@ -839,15 +747,15 @@ sample_kernel(const T* logits, const Sample s, int* status) {
     u64 equal_before = r.before_me(equal, sh.part[0], &all);
     if (threadIdx.x == 0) sh.slot[r.slots][0] = all;
     tc::cluster_sync();
-    equal_before += remote_sum(&sh.slot[r.slots][0], r.ranks, r.rank);
+    equal_before += r.remote_sum(&sh.slot[r.slots][0], r.rank);
     room = r.ties > equal_before ? r.ties - equal_before : 0;
     own += min(room, equal) * tie;
   }
   u64 before = r.before_me(own, sh.part[1], &all);
   if (threadIdx.x == 0) sh.slot[r.slots][1] = all;
   tc::cluster_sync();
-  before += remote_sum(&sh.slot[r.slots][1], r.ranks, r.rank);
-  const u64 total = remote_sum(&sh.slot[r.slots][1], r.ranks, r.ranks);
+  before += r.remote_sum(&sh.slot[r.slots][1], r.rank);
+  const u64 total = r.remote_sum(&sh.slot[r.slots][1], r.ranks);
   u64 at = (u64)((double)u * (double)total);
   if (at >= total) at = total - 1;
   if (at >= before && at - before < own) {
