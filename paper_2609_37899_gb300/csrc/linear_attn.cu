@@ -54,8 +54,8 @@ struct Tile {
 };
 
 // The recurrence step by step in fp32: one CTA per problem, segment, sequence and
-// head, the state in registers, RUNS runs of four rows by four columns per thread.  Threads of `groups`
-// neighbouring lanes hold the rows of the same columns.  A few steps at a
+// head, the state in registers, RUNS runs of four rows by four columns per thread.
+// Threads of `groups` neighbouring lanes hold the rows of the same columns.  A few steps at a
 // time: what they read and the sums over their rows do not wait for one another, only
 // the state itself does.  The last kLoaders threads stage the next tile.
 // Instruction issue bounds it: three fp32 instructions per element of the state and
@@ -63,7 +63,7 @@ struct Tile {
 // 16 x 2048 x 8 heads of 128 x 128 took 1000 us.
 template <typename T, int RUNS, bool OUT>
 __global__ void __launch_bounds__(most_threads(RUNS))
-plain_kernel(const __grid_constant__ Call call, const __grid_constant__ Cut cut, int groups) {
+plain_kernel(const __grid_constant__ Call call, const __grid_constant__ Cut cut) {
   constexpr int kRows = 4 * RUNS;
   extern __shared__ __align__(16) float smem[];
   __shared__ Decay decay;
@@ -76,6 +76,8 @@ plain_kernel(const __grid_constant__ Call call, const __grid_constant__ Cut cut,
   const int64_t rest = blockIdx.x / call.problems;
   const int seg = (int)(rest % cut.launched);
   const int64_t bh = rest / cut.launched, b = bh / call.heads, h = bh % call.heads;
+  int groups = 1;  // of this problem: the CTA's threads are those of the widest
+  while (groups * kRows < p.a) groups *= 2;
   const int64_t which = bh * call.problems + blockIdx.x % call.problems;
   const int64_t len = length_of(call, b);
   const float g = decay_of(call, h);
@@ -106,17 +108,20 @@ plain_kernel(const __grid_constant__ Call call, const __grid_constant__ Cut cut,
         const int each = pieces ? 4 : 1, across = wide / each;
         const int i = thread % across * each, per = kLoaders / across;
         if (thread >= per * across) return;
-        for (int k = thread / across; k < kTile; k += per) {
-          const bool there = k < n && i < width;
-          const T* src = there ? from + step_of(k0 + k) * stride + i : from;
-          const uint32_t dst = tc::smem_u32(to + k * wide + i);
+        const int k1 = thread / across, upto = i < width ? n : 0;
+        const T* src = from + step_of(k0 + k1) * stride + i;
+        const int64_t next = (p.reversed ? -per : per) * stride;
+        uint32_t dst = tc::smem_u32(to + k1 * wide + i);
+#pragma unroll 4
+        for (int k = k1; k < kTile; k += per, src += next, dst += per * wide * 4) {
+          const bool there = k < upto;  // zeros otherwise
           if (pieces)
-            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src),
-                         "r"(there ? 16 : 0)
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst),
+                         "l"(there ? src : from), "r"(there ? 16 : 0)
                          : "memory");
           else
-            asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src),
-                         "r"(there ? 4 : 0)
+            asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst),
+                         "l"(there ? src : from), "r"(there ? 4 : 0)
                          : "memory");
         }
       } else {
@@ -162,6 +167,7 @@ plain_kernel(const __grid_constant__ Call call, const __grid_constant__ Cut cut,
   // row of register r: runs of four, `groups` runs apart
   const int group = threadIdx.x % groups, c0 = threadIdx.x / groups * kCols;
   const bool holds = !loads && c0 < tile.cols;
+  const bool works = __any_sync(0xffffffffu, holds);
   const auto row_of = [&](int r) { return (r / 4 * groups + group) * 4 + r % 4; };
   const bool joined = cut.segments > 1 && seg > 0;
   const float* from = joined ? cut.starts + (which * cut.segments + seg) * call.state
@@ -198,12 +204,14 @@ plain_kernel(const __grid_constant__ Call call, const __grid_constant__ Cut cut,
   }
   __syncthreads();
   int buf = 0;
+  const int64_t next_out = p.reversed ? -p.os.t : p.os.t;
   for (int64_t k0 = 0; k0 < count; k0 += kTile) {
     if (loads) {
       stage_next(k0 + 2 * kTile, (buf + 2) % kTiles);
       arrived(false);
-    } else {
+    } else if (works) {
       const int n = count - k0 < kTile ? (int)(count - k0) : kTile;
+      T* to = out + step_of(k0) * p.os.t + c0;
       for (int k = 0; k < n; k += kAtOnce) {
         float o[kAtOnce][kCols];
 #pragma unroll
@@ -247,8 +255,7 @@ plain_kernel(const __grid_constant__ Call call, const __grid_constant__ Cut cut,
 #pragma unroll
               for (int j = 0; j < kCols; ++j) o[u][j] += __shfl_xor_sync(0xffffffffu, o[u][j], s);
 #pragma unroll
-          for (int u = 0; u < kAtOnce; ++u) {
-            T* to = out + step_of(k0 + k + u) * p.os.t + c0;
+          for (int u = 0; u < kAtOnce; ++u, to += next_out) {
 #pragma unroll
             for (int j = 0; j < kCols; ++j)
               if (stores[j] && k + u < n) to[j] = from_f32<T>(p.g * o[u][j]);
@@ -468,13 +475,13 @@ cudaError_t plain(const Call& call, Cut cut, const Spread& s, cudaStream_t st) {
     cut.launched = cut.segments - 1;
     cudaError_t e = launch_overlapped(plain_kernel<T, RUNS, false>,
                                       dim3((unsigned)(rows * cut.launched)), threads_of(s), smem, st,
-                                      call, cut, s.groups);
+                                      call, cut);
     if (e == cudaSuccess) e = launch_join(call, cut, st);
     if (e != cudaSuccess) return e;
   }
   cut.launched = cut.segments;
   return launch_overlapped(plain_kernel<T, RUNS, true>, dim3((unsigned)(rows * cut.segments)),
-                           threads_of(s), smem, st, call, cut, s.groups);
+                           threads_of(s), smem, st, call, cut);
 }
 
 template <typename T>
