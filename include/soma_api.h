@@ -647,12 +647,14 @@ int soma_linear_ce_backward(const void* h, const void* emb, soma_linear_ce_dims 
  * output of its sequence and head, earlier ones and other documents' too.
  *
  * 16-bit types run on the tensor cores where rows allow tiled copies: addresses
- * and strides that are multiples of 16 bytes, and widths of 8 elements.  There
- * scale l^{i-j} <q_i, k_j>, the state that a chunk of 128 steps starts from and
- * the decayed v of a chunk are rounded to the type for the products that they
- * enter (states that are in memory take what the rounding of v takes off, too);
- * sums and states are fp32.  fp16: those three are scaled by powers of two to the
- * range of the type.  Other layouts, and fp32, take kernels of fp32 arithmetic. */
+ * and strides that are multiples of 16 bytes, widths that are multiples of 8, and
+ * strides that nest (each a multiple of the next smaller one, or widths that are
+ * multiples of 16).  There scale l^{i-j} <q_i, k_j> and the state that a chunk of
+ * 128 steps starts from are rounded to the type for the products that they enter,
+ * and the decayed v, for the state, to twice its bits; sums and states are fp32.
+ * fp16: those three are scaled by powers of two to the range of the type.  Other
+ * layouts, and fp32, take kernels of fp32 arithmetic, which are several times
+ * slower. */
 typedef struct soma_attn_dims {
   int64_t batch; /* 0 .. 2^31 - 1 */
   int64_t steps; /* 0 .. 2^31 - 1 */
@@ -662,7 +664,8 @@ typedef struct soma_attn_dims {
 
 /* Elements between neighbouring sequences, steps and heads; the elements of a
  * head are adjacent.  Negative strides are invalid.  Inputs may repeat (stride
- * 0: heads that share k and v); gradients are those of each head. */
+ * 0: heads that share k and v); gradients are those of each head, and no stride
+ * of an output is less than its width where there are two or more along it. */
 typedef struct soma_attn_strides {
   int64_t b, t, h;
 } soma_attn_strides;

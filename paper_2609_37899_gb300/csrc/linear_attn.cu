@@ -314,9 +314,10 @@ __global__ void __launch_bounds__(256)
 join_kernel(const __grid_constant__ Call call, const __grid_constant__ Cut cut) {
   admit_successor();
   after_predecessor();
-  const int64_t which = blockIdx.y, bh = which / call.problems;
+  const int64_t parts = (call.state + 255) / 256, which = blockIdx.x / parts;
+  const int64_t bh = which / call.problems;
   const Problem& p = call.p[which % call.problems];
-  const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int64_t e = blockIdx.x % parts * 256 + threadIdx.x;
   if (e >= call.state) return;
   const int64_t i = e / p.c, c = e % p.c;
   float s = p.s_in ? p.s_in[bh * call.state + i * p.in_row + c * p.in_col] : 0.f;
@@ -439,6 +440,12 @@ bool tensor_ok(const void* p, const soma_attn_strides& s, int dtype) {
   return aligned(p, width(dtype)) && s.b >= 0 && s.t >= 0 && s.h >= 0;
 }
 
+// An output's rows lie apart.
+bool apart(const soma_attn_strides& s, const soma_attn_dims& d, int width) {
+  return (d.batch < 2 || s.b >= width) && (d.steps < 2 || s.t >= width) &&
+         (d.heads < 2 || s.h >= width);
+}
+
 bool overlap(const float* p, const float* q, int64_t count) {
   if (!p || !q) return false;
   const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
@@ -462,20 +469,14 @@ template <typename T, int RUNS>
 cudaError_t plain(const Call& call, Cut cut, const Spread& s, cudaStream_t st) {
   const size_t smem = sizeof(float) * kTiles * kTile * (2 * s.groups * 4 * RUNS + s.cols);
   constexpr int most = sizeof(float) * kTiles * kTile * (2 * 128 + 128);
-  static const cudaError_t set = [] {
-    const cudaError_t e = cudaFuncSetAttribute(plain_kernel<T, RUNS, true>,
-                                               cudaFuncAttributeMaxDynamicSharedMemorySize, most);
-    return e != cudaSuccess ? e
-                            : cudaFuncSetAttribute(plain_kernel<T, RUNS, false>,
-                                                   cudaFuncAttributeMaxDynamicSharedMemorySize, most);
-  }();
-  if (set != cudaSuccess) return set;
+  cudaError_t e = allow_shared<plain_kernel<T, RUNS, true>>(most);
+  if (e == cudaSuccess) e = allow_shared<plain_kernel<T, RUNS, false>>(most);
+  if (e != cudaSuccess) return e;
   const int64_t rows = call.problems * call.batch * call.heads;
   if (cut.segments > 1) {
     cut.launched = cut.segments - 1;
-    cudaError_t e = launch_overlapped(plain_kernel<T, RUNS, false>,
-                                      dim3((unsigned)(rows * cut.launched)), threads_of(s), smem, st,
-                                      call, cut);
+    e = launch_overlapped(plain_kernel<T, RUNS, false>, dim3((unsigned)(rows * cut.launched)),
+                          threads_of(s), smem, st, call, cut);
     if (e == cudaSuccess) e = launch_join(call, cut, st);
     if (e != cudaSuccess) return e;
   }
@@ -623,9 +624,9 @@ void put_states(Problem* p, const soma_attn_dims& d, bool turned, const float* i
 }  // namespace
 
 cudaError_t launch_join(const Call& call, const Cut& cut, cudaStream_t st) {
-  const unsigned rows = (unsigned)(call.batch * call.heads * call.problems);
-  return launch_overlapped(join_kernel, dim3((unsigned)((call.state + 255) / 256), rows), 256, 0, st,
-                           call, cut);
+  const int64_t rows = call.batch * call.heads * call.problems;
+  return launch_overlapped(join_kernel, dim3((unsigned)(rows * ((call.state + 255) / 256))), 256, 0,
+                           st, call, cut);
 }
 
 }  // namespace attn
@@ -656,7 +657,9 @@ int soma_linear_attn_forward(const void* q, soma_attn_strides q_strides, const v
       !aligned(s_last, 4))
     return SOMA_ERR_INVALID_ARG;
   if (d.batch == 0 || d.heads == 0) return SOMA_OK;
-  if (!log_decay || (d.steps > 0 && (!q || !k || !v || !o))) return SOMA_ERR_INVALID_ARG;
+  if (!log_decay || (d.steps > 0 && (!q || !k || !v || !o)) ||
+      !apart(o_strides, d, d.value_dim))
+    return SOMA_ERR_INVALID_ARG;
   if (overlap(s0, s_last, d.batch * d.heads * d.key_dim * d.value_dim)) return SOMA_ERR_INVALID_ARG;
   Cut cut = cut_of(d, dtype, 1);
   const Parts parts = parts_of(d, cut, 1);
@@ -693,7 +696,9 @@ int soma_linear_attn_backward(const void* q, soma_attn_strides q_strides, const 
       !aligned(s0, 4) || !aligned(lengths, 4) || !aligned(ds_last, 4) || !aligned(ds0, 4))
     return SOMA_ERR_INVALID_ARG;
   if (d.batch == 0 || d.heads == 0) return SOMA_OK;
-  if (!log_decay || (d.steps > 0 && (!q || !k || !v || !d_out || !dq || !dk || !dv)))
+  if (!log_decay || (d.steps > 0 && (!q || !k || !v || !d_out || !dq || !dk || !dv)) ||
+      !apart(dq_strides, d, d.key_dim) || !apart(dk_strides, d, d.key_dim) ||
+      !apart(dv_strides, d, d.value_dim))
     return SOMA_ERR_INVALID_ARG;
   const int64_t states = d.batch * d.heads * d.key_dim * d.value_dim;
   if (overlap(s0, ds0, states) || overlap(ds_last, ds0, states)) return SOMA_ERR_INVALID_ARG;
@@ -730,7 +735,9 @@ int soma_linear_attn_step(const void* q, soma_attn_strides q_strides, const void
       !std::isfinite(scale) || !aligned(log_decay, 4) || !aligned(s, 4))
     return SOMA_ERR_INVALID_ARG;
   if (d.batch == 0 || d.heads == 0) return SOMA_OK;
-  if (!log_decay || !q || !k || !v || !o || !s) return SOMA_ERR_INVALID_ARG;
+  d.steps = 1;
+  if (!log_decay || !q || !k || !v || !o || !s || !apart(o_strides, d, d.value_dim))
+    return SOMA_ERR_INVALID_ARG;
   int* status = status_ptr();
   if (!status) return SOMA_ERR_CUDA;
   Call call = make_call(d, log_decay, nullptr, nullptr, status);

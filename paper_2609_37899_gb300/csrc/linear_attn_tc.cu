@@ -872,24 +872,32 @@ bool make_source(Source* s, const void* base, const soma_attn_strides& st, int64
   return false;
 }
 
+// The registers that a kernel's threads are launched with: its warps share those
+// among them (setmaxnreg), and would wait for ever for more.
+template <auto KERNEL>
+bool launched_with(int registers) {
+  static const int has = [] {
+    cudaFuncAttributes a;
+    return cudaFuncGetAttributes(&a, KERNEL) == cudaSuccess ? a.numRegs : 0;
+  }();
+  return has == registers;
+}
+
 template <typename T, int W>
 cudaError_t launch(const Sources& sources, const Call& call, Cut cut, cudaStream_t st) {
   constexpr size_t smem = Layout<W>::bytes + sizeof(Shared);
   static_assert(smem <= 227 * 1024, "shared memory of a CTA");
-  static const cudaError_t set = [] {
-    const cudaError_t e = cudaFuncSetAttribute(
-        chunk_kernel<T, W, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-    return e != cudaSuccess ? e
-                            : cudaFuncSetAttribute(chunk_kernel<T, W, false>,
-                                                   cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                                   (int)smem);
-  }();
-  if (set != cudaSuccess) return set;
+  if (!launched_with<chunk_kernel<T, W, true>>(Layout<W>::launched) ||
+      !launched_with<chunk_kernel<T, W, false>>(Layout<W>::launched))
+    return cudaErrorInvalidConfiguration;
+  cudaError_t e = allow_shared<chunk_kernel<T, W, true>>(smem);
+  if (e == cudaSuccess) e = allow_shared<chunk_kernel<T, W, false>>(smem);
+  if (e != cudaSuccess) return e;
   const int64_t rows = call.batch * call.heads * call.problems;
   if (cut.segments > 1) {
     cut.launched = cut.segments - 1;
-    cudaError_t e = launch_overlapped(chunk_kernel<T, W, false>, dim3((unsigned)(rows * cut.launched)),
-                                      Layout<W>::threads, smem, st, sources, call, cut);
+    e = launch_overlapped(chunk_kernel<T, W, false>, dim3((unsigned)(rows * cut.launched)),
+                          Layout<W>::threads, smem, st, sources, call, cut);
     if (e != cudaSuccess) return e;
     e = launch_join(call, cut, st);
     if (e != cudaSuccess) return e;

@@ -6,6 +6,8 @@
 // when the predecessor has finished and its writes are visible.
 #pragma once
 
+#include <atomic>
+#include <cstdint>
 #include <cuda_runtime.h>
 #include <utility>
 
@@ -34,6 +36,21 @@ cudaError_t launch_overlapped(void (*kernel)(P...), dim3 grid, int threads, size
   cfg.attrs = &attr;
   cfg.numAttrs = 1;
   return cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(std::forward<A>(args))...);
+}
+
+// Allows launches of KERNEL with up to `bytes` of dynamic shared memory on the
+// current device; asked once for each device.
+template <auto KERNEL>
+cudaError_t allow_shared(size_t bytes) {
+  static std::atomic<uint64_t> asked{0};
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  const uint64_t bit = dev < 64 ? (uint64_t)1 << dev : 0;
+  if (bit && (asked.load(std::memory_order_relaxed) & bit)) return cudaSuccess;
+  e = cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+  if (e == cudaSuccess) asked.fetch_or(bit, std::memory_order_relaxed);
+  return e;
 }
 
 }  // namespace soma

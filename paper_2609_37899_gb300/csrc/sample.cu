@@ -804,11 +804,9 @@ int cluster_of(int64_t rows, int64_t vocab, int before) {
 
 template <typename T, int THREADS, bool HELD>
 cudaError_t launch(const void* logits, Sample s, int n, int* status, cudaStream_t st) {
-  const auto kernel = sample_kernel<T, THREADS, HELD>;
   constexpr int most = sizeof(Shared<THREADS>) + (HELD ? THREADS * kHeld * sizeof(T) : 0);
-  static const cudaError_t set =
-      cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
-  if (set != cudaSuccess) return set;
+  const cudaError_t e = allow_shared<sample_kernel<T, THREADS, HELD>>(most);
+  if (e != cudaSuccess) return e;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
@@ -822,7 +820,7 @@ cudaError_t launch(const void* logits, Sample s, int n, int* status, cudaStream_
   cfg.stream = st;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  return cudaLaunchKernelEx(&cfg, kernel, static_cast<const T*>(logits), (const Sample)s, status);
+  return cudaLaunchKernelEx(&cfg, sample_kernel<T, THREADS, HELD>, static_cast<const T*>(logits), (const Sample)s, status);
 }
 
 bool aligned(const void* p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }

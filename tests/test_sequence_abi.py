@@ -25,7 +25,7 @@ def test_structures_have_the_sizes_of_the_abi(soma):
 
 def test_linear_attn_refusals(soma):
     L, D, S = soma.lib(), soma.soma_attn_dims, soma.soma_attn_strides
-    ok, s = D(2, 3, 4, 8, 16), S(96, 32, 8)
+    ok, s = D(2, 3, 4, 8, 16), S(192, 64, 16)
 
     def fwd(q=FAKE, st=s, dtype=1, d=ok, decay=FAKE, scale=1.0, s0=None, lengths=None, o=FAKE, s_last=None):
         return L.soma_linear_attn_forward(q, st, FAKE, s, FAKE, s, dtype, d, decay, scale, s0, lengths,
@@ -50,13 +50,30 @@ def test_linear_attn_refusals(soma):
         assert f(dtype=3) == 1 and f(scale=INF) == 1 and f(scale=NAN) == 1
     assert fwd(q=None) == 1 and fwd(o=None) == 1 and fwd(decay=None) == 1
     assert fwd(q=ODD) == 1 and fwd(o=ODD) == 1 and fwd(decay=ODD) == 1 and fwd(s0=ODD) == 1
-    assert fwd(lengths=ODD) == 1 and fwd(s_last=ODD) == 1 and fwd(st=S(96, -32, 8)) == 1
+    assert fwd(lengths=ODD) == 1 and fwd(s_last=ODD) == 1 and fwd(st=S(192, -64, 16)) == 1
     assert bwd(do=None) == 1 and bwd(dq=None) == 1 and bwd(dv=ODD) == 1 and bwd(ds0=ODD) == 1
     assert step(q=None) == 1 and step(state=None) == 1 and step(state=ODD) == 1 and step(q=ODD) == 1
+    # outputs whose rows would lie on one another
+    for st in (S(192, 64, 0), S(192, 0, 16), S(0, 64, 16), S(192, 64, 15)):
+        assert L.soma_linear_attn_forward(FAKE, s, FAKE, s, FAKE, s, 1, ok, FAKE, 1.0, None, None, None,
+                                          FAKE, st, None, None, 0, None) == 1
+        if st.t:
+            assert L.soma_linear_attn_step(FAKE, s, FAKE, s, FAKE, s, 1, ok, FAKE, 1.0, FAKE, FAKE, st,
+                                           None) == 1
     states = 2 * 4 * 8 * 16
     for off in (0, 4, 4 * (states - 1), -4 * (states - 1)):
         a, b = ctypes.c_void_p(0x20000), ctypes.c_void_p(0x20000 + off)
         assert fwd(s0=a, s_last=b) == 1 and bwd(s0=a, ds0=b) == 1 and bwd(dsl=a, ds0=b) == 1
+    # few heads and many steps: a workspace
+    long, need = D(1, 1 << 16, 1, 64, 64), [L.soma_linear_attn_workspace_bytes(D(1, 1 << 16, 1, 64, 64), 1, k) for k in (0, 1)]
+    assert 0 < need[0] < need[1]
+    far = S(1 << 22, 64, 64)
+    for ws, n in ((None, need[0]), (ODD, need[0]), (FAKE, need[0] - 1)):
+        assert L.soma_linear_attn_forward(FAKE, far, FAKE, far, FAKE, far, 1, long, FAKE, 1.0, None, None,
+                                          None, FAKE, far, None, ws, n, None) == 3
+    assert L.soma_linear_attn_backward(FAKE, far, FAKE, far, FAKE, far, 1, long, FAKE, 1.0, None, None, None,
+                                       FAKE, far, None, FAKE, far, FAKE, far, FAKE, far, None, FAKE,
+                                       need[1] - 1, None) == 3
     # nothing to do is fine without pointers
     none = D(0, 3, 4, 8, 16)
     assert fwd(q=None, o=None, decay=None, d=none) == 0 and step(q=None, state=None, d=none) == 0
