@@ -2,6 +2,7 @@
 // points, the kernels of fp32 arithmetic and the one-token form
 // (soma_linear_attn_* in include/soma_api.h have the formulas).
 #include <cmath>
+#include <type_traits>
 
 #define SOMA_CHECK_FILE 14
 #include "checked.cuh"
@@ -18,8 +19,12 @@ namespace {
 constexpr int kTile = 16;       // steps that are staged at once
 constexpr int kAtOnce = 2;      // and gone through in one go
 constexpr int kCols = 4;        // and columns
-constexpr int kLoaders = 128;   // threads that stage the next steps meanwhile
+constexpr int kSums = kAtOnce * kCols;
 constexpr int kStepThreads = 256;
+constexpr int kLoaders = 128;
+// Log decays from here up are put off to a tile's end: z is multiplied by up to
+// exp(0.5 * 15) = 1808 then, which fp32's range allows.
+constexpr float kMildest = -0.5f;
 
 // exp(g) by fp32 numbers that have it as their mean: `up` is due `share` / 2^32 of
 // the steps, `low` in the others.  The nearest fp32 number would be off by up to
@@ -31,12 +36,12 @@ struct Decay {
     return (uint32_t)(step + 1) * share < share ? up : low;
   }
 };
-__device__ Decay split_decay(float g) {
-  const double l = exp((double)g);
+__device__ Decay split_decay(double g) {
+  const double l = exp(g);
   Decay d;
   d.low = __double2float_rd(l);
   d.up = __double2float_ru(l);
-  d.share = d.up > d.low ? (uint32_t)((l - d.low) / ((double)d.up - d.low) * 4294967295.0) : 0;
+  d.share = d.up > d.low ? (uint32_t)((l - d.low) * (1.f / (d.up - d.low)) * 4294967295.0) : 0;
   return d;
 }
 
@@ -53,25 +58,44 @@ struct Tile {
   __device__ float* z(int buf) const { return y(buf) + kTile * rows; }
 };
 
+// Adds what a lane and its partner hold: the first N sums for the lower of them,
+// the next N for the upper.
+template <int N>
+__device__ __forceinline__ void fold(float (&o)[kSums], bool upper, int partner) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const float sent = upper ? o[i] : o[i + N];
+    o[i] = (upper ? o[i + N] : o[i]) + __shfl_xor_sync(0xffffffffu, sent, partner);
+  }
+}
+
 // The recurrence step by step in fp32: one CTA per problem, segment, sequence and
 // head, the state in registers, RUNS runs of four rows by four columns per thread.
-// Threads of `groups` neighbouring lanes hold the rows of the same columns.  A few steps at a
+// Up to eight neighbouring lanes (`groups`) hold the rows of the same columns.  A few steps at a
 // time: what they read and the sums over their rows do not wait for one another, only
-// the state itself does.  The last kLoaders threads stage the next tile.
-// Instruction issue bounds it: three fp32 instructions per element of the state and
-// step.  Packed pairs (fma.rn.f32x2) issue at half the rate here and need moves:
-// 16 x 2048 x 8 heads of 128 x 128 took 1000 us.
+// the state itself does.
+// Within a tile the state is kept as S l^-k, k steps into the tile, so that it is
+// decayed once per tile and the decays go into the factors of z and of the output: two
+// fp32 instructions per element of the state and step.  Strong decays, whose powers
+// would cost range, are applied at each step, a third instruction.
+// 16 x 2048 x 8 heads of 128 x 128 in fp32: 797 us forward, 2303 backward (floors of
+// their bytes 80 and 139).  Shared memory bounds it, four cycles for every 16 bytes of
+// a lane that feed 16 multiply-adds, next to instruction issue; few warps fit beside
+// the state to cover their latency.  Packed pairs (fma.rn.f32x2) were no faster.
 template <typename T, int RUNS, bool OUT>
 __global__ void __launch_bounds__(most_threads(RUNS))
-plain_kernel(const __grid_constant__ Call call, const __grid_constant__ Cut cut) {
+plain_kernel(const __grid_constant__ Call call, const __grid_constant__ Cut cut, int loaders) {
   constexpr int kRows = 4 * RUNS;
   extern __shared__ __align__(16) float smem[];
   __shared__ Decay decay;
-  __shared__ float multiplier[kTiles][kTile];
+  __shared__ float multiplier[kTiles][kTile];  // of the state, before a step
+  __shared__ float2 factor[kTile];             // of z and of the output
+  __shared__ float first_decay;
   admit_successor();
   after_predecessor();
-  const int workers = blockDim.x - kLoaders;
-  const bool loads = (int)threadIdx.x >= workers;
+  // the last `loaders` threads stage, or if there are none, all
+  const int workers = blockDim.x - loaders;
+  const bool loads = !loaders || (int)threadIdx.x >= workers;
   const Problem& p = call.p[blockIdx.x % call.problems];
   const int64_t rest = blockIdx.x / call.problems;
   const int seg = (int)(rest % cut.launched);
@@ -81,7 +105,15 @@ plain_kernel(const __grid_constant__ Call call, const __grid_constant__ Cut cut)
   const int64_t which = bh * call.problems + blockIdx.x % call.problems;
   const int64_t len = length_of(call, b);
   const float g = decay_of(call, h);
-  if (threadIdx.x == 0) decay = split_decay(g);
+  const bool put_off = g >= kMildest;  // the decays of a tile
+  if (threadIdx.x == 0) {
+    decay = split_decay(put_off ? kTile * (double)g : (double)g);
+    first_decay = expf(g);
+  }
+  if (threadIdx.x < kTile) {
+    const float e = put_off ? (float)threadIdx.x : 0.f;
+    factor[threadIdx.x] = make_float2(p.f * power_of(-g, e), p.g * power_of(g, e));
+  }
   // this segment's steps [first, last) in time, and how many of the sequence come
   // before them in the recurrence's order
   const int place = p.reversed ? cut.segments - 1 - seg : seg;
@@ -95,39 +127,43 @@ plain_kernel(const __grid_constant__ Call call, const __grid_constant__ Cut cut)
   // steps k0 .. of the segment, rows and columns and steps past the end as zeros
   bool fresh = false;  // a document started in what this thread has seen
   const auto stage = [&](int64_t k0, int buf) {
-    const int thread = (int)threadIdx.x - workers;
-    const T* x = static_cast<const T*>(p.x) + b * p.xs.b + h * p.xs.h;
-    const T* y = static_cast<const T*>(p.y) + b * p.ys.b + h * p.ys.h;
-    const T* z = static_cast<const T*>(p.z) + b * p.zs.b + h * p.zs.h;
+    const int thread = threadIdx.x - (loaders ? workers : 0);
+    const int all = loaders ? loaders : blockDim.x;
     const int n = count - k0 < kTile ? (int)(count - k0) : kTile;
-    const auto copy = [&](const T* from, int64_t stride, int width, int wide, float* to) {
+    const auto copy = [&](const void* base, const soma_attn_strides& s, int width, int wide,
+                          float* to) {
+      const T* from = static_cast<const T*>(base) + b * s.b + h * s.h;
+      const int64_t stride = s.t;
       if (std::is_same<T, float>::value) {
         // asynchronous: whole tiles are on their way
         const bool pieces = width % 4 == 0 && stride % 4 == 0 &&
                             (reinterpret_cast<uintptr_t>(from) & 15) == 0;
         const int each = pieces ? 4 : 1, across = wide / each;
-        const int i = thread % across * each, per = kLoaders / across;
-        if (thread >= per * across) return;
-        const int k1 = thread / across, upto = i < width ? n : 0;
-        const T* src = from + step_of(k0 + k1) * stride + i;
+        const int at_once = min(across, all), per = all / at_once;
         const int64_t next = (p.reversed ? -per : per) * stride;
-        uint32_t dst = tc::smem_u32(to + k1 * wide + i);
-#pragma unroll 4
-        for (int k = k1; k < kTile; k += per, src += next, dst += per * wide * 4) {
-          const bool there = k < upto;  // zeros otherwise
-          if (pieces)
-            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst),
-                         "l"(there ? src : from), "r"(there ? 16 : 0)
-                         : "memory");
-          else
-            asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst),
-                         "l"(there ? src : from), "r"(there ? 4 : 0)
-                         : "memory");
+        const int k1 = thread / at_once;
+        if (k1 >= per) return;
+        for (int i = thread % at_once * each; i < wide; i += at_once * each) {
+          const int upto = i < width ? n : 0;
+          const T* src = from + step_of(k0 + k1) * stride + i;
+          uint32_t dst = tc::smem_u32(to + k1 * wide + i);
+#pragma unroll 2
+          for (int k = k1; k < kTile; k += per, src += next, dst += per * wide * 4) {
+            const bool there = k < upto;  // zeros otherwise
+            if (pieces)
+              asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst),
+                           "l"(there ? src : from), "r"(there ? 16 : 0)
+                           : "memory");
+            else
+              asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst),
+                           "l"(there ? src : from), "r"(there ? 4 : 0)
+                           : "memory");
+          }
         }
       } else {
         // 16 loads are on their way before the first is stored
         constexpr int kAhead = 16;
-        const int i = thread % wide, per = kLoaders / wide;
+        const int i = thread % wide, per = all / wide;
         if (thread >= per * wide) return;
         for (int k = thread / wide; k < kTile; k += per * kAhead) {
           T v[kAhead];
@@ -144,20 +180,19 @@ plain_kernel(const __grid_constant__ Call call, const __grid_constant__ Cut cut)
         }
       }
     };
-    if (OUT) copy(x, p.xs.t, p.a, tile.rows, tile.x(buf));
-    copy(y, p.ys.t, p.a, tile.rows, tile.y(buf));
-    copy(z, p.zs.t, p.c, tile.cols, tile.z(buf));
+#pragma unroll 1
+    for (int w = OUT ? 0 : 1; w < 3; ++w)
+      copy(w == 0 ? p.x : w == 1 ? p.y : p.z, w == 0 ? p.xs : w == 1 ? p.ys : p.zs,
+           w == 2 ? p.c : p.a, w == 2 ? tile.cols : tile.rows,
+           w == 0 ? tile.x(buf) : w == 1 ? tile.y(buf) : tile.z(buf));
     if (thread < kTile) {
       float m = 1.f;
       if (thread < n) {
         const int64_t t = step_of(k0 + thread);
-        m = decay.at(done + k0 + thread);
-        if (p.reversed) {
-          if (t == len - 1) m = 1.f;
-          else if (resets && resets[t + 1]) m = 0.f;
-        } else if (resets && resets[t]) {
-          m = 0.f;
-        }
+        const bool none = p.reversed && t == len - 1;  // the decay that belongs to no step
+        if (!put_off) m = none ? 1.f : decay.at(done + k0 + thread);
+        else if (thread == 0) m = k0 ? decay.at(k0 / kTile) : none ? 1.f : first_decay;
+        if (resets && !none && resets[p.reversed ? t + 1 : t]) m = 0.f;
         fresh = fresh || m == 0.f;
       }
       multiplier[buf][thread] = m;
@@ -166,7 +201,7 @@ plain_kernel(const __grid_constant__ Call call, const __grid_constant__ Cut cut)
 
   // row of register r: runs of four, `groups` runs apart
   const int group = threadIdx.x % groups, c0 = threadIdx.x / groups * kCols;
-  const bool holds = !loads && c0 < tile.cols;
+  const bool holds = (!loaders || !loads) && c0 < tile.cols;
   const bool works = __any_sync(0xffffffffu, holds);
   const auto row_of = [&](int r) { return (r / 4 * groups + group) * 4 + r % 4; };
   const bool joined = cut.segments > 1 && seg > 0;
@@ -178,14 +213,19 @@ plain_kernel(const __grid_constant__ Call call, const __grid_constant__ Cut cut)
 #pragma unroll
   for (int r = 0; r < kRows; ++r)
 #pragma unroll
-    for (int j = 0; j < kCols; ++j) {
-      const int i = row_of(r), c = c0 + j;
-      S[r][j] = from && holds && i < p.a && c < p.c ? from[i * from_row + c * from_col] : 0.f;
-    }
-  // of the columns, lane `group` stores those that leave `group` by `groups`
-  bool stores[kCols];
+    for (int j = 0; j < kCols; ++j) S[r][j] = 0.f;
+  if (from && holds)
 #pragma unroll
-  for (int j = 0; j < kCols; ++j) stores[j] = holds && j % groups == group && c0 + j < p.c;
+    for (int r = 0; r < kRows; ++r)
+#pragma unroll
+      for (int j = 0; j < kCols; ++j) {
+        const int i = row_of(r), c = c0 + j;
+        if (i < p.a && c < p.c) S[r][j] = from[i * from_row + c * from_col];
+      }
+  // Of the sums of kAtOnce steps (in rows of kCols), a lane gets kSums / groups from
+  // `mine` on, `mine_cols` of them or fewer in its columns.
+  const int mine = (group & 1) * 4 + (group & 2) + (group >> 2);
+  const int mine_cols = holds ? p.c - c0 - mine % kCols : 0;
 
   __syncthreads();  // the decay
   T* out = static_cast<T*>(p.out) + b * p.os.b + h * p.os.h;
@@ -197,76 +237,93 @@ plain_kernel(const __grid_constant__ Call call, const __grid_constant__ Cut cut)
     if (k0 < count) stage(k0, buf);
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
-  if (loads) {
-    stage_next(0, 0);
-    stage_next(kTile, 1);
-    arrived(false);
-  }
-  __syncthreads();
-  int buf = 0;
+  int buf = kTiles - 2;
   const int64_t next_out = p.reversed ? -p.os.t : p.os.t;
-  for (int64_t k0 = 0; k0 < count; k0 += kTile) {
+  // a tile's steps; kEach: every step decays the state, which is whole then
+  const auto go = [&](auto each, int n, T* to) {
+    constexpr bool kEach = decltype(each)::value;
+    if (!kEach) {
+      const float m = multiplier[buf][0];
+#pragma unroll
+      for (int r = 0; r < kRows; ++r)
+#pragma unroll
+        for (int j = 0; j < kCols; ++j) S[r][j] *= m;
+    }
+    for (int k = 0; k < n; k += kAtOnce) {
+      float o[kSums];
+#pragma unroll
+      for (int u = 0; u < kAtOnce; ++u) {
+        const float m = multiplier[buf][k + u], f = factor[k + u].x;
+        const float* z = tile.z(buf) + (k + u) * tile.cols + c0;
+        const float4 v4 =
+            holds ? *reinterpret_cast<const float4*>(z) : make_float4(0.f, 0.f, 0.f, 0.f);
+        const float v[kCols] = {f * v4.x, f * v4.y, f * v4.z, f * v4.w};
+        if (m == 0.f) {  // nothing passes, whatever it is
+#pragma unroll
+          for (int r = 0; r < kRows; ++r)
+#pragma unroll
+            for (int j = 0; j < kCols; ++j) S[r][j] = 0.f;
+        }
+#pragma unroll
+        for (int j = 0; j < kCols; ++j) o[u * kCols + j] = 0.f;
+#pragma unroll
+        for (int q = 0; q < RUNS; ++q) {
+          const int at = (k + u) * tile.rows + (q * groups + group) * 4;
+          const float4 y4 = *reinterpret_cast<const float4*>(tile.y(buf) + at);
+          const float yr[4] = {y4.x, y4.y, y4.z, y4.w};
+          float xr[4];
+          if (OUT) {
+            const float4 x4 = *reinterpret_cast<const float4*>(tile.x(buf) + at);
+            xr[0] = x4.x; xr[1] = x4.y; xr[2] = x4.z; xr[3] = x4.w;
+          }
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int j = 0; j < kCols; ++j) {
+              float& s = S[4 * q + r][j];
+              s = kEach ? fmaf(m, s, yr[r] * v[j]) : fmaf(yr[r], v[j], s);
+              if (OUT) o[u * kCols + j] = fmaf(xr[r], s, o[u * kCols + j]);
+            }
+        }
+      }
+      if (OUT) {
+        if (groups > 1) fold<4>(o, group & 1, 1);
+        if (groups > 2) fold<2>(o, group & 2, 2);
+        if (groups > 4) fold<1>(o, group & 4, 4);
+#pragma unroll
+        for (int i = 0; i < kSums; ++i) {
+          const int u = k + mine / kCols + i / kCols;
+          if (i * groups < kSums && i % kCols < mine_cols && u < n)
+            to[i % kCols + i / kCols * next_out] = from_f32<T>(factor[u].y * o[i]);
+        }
+        to += kAtOnce * next_out;
+      }
+    }
+  };
+  // Two tiles ahead of use; the copying code is there once, as cold instructions
+  // are most of a short call's time.
+  for (int64_t k0 = -2 * kTile; k0 < count; k0 += kTile) {
     if (loads) {
       stage_next(k0 + 2 * kTile, (buf + 2) % kTiles);
       arrived(false);
-    } else if (works) {
+    }
+    if (works && k0 >= 0) {
       const int n = count - k0 < kTile ? (int)(count - k0) : kTile;
-      T* to = out + step_of(k0) * p.os.t + c0;
-      for (int k = 0; k < n; k += kAtOnce) {
-        float o[kAtOnce][kCols];
-#pragma unroll
-        for (int u = 0; u < kAtOnce; ++u) {
-          const float m = multiplier[buf][k + u];
-          const float4 v4 = holds ? *reinterpret_cast<const float4*>(tile.z(buf) + (k + u) * tile.cols + c0)
-                                  : make_float4(0.f, 0.f, 0.f, 0.f);
-          const float v[kCols] = {p.f * v4.x, p.f * v4.y, p.f * v4.z, p.f * v4.w};
-          if (m == 0.f) {  // nothing passes, whatever it is
-#pragma unroll
-            for (int r = 0; r < kRows; ++r)
-#pragma unroll
-              for (int j = 0; j < kCols; ++j) S[r][j] = 0.f;
-          }
-#pragma unroll
-          for (int j = 0; j < kCols; ++j) o[u][j] = 0.f;
-#pragma unroll
-          for (int q = 0; q < RUNS; ++q) {
-            const int at = (k + u) * tile.rows + (q * groups + group) * 4;
-            const float4 y4 = *reinterpret_cast<const float4*>(tile.y(buf) + at);
-            const float yr[4] = {y4.x, y4.y, y4.z, y4.w};
-            float xr[4];
-            if (OUT) {
-              const float4 x4 = *reinterpret_cast<const float4*>(tile.x(buf) + at);
-              xr[0] = x4.x; xr[1] = x4.y; xr[2] = x4.z; xr[3] = x4.w;
-            }
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-#pragma unroll
-              for (int j = 0; j < kCols; ++j) {
-                float& s = S[4 * q + r][j];
-                s = fmaf(m, s, yr[r] * v[j]);
-                if (OUT) o[u][j] = fmaf(xr[r], s, o[u][j]);
-              }
-          }
-        }
-        if (OUT) {
-          for (int s = 1; s < groups; s <<= 1)
-#pragma unroll
-            for (int u = 0; u < kAtOnce; ++u)
-#pragma unroll
-              for (int j = 0; j < kCols; ++j) o[u][j] += __shfl_xor_sync(0xffffffffu, o[u][j], s);
-#pragma unroll
-          for (int u = 0; u < kAtOnce; ++u, to += next_out) {
-#pragma unroll
-            for (int j = 0; j < kCols; ++j)
-              if (stores[j] && k + u < n) to[j] = from_f32<T>(p.g * o[u][j]);
-          }
-        }
-      }
+      T* to = out + step_of(k0) * p.os.t + c0 + mine / kCols * next_out + mine % kCols;
+      if (put_off) go(std::false_type(), n, to);
+      else go(std::true_type(), n, to);
     }
     __syncthreads();
     buf = (buf + 1) % kTiles;
   }
   if (loads) arrived(true);
+  if (put_off && count > 0) {  // the state itself
+    const float l = power_of(decay_of(call, h), (float)((count - 1) % kTile));
+#pragma unroll
+    for (int r = 0; r < kRows; ++r)
+#pragma unroll
+      for (int j = 0; j < kCols; ++j) S[r][j] *= l;
+  }
 
   if (!OUT) {
     // what the segment adds, and what it leaves of the state before it: the
@@ -296,7 +353,10 @@ plain_kernel(const __grid_constant__ Call call, const __grid_constant__ Cut cut)
   for (int64_t e = threadIdx.x; e < (end - begin) * p.c; e += blockDim.x)
     out[(begin + e / p.c) * p.os.t + e % p.c] = from_f32<T>(0.f);
   if (!p.s_out || !holds || seg != cut.segments - 1) return;
-  const float left = !p.reversed || len == 0 ? 1.f : resets && resets[0] ? 0.f : decay.at(len);
+  const float left = !p.reversed || len == 0 ? 1.f
+                     : resets && resets[0]     ? 0.f
+                     : put_off                 ? first_decay
+                                               : decay.at(len);
 #pragma unroll
   for (int r = 0; r < kRows; ++r)
 #pragma unroll
@@ -452,6 +512,8 @@ bool overlap(const float* p, const float* q, int64_t count) {
   return (a < b ? b - a : a - b) < (uintptr_t)count * sizeof(float);
 }
 
+constexpr size_t kSharedOfSm = 228 * 1024;
+
 // Threads of a CTA of the plain kernel: `groups` of them share columns, each with
 // `runs` runs of four rows, as few as hold all rows.
 struct Spread {
@@ -459,30 +521,45 @@ struct Spread {
 };
 Spread spread_of(int rows, int columns) {
   Spread s = {1, 0, (columns + kCols - 1) / kCols * kCols};
-  while (s.groups * 16 < rows) s.groups *= 2;
+  while (s.groups * 16 < rows) s.groups *= 2;  // 8 at most: key and value dims end at 128
   s.runs = (rows + 4 * s.groups - 1) / (4 * s.groups);
   return s;
 }
-int threads_of(const Spread& s) { return (s.groups * (s.cols / kCols) + 31) / 32 * 32 + kLoaders; }
+size_t shared_of(const Spread& s) {
+  return sizeof(float) * kTiles * kTile * (2 * s.groups * 4 * s.runs + s.cols);
+}
+// Threads that stage the next steps while the others work.  None in fp32 with few
+// threads, where all of them do it: the copies are asynchronous, and the registers
+// of four more warps would keep another CTA away (64 x 64: 290 us instead of 409 for
+// 16 x 2048 x 8; 33 x 65, backward, 4 x 777 x 7: 137 instead of 163).  With eight
+// warps at work it is the other way round (128 x 128: 916 and 763 us).
+int loaders_of(const Spread& s, int dtype) {
+  return dtype == SOMA_FP32 && s.groups * (s.cols / kCols) <= 160 ? 0 : kLoaders;
+}
+int threads_of(const Spread& s, int dtype) {
+  return (s.groups * (s.cols / kCols) + 31) / 32 * 32 + loaders_of(s, dtype);
+}
 
 template <typename T, int RUNS>
 cudaError_t plain(const Call& call, Cut cut, const Spread& s, cudaStream_t st) {
-  const size_t smem = sizeof(float) * kTiles * kTile * (2 * s.groups * 4 * RUNS + s.cols);
+  const size_t smem = shared_of(s);
   constexpr int most = sizeof(float) * kTiles * kTile * (2 * 128 + 128);
   cudaError_t e = allow_shared<plain_kernel<T, RUNS, true>>(most);
   if (e == cudaSuccess) e = allow_shared<plain_kernel<T, RUNS, false>>(most);
   if (e != cudaSuccess) return e;
   const int64_t rows = call.problems * call.batch * call.heads;
+  const int dtype = std::is_same<T, float>::value ? SOMA_FP32 : SOMA_BF16;
+  const int loaders = loaders_of(s, dtype);
   if (cut.segments > 1) {
     cut.launched = cut.segments - 1;
     e = launch_overlapped(plain_kernel<T, RUNS, false>, dim3((unsigned)(rows * cut.launched)),
-                          threads_of(s), smem, st, call, cut);
+                          threads_of(s, dtype), smem, st, call, cut, loaders);
     if (e == cudaSuccess) e = launch_join(call, cut, st);
     if (e != cudaSuccess) return e;
   }
   cut.launched = cut.segments;
   return launch_overlapped(plain_kernel<T, RUNS, true>, dim3((unsigned)(rows * cut.segments)),
-                           threads_of(s), smem, st, call, cut);
+                           threads_of(s, dtype), smem, st, call, cut, loaders);
 }
 
 template <typename T>
@@ -527,7 +604,9 @@ Cut cut_of(const soma_attn_dims& d, int dtype, int problems) {
   } else {
     const int wide = d.key_dim > d.value_dim ? d.key_dim : d.value_dim;
     const Spread s = spread_of(problems > 1 ? wide : d.key_dim, problems > 1 ? wide : d.value_dim);
-    resident *= most_threads(s.runs) / threads_of(s);
+    const int by_threads = most_threads(s.runs) / threads_of(s, dtype);
+    const int by_shared = (int)(kSharedOfSm / (shared_of(s) + 2048));
+    resident *= by_threads < by_shared ? by_threads : by_shared;
   }
   Cut best = {};
   best.segments = 1;
