@@ -939,8 +939,9 @@ def _here(**tensors):
     """Refuses tensors of another device than the current one, whose stream the call goes to."""
     index = torch.cuda.current_device()
     for name, t in tensors.items():
-        if t is not None and t.is_cuda and t.device.index != index:
-            raise ValueError(f"{name}: on {t.device}, but the current device is cuda:{index}")
+        if t is not None and t.is_cuda and t.get_device() != index:
+            raise ValueError(f"{name}: on cuda:{t.get_device()}, but the current device is "
+                             f"cuda:{index}")
 
 
 def _attn_dims(q, v) -> soma_attn_dims:

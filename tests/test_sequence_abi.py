@@ -131,7 +131,10 @@ def test_the_binding_refuses_what_it_can_see(soma):
 
 def test_the_binding_refuses_another_device(soma, monkeypatch):
     class There:
-        is_cuda, device = True, torch.device("cuda:1")
+        is_cuda = True
+
+        def get_device(self):
+            return 1
 
     monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
     with pytest.raises(ValueError, match="current device is cuda:0"):
