@@ -654,7 +654,8 @@ int soma_linear_ce_backward(const void* h, const void* emb, soma_linear_ce_dims 
  * and the decayed v, for the state, to twice its bits; sums and states are fp32.
  * fp16: those three are scaled by powers of two to the range of the type.  Other
  * layouts, and fp32, take kernels of fp32 arithmetic, which are several times
- * slower. */
+ * slower; within 16 steps they scale k_j v_j^T, and the like of the gradients, by
+ * up to 1808, so that those and the states are to stay below 1e35. */
 typedef struct soma_attn_dims {
   int64_t batch; /* 0 .. 2^31 - 1 */
   int64_t steps; /* 0 .. 2^31 - 1 */

@@ -135,3 +135,22 @@ def test_documents_of_one_step():
         out = _run(s)
         _check(s, out)
         assert not out["ds0"].any()
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("B,T", [(3, 300), (1, 3000), (2, 17), (2, 16), (2, 15)])
+def test_mild_and_strong_decays_of_one_call(B, T, dtype):
+    """Decays that the fp32 kernels put off to the end of 16 steps, and such that they do not, next to
+    one another: exp(-1/2) is the last of the first kind."""
+    decay = [0.0, -1e-3, -0.4999, -0.5, -0.50001, -3.0, -90.0]
+    s = _case(B, T, len(decay), 33, 21, dtype, seed=B + T, ragged=B > 1, resets=True, decay=decay)
+    _check(s, _run(s))
+
+
+def test_large_values_in_32_bits():
+    """Products of 1e34, with the strongest decay that is put off."""
+    s = _case(2, 200, 2, 32, 32, "fp32", seed=9, decay=-0.5)
+    s["v"] *= 1e33
+    s["do"] *= 1e-3
+    s["s0"] *= 1e33
+    _check(s, _run(s))
