@@ -187,6 +187,7 @@ def _open(path: str):
                                                  u64, vp, i32, i32, vp, vp, vp, sz, vp])
         _sig(L, "soma_debug_wait_timeout", i32, [ctypes.c_uint32, vp])
         _sig(L, "soma_debug_scan_timeout", i32, [vp, vp, ctypes.c_uint32, vp])
+        _sig(L, "soma_debug_attn_timeout", i32, [vp, vp, ctypes.c_uint32, vp])
         bd = soma_body_dims
         _sig(L, "soma_body_param_count", i64, [bd])
         _sig(L, "soma_body_workspace_bytes", sz, [bd, i32, i32, i32, i32])
@@ -465,6 +466,16 @@ def debug_scan_timeout(src: torch.Tensor, max_polls: int, stream=None) -> torch.
     _check(lib().soma_debug_scan_timeout(_dev(src, torch.float32, "src", 1024),
                                          ctypes.c_void_p(out.data_ptr()), max_polls,
                                          _stream(stream)), "soma_debug_scan_timeout")
+    return out
+
+
+def debug_attn_timeout(src: torch.Tensor, max_polls: int, stream=None) -> torch.Tensor:
+    """A place of linear attention's kernels that is never handed back (see soma_api.h): what arrived
+    of src fp32 [5, 256], and the copies made of x, y and z, as one tensor of 1027."""
+    out = torch.full((1027,), float("nan"), device=src.device)
+    _check(lib().soma_debug_attn_timeout(_dev(src, torch.float32, "src", 1280),
+                                         ctypes.c_void_p(out.data_ptr()), max_polls,
+                                         _stream(stream)), "soma_debug_attn_timeout")
     return out
 
 

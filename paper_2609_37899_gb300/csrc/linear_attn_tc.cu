@@ -86,13 +86,38 @@ struct Shared {
 
 // A bounded wait of a whole warp; on running out it records the timeout and
 // raises the CTA's abort flag, after which no wait waits.
-__device__ __forceinline__ bool wait(uint64_t* bar, uint32_t parity, Shared* sh, int* status) {
+__device__ __forceinline__ bool wait(uint64_t* bar, uint32_t parity, Shared* sh, int* status,
+                                     uint32_t max_polls = 1u << 22) {
   if (__all_sync(0xffffffffu, tc::mbar_try_wait(bar, parity))) return true;
-  const bool ok = !sh->abort && tc::mbar_wait(bar, parity);
+  const bool ok = !sh->abort && tc::mbar_wait(bar, parity, max_polls);
   if (__all_sync(0xffffffffu, ok)) return true;
   if (!sh->abort) atomicCAS(status, 0, SOMA_ERR_TIMEOUT);
   sh->abort = 1;
   return false;
+}
+
+// The tiles that a CTA has asked for; those of y go to its two places in turn.
+struct Copies {
+  uint32_t x, y, z;
+};
+
+// Whether the loading warp (all of it) may copy into a place that it has waited
+// for.  After an abort the others go on without waiting and hand places back
+// whose copies may still be on their way, with their barriers not free.
+__device__ __forceinline__ bool may_copy(const Shared& sh) {
+  return !__any_sync(0xffffffffu, sh.abort);
+}
+
+// The loading warp's last act: the last copy into each place has landed before the
+// CTA leaves its shared memory to another.  In a whole run the products have waited
+// for it; after an abort, whoever gave up, it may be on its way.
+__device__ __forceinline__ void land(Shared& sh, const Copies& c) {
+  if (c.x) tc::mbar_wait(&sh.x_full, (c.x - 1) & 1);
+  for (uint32_t i = 0; i < 2; ++i) {
+    const uint32_t n = (c.y + 1 - i) / 2;
+    if (n) tc::mbar_wait(&sh.y_full[i], (n - 1) & 1);
+  }
+  if (c.z) tc::mbar_wait(&sh.z_full, (c.z - 1) & 1);
 }
 
 // How a tensor [batch][steps][heads][width] is seen by its tensor map, 64 columns
@@ -716,27 +741,26 @@ chunk_kernel(const __grid_constant__ Sources sources, const __grid_constant__ Ca
       }
       __syncwarp();
     };
-    int k = 0;
-    for (; k < count; ++k) {
+    const auto free = [&](uint64_t* bar, uint32_t parity) {
+      return wait(bar, parity, &sh, status) && may_copy(sh);
+    };
+    Copies copies = {};
+    for (int k = 0; k < count; ++k) {
       const int t0 = start_of(k);
       const uint32_t s = k & 1, round = (k >> 1) & 1;
       if (OUT) {
-        if (!wait(&sh.x_empty, (k & 1) ^ 1, &sh, status)) break;
+        if (!free(&sh.x_empty, (k & 1) ^ 1)) break;
         load(L::x, sx, p.a, t0, &sh.x_full);
+        ++copies.x;
       }
-      if (!wait(&sh.y_empty[s], round ^ 1, &sh, status)) break;
+      if (!free(&sh.y_empty[s], round ^ 1)) break;
       load(L::y + s * L::tile, sy, p.a, t0, &sh.y_full[s]);
-      if (!wait(&sh.z_empty, (k & 1) ^ 1, &sh, status)) break;
+      ++copies.y;
+      if (!free(&sh.z_empty, (k & 1) ^ 1)) break;
       load(L::z, sz, p.c, t0, &sh.z_full);
+      ++copies.z;
     }
-    // an aborting CTA leaves only after its copies have landed
-    if (k < count) {
-      for (int j = max(0, k - 1); j <= k; ++j) {
-        tc::mbar_wait(&sh.y_full[j & 1], (j >> 1) & 1, 1u << 16);
-        tc::mbar_wait(&sh.z_full, j & 1, 1u << 16);
-        if (OUT) tc::mbar_wait(&sh.x_full, j & 1, 1u << 16);
-      }
-    }
+    land(sh, copies);
   } else if (warp == L::issuer) {
     // ---- P, O1 and O2: the whole warp waits, one elected thread issues ---------
     if (OUT) {
@@ -826,6 +850,52 @@ chunk_kernel(const __grid_constant__ Sources sources, const __grid_constant__ Ca
   __syncthreads();
   tc::tc_fence_after();
   if (warp == L::issuer) tc::tmem_dealloc(tmem, L::columns);
+}
+
+// A wait of the loader's that runs out, with copies under way: x, both places of y
+// and z are filled from src, y's first place is waited for, handed back and filled
+// again, z's is never handed back.  out: the four tiles as they are when the CTA
+// would leave, then the copies made of each (one more is refused).
+constexpr int kTimeoutTest = 256;  // floats of a tile
+__global__ void __launch_bounds__(32)
+copies_timeout_kernel(const float* src, float* out, uint32_t max_polls, int* status) {
+  __shared__ __align__(128) float tiles[4][kTimeoutTest];
+  __shared__ Shared sh;
+  if (threadIdx.x == 0) {
+    tc::mbar_init(&sh.x_full, 1);
+    tc::mbar_init(&sh.y_full[0], 1);
+    tc::mbar_init(&sh.y_full[1], 1);
+    tc::mbar_init(&sh.z_full, 1);
+    tc::mbar_init(&sh.z_empty, 1);
+    tc::mbar_fence_init();
+    sh.abort = 0;
+  }
+  __syncwarp();
+  Copies copies = {};
+  const auto copy = [&](int tile, int from, uint64_t* bar, uint32_t& count) {
+    if (!may_copy(sh)) return;
+    ++count;
+    if (threadIdx.x == 0) {
+      tc::mbar_arrive_expect_tx(bar, sizeof(tiles[0]));
+      tc::bulk_g2s(tiles[tile], src + from * kTimeoutTest, sizeof(tiles[0]), bar);
+    }
+    __syncwarp();
+  };
+  copy(0, 0, &sh.x_full, copies.x);
+  copy(1, 1, &sh.y_full[0], copies.y);
+  copy(2, 2, &sh.y_full[1], copies.y);
+  copy(3, 3, &sh.z_full, copies.z);
+  if (wait(&sh.y_full[0], 0, &sh, status)) copy(1, 4, &sh.y_full[0], copies.y);
+  wait(&sh.z_empty, 0, &sh, status, max_polls);
+  copy(3, 0, &sh.z_full, copies.z);
+  land(sh, copies);
+  __syncwarp();
+  for (int i = threadIdx.x; i < 4 * kTimeoutTest; i += 32) out[i] = tiles[i / kTimeoutTest][i % kTimeoutTest];
+  if (threadIdx.x == 0) {
+    out[4 * kTimeoutTest] = (float)copies.x;
+    out[4 * kTimeoutTest + 1] = (float)copies.y;
+    out[4 * kTimeoutTest + 2] = (float)copies.z;
+  }
 }
 
 // ------------------------------------------------------------------- host --
@@ -939,3 +1009,17 @@ bool launch_chunks(const Call& call, const Cut& cut, int dtype, cudaStream_t st,
 
 }  // namespace attn
 }  // namespace soma
+
+using namespace soma;
+using namespace soma::attn;
+
+extern "C" int soma_debug_attn_timeout(const float* src, float* out, uint32_t max_polls,
+                                       void* stream) {
+  if (!src || !out || (reinterpret_cast<uintptr_t>(src) & 15) ||
+      (reinterpret_cast<uintptr_t>(out) & 3) || max_polls < 1 || max_polls > (1u << 22))
+    return SOMA_ERR_INVALID_ARG;
+  int* status = status_ptr();
+  if (!status) return SOMA_ERR_CUDA;
+  copies_timeout_kernel<<<1, 32, 0, (cudaStream_t)stream>>>(src, out, max_polls, status);
+  return cudaGetLastError() == cudaSuccess ? SOMA_OK : SOMA_ERR_CUDA;
+}
