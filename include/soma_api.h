@@ -644,8 +644,11 @@ int soma_linear_ce_backward(const void* h, const void* emb, soma_linear_ce_dims 
  * and so o_t = scale (sum_{j<=t} l^{t-j} <q_t, k_j> v_j + l^{t+1} S_{-1}^T q_t).
  * States are fp32 [batch][heads][key_dim][value_dim]; q, k, v, o and their
  * gradients are of one soma_dtype.  log_decay: fp32 [heads], each at most 0 and
- * given, not learned (-infinity: a step sees itself alone); a head whose decay
- * is above 0 or NaN has NaN outputs, and SOMA_ERR_NONFINITE is recorded.
+ * given, not learned (-infinity: a step sees itself alone).  A head whose log
+ * decay is above 0 or NaN records SOMA_ERR_NONFINITE and has NaN for o, dq, dk and
+ * dv of every step within its sequence and for the states; but a sequence of no
+ * steps leaves its states as they are, and ds0 is 0 where the first step starts a
+ * document.
  *
  * lengths and resets are as in the gated linear recurrence: sequence b ends
  * after lengths[b] steps (clamped to 0 .. steps), later steps are not read,

@@ -62,9 +62,10 @@ struct Cut {
   float2* fades;     // ... what a segment keeps of the state before it
 };
 
-// exp(e g) with the product's rounding carried along.
+// exp(e g) with the product's rounding carried along.  A NaN stays one where
+// nothing decays: it reaches all that a head's steps do.
 __device__ __forceinline__ float power_of(float g, float e) {
-  if (e == 0.f) return 1.f;
+  if (e == 0.f) return isnan(g) ? g : 1.f;
   const float y = g * e;
   if (y < -104.f) return 0.f;
   return expf(y) * (1.f + fmaf(g, e, -y));
@@ -75,6 +76,7 @@ struct Fade {
   float keep, change;
 };
 __device__ __forceinline__ Fade fade_of(float g, float e) {
+  if (e == 0.f) return {1.f, 0.f};  // no steps: the state as it is, whatever g
   const float y = g * e;
   if (!(y > -0.5f)) return {power_of(g, e), 0.f};
   return {1.f, expm1f(y) + fmaf(g, e, -y)};
