@@ -660,7 +660,7 @@ int soma_linear_ce_backward(const void* h, const void* emb, soma_linear_ce_dims 
  * 16-bit types run on the tensor cores where rows allow tiled copies: addresses
  * and strides that are multiples of 16 bytes, widths that are multiples of 8, and
  * strides that nest (each a multiple of the next smaller one, or widths that are
- * multiples of 16).  There scale l^{i-j} <q_i, k_j> and the state that a chunk of
+ * multiples of 16); the stride of a dimension of one element may be any.  There scale l^{i-j} <q_i, k_j> and the state that a chunk of
  * 128 steps starts from are rounded to the type for the products that they enter,
  * and the decayed v, for the state, to twice its bits; sums and states are fp32.
  * fp16: those three are scaled by powers of two to the range of the type.  Other

@@ -589,9 +589,12 @@ cudaError_t step(const Call& call, cudaStream_t st) {
   return launch_overlapped(step_kernel<T, 1>, grid, kStepThreads, 0, st, call, kStepThreads / p.c);
 }
 
-// Whether the tensor-core kernels can read and write a tensor.
-bool tiled(const void* p, const soma_attn_strides& s) {
-  return aligned(p, 16) && s.b % 8 == 0 && s.t % 8 == 0 && s.h % 8 == 0;
+// Whether the tensor-core kernels can read and write a tensor of `call`.  The
+// stride of a dimension of one element leads nowhere and may be any.
+bool tiled(const Call& call, const void* p, const soma_attn_strides& s) {
+  const auto pieces = [](int64_t size, int64_t stride) { return size < 2 || stride % 8 == 0; };
+  return aligned(p, 16) && pieces(call.batch, s.b) && pieces(call.steps, s.t) &&
+         pieces(call.heads, s.h);
 }
 
 // The cut with the least estimated time, in units of one CTA's work: a chunk on
@@ -654,8 +657,8 @@ cudaError_t run(const Call& call, const Cut& cut, int dtype, cudaStream_t st) {
   bool chunked = dtype != SOMA_FP32 && call.steps > 0;
   for (int k = 0; k < call.problems; ++k) {
     const Problem& p = call.p[k];
-    chunked = chunked && p.a % 8 == 0 && p.c % 8 == 0 && tiled(p.x, p.xs) && tiled(p.y, p.ys) &&
-              tiled(p.z, p.zs) && tiled(p.out, p.os);
+    chunked = chunked && p.a % 8 == 0 && p.c % 8 == 0 && tiled(call, p.x, p.xs) &&
+              tiled(call, p.y, p.ys) && tiled(call, p.z, p.zs) && tiled(call, p.out, p.os);
   }
   cudaError_t e;
   if (chunked && launch_chunks(call, cut, dtype, st, &e)) return e;
