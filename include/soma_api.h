@@ -684,8 +684,10 @@ typedef struct soma_attn_strides {
 
 /* Bytes of workspace of the forward (backward = 0) or the backward call (1), 0
  * for many sizes; -1 if the sizes are invalid.  One workspace of the larger size
- * serves both. */
+ * serves both.  A smaller batch may need more: fewer sequences are cut into more
+ * segments.  ..._upto: the most that any batch from 0 to d.batch needs. */
 int64_t soma_linear_attn_workspace_bytes(soma_attn_dims d, int dtype, int backward);
+int64_t soma_linear_attn_workspace_bytes_upto(soma_attn_dims d, int dtype, int backward);
 
 /*   q, k          [batch][steps][heads][key_dim] by q_strides, k_strides
  *   v, o          [batch][steps][heads][value_dim] by v_strides, o_strides

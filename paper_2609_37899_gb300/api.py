@@ -217,6 +217,7 @@ def _open(path: str):
                                                  vp, sz, vp])
         ad, at = soma_attn_dims, soma_attn_strides
         _sig(L, "soma_linear_attn_workspace_bytes", i64, [ad, i32, i32])
+        _sig(L, "soma_linear_attn_workspace_bytes_upto", i64, [ad, i32, i32])
         _sig(L, "soma_linear_attn_forward", i32, [vp, at, vp, at, vp, at, i32, ad, vp, f32, vp, vp,
                                                   vp, vp, at, vp, vp, sz, vp])
         _sig(L, "soma_linear_attn_backward", i32, [vp, at, vp, at, vp, at, i32, ad, vp, f32, vp, vp,
@@ -974,9 +975,10 @@ def _attn_dtype(q) -> int:
 
 def linear_attn_workspace_bytes(batch: int, steps: int, heads: int, key_dim: int, value_dim: int,
                                 dtype: torch.dtype, backward: bool = True) -> int:
-    """Bytes that linear_attn_forward needs, and linear_attn_backward with `backward`."""
+    """Bytes that serve linear_attn_forward, and linear_attn_backward with `backward`, of these
+    sizes and of every smaller batch."""
     d = soma_attn_dims(batch, steps, heads, key_dim, value_dim)
-    return max(int(lib().soma_linear_attn_workspace_bytes(d, DTYPES.get(dtype, -1), k))
+    return max(int(lib().soma_linear_attn_workspace_bytes_upto(d, DTYPES.get(dtype, -1), k))
                for k in range(1 + bool(backward)))
 
 

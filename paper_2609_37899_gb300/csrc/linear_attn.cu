@@ -597,23 +597,27 @@ bool tiled(const Call& call, const void* p, const soma_attn_strides& s) {
          pieces(call.heads, s.h);
 }
 
+bool chunked_widths(const soma_attn_dims& d, int dtype) {
+  return dtype != SOMA_FP32 && d.key_dim % 8 == 0 && d.value_dim % 8 == 0;
+}
+
+// CTAs that the GPU holds at once.
+int64_t resident_of(const soma_attn_dims& d, int dtype, int problems) {
+  if (chunked_widths(d, dtype)) return d.key_dim <= 64 && d.value_dim <= 64 ? 304 : 152;
+  const int wide = d.key_dim > d.value_dim ? d.key_dim : d.value_dim;
+  const Spread s = spread_of(problems > 1 ? wide : d.key_dim, problems > 1 ? wide : d.value_dim);
+  const int by_threads = most_threads(s.runs) / threads_of(s, dtype);
+  const int by_shared = (int)(kSharedOfSm / (shared_of(s) + 2048));
+  return 152 * (by_threads < by_shared ? by_threads : by_shared);
+}
+
 // The cut with the least estimated time, in units of one CTA's work: a chunk on
 // the tensor cores, a tile of steps elsewhere.  The states of all segments but
 // the last come first (half the work), then the outputs; a CTA's begin and end
 // take about two units, the join between the launches as much.
 Cut cut_of(const soma_attn_dims& d, int dtype, int problems) {
-  const bool chunked = dtype != SOMA_FP32 && d.key_dim % 8 == 0 && d.value_dim % 8 == 0;
-  const int unit = chunked ? kChunk : kTile, ends = 2;
-  int64_t resident = 152;
-  if (chunked) {
-    if (d.key_dim <= 64 && d.value_dim <= 64) resident = 304;
-  } else {
-    const int wide = d.key_dim > d.value_dim ? d.key_dim : d.value_dim;
-    const Spread s = spread_of(problems > 1 ? wide : d.key_dim, problems > 1 ? wide : d.value_dim);
-    const int by_threads = most_threads(s.runs) / threads_of(s, dtype);
-    const int by_shared = (int)(kSharedOfSm / (shared_of(s) + 2048));
-    resident *= by_threads < by_shared ? by_threads : by_shared;
-  }
+  const int unit = chunked_widths(d, dtype) ? kChunk : kTile, ends = 2;
+  const int64_t resident = resident_of(d, dtype, problems);
   Cut best = {};
   best.segments = 1;
   const int64_t rows = d.batch * d.heads * problems, units = (d.steps + unit - 1) / unit;
@@ -726,6 +730,23 @@ int64_t soma_linear_attn_workspace_bytes(soma_attn_dims d, int dtype, int backwa
   if (!dims_ok(d) || !dtype_ok(dtype) || (backward != 0 && backward != 1)) return -1;
   const int problems = backward ? 3 : 1;
   return (int64_t)parts_of(d, cut_of(d, dtype, problems), problems).bytes;
+}
+
+int64_t soma_linear_attn_workspace_bytes_upto(soma_attn_dims d, int dtype, int backward) {
+  if (soma_linear_attn_workspace_bytes(d, dtype, backward) < 0) return -1;
+  // A call of three rounds of CTAs or more is not cut.  With x rounds and n segments
+  // the launches cost at least (1.5 - 0.5 / n) x of one segment's time, which from
+  // n = 3 on is more than ceil(x); two segments cost ceil(2 x) / 2 + ceil(x) / 4,
+  // which is at least ceil(x) from two rounds on.
+  const int problems = backward ? 3 : 1;
+  const int64_t rows = 3 * resident_of(d, dtype, problems), batch = d.batch;
+  int64_t most = 0;
+  for (d.batch = 1; d.batch <= batch && (d.batch - 1) * d.heads * problems <= rows; ++d.batch) {
+    const int64_t bytes = (int64_t)parts_of(d, cut_of(d, dtype, problems), problems).bytes;
+    if (bytes > most) most = bytes;
+    if (d.heads == 0) break;
+  }
+  return most;
 }
 
 int soma_linear_attn_forward(const void* q, soma_attn_strides q_strides, const void* k,
