@@ -62,9 +62,10 @@ class ScanExpert:
         def new(*shape, like=dtype):
             return torch.empty(*shape, dtype=like, device=device)
 
-        self.h, self.y = new(batch, steps, dim), new(n, dim)
+        self.h = new(batch, steps, dim)
         self.loss, self.lse = new(n, like=torch.float32), new(n, like=torch.float32)
-        self.da, self.dy, self.dh = new(n, self.projections * dim), new(n, dim), new(n, dim)
+        self.da, self.dy = new(n, self.projections * dim), new(n, dim)
+        self.dh = None  # the gradient before dropout, from the first step that drops on
         self.demb, self.dw = new(vocab, dim), new(self.projections * dim, dim)
         self.ce_ws = api.linear_ce_alloc_workspace(n, vocab, dim, dtype, device=device)
         self._mixer_buffers(new, device)
@@ -72,6 +73,7 @@ class ScanExpert:
     def _mixer_buffers(self, new, device):
         B, T, d = self.batch, self.steps, self.dim
         self.c_last = new(B, d, like=torch.float32)
+        self.dgates = self.da.view(B, T, 4, d)
         self.marks = api.scan_alloc_checkpoints(B, T, d, device)
         self.scan_ws = torch.empty(max(1, api.scan_workspace_bytes(B, T, d)), dtype=torch.uint8,
                                    device=device)
@@ -84,9 +86,9 @@ class ScanExpert:
 
     def _mix_backward(self, dh):
         """The gradient of the projections into da."""
-        B, T, d = self.batch, self.steps, self.dim
-        api.scan_backward(self.gates, self.marks, dh.view(B, T, d), self.da.view(B, T, 4, d),
-                          lengths=self.lengths, resets=self.resets, workspace=self.scan_ws)
+        api.scan_backward(self.gates, self.marks, dh.view(self.batch, self.steps, self.dim),
+                          self.dgates, lengths=self.lengths, resets=self.resets,
+                          workspace=self.scan_ws)
 
     def forward(self, tokens: torch.Tensor, resets: torch.Tensor | None = None,
                 lengths: torch.Tensor | None = None) -> torch.Tensor:
@@ -99,13 +101,14 @@ class ScanExpert:
         if lengths is not None:
             past = torch.arange(T, device=tokens.device)[None] >= lengths[:, None]
             self.targets = torch.where(past.reshape(-1), -100, self.targets)
-        self.x = self.emb[self.inputs].reshape(-1, d)
-        self._mix(self.x @ self.w.T, lengths, resets)
+        self.x = self.emb[self.inputs].contiguous()
+        self._mix(self.x.reshape(-1, d) @ self.w.T, lengths, resets)
         if self.dropout:
-            api.dropout(self.h.view(-1, d), self.y, self.dropout, self.seed, offset=self.t,
-                        residual=self.x)
+            y = torch.empty_like(self.h)
+            api.dropout(self.h, y, self.dropout, self.seed, offset=self.t, residual=self.x)
         else:
-            torch.add(self.x, self.h.view(-1, d), out=self.y)
+            y = self.x + self.h
+        self.y = y.view(-1, d)
         api.linear_ce_forward(self.y, self.emb, self.targets, self.loss, self.lse, self.ce_ws)
         return self.loss
 
@@ -115,10 +118,12 @@ class ScanExpert:
                                self.ce_ws)
         dh = self.dy
         if self.dropout:
+            if self.dh is None:
+                self.dh = torch.empty_like(self.dy)
             dh = self.dh
             api.dropout(self.dy, dh, self.dropout, self.seed, offset=self.t)
         self._mix_backward(dh)
-        torch.mm(self.da.T, self.x, out=self.dw)
+        torch.mm(self.da.T, self.x.reshape(-1, self.dim), out=self.dw)
         dx = torch.addmm(self.dy, self.da, self.w)
         # the embedding's rows add up in fp32: a frequent token has many
         into = self.demb.float().index_add_(0, self.inputs.reshape(-1), dx.float())
