@@ -1130,6 +1130,8 @@ def sample(logits: torch.Tensor, u: torch.Tensor, tokens: torch.Tensor, temperat
         if torch.is_tensor(x):
             own[name] = x
             setattr(cfg, name + "s", _dev(x, dtype, name, R).value)
+        elif name == "top_k":  # a structure would keep its last 32 bits alone
+            cfg.top_k = max(-1, min(x, 2 ** 31 - 1))
         else:
             setattr(cfg, name, x)
     _here(logits=logits, u=u, tokens=tokens, logprob=logprob, **own)
