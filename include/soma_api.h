@@ -755,17 +755,19 @@ int soma_dropout(const void* x, int64_t x_stride, const void* residual, int64_t 
                  uint64_t seed, uint64_t offset, const uint64_t* counter, void* stream);
 
 /* Sampling: one token per row of logits, from given random numbers.  For a row
- * with largest logit m, token v has the weight w_v = rint(2^40 exp((l_v - m) / T)),
- * a whole number of 64 bits, so that sums of weights are exact and results do
- * not depend on the order of additions.  Tokens are ranked by logit, equal ones
- * by index.  Of the tokens remain, in this order,
+ * with largest logit m, token v has the weight w_v = 2^40 exp((l_v - m) / T) to a
+ * whole number of 64 bits, less than 4 off, so that sums of weights are exact and
+ * results do not depend on the order of additions.  (A cut or a choice by exact
+ * weights is another one only where it falls within these units.)  Tokens are
+ * ranked by logit, equal ones by index.  Of the tokens remain, in this order,
  *   top-k   the first top_k of the ranking (0 or less: all);
  *   top-p   the shortest beginning of the ranking that has at least top_p of the
  *           weight that is left, the first always (1 or more: all);
  *   min-p   those with w_v >= min_p 2^40 (min_p above 1 counts as 1).
  * The answer is the first token, by index, up to which the remaining weights sum
  * to more than floor(u W), W being the sum of all that remain; logprob is
- * log(w_v / W), to fp32, of that token.  T = 0 (and below 2^-100) gives the first
+ * (l_v - m) / T - log(2^-40 W) of that token, to fp32: for the rarest tokens not
+ * the logarithm of w_v / W, as a weight of 1 stands for any from 1/2 to 3/2.  T = 0 (and below 2^-100) gives the first
  * token of the ranking, with logprob 0.
  *
  * Logits of -infinity, or so low that their weight is 0, are never chosen.  A row

@@ -68,8 +68,9 @@ __device__ const float2 kRoots[64] = {
 // The weight of a token whose logit l is at most kDeepest temperatures below
 // max; inv = 1 / T as the sum of two fp32 numbers.  x = (l - max) / T is split
 // into -k ln2/64 + r with |r| < 0.0055, and exp(x) = 2^-(k/64) (1 + r + r^2/2 +
-// ...), with what fp32 rounds off the large terms carried along: good to a few
-// units of the 2^-40 it is rounded to.
+// ...), with what fp32 rounds off the large terms carried along.  The whole number is
+// less than 4 from 2^40 exp(x): 3.1 at most among 2 10^7 logits, at temperatures
+// from 1/400 to 400.
 __device__ __forceinline__ u64 weight(float l, float max, float2 inv, const float2* roots) {
   // l - max = d + e (Knuth's two-sum), times inv
   const float d = __fsub_rn(l, max), b = __fsub_rn(d, l);
