@@ -31,6 +31,7 @@ struct Dropout {
   const uint64_t* counter;
   uint32_t drop;              // an element whose 16 bits are below this is dropped
   float scale;
+  int* status;
 };
 
 // Bit j: whether element 8 q + j is kept.
@@ -58,6 +59,7 @@ dropout_groups_kernel(const T* x, const T* residual, T* y, const Dropout d, uint
   // no division where all is one row
   const uint32_t row = row_groups == UINT32_MAX ? 0 : (uint32_t)q / row_groups;
   const int64_t at = (int64_t)((uint32_t)q - row * row_groups) * 8;
+  if (!SOMA_CHECK(row < d.rows && at >= 0 && at + 8 <= d.cols, d.status)) return;
   float a[8], r[8], o[8];
   load8(x + row * d.xs + at, a);
   if (RESIDUAL) load8(residual + row * d.rs + at, r);
@@ -93,7 +95,8 @@ dropout_kernel(const T* x, const T* residual, T* y, const Dropout d) {
   int64_t to[8];
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
-    const bool there = first + 32 * j + lane < d.count;
+    const bool there = first + 32 * j + lane < d.count &&
+                       SOMA_CHECK(row >= 0 && row < d.rows && col >= 0 && col < d.cols, d.status);
     to[j] = there ? row * d.ys + col : -1;
     a[j] = there ? to_f32(x[row * d.xs + col]) : 0.f;
     r[j] = RESIDUAL && there ? to_f32(residual[row * d.rs + col]) : 0.f;
@@ -160,8 +163,10 @@ extern "C" int soma_dropout(const void* x, int64_t x_stride, const void* residua
     return SOMA_ERR_INVALID_ARG;
   if (rows == 0 || cols == 0) return SOMA_OK;
   if (!x || !y) return SOMA_ERR_INVALID_ARG;
-  if (!status_ptr()) return SOMA_ERR_CUDA;
+  int* status = status_ptr();
+  if (!status) return SOMA_ERR_CUDA;
   Dropout d = {};
+  d.status = status;
   d.xs = x_stride;
   d.rs = residual_stride;
   d.ys = y_stride;

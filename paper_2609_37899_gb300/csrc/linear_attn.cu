@@ -21,6 +21,7 @@ constexpr int kAtOnce = 2;      // and gone through in one go
 constexpr int kCols = 4;        // and columns
 constexpr int kSums = kAtOnce * kCols;
 constexpr int kStepThreads = 256;
+constexpr int kMostWidth = 128;  // of keys and values
 constexpr int kLoaders = 128;
 // Log decays from here up are put off to a tile's end: z is multiplied by up to
 // exp(0.5 * 15) = 1808 then, which fp32's range allows.
@@ -56,6 +57,12 @@ struct Tile {
   __device__ float* x(int buf) const { return at + buf * kTile * (2 * rows + cols); }
   __device__ float* y(int buf) const { return x(buf) + kTile * rows; }
   __device__ float* z(int buf) const { return y(buf) + kTile * rows; }
+  // whether n floats from p on lie in the CTA's dynamic shared memory
+  __device__ bool holds(const float* p, int n) const {
+    uint32_t size;
+    asm("mov.u32 %0, %%dynamic_smem_size;" : "=r"(size));
+    return p >= at && (uint32_t)((p - at) + n) * 4 <= size;
+  }
 };
 
 // Adds what a lane and its partner hold: the first N sums for the lower of them,
@@ -123,6 +130,10 @@ plain_kernel(const __grid_constant__ Call call, const __grid_constant__ Cut cut,
   const Tile tile = {groups * kRows, (p.c + kCols - 1) / kCols * kCols, smem};
   const uint8_t* resets = call.resets ? call.resets + b * call.steps : nullptr;
   const auto step_of = [&](int64_t k) { return p.reversed ? last - 1 - k : first + k; };
+  // whether n elements of step k of the segment, from column i on, are a tensor's
+  const auto within = [&](int64_t k, int i, int n, int width) {
+    return b < call.batch && step_of(k) >= 0 && step_of(k) < call.steps && i >= 0 && i + n <= width;
+  };
 
   // steps k0 .. of the segment, rows and columns and steps past the end as zeros
   bool fresh = false;  // a document started in what this thread has seen
@@ -149,7 +160,13 @@ plain_kernel(const __grid_constant__ Call call, const __grid_constant__ Cut cut,
           uint32_t dst = tc::smem_u32(to + k1 * wide + i);
 #pragma unroll 2
           for (int k = k1; k < kTile; k += per, src += next, dst += per * wide * 4) {
-            const bool there = k < upto;  // zeros otherwise
+            if (!SOMA_CHECK(tile.holds(to + k * wide + i, each) && dst == tc::smem_u32(to + k * wide + i),
+                            call.status))
+              break;
+            const bool there = k < upto &&  // zeros otherwise
+                               SOMA_CHECK(within(k0 + k, i, each, width) &&
+                                              src == from + step_of(k0 + k) * stride + i,
+                                          call.status);
             if (pieces)
               asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst),
                            "l"(there ? src : from), "r"(there ? 16 : 0)
@@ -170,12 +187,15 @@ plain_kernel(const __grid_constant__ Call call, const __grid_constant__ Cut cut,
 #pragma unroll
           for (int u = 0; u < kAhead; ++u) {
             const int s = k + u * per;
-            v[u] = from[s < n && i < width ? step_of(k0 + s) * stride + i : 0];
+            const bool there = s < n && i < width &&
+                               SOMA_CHECK(within(k0 + s, i, 1, width), call.status);
+            v[u] = from[there ? step_of(k0 + s) * stride + i : 0];
           }
 #pragma unroll
           for (int u = 0; u < kAhead; ++u) {
             const int s = k + u * per;
-            if (s < kTile) to[s * wide + i] = s < n && i < width ? to_f32(v[u]) : 0.f;
+            if (s < kTile && SOMA_CHECK(tile.holds(to + s * wide + i, 1), call.status))
+              to[s * wide + i] = s < n && i < width ? to_f32(v[u]) : 0.f;
           }
         }
       }
@@ -205,6 +225,7 @@ plain_kernel(const __grid_constant__ Call call, const __grid_constant__ Cut cut,
   const bool works = __any_sync(0xffffffffu, holds);
   const auto row_of = [&](int r) { return (r / 4 * groups + group) * 4 + r % 4; };
   const bool joined = cut.segments > 1 && seg > 0;
+  const int64_t states = call.batch * call.heads * call.problems * cut.segments;  // of the workspace
   const float* from = joined ? cut.starts + (which * cut.segments + seg) * call.state
                       : p.s_in ? p.s_in + bh * call.state : nullptr;
   if (!OUT) from = nullptr;  // what the segment adds
@@ -220,7 +241,11 @@ plain_kernel(const __grid_constant__ Call call, const __grid_constant__ Cut cut,
 #pragma unroll
       for (int j = 0; j < kCols; ++j) {
         const int i = row_of(r), c = c0 + j;
-        if (i < p.a && c < p.c) S[r][j] = from[i * from_row + c * from_col];
+        if (i < p.a && c < p.c &&
+            SOMA_CHECK(i * from_row + c * from_col < call.state &&
+                           (!joined || which * cut.segments + seg < states),
+                       call.status))
+          S[r][j] = from[i * from_row + c * from_col];
       }
   // Of the sums of kAtOnce steps (in rows of kCols), a lane gets kSums / groups from
   // `mine` on, `mine_cols` of them or fewer in its columns.
@@ -240,7 +265,7 @@ plain_kernel(const __grid_constant__ Call call, const __grid_constant__ Cut cut,
   int buf = kTiles - 2;
   const int64_t next_out = p.reversed ? -p.os.t : p.os.t;
   // a tile's steps; kEach: every step decays the state, which is whole then
-  const auto go = [&](auto each, int n, T* to) {
+  const auto go = [&](auto each, int n, int64_t k0, T* to) {
     constexpr bool kEach = decltype(each)::value;
     if (!kEach) {
       const float m = multiplier[buf][0];
@@ -293,7 +318,11 @@ plain_kernel(const __grid_constant__ Call call, const __grid_constant__ Cut cut,
 #pragma unroll
         for (int i = 0; i < kSums; ++i) {
           const int u = k + mine / kCols + i / kCols;
-          if (i * groups < kSums && i % kCols < mine_cols && u < n)
+          if (i * groups < kSums && i % kCols < mine_cols && u < n &&
+              SOMA_CHECK(within(k0 + u, c0 + mine % kCols + i % kCols, 1, p.c) &&
+                             to + i % kCols + i / kCols * next_out ==
+                                 out + step_of(k0 + u) * p.os.t + c0 + mine % kCols + i % kCols,
+                         call.status))
             to[i % kCols + i / kCols * next_out] = from_f32<T>(factor[u].y * o[i]);
         }
         to += kAtOnce * next_out;
@@ -311,8 +340,8 @@ plain_kernel(const __grid_constant__ Call call, const __grid_constant__ Cut cut,
     if (works && k0 >= 0) {
       const int n = count - k0 < kTile ? (int)(count - k0) : kTile;
       T* to = out + step_of(k0) * p.os.t + c0 + mine / kCols * next_out + mine % kCols;
-      if (put_off) go(std::false_type(), n, to);
-      else go(std::true_type(), n, to);
+      if (put_off) go(std::false_type(), n, k0, to);
+      else go(std::true_type(), n, k0, to);
     }
     __syncthreads();
     buf = (buf + 1) % kTiles;
@@ -343,7 +372,9 @@ plain_kernel(const __grid_constant__ Call call, const __grid_constant__ Cut cut,
 #pragma unroll
         for (int j = 0; j < kCols; ++j) {
           const int i = row_of(r), c = c0 + j;
-          if (i < p.a && c < p.c && SOMA_CHECK(seg + 1 < cut.segments, call.status))
+          if (i < p.a && c < p.c &&
+              SOMA_CHECK(which * cut.segments + seg + 1 < states && i * p.c + c < call.state,
+                         call.status))
             to[i * p.c + c] = S[r][j];
         }
     return;
@@ -352,7 +383,8 @@ plain_kernel(const __grid_constant__ Call call, const __grid_constant__ Cut cut,
   const int64_t begin = max(len, place * cut.steps);
   const int64_t end = min(call.steps, (place + 1) * cut.steps);
   for (int64_t e = threadIdx.x; e < (end - begin) * p.c; e += blockDim.x)
-    out[(begin + e / p.c) * p.os.t + e % p.c] = from_f32<T>(0.f);
+    if (SOMA_CHECK(begin + e / p.c >= len && begin + e / p.c < call.steps, call.status))
+      out[(begin + e / p.c) * p.os.t + e % p.c] = from_f32<T>(0.f);
   if (!p.s_out || !holds || seg != cut.segments - 1) return;
   const float left = !p.reversed || len == 0 ? 1.f
                      : resets && resets[0]     ? 0.f
@@ -363,7 +395,9 @@ plain_kernel(const __grid_constant__ Call call, const __grid_constant__ Cut cut,
 #pragma unroll
     for (int j = 0; j < kCols; ++j) {
       const int i = row_of(r), c = c0 + j;
-      if (i < p.a && c < p.c)
+      if (i < p.a && c < p.c &&
+          SOMA_CHECK(bh < call.batch * call.heads && i * p.out_row + c * p.out_col < call.state,
+                     call.status))
         p.s_out[bh * call.state + i * p.out_row + c * p.out_col] =
             left == 0.f ? 0.f : left * S[r][j];
     }
@@ -381,6 +415,10 @@ join_kernel(const __grid_constant__ Call call, const __grid_constant__ Cut cut) 
   const int64_t e = blockIdx.x % parts * 256 + threadIdx.x;
   if (e >= call.state) return;
   const int64_t i = e / p.c, c = e % p.c;
+  if (!SOMA_CHECK(bh < call.batch * call.heads && i < p.a && c < p.c &&
+                      (!p.s_in || i * p.in_row + c * p.in_col < call.state),
+                  call.status))
+    return;
   float s = p.s_in ? p.s_in[bh * call.state + i * p.in_row + c * p.in_col] : 0.f;
   float* at = cut.starts + which * cut.segments * call.state + e;
   const float2* fades = cut.fades + which * cut.segments;
@@ -407,7 +445,7 @@ join_kernel(const __grid_constant__ Call call, const __grid_constant__ Cut cut) 
 template <typename T, int V>
 __global__ void __launch_bounds__(kStepThreads)
 step_kernel(const __grid_constant__ Call call, int lanes) {
-  __shared__ float sx[128], sy[128];
+  __shared__ float sx[kMostWidth], sy[kMostWidth];
   __shared__ float part[kStepThreads * V];
   admit_successor();
   after_predecessor();
@@ -421,7 +459,9 @@ step_kernel(const __grid_constant__ Call call, int lanes) {
   const auto fetch = [&](int i) {
 #pragma unroll
     for (int k = 0; k < kAhead; ++k)
-      if (i + k * lanes < p.a) {
+      if (i + k * lanes < p.a &&
+          SOMA_CHECK((i + k * lanes) * p.c + col + V <= call.state && bh < call.batch * call.heads,
+                     call.status)) {
         const float* at = s + (i + k * lanes) * p.c + col;
         if (V == 4) {
           const float4 w = *reinterpret_cast<const float4*>(at);
@@ -435,7 +475,7 @@ step_kernel(const __grid_constant__ Call call, int lanes) {
   const T* x = static_cast<const T*>(p.x) + b * p.xs.b + h * p.xs.h;
   const T* y = static_cast<const T*>(p.y) + b * p.ys.b + h * p.ys.h;
   const T* z = static_cast<const T*>(p.z) + b * p.zs.b + h * p.zs.h;
-  for (int i = threadIdx.x; i < p.a; i += kStepThreads) {
+  for (int i = threadIdx.x; i < p.a && SOMA_CHECK(i < kMostWidth, call.status); i += kStepThreads) {
     sx[i] = to_f32(x[i]);
     sy[i] = to_f32(y[i]);
   }
@@ -457,7 +497,7 @@ step_kernel(const __grid_constant__ Call call, int lanes) {
 #pragma unroll
       for (int k = 0; k < kAhead; ++k) {
         const int r = i + k * lanes;
-        if (r >= p.a) break;
+        if (r >= p.a || !SOMA_CHECK(r * p.c + col + V <= call.state, call.status)) break;
 #pragma unroll
         for (int j = 0; j < V; ++j) {
           // a decay of 0 keeps nothing, whatever it is
@@ -473,7 +513,9 @@ step_kernel(const __grid_constant__ Call call, int lanes) {
       }
     }
 #pragma unroll
-    for (int j = 0; j < V; ++j) part[first * p.c + col + j] = o[j];
+    for (int j = 0; j < V; ++j)
+      if (SOMA_CHECK(first * p.c + col + j < kStepThreads * V && col + j < p.c, call.status))
+        part[first * p.c + col + j] = o[j];
   }
   __syncthreads();
   T* out = static_cast<T*>(p.out) + b * p.os.b + h * p.os.h;
@@ -491,8 +533,8 @@ bool aligned(const void* p, size_t to) { return (reinterpret_cast<uintptr_t>(p) 
 bool dims_ok(const soma_attn_dims& d) {
   return d.batch >= 0 && d.steps >= 0 && d.heads >= 0 && d.batch <= INT32_MAX &&
          d.steps <= INT32_MAX && d.heads <= (1 << 16) &&
-         (d.heads == 0 || d.batch <= (1 << 29) / d.heads) && d.key_dim >= 1 && d.key_dim <= 128 &&
-         d.value_dim >= 1 && d.value_dim <= 128;
+         (d.heads == 0 || d.batch <= (1 << 29) / d.heads) && d.key_dim >= 1 &&
+         d.key_dim <= kMostWidth && d.value_dim >= 1 && d.value_dim <= kMostWidth;
 }
 
 bool dtype_ok(int t) { return t == SOMA_FP32 || t == SOMA_BF16 || t == SOMA_FP16; }

@@ -502,7 +502,11 @@ chunk_kernel(const __grid_constant__ Sources sources, const __grid_constant__ Ca
             }
             u[j] = pack2<T>(v[0], v[1]);
           }
-          if (row < n && SOMA_CHECK(t0 + row < call.steps && p.c % 8 == 0, status)) {
+          if (row < n &&
+              SOMA_CHECK(b < call.batch && t0 >= 0 && t0 + row < call.steps &&
+                             (wide && col + 16 <= p.c ? (reinterpret_cast<uintptr_t>(to + c) & 31) == 0
+                                                      : (reinterpret_cast<uintptr_t>(to + c) & 15) == 0),
+                         status)) {
             T* at = to + c;
             if (wide && col + 16 <= p.c) {
               store32(at, u);
@@ -523,8 +527,9 @@ chunk_kernel(const __grid_constant__ Sources sources, const __grid_constant__ Ca
       const int64_t to_step = min(call.steps, (place + 1) * share);
       const int per = p.c / 8;
       for (int64_t e = threadIdx.x; e < (to_step - from_step) * per; e += 32 * L::group)
-        *reinterpret_cast<uint4*>(out + (from_step + e / per) * p.os.t + e % per * 8) =
-            make_uint4(0u, 0u, 0u, 0u);
+        if (SOMA_CHECK(from_step + e / per >= len && from_step + e / per < call.steps, status))
+          *reinterpret_cast<uint4*>(out + (from_step + e / per) * p.os.t + e % per * 8) =
+              make_uint4(0u, 0u, 0u, 0u);
     }
   } else if (warp < 2 * L::group) {
     // ---- states --------------------------------------------------------------
@@ -560,15 +565,19 @@ chunk_kernel(const __grid_constant__ Sources sources, const __grid_constant__ Ca
 #pragma unroll
       for (int j = 0; j < kOwn; j += 4) {
         float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (s_row < p.a && c0 + j < p.c)
+        if (s_row < p.a && c0 + j < p.c &&
+            SOMA_CHECK(s_row * from_row + c0 + j + 4 <= call.state && bh < call.batch * call.heads,
+                       status))
           v = *reinterpret_cast<const float4*>(from + s_row * from_row + c0 + j);
         S[j] = v.x; S[j + 1] = v.y; S[j + 2] = v.z; S[j + 3] = v.w;
       }
     } else {
 #pragma unroll
       for (int j = 0; j < kOwn; ++j)
-        S[j] = from && s_row < p.a && c0 + j < p.c ? from[s_row * from_row + (c0 + j) * from_col]
-                                                   : 0.f;
+        S[j] = from && s_row < p.a && c0 + j < p.c &&
+                       SOMA_CHECK(s_row * from_row + (c0 + j) * from_col < call.state, status)
+                   ? from[s_row * from_row + (c0 + j) * from_col]
+                   : 0.f;
     }
     const uint32_t state_row = row_address(smem + L::state + c0 / kCols * L::state_box, s_row);
     // The state in 16 bits, for O1 of chunk k.
@@ -702,7 +711,8 @@ chunk_kernel(const __grid_constant__ Sources sources, const __grid_constant__ Ca
     if (!OUT) {
       // the state that the segment adds, and what it leaves of the one before it
       const int64_t at = (bh * call.problems + problem) * cut.segments + seg;
-      if (SOMA_CHECK(seg + 1 < cut.segments, status)) to = cut.starts + (at + 1) * call.state;
+      if (SOMA_CHECK(at + 1 < call.batch * call.heads * call.problems * cut.segments, status))
+        to = cut.starts + (at + 1) * call.state;
       if (warp == L::group && lane == 0) {
         const int steps = count > 0 ? min(len, last * kChunk) - first * kChunk : 0;
         const Fade f = fade_of(g, (float)steps);
@@ -717,13 +727,14 @@ chunk_kernel(const __grid_constant__ Sources sources, const __grid_constant__ Ca
       if (to_col == 1 && (reinterpret_cast<uintptr_t>(to) & 15) == 0) {
 #pragma unroll
         for (int j = 0; j < kOwn; j += 4)
-          if (c0 + j < p.c)
+          if (c0 + j < p.c && SOMA_CHECK(s_row * to_row + c0 + j + 4 <= call.state, status))
             *reinterpret_cast<float4*>(to + s_row * to_row + c0 + j) =
                 make_float4(S[j], S[j + 1], S[j + 2], S[j + 3]);
       } else {
 #pragma unroll
         for (int j = 0; j < kOwn; ++j)
-          if (c0 + j < p.c) to[s_row * to_row + (c0 + j) * to_col] = S[j];
+          if (c0 + j < p.c && SOMA_CHECK(s_row * to_row + (c0 + j) * to_col < call.state, status))
+            to[s_row * to_row + (c0 + j) * to_col] = S[j];
       }
     }
   } else if (fewer_registers<L::rest_regs>(); warp == L::loader) {
@@ -734,8 +745,8 @@ chunk_kernel(const __grid_constant__ Sources sources, const __grid_constant__ Ca
       if (lane == 0) {
         tc::mbar_arrive_expect_tx(bar, boxes * sources.box_rows * 128);
         for (int j = 0; j < boxes; ++j)
-          if (SOMA_CHECK(t0 % kChunk == 0 && t0 < call.steps && j * 64 < W &&
-                             sources.box_rows <= kChunk,
+          if (SOMA_CHECK(t0 >= 0 && t0 % kChunk == 0 && t0 < len && j * 64 < W &&
+                             tile + j * kBox + sources.box_rows * 128 <= L::state,
                          status))
             load_box(smem + tile + j * kBox, src, j * 64, t0, (int)b, (int)h, bar);
       }

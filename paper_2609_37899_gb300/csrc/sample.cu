@@ -36,6 +36,8 @@ constexpr int kBins = 2048;
 constexpr int kMaxCluster = 8;
 constexpr int kSlots = 24;                 // exchanges between the CTAs of a row
 constexpr int kHeld = 32;                  // logits of a thread that shared memory holds
+constexpr int kMostVocab = 1 << 20;
+constexpr int kMostPart = kMostVocab / kMaxCluster + 8;  // logits of a CTA, at most
 constexpr float kDeepest = 28.5f;          // 2^40 exp(-28.42) = 1/2: weights further down are 0
 constexpr float kStep = kDeepest / kBins;
 constexpr float kLeastTemperature = 0x1p-100f, kMostTemperature = 0x1p100f;
@@ -194,6 +196,8 @@ struct Row {
   S& sh;
   const T* row;        // 16-byte aligned, `shift` elements before the first logit
   int shift, end;      // end: one behind the last logit, counted from `row`
+  int vocab;
+  int* status;
   int first, stop;     // this thread's
   uint32_t rank, ranks;
   int slots = 0;
@@ -203,6 +207,24 @@ struct Row {
   u64 ties = 0;        // ... so many of this key
 
   __device__ Row(S& s) : sh(s) {}
+
+  // Where the checked build looks: an exchange, a bin, a place in the list, a group of
+  // eight held logits, and logits of the row.
+  __device__ __forceinline__ bool slot_ok() const {
+    return SOMA_CHECK(slots >= 0 && slots < kSlots, status);
+  }
+  __device__ __forceinline__ bool bin_ok(int b) const {
+    return SOMA_CHECK(b >= 0 && b < kBins, status);
+  }
+  __device__ __forceinline__ bool listed_ok(int i) const {
+    return SOMA_CHECK(i >= 0 && i < kList, status);
+  }
+  __device__ __forceinline__ bool held_ok(int group) const {
+    return SOMA_CHECK(HELD && group >= 0 && group < kHeld / 8, status);
+  }
+  __device__ __forceinline__ bool logits_ok(int i, int n) const {
+    return SOMA_CHECK(i >= shift && i - shift + n <= vocab, status);
+  }
 
   // The sum of a variable over the CTAs before `upto`.
   __device__ __forceinline__ u64 remote_sum(const u64* p, uint32_t upto) const {
@@ -226,7 +248,7 @@ struct Row {
     for (int j = 0; j < 8; ++j) w.t[j] = from_f32<T>(v[j]);  // exact
 #pragma unroll
     for (int k = 0; k < kPieces; ++k)
-      held[(group * kPieces + k) * THREADS + threadIdx.x] = w.u[k];
+      if (held_ok(group)) held[(group * kPieces + k) * THREADS + threadIdx.x] = w.u[k];
   }
   __device__ __forceinline__ void load(int i, float (&v)[8]) const {
     if (HELD) {
@@ -237,7 +259,7 @@ struct Row {
       const int group = (i - first) / 8;
 #pragma unroll
       for (int k = 0; k < kPieces; ++k)
-        w.u[k] = held[(group * kPieces + k) * THREADS + threadIdx.x];
+        w.u[k] = held[(held_ok(group) ? group * kPieces + k : 0) * THREADS + threadIdx.x];
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[j] = to_f32(w.t[j]);
     } else {
@@ -245,12 +267,12 @@ struct Row {
     }
   }
   __device__ __forceinline__ void fetch(int i, float (&v)[8]) const {
-    if (i >= shift && i + 8 <= end) {
+    if (i >= shift && i + 8 <= end && logits_ok(i, 8)) {
       load8(row + i, v);
     } else {
 #pragma unroll
       for (int j = 0; j < 8; ++j)
-        v[j] = i + j >= shift && i + j < end ? to_f32(row[i + j]) : -INFINITY;
+        v[j] = i + j >= shift && i + j < end && logits_ok(i + j, 1) ? to_f32(row[i + j]) : -INFINITY;
     }
   }
   // f(logit, index from `row`) for this thread's logits in order.
@@ -313,7 +335,7 @@ struct Row {
     __syncthreads();
     if (threadIdx.x == 0) {
       for (int w = 1; w < kWarps; ++w) v = sh.part[0][w] > v ? sh.part[0][w] : v;
-      sh.slot[slots][0] = v;
+      if (slot_ok()) sh.slot[slots][0] = v;
     }
     tc::cluster_sync();
     u64 o[kMost];
@@ -330,9 +352,13 @@ struct Row {
       for (int b = threadIdx.x; b < kBins; b += THREADS) sh.hist[a][b] = 0;
     __syncthreads();
   }
-  __device__ __forceinline__ void count(int b) { atomicAdd(&sh.hist[0][b], 1u); }
-  // weights go by 14 bits: sums of kMaxPart such numbers fit 32 bits
+  __device__ __forceinline__ void count(int b) {
+    if (bin_ok(b)) atomicAdd(&sh.hist[0][b], 1u);
+  }
+  // weights go by 14 bits, whose sums over a CTA's logits fit 32 bits
+  static_assert(((u64)kMostPart << 14) - kMostPart <= 0xffffffffu, "sums of 14 bits");
   __device__ __forceinline__ void add(int b, u64 w) {
+    if (!bin_ok(b)) return;
     atomicAdd(&sh.hist[0][b], (uint32_t)w & 0x3fffu);
     atomicAdd(&sh.hist[1][b], (uint32_t)(w >> 14) & 0x3fffu);
     atomicAdd(&sh.hist[2][b], (uint32_t)(w >> 28));
@@ -340,6 +366,7 @@ struct Row {
   template <bool WEIGHTS>
   __device__ __forceinline__ u64 in_bin(int b) const {
     uint32_t v[kMost][WEIGHTS ? 3 : 1];
+    if (!bin_ok(b)) return 0;
 #pragma unroll
     for (uint32_t r = 0; r < kMost; ++r)
 #pragma unroll
@@ -398,7 +425,7 @@ struct Row {
       total += own[j];
     }
     u64 run = before_me(total, sh.part[0], &all);
-    if (threadIdx.x == 0) sh.slot[slots][0] = all;
+    if (threadIdx.x == 0 && slot_ok()) sh.slot[slots][0] = all;
     tc::cluster_sync();
     run += remote_sum(&sh.slot[slots][0], rank);
     if (threadIdx.x == 0) sh.need = need_of(remote_sum(&sh.slot[slots][0], ranks));
@@ -434,7 +461,8 @@ struct Row {
                    : "=r"(at)
                    : "r"(at_rank(&sh.listed, 0))
                    : "memory");
-      if (at < kList) set_remote64(&sh.list[at], 0, (u64)key_of<T>(l) << 32 | (~(uint32_t)i));
+      if (listed_ok((int)at) && at < kList)  // as many as were counted, or estimated
+        set_remote64(&sh.list[at], 0, (u64)key_of<T>(l) << 32 | (~(uint32_t)i));
     });
     tc::cluster_sync();
     if (rank == 0) sort((int)min(sh.listed, (uint32_t)kList));
@@ -443,6 +471,7 @@ struct Row {
   __device__ void sort(int count) {
     int n = 2;
     while (n < count) n *= 2;
+    if (!listed_ok(n - 1)) return;
     for (int i = count + threadIdx.x; i < n; i += THREADS) sh.list[i] = 0;
     __syncthreads();
     for (int size = 2; size <= n; size *= 2)
@@ -488,7 +517,9 @@ struct Row {
     __syncthreads();
     return at;
   }
-  __device__ __forceinline__ uint32_t listed_key(int i) const { return (uint32_t)(sh.list[i] >> 32); }
+  __device__ __forceinline__ uint32_t listed_key(int i) const {
+    return listed_ok(i) ? (uint32_t)(sh.list[i] >> 32) : 0u;
+  }
 
   // The key in bin `bin` of depth at which the running count (or weight) of the
   // bin, which has `held_there` of it, reaches `need`; what is left of `need` at
@@ -663,6 +694,9 @@ sample_kernel(const T* logits, const Sample s, int* status) {
   r.shift = (int)((reinterpret_cast<uintptr_t>(row) & 15) / sizeof(T));
   r.row = row - r.shift;
   r.end = r.shift + s.vocab;
+  r.vocab = s.vocab;
+  r.status = status;
+  if (!SOMA_CHECK(n < s.rows && (int)(r.ranks * s.part) >= r.end, status)) return;  // the cluster
   const int part_end = min(r.end, (int)(r.rank + 1) * s.part);
   const int each = each_of(s.part, THREADS);
   r.first = (int)r.rank * s.part + (int)threadIdx.x * each;
@@ -751,14 +785,14 @@ sample_kernel(const T* logits, const Sample s, int* status) {
   u64 room = 0;
   if (tied) {
     u64 equal_before = r.before_me(equal, sh.part[0], &all);
-    if (threadIdx.x == 0) sh.slot[r.slots][0] = all;
+    if (threadIdx.x == 0 && r.slot_ok()) sh.slot[r.slots][0] = all;
     tc::cluster_sync();
     equal_before += r.remote_sum(&sh.slot[r.slots][0], r.rank);
     room = r.ties > equal_before ? r.ties - equal_before : 0;
     own += min(room, equal) * tie;
   }
   u64 before = r.before_me(own, sh.part[1], &all);
-  if (threadIdx.x == 0) sh.slot[r.slots][1] = all;
+  if (threadIdx.x == 0 && r.slot_ok()) sh.slot[r.slots][1] = all;
   tc::cluster_sync();
   before += r.remote_sum(&sh.slot[r.slots][1], r.rank);
   const u64 total = r.remote_sum(&sh.slot[r.slots][1], r.ranks);
@@ -852,7 +886,8 @@ using namespace soma;
 extern "C" int soma_sample(const void* logits, int64_t stride, int dtype, int64_t rows,
                            int64_t vocab, soma_sample_config cfg, const float* u, int64_t* tokens,
                            float* logprobs, void* stream) {
-  if (rows < 0 || rows > (1 << 24) || vocab < 1 || vocab > (1 << 20)) return SOMA_ERR_UNSUPPORTED;
+  if (rows < 0 || rows > (1 << 24) || vocab < 1 || vocab > kMostVocab)
+    return SOMA_ERR_UNSUPPORTED;
   if (dtype != SOMA_FP32 && dtype != SOMA_BF16 && dtype != SOMA_FP16) return SOMA_ERR_INVALID_ARG;
   if (stride < vocab || !aligned(logits, dtype == SOMA_FP32 ? 4 : 2) || !aligned(u, 4) ||
       !aligned(tokens, 8) || !aligned(logprobs, 4) || !aligned(cfg.temperatures, 4) ||
