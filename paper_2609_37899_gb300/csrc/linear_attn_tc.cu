@@ -714,8 +714,8 @@ chunk_kernel(const __grid_constant__ Sources sources, const __grid_constant__ Ca
       if (SOMA_CHECK(at + 1 < call.batch * call.heads * call.problems * cut.segments, status))
         to = cut.starts + (at + 1) * call.state;
       if (warp == L::group && lane == 0) {
-        const int steps = count > 0 ? min(len, last * kChunk) - first * kChunk : 0;
-        const Fade f = fade_of(g, (float)steps);
+        const int64_t end = min((int64_t)len, (int64_t)last * kChunk);  // up to 2^31
+        const Fade f = fade_of(g, count > 0 ? (float)(end - (int64_t)first * kChunk) : 0.f);
         cut.fades[at] = whole ? make_float2(f.keep, f.change) : make_float2(0.f, 0.f);
       }
     } else if (final_one && p.s_out) {
