@@ -24,6 +24,7 @@
 //
 // Long sequences of few heads are cut into segments: one launch for the state
 // that each segment adds, one that joins them, one for the outputs.
+#include <atomic>
 #include <cmath>
 
 #define SOMA_CHECK_FILE 15
@@ -960,25 +961,31 @@ bool make_source(Source* s, const void* base, const soma_attn_strides& st, int64
   return false;
 }
 
-// The registers that a kernel's threads are launched with: its warps share those
-// among them (setmaxnreg), and would wait for ever for more.
+// Whether a kernel's threads are launched with so many registers: its warps share
+// those among them (setmaxnreg), and would wait for ever for more.  Another number
+// than the launch bounds give here is an error of the build, which is said, not
+// served by the kernels without tensor cores.  A failed query is not remembered.
 template <auto KERNEL>
-bool launched_with(int registers) {
-  static const int has = [] {
+cudaError_t launched_with(int registers) {
+  static std::atomic<int> known{0};
+  int has = known.load(std::memory_order_relaxed);
+  if (has == 0) {
     cudaFuncAttributes a;
-    return cudaFuncGetAttributes(&a, KERNEL) == cudaSuccess ? a.numRegs : 0;
-  }();
-  return has == registers;
+    const cudaError_t e = cudaFuncGetAttributes(&a, KERNEL);
+    if (e != cudaSuccess) return e;
+    has = a.numRegs;
+    known.store(has, std::memory_order_relaxed);
+  }
+  return has == registers ? cudaSuccess : cudaErrorInvalidConfiguration;
 }
 
 template <typename T, int W>
 cudaError_t launch(const Sources& sources, const Call& call, Cut cut, cudaStream_t st) {
   constexpr size_t smem = Layout<W>::bytes + sizeof(Shared);
   static_assert(smem <= 227 * 1024, "shared memory of a CTA");
-  if (!launched_with<chunk_kernel<T, W, true>>(Layout<W>::launched) ||
-      !launched_with<chunk_kernel<T, W, false>>(Layout<W>::launched))
-    return cudaErrorInvalidConfiguration;
-  cudaError_t e = allow_shared<chunk_kernel<T, W, true>>(smem);
+  cudaError_t e = launched_with<chunk_kernel<T, W, true>>(Layout<W>::launched);
+  if (e == cudaSuccess) e = launched_with<chunk_kernel<T, W, false>>(Layout<W>::launched);
+  if (e == cudaSuccess) e = allow_shared<chunk_kernel<T, W, true>>(smem);
   if (e == cudaSuccess) e = allow_shared<chunk_kernel<T, W, false>>(smem);
   if (e != cudaSuccess) return e;
   const int64_t rows = call.batch * call.heads * call.problems;
