@@ -306,7 +306,7 @@ int soma_debug_scan_timeout(const float* src, float* out, uint32_t max_polls, vo
 /* soma_debug_attn_timeout: the same for the copies of linear attention's
  *   tensor-core kernels.  Tiles x, y (its first place twice) and z are copied
  *   from src (device fp32 [5][256], 16-byte aligned), then a place is waited for
- *   that nothing hands back.  The kernel records SOMA_ERR_TIMEOUT, refuses a
+ *   that nothing hands back.  The kernel records SOMA_ERR_TIMEOUT, makes no
  *   further copy, waits for those it made and writes what arrived to
  *   out[0 .. 1023] (src's rows 0, 4, 2 and 3) and the copies of x, y and z (1, 3
  *   and 1) to out[1024 .. 1026]. */

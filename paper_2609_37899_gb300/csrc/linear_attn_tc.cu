@@ -97,17 +97,13 @@ __device__ __forceinline__ bool wait(uint64_t* bar, uint32_t parity, Shared* sh,
   return false;
 }
 
-// The tiles that a CTA has asked for; those of y go to its two places in turn.
+// The tiles that a CTA has asked for; those of y go to its two places in turn.  A
+// place is handed back only by who has seen its copy land, also after an abort (the
+// products' issuers break off then, and the states' warps keep z), so what has been
+// handed back may be copied into, and one copy at most is under way in each place.
 struct Copies {
   uint32_t x, y, z;
 };
-
-// Whether the loading warp (all of it) may copy into a place that it has waited
-// for.  After an abort the others go on without waiting and hand places back
-// whose copies may still be on their way, with their barriers not free.
-__device__ __forceinline__ bool may_copy(const Shared& sh) {
-  return !__any_sync(0xffffffffu, sh.abort);
-}
 
 // The loading warp's last act: the last copy into each place has landed before the
 // CTA leaves its shared memory to another.  In a whole run the products have waited
@@ -608,6 +604,7 @@ chunk_kernel(const __grid_constant__ Sources sources, const __grid_constant__ Ca
 
     uint32_t flags = flags_of(0);
     bool whole = true;  // no document started in this segment
+    bool landed = true;  // every z so far has been seen
     const Fade full = fade_of(g, (float)kChunk);
     for (int k = 0; k < count; ++k) {
       if (k + 1 == count && !state_wanted) break;
@@ -628,7 +625,7 @@ chunk_kernel(const __grid_constant__ Sources sources, const __grid_constant__ Ca
       // been waited for: their places are free.
       const float w = counts ? p.f * sh.power[reversed ? row + 1 : n - 1 - row] : 0.f;
       float z_scale = 1.f;
-      wait(&sh.z_full, odd, &sh, status);
+      landed = wait(&sh.z_full, odd, &sh, status) && landed;
       const auto fetch = [&](int j) {
         const uint4 v = load_piece(z_row, j);
         return counts ? v : make_uint4(0u, 0u, 0u, 0u);  // whatever it is
@@ -678,7 +675,7 @@ chunk_kernel(const __grid_constant__ Sources sources, const __grid_constant__ Ca
       }
       tc::fence_async_smem();
       arrive(&sh.z_ready);
-      arrive(&sh.z_empty);
+      if (landed) arrive(&sh.z_empty);
 
       const Fade fade = n == kChunk ? full : fade_of(g, (float)n);
       const float back = reciprocal(z_scale);
@@ -753,22 +750,19 @@ chunk_kernel(const __grid_constant__ Sources sources, const __grid_constant__ Ca
       }
       __syncwarp();
     };
-    const auto free = [&](uint64_t* bar, uint32_t parity) {
-      return wait(bar, parity, &sh, status) && may_copy(sh);
-    };
     Copies copies = {};
     for (int k = 0; k < count; ++k) {
       const int t0 = start_of(k);
       const uint32_t s = k & 1, round = (k >> 1) & 1;
       if (OUT) {
-        if (!free(&sh.x_empty, (k & 1) ^ 1)) break;
+        if (!wait(&sh.x_empty, (k & 1) ^ 1, &sh, status)) break;
         load(L::x, sx, p.a, t0, &sh.x_full);
         ++copies.x;
       }
-      if (!free(&sh.y_empty[s], round ^ 1)) break;
+      if (!wait(&sh.y_empty[s], round ^ 1, &sh, status)) break;
       load(L::y + s * L::tile, sy, p.a, t0, &sh.y_full[s]);
       ++copies.y;
-      if (!free(&sh.z_empty, (k & 1) ^ 1)) break;
+      if (!wait(&sh.z_empty, (k & 1) ^ 1, &sh, status)) break;
       load(L::z, sz, p.c, t0, &sh.z_full);
       ++copies.z;
     }
@@ -865,9 +859,9 @@ chunk_kernel(const __grid_constant__ Sources sources, const __grid_constant__ Ca
 }
 
 // A wait of the loader's that runs out, with copies under way: x, both places of y
-// and z are filled from src, y's first place is waited for, handed back and filled
-// again, z's is never handed back.  out: the four tiles as they are when the CTA
-// would leave, then the copies made of each (one more is refused).
+// and z are filled from src, y's first place is waited for and filled again, z's is
+// never handed back.  out: the four tiles as they are when the CTA would leave, then
+// the copies made of each.
 constexpr int kTimeoutTest = 256;  // floats of a tile
 __global__ void __launch_bounds__(32)
 copies_timeout_kernel(const float* src, float* out, uint32_t max_polls, int* status) {
@@ -885,7 +879,6 @@ copies_timeout_kernel(const float* src, float* out, uint32_t max_polls, int* sta
   __syncwarp();
   Copies copies = {};
   const auto copy = [&](int tile, int from, uint64_t* bar, uint32_t& count) {
-    if (!may_copy(sh)) return;
     ++count;
     if (threadIdx.x == 0) {
       tc::mbar_arrive_expect_tx(bar, sizeof(tiles[0]));
@@ -898,8 +891,7 @@ copies_timeout_kernel(const float* src, float* out, uint32_t max_polls, int* sta
   copy(2, 2, &sh.y_full[1], copies.y);
   copy(3, 3, &sh.z_full, copies.z);
   if (wait(&sh.y_full[0], 0, &sh, status)) copy(1, 4, &sh.y_full[0], copies.y);
-  wait(&sh.z_empty, 0, &sh, status, max_polls);
-  copy(3, 0, &sh.z_full, copies.z);
+  if (wait(&sh.z_empty, 0, &sh, status, max_polls)) copy(3, 0, &sh.z_full, copies.z);
   land(sh, copies);
   __syncwarp();
   for (int i = threadIdx.x; i < 4 * kTimeoutTest; i += 32) out[i] = tiles[i / kTimeoutTest][i % kTimeoutTest];
