@@ -664,8 +664,8 @@ int soma_linear_ce_backward(const void* h, const void* emb, soma_linear_ce_dims 
  * 128 steps starts from are rounded to the type for the products that they enter,
  * and the decayed v, for the state, to twice its bits; sums and states are fp32.
  * fp16: those three are scaled by powers of two to the range of the type.  Other
- * layouts, and fp32, take kernels of fp32 arithmetic, which are several times
- * slower; within 16 steps they scale k_j v_j^T, and the like of the gradients, by
+ * layouts, and fp32, take kernels of fp32 arithmetic, which are 10 to 20 times
+ * slower for long sequences; within 16 steps they scale k_j v_j^T, and the like of the gradients, by
  * up to 1808, so that those and the states are to stay below 1e35. */
 typedef struct soma_attn_dims {
   int64_t batch; /* 0 .. 2^31 - 1 */

@@ -3,9 +3,9 @@
 //
 // Eight elements of a row-major count share a Philox block, 16 bits each, so a
 // thread owns such a group: 60 instructions of generator for 8 elements.
-// 65536 x 1376 bf16: 85 us with a residual and 68 without, 6.4 and 5.3 TB/s (in fp32
-// 158 and 109 us, 6.8 and 6.6 TB/s): two streams of 16 bits do not quite hide the
-// generator.  Comparing halves where they are instead of making a mask, and packed
+// 65536 x 1376 bf16, after a flush of L2: 84 us with a residual and 68 without, 6.4 and
+// 5.3 TB/s (in fp32 158 and 109 us, 6.9 and 6.6 TB/s): two streams of 16 bits do not
+// quite hide the generator.  Comparing halves where they are instead of making a mask, and packed
 // conversions, were 2 to 6 us slower.
 #include <cmath>
 
@@ -74,8 +74,8 @@ dropout_groups_kernel(const T* x, const T* residual, T* y, const Dropout d, uint
 
 // Any strides: a warp owns 256 elements in a row-major count, each lane the mask
 // of one group.  Lane l reads elements l, 32 + l, ... and gets their groups'
-// masks from the lanes that made them.  3001 x 681 fp16: 11 us with a residual, bound
-// by 2-byte accesses; 60000 x 681 142 us, 1.7 TB/s.
+// masks from the lanes that made them.  One element per lane and access: 3001 x 681
+// fp16 14 us with a residual, 60000 x 681 143 us, 1.7 TB/s.
 template <typename T, bool RESIDUAL>
 __global__ void __launch_bounds__(kThreads)
 dropout_kernel(const T* x, const T* residual, T* y, const Dropout d) {

@@ -85,10 +85,12 @@ __device__ __forceinline__ void fold(float (&o)[kSums], bool upper, int partner)
 // decayed once per tile and the decays go into the factors of z and of the output: two
 // fp32 instructions per element of the state and step.  Strong decays, whose powers
 // would cost range, are applied at each step, a third instruction.
-// 16 x 2048 x 8 heads of 128 x 128 in fp32: 797 us forward, 2303 backward (floors of
-// their bytes 80 and 139).  Instruction issue bounds it (67% of the slots, half of
-// them multiply-adds), and shared memory is busy for 42% of the time: few warps fit
-// beside the state to cover latencies.  Packed pairs (fma.rn.f32x2) were no faster.
+// 16 x 2048 x 8 heads of 128 x 128 in fp32: 788 us forward, 2285 backward, in some
+// runs up to 909 and 2390 (floors of their bytes 80 and 139).  Instruction issue bounds
+// it (67% of the slots, half of them multiply-adds), and shared memory is busy for 42%
+// of the time: few warps fit beside the state to cover latencies.  Packed pairs
+// (fma.rn.f32x2) were no faster.  In bf16, for layouts that the tensor cores do not
+// take: 1378 and 3929; 64 x 64: 819 and 1657.
 template <typename T, int RUNS, bool OUT>
 __global__ void __launch_bounds__(most_threads(RUNS))
 plain_kernel(const __grid_constant__ Call call, const __grid_constant__ Cut cut, int loaders) {
@@ -330,7 +332,7 @@ plain_kernel(const __grid_constant__ Call call, const __grid_constant__ Cut cut,
     }
   };
   // Two tiles ahead of use; the copying code is there once, as cold instructions
-  // are much of a short call's time (4 x 777 x 7 heads of 33 x 65: 66 us, with the first
+  // are much of a short call's time (4 x 777 x 7 heads of 33 x 65: 69 us, with the first
   // two tiles' copies and each operand's written out 84).
   for (int64_t k0 = -2 * kTile; k0 < count; k0 += kTile) {
     if (loads) {
@@ -575,9 +577,9 @@ size_t shared_of(const Spread& s) {
 }
 // Threads that stage the next steps while the others work.  None in fp32 with few
 // threads, where all of them do it: the copies are asynchronous, and the registers
-// of four more warps would keep another CTA away (64 x 64: 290 us instead of 409 for
-// 16 x 2048 x 8; 33 x 65, backward, 4 x 777 x 7: 137 instead of 163).  With eight
-// warps at work it is the other way round (128 x 128: 916 and 763 us).
+// of four more warps would keep another CTA away (64 x 64: 302 us instead of 445 for
+// 16 x 2048 x 8; 33 x 65, backward, 4 x 777 x 7: 146 instead of 177).  With eight
+// warps at work it is the other way round (128 x 128: 1093 and 788 us).
 int loaders_of(const Spread& s, int dtype) {
   return dtype == SOMA_FP32 && s.groups * (s.cols / kCols) <= 160 ? 0 : kLoaders;
 }

@@ -15,12 +15,14 @@
 // do the rest side by side: D o P and out, and w Z and S, which stays in
 // registers in fp32.  P of the next chunk runs under out.
 //
-// bf16, 16 x 4096 x 8 heads of 128 x 128: 137 us forward, 439 backward (floors of
-// their bytes 80 and 139; three problems of four tensors each are read there).  The tensor
-// pipe is active for 29% of the cycles, issue slots 33%, shared memory's port about
-// 45%: products and the groups of warps wait for one another in turn, and 224 KB of
-// shared memory leave no room for a second X or Z that would take them apart.  A
-// chunk takes 4 us; its begin and end, with cold caches, 8 us per CTA.
+// bf16, 16 x 4096 x 8 heads of 128 x 128: 129 to 135 us forward and 385 backward after
+// a flush of L2 (floors of their bytes 80 and 139; three problems of four tensors each
+// are read there).  Of 16 x 2048 x 8's time the tensor pipe is active for 23% forward
+// and 22% backward, issue slots are busy for 33 and 30%, shared memory's data pipe for
+// 39 and 34%: products and the groups of warps wait for one another in turn, and with
+// chunks of 128 steps the 224 KB of shared memory have no room for a second X or Z
+// that would take them apart (shorter chunks were not tried).  A chunk takes 4 us; a
+// CTA's begin and end, with cold caches, 8 us.
 //
 // Long sequences of few heads are cut into segments: one launch for the state
 // that each segment adds, one that joins them, one for the outputs.

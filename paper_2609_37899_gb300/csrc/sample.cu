@@ -12,8 +12,9 @@
 // Weights are whole numbers, so sums do not depend on their order and every CTA
 // of a cluster comes to the same cut by itself.
 //
-// Few rows are bound by latency, a dozen meetings of the cluster: 1 x 131072 bf16,
-// top-k 50 and top-p 0.9: 19 us a call; 64 x 50021 with settings per row 33.  Many by
+// Few rows are bound by latency, one step after another, six meetings of the cluster
+// among them: 1 x 131072 bf16, top-k 50 and top-p 0.9: 19 us a call (25 after a flush
+// of L2); 64 x 50021 with settings per row 33 to 38.  Many by
 // instruction issue, some 300 per logit over two evaluations of its weight and four
 // scans: 256 x 131072 fp32, top-p alone, 413 us, 0.05 of the copy rate.
 #include <cmath>
