@@ -660,13 +660,17 @@ int soma_linear_ce_backward(const void* h, const void* emb, soma_linear_ce_dims 
  * 16-bit types run on the tensor cores where rows allow tiled copies: addresses
  * and strides that are multiples of 16 bytes, widths that are multiples of 8, and
  * strides that nest (each a multiple of the next smaller one, or widths that are
- * multiples of 16); the stride of a dimension of one element may be any.  There scale l^{i-j} <q_i, k_j> and the state that a chunk of
- * 128 steps starts from are rounded to the type for the products that they enter,
- * and the decayed v, for the state, to twice its bits; sums and states are fp32.
- * fp16: those three are scaled by powers of two to the range of the type.  Other
- * layouts, and fp32, take kernels of fp32 arithmetic, which are 10 to 20 times
- * slower for long sequences; within 16 steps they scale k_j v_j^T, and the like of the gradients, by
- * up to 1808, so that those and the states are to stay below 1e35. */
+ * multiples of 16); the stride of a dimension of one element may be any.  There
+ * scale l^{i-j} <q_i, k_j> and the state that a chunk of 128 steps starts from are
+ * rounded to the type for the products that they enter, and the decayed v, for the
+ * state, to twice its bits; sums and states are fp32.  So bf16 states are 2^-16 of
+ * their terms off (2.5e-6 of their norm; fp32 sums of the same inputs 3e-7, fp16
+ * 5e-7), and o and the gradients 2.3e-3 of theirs (fp16: 2.9e-4), of which their own
+ * rounding is 1.7e-3 (2.1e-4).  fp16: those three are scaled by powers of two to the
+ * range of the type.  Other layouts, and fp32, take kernels of fp32 arithmetic, which
+ * are 10 to 20 times slower for long sequences; within 16 steps they scale k_j v_j^T,
+ * and the like of the gradients, by up to 1808, so that those and the states are to
+ * stay below 1e35. */
 typedef struct soma_attn_dims {
   int64_t batch; /* 0 .. 2^31 - 1 */
   int64_t steps; /* 0 .. 2^31 - 1 */
